@@ -332,6 +332,136 @@ amk_status amk_plan_check(const amk_config* cfg, const uint64_t* tables, size_t 
 amk_status amk_argmax_static(const float* x, int64_t n, int32_t* token, char* msg, size_t msg_bytes,
                              void* cuda_stream);
 
+/*
+ * Operators around the decode step: what a serving program calls between a prompt and the next step.  None of
+ * them needs a handle; all are asynchronous on cuda_stream, allocate nothing, keep nothing between calls, may be
+ * captured into a graph, and run on the CURRENT device, whose memory every DEVICE pointer must be.  `msg` (HOST
+ * out, msg_bytes bytes, may be NULL) receives the reason in words when the status is not AMK_OK.  Two calls may
+ * run at the same time if they share no output and no workspace.
+ *
+ * A value that a mask hides is never used: NaN or infinity in a K or V row reaches only the queries that attend to
+ * that row.  A query that attends to nothing gets zeros and a log-sum-exp of -infinity.
+ */
+
+/*
+ * Causal attention over whole prompts packed one behind the other (the paper's step attends for one new token,
+ * Section 4; this is the same attention -- scale, grouped heads, positions 0..i -- for every token of a prompt):
+ *   out[i][h] = sum_j p_j v[j][h / (n_q/n_kv)],  p = softmax_j(scale q[i][h] . k[j][h / (n_q/n_kv)]),
+ * over the tokens j <= i of token i's own prompt.  q and k carry their rotation already.
+ *   q, k, v       DEVICE bf16: row (token), head and element; rows and heads at the given strides (in elements),
+ *                 elements contiguous.  The three may be slices of one fused projection.
+ *   out           DEVICE bf16, rows and heads at the given strides; must not overlap the inputs
+ *   lse           DEVICE float [total][n_q_heads], natural logarithm of each row's sum of exponentials, or NULL
+ *   cu_seqlens    DEVICE int32 [n_seqs + 1]: prompt s is rows [cu[s], cu[s+1]); lengths of zero are allowed.  Rows of no
+ *                 prompt (before cu[0], from cu[n_seqs] on) are left as they were.  A prompt whose bounds are
+ *                 not 0 <= cu[s] <= cu[s+1] <= total is skipped.
+ * Pointers 16-byte aligned, strides multiples of 8 elements.  Arithmetic: scores and sums fp32, the softmax numerators
+ * enter the second product as bf16 (relative error 2^-8 at most, each on its own), one rounding to bf16 at the end.
+ * Errors: INVALID_ARG (struct size, NULL, alignment, strides, sizes), UNSUPPORTED (head_dim, head counts as
+ * amk_config's), CUDA.
+ */
+typedef struct amk_prompt_args {
+  uint32_t struct_size;      /* = sizeof(amk_prompt_args)                                              */
+  uint32_t head_dim;         /* 64 or 128                                                              */
+  uint32_t n_q_heads;        /* multiple of n_kv_heads; n_q_heads / n_kv_heads <= 16                   */
+  uint32_t n_kv_heads;
+  uint32_t n_seqs;
+  float scale;               /* > 0, or 0: 1 / sqrt(head_dim)                                          */
+  int64_t total;             /* rows of q, k, v and out; below 2^31                                    */
+  const void* q;
+  const void* k;
+  const void* v;
+  void* out;
+  float* lse;
+  const int32_t* cu_seqlens;
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head, out_row, out_head; /* strides, elements         */
+} amk_prompt_args;
+amk_status amk_prompt_attention(const amk_prompt_args* args, char* msg, size_t msg_bytes, void* cuda_stream);
+
+/*
+ * Attention of drafted tokens over a KV cache (one layer): each of n_seqs sequences has n_rows drafted tokens whose K/V
+ * rows lie behind its context, in slots [len, len + n_rows).  Token i attends to every slot [0, len) and to the slots
+ * len + j whose bit j is set in its row of the mask (a tree: its ancestors and itself).  n_rows = 1 without a mask
+ * is the attention of the decode step.
+ *   q, out        DEVICE bf16 [n_seqs][n_rows][n_q_heads][head_dim] at the given strides (elements)
+ *   k, v          DEVICE, kv_dtype (amk_kvdtype): one layer of the cache, [n_seqs][n_kv_heads][n_slots][head_dim] at
+ *                 the given strides (elements of that type); only rows [0, len + n_rows) are read for their values
+ *   cache_len     DEVICE int32 [n_seqs]: len.  Read on the device, so a captured call follows it.  A sequence whose
+ *                 len is not 0 <= len <= n_slots - n_rows gets NaN in out and lse, and nothing out of range is read.
+ *   mask          DEVICE uint64 [n_seqs][n_rows][ceil(n_rows / 64)], bit j % 64 of word j / 64; or NULL: a chain, token i
+ *                 attends to the drafted tokens j <= i
+ *   lse           DEVICE float [n_seqs][n_rows][n_q_heads] or NULL
+ *   max_len       upper bound of the lengths in cache_len, for the division of the work alone (results do not depend on
+ *                 whether it holds); 0: n_slots - n_rows
+ *   workspace     DEVICE, 256-byte aligned, at least amk_tree_workspace_bytes of the same arguments; scratch,
+ *                 needs no initial value; two calls that may overlap need one each
+ * Pointers 16-byte aligned, strides multiples of 16 bytes.  The 8-bit cache is widened to bf16 exactly.
+ * Errors as amk_prompt_attention.
+ */
+typedef struct amk_tree_args {
+  uint32_t struct_size;      /* = sizeof(amk_tree_args)                                                */
+  uint32_t head_dim;         /* 64 or 128                                                              */
+  uint32_t n_q_heads;        /* multiple of n_kv_heads; n_q_heads / n_kv_heads <= 16                   */
+  uint32_t n_kv_heads;
+  uint32_t kv_dtype;         /* amk_kvdtype                                                            */
+  uint32_t n_seqs;
+  uint32_t n_rows;           /* drafted tokens per sequence, 1 .. AMK_TREE_MAX_ROWS                    */
+  uint32_t n_slots;          /* rows of the cache                                                      */
+  uint32_t max_len;
+  float scale;               /* > 0, or 0: 1 / sqrt(head_dim)                                          */
+  const void* q;
+  const void* k;
+  const void* v;
+  void* out;
+  float* lse;
+  const int32_t* cache_len;
+  const uint64_t* mask;
+  void* workspace;
+  uint64_t workspace_bytes;
+  int64_t q_seq, q_row, q_head, k_seq, k_head, k_row, v_seq, v_head, v_row, out_seq, out_row, out_head;
+} amk_tree_args;
+#define AMK_TREE_MAX_ROWS 1024
+amk_status amk_tree_workspace_bytes(const amk_tree_args* args, size_t* bytes, char* msg, size_t msg_bytes);
+amk_status amk_tree_attention(const amk_tree_args* args, char* msg, size_t msg_bytes, void* cuda_stream);
+
+/*
+ * Log probabilities of given tokens, in one pass over the logits: with m = max x, s = sum e^(x-m),
+ *   logprob[r] = x[token[r]] - m - log s,   entropy[r] = log s - sum e^(x-m) (x-m) / s  (natural logarithms),
+ * and the top_k largest logits of the row, largest first, the lowest index first among equal ones.
+ *   logits        DEVICE float (dtype 0) or bf16 (dtype 1) [rows][vocab], rows at row_stride elements; any alignment
+ *                 of the element type
+ *   tokens        DEVICE int32 [rows]; a token outside [0, vocab) gives NaN
+ *   logprob, entropy   DEVICE float [rows], either may be NULL
+ *   top_tokens / top_logprobs   DEVICE int32 / float [rows][top_k], NULL when top_k = 0
+ * A logit of -infinity has probability zero (logprob -infinity, no share of the entropy).  NaN among the logits, a
+ * maximum of +infinity or a row of nothing but -infinity makes the row's logprob, entropy and top_logprobs NaN; NaN
+ * elements are never alternatives; places without an alternative hold token -1 and NaN.
+ * Errors: INVALID_ARG (NULL, alignment, sizes), UNSUPPORTED (top_k > AMK_LOGPROBS_MAX_TOP, dtype), CUDA.
+ */
+#define AMK_LOGPROBS_MAX_TOP 32
+amk_status amk_token_logprobs(const void* logits, uint32_t dtype, int64_t rows, int64_t vocab, int64_t row_stride,
+                              const int32_t* tokens, uint32_t top_k, float* logprob, float* entropy,
+                              int32_t* top_tokens, float* top_logprobs, char* msg, size_t msg_bytes,
+                              void* cuda_stream);
+
+/*
+ * Moves kept rows of KV caches together, in place: for every cache c and every plane p (K and V of each layer and
+ * head: 2 * L * n_kv_heads planes of max_seq rows),
+ *   row base[c] + i  <-  old row keep[c][i],  i < count[c],
+ * as if all were read before any is written.  After a draft is verified: keep = the accepted tokens' slots, base =
+ * the context's length.  To drop the middle of a long context: keep = the slots to retain, base = where they go.
+ *   kv            DEVICE: n_caches caches of n_planes * max_seq * row_bytes contiguous bytes, cache_stride bytes apart
+ *                 (a decoder's cache: n_planes = 2 * L * n_kv_heads, row_bytes = head_dim * element size)
+ *   base, count   DEVICE int32 [n_caches];  keep  DEVICE int32 [n_caches][max_keep]
+ * A cache is left as it was unless 0 <= count <= max_keep, base >= 0, keep is strictly ascending over its first
+ * `count` entries, keep[0] >= base and keep[count - 1] < max_seq.  All other rows keep their content.
+ * kv 16-byte aligned; row_bytes and cache_stride multiples of 16, row_bytes at most 1024.
+ * Errors: INVALID_ARG (NULL, alignment, sizes), CUDA.
+ */
+amk_status amk_kv_compact(void* kv, int64_t n_caches, int64_t cache_stride, int64_t n_planes, int64_t max_seq,
+                          int64_t row_bytes, const int32_t* base, const int32_t* keep, int64_t max_keep,
+                          const int32_t* count, char* msg, size_t msg_bytes, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -8,6 +8,8 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
+import threading
 from typing import Dict, List, Optional, Sequence
 
 import torch
@@ -56,6 +58,27 @@ class amk_plan(C.Structure):
         (n, C.c_uint64) for n in ("packed_bytes", "workspace_bytes", "kv_bytes", "weight_stream_bytes")]
 
 
+class amk_prompt_args(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("struct_size", "head_dim", "n_q_heads", "n_kv_heads", "n_seqs")] + [
+        ("scale", C.c_float), ("total", C.c_int64)] + [
+        (n, C.c_void_p) for n in ("q", "k", "v", "out", "lse", "cu_seqlens")] + [
+        (n, C.c_int64) for n in ("q_row", "q_head", "k_row", "k_head", "v_row", "v_head", "out_row", "out_head")]
+
+
+class amk_tree_args(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("struct_size", "head_dim", "n_q_heads", "n_kv_heads", "kv_dtype", "n_seqs",
+                                          "n_rows", "n_slots", "max_len")] + [("scale", C.c_float)] + [
+        (n, C.c_void_p) for n in ("q", "k", "v", "out", "lse", "cache_len", "mask", "workspace")] + [
+        ("workspace_bytes", C.c_uint64)] + [
+        (n, C.c_int64) for n in ("q_seq", "q_row", "q_head", "k_seq", "k_head", "k_row", "v_seq", "v_head", "v_row",
+                                 "out_seq", "out_row", "out_head")]
+
+
+# the same two structs as struct formats: packing one costs a microsecond, filling a ctypes structure several
+_PROMPT = struct.Struct("@5Ifq6P8q")
+_TREE = struct.Struct("@9If8PQ12q")
+
+
 def _load() -> C.CDLL:
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is missing: build it with `python -m paper_2606_09682_b200.build` "
@@ -84,6 +107,12 @@ def _load() -> C.CDLL:
         "amk_quantize_int8_grouped": (C.c_int, [vp, i64, i64, vp, vp, vp]),
         "amk_quantize_int4": (C.c_int, [vp, i64, i64, vp, vp, vp, vp]),
         "amk_argmax_static": (C.c_int, [vp, i64, vp, C.c_char_p, sz, vp]),
+        "amk_prompt_attention": (C.c_int, [C.c_char_p, C.c_char_p, sz, vp]),
+        "amk_tree_workspace_bytes": (C.c_int, [C.c_char_p, C.POINTER(sz), C.c_char_p, sz]),
+        "amk_tree_attention": (C.c_int, [C.c_char_p, C.c_char_p, sz, vp]),
+        "amk_token_logprobs": (C.c_int, [vp, C.c_uint32, i64, i64, i64, vp, C.c_uint32, vp, vp, vp, vp, C.c_char_p, sz,
+                                         vp]),
+        "amk_kv_compact": (C.c_int, [vp, i64, i64, i64, i64, i64, vp, vp, i64, vp, C.c_char_p, sz, vp]),
         "amk_plan_export": (C.c_int, [C.POINTER(amk_config), vp, sz, C.POINTER(sz)]),
         "amk_plan_check": (C.c_int, [C.POINTER(amk_config), vp, sz, C.c_char_p, sz]),
     }
@@ -97,7 +126,17 @@ lib = _load()
 EXPORTS = ("amk_status_str", "amk_packed_bytes", "amk_workspace_bytes", "amk_kv_bytes", "amk_create",
            "amk_decode_step", "amk_decode_greedy", "amk_last_status", "amk_plan_info", "amk_debug_hidden",
            "amk_debug_trace", "amk_debug_unpack", "amk_debug_drop_signal", "amk_debug_set_step_count", "amk_last_kernel_ns", "amk_destroy", "amk_quantize_int8", "amk_quantize_int8_grouped", "amk_quantize_int4",
-           "amk_argmax_static", "amk_plan_export", "amk_plan_check")
+           "amk_argmax_static", "amk_plan_export", "amk_plan_check",
+           "amk_prompt_attention", "amk_tree_workspace_bytes", "amk_tree_attention", "amk_token_logprobs",
+           "amk_kv_compact")
+
+
+class _Nothing:
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        return False
 
 
 class AmkError(RuntimeError):
@@ -223,6 +262,171 @@ def amk_argmax_static(x: torch.Tensor, token: torch.Tensor, n: int = -1) -> None
         raise AmkError(code, msg.value.decode() or "amk_argmax_static")
 
 
+AMK_TREE_MAX_ROWS = 1024
+AMK_LOGPROBS_MAX_TOP = 32
+_local = threading.local()
+
+
+def _need(ok: bool, what: str) -> None:
+    if not ok:
+        raise AmkError(AMK_ERR_INVALID_ARG, what)
+
+
+def _same_device(name: str, first: torch.Tensor, *others) -> None:
+    dev = first.device
+    _need(dev.type == "cuda", f"{name}: tensors must be cuda tensors")
+    for t in others:
+        _need(t is None or t.device == dev, f"{name}: tensors on different devices")
+
+
+def _run(fn, name: str, device: torch.device, *args) -> None:
+    """Calls a library entry point that ends in (msg, msg_bytes, stream) on the tensors' device and its current stream."""
+    msg = getattr(_local, "msg", None)
+    if msg is None:
+        msg = _local.msg = C.create_string_buffer(256)
+    if device.index == torch.cuda.current_device():
+        code = fn(*args, msg, 256, torch.cuda.current_stream().cuda_stream)
+    else:
+        with torch.cuda.device(device):
+            code = fn(*args, msg, 256, torch.cuda.current_stream().cuda_stream)
+    if code != AMK_OK:
+        raise AmkError(code, msg.value.decode() or name)
+
+
+def amk_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqlens: torch.Tensor,
+                         scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                         lse: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Causal attention over packed prompts: q [total][n_q][hd], k, v [total][n_kv][hd] bf16 (any row and head strides),
+    cu_seqlens int32 [n_seqs + 1], all cuda.  Returns out [total][n_q][hd] bf16; ``lse`` (fp32 [total][n_q],
+    contiguous) is filled if given.  Rows that belong to no prompt are left as they were (undefined if ``out`` is not
+    given)."""
+    name = "amk_prompt_attention"
+    _need(q.dim() == 3 and k.dim() == 3 and v.dim() == 3, f"{name}: q, k and v are [total][heads][head_dim]")
+    total, nq, hd = q.shape
+    nkv = k.shape[1]
+    _same_device(name, q, k, v, cu_seqlens, out, lse)
+    _need(q.dtype == k.dtype == v.dtype == torch.bfloat16, f"{name}: q, k and v are bf16")
+    _need(k.shape == v.shape and k.shape[0] == total and k.shape[2] == hd, f"{name}: shapes of q, k and v do not fit")
+    _need(cu_seqlens.dtype == torch.int32 and cu_seqlens.dim() == 1 and cu_seqlens.is_contiguous() and
+          cu_seqlens.numel() >= 1, f"{name}: cu_seqlens is a contiguous int32 vector of n_seqs + 1 entries")
+    if out is None:
+        out = torch.empty((total, nq, hd), dtype=torch.bfloat16, device=q.device)
+    else:
+        _need(out.shape == q.shape and out.dtype == torch.bfloat16, f"{name}: out is bf16 of q's shape")
+    if lse is not None:
+        _need(lse.shape == (total, nq) and lse.dtype == torch.float32 and lse.is_contiguous(),
+              f"{name}: lse is contiguous fp32 [total][n_q]")
+    (qr, qh, q1), (kr, kh, k1), (vr, vh, v1), (orow, oh, o1) = q.stride(), k.stride(), v.stride(), out.stride()
+    _need(q1 == 1 and k1 == 1 and v1 == 1 and o1 == 1, f"{name}: the last dimension must be contiguous")
+    args = _PROMPT.pack(_PROMPT.size, hd, nq, nkv, cu_seqlens.numel() - 1, scale or 0.0, total, q.data_ptr(),
+                        k.data_ptr(), v.data_ptr(), out.data_ptr(), 0 if lse is None else lse.data_ptr(),
+                        cu_seqlens.data_ptr(), qr, qh, kr, kh, vr, vh, orow, oh)
+    _run(lib.amk_prompt_attention, name, q.device, args)
+    return out
+
+
+def amk_tree_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cache_len: torch.Tensor,
+                       mask: Optional[torch.Tensor] = None, max_len: Optional[int] = None,
+                       scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                       lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of drafted tokens over one layer of a KV cache: q [n_seqs][rows][n_q][hd] bf16, k, v
+    [n_seqs][n_kv][slots][hd] (bf16, or e4m3 as uint8 / float8_e4m3fn), cache_len int32 [n_seqs]; the drafted tokens'
+    own rows lie in slots [cache_len, cache_len + rows).  ``mask``: int64 [n_seqs][rows][ceil(rows / 64)], bit j of a row
+    set where it attends to drafted token j; None: a chain.  ``max_len``: an upper bound of cache_len, a hint for
+    the division of the work.  ``workspace``: uint8 scratch of ``amk_tree_workspace_bytes``, taken from torch's
+    allocator if not given.  Returns out, of q's shape; ``lse`` (fp32 [n_seqs][rows][n_q]) is filled if given."""
+    name = "amk_tree_attention"
+    _need(q.dim() == 4 and k.dim() == 4 and v.dim() == 4, f"{name}: q, k and v have four dimensions")
+    seqs, rows, nq, hd = q.shape
+    _, nkv, slots, _ = k.shape
+    _same_device(name, q, k, v, cache_len, mask, out, lse, workspace)
+    _need(q.dtype == torch.bfloat16, f"{name}: q is bf16")
+    _need(k.dtype == v.dtype and k.dtype in (torch.bfloat16, torch.uint8, torch.float8_e4m3fn),
+          f"{name}: the cache is bf16, or e4m3 as uint8 or float8_e4m3fn")
+    _need(k.shape == v.shape and k.shape[0] == seqs and k.shape[3] == hd, f"{name}: shapes of q, k and v do not fit")
+    _need(cache_len.dtype == torch.int32 and cache_len.shape == (seqs,) and cache_len.is_contiguous(),
+          f"{name}: cache_len is a contiguous int32 vector with an entry for each sequence")
+    if mask is not None:
+        _need(mask.dtype == torch.int64 and mask.shape == (seqs, rows, (rows + 63) // 64) and mask.is_contiguous(),
+              f"{name}: mask is contiguous int64 [n_seqs][rows][ceil(rows / 64)]")
+    if out is None:
+        out = torch.empty((seqs, rows, nq, hd), dtype=torch.bfloat16, device=q.device)
+    else:
+        _need(out.shape == q.shape and out.dtype == torch.bfloat16, f"{name}: out is bf16 of q's shape")
+    if lse is not None:
+        _need(lse.shape == (seqs, rows, nq) and lse.dtype == torch.float32 and lse.is_contiguous(),
+              f"{name}: lse is contiguous fp32 [n_seqs][rows][n_q]")
+    _need(max_len is None or 0 <= max_len <= slots, f"{name}: max_len between 0 and the slots of the cache")
+    (qs, qr, qh, q1), (ks, kh, kr, k1), (vs, vh, vr, v1) = q.stride(), k.stride(), v.stride()
+    os_, orow, oh, o1 = out.stride()
+    _need(q1 == 1 and k1 == 1 and v1 == 1 and o1 == 1, f"{name}: the last dimension must be contiguous")
+    head = (_TREE.size, hd, nq, nkv, AMK_KV_BF16 if k.dtype == torch.bfloat16 else AMK_KV_FP8_E4M3, seqs, rows, slots,
+            max_len or 0, scale or 0.0, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
+            0 if lse is None else lse.data_ptr(), cache_len.data_ptr(), 0 if mask is None else mask.data_ptr())
+    tail = (qs, qr, qh, ks, kh, kr, vs, vh, vr, os_, orow, oh)
+    if workspace is None:
+        n = amk_tree_workspace_bytes(_TREE.pack(*head, 0, 0, *tail), q.device)
+        workspace = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
+    ws = (0, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    _run(lib.amk_tree_attention, name, q.device, _TREE.pack(*head, *ws, *tail))
+    return out
+
+
+def amk_tree_workspace_bytes(args, device=None) -> int:
+    """Scratch bytes of a tree call; ``args``: an amk_tree_args (or its bytes).  Depends on the device's SM count."""
+    n = C.c_size_t()
+    msg = C.create_string_buffer(256)
+    with torch.cuda.device(device) if device is not None else _Nothing():
+        code = lib.amk_tree_workspace_bytes(bytes(args), C.byref(n), msg, 256)
+    if code != AMK_OK:
+        raise AmkError(code, msg.value.decode() or "amk_tree_workspace_bytes")
+    return n.value
+
+
+def amk_token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, top_k: int = 0):
+    """logits [rows][vocab] (fp32 or bf16, cuda, rows at any stride), tokens int32 [rows] -> (logprob [rows], entropy
+    [rows], top tokens int32 [rows][top_k], their log probabilities [rows][top_k]); log probabilities fp32, natural."""
+    name = "amk_token_logprobs"
+    _need(logits.dim() == 2, f"{name}: logits are [rows][vocab]")
+    rows, vocab = logits.shape
+    _same_device(name, logits, tokens)
+    _need(logits.dtype in (torch.float32, torch.bfloat16), f"{name}: logits are fp32 or bf16")
+    _need(tokens.dtype == torch.int32 and tokens.shape == (rows,) and tokens.is_contiguous(),
+          f"{name}: tokens is a contiguous int32 vector with an entry for each row")
+    stride, one = logits.stride()
+    _need(one == 1 or vocab <= 1, f"{name}: the last dimension must be contiguous")
+    _need(top_k >= 0, f"{name}: top_k is negative")
+    dev = logits.device
+    both = torch.empty((2, rows), dtype=torch.float32, device=dev)
+    top_tokens = torch.empty((rows, top_k), dtype=torch.int32, device=dev)
+    top_logprobs = torch.empty((rows, top_k), dtype=torch.float32, device=dev)
+    _run(lib.amk_token_logprobs, name, dev, logits.data_ptr(), int(logits.dtype == torch.bfloat16), rows, vocab, stride,
+         tokens.data_ptr(), top_k, both.data_ptr(), both.data_ptr() + 4 * rows, top_tokens.data_ptr(),
+         top_logprobs.data_ptr())
+    return both[0], both[1], top_tokens, top_logprobs
+
+
+def amk_kv_compact(kv: torch.Tensor, base: torch.Tensor, keep: torch.Tensor, count: torch.Tensor) -> None:
+    """In place: in every plane of every cache, row base[c] + i becomes what row keep[c][i] was, i < count[c].
+    kv [n_caches][...][max_seq][hd] (cuda, each cache contiguous), base and count int32 [n_caches], keep int32
+    [n_caches][max_keep], strictly ascending from at least base[c] over its first count[c] entries (a cache whose list is
+    not stays as it was)."""
+    name = "amk_kv_compact"
+    _need(kv.dim() >= 3, f"{name}: kv is [n_caches][...][max_seq][head_dim]")
+    _same_device(name, kv, base, keep, count)
+    caches, slots, row = kv.shape[0], kv.shape[-2], kv.shape[-1] * kv.element_size()
+    _need(base.dtype == keep.dtype == count.dtype == torch.int32, f"{name}: base, keep and count are int32")
+    _need(base.shape == (caches,) and count.shape == (caches,) and keep.dim() == 2 and keep.shape[0] == caches and
+          base.is_contiguous() and keep.is_contiguous() and count.is_contiguous(),
+          f"{name}: base [n_caches], keep [n_caches][max_keep] and count [n_caches] must be contiguous")
+    if caches == 0 or kv.numel() == 0:
+        return
+    _need(kv[0].is_contiguous(), f"{name}: each cache must be contiguous")
+    planes = kv.numel() // caches // slots // kv.shape[-1]
+    _run(lib.amk_kv_compact, name, kv.device, kv.data_ptr(), caches, kv.stride(0) * kv.element_size(), planes, slots, row,
+         base.data_ptr(), keep.data_ptr(), keep.shape[1], count.data_ptr())
+
+
 def quantize_weights(weights: Dict, wdtype: str) -> Dict:
     """Run the library's quantiser over the seven per-layer linears of a bf16 weight dict (cuda tensors)."""
     if wdtype == "bf16":
@@ -337,6 +541,17 @@ class Decoder:
         buf = self._alloc(n)
         buf.zero_()
         return buf if fp8 else buf.view(torch.bfloat16)
+
+    def cache_views(self, kv: torch.Tensor):
+        """(K, V) views [n_layers][n_kv_heads][max_seq][head_dim] of a cache made by ``new_cache``."""
+        s = self.shape
+        both = kv.view(2, s.n_layers, s.n_kv_heads, s.max_seq, s.head_dim)
+        return both[0], both[1]
+
+    def amk_kv_compact(self, kv: torch.Tensor, base: torch.Tensor, keep: torch.Tensor, count: torch.Tensor) -> None:
+        """amk_kv_compact over this decoder's cache: base and count int32 [1], keep int32 [1][max_keep]."""
+        s = self.shape
+        amk_kv_compact(kv.view(1, 2 * s.n_layers * s.n_kv_heads, s.max_seq, s.head_dim), base, keep, count)
 
     def plan(self) -> amk_plan:
         p = amk_plan()
