@@ -425,6 +425,13 @@ amk_status amk_tree_workspace_bytes(const amk_tree_args* args, size_t* bytes, ch
 amk_status amk_tree_attention(const amk_tree_args* args, char* msg, size_t msg_bytes, void* cuda_stream);
 
 /*
+ * The attention kernels bound every wait inside them (two seconds).  Synchronises the stream and reports in *st (HOST
+ * out) whether one ran out on the current device since this was last asked: AMK_OK, or AMK_ERR_TIMEOUT (the outputs
+ * of the calls since then are undefined; the next call is legal).
+ */
+amk_status amk_operator_status(amk_status* st, char* msg, size_t msg_bytes, void* cuda_stream);
+
+/*
  * Log probabilities of given tokens, in one pass over the logits: with m = max x, s = sum e^(x-m),
  *   logprob[r] = x[token[r]] - m - log s,   entropy[r] = log s - sum e^(x-m) (x-m) / s  (natural logarithms),
  * and the top_k largest logits of the row, largest first, the lowest index first among equal ones.

@@ -110,6 +110,7 @@ def _load() -> C.CDLL:
         "amk_prompt_attention": (C.c_int, [C.c_char_p, C.c_char_p, sz, vp]),
         "amk_tree_workspace_bytes": (C.c_int, [C.c_char_p, C.POINTER(sz), C.c_char_p, sz]),
         "amk_tree_attention": (C.c_int, [C.c_char_p, C.c_char_p, sz, vp]),
+        "amk_operator_status": (C.c_int, [C.POINTER(C.c_int), C.c_char_p, sz, vp]),
         "amk_token_logprobs": (C.c_int, [vp, C.c_uint32, i64, i64, i64, vp, C.c_uint32, vp, vp, vp, vp, C.c_char_p, sz,
                                          vp]),
         "amk_kv_compact": (C.c_int, [vp, i64, i64, i64, i64, i64, vp, vp, i64, vp, C.c_char_p, sz, vp]),
@@ -127,7 +128,8 @@ EXPORTS = ("amk_status_str", "amk_packed_bytes", "amk_workspace_bytes", "amk_kv_
            "amk_decode_step", "amk_decode_greedy", "amk_last_status", "amk_plan_info", "amk_debug_hidden",
            "amk_debug_trace", "amk_debug_unpack", "amk_debug_drop_signal", "amk_debug_set_step_count", "amk_last_kernel_ns", "amk_destroy", "amk_quantize_int8", "amk_quantize_int8_grouped", "amk_quantize_int4",
            "amk_argmax_static", "amk_plan_export", "amk_plan_check",
-           "amk_prompt_attention", "amk_tree_workspace_bytes", "amk_tree_attention", "amk_token_logprobs",
+           "amk_prompt_attention", "amk_tree_workspace_bytes", "amk_tree_attention", "amk_operator_status",
+           "amk_token_logprobs",
            "amk_kv_compact")
 
 
@@ -381,6 +383,15 @@ def amk_tree_workspace_bytes(args, device=None) -> int:
     if code != AMK_OK:
         raise AmkError(code, msg.value.decode() or "amk_tree_workspace_bytes")
     return n.value
+
+
+def amk_operator_status(device=None) -> int:
+    """Synchronises; AMK_OK, or AMK_ERR_TIMEOUT if a bounded wait of an attention kernel ran out on the device since last
+    asked."""
+    st = C.c_int()
+    _run(lib.amk_operator_status, "amk_operator_status", torch.device("cuda", torch.cuda.current_device())
+         if device is None else torch.device(device), C.byref(st))
+    return st.value
 
 
 def amk_token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, top_k: int = 0):

@@ -11,7 +11,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libamk.so")
 SOURCES = ["amk_host.cu", "amk_kernel.cu", "amk_kernel_trace.cu", "amk_pack.cu", "amk_static.cu",
            "amk_attn.cu", "amk_logprobs.cu", "amk_compact.cu"]
-HEADERS = ["amk_layout.h", "amk_internal.h", "amk_ptx.cuh", "amk_kernel_impl.cuh", "amk_op_util.h", os.path.join(ROOT, "include", "amk.h")]
+HEADERS = ["amk_layout.h", "amk_internal.h", "amk_ptx.cuh", "amk_kernel_impl.cuh", "amk_op_util.h",
+           "amk_attn.cuh", "amk_tc.cuh", os.path.join(ROOT, "include", "amk.h")]
 
 
 def _stale() -> bool:

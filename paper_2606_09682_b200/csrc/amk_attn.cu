@@ -1,116 +1,120 @@
 // amk_prompt_attention and amk_tree_attention: argument checks and launches.
-#include <cuda_bf16.h>
-#include <cuda_fp8.h>
+#include <cuda.h>
 #include <cuda_runtime.h>
 #include <math.h>
-#include <math_constants.h>
 
+#include <atomic>
+
+#include "amk_attn.cuh"
 #include "amk_op_util.h"
-#include "amk_ptx.cuh"
 
 namespace {
 
 using amk::Reason;
 
-struct Params {
-  const unsigned char *q, *k, *v;
-  __nv_bfloat16* out;
-  float* lse;
-  const int* lens;                 // prompt: cu_seqlens; tree: cache_len
-  const unsigned long long* mask;
-  int64_t q_seq, q_row, q_head, k_seq, k_row, k_head, v_seq, v_row, v_head, o_seq, o_row, o_head;
-  int n_seqs, nq, rep, rows, slots;   // rows: prompt: all tokens; tree: drafted tokens of a sequence
-  float scale;
-};
+using amk::AttnParams;
 
-template <bool FP8>
-__device__ __forceinline__ float element(const unsigned char* p, int64_t i) {
-  if (FP8) {
-    __nv_fp8_e4m3 e;
-    e.__x = p[i];
-    return (float)e;
-  }
-  return __uint_as_float((unsigned)((const unsigned short*)p)[i] << 16);
+// cuTensorMapEncodeTiled of the driver that is loaded, or null
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiled encode_tiled() {
+  static const EncodeTiled fn = [] {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &q) != cudaSuccess ||
+        q != cudaDriverEntryPointSuccess) {
+      (void)cudaGetLastError();
+      f = nullptr;
+    }
+    return (EncodeTiled)f;
+  }();
+  return fn;
 }
 
-// One warp per (token, head): 32 keys at a time, one per lane.
+// A cache or a projection as {element, row, head, sequence}; boxes of 128 rows x 64 elements (bf16, swizzled for the
+// tensor cores) or whole 8-bit rows.  Strides in elements; an axis of one entry has a legal stride already.
+bool make_map(CUtensorMap* map, const void* base, bool fp8, int64_t hd, int64_t rows, int64_t heads, int64_t seqs,
+              int64_t row, int64_t head, int64_t seq) {
+  const EncodeTiled encode = encode_tiled();
+  if (!encode) return false;
+  const cuuint64_t esz = fp8 ? 1 : 2;
+  const cuuint64_t dims[4] = {(cuuint64_t)hd, (cuuint64_t)rows, (cuuint64_t)heads, (cuuint64_t)seqs};
+  const cuuint64_t strides[3] = {(cuuint64_t)row * esz, (cuuint64_t)head * esz, (cuuint64_t)seq * esz};
+  const cuuint32_t box[4] = {fp8 ? (cuuint32_t)hd : 64u, (cuuint32_t)amk::kTile, 1, 1}, steps[4] = {1, 1, 1, 1};
+  return encode(map, fp8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base),
+                dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                fp8 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// The shared-memory limit of a kernel, raised once on each device.
 template <int HD, bool TREE, bool FP8>
-__global__ void __launch_bounds__(128) attn_kernel(const Params p) {
-  __shared__ float qs[4][HD];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t w = (int64_t)blockIdx.x * 4 + warp;
-  const int h = (int)(w % p.nq), g = h / p.rep;
-  const int64_t row = w / p.nq;
-  int64_t n_keys, seq = 0, tok = row, first = 0, len = 0;
-  const unsigned long long* mask = nullptr;
-  bool bad = false;
-  if (TREE) {
-    if (row >= (int64_t)p.n_seqs * p.rows) return;
-    seq = row / p.rows, tok = row % p.rows;
-    len = p.lens[seq];
-    bad = len < 0 || len > p.slots - p.rows;
-    n_keys = bad ? 0 : len + p.rows;
-    if (p.mask) mask = p.mask + row * ((p.rows + 63) / 64);
-  } else {
-    if (row >= p.rows) return;
-    int lo = -1;
-    for (int s = 0; s < p.n_seqs; s++) {
-      const int a = p.lens[s], b = p.lens[s + 1];
-      if (a >= 0 && a <= row && row < b && b <= p.rows) lo = a;
-    }
-    if (lo < 0) return;
-    first = lo;
-    n_keys = row - lo + 1;
-  }
-  const unsigned char* q = p.q + (seq * p.q_seq + tok * p.q_row + h * p.q_head) * 2;
-  const int esz = FP8 ? 1 : 2;
-  const unsigned char* k = p.k + (seq * p.k_seq + first * p.k_row + g * p.k_head) * esz;
-  const unsigned char* v = p.v + (seq * p.v_seq + first * p.v_row + g * p.v_head) * esz;
-  for (int d = lane; d < HD; d += 32) qs[warp][d] = element<false>(q, d);
-  __syncwarp();
-  float m = -CUDART_INF_F, l = 0, o[HD / 32] = {};
-  for (int64_t j0 = 0; j0 < n_keys; j0 += 32) {
-    const int64_t j = j0 + lane;
-    bool ok = j < n_keys;
-    if (TREE && ok && j >= len) ok = mask ? (mask[(j - len) / 64] >> ((j - len) % 64)) & 1 : j - len <= tok;
-    float s = -CUDART_INF_F;
-    if (ok) {
-      s = 0;
-      for (int d = 0; d < HD; d++) s += qs[warp][d] * element<FP8>(k, j * p.k_row + d);
-      s *= p.scale;
-    }
-    float mx = s;
-    for (int x = 16; x; x >>= 1) mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, x));
-    mx = fmaxf(mx, m);
-    const float c = mx == -CUDART_INF_F ? 1.f : expf(m - mx);
-    const float e = ok ? expf(s - mx) : 0.f;
-    m = mx;
-    float sum = e;
-    for (int x = 16; x; x >>= 1) sum += __shfl_xor_sync(~0u, sum, x);
-    l = l * c + sum;
-    for (int d = 0; d < HD / 32; d++) o[d] *= c;
-    for (unsigned live = __ballot_sync(~0u, ok); live; live &= live - 1) {
-      const int i = __ffs(live) - 1;
-      const float pi = __shfl_sync(~0u, e, i);
-      for (int d = 0; d < HD / 32; d++) o[d] += pi * element<FP8>(v, (j0 + i) * p.v_row + d * 32 + lane);
-    }
-  }
-  const float inv = bad ? CUDART_NAN_F : l == 0.f ? 0.f : 1.f / l;
-  __nv_bfloat16* out = p.out + seq * p.o_seq + tok * p.o_row + h * p.o_head;
-  for (int d = 0; d < HD / 32; d++) out[d * 32 + lane] = __float2bfloat16_rn(o[d] * inv);
-  if (p.lse && lane == 0)
-    p.lse[row * p.nq + h] = bad ? CUDART_NAN_F : l == 0.f ? -CUDART_INF_F : m + logf(l);
+cudaError_t allow_smem() {
+  static std::atomic<unsigned long long> done{0};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const unsigned long long bit = 1ull << (dev & 63);
+  if (dev < 64 && (done.load(std::memory_order_acquire) & bit)) return cudaSuccess;
+  e = cudaFuncSetAttribute(amk::attn_kernel<HD, TREE, FP8>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                           amk::AttnSmem<HD, FP8>::kBytes);
+  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_release);
+  return e;
 }
 
-template <bool TREE>
-cudaError_t launch(const Params& p, int hd, bool fp8, cudaStream_t st) {
-  const int64_t warps = (TREE ? (int64_t)p.n_seqs * p.rows : p.rows) * p.nq;
-  const unsigned blocks = (unsigned)((warps + 3) / 4);
-  if (hd == 64)
-    fp8 ? attn_kernel<64, TREE, TREE><<<blocks, 128, 0, st>>>(p) : attn_kernel<64, TREE, false><<<blocks, 128, 0, st>>>(p);
-  else
-    fp8 ? attn_kernel<128, TREE, TREE><<<blocks, 128, 0, st>>>(p) : attn_kernel<128, TREE, false><<<blocks, 128, 0, st>>>(p);
+template <int HD, bool TREE, bool FP8>
+cudaError_t launch_attn(const AttnParams& p, const CUtensorMap& k, const CUtensorMap& v, unsigned blocks,
+                        cudaStream_t st) {
+  const cudaError_t e = allow_smem<HD, TREE, FP8>();
+  if (e != cudaSuccess) return e;
+  amk::attn_kernel<HD, TREE, FP8><<<blocks, FP8 ? 512 : 384, amk::AttnSmem<HD, FP8>::kBytes, st>>>(p, k, v);
   return cudaGetLastError();
+}
+
+template <int HD>
+cudaError_t launch_join(const AttnParams& p, unsigned blocks, cudaStream_t st) {
+  // starts while the attention kernel runs and waits there for its end: the launch is off the path
+  cudaLaunchAttribute at;
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(p.rows * p.rep + 7) / 8, (unsigned)p.nkv, (unsigned)p.n_seqs);
+  cfg.blockDim = dim3(256);
+  cfg.stream = st;
+  cfg.attrs = &at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, amk::attn_join_kernel<HD>, p, (int)blocks);
+}
+
+int sm_count() {
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return 148;
+  }
+  return n;
+}
+
+// How a tree call is divided: rows of a block, blocks, scratch.
+struct TreePlan {
+  int part_rows, row_tiles;
+  unsigned blocks;
+  size_t bytes;
+};
+constexpr int kMinTiles = 2;
+TreePlan tree_plan(const amk_tree_args& a) {
+  TreePlan t;
+  const int64_t rows = (int64_t)a.n_rows * (a.n_q_heads / a.n_kv_heads);
+  t.part_rows = rows <= amk::kTile ? amk::kTile : 2 * amk::kTile;
+  t.row_tiles = (int)((rows + t.part_rows - 1) / t.part_rows);
+  const int64_t most = a.n_slots - a.n_rows, len = a.max_len && a.max_len < most ? a.max_len : most;
+  const int64_t tiles = (len + a.n_rows + amk::kTile - 1) / amk::kTile;
+  const int64_t runs = (tiles * a.n_kv_heads * t.row_tiles * a.n_seqs + kMinTiles - 1) / kMinTiles;
+  const int sms = sm_count();
+  t.blocks = (unsigned)(runs < sms ? runs : sms);
+  t.bytes = (size_t)2 * t.blocks * t.part_rows * (a.head_dim + 1) * 4;
+  return t;
 }
 
 amk_status check_heads(const Reason& fail, uint32_t hd, uint32_t nq, uint32_t nkv, float scale) {
@@ -181,15 +185,22 @@ extern "C" amk_status amk_prompt_attention(const amk_prompt_args* args, char* ms
   AMK_TRY(check_stride(fail, "k head", a.n_kv_heads, &a.k_head, hd, 2));
   AMK_TRY(check_stride(fail, "v head", a.n_kv_heads, &a.v_head, hd, 2));
   AMK_TRY(check_stride(fail, "out head", a.n_q_heads, &a.out_head, hd, 2));
-  Params p{};
-  p.q = (const unsigned char*)a.q, p.k = (const unsigned char*)a.k, p.v = (const unsigned char*)a.v;
-  p.out = (__nv_bfloat16*)a.out, p.lse = a.lse, p.lens = a.cu_seqlens;
-  p.q_row = a.q_row, p.q_head = a.q_head, p.k_row = a.k_row, p.k_head = a.k_head;
-  p.v_row = a.v_row, p.v_head = a.v_head, p.o_row = a.out_row, p.o_head = a.out_head;
-  p.n_seqs = (int)a.n_seqs, p.nq = (int)a.n_q_heads, p.rep = (int)(a.n_q_heads / a.n_kv_heads);
+  AttnParams p{};
+  p.q = (const unsigned short*)a.q, p.out = (__nv_bfloat16*)a.out, p.lse = a.lse, p.lens = a.cu_seqlens;
+  p.q_row = a.q_row, p.q_head = a.q_head, p.o_row = a.out_row, p.o_head = a.out_head;
+  p.n_seqs = (int)a.n_seqs, p.nq = (int)a.n_q_heads, p.nkv = (int)a.n_kv_heads, p.rep = p.nq / p.nkv;
   p.rows = (int)a.total;
   p.scale = a.scale > 0.f ? a.scale : 1.f / sqrtf((float)hd);
-  const cudaError_t e = launch<false>(p, (int)hd, false, (cudaStream_t)cuda_stream);
+  // blocks of 256 / rep tokens: every prompt may leave one that is not full
+  const int64_t blocks = (a.total / (2 * amk::kTile / p.rep) + (a.total < a.n_seqs ? a.total : a.n_seqs)) * p.nkv;
+  if (blocks > 0x7fffffff) return fail(AMK_ERR_UNSUPPORTED, "%lld blocks of queries", (long long)blocks);
+  CUtensorMap mk, mv;
+  if (!make_map(&mk, a.k, false, hd, a.total, p.nkv, 1, a.k_row, a.k_head, hd) ||
+      !make_map(&mv, a.v, false, hd, a.total, p.nkv, 1, a.v_row, a.v_head, hd))
+    return fail(AMK_ERR_CUDA, "cuTensorMapEncodeTiled failed or is missing");
+  const cudaStream_t st = (cudaStream_t)cuda_stream;
+  const cudaError_t e = hd == 64 ? launch_attn<64, false, false>(p, mk, mv, (unsigned)blocks, st)
+                                 : launch_attn<128, false, false>(p, mk, mv, (unsigned)blocks, st);
   return e == cudaSuccess ? AMK_OK : fail(AMK_ERR_CUDA, "launch failed: %s", cudaGetErrorString(e));
 }
 
@@ -198,8 +209,26 @@ extern "C" amk_status amk_tree_workspace_bytes(const amk_tree_args* args, size_t
   const Reason fail(msg, msg_bytes, "amk_tree_workspace_bytes");
   if (!bytes) return fail(AMK_ERR_INVALID_ARG, "NULL pointer");
   AMK_TRY(check_tree(fail, args));
-  *bytes = 0;
+  *bytes = tree_plan(*args).bytes;
   return AMK_OK;
+}
+
+extern "C" amk_status amk_operator_status(amk_status* st, char* msg, size_t msg_bytes, void* cuda_stream) {
+  const Reason fail(msg, msg_bytes, "amk_operator_status");
+  if (!st) return fail(AMK_ERR_INVALID_ARG, "NULL pointer");
+  *st = AMK_OK;
+  unsigned expired = 0;
+  cudaError_t e = cudaStreamSynchronize((cudaStream_t)cuda_stream);
+  if (e == cudaSuccess)
+    e = cudaMemcpyFromSymbolAsync(&expired, amk::g_attn_expired, 4, 0, cudaMemcpyDeviceToHost, (cudaStream_t)cuda_stream);
+  if (e == cudaSuccess) e = cudaStreamSynchronize((cudaStream_t)cuda_stream);
+  if (e == cudaSuccess && expired) {
+    const unsigned zero = 0;
+    e = cudaMemcpyToSymbolAsync(amk::g_attn_expired, &zero, 4, 0, cudaMemcpyHostToDevice, (cudaStream_t)cuda_stream);
+    if (e == cudaSuccess) e = cudaStreamSynchronize((cudaStream_t)cuda_stream);
+    *st = AMK_ERR_TIMEOUT;
+  }
+  return e == cudaSuccess ? AMK_OK : fail(AMK_ERR_CUDA, "%s", cudaGetErrorString(e));
 }
 
 extern "C" amk_status amk_tree_attention(const amk_tree_args* args, char* msg, size_t msg_bytes,
@@ -228,16 +257,31 @@ extern "C" amk_status amk_tree_attention(const amk_tree_args* args, char* msg, s
   AMK_TRY(check_stride(fail, "out sequence", a.n_seqs, &a.out_seq, hd, 2));
   AMK_TRY(check_stride(fail, "out row", a.n_rows, &a.out_row, hd, 2));
   AMK_TRY(check_stride(fail, "out head", a.n_q_heads, &a.out_head, hd, 2));
-  Params p{};
-  p.q = (const unsigned char*)a.q, p.k = (const unsigned char*)a.k, p.v = (const unsigned char*)a.v;
-  p.out = (__nv_bfloat16*)a.out, p.lse = a.lse, p.lens = a.cache_len, p.mask = (const unsigned long long*)a.mask;
+  const TreePlan t = tree_plan(a);
+  if (!a.workspace || a.workspace_bytes < t.bytes)
+    return fail(AMK_ERR_INVALID_ARG, "workspace of %llu bytes, %zu are needed", (unsigned long long)(a.workspace ? a.workspace_bytes : 0),
+                t.bytes);
+  AttnParams p{};
+  p.q = (const unsigned short*)a.q, p.out = (__nv_bfloat16*)a.out, p.lse = a.lse, p.lens = a.cache_len;
+  p.mask = (const unsigned long long*)a.mask;
+  p.part_o = (float*)a.workspace, p.part_lse = p.part_o + (size_t)2 * t.blocks * t.part_rows * a.head_dim;
   p.q_seq = a.q_seq, p.q_row = a.q_row, p.q_head = a.q_head;
-  p.k_seq = a.k_seq, p.k_row = a.k_row, p.k_head = a.k_head;
-  p.v_seq = a.v_seq, p.v_row = a.v_row, p.v_head = a.v_head;
   p.o_seq = a.out_seq, p.o_row = a.out_row, p.o_head = a.out_head;
-  p.n_seqs = (int)a.n_seqs, p.nq = (int)a.n_q_heads, p.rep = (int)(a.n_q_heads / a.n_kv_heads);
+  p.n_seqs = (int)a.n_seqs, p.nq = (int)a.n_q_heads, p.nkv = (int)a.n_kv_heads, p.rep = p.nq / p.nkv;
   p.rows = (int)a.n_rows, p.slots = (int)a.n_slots;
+  p.part_rows = t.part_rows, p.row_tiles = t.row_tiles, p.min_tiles = kMinTiles;
   p.scale = a.scale > 0.f ? a.scale : 1.f / sqrtf((float)hd);
-  const cudaError_t e = launch<true>(p, (int)hd, esz == 1, (cudaStream_t)cuda_stream);
+  const bool fp8 = esz == 1;
+  CUtensorMap mk, mv;
+  if (!make_map(&mk, a.k, fp8, hd, a.n_slots, p.nkv, a.n_seqs, a.k_row, a.k_head, a.k_seq) ||
+      !make_map(&mv, a.v, fp8, hd, a.n_slots, p.nkv, a.n_seqs, a.v_row, a.v_head, a.v_seq))
+    return fail(AMK_ERR_CUDA, "cuTensorMapEncodeTiled failed or is missing");
+  const cudaStream_t st = (cudaStream_t)cuda_stream;
+  cudaError_t e;
+  if (hd == 64)
+    e = fp8 ? launch_attn<64, true, true>(p, mk, mv, t.blocks, st) : launch_attn<64, true, false>(p, mk, mv, t.blocks, st);
+  else
+    e = fp8 ? launch_attn<128, true, true>(p, mk, mv, t.blocks, st) : launch_attn<128, true, false>(p, mk, mv, t.blocks, st);
+  if (e == cudaSuccess) e = hd == 64 ? launch_join<64>(p, t.blocks, st) : launch_join<128>(p, t.blocks, st);
   return e == cudaSuccess ? AMK_OK : fail(AMK_ERR_CUDA, "launch failed: %s", cudaGetErrorString(e));
 }
