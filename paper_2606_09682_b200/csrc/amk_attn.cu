@@ -189,6 +189,7 @@ extern "C" amk_status amk_prompt_attention(const amk_prompt_args* args, char* ms
   p.q = (const unsigned short*)a.q, p.out = (__nv_bfloat16*)a.out, p.lse = a.lse, p.lens = a.cu_seqlens;
   p.q_row = a.q_row, p.q_head = a.q_head, p.o_row = a.out_row, p.o_head = a.out_head;
   p.n_seqs = (int)a.n_seqs, p.nq = (int)a.n_q_heads, p.nkv = (int)a.n_kv_heads, p.rep = p.nq / p.nkv;
+  p.rep_inv = p.rep == 1 ? 0 : (unsigned)(((1ull << 32) + p.rep - 1) / p.rep);
   p.rows = (int)a.total;
   p.scale = a.scale > 0.f ? a.scale : 1.f / sqrtf((float)hd);
   // blocks of 256 / rep tokens: every prompt may leave one that is not full
@@ -268,6 +269,7 @@ extern "C" amk_status amk_tree_attention(const amk_tree_args* args, char* msg, s
   p.q_seq = a.q_seq, p.q_row = a.q_row, p.q_head = a.q_head;
   p.o_seq = a.out_seq, p.o_row = a.out_row, p.o_head = a.out_head;
   p.n_seqs = (int)a.n_seqs, p.nq = (int)a.n_q_heads, p.nkv = (int)a.n_kv_heads, p.rep = p.nq / p.nkv;
+  p.rep_inv = p.rep == 1 ? 0 : (unsigned)(((1ull << 32) + p.rep - 1) / p.rep);
   p.rows = (int)a.n_rows, p.slots = (int)a.n_slots;
   p.part_rows = t.part_rows, p.row_tiles = t.row_tiles, p.min_tiles = kMinTiles;
   p.scale = a.scale > 0.f ? a.scale : 1.f / sqrtf((float)hd);

@@ -29,10 +29,15 @@ struct AttnParams {
   int part_rows;                   // tree: 128 (both warpgroups work on the same rows) or 256
   int row_tiles;                   // tree: blocks of part_rows rows per (sequence, kv head)
   int min_tiles;                   // tree: key tiles a block takes at least
+  unsigned rep_inv;                // ceil(2^32 / rep), 0 for rep = 1
   float scale;
 };
 
 constexpr int kTile = 128;         // rows of a Q tile, keys of a K/V tile
+// row / rep, exact for rows below 2^28
+__device__ __forceinline__ int div_rep(const AttnParams& p, int row) {
+  return p.rep_inv ? (int)__umulhi((unsigned)row, p.rep_inv) : row;
+}
 constexpr float kLog2e = 1.4426950408889634f;
 
 // Set when a bounded wait of an attention kernel ran out; read and cleared by amk_operator_status.
@@ -49,6 +54,37 @@ __device__ __forceinline__ unsigned pack_bf16(float lo, float hi) {   // round t
   return r;
 }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+// two fp32 lanes in one instruction
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+  uint64_t d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
+  return d;
+}
+__device__ __forceinline__ void unpair(float& lo, float& hi, uint64_t a) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(a));
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+// acc + 0 * w for two bf16 at once: NaN from the first value on that is not finite
+__device__ __forceinline__ unsigned zero_times(unsigned w, unsigned acc) {
+  unsigned d;
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(w), "r"(0u), "r"(acc));
+  return d;
+}
+
 // ---- what the blocks work on ------------------------------------------------------------------------------------
 // One unit: a block of query rows of one (sequence, kv head) and a run of its key tiles.
 struct Unit {
@@ -61,11 +97,6 @@ struct Unit {
 };
 
 // Tree: the key tiles of all (sequence, kv head, row block) in that order, cut into equal runs, one for each block.
-struct TreeWalk {
-  int64_t at, end, per;   // flat tile index now, end of this block's run
-  int seq, len, tiles;    // current sequence
-  int64_t seq_at;         // flat index of its first tile
-};
 __device__ __forceinline__ int tree_tiles(const AttnParams& p, int len) {   // key tiles of one item; 0: bad length
   return len < 0 || len > p.slots - p.rows ? 0 : (len + p.rows + kTile - 1) / kTile;
 }
@@ -112,20 +143,21 @@ struct AttnHead {
   int skip[2];                         // this step's P V was done by the warpgroup itself
   float m[kTile], l[kTile];            // second warpgroup's statistics (both on the same rows)
   int unit[8];
-  int64_t walk[6];
+  int64_t walk[1];
 };
 static_assert(sizeof(AttnHead) <= 2048, "head");
 
-constexpr unsigned long long kWaitNs = 2000000000ull;
-// Waits for the phase of the given parity, two seconds at most.
+constexpr long long kWaitCycles = 4000000000ll;
+// Waits for the phase of the given parity, about two seconds at most (the SM's cycle counter: the global timer is read
+// through a unit that all SMs share).
 __device__ __forceinline__ void attn_wait(uint64_t* bar, unsigned parity, AttnHead& h) {
   if (mbar_try_wait(bar, parity)) return;
-  const unsigned long long t0 = globaltimer_ns();
+  const long long t0 = clock64();
   for (;;) {
     for (int i = 0; i < 32; i++)
       if (mbar_try_wait(bar, parity)) return;
     if (*(volatile int*)&h.dead) return;
-    if (globaltimer_ns() - t0 > kWaitNs) {
+    if (clock64() - t0 > kWaitCycles) {
       *(volatile int*)&h.dead = 1;
       atomicExch(&g_attn_expired, 1u);
       return;
@@ -148,36 +180,30 @@ struct Units;
 
 template <>
 struct Units<true> {
-  int64_t at, end, seq_at;
-  int seq, len, tiles, per_seq;
+  int64_t left;                    // key tiles of this block's run that are still to come
+  int seq, len, tiles, item, within, items;
   __device__ __forceinline__ void init(const AttnParams& p, const AttnHead& h) {
-    at = h.walk[0], end = h.walk[1], seq_at = h.walk[2];
-    seq = (int)h.walk[3];
-    per_seq = p.nkv * p.row_tiles;
-    if (at < end) load(p);
-  }
-  __device__ __forceinline__ void load(const AttnParams& p) {
-    len = p.lens[seq];
+    left = h.walk[0];
+    seq = h.unit[0], item = h.unit[1], within = h.unit[2], len = h.unit[3];
     tiles = tree_tiles(p, len);
+    items = p.nkv * p.row_tiles;
   }
   __device__ __forceinline__ bool next(const AttnParams& p, const AttnHead&, Unit& u) {
-    if (at >= end) return false;
-    while (seq_at + (int64_t)tiles * per_seq <= at) {   // at < total: ends before the sequences do
-      seq_at += (int64_t)tiles * per_seq;
-      seq++;
-      load(p);
+    if (left <= 0) return false;
+    while (item == items || tiles == 0) {   // something is left: a sequence with tiles follows
+      item = 0;
+      len = p.lens[++seq];
+      tiles = tree_tiles(p, len);
     }
-    const int64_t rel = at - seq_at;
-    const int item = (int)(rel / tiles), within = (int)(rel - (int64_t)item * tiles);
-    const int64_t left = end - at;
     const int run = left < tiles - within ? (int)left : tiles - within;
-    u.seq = seq, u.head = item / p.row_tiles, u.len = len;
-    const int rt = item - u.head * p.row_tiles;
-    u.row0 = rt * p.part_rows;
+    u.seq = seq, u.head = p.row_tiles == 1 ? item : item / p.row_tiles, u.len = len;
+    u.row0 = (item - u.head * p.row_tiles) * p.part_rows;
     u.n_rows = min(p.part_rows, p.rows * p.rep - u.row0);
     u.tok0 = 0, u.n_tok = p.rows, u.key0 = 0;
     u.tile_begin = within, u.tile_end = within + run, u.item_tiles = tiles;
-    at += run;
+    left -= run;
+    within = 0;
+    item++;
     return true;
   }
 };
@@ -205,7 +231,7 @@ __device__ __forceinline__ int unit_steps(const AttnParams& p, const Unit& u, bo
   if (u.n_rows <= first) return 0;
   if (TREE) return n;
   const int last = min(u.n_rows, first + kTile) - 1;
-  return (u.tok0 + last / p.rep) / kTile + 1;
+  return (u.tok0 + div_rep(p, last)) / kTile + 1;
 }
 
 // 32 bits of a drafted token's mask from drafted index idx on (idx may be negative: bits below 0 are 0)
@@ -229,6 +255,41 @@ __device__ __forceinline__ unsigned tree_bits32(const unsigned long long* w, int
   return left >= 32 ? (unsigned)v : (unsigned)v & ((1u << left) - 1u);
 }
 
+// O += P V of one tile for this warp's rows, key by key and only for the keys that a row sees: for tiles with values
+// that are not finite behind a mask, where 0 * V would not be 0.
+template <int HD>
+__device__ __noinline__ void product_by_key(const float* pl, const uint4 see, const unsigned char* vt, unsigned to, bool more) {
+  for (int x = 0; x < HD; x += 32) {
+    unsigned o[32];
+    tmem_ld32(o, to + x);
+    tmem_wait_ld();
+    tmem_pin(o);
+    float a[32];
+#pragma unroll
+    for (int k = 0; k < 32; k++) a[k] = more ? __uint_as_float(o[k]) : 0.f;
+    for (int k = 0; k < kTile; k++) {
+      const unsigned w = k < 64 ? (k < 32 ? see.x : see.y) : (k < 96 ? see.z : see.w);
+      if (!(w >> (k & 31) & 1)) continue;
+#pragma unroll
+      for (int ch = 0; ch < 4; ch++) {
+        const int cc = x / 8 + ch;
+        const uint4 v = *(const uint4*)(vt + cc / 8 * kBox + k * 128 + (((cc & 7) ^ (k & 7)) << 4));
+        const unsigned vv[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+          a[ch * 8 + 2 * e] += pl[k] * bf16_lo(vv[e]);
+          a[ch * 8 + 2 * e + 1] += pl[k] * bf16_hi(vv[e]);
+        }
+      }
+    }
+    __syncwarp();
+#pragma unroll
+    for (int k = 0; k < 32; k++) o[k] = __float_as_uint(a[k]);
+    tmem_st32(to + x, o);
+  }
+  tmem_wait_st();
+}
+
 // ---- the kernel -------------------------------------------------------------------------------------------------
 template <int HD, bool TREE, bool FP8>
 __global__ void __launch_bounds__(FP8 ? 512 : 384, 1)
@@ -248,7 +309,7 @@ __global__ void __launch_bounds__(FP8 ? 512 : 384, 1)
       const int64_t per = tree_per_block(p, total, gridDim.x);
       const int64_t at = (int64_t)blockIdx.x * per, end = at + per < total ? at + per : total;
       int64_t before = 0;
-      int seq = 0;
+      int seq = 0, item = 0, within = 0, len = 0;
       if (at < end) {
         const int64_t items = (int64_t)p.nkv * p.row_tiles;
         for (int b0 = 0;; b0 += 32) {
@@ -264,12 +325,16 @@ __global__ void __launch_bounds__(FP8 ? 512 : 384, 1)
             const int f = __ffs(hit) - 1;
             seq = b0 + f;
             before += __shfl_sync(~0u, n - own, f);
+            len = p.lens[seq];
+            const int tiles = tree_tiles(p, len);
+            const int64_t rel = at - before;
+            item = (int)(rel / tiles), within = (int)(rel - (int64_t)item * tiles);
             break;
           }
           before += __shfl_sync(~0u, n, 31);
         }
       }
-      if (lane == 0) h.walk[0] = at, h.walk[1] = end, h.walk[2] = before, h.walk[3] = seq;
+      if (lane == 0) h.walk[0] = end - at, h.unit[0] = seq, h.unit[1] = item, h.unit[2] = within, h.unit[3] = len;
     } else {
       // the blocks of all prompts in order; the last block of a long prompt has the most keys and goes first
       const int head = blockIdx.x % p.nkv, per = 2 * kTile / p.rep;
@@ -354,97 +419,122 @@ __global__ void __launch_bounds__(FP8 ? 512 : 384, 1)
         const unsigned short* q = p.q + (int64_t)u.seq * p.q_seq + (int64_t)(u.key0 + u.tok0) * p.q_row +
                                   (int64_t)u.head * p.rep * p.q_head;
 #pragma unroll
-        for (int i = 0; i < kChunks; i++) {
-          const int e = i * kTile + wt, r = e / kChunks, ch = e % kChunks;
-          uint4 v = make_uint4(0, 0, 0, 0);
-          if (r < rows_here) {
-            const int row = row_first + r, tok = row / p.rep, hh = row - tok * p.rep;
-            v = *(const uint4*)(q + tok * p.q_row + hh * p.q_head + ch * 8);
+        for (int i0 = 0; i0 < kChunks; i0 += 8) {        // eight loads in flight before the first store
+          uint4 v[8];
+#pragma unroll
+          for (int i = 0; i < 8; i++) {
+            const int e = (i0 + i) * kTile + wt, r = e / kChunks, ch = e % kChunks;
+            v[i] = make_uint4(0, 0, 0, 0);
+            if (r < rows_here) {
+              const int row = row_first + r, tok = div_rep(p, row), hh = row - tok * p.rep;
+              v[i] = __ldg((const uint4*)(q + tok * p.q_row + hh * p.q_head + ch * 8));
+            }
           }
-          *(uint4*)(qs + ch / 8 * kBox + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) = v;
+#pragma unroll
+          for (int i = 0; i < 8; i++) {
+            const int e = (i0 + i) * kTile + wt, r = e / kChunks, ch = e % kChunks;
+            *(uint4*)(qs + ch / 8 * kBox + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) = v[i];
+          }
         }
         fence_async_smem();
         mbar_arrive(&h.q_full[t]);
       }
-      const int row = row_first + wt, tok = row / p.rep, hh = row - tok * p.rep;
+      const int row = row_first + wt, tok = div_rep(p, row), hh = row - tok * p.rep;
       const bool valid = wt < rows_here;
+      const bool live = (wt & ~31) < rows_here;        // this warp has rows; the others only keep step
       const unsigned long long* words = nullptr;
       if (TREE && p.mask && valid) words = p.mask + ((int64_t)u.seq * p.rows + tok) * ((p.rows + 63) / 64);
-      const int64_t key_end = TREE ? (int64_t)u.len + p.rows : u.tok0 + u.n_tok;    // keys nobody here sees: from it on
+      const int key_end = TREE ? u.len + p.rows : u.tok0 + u.n_tok;    // keys nobody here sees: from it on
       // first key that a row of this tile may not see
-      const int64_t all_see = TREE ? u.len : (int64_t)u.tok0 + row_first / p.rep + 1;
+      const int all_see = TREE ? u.len : u.tok0 + div_rep(p, row_first) + 1;
       float m = -CUDART_INF_F, l = 0.f;
       for (int i = 0; i < steps; i++) {
         const int rel = dual ? 2 * i + t : i;
-        const int64_t key = (int64_t)(u.tile_begin + rel) * kTile;
+        const int key = (u.tile_begin + rel) * kTile;
         attn_wait(&h.s_full[t], s_phase & 1, h);
         s_phase++;
         __syncwarp();
         tc_fence_after();
         unsigned sb[4][32];
-#pragma unroll
-        for (int k = 0; k < 4; k++) tmem_ld32(sb[k], ts + 32 * k);
-        tmem_wait_ld();
-#pragma unroll
-        for (int k = 0; k < 4; k++) tmem_pin(sb[k]);
+        unsigned see[4] = {~0u, ~0u, ~0u, ~0u};
 #define AMK_S(k) __uint_as_float(sb[(k) >> 5][(k) & 31])
         const bool masked = key + kTile > all_see;
-        unsigned see[4] = {~0u, ~0u, ~0u, ~0u};
-        if (masked) {
+        if (live) {
 #pragma unroll
-          for (int w = 0; w < 4; w++) {
-            const int64_t first = key + 32 * w;
-            if (TREE) {
-              const int64_t ctx = u.len - first;                  // context keys from `first` on
-              if (ctx < 32) see[w] = (ctx > 0 ? (1u << ctx) - 1u : 0u) | tree_bits32(words, p.mask ? (words ? p.rows : 0) : p.rows, tok, (int)-ctx);
-            } else {
-              const int64_t n = (int64_t)u.tok0 + tok + 1 - first;
-              see[w] = n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u;
+          for (int k = 0; k < 4; k++) tmem_ld32(sb[k], ts + 32 * k);
+          tmem_wait_ld();
+#pragma unroll
+          for (int k = 0; k < 4; k++) tmem_pin(sb[k]);
+          if (masked) {
+#pragma unroll
+            for (int w = 0; w < 4; w++) {
+              const int first = key + 32 * w;
+              if (TREE) {
+                const int ctx = u.len - first;                  // context keys from `first` on
+                if (ctx < 32)
+                  see[w] = (ctx > 0 ? (1u << ctx) - 1u : 0u) |
+                           tree_bits32(words, p.mask ? (words ? p.rows : 0) : p.rows, tok, -ctx);
+              } else {
+                const int n = u.tok0 + tok + 1 - first;
+                see[w] = n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u;
+              }
+            }
+#pragma unroll
+            for (int k = 0; k < kTile; k++)
+              if (!(see[k >> 5] >> (k & 31) & 1)) sb[k >> 5][k & 31] = 0xff800000u;   // -infinity
+          }
+          float mx[4];
+#pragma unroll
+          for (int k = 0; k < 4; k++) mx[k] = AMK_S(32 * k);
+#pragma unroll
+          for (int j = 1; j < 31; j += 2)
+#pragma unroll
+            for (int k = 0; k < 4; k++) mx[k] = max3(mx[k], AMK_S(32 * k + j), AMK_S(32 * k + j + 1));
+#pragma unroll
+          for (int k = 0; k < 4; k++) mx[k] = fmaxf(mx[k], AMK_S(32 * k + 31));
+          mx[0] = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]);
+          if (i == 0) {
+            m = mx[0];
+          } else {
+            const bool need = mx[0] > m && (mx[0] - m) * c > 8.f;
+            if (__any_sync(~0u, need)) {
+              const float mn = fmaxf(m, mx[0]);
+              const float f = m == mn ? 1.f : exp2_fast((m - mn) * c);
+#pragma unroll
+              for (int x = 0; x < HD; x += 32) {
+                unsigned o[32];
+                tmem_ld32(o, to + x);
+                tmem_wait_ld();
+                tmem_pin(o);
+#pragma unroll
+                for (int k = 0; k < 32; k++) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+                tmem_st32(to + x, o);
+              }
+              l *= f;
+              m = mn;
             }
           }
+          const float mc = m == -CUDART_INF_F ? 0.f : -m * c;
+          const uint64_t c2 = pair(c, c), mc2 = pair(mc, mc);
+          uint64_t sum[2] = {0, 0};
 #pragma unroll
-          for (int k = 0; k < kTile; k++)
-            if (!(see[k >> 5] >> (k & 31) & 1)) sb[k >> 5][k & 31] = 0xff800000u;   // -infinity
-        }
-        float mx = AMK_S(0);
-#pragma unroll
-        for (int k = 1; k < kTile; k++) mx = fmaxf(mx, AMK_S(k));
-        if (i == 0) {
-          m = mx;
-        } else {
-          const bool need = mx > m && (mx - m) * c > 8.f;
-          if (__any_sync(~0u, need)) {
-            const float mn = fmaxf(m, mx);
-            const float f = m == mn ? 1.f : exp2_fast((m - mn) * c);
-#pragma unroll
-            for (int x = 0; x < HD; x += 32) {
-              unsigned o[32];
-              tmem_ld32(o, to + x);
-              tmem_wait_ld();
-              tmem_pin(o);
-#pragma unroll
-              for (int k = 0; k < 32; k++) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
-              tmem_st32(to + x, o);
-            }
-            l *= f;
-            m = mn;
+          for (int k = 0; k < kTile; k += 2) {
+            float e0, e1;
+            unpair(e0, e1, fma2(pair(AMK_S(k), AMK_S(k + 1)), c2, mc2));
+            e0 = exp2_fast(e0), e1 = exp2_fast(e1);
+            sb[k >> 5][k & 31] = __float_as_uint(e0), sb[k >> 5][(k & 31) + 1] = __float_as_uint(e1);
+            sum[k >> 1 & 1] = add2(sum[k >> 1 & 1], pair(e0, e1));
           }
-        }
-        const float mc = m == -CUDART_INF_F ? 0.f : m * c;
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+          float s0, s1;
+          unpair(s0, s1, add2(sum[0], sum[1]));
+          l += s0 + s1;
 #pragma unroll
-        for (int k = 0; k < kTile; k++) {
-          const float e = exp2_fast(fmaf(AMK_S(k), c, -mc));
-          sb[k >> 5][k & 31] = __float_as_uint(e);
-          sum[k & 3] += e;
-        }
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+          for (int x = 0; x < 2; x++) {
+            unsigned r[32];
 #pragma unroll
-        for (int x = 0; x < 2; x++) {
-          unsigned r[32];
-#pragma unroll
-          for (int k = 0; k < 32; k++) r[k] = pack_bf16(AMK_S(x * 64 + 2 * k), AMK_S(x * 64 + 2 * k + 1));
-          tmem_st32(ts + x * 32, r);
+            for (int k = 0; k < 32; k++) r[k] = pack_bf16(AMK_S(x * 64 + 2 * k), AMK_S(x * 64 + 2 * k + 1));
+            tmem_st32(ts + x * 32, r);
+          }
         }
         unsigned slow = 0;
         if (masked) {
@@ -454,7 +544,7 @@ __global__ void __launch_bounds__(FP8 ? 512 : 384, 1)
           attn_wait(&h.full[st], pos / L::kStages & 1, h);
           unsigned char* vt = smem + L::kRing + st * L::kTileBytes;
           unsigned char* vr = vt + wt * 128;
-          bool broken = false;
+          unsigned broken = 0;                         // becomes NaN (two bf16)
           if (key + wt >= key_end) {
 #pragma unroll
             for (int ch = 0; ch < HD / 8; ch++) *(uint4*)(vr + ch / 8 * kBox + ((ch & 7) << 4)) = make_uint4(0, 0, 0, 0);
@@ -463,45 +553,16 @@ __global__ void __launch_bounds__(FP8 ? 512 : 384, 1)
 #pragma unroll
             for (int ch = 0; ch < HD / 8; ch++) {
               const uint4 v = *(const uint4*)(vr + ch / 8 * kBox + (((ch & 7) ^ (wt & 7)) << 4));
-              const unsigned vv[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-              for (int k = 0; k < 4; k++)
-                broken |= (vv[k] & 0x7f80u) == 0x7f80u || (vv[k] & 0x7f800000u) == 0x7f800000u;
+              broken = zero_times(v.w, zero_times(v.z, zero_times(v.y, zero_times(v.x, broken))));
             }
           }
-          slow = any_of_warpgroup(broken, 1 + t);
-          if (slow) {
-            float pl[kTile];                           // (in local memory: this path walks it)
-            const unsigned sl[4] = {see[0], see[1], see[2], see[3]};
+          slow = any_of_warpgroup((broken & 0x7fff7fffu) != 0, 1 + t);
+          if (slow && live) {
+            float pl[kTile];                           // (in local memory: the function walks it)
 #pragma unroll
             for (int k = 0; k < kTile; k++) pl[k] = AMK_S(k);
-            for (int x = 0; x < HD; x += 32) {
-              unsigned o[32];
-              tmem_ld32(o, to + x);
-              tmem_wait_ld();
-              tmem_pin(o);
-              float a[32];
-#pragma unroll
-              for (int k = 0; k < 32; k++) a[k] = i ? __uint_as_float(o[k]) : 0.f;
-              for (int k = 0; k < kTile; k++) {
-                if (!(sl[k >> 5] >> (k & 31) & 1)) continue;
-#pragma unroll
-                for (int ch = 0; ch < 4; ch++) {
-                  const int cc = x / 8 + ch;
-                  const uint4 v = *(const uint4*)(vt + cc / 8 * kBox + k * 128 + (((cc & 7) ^ (k & 7)) << 4));
-                  const unsigned vv[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                  for (int e = 0; e < 4; e++) {
-                    a[ch * 8 + 2 * e] += pl[k] * bf16_lo(vv[e]);
-                    a[ch * 8 + 2 * e + 1] += pl[k] * bf16_hi(vv[e]);
-                  }
-                }
-              }
-              __syncwarp();
-#pragma unroll
-              for (int k = 0; k < 32; k++) o[k] = __float_as_uint(a[k]);
-              tmem_st32(to + x, o);
-            }
+            const uint4 sl = make_uint4(see[0], see[1], see[2], see[3]);
+            product_by_key<HD>(pl, sl, vt, to, i > 0);
           }
         }
         tmem_wait_st();
@@ -542,7 +603,7 @@ __global__ void __launch_bounds__(FP8 ? 512 : 384, 1)
           from1 = to + HD;
         }
       }
-      if (steps && !(dual && t == 1)) {
+      if (steps && live && !(dual && t == 1)) {
         const bool whole = !TREE || (u.tile_begin == 0 && u.tile_end == u.item_tiles);
         const float inv = l == 0.f ? 0.f : 1.f / l;
         const float lse2 = l == 0.f ? -CUDART_INF_F : m * c + log2f(l);
@@ -752,7 +813,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(const AttnParams p, int 
   const int rows = p.rows * p.rep;
   const int row = blockIdx.x * 8 + warp;
   if (row >= rows) return;
-  const int tok = row / p.rep, q_head = head * p.rep + row - tok * p.rep;
+  const int tok = div_rep(p, row), q_head = head * p.rep + row - tok * p.rep;
   __nv_bfloat16* out = p.out + (int64_t)seq * p.o_seq + tok * p.o_row + q_head * p.o_head;
   float* lse = p.lse ? p.lse + ((int64_t)seq * p.rows + tok) * p.nq + q_head : nullptr;
   constexpr int kEach = HD / 32;
