@@ -68,7 +68,7 @@ cudaError_t launch_attn(const AttnParams& p, const CUtensorMap& k, const CUtenso
                         cudaStream_t st) {
   const cudaError_t e = allow_smem<HD, TREE, FP8>();
   if (e != cudaSuccess) return e;
-  amk::attn_kernel<HD, TREE, FP8><<<blocks, FP8 ? 512 : 384, amk::AttnSmem<HD, FP8>::kBytes, st>>>(p, k, v);
+  amk::attn_kernel<HD, TREE, FP8><<<blocks, FP8 ? 768 : 640, amk::AttnSmem<HD, FP8>::kBytes, st>>>(p, k, v);
   return cudaGetLastError();
 }
 
@@ -79,7 +79,7 @@ cudaError_t launch_join(const AttnParams& p, unsigned blocks, cudaStream_t st) {
   at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at.val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(p.rows * p.rep + 7) / 8, (unsigned)p.nkv, (unsigned)p.n_seqs);
+  cfg.gridDim = dim3((unsigned)(p.rows * p.rep * (HD / 16) + 255) / 256, (unsigned)p.nkv, (unsigned)p.n_seqs);
   cfg.blockDim = dim3(256);
   cfg.stream = st;
   cfg.attrs = &at;

@@ -121,17 +121,18 @@ namespace amk {
 // Tiles of 64 elements x 128 rows of 128 bytes, swizzled by TMA's 128-byte pattern: the 16-byte chunk c of row r lies
 // at r * 128 + ((c ^ (r & 7)) << 4).
 constexpr int kBox = 64 * kTile * 2;
+constexpr int kHeadBytes = 4096;
 template <int HD, bool FP8>
 struct AttnSmem {
   static constexpr int kTileBytes = HD / 64 * kBox;                // one bf16 tile of 128 rows
-  static constexpr int kStages = FP8 ? (HD == 128 ? 3 : 6) : (HD == 128 ? 5 : 10);
+  static constexpr int kStages = FP8 ? (HD == 128 ? 3 : 6) : (HD == 128 ? 4 : 8);
   static constexpr int kRawBytes = FP8 ? HD * kTile : 0;           // one 8-bit tile
-  static constexpr int kRawStages = FP8 ? (HD == 128 ? 4 : 8) : 0;
+  static constexpr int kRawStages = FP8 ? (HD == 128 ? 3 : 6) : 0;
   static constexpr int kQ = 0;
   static constexpr int kRing = 2 * kTileBytes;
   static constexpr int kRaw = kRing + kStages * kTileBytes;
   static constexpr int kHead = kRaw + kRawStages * kRawBytes;      // AttnHead
-  static constexpr int kBytes = kHead + 2048 + 1024;               // + alignment of the dynamic buffer
+  static constexpr int kBytes = kHead + kHeadBytes + 1024;               // + alignment of the dynamic buffer
   static_assert(kBytes <= 227 * 1024, "shared memory of one SM");
 };
 struct AttnHead {
@@ -141,11 +142,12 @@ struct AttnHead {
   unsigned tmem;
   int dead;                            // a bounded wait ran out: nobody waits or issues any more
   int skip[2];                         // this step's P V was done by the warpgroup itself
-  float m[kTile], l[kTile];            // second warpgroup's statistics (both on the same rows)
+  float mx[2][2][kTile];               // [tile][half]: row maxima, and at the end row sums, of half the columns
+  float m[kTile], l[kTile];            // the second tile's statistics (both tiles of the same rows)
   int unit[8];
   int64_t walk[1];
 };
-static_assert(sizeof(AttnHead) <= 2048, "head");
+static_assert(sizeof(AttnHead) <= kHeadBytes, "head");
 
 constexpr long long kWaitCycles = 4000000000ll;
 // Waits for the phase of the given parity, about two seconds at most (the SM's cycle counter: the global timer is read
@@ -164,10 +166,11 @@ __device__ __forceinline__ void attn_wait(uint64_t* bar, unsigned parity, AttnHe
     }
   }
 }
-__device__ __forceinline__ unsigned any_of_warpgroup(unsigned pred, int id) {
+// barrier ids: 1..8 a pair of warps (the two halves of 32 rows), 9, 10 a tile, 11 both tiles
+__device__ __forceinline__ unsigned any_of_tile(unsigned pred, int id) {
   unsigned r;
   asm volatile(
-      "{ .reg .pred p, q; setp.ne.u32 p, %1, 0; bar.red.or.pred q, %2, 128, p; selp.u32 %0, 1, 0, q; }"
+      "{ .reg .pred p, q; setp.ne.u32 p, %1, 0; bar.red.or.pred q, %2, 256, p; selp.u32 %0, 1, 0, q; }"
       : "=r"(r)
       : "r"(pred), "r"(id)
       : "memory");
@@ -192,7 +195,7 @@ struct Units<true> {
     if (left <= 0) return false;
     while (item == items || tiles == 0) {   // something is left: a sequence with tiles follows
       item = 0;
-      len = p.lens[++seq];
+      len = __ldg(p.lens + ++seq);
       tiles = tree_tiles(p, len);
     }
     const int run = left < tiles - within ? (int)left : tiles - within;
@@ -234,31 +237,43 @@ __device__ __forceinline__ int unit_steps(const AttnParams& p, const Unit& u, bo
   return (u.tok0 + div_rep(p, last)) / kTile + 1;
 }
 
-// 32 bits of a drafted token's mask from drafted index idx on (idx may be negative: bits below 0 are 0)
-__device__ __forceinline__ unsigned tree_bits32(const unsigned long long* w, int rows, int tok, int idx) {
+// 32 bits of a drafted token's mask from drafted index idx on (idx may be negative: bits below 0 are 0).  w0 is the
+// mask's first word, w its words; without a mask (w null) a chain: indices 0..tok.
+__device__ __forceinline__ unsigned tree_bits32(const unsigned long long* w, unsigned long long w0, int rows, int tok, int idx) {
   if (idx >= rows || idx <= -32) return 0;
-  if (!w) {   // a chain: indices 0..tok
-    const int n = tok + 1 - idx;   // bits below n
+  if (!w) {
+    const int n = tok + 1 - idx;      // bits below n
     unsigned r = n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u;
     if (idx < 0) r &= ~0u << -idx;
     return r;
   }
   unsigned long long v;
   if (idx < 0) {
-    v = w[0] << -idx;
+    v = w0 << -idx;
   } else {
     const int word = idx >> 6, off = idx & 63;
-    v = w[word] >> off;
+    v = (word ? w[word] : w0) >> off;
     if (off > 32 && (word + 1) * 64 < rows) v |= w[word + 1] << (64 - off);
   }
-  const int left = rows - idx;      // bits from the last drafted token on are nobody's
+  const int left = rows - idx;        // bits from the last drafted token on are nobody's
   return left >= 32 ? (unsigned)v : (unsigned)v & ((1u << left) - 1u);
 }
 
-// O += P V of one tile for this warp's rows, key by key and only for the keys that a row sees: for tiles with values
-// that are not finite behind a mask, where 0 * V would not be 0.
+// O += P V of 64 keys for this warp's rows, key by key and only for the keys that a row sees: for tiles with values that
+// are not finite behind a mask, where 0 * V would not be 0.  P in TMEM as the matrix unit would read it; vt: the tile, used
+// from its row `key` on.
 template <int HD>
-__device__ __noinline__ void product_by_key(const float* pl, const uint4 see, const unsigned char* vt, unsigned to, bool more) {
+__device__ __noinline__ void product_by_key(unsigned tp, unsigned see0, unsigned see1, const unsigned char* vt, int key,
+                                            unsigned to, bool more) {
+  float pl[64];                                        // (in local memory: walked by key)
+  {
+    unsigned r[32];
+    tmem_ld32(r, tp);
+    tmem_wait_ld();
+    tmem_pin(r);
+#pragma unroll
+    for (int k = 0; k < 32; k++) pl[2 * k] = bf16_lo(r[k]), pl[2 * k + 1] = bf16_hi(r[k]);
+  }
   for (int x = 0; x < HD; x += 32) {
     unsigned o[32];
     tmem_ld32(o, to + x);
@@ -267,13 +282,13 @@ __device__ __noinline__ void product_by_key(const float* pl, const uint4 see, co
     float a[32];
 #pragma unroll
     for (int k = 0; k < 32; k++) a[k] = more ? __uint_as_float(o[k]) : 0.f;
-    for (int k = 0; k < kTile; k++) {
-      const unsigned w = k < 64 ? (k < 32 ? see.x : see.y) : (k < 96 ? see.z : see.w);
-      if (!(w >> (k & 31) & 1)) continue;
+    for (int k = 0; k < 64; k++) {
+      if (!((k < 32 ? see0 : see1) >> (k & 31) & 1)) continue;
+      const int r = key + k;
 #pragma unroll
       for (int ch = 0; ch < 4; ch++) {
         const int cc = x / 8 + ch;
-        const uint4 v = *(const uint4*)(vt + cc / 8 * kBox + k * 128 + (((cc & 7) ^ (k & 7)) << 4));
+        const uint4 v = *(const uint4*)(vt + cc / 8 * kBox + r * 128 + (((cc & 7) ^ (r & 7)) << 4));
         const unsigned vv[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
         for (int e = 0; e < 4; e++) {
@@ -292,10 +307,10 @@ __device__ __noinline__ void product_by_key(const float* pl, const uint4 see, co
 
 // ---- the kernel -------------------------------------------------------------------------------------------------
 template <int HD, bool TREE, bool FP8>
-__global__ void __launch_bounds__(FP8 ? 512 : 384, 1)
+__global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
     attn_kernel(const AttnParams p, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
   using L = AttnSmem<HD, FP8>;
-  constexpr int kProducer = FP8 ? 12 : 8, kIssuer = kProducer + 1;
+  constexpr int kProducer = FP8 ? 20 : 16, kIssuer = kProducer + 1;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = (unsigned char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   AttnHead& h = *(AttnHead*)(smem + L::kHead);
@@ -370,8 +385,8 @@ __global__ void __launch_bounds__(FP8 ? 512 : 384, 1)
       for (int i = 0; i < L::kStages; i++) mbar_init(&h.full[i], FP8 ? 128 : 1), mbar_init(&h.empty[i], 1);
       for (int i = 0; i < L::kRawStages; i++) mbar_init(&h.raw_full[i], 1), mbar_init(&h.raw_empty[i], 128);
       for (int t = 0; t < 2; t++) {
-        mbar_init(&h.q_full[t], 128), mbar_init(&h.s_full[t], 1);
-        mbar_init(&h.p_full[t], 128), mbar_init(&h.o_done[t], 1);
+        mbar_init(&h.q_full[t], 256), mbar_init(&h.s_full[t], 1);
+        mbar_init(&h.p_full[t], 256), mbar_init(&h.o_done[t], 1);
       }
       mbar_init(&h.fin, 1);
       h.dead = 0;
@@ -382,7 +397,7 @@ __global__ void __launch_bounds__(FP8 ? 512 : 384, 1)
   __syncthreads();
   tc_fence_after();
   const unsigned tmem = h.tmem;
-  // TMEM columns: S0 (P0 over it), S1, O0, O1
+  // TMEM columns: S0, S1, O0, O1; P of keys 0..63 over S columns 0..31, of keys 64..127 over 64..95
   if (TREE) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
   Units<TREE> units;
@@ -390,118 +405,141 @@ __global__ void __launch_bounds__(FP8 ? 512 : 384, 1)
   Unit u;
 
   if (!FP8) {
-    // 384 threads of 168 registers at launch: 256 x 208 + 128 x 88 = 64512, all of them
-    if (warp < 8) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
-    else asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    // 640 threads of 96 registers at launch: 512 x 104 + 128 x 64 = 61440, all of them
+    if (warp < 16) asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
+    else asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
   } else {
-    // 512 threads of 128 registers at launch: 256 x 184 + 128 x 72 + 128 x 56 = 63488 of the 65536
-    if (warp < 8) asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
-    else if (warp < 12) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-    else asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    // 768 threads of 80 registers at launch: 512 x 96 + 128 x 56 + 128 x 40 = 61440, all of them
+    if (warp < 16) asm volatile("setmaxnreg.inc.sync.aligned.u32 96;");
+    else if (warp < 20) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    else asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
   }
 
-  if (warp < 8) {
-    // ================================ softmax: one warpgroup for each row tile, one thread for each row ================
-    const int t = warp >> 2, wt = threadIdx.x & 127;
-    const unsigned lanes = (unsigned)(warp & 3) * 32 << 16;
+  if (warp < 16) {
+    // ================================ softmax: two warpgroups for each row tile, half a row for each thread ============
+    const int t = warp >> 3, half = warp >> 2 & 1, quarter = warp & 3, wr = quarter * 32 + lane, id = threadIdx.x & 255;
+    const int pair_id = 1 + t * 4 + quarter, tile_id = 9 + t;
+    const unsigned lanes = (unsigned)quarter * 32 << 16;
     const unsigned ts = tmem + lanes + t * kTile, to = tmem + lanes + 2 * kTile + t * HD;
     unsigned char* qs = smem + L::kQ + t * L::kTileBytes;
     const float c = p.scale * kLog2e;
     unsigned s_phase = 0, o_phase = 0;
     int ring = 0;                                     // ring position of the unit's first tile
+    bool again = false;
     while (units.next(p, h, u)) {
       const int steps = unit_steps<TREE>(p, u, dual, t);
       const int row_first = u.row0 + (dual ? 0 : t * kTile);                       // first row of this tile
       const int rows_here = dual ? u.n_rows : u.n_rows - t * kTile;                // may be <= 0
+      const unsigned short* q = p.q + (int64_t)u.seq * p.q_seq + (int64_t)(u.key0 + u.tok0) * p.q_row +
+                                (int64_t)u.head * p.rep * p.q_head;
+      const int row = row_first + wr, tok = div_rep(p, row), hh = row - tok * p.rep;
+      const bool valid = wr < rows_here;
+      const bool live = quarter * 32 < rows_here;      // this warp has rows; the others only keep step
+      if (again && steps) named_barrier(tile_id, 256); // the last unit's output has left the tile's shared memory
+      again = true;
+      const unsigned long long* words = nullptr;
+      unsigned long long word0 = 0;
       if (steps) {
-        // Q, 16 bytes at a time; rows that do not exist are zero
-        constexpr int kChunks = HD / 8;
-        const unsigned short* q = p.q + (int64_t)u.seq * p.q_seq + (int64_t)(u.key0 + u.tok0) * p.q_row +
-                                  (int64_t)u.head * p.rep * p.q_head;
+        // Q, 16 bytes at a time, all loads in flight before the first store; rows that do not exist are zero
+        constexpr int kChunks = HD / 8, kEach = kTile * kChunks / 256;
+        uint4 v[kEach];
 #pragma unroll
-        for (int i0 = 0; i0 < kChunks; i0 += 8) {        // eight loads in flight before the first store
-          uint4 v[8];
-#pragma unroll
-          for (int i = 0; i < 8; i++) {
-            const int e = (i0 + i) * kTile + wt, r = e / kChunks, ch = e % kChunks;
-            v[i] = make_uint4(0, 0, 0, 0);
-            if (r < rows_here) {
-              const int row = row_first + r, tok = div_rep(p, row), hh = row - tok * p.rep;
-              v[i] = __ldg((const uint4*)(q + tok * p.q_row + hh * p.q_head + ch * 8));
-            }
+        for (int i = 0; i < kEach; i++) {
+          const int e = i * 256 + id, r = e / kChunks, ch = e % kChunks;
+          v[i] = make_uint4(0, 0, 0, 0);
+          if (r < rows_here) {
+            const int row = row_first + r, tok = div_rep(p, row), hh = row - tok * p.rep;
+            v[i] = __ldg((const uint4*)(q + tok * p.q_row + hh * p.q_head + ch * 8));
           }
+        }
+        if (TREE && p.mask) {
+          words = p.mask + ((int64_t)u.seq * p.rows + min(tok, p.rows - 1)) * ((p.rows + 63) / 64);
+          word0 = __ldg(words);
+        }
 #pragma unroll
-          for (int i = 0; i < 8; i++) {
-            const int e = (i0 + i) * kTile + wt, r = e / kChunks, ch = e % kChunks;
-            *(uint4*)(qs + ch / 8 * kBox + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) = v[i];
-          }
+        for (int i = 0; i < kEach; i++) {
+          const int e = i * 256 + id, r = e / kChunks, ch = e % kChunks;
+          *(uint4*)(qs + ch / 8 * kBox + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) = v[i];
         }
         fence_async_smem();
         mbar_arrive(&h.q_full[t]);
       }
-      const int row = row_first + wt, tok = div_rep(p, row), hh = row - tok * p.rep;
-      const bool valid = wt < rows_here;
-      const bool live = (wt & ~31) < rows_here;        // this warp has rows; the others only keep step
-      const unsigned long long* words = nullptr;
-      if (TREE && p.mask && valid) words = p.mask + ((int64_t)u.seq * p.rows + tok) * ((p.rows + 63) / 64);
-      const int key_end = TREE ? u.len + p.rows : u.tok0 + u.n_tok;    // keys nobody here sees: from it on
+      if (TREE) {
+        // the next unit's Q into L2: behind the stream of tiles a load from HBM takes microseconds
+        Units<TREE> ahead = units;
+        Unit n;
+        if (ahead.next(p, h, n)) {
+          const int r = id >> 1, first = n.row0 + (dual ? 0 : t * kTile);
+          if (r < (dual ? n.n_rows : n.n_rows - t * kTile)) {
+            const int row = first + r, tok = div_rep(p, row), hh = row - tok * p.rep;
+            const unsigned short* a = p.q + (int64_t)n.seq * p.q_seq + (int64_t)n.head * p.rep * p.q_head + tok * p.q_row +
+                                      hh * p.q_head + (id & 1) * (HD / 2);
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(a));
+          }
+        }
+      }
+      const int key_end = TREE ? u.len + p.rows : u.tok0 + u.n_tok;                // keys nobody here sees: from it on
       // first key that a row of this tile may not see
       const int all_see = TREE ? u.len : u.tok0 + div_rep(p, row_first) + 1;
       float m = -CUDART_INF_F, l = 0.f;
       for (int i = 0; i < steps; i++) {
         const int rel = dual ? 2 * i + t : i;
         const int key = (u.tile_begin + rel) * kTile;
+        const bool masked = key + kTile > all_see;
         attn_wait(&h.s_full[t], s_phase & 1, h);
         s_phase++;
         __syncwarp();
         tc_fence_after();
-        unsigned sb[4][32];
-        unsigned see[4] = {~0u, ~0u, ~0u, ~0u};
-#define AMK_S(k) __uint_as_float(sb[(k) >> 5][(k) & 31])
-        const bool masked = key + kTile > all_see;
+        // S is read from TMEM twice, for the maximum and for the exponentials: it costs less than the registers that would
+        // keep it, and spilled registers would travel behind the stream of tiles.
+        unsigned see[2] = {~0u, ~0u};
         if (live) {
-#pragma unroll
-          for (int k = 0; k < 4; k++) tmem_ld32(sb[k], ts + 32 * k);
-          tmem_wait_ld();
-#pragma unroll
-          for (int k = 0; k < 4; k++) tmem_pin(sb[k]);
           if (masked) {
 #pragma unroll
-            for (int w = 0; w < 4; w++) {
-              const int first = key + 32 * w;
+            for (int w = 0; w < 2; w++) {
+              const int first = key + half * 64 + 32 * w;
               if (TREE) {
-                const int ctx = u.len - first;                  // context keys from `first` on
-                if (ctx < 32)
-                  see[w] = (ctx > 0 ? (1u << ctx) - 1u : 0u) |
-                           tree_bits32(words, p.mask ? (words ? p.rows : 0) : p.rows, tok, -ctx);
+                const int ctx = u.len - first;                      // context keys from `first` on
+                if (ctx < 32) see[w] = (ctx > 0 ? (1u << ctx) - 1u : 0u) | tree_bits32(words, word0, p.rows, tok, -ctx);
               } else {
                 const int n = u.tok0 + tok + 1 - first;
                 see[w] = n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u;
               }
             }
-#pragma unroll
-            for (int k = 0; k < kTile; k++)
-              if (!(see[k >> 5] >> (k & 31) & 1)) sb[k >> 5][k & 31] = 0xff800000u;   // -infinity
           }
-          float mx[4];
+          float top = -CUDART_INF_F;
 #pragma unroll
-          for (int k = 0; k < 4; k++) mx[k] = AMK_S(32 * k);
+          for (int x = 0; x < 2; x++) {
+            unsigned w[32];
+            tmem_ld32(w, ts + half * 64 + x * 32);
+            tmem_wait_ld();
+            tmem_pin(w);
+            if (masked) {
 #pragma unroll
-          for (int j = 1; j < 31; j += 2)
+              for (int k = 0; k < 32; k++)
+                if (!(see[x] >> k & 1)) w[k] = 0xff800000u;          // -infinity
+            }
+            float mx[4];
 #pragma unroll
-            for (int k = 0; k < 4; k++) mx[k] = max3(mx[k], AMK_S(32 * k + j), AMK_S(32 * k + j + 1));
+            for (int k = 0; k < 4; k++) mx[k] = fmaxf(__uint_as_float(w[8 * k]), __uint_as_float(w[8 * k + 1]));
 #pragma unroll
-          for (int k = 0; k < 4; k++) mx[k] = fmaxf(mx[k], AMK_S(32 * k + 31));
-          mx[0] = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]);
+            for (int j = 2; j < 8; j += 2)
+#pragma unroll
+              for (int k = 0; k < 4; k++) mx[k] = max3(mx[k], __uint_as_float(w[8 * k + j]), __uint_as_float(w[8 * k + j + 1]));
+            top = max3(top, max3(mx[0], mx[1], mx[2]), mx[3]);
+          }
+          h.mx[t][half][wr] = top;
+          named_barrier(pair_id, 64);
+          top = fmaxf(top, h.mx[t][half ^ 1][wr]);
           if (i == 0) {
-            m = mx[0];
+            m = top;
           } else {
-            const bool need = mx[0] > m && (mx[0] - m) * c > 8.f;
-            if (__any_sync(~0u, need)) {
-              const float mn = fmaxf(m, mx[0]);
+            const bool need = top > m && (top - m) * c > 8.f;
+            if (__any_sync(~0u, need)) {              // the same in both halves
+              const float mn = fmaxf(m, top);
               const float f = m == mn ? 1.f : exp2_fast((m - mn) * c);
-#pragma unroll
-              for (int x = 0; x < HD; x += 32) {
+#pragma unroll 1
+              for (int x = half * (HD / 2); x < (half + 1) * (HD / 2); x += 32) {
                 unsigned o[32];
                 tmem_ld32(o, to + x);
                 tmem_wait_ld();
@@ -518,23 +556,29 @@ __global__ void __launch_bounds__(FP8 ? 512 : 384, 1)
           const uint64_t c2 = pair(c, c), mc2 = pair(mc, mc);
           uint64_t sum[2] = {0, 0};
 #pragma unroll
-          for (int k = 0; k < kTile; k += 2) {
-            float e0, e1;
-            unpair(e0, e1, fma2(pair(AMK_S(k), AMK_S(k + 1)), c2, mc2));
-            e0 = exp2_fast(e0), e1 = exp2_fast(e1);
-            sb[k >> 5][k & 31] = __float_as_uint(e0), sb[k >> 5][(k & 31) + 1] = __float_as_uint(e1);
-            sum[k >> 1 & 1] = add2(sum[k >> 1 & 1], pair(e0, e1));
+          for (int x = 0; x < 2; x++) {
+            unsigned w[32], r[16];
+            tmem_ld32(w, ts + half * 64 + x * 32);
+            tmem_wait_ld();
+            tmem_pin(w);
+            if (masked) {
+#pragma unroll
+              for (int k = 0; k < 32; k++)
+                if (!(see[x] >> k & 1)) w[k] = 0xff800000u;
+            }
+#pragma unroll
+            for (int k = 0; k < 32; k += 2) {
+              float e0, e1;
+              unpair(e0, e1, fma2(pair(__uint_as_float(w[k]), __uint_as_float(w[k + 1])), c2, mc2));
+              e0 = exp2_fast(e0), e1 = exp2_fast(e1);
+              sum[k >> 1 & 1] = add2(sum[k >> 1 & 1], pair(e0, e1));
+              r[k / 2] = pack_bf16(e0, e1);
+            }
+            tmem_st16(ts + half * 64 + x * 16, r);    // over S columns of its own that it has read
           }
           float s0, s1;
           unpair(s0, s1, add2(sum[0], sum[1]));
           l += s0 + s1;
-#pragma unroll
-          for (int x = 0; x < 2; x++) {
-            unsigned r[32];
-#pragma unroll
-            for (int k = 0; k < 32; k++) r[k] = pack_bf16(AMK_S(x * 64 + 2 * k), AMK_S(x * 64 + 2 * k + 1));
-            tmem_st32(ts + x * 32, r);
-          }
         }
         unsigned slow = 0;
         if (masked) {
@@ -543,33 +587,34 @@ __global__ void __launch_bounds__(FP8 ? 512 : 384, 1)
           const int pos = ring + 2 * rel + 1, st = pos % L::kStages;
           attn_wait(&h.full[st], pos / L::kStages & 1, h);
           unsigned char* vt = smem + L::kRing + st * L::kTileBytes;
-          unsigned char* vr = vt + wt * 128;
+          const int r = id & 127;
           unsigned broken = 0;                         // becomes NaN (two bf16)
-          if (key + wt >= key_end) {
 #pragma unroll
-            for (int ch = 0; ch < HD / 8; ch++) *(uint4*)(vr + ch / 8 * kBox + ((ch & 7) << 4)) = make_uint4(0, 0, 0, 0);
-            fence_async_smem();
-          } else {
-#pragma unroll
-            for (int ch = 0; ch < HD / 8; ch++) {
-              const uint4 v = *(const uint4*)(vr + ch / 8 * kBox + (((ch & 7) ^ (wt & 7)) << 4));
+          for (int j = 0; j < HD / 16; j++) {
+            const int ch = (id >> 7) * (HD / 16) + j;
+            uint4* at = (uint4*)(vt + ch / 8 * kBox + r * 128 + (((ch & 7) ^ (r & 7)) << 4));
+            if (key + r >= key_end) {
+              *at = make_uint4(0, 0, 0, 0);
+            } else {
+              const uint4 v = *at;
               broken = zero_times(v.w, zero_times(v.z, zero_times(v.y, zero_times(v.x, broken))));
             }
           }
-          slow = any_of_warpgroup((broken & 0x7fff7fffu) != 0, 1 + t);
+          fence_async_smem();
+          slow = any_of_tile((broken & 0x7fff7fffu) != 0, tile_id);
           if (slow && live) {
-            float pl[kTile];                           // (in local memory: the function walks it)
-#pragma unroll
-            for (int k = 0; k < kTile; k++) pl[k] = AMK_S(k);
-            const uint4 sl = make_uint4(see[0], see[1], see[2], see[3]);
-            product_by_key<HD>(pl, sl, vt, to, i > 0);
+            tmem_wait_st();
+            if (half == 0) product_by_key<HD>(ts, see[0], see[1], vt, 0, to, i > 0);
+            tc_fence_before();
+            named_barrier(pair_id, 64);
+            tc_fence_after();
+            if (half == 1) product_by_key<HD>(ts + 64, see[0], see[1], vt, 64, to, true);
           }
         }
         tmem_wait_st();
         tc_fence_before();
-        if (wt == 0) h.skip[t] = slow;
+        if (id == 0) h.skip[t] = slow;
         mbar_arrive(&h.p_full[t]);
-#undef AMK_S
       }
       ring += 2 * (u.tile_end - u.tile_begin);
       if (steps) {
@@ -577,22 +622,27 @@ __global__ void __launch_bounds__(FP8 ? 512 : 384, 1)
         o_phase++;
         __syncwarp();
         tc_fence_after();
+        if (live) {                                    // the row's sum: both halves'
+          h.mx[t][half][wr] = l;
+          named_barrier(pair_id, 64);
+          l += h.mx[t][half ^ 1][wr];
+          named_barrier(pair_id, 64);                  // (the next unit writes there)
+        }
       }
 
       // O / l, or this block's part of it
       float f0 = 1.f, f1 = 0.f;
       bool two = false;
-      unsigned from0 = to, from1 = to;
       if (dual) {
         if (t == 1) {
-          h.m[wt] = m, h.l[wt] = l;
+          if (half == 0) h.m[wr] = m, h.l[wr] = l;
           tc_fence_before();
         }
-        named_barrier(3, 256);
+        named_barrier(11, 512);
         if (t == 0) {
           tc_fence_after();
           two = u.tile_end - u.tile_begin > 1;
-          const float m1 = h.m[wt], l1 = h.l[wt];
+          const float m1 = h.m[wr], l1 = h.l[wr];
           const float mn = fmaxf(m, m1);
           if (two && mn != -CUDART_INF_F) {
             f0 = m == mn ? 1.f : exp2_fast((m - mn) * c);
@@ -600,56 +650,73 @@ __global__ void __launch_bounds__(FP8 ? 512 : 384, 1)
             l = l * f0 + l1 * f1;
             m = mn;
           }
-          from1 = to + HD;
         }
       }
       if (steps && live && !(dual && t == 1)) {
         const bool whole = !TREE || (u.tile_begin == 0 && u.tile_end == u.item_tiles);
         const float inv = l == 0.f ? 0.f : 1.f / l;
         const float lse2 = l == 0.f ? -CUDART_INF_F : m * c + log2f(l);
-        const int64_t gtok = TREE ? (int64_t)u.seq * p.rows + tok : (int64_t)u.key0 + u.tok0 + tok;
-        const int head = u.head * p.rep + hh;
-        __nv_bfloat16* out = p.out + (TREE ? (int64_t)u.seq * p.o_seq + tok * p.o_row : gtok * p.o_row) + head * p.o_head;
-        const int64_t slot = TREE ? ((int64_t)2 * blockIdx.x + (u.tile_begin == 0 ? 1 : 0)) * p.part_rows + wt + (dual ? 0 : t * kTile) : 0;
-        float* part = TREE ? p.part_o + slot * HD : nullptr;
-#pragma unroll
-        for (int x = 0; x < HD; x += 32) {
+        const int64_t slot = TREE ? (int64_t)2 * blockIdx.x + (u.tile_begin == 0 ? 1 : 0) : 0;
+        const int part_row = wr + (dual ? 0 : t * kTile);
+#pragma unroll 1
+        for (int x = half * (HD / 2); x < (half + 1) * (HD / 2); x += 32) {
           unsigned o[32];
-          tmem_ld32(o, from0 + x);
+          float v[32];
+          tmem_ld32(o, to + x);
           tmem_wait_ld();
           tmem_pin(o);
-          float v[32];
 #pragma unroll
           for (int k = 0; k < 32; k++) v[k] = __uint_as_float(o[k]) * f0;
           if (two) {
-            tmem_ld32(o, from1 + x);
+            tmem_ld32(o, to + HD + x);
             tmem_wait_ld();
             tmem_pin(o);
 #pragma unroll
             for (int k = 0; k < 32; k++) v[k] += __uint_as_float(o[k]) * f1;
           }
-          if (valid) {
 #pragma unroll
-            for (int k = 0; k < 32; k++) v[k] = l == 0.f ? 0.f : v[k] * inv;
-            if (whole) {
+          for (int k = 0; k < 32; k++) v[k] = l == 0.f ? 0.f : v[k] * inv;
+          if (whole) {
+            // over the tile's Q, 16-byte chunks permuted within a row so that neither side meets a bank twice
 #pragma unroll
-              for (int k = 0; k < 32; k += 8)
-                *(uint4*)(out + x + k) = make_uint4(pack_bf16(v[k], v[k + 1]), pack_bf16(v[k + 2], v[k + 3]),
-                                                    pack_bf16(v[k + 4], v[k + 5]), pack_bf16(v[k + 6], v[k + 7]));
-            } else {
+            for (int k = 0; k < 32; k += 8)
+              *(uint4*)(qs + wr * (HD * 2) + (((x + k) / 8 ^ (wr & 7)) << 4)) =
+                  make_uint4(pack_bf16(v[k], v[k + 1]), pack_bf16(v[k + 2], v[k + 3]), pack_bf16(v[k + 4], v[k + 5]),
+                             pack_bf16(v[k + 6], v[k + 7]));
+          } else if (valid) {
+            // [slot][column / 4][row][4]: a warp's rows lie side by side
+            float* part = p.part_o + ((slot * (HD / 4) + x / 4) * p.part_rows + part_row) * 4;
 #pragma unroll
-              for (int k = 0; k < 32; k += 4) *(float4*)(part + x + k) = make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
+            for (int k = 0; k < 32; k += 4) *(float4*)(part + (int64_t)k * p.part_rows) = make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
+          }
+        }
+        if (whole) {
+          named_barrier(pair_id, 64);
+          constexpr int kChunks = HD / 8;
+          __nv_bfloat16* out = p.out + (int64_t)u.seq * p.o_seq + (int64_t)(u.key0 + u.tok0) * p.o_row +
+                               (int64_t)u.head * p.rep * p.o_head;
+#pragma unroll
+          for (int i = 0; i < 32 * kChunks / 64; i++) {
+            const int e = i * 64 + half * 32 + lane, r = quarter * 32 + e / kChunks, ch = e % kChunks;
+            if (r < rows_here) {
+              const int row = row_first + r, tok = div_rep(p, row), hh = row - tok * p.rep;
+              *(uint4*)(out + tok * p.o_row + hh * p.o_head + ch * 8) =
+                  *(const uint4*)(qs + r * (HD * 2) + ((ch ^ (r & 7)) << 4));
             }
           }
         }
-        if (valid) {
-          if (!whole) p.part_lse[slot] = lse2;
-          else if (p.lse) p.lse[gtok * p.nq + head] = lse2 * 0.6931471805599453f;
+        if (valid && half == 0) {
+          if (!whole) {
+            p.part_lse[slot * p.part_rows + part_row] = lse2;
+          } else if (p.lse) {
+            const int64_t gtok = TREE ? (int64_t)u.seq * p.rows + tok : (int64_t)u.key0 + u.tok0 + tok;
+            p.lse[gtok * p.nq + u.head * p.rep + hh] = lse2 * 0.6931471805599453f;
+          }
         }
       }
       if (dual) {
         tc_fence_before();
-        named_barrier(3, 256);       // the second warpgroup's O and statistics have been read
+        named_barrier(11, 512);      // the second tile's O and statistics have been read
         tc_fence_after();
       }
     }
@@ -660,11 +727,16 @@ __global__ void __launch_bounds__(FP8 ? 512 : 384, 1)
       uint64_t* full = FP8 ? h.raw_full : h.full;
       uint64_t* empty = FP8 ? h.raw_empty : h.empty;
       unsigned issued = 0;
-      bool on = true;
+      bool on = true, gate = TREE;
       while (units.next(p, h, u)) {
         for (int j = u.tile_begin; j < u.tile_end; j++) {
           for (int kv = 0; kv < 2; kv++) {
             const int st = issued % kN;
+            if (gate && issued == 2) {   // the first Q is not to queue behind the whole ring
+              gate = false;
+              for (int t = 0; t < 2; t++)
+                if (unit_steps<TREE>(p, u, dual, t)) attn_wait(&h.q_full[t], 0, h);
+            }
             attn_wait(&empty[st], (issued / kN & 1) ^ 1, h);
             on = on && !*(volatile int*)&h.dead;
             if (!on) continue;
@@ -729,7 +801,7 @@ __global__ void __launch_bounds__(FP8 ? 512 : 384, 1)
                 const unsigned va = ring0 + st * L::kTileBytes;
 #pragma unroll
                 for (int k = 0; k < kTile / 16; k++)
-                  mma_ts(tmem + 2 * kTile + t * HD, tmem + t * kTile + k * 8, smem_desc(va + k * 2048, kBox, 1024), kIdO,
+                  mma_ts(tmem + 2 * kTile + t * HD, tmem + t * kTile + k / 4 * 64 + k % 4 * 8, smem_desc(va + k * 2048, kBox, 1024), kIdO,
                          i > 0 || k > 0);
               }
               if (i + 1 == n) mma_commit(&h.o_done[t]);
@@ -746,7 +818,7 @@ __global__ void __launch_bounds__(FP8 ? 512 : 384, 1)
       }
     }
     __syncwarp();
-  } else if (FP8 && warp >= 8 && warp < 12) {
+  } else if (FP8 && warp >= 16 && warp < 20) {
     // ================================ 8-bit tiles widened to bf16 ======================================================
     const int wt = threadIdx.x & 127;
     constexpr int kChunks = HD / 16;                  // 16-byte chunks of an 8-bit row
@@ -792,14 +864,15 @@ __global__ void __launch_bounds__(FP8 ? 512 : 384, 1)
 }
 
 // ---- parts of one item joined (tree) ----------------------------------------------------------------------------
-// One warp for each (row of an item); items whose tiles one block had are complete already, sequences of a bad length
-// become NaN.  O = sum_i w_i O_i / sum_i w_i, w_i = 2^(lse_i - max): the parts carry O_i / l_i and log2 of their sums.
+// Items whose tiles one block had are complete already; sequences of a bad length become NaN.
+//   O = sum_i w_i O_i / sum_i w_i,  w_i = 2^(lse_i - max): the parts carry O_i / l_i and log2 of their sums.
+// One thread for 16 columns of a row, neighbouring threads neighbouring rows.
 template <int HD>
 __global__ void __launch_bounds__(256) attn_join_kernel(const AttnParams p, int blocks) {
+  constexpr int kGroups = HD / 16, kRows = 256 / kGroups;
   __shared__ int64_t sh[2];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int head = blockIdx.y, seq = blockIdx.z;
-  asm volatile("griddepcontrol.wait;" ::: "memory");
   const int tiles = tree_tiles(p, p.lens[seq]);
   if (warp == 0) {
     int64_t before = 0;
@@ -810,53 +883,47 @@ __global__ void __launch_bounds__(256) attn_join_kernel(const AttnParams p, int 
     if (lane == 0) sh[0] = before * p.nkv * p.row_tiles, sh[1] = tree_per_block(p, total, blocks);
   }
   __syncthreads();
-  const int rows = p.rows * p.rep;
-  const int row = blockIdx.x * 8 + warp;
-  if (row >= rows) return;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int row = blockIdx.x * kRows + threadIdx.x % kRows, col = threadIdx.x / kRows * 16;
+  if (row >= p.rows * p.rep) return;
   const int tok = div_rep(p, row), q_head = head * p.rep + row - tok * p.rep;
-  __nv_bfloat16* out = p.out + (int64_t)seq * p.o_seq + tok * p.o_row + q_head * p.o_head;
-  float* lse = p.lse ? p.lse + ((int64_t)seq * p.rows + tok) * p.nq + q_head : nullptr;
-  constexpr int kEach = HD / 32;
-  float v[kEach] = {};
+  float v[16] = {};
+  float lse = CUDART_NAN_F;
   if (tiles == 0) {
 #pragma unroll
-    for (int k = 0; k < kEach; k++) v[k] = CUDART_NAN_F;
-    if (lse && lane == 0) *lse = CUDART_NAN_F;
+    for (int k = 0; k < 16; k++) v[k] = CUDART_NAN_F;
   } else {
     const int rt = row / p.part_rows;
     const int64_t first = sh[0] + ((int64_t)head * p.row_tiles + rt) * tiles, per = sh[1];
     const int c0 = (int)(first / per), c1 = (int)((first + tiles - 1) / per);
     if (c0 == c1) return;
-    const int64_t local = row - rt * p.part_rows;
-    auto slot = [&](int b) { return ((int64_t)2 * b + (b == c0 ? 1 : 0)) * p.part_rows + local; };
-    float m = -CUDART_INF_F;
-    bool nan = false;
-    for (int b = c0 + lane; b <= c1; b += 32) {
-      const float x = p.part_lse[slot(b)];
-      nan |= x != x;
-      m = fmaxf(m, x);
-    }
-#pragma unroll
-    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
-    float sum = 0.f;
+    const int local = row - rt * p.part_rows;
+    auto slot = [&](int b) { return (int64_t)2 * b + (b == c0 ? 1 : 0); };
+    float m = -CUDART_INF_F, sum = 0.f;
+    for (int b = c0; b <= c1; b++) m = fmaxf(m, p.part_lse[slot(b) * p.part_rows + local]);
+#pragma unroll 2
     for (int b = c0; b <= c1; b++) {
-      const float w = m == -CUDART_INF_F ? 0.f : exp2f(p.part_lse[slot(b)] - m);
+      const float x = p.part_lse[slot(b) * p.part_rows + local];
+      const float w = x == -CUDART_INF_F ? 0.f : exp2f(x - m);    // (all -infinity: nothing was seen)
       sum += w;
-      const float* o = p.part_o + slot(b) * HD + lane * kEach;
-      float x[kEach];
-      if (kEach == 4) *(float4*)x = *(const float4*)o;
-      else *(float2*)x = *(const float2*)o;
+      const float* o = p.part_o + ((slot(b) * (HD / 4) + col / 4) * p.part_rows + local) * 4;
 #pragma unroll
-      for (int k = 0; k < kEach; k++) v[k] += w * x[k];
+      for (int k = 0; k < 16; k += 4) {
+        const float4 y = *(const float4*)(o + (int64_t)k * p.part_rows);
+        v[k] += w * y.x, v[k + 1] += w * y.y, v[k + 2] += w * y.z, v[k + 3] += w * y.w;
+      }
     }
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
-    for (int k = 0; k < kEach; k++) v[k] *= inv;
-    if (__any_sync(~0u, nan)) m = CUDART_NAN_F;
-    if (lse && lane == 0) *lse = sum == 0.f ? (m == m ? -CUDART_INF_F : m) : (m + log2f(sum)) * 0.6931471805599453f;
+    for (int k = 0; k < 16; k++) v[k] *= inv;
+    lse = sum == 0.f ? -CUDART_INF_F : (m + log2f(sum)) * 0.6931471805599453f;
   }
-  if (kEach == 4) *(uint2*)(out + lane * 4) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[kEach - 2], v[kEach - 1]));
-  else *(unsigned*)(out + lane * 2) = pack_bf16(v[0], v[1]);
+  __nv_bfloat16* out = p.out + (int64_t)seq * p.o_seq + tok * p.o_row + q_head * p.o_head + col;
+#pragma unroll
+  for (int k = 0; k < 16; k += 8)
+    *(uint4*)(out + k) = make_uint4(pack_bf16(v[k], v[k + 1]), pack_bf16(v[k + 2], v[k + 3]), pack_bf16(v[k + 4], v[k + 5]),
+                                    pack_bf16(v[k + 6], v[k + 7]));
+  if (p.lse && col == 0) p.lse[((int64_t)seq * p.rows + tok) * p.nq + q_head] = lse;
 }
 
 }  // namespace amk
