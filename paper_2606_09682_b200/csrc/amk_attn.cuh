@@ -33,6 +33,7 @@ struct AttnParams {
   float scale;
 };
 
+constexpr int kPoly = 1, kPolyOf = 4;   // of kPolyOf pairs of exponentials so many are made by exp2_poly
 constexpr int kTile = 128;         // rows of a Q tile, keys of a K/V tile
 // row / rep, exact for rows below 2^28
 __device__ __forceinline__ int div_rep(const AttnParams& p, int row) {
@@ -54,9 +55,21 @@ __device__ __forceinline__ unsigned pack_bf16(float lo, float hi) {   // round t
   return r;
 }
 
+// The same value in every lane, and the compiler knows it: addresses that follow from it stay in uniform registers,
+// where the matrix instructions want them.
+template <class T>
+__device__ __forceinline__ T uniform(T x) {
+  return (T)__shfl_sync(~0u, (int)x, 0);
+}
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+// the same, but NaN if one of them is
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
 // two fp32 lanes in one instruction
@@ -77,6 +90,29 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   uint64_t d;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
+}
+// 2^x of two values on the fma pipe, relative error 1e-7, for x in about [-126, 127]; below, 2^-126 (no matter to any sum).
+// x = n + f with f in [-1/2, 1/2]: adding 1.5 * 2^23 leaves n in the low bits, 2^f is the polynomial of degree 5 whose
+// largest relative error is least (Remez exchange, 7.5e-8), n goes into the exponent.  The exponential unit makes
+// 4 values a cycle and scheduler, which is what a tile's softmax waits for; a share of them is made here beside it.
+__device__ __forceinline__ void exp2_poly(float& e0, float& e1, uint64_t x) {
+  float x0, x1;
+  unpair(x0, x1, x);
+  x = pair(fmaxf(x0, -126.f), fmaxf(x1, -126.f));
+  constexpr float kShift = 12582912.f;
+  const uint64_t t = add2(x, pair(kShift, kShift));
+  const uint64_t f = add2(x, add2(pair(kShift, kShift), t ^ 0x8000000080000000ull));   // x - (t - shift)
+  uint64_t y = pair(1.3276472e-3f, 1.3276472e-3f);
+  y = fma2(y, f, pair(9.6755413e-3f, 9.6755413e-3f));
+  y = fma2(y, f, pair(5.5507133e-2f, 5.5507133e-2f));
+  y = fma2(y, f, pair(2.4022120e-1f, 2.4022120e-1f));
+  y = fma2(y, f, pair(6.9314697e-1f, 6.9314697e-1f));
+  y = fma2(y, f, pair(1.f, 1.f));
+  float t0, t1, y0, y1;
+  unpair(t0, t1, t);
+  unpair(y0, y1, y);
+  e0 = __uint_as_float(__float_as_uint(y0) + (__float_as_uint(t0) << 23));
+  e1 = __uint_as_float(__float_as_uint(y1) + (__float_as_uint(t1) << 23));
 }
 // acc + 0 * w for two bf16 at once: NaN from the first value on that is not finite
 __device__ __forceinline__ unsigned zero_times(unsigned w, unsigned acc) {
@@ -150,21 +186,38 @@ struct AttnHead {
 static_assert(sizeof(AttnHead) <= kHeadBytes, "head");
 
 constexpr long long kWaitCycles = 4000000000ll;
-// Waits for the phase of the given parity, about two seconds at most (the SM's cycle counter: the global timer is read
-// through a unit that all SMs share).
-__device__ __forceinline__ void attn_wait(uint64_t* bar, unsigned parity, AttnHead& h) {
-  if (mbar_try_wait(bar, parity)) return;
+// A whole warp waits for the phase of the given parity, about two seconds at most (the SM's cycle counter: the global
+// timer is read through a unit that all SMs share); false if that ran out.  The votes keep the warp's control flow
+// uniform: behind a wait that each lane leaves by itself, the matrix instructions of one tile took ten times as long
+// to issue (700 cycles instead of 70).
+__device__ __forceinline__ bool attn_wait(uint64_t* bar, unsigned parity, AttnHead& h) {
+  if (__all_sync(~0u, mbar_try_wait(bar, parity))) return true;
   const long long t0 = clock64();
   for (;;) {
     for (int i = 0; i < 32; i++)
-      if (mbar_try_wait(bar, parity)) return;
-    if (*(volatile int*)&h.dead) return;
-    if (clock64() - t0 > kWaitCycles) {
+      if (__all_sync(~0u, mbar_try_wait(bar, parity))) return true;
+    if (__any_sync(~0u, *(volatile int*)&h.dead)) return false;
+    if (__any_sync(~0u, clock64() - t0 > kWaitCycles)) {
       *(volatile int*)&h.dead = 1;
       atomicExch(&g_attn_expired, 1u);
-      return;
+      return false;
     }
   }
+}
+// One arrival for the whole warp: 32 of them would queue up at the barrier's word.
+__device__ __forceinline__ void warp_arrive(uint64_t* bar, int lane) {
+  __syncwarp();
+  if (lane == 0) mbar_arrive(bar);
+}
+// whether a predicate holds in any thread of a pair of warps
+__device__ __forceinline__ bool any_of_pair(bool pred, int id) {
+  unsigned r;
+  asm volatile(
+      "{ .reg .pred p, q; setp.ne.u32 p, %1, 0; bar.red.or.pred q, %2, 64, p; selp.u32 %0, 1, 0, q; }"
+      : "=r"(r)
+      : "r"((unsigned)pred), "r"(id)
+      : "memory");
+  return r != 0;
 }
 // barrier ids: 1..8 a pair of warps (the two halves of 32 rows), 9, 10 a tile, 11 both tiles
 __device__ __forceinline__ unsigned any_of_tile(unsigned pred, int id) {
@@ -314,7 +367,7 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = (unsigned char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   AttnHead& h = *(AttnHead*)(smem + L::kHead);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   const bool dual = TREE && p.part_rows == kTile;
 
   if (warp == 0) {
@@ -382,11 +435,11 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
   if (warp == kIssuer) {
     tmem_alloc(&h.tmem, 512);
     if (lane == 0) {
-      for (int i = 0; i < L::kStages; i++) mbar_init(&h.full[i], FP8 ? 128 : 1), mbar_init(&h.empty[i], 1);
-      for (int i = 0; i < L::kRawStages; i++) mbar_init(&h.raw_full[i], 1), mbar_init(&h.raw_empty[i], 128);
+      for (int i = 0; i < L::kStages; i++) mbar_init(&h.full[i], FP8 ? 4 : 1), mbar_init(&h.empty[i], 1);
+      for (int i = 0; i < L::kRawStages; i++) mbar_init(&h.raw_full[i], 1), mbar_init(&h.raw_empty[i], 4);
       for (int t = 0; t < 2; t++) {
-        mbar_init(&h.q_full[t], 256), mbar_init(&h.s_full[t], 1);
-        mbar_init(&h.p_full[t], 256), mbar_init(&h.o_done[t], 1);
+        mbar_init(&h.q_full[t], 8), mbar_init(&h.s_full[t], 1);
+        mbar_init(&h.p_full[t], 8), mbar_init(&h.o_done[t], 1);
       }
       mbar_init(&h.fin, 1);
       h.dead = 0;
@@ -396,7 +449,7 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const unsigned tmem = h.tmem;
+  const unsigned tmem = uniform(h.tmem);
   // TMEM columns: S0, S1, O0, O1; P of keys 0..63 over S columns 0..31, of keys 64..127 over 64..95
   if (TREE) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
@@ -462,7 +515,7 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
           *(uint4*)(qs + ch / 8 * kBox + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) = v[i];
         }
         fence_async_smem();
-        mbar_arrive(&h.q_full[t]);
+        warp_arrive(&h.q_full[t], lane);
       }
       if (TREE) {
         // the next unit's Q into L2: behind the stream of tiles a load from HBM takes microseconds
@@ -490,10 +543,52 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
         s_phase++;
         __syncwarp();
         tc_fence_after();
-        // S is read from TMEM twice, for the maximum and for the exponentials: it costs less than the registers that would
-        // keep it, and spilled registers would travel behind the stream of tiles.
         unsigned see[2] = {~0u, ~0u};
-        if (live) {
+        bool exact = i == 0 || masked;
+        if (live && !exact) {
+          // The running maximum seldom rises by more than the 2^8 that P may grow to: P is made with the old one in one
+          // pass, and made again if it did.
+          const float mc = m == -CUDART_INF_F ? 0.f : -m * c;
+          const uint64_t c2 = pair(c, c), mc2 = pair(mc, mc);
+          uint64_t sum[2] = {0, 0};
+          unsigned r[32];
+          float top = -CUDART_INF_F;
+#pragma unroll
+          for (int x = 0; x < 2; x++) {
+            unsigned w[32];
+            tmem_ld32(w, ts + half * 64 + x * 32);
+            tmem_wait_ld();
+            tmem_pin(w);
+            float tops[2] = {-CUDART_INF_F, -CUDART_INF_F};
+#pragma unroll
+            for (int k = 0; k < 32; k += 2) {
+              const float a0 = __uint_as_float(w[k]), a1 = __uint_as_float(w[k + 1]);
+              tops[k >> 1 & 1] = max3_nan(tops[k >> 1 & 1], a0, a1);
+              const uint64_t z = fma2(pair(a0, a1), c2, mc2);
+              float e0, e1;
+              if ((k >> 1) % kPolyOf < kPoly) {
+                exp2_poly(e0, e1, z);
+              } else {
+                unpair(e0, e1, z);
+                e0 = exp2_fast(e0), e1 = exp2_fast(e1);
+              }
+              sum[k >> 1 & 1] = add2(sum[k >> 1 & 1], pair(e0, e1));
+              r[x * 16 + k / 2] = pack_bf16(e0, e1);
+            }
+            top = max3_nan(top, tops[0], tops[1]);
+          }
+          // (a NaN among the scores, or a first finite one, takes the careful way too)
+          exact = any_of_pair(!((top - m) * c <= 8.f), pair_id);
+          if (!exact) {
+            tmem_st32(ts + half * 64, r);
+            float s0, s1;
+            unpair(s0, s1, add2(sum[0], sum[1]));
+            l += s0 + s1;
+          }
+        }
+        // The careful way: maximum first.  S is read from TMEM twice: that costs less than the registers that would keep
+        // it, and spilled registers would travel behind the stream of tiles.
+        if (live && exact) {
           if (masked) {
 #pragma unroll
             for (int w = 0; w < 2; w++) {
@@ -613,8 +708,8 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
         }
         tmem_wait_st();
         tc_fence_before();
-        if (id == 0) h.skip[t] = slow;
-        mbar_arrive(&h.p_full[t]);
+        if (masked && id == 0) h.skip[t] = slow;
+        warp_arrive(&h.p_full[t], lane);
       }
       ring += 2 * (u.tile_end - u.tile_begin);
       if (steps) {
@@ -722,102 +817,111 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
     }
   } else if (warp == kProducer) {
     // ================================ K and V tiles into the ring ======================================================
-    if (lane == 0) {
-      constexpr int kN = FP8 ? L::kRawStages : L::kStages;
-      uint64_t* full = FP8 ? h.raw_full : h.full;
-      uint64_t* empty = FP8 ? h.raw_empty : h.empty;
-      unsigned issued = 0;
-      bool on = true, gate = TREE;
-      while (units.next(p, h, u)) {
-        for (int j = u.tile_begin; j < u.tile_end; j++) {
-          for (int kv = 0; kv < 2; kv++) {
-            const int st = issued % kN;
-            if (gate && issued == 2) {   // the first Q is not to queue behind the whole ring
-              gate = false;
-              for (int t = 0; t < 2; t++)
-                if (unit_steps<TREE>(p, u, dual, t)) attn_wait(&h.q_full[t], 0, h);
-            }
-            attn_wait(&empty[st], (issued / kN & 1) ^ 1, h);
-            on = on && !*(volatile int*)&h.dead;
-            if (!on) continue;
-            const CUtensorMap* map = kv ? &map_v : &map_k;
-            const int y = u.key0 + j * kTile;
-            if (FP8) {
-              mbar_expect_tx(&full[st], L::kRawBytes);
-              tma_load_4d(smem + L::kRaw + st * L::kRawBytes, map, 0, y, u.head, u.seq, &full[st]);
-            } else {
-              unsigned char* dst = smem + L::kRing + st * L::kTileBytes;
-              mbar_expect_tx(&full[st], L::kTileBytes);
-              for (int x = 0; x < HD / 64; x++) tma_load_4d(dst + x * kBox, map, x * 64, y, u.head, u.seq, &full[st]);
-            }
-            issued++;
+    constexpr int kN = FP8 ? L::kRawStages : L::kStages;
+    uint64_t* full = FP8 ? h.raw_full : h.full;
+    uint64_t* empty = FP8 ? h.raw_empty : h.empty;
+    const bool leader = elect_one();
+    unsigned issued = 0;
+    bool on = true, gate = TREE;
+    while (uniform(units.next(p, h, u))) {
+      const int tile_end = uniform(u.tile_end);
+      for (int j = uniform(u.tile_begin); j < tile_end; j++) {
+        for (int kv = 0; kv < 2; kv++) {
+          const int st = issued % kN;
+          if (gate && issued == 2) {   // the first Q is not to queue behind the whole ring
+            gate = false;
+            for (int t = 0; t < 2; t++)
+              if (unit_steps<TREE>(p, u, dual, t)) attn_wait(&h.q_full[t], 0, h);
           }
+          on = attn_wait(&empty[st], (issued / kN & 1) ^ 1, h) && on;
+          if (!on) continue;
+          const CUtensorMap* map = kv ? &map_v : &map_k;
+          const int y = uniform(u.key0) + j * kTile, z = uniform(u.head), w = uniform(u.seq);
+          if (FP8) {
+            expect_tx(leader, &full[st], L::kRawBytes);
+            tma_load_4d(leader, smem + L::kRaw + st * L::kRawBytes, map, 0, y, z, w, &full[st]);
+          } else {
+            unsigned char* dst = smem + L::kRing + st * L::kTileBytes;
+            expect_tx(leader, &full[st], L::kTileBytes);
+#pragma unroll
+            for (int x = 0; x < HD / 64; x++) tma_load_4d(leader, dst + x * kBox, map, x * 64, y, z, w, &full[st]);
+          }
+          issued++;
         }
       }
-      if (*(volatile int*)&h.dead) {   // copies in flight land before the block ends
-        for (unsigned i = issued > kN ? issued - kN : 0; i < issued; i++)
-          for (int n = 0; n < 1 << 16 && !mbar_try_wait(&full[i % kN], i / kN & 1); n++) {}
-      }
     }
-    __syncwarp();
+    if (uniform(*(volatile int*)&h.dead)) {    // copies in flight land before the block ends
+      for (unsigned i = issued > kN ? issued - kN : 0; i < issued; i++)
+        for (int n = 0; n < 1 << 16 && !__all_sync(~0u, mbar_try_wait(&full[i % kN], i / kN & 1)); n++) {}
+    }
   } else if (warp == kIssuer) {
     // ================================ the matrix products ==============================================================
-    if (lane == 0) {
-      constexpr unsigned kIdS = mma_idesc(kTile, kTile, false), kIdO = mma_idesc(kTile, HD, true);
-      unsigned q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
-      int ring = 0;
-      const unsigned q0 = smem_u32(smem + L::kQ), ring0 = smem_u32(smem + L::kRing);
-      while (units.next(p, h, u)) {
-        const int n0 = unit_steps<TREE>(p, u, dual, 0), n1 = unit_steps<TREE>(p, u, dual, 1);
-        const int most = max(n0, n1);
-        auto scores = [&](int t, int i) {
-          const int pos = ring + 2 * (dual ? 2 * i + t : i), st = pos % L::kStages;
-          attn_wait(&h.full[st], pos / L::kStages & 1, h);
-          if (*(volatile int*)&h.dead) return;
-          tc_fence_after();
-          const unsigned qa = q0 + t * L::kTileBytes, ka = ring0 + st * L::kTileBytes;
+    // The whole warp walks the steps, so that addresses and phases stay warp-uniform; one lane issues.
+    const bool leader = elect_one();
+    constexpr unsigned kIdS = mma_idesc(kTile, kTile, false), kIdO = mma_idesc(kTile, HD, true);
+    const uint64_t q_desc = smem_desc(smem_u32(smem + L::kQ), 16, 1024);
+    const uint64_t k_desc = smem_desc(smem_u32(smem + L::kRing), 16, 1024);
+    const uint64_t v_desc = smem_desc(smem_u32(smem + L::kRing), kBox, 1024);
+    constexpr uint64_t kTileStep = L::kTileBytes >> 4;          // descriptors count in 16 bytes
+    unsigned q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
+    int ring = 0;
+    bool on = true;
+    while (uniform(units.next(p, h, u))) {
+      const int n0 = uniform(unit_steps<TREE>(p, u, dual, 0)), n1 = uniform(unit_steps<TREE>(p, u, dual, 1));
+      const int most = max(n0, n1), tile_begin = uniform(u.tile_begin);
+      int all_see[2];                                           // first key that a row of tile t may not see
 #pragma unroll
-          for (int k = 0; k < HD / 16; k++)
-            mma_ss(tmem + t * kTile, smem_desc(qa + k / 4 * kBox + k % 4 * 32, 16, 1024),
-                   smem_desc(ka + k / 4 * kBox + k % 4 * 32, 16, 1024), kIdS, k > 0);
-          mma_commit(&h.s_full[t]);
-          if (dual || t == 1 || i >= n1) mma_commit(&h.empty[st]);
-        };
+      for (int t = 0; t < 2; t++) all_see[t] = uniform(TREE ? u.len : u.tok0 + div_rep(p, u.row0 + t * kTile) + 1);
+      auto scores = [&](int t, int i) {
+        const int pos = ring + 2 * (dual ? 2 * i + t : i), st = pos % L::kStages;
+        on = attn_wait(&h.full[st], pos / L::kStages & 1, h) && on;
+        if (!on) return;
+        tc_fence_after();
+        const uint64_t qa = q_desc + t * kTileStep, ka = k_desc + st * kTileStep;
+#pragma unroll
+        for (int k = 0; k < HD / 16; k++) {
+          const int off = (k / 4 * kBox + k % 4 * 32) >> 4;
+          mma_ss(leader, tmem + t * kTile, qa + off, ka + off, kIdS, k > 0);
+        }
+        mma_commit(leader, &h.s_full[t]);
+        if (dual || t == 1 || i >= n1) mma_commit(leader, &h.empty[st]);
+      };
+#pragma unroll
+      for (int t = 0; t < 2; t++) {
+        if (!(t ? n1 : n0)) continue;
+        on = attn_wait(&h.q_full[t], q_phase[t]++ & 1, h) && on;
+        scores(t, 0);
+      }
+      for (int i = 0; i < most; i++) {
+#pragma unroll
         for (int t = 0; t < 2; t++) {
-          if (!(t ? n1 : n0)) continue;
-          attn_wait(&h.q_full[t], q_phase[t]++ & 1, h);
-          scores(t, 0);
-        }
-        for (int i = 0; i < most; i++) {
-          for (int t = 0; t < 2; t++) {
-            const int n = t ? n1 : n0;
-            if (i >= n) continue;
-            const int pos = ring + 2 * (dual ? 2 * i + t : i) + 1, st = pos % L::kStages;
-            attn_wait(&h.p_full[t], p_phase[t]++ & 1, h);
-            attn_wait(&h.full[st], pos / L::kStages & 1, h);
-            if (!*(volatile int*)&h.dead) {
-              tc_fence_after();
-              if (!*(volatile int*)&h.skip[t]) {
-                const unsigned va = ring0 + st * L::kTileBytes;
+          const int n = t ? n1 : n0;
+          if (i >= n) continue;
+          const int rel = dual ? 2 * i + t : i, pos = ring + 2 * rel + 1, st = pos % L::kStages;
+          const bool masked = (tile_begin + rel + 1) * kTile > all_see[t];
+          on = attn_wait(&h.full[st], pos / L::kStages & 1, h) && on;
+          on = attn_wait(&h.p_full[t], p_phase[t]++ & 1, h) && on;
+          if (on) {
+            tc_fence_after();
+            if (!masked || !uniform(*(volatile int*)&h.skip[t])) {
+              const uint64_t va = v_desc + st * kTileStep;
 #pragma unroll
-                for (int k = 0; k < kTile / 16; k++)
-                  mma_ts(tmem + 2 * kTile + t * HD, tmem + t * kTile + k / 4 * 64 + k % 4 * 8, smem_desc(va + k * 2048, kBox, 1024), kIdO,
-                         i > 0 || k > 0);
-              }
-              if (i + 1 == n) mma_commit(&h.o_done[t]);
-              if (dual || t == 1 || i >= n1) mma_commit(&h.empty[st]);
+              for (int k = 0; k < kTile / 16; k++)
+                mma_ts(leader, tmem + 2 * kTile + t * HD, tmem + t * kTile + k / 4 * 64 + k % 4 * 8, va + k * 128, kIdO,
+                       i > 0 || k > 0);
             }
-            if (i + 1 < n) scores(t, i + 1);
+            if (i + 1 == n) mma_commit(leader, &h.o_done[t]);
+            if (dual || t == 1 || i >= n1) mma_commit(leader, &h.empty[st]);
           }
+          if (i + 1 < n) scores(t, i + 1);
         }
-        ring += 2 * (u.tile_end - u.tile_begin);
       }
-      if (*(volatile int*)&h.dead) {   // products in flight end before TMEM is given back
-        mma_commit(&h.fin);
-        for (int n = 0; n < 1 << 16 && !mbar_try_wait(&h.fin, 0); n++) {}
-      }
+      ring += uniform(2 * (u.tile_end - u.tile_begin));
     }
-    __syncwarp();
+    if (uniform(*(volatile int*)&h.dead)) {    // products in flight end before TMEM is given back
+      mma_commit(leader, &h.fin);
+      for (int n = 0; n < 1 << 16 && !__all_sync(~0u, mbar_try_wait(&h.fin, 0)); n++) {}
+    }
   } else if (FP8 && warp >= 16 && warp < 20) {
     // ================================ 8-bit tiles widened to bf16 ======================================================
     const int wt = threadIdx.x & 127;
@@ -852,8 +956,8 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
           }
         }
         fence_async_smem();
-        mbar_arrive(&h.full[st]);
-        mbar_arrive(&h.raw_empty[raw]);
+        warp_arrive(&h.full[st], lane);
+        warp_arrive(&h.raw_empty[raw], lane);
       }
     }
   }

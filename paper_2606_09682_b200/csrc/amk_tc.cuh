@@ -21,6 +21,13 @@ __host__ __device__ constexpr unsigned mma_idesc(int m, int n, bool b_mn) {
   return 1u << 4 | 1u << 7 | 1u << 10 | (b_mn ? 1u << 16 : 0u) | (unsigned)(n >> 3) << 17 | (unsigned)(m >> 4) << 24;
 }
 
+// true in one lane of a converged warp
+__device__ __forceinline__ bool elect_one() {
+  unsigned r;
+  asm volatile("{ .reg .pred p; elect.sync _|p, 0xffffffff; selp.u32 %0, 1, 0, p; }" : "=r"(r));
+  return r != 0;
+}
+
 // ---- tcgen05 ----------------------------------------------------------------------------------------------------
 __device__ __forceinline__ void tmem_alloc(unsigned* smem_out, unsigned columns) {   // one whole warp
   asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(smem_out)), "r"(columns)
@@ -32,24 +39,29 @@ __device__ __forceinline__ void tmem_free(unsigned base, unsigned columns) {    
 }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void mma_ss(unsigned d, uint64_t a, uint64_t b, unsigned idesc, unsigned accumulate) {
+// These three are executed by the whole converged warp and issued by the lane in which `leader` holds: the predicate is
+// on the instruction, so that the code around them has no single-lane region and its addresses stay uniform.
+__device__ __forceinline__ void mma_ss(bool leader, unsigned d, uint64_t a, uint64_t b, unsigned idesc, bool accumulate) {
   asm volatile(
-      "{ .reg .pred p; setp.ne.u32 p, %4, 0;\n"
-      "  tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      "{ .reg .pred p, q; setp.ne.u32 p, %4, 0; setp.ne.u32 q, %5, 0;\n"
+      "  @q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"((unsigned)accumulate), "r"((unsigned)leader)
       : "memory");
 }
-__device__ __forceinline__ void mma_ts(unsigned d, unsigned a, uint64_t b, unsigned idesc, unsigned accumulate) {
+__device__ __forceinline__ void mma_ts(bool leader, unsigned d, unsigned a, uint64_t b, unsigned idesc, bool accumulate) {
   asm volatile(
-      "{ .reg .pred p; setp.ne.u32 p, %4, 0;\n"
-      "  tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }" ::"r"(d),
-      "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      "{ .reg .pred p, q; setp.ne.u32 p, %4, 0; setp.ne.u32 q, %5, 0;\n"
+      "  @q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }" ::"r"(d),
+      "r"(a), "l"(b), "r"(idesc), "r"((unsigned)accumulate), "r"((unsigned)leader)
       : "memory");
 }
-// the barrier gets one arrival when every tcgen05 operation this thread has issued so far is complete
-__device__ __forceinline__ void mma_commit(uint64_t* bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar))
-               : "memory");
+// the barrier gets one arrival when every tcgen05 operation this lane has issued so far is complete
+__device__ __forceinline__ void mma_commit(bool leader, uint64_t* bar) {
+  asm volatile(
+      "{ .reg .pred q; setp.ne.u32 q, %1, 0;\n"
+      "  @q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0]; }" ::"r"(smem_u32(bar)),
+      "r"((unsigned)leader)
+      : "memory");
 }
 // 32 columns of this warp's 32 lanes (lane of TMEM = lane of the warp within its quarter)
 __device__ __forceinline__ void tmem_ld32(unsigned (&r)[32], unsigned addr) {
@@ -88,12 +100,22 @@ __device__ __forceinline__ void tmem_pin(unsigned (&r)[32]) {
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // ---- TMA --------------------------------------------------------------------------------------------------------
-// One box of a four-dimensional tensor map into shared memory; the byte offset of coordinate x is a multiple of 16.
-__device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, int x, int y, int z, int w, uint64_t* bar) {
+// One box of a four-dimensional tensor map into shared memory, issued by the leading lane of a converged warp; the byte
+// offset of coordinate x is a multiple of 16.
+__device__ __forceinline__ void tma_load_4d(bool leader, void* dst, const CUtensorMap* map, int x, int y, int z, int w,
+                                            uint64_t* bar) {
   asm volatile(
-      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2,%3,%4,%5}], [%6];" ::"r"(
+      "{ .reg .pred q; setp.ne.u32 q, %7, 0;\n"
+      "  @q cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2,%3,%4,%5}], [%6]; }" ::"r"(
           smem_u32(dst)),
-      "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar))
+      "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar)), "r"((unsigned)leader)
+      : "memory");
+}
+__device__ __forceinline__ void expect_tx(bool leader, uint64_t* bar, unsigned bytes) {
+  asm volatile(
+      "{ .reg .pred q; setp.ne.u32 q, %2, 0;\n"
+      "  @q mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1; }" ::"r"(smem_u32(bar)),
+      "r"(bytes), "r"((unsigned)leader)
       : "memory");
 }
 // shared memory written by this thread becomes visible to the asynchronous units (tensor cores, TMA)
