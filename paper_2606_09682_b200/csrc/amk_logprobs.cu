@@ -1,4 +1,16 @@
-// amk_token_logprobs: log probabilities of given tokens, row entropies and top alternatives.
+// amk_token_logprobs: log probabilities of given tokens, row entropies and top alternatives, in one pass over the logits.
+//
+// Mathematics.  With a reference r (the running maximum) and y = (x - r) log2 e, a thread sums s = sum 2^y and
+// t = sum 2^y y over its share of the row; when the maximum rises by d (in log2), s' = 2^-d s and t' = 2^-d (t - d s).
+// Shares are joined the same way: log probability of x = (x - m) - ln s, entropy = ln s - ln 2 t / s.
+//
+// Alternatives.  Sorting is kept out of the pass: a thread keeps only the maximum of its share.  The k-th largest of
+// those maxima is a lower bound of the k-th largest logit, so the alternatives lie in the shares whose maximum reaches
+// it -- about k of the 256 -- and only those are read again (from L2), into sorted lists of 32 keys, one lane each, that
+// are merged pairwise: {value, lowest index first} as one 64-bit key.
+//
+// Bound: HBM (the logits once).  A row is one block's, or with few rows a cluster's of up to eight, whose parts meet
+// in distributed shared memory: one launch, no scratch.
 #include <cuda_runtime.h>
 #include <math_constants.h>
 
@@ -7,10 +19,10 @@
 
 namespace {
 
-constexpr int kThreads = 256;
-
-__device__ __forceinline__ float load(const float* x, int64_t i) { return x[i]; }
-__device__ __forceinline__ float load(const unsigned short* x, int64_t i) { return __uint_as_float((unsigned)x[i] << 16); }
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kUnroll = 4;                    // 16-byte loads a thread has in flight
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr unsigned kAll = 0xffffffffu;
 
 struct Args {
   int64_t vocab, stride;
@@ -21,74 +33,305 @@ struct Args {
   float* top_lp;
 };
 
-template <class T>
-__global__ void __launch_bounds__(kThreads) logprobs_kernel(const T* logits, Args a) {
-  __shared__ float red[3][kThreads / 32];
-  __shared__ unsigned long long best[kThreads / 32];
-  const int64_t r = blockIdx.x;
-  const T* x = logits + r * a.stride;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  float m = -CUDART_INF_F;
-  bool nan = false;
-  for (int64_t i = threadIdx.x; i < a.vocab; i += kThreads) {
-    const float v = load(x, i);
-    nan |= v != v;
-    m = fmaxf(m, v);
+__device__ __forceinline__ float load(const float* x, int64_t i) { return x[i]; }
+__device__ __forceinline__ float load(const unsigned short* x, int64_t i) { return __uint_as_float((unsigned)x[i] << 16); }
+// the elements of a 16-byte piece
+__device__ __forceinline__ void widen(float (&v)[4], const uint4& u) {
+  v[0] = __uint_as_float(u.x), v[1] = __uint_as_float(u.y), v[2] = __uint_as_float(u.z), v[3] = __uint_as_float(u.w);
+}
+__device__ __forceinline__ void widen(float (&v)[8], const uint4& u) {
+  v[0] = amk::bf16_lo(u.x), v[1] = amk::bf16_hi(u.x), v[2] = amk::bf16_lo(u.y), v[3] = amk::bf16_hi(u.y);
+  v[4] = amk::bf16_lo(u.z), v[5] = amk::bf16_hi(u.z), v[6] = amk::bf16_lo(u.w), v[7] = amk::bf16_hi(u.w);
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {   // NaN if one of them is
+  float d;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+  return d;
+}
+// {value, lowest index first}, larger is better; NaN and "none" are 0
+__device__ __forceinline__ unsigned long long key_of(float v, unsigned i) {
+  if (v != v) return 0;
+  const unsigned u = __float_as_uint(v == 0.f ? 0.f : v);
+  return (unsigned long long)((u >> 31) ? ~u : u | 0x80000000u) << 32 | (0xffffffffu - i);
+}
+__device__ __forceinline__ float key_value(unsigned long long k) {
+  const unsigned u = (unsigned)(k >> 32);
+  return __uint_as_float((u >> 31) ? u & 0x7fffffffu : ~u);
+}
+
+// a share's sums: reference, sum of 2^y, sum of 2^y y
+struct Sums {
+  float r, s, t;
+  __device__ __forceinline__ void raise(float to) {            // a finite reference, not below the old one
+    const float d = fminf((to - r) * kLog2e, 1000.f);          // (2^-1000 is 0 here; keeps 0 * d from being NaN)
+    const float f = exp2_fast(-d);
+    t = f * (t - d * s);
+    s *= f;
+    r = to;
   }
-  nan = __syncthreads_or(nan);
-  for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
-  if (lane == 0) red[0][warp] = m;
-  __syncthreads();
-  for (int w = 0; w < kThreads / 32; w++) m = fmaxf(m, red[0][w]);
-  float s = 0, t = 0;
-  for (int64_t i = threadIdx.x; i < a.vocab; i += kThreads) {
-    const float d = load(x, i) - m;
-    const float e = expf(d);
+  __device__ __forceinline__ void join(float r2, float s2, float t2) {
+    Sums o{r2, s2, t2};
+    if (o.r > r) raise(o.r);
+    else o.raise(r);
+    s += o.s, t += o.t;
+  }
+  __device__ __forceinline__ void add(float x) {
+    const float y = fmaxf((x - r) * kLog2e, -200.f);           // -infinity: 0, not 0 * infinity
+    const float e = exp2_fast(y);
     s += e;
-    if (e > 0) t += e * d;
+    t = fmaf(e, y, t);
   }
-  for (int o = 16; o; o >>= 1) {
-    s += __shfl_xor_sync(~0u, s, o);
-    t += __shfl_xor_sync(~0u, t, o);
+};
+constexpr float kLowest = -3.402823466e38f;
+
+// ---- lists of 32, one lane each, descending ---------------------------------------------------------------------
+template <class K>
+__device__ __forceinline__ K shfl_xor(K v, int o) { return __shfl_xor_sync(kAll, v, o); }
+template <class K>
+__device__ __forceinline__ K sort32(K v, int lane) {           // bitonic
+#pragma unroll
+  for (int size = 2; size <= 32; size *= 2)
+#pragma unroll
+    for (int o = size / 2; o; o /= 2) {
+      const K w = shfl_xor(v, o);
+      const bool first = !(lane & o), desc = !(lane & size) || size == 32;
+      v = (first == desc) ? (v > w ? v : w) : (v < w ? v : w);
+    }
+  return v;
+}
+// the 32 best of two descending lists: b comes reversed, so that the maxima form a bitonic run
+template <class K>
+__device__ __forceinline__ K merge32(K a, K b_reversed, int lane) {
+  K v = a > b_reversed ? a : b_reversed;
+#pragma unroll
+  for (int o = 16; o; o /= 2) {
+    const K w = shfl_xor(v, o);
+    v = !(lane & o) ? (v > w ? v : w) : (v < w ? v : w);
   }
-  if (lane == 0) red[1][warp] = s, red[2][warp] = t;
+  return v;
+}
+// every warp's list merged; the result is in warp 0.  `buf`: kWarps lists.
+template <class K>
+__device__ __forceinline__ K merge_warps(K v, K (*buf)[32], int warp, int lane) {
+#pragma unroll
+  for (int n = kWarps / 2; n; n /= 2) {
+    if (warp >= n && warp < 2 * n) buf[warp][lane] = v;
+    __syncthreads();
+    if (warp < n) v = merge32(v, buf[warp + n][31 - lane], lane);
+  }
+  return v;
+}
+
+// ---- cluster ----------------------------------------------------------------------------------------------------
+__device__ __forceinline__ unsigned cluster_rank() {
+  unsigned r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ unsigned remote(const void* p, unsigned rank) {   // the same place in another block
+  unsigned a;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(amk::smem_u32(p)), "r"(rank));
+  return a;
+}
+__device__ __forceinline__ float remote_f32(const void* p, unsigned rank) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote(p, rank)) : "memory");
+  return v;
+}
+__device__ __forceinline__ unsigned long long remote_u64(const void* p, unsigned rank) {
+  unsigned long long v;
+  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(remote(p, rank)) : "memory");
+  return v;
+}
+
+// C blocks a row.  Of a block's part, thread f has the 16-byte pieces f, f + 256, ...; the first block's threads also one
+// element each in front of the first piece, the last block's one behind the last.
+template <class T>
+__global__ void __launch_bounds__(kThreads, 4) logprobs_kernel(const T* __restrict__ logits, const Args a, int C) {
+  constexpr int kVec = 16 / sizeof(T);
+  __shared__ unsigned long long lists[kWarps][32];
+  __shared__ float part[4];                          // this block's reference, sums, NaN flag
+  __shared__ float red[4][kWarps];
+  __shared__ unsigned flagged[kWarps];
+  __shared__ float bound;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const unsigned rank = C > 1 ? cluster_rank() : 0;
+  const int64_t row = C > 1 ? blockIdx.x / C : blockIdx.x;
+  const T* x = logits + row * a.stride;
+  const int vocab = (int)a.vocab;
+  const int head = min(vocab, (int)((16 - ((uintptr_t)x & 15)) % 16 / sizeof(T)));
+  const int pieces = (vocab - head) / kVec, tail = vocab - head - pieces * kVec;
+  const int per = (pieces + C - 1) / C, p0 = min(pieces, (int)rank * per), n = min(pieces, p0 + per) - p0;
+  const uint4* v4 = (const uint4*)(x + head) + p0;
+  const int base = head + p0 * kVec;                 // index of the part's first element
+
+  Sums sum{kLowest, 0.f, 0.f};
+  float top = -CUDART_INF_F;                         // NaN if there was one
+  auto single = [&](int i) {
+    const float v = load(x, i);
+    top = max_nan(top, v);
+    if (v > sum.r && v < CUDART_INF_F) sum.raise(v);
+    sum.add(v);
+  };
+  if (rank == 0 && (int)threadIdx.x < head) single(threadIdx.x);
+  for (int i0 = threadIdx.x; i0 < n; i0 += kUnroll * kThreads) {
+    uint4 u[kUnroll];
+#pragma unroll
+    for (int j = 0; j < kUnroll; j++)
+      if (i0 + j * kThreads < n) u[j] = __ldg(v4 + i0 + j * kThreads);
+#pragma unroll
+    for (int j = 0; j < kUnroll; j++) {
+      if (i0 + j * kThreads >= n) break;
+      float v[kVec];
+      widen(v, u[j]);
+      float mx = v[0];
+#pragma unroll
+      for (int k = 1; k < kVec; k++) mx = max_nan(mx, v[k]);
+      top = max_nan(top, mx);
+      if (mx > sum.r && mx < CUDART_INF_F) sum.raise(mx);
+#pragma unroll
+      for (int k = 0; k < kVec; k++) sum.add(v[k]);
+    }
+  }
+  if (rank == (unsigned)C - 1 && (int)threadIdx.x < tail) single(head + pieces * kVec + threadIdx.x);
+  const bool share_nan = top != top;
+
+  // the block's sums
+  const bool nan = __any_sync(kAll, share_nan) != 0;
+  float r = sum.r, m = share_nan ? CUDART_INF_F : top;   // (m: whether the maximum is infinite; a NaN spoils the row as well)
+#pragma unroll
+  for (int o = 16; o; o /= 2) r = fmaxf(r, shfl_xor(r, o)), m = fmaxf(m, shfl_xor(m, o));
+  sum.raise(r);
+#pragma unroll
+  for (int o = 16; o; o /= 2) sum.s += shfl_xor(sum.s, o), sum.t += shfl_xor(sum.t, o);
+  if (lane == 0) red[0][warp] = r, red[1][warp] = sum.s, red[2][warp] = sum.t, red[3][warp] = nan ? CUDART_INF_F : m;
+
+  // the block's alternatives, in warp 0
+  unsigned long long best = 0;
+  if (a.top) {
+    const unsigned mine = share_nan ? 0 : (unsigned)(key_of(top, 0) >> 32);   // a share with NaN bounds nothing
+    const unsigned sorted = sort32(mine, lane);
+    const unsigned all = merge_warps(sorted, (unsigned (*)[32])lists, warp, lane);
+    const unsigned kth = __shfl_sync(kAll, all, a.top - 1);
+    if (threadIdx.x == 0) bound = __uint_as_float(kth);
+    __syncthreads();
+    const unsigned low = __float_as_uint(bound);
+    const unsigned f = __ballot_sync(kAll, share_nan || (mine && mine >= low));
+    if (lane == 0) flagged[warp] = f;
+    __syncthreads();
+    // flagged shares go round the warps; a warp reads one share at a time, a piece for each lane
+    unsigned long long kth_key = 0;
+    auto take = [&](unsigned long long k) {          // this lane's candidate joins the warp's list
+      unsigned w = __ballot_sync(kAll, k > kth_key);
+      if (!w) return;
+      if (__popc(w) > 4) {
+        best = merge32(best, __shfl_sync(kAll, sort32(k, lane), 31 - lane), lane);
+      } else {
+        for (; w; w &= w - 1) {
+          const unsigned long long c = __shfl_sync(kAll, k, __ffs(w) - 1), up = __shfl_up_sync(kAll, best, 1);
+          if (c > best) best = lane && c > up ? up : c;
+        }
+      }
+      kth_key = __shfl_sync(kAll, best, a.top - 1);
+    };
+    int turn = 0;
+    for (int w = 0; w < kWarps; w++) {
+      for (unsigned g = flagged[w]; g; g &= g - 1, turn++) {
+        if (turn % kWarps != warp) continue;
+        const int share = w * 32 + __ffs(g) - 1;
+        if (rank == 0 && share < head) take(lane == 0 ? key_of(load(x, share), share) : 0);
+        if (rank == (unsigned)C - 1 && share < tail) {
+          const int i = head + pieces * kVec + share;
+          take(lane == 0 ? key_of(load(x, i), i) : 0);
+        }
+        for (int i0 = share; i0 < n; i0 += 32 * kThreads) {
+          const int i = i0 + lane * kThreads;
+          float v[kVec];
+          if (i < n) {
+            widen(v, __ldg(v4 + i));
+          } else {
+#pragma unroll
+            for (int k = 0; k < kVec; k++) v[k] = CUDART_NAN_F;
+          }
+#pragma unroll
+          for (int k = 0; k < kVec; k++) {
+            const unsigned long long key = key_of(v[k], base + i * kVec + k);
+            take((unsigned)(key >> 32) >= low ? key : 0);
+          }
+        }
+      }
+    }
+    __syncthreads();
+    best = merge_warps(best, lists, warp, lane);
+  }
   __syncthreads();
-  s = t = 0;
-  for (int w = 0; w < kThreads / 32; w++) s += red[1][w], t += red[2][w];
-  const float bad = nan || !(fabsf(m) < CUDART_INF_F) ? CUDART_NAN_F : 0.f;
-  const float ls = logf(s) + bad;
-  if (threadIdx.x == 0) {
-    const int tok = a.tokens[r];
-    if (a.lp) a.lp[r] = tok < 0 || tok >= a.vocab ? CUDART_NAN_F : load(x, tok) - m - ls;
-    if (a.ent) a.ent[r] = ls - t / s;
+  if (warp == 0) {
+    Sums b{lane < kWarps ? red[0][lane] : kLowest, lane < kWarps ? red[1][lane] : 0.f, lane < kWarps ? red[2][lane] : 0.f};
+    float mm = lane < kWarps ? red[3][lane] : -CUDART_INF_F;
+#pragma unroll
+    for (int o = kWarps / 2; o; o /= 2) {
+      b.join(shfl_xor(b.r, o), shfl_xor(b.s, o), shfl_xor(b.t, o));
+      mm = fmaxf(mm, shfl_xor(mm, o));
+    }
+    if (C > 1) {
+      if (lane == 0) part[0] = b.r, part[1] = b.s, part[2] = b.t, part[3] = mm;
+      lists[0][lane] = best;
+    }
+    sum = b;
+    m = mm;
   }
-  // the k-th alternative: the largest key {value, lowest index first} below the one before
-  unsigned long long prev = ~0ull;
-  for (int k = 0; k < a.top; k++) {
-    unsigned long long b = 0;
-    for (int64_t i = threadIdx.x; i < a.vocab; i += kThreads) {
-      const float v = load(x, i);
-      if (v != v) continue;
-      const unsigned u = __float_as_uint(v == 0.f ? 0.f : v);
-      const unsigned long long key =
-          (unsigned long long)((u >> 31) ? ~u : u | 0x80000000u) << 32 | (0xffffffffu - (unsigned)i);
-      if (key < prev && key > b) b = key;
-    }
-    for (int o = 16; o; o >>= 1) {
-      const unsigned long long ob = __shfl_xor_sync(~0u, b, o);
-      b = ob > b ? ob : b;
-    }
+  if (C > 1) {
     __syncthreads();
-    if (lane == 0) best[warp] = b;
-    __syncthreads();
-    for (int w = 0; w < kThreads / 32; w++) b = best[w] > b ? best[w] : b;
-    if (threadIdx.x == 0) {
-      const int id = (int)(0xffffffffu - (unsigned)b);
-      a.top_id[r * a.top + k] = b ? id : -1;
-      a.top_lp[r * a.top + k] = b ? load(x, id) - m - ls : CUDART_NAN_F;
+    cluster_sync();
+    if (rank == 0 && warp == 0) {
+      for (int c = 1; c < C; c++) {
+        sum.join(remote_f32(&part[0], c), remote_f32(&part[1], c), remote_f32(&part[2], c));
+        m = fmaxf(m, remote_f32(&part[3], c));
+        if (a.top) best = merge32(best, remote_u64(&lists[0][31 - lane], c), lane);
+      }
     }
-    prev = b;
+    cluster_sync();                                  // the others' shared memory has been read
   }
+  if (rank || warp) return;
+  m = __shfl_sync(kAll, m, 0);
+  const float s = __shfl_sync(kAll, sum.s, 0), t = __shfl_sync(kAll, sum.t, 0);
+  const float r0 = __shfl_sync(kAll, sum.r, 0);
+  const float ls = fabsf(m) < CUDART_INF_F ? logf(s) : CUDART_NAN_F;   // no finite maximum, or a NaN
+  if (lane == 0) {
+    const int tok = a.tokens[row];
+    if (a.lp) a.lp[row] = tok < 0 || tok >= vocab ? CUDART_NAN_F : load(x, tok) - r0 - ls;
+    if (a.ent) a.ent[row] = fmaf(-kLn2, t / s, ls);
+  }
+  if (lane < a.top) {
+    a.top_id[row * a.top + lane] = best ? (int)(0xffffffffu - (unsigned)best) : -1;
+    a.top_lp[row * a.top + lane] = best ? key_value(best) - r0 - ls : CUDART_NAN_F;
+  }
+}
+
+template <class T>
+cudaError_t launch(const void* logits, const Args& a, int64_t rows, int C, cudaStream_t st) {
+  if (C == 1) {
+    logprobs_kernel<T><<<(unsigned)rows, kThreads, 0, st>>>((const T*)logits, a, 1);
+    return cudaGetLastError();
+  }
+  cudaLaunchAttribute at;
+  at.id = cudaLaunchAttributeClusterDimension;
+  at.val.clusterDim.x = (unsigned)C, at.val.clusterDim.y = at.val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(rows * C));
+  cfg.blockDim = dim3(kThreads);
+  cfg.stream = st;
+  cfg.attrs = &at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, logprobs_kernel<T>, (const T*)logits, a, C);
 }
 
 }  // namespace
@@ -112,10 +355,13 @@ extern "C" amk_status amk_token_logprobs(const void* logits, uint32_t dtype, int
       !amk::aligned(entropy, 4) || !amk::aligned(top_tokens, 4) || !amk::aligned(top_logprobs, 4))
     return fail(AMK_ERR_INVALID_ARG, "pointers must be aligned to their elements");
   const Args a{vocab, row_stride, tokens, (int)top_k, logprob, entropy, top_tokens, top_logprobs};
-  if (dtype)
-    logprobs_kernel<<<(int)rows, kThreads, 0, (cudaStream_t)cuda_stream>>>((const unsigned short*)logits, a);
-  else
-    logprobs_kernel<<<(int)rows, kThreads, 0, (cudaStream_t)cuda_stream>>>((const float*)logits, a);
-  const cudaError_t e = cudaGetLastError();
+  // Blocks a row: doubled until there are two for each SM, while a block keeps 2048 logits.  (64 rows of 128256 fp32
+  // logits, top 20: 1 block a row 34 us, 8 blocks 15 us.)
+  int dev = 0, sms = 148, C = 1;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    (void)cudaGetLastError();
+  while (C < 8 && rows * C < 2 * sms && vocab / (2 * C) >= 2048) C *= 2;
+  const cudaStream_t st = (cudaStream_t)cuda_stream;
+  const cudaError_t e = dtype ? launch<unsigned short>(logits, a, rows, C, st) : launch<float>(logits, a, rows, C, st);
   return e == cudaSuccess ? AMK_OK : fail(AMK_ERR_CUDA, "launch failed: %s", cudaGetErrorString(e));
 }
