@@ -267,18 +267,22 @@ def amk_argmax_static(x: torch.Tensor, token: torch.Tensor, n: int = -1) -> None
 AMK_TREE_MAX_ROWS = 1024
 AMK_LOGPROBS_MAX_TOP = 32
 _local = threading.local()
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
-def _need(ok: bool, what: str) -> None:
-    if not ok:
-        raise AmkError(AMK_ERR_INVALID_ARG, what)
+def _refuse(name: str, what: str):
+    raise AmkError(AMK_ERR_INVALID_ARG, f"{name}: {what}")
 
 
-def _same_device(name: str, first: torch.Tensor, *others) -> None:
+def _device_of(name: str, first: torch.Tensor, *others) -> torch.device:
     dev = first.device
-    _need(dev.type == "cuda", f"{name}: tensors must be cuda tensors")
+    if dev.type != "cuda":
+        _refuse(name, "tensors must be cuda tensors")
     for t in others:
-        _need(t is None or t.device == dev, f"{name}: tensors on different devices")
+        if t is not None and t.device != dev:
+            _refuse(name, "tensors on different devices")
+    return dev
 
 
 def _run(fn, name: str, device: torch.device, *args) -> None:
@@ -286,11 +290,12 @@ def _run(fn, name: str, device: torch.device, *args) -> None:
     msg = getattr(_local, "msg", None)
     if msg is None:
         msg = _local.msg = C.create_string_buffer(256)
-    if device.index == torch.cuda.current_device():
-        code = fn(*args, msg, 256, torch.cuda.current_stream().cuda_stream)
+    index = device.index
+    if index == torch.cuda.current_device():
+        code = fn(*args, msg, 256, _raw_stream(index))
     else:
-        with torch.cuda.device(device):
-            code = fn(*args, msg, 256, torch.cuda.current_stream().cuda_stream)
+        with torch.cuda.device(index):
+            code = fn(*args, msg, 256, _raw_stream(index))
     if code != AMK_OK:
         raise AmkError(code, msg.value.decode() or name)
 
@@ -303,28 +308,34 @@ def amk_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_s
     contiguous) is filled if given.  Rows that belong to no prompt are left as they were (undefined if ``out`` is not
     given)."""
     name = "amk_prompt_attention"
-    _need(q.dim() == 3 and k.dim() == 3 and v.dim() == 3, f"{name}: q, k and v are [total][heads][head_dim]")
-    total, nq, hd = q.shape
-    nkv = k.shape[1]
-    _same_device(name, q, k, v, cu_seqlens, out, lse)
-    _need(q.dtype == k.dtype == v.dtype == torch.bfloat16, f"{name}: q, k and v are bf16")
-    _need(k.shape == v.shape and k.shape[0] == total and k.shape[2] == hd, f"{name}: shapes of q, k and v do not fit")
-    _need(cu_seqlens.dtype == torch.int32 and cu_seqlens.dim() == 1 and cu_seqlens.is_contiguous() and
-          cu_seqlens.numel() >= 1, f"{name}: cu_seqlens is a contiguous int32 vector of n_seqs + 1 entries")
+    if q.dim() != 3 or k.dim() != 3 or v.dim() != 3:
+        _refuse(name, "q, k and v are [total][heads][head_dim]")
+    total, nq, hd = shape = q.shape
+    kshape = k.shape
+    dev = _device_of(name, q, k, v, cu_seqlens, out, lse)
+    if not (q.dtype is k.dtype is v.dtype is torch.bfloat16):
+        _refuse(name, "q, k and v are bf16")
+    if kshape != v.shape or kshape[0] != total or kshape[2] != hd:
+        _refuse(name, "shapes of q, k and v do not fit")
+    if cu_seqlens.dtype is not torch.int32 or cu_seqlens.dim() != 1 or not cu_seqlens.is_contiguous() or not len(cu_seqlens):
+        _refuse(name, "cu_seqlens is a contiguous int32 vector of n_seqs + 1 entries")
     if out is None:
-        out = torch.empty((total, nq, hd), dtype=torch.bfloat16, device=q.device)
-    else:
-        _need(out.shape == q.shape and out.dtype == torch.bfloat16, f"{name}: out is bf16 of q's shape")
-    if lse is not None:
-        _need(lse.shape == (total, nq) and lse.dtype == torch.float32 and lse.is_contiguous(),
-              f"{name}: lse is contiguous fp32 [total][n_q]")
+        out = torch.empty(shape, dtype=torch.bfloat16, device=dev)
+    elif out.shape != shape or out.dtype is not torch.bfloat16:
+        _refuse(name, "out is bf16 of q's shape")
+    if lse is not None and (lse.shape != (total, nq) or lse.dtype is not torch.float32 or not lse.is_contiguous()):
+        _refuse(name, "lse is contiguous fp32 [total][n_q]")
     (qr, qh, q1), (kr, kh, k1), (vr, vh, v1), (orow, oh, o1) = q.stride(), k.stride(), v.stride(), out.stride()
-    _need(q1 == 1 and k1 == 1 and v1 == 1 and o1 == 1, f"{name}: the last dimension must be contiguous")
-    args = _PROMPT.pack(_PROMPT.size, hd, nq, nkv, cu_seqlens.numel() - 1, scale or 0.0, total, q.data_ptr(),
+    if not (q1 == k1 == v1 == o1 == 1):
+        _refuse(name, "the last dimension must be contiguous")
+    args = _PROMPT.pack(_PROMPT.size, hd, nq, kshape[1], len(cu_seqlens) - 1, scale or 0.0, total, q.data_ptr(),
                         k.data_ptr(), v.data_ptr(), out.data_ptr(), 0 if lse is None else lse.data_ptr(),
                         cu_seqlens.data_ptr(), qr, qh, kr, kh, vr, vh, orow, oh)
-    _run(lib.amk_prompt_attention, name, q.device, args)
+    _run(lib.amk_prompt_attention, name, dev, args)
     return out
+
+
+_tree_bytes: Dict = {}                                # scratch bytes by device and shape
 
 
 def amk_tree_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cache_len: torch.Tensor,
@@ -338,39 +349,55 @@ def amk_tree_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cache_
     the division of the work.  ``workspace``: uint8 scratch of ``amk_tree_workspace_bytes``, taken from torch's
     allocator if not given.  Returns out, of q's shape; ``lse`` (fp32 [n_seqs][rows][n_q]) is filled if given."""
     name = "amk_tree_attention"
-    _need(q.dim() == 4 and k.dim() == 4 and v.dim() == 4, f"{name}: q, k and v have four dimensions")
-    seqs, rows, nq, hd = q.shape
-    _, nkv, slots, _ = k.shape
-    _same_device(name, q, k, v, cache_len, mask, out, lse, workspace)
-    _need(q.dtype == torch.bfloat16, f"{name}: q is bf16")
-    _need(k.dtype == v.dtype and k.dtype in (torch.bfloat16, torch.uint8, torch.float8_e4m3fn),
-          f"{name}: the cache is bf16, or e4m3 as uint8 or float8_e4m3fn")
-    _need(k.shape == v.shape and k.shape[0] == seqs and k.shape[3] == hd, f"{name}: shapes of q, k and v do not fit")
-    _need(cache_len.dtype == torch.int32 and cache_len.shape == (seqs,) and cache_len.is_contiguous(),
-          f"{name}: cache_len is a contiguous int32 vector with an entry for each sequence")
-    if mask is not None:
-        _need(mask.dtype == torch.int64 and mask.shape == (seqs, rows, (rows + 63) // 64) and mask.is_contiguous(),
-              f"{name}: mask is contiguous int64 [n_seqs][rows][ceil(rows / 64)]")
+    if q.dim() != 4 or k.dim() != 4 or v.dim() != 4:
+        _refuse(name, "q, k and v have four dimensions")
+    seqs, rows, nq, hd = shape = q.shape
+    kseqs, nkv, slots, khd = k.shape
+    dev = _device_of(name, q, k, v, cache_len, mask, out, lse, workspace)
+    dtype = k.dtype
+    if q.dtype is not torch.bfloat16:
+        _refuse(name, "q is bf16")
+    if v.dtype is not dtype or dtype not in (torch.bfloat16, torch.uint8, torch.float8_e4m3fn):
+        _refuse(name, "the cache is bf16, or e4m3 as uint8 or float8_e4m3fn")
+    if k.shape != v.shape or kseqs != seqs or khd != hd:
+        _refuse(name, "shapes of q, k and v do not fit")
+    if cache_len.dtype is not torch.int32 or cache_len.shape != (seqs,) or not cache_len.is_contiguous():
+        _refuse(name, "cache_len is a contiguous int32 vector with an entry for each sequence")
+    if mask is not None and (mask.dtype is not torch.int64 or mask.shape != (seqs, rows, (rows + 63) // 64) or
+                             not mask.is_contiguous()):
+        _refuse(name, "mask is contiguous int64 [n_seqs][rows][ceil(rows / 64)]")
     if out is None:
-        out = torch.empty((seqs, rows, nq, hd), dtype=torch.bfloat16, device=q.device)
-    else:
-        _need(out.shape == q.shape and out.dtype == torch.bfloat16, f"{name}: out is bf16 of q's shape")
-    if lse is not None:
-        _need(lse.shape == (seqs, rows, nq) and lse.dtype == torch.float32 and lse.is_contiguous(),
-              f"{name}: lse is contiguous fp32 [n_seqs][rows][n_q]")
-    _need(max_len is None or 0 <= max_len <= slots, f"{name}: max_len between 0 and the slots of the cache")
+        out = torch.empty(shape, dtype=torch.bfloat16, device=dev)
+    elif out.shape != shape or out.dtype is not torch.bfloat16:
+        _refuse(name, "out is bf16 of q's shape")
+    if lse is not None and (lse.shape != (seqs, rows, nq) or lse.dtype is not torch.float32 or not lse.is_contiguous()):
+        _refuse(name, "lse is contiguous fp32 [n_seqs][rows][n_q]")
+    if max_len is not None and not 0 <= max_len <= slots:
+        _refuse(name, "max_len between 0 and the slots of the cache")
     (qs, qr, qh, q1), (ks, kh, kr, k1), (vs, vh, vr, v1) = q.stride(), k.stride(), v.stride()
     os_, orow, oh, o1 = out.stride()
-    _need(q1 == 1 and k1 == 1 and v1 == 1 and o1 == 1, f"{name}: the last dimension must be contiguous")
-    head = (_TREE.size, hd, nq, nkv, AMK_KV_BF16 if k.dtype == torch.bfloat16 else AMK_KV_FP8_E4M3, seqs, rows, slots,
-            max_len or 0, scale or 0.0, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
-            0 if lse is None else lse.data_ptr(), cache_len.data_ptr(), 0 if mask is None else mask.data_ptr())
-    tail = (qs, qr, qh, ks, kh, kr, vs, vh, vr, os_, orow, oh)
+    if not (q1 == k1 == v1 == o1 == 1):
+        _refuse(name, "the last dimension must be contiguous")
+    plan = (_TREE.size, hd, nq, nkv, AMK_KV_BF16 if dtype is torch.bfloat16 else AMK_KV_FP8_E4M3, seqs, rows, slots,
+            max_len or 0)
     if workspace is None:
-        n = amk_tree_workspace_bytes(_TREE.pack(*head, 0, 0, *tail), q.device)
-        workspace = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
-    ws = (0, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
-    _run(lib.amk_tree_attention, name, q.device, _TREE.pack(*head, *ws, *tail))
+        key = (dev.index, plan)
+        need = _tree_bytes.get(key)
+        if need is None:
+            need = amk_tree_workspace_bytes(_TREE.pack(*plan, *(0,) * 22), dev)
+            if len(_tree_bytes) >= 4096:
+                _tree_bytes.clear()
+            _tree_bytes[key] = need
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        have = need
+    else:
+        if not workspace.is_contiguous():
+            _refuse(name, "the workspace must be contiguous")
+        have = workspace.numel() * workspace.element_size()
+    args = _TREE.pack(*plan, scale or 0.0, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
+                      0 if lse is None else lse.data_ptr(), cache_len.data_ptr(), 0 if mask is None else mask.data_ptr(),
+                      workspace.data_ptr(), have, qs, qr, qh, ks, kh, kr, vs, vh, vr, os_, orow, oh)
+    _run(lib.amk_tree_attention, name, dev, args)
     return out
 
 
@@ -389,8 +416,9 @@ def amk_operator_status(device=None) -> int:
     """Synchronises; AMK_OK, or AMK_ERR_TIMEOUT if a bounded wait of an attention kernel ran out on the device since last
     asked."""
     st = C.c_int()
-    _run(lib.amk_operator_status, "amk_operator_status", torch.device("cuda", torch.cuda.current_device())
-         if device is None else torch.device(device), C.byref(st))
+    dev = torch.device("cuda" if device is None else device)
+    _run(lib.amk_operator_status, "amk_operator_status",
+         torch.device("cuda", torch.cuda.current_device()) if dev.index is None else dev, C.byref(st))
     return st.value
 
 
@@ -398,23 +426,28 @@ def amk_token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, top_k: int = 
     """logits [rows][vocab] (fp32 or bf16, cuda, rows at any stride), tokens int32 [rows] -> (logprob [rows], entropy
     [rows], top tokens int32 [rows][top_k], their log probabilities [rows][top_k]); log probabilities fp32, natural."""
     name = "amk_token_logprobs"
-    _need(logits.dim() == 2, f"{name}: logits are [rows][vocab]")
+    if logits.dim() != 2:
+        _refuse(name, "logits are [rows][vocab]")
     rows, vocab = logits.shape
-    _same_device(name, logits, tokens)
-    _need(logits.dtype in (torch.float32, torch.bfloat16), f"{name}: logits are fp32 or bf16")
-    _need(tokens.dtype == torch.int32 and tokens.shape == (rows,) and tokens.is_contiguous(),
-          f"{name}: tokens is a contiguous int32 vector with an entry for each row")
+    dev = _device_of(name, logits, tokens)
+    dtype = logits.dtype
+    if dtype is not torch.float32 and dtype is not torch.bfloat16:
+        _refuse(name, "logits are fp32 or bf16")
+    if tokens.dtype is not torch.int32 or tokens.shape != (rows,) or not tokens.is_contiguous():
+        _refuse(name, "tokens is a contiguous int32 vector with an entry for each row")
     stride, one = logits.stride()
-    _need(one == 1 or vocab <= 1, f"{name}: the last dimension must be contiguous")
-    _need(top_k >= 0, f"{name}: top_k is negative")
-    dev = logits.device
+    if one != 1 and vocab > 1:
+        _refuse(name, "the last dimension must be contiguous")
+    if top_k < 0:
+        _refuse(name, "top_k is negative")
     both = torch.empty((2, rows), dtype=torch.float32, device=dev)
     top_tokens = torch.empty((rows, top_k), dtype=torch.int32, device=dev)
     top_logprobs = torch.empty((rows, top_k), dtype=torch.float32, device=dev)
-    _run(lib.amk_token_logprobs, name, dev, logits.data_ptr(), int(logits.dtype == torch.bfloat16), rows, vocab, stride,
-         tokens.data_ptr(), top_k, both.data_ptr(), both.data_ptr() + 4 * rows, top_tokens.data_ptr(),
-         top_logprobs.data_ptr())
-    return both[0], both[1], top_tokens, top_logprobs
+    p = both.data_ptr()
+    _run(lib.amk_token_logprobs, name, dev, logits.data_ptr(), 1 if dtype is torch.bfloat16 else 0, rows, vocab, stride,
+         tokens.data_ptr(), top_k, p, p + 4 * rows, top_tokens.data_ptr(), top_logprobs.data_ptr())
+    logprob, entropy = both.unbind(0)
+    return logprob, entropy, top_tokens, top_logprobs
 
 
 def amk_kv_compact(kv: torch.Tensor, base: torch.Tensor, keep: torch.Tensor, count: torch.Tensor) -> None:
@@ -423,19 +456,23 @@ def amk_kv_compact(kv: torch.Tensor, base: torch.Tensor, keep: torch.Tensor, cou
     [n_caches][max_keep], strictly ascending from at least base[c] over its first count[c] entries (a cache whose list is
     not stays as it was)."""
     name = "amk_kv_compact"
-    _need(kv.dim() >= 3, f"{name}: kv is [n_caches][...][max_seq][head_dim]")
-    _same_device(name, kv, base, keep, count)
-    caches, slots, row = kv.shape[0], kv.shape[-2], kv.shape[-1] * kv.element_size()
-    _need(base.dtype == keep.dtype == count.dtype == torch.int32, f"{name}: base, keep and count are int32")
-    _need(base.shape == (caches,) and count.shape == (caches,) and keep.dim() == 2 and keep.shape[0] == caches and
-          base.is_contiguous() and keep.is_contiguous() and count.is_contiguous(),
-          f"{name}: base [n_caches], keep [n_caches][max_keep] and count [n_caches] must be contiguous")
-    if caches == 0 or kv.numel() == 0:
+    if kv.dim() < 3:
+        _refuse(name, "kv is [n_caches][...][max_seq][head_dim]")
+    dev = _device_of(name, kv, base, keep, count)
+    shape = kv.shape
+    caches, slots, elements, esz = shape[0], shape[-2], shape[-1], kv.element_size()
+    if not (base.dtype is keep.dtype is count.dtype is torch.int32):
+        _refuse(name, "base, keep and count are int32")
+    if base.shape != (caches,) or count.shape != (caches,) or keep.dim() != 2 or keep.shape[0] != caches or not (
+            base.is_contiguous() and keep.is_contiguous() and count.is_contiguous()):
+        _refuse(name, "base [n_caches], keep [n_caches][max_keep] and count [n_caches] must be contiguous")
+    total = kv.numel()
+    if total == 0:
         return
-    _need(kv[0].is_contiguous(), f"{name}: each cache must be contiguous")
-    planes = kv.numel() // caches // slots // kv.shape[-1]
-    _run(lib.amk_kv_compact, name, kv.device, kv.data_ptr(), caches, kv.stride(0) * kv.element_size(), planes, slots, row,
-         base.data_ptr(), keep.data_ptr(), keep.shape[1], count.data_ptr())
+    if not kv.is_contiguous() and not kv[0].is_contiguous():
+        _refuse(name, "each cache must be contiguous")
+    _run(lib.amk_kv_compact, name, dev, kv.data_ptr(), caches, kv.stride(0) * esz, total // (caches * slots * elements), slots,
+         elements * esz, base.data_ptr(), keep.data_ptr(), keep.shape[1], count.data_ptr())
 
 
 def quantize_weights(weights: Dict, wdtype: str) -> Dict:
