@@ -79,8 +79,8 @@ cudaError_t launch_join(const AttnParams& p, unsigned blocks, cudaStream_t st) {
   at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at.val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(p.rows * p.rep * (HD / 16) + 255) / 256, (unsigned)p.nkv, (unsigned)p.n_seqs);
-  cfg.blockDim = dim3(256);
+  cfg.gridDim = dim3((unsigned)(p.rows * p.rep + 31) / 32, (unsigned)p.nkv, (unsigned)p.n_seqs);
+  cfg.blockDim = dim3(HD * 2);                       // a warp for each 16 columns
   cfg.stream = st;
   cfg.attrs = &at;
   cfg.numAttrs = 1;
@@ -110,8 +110,8 @@ TreePlan tree_plan(const amk_tree_args& a) {
   t.row_tiles = (int)((rows + t.part_rows - 1) / t.part_rows);
   const int64_t most = a.n_slots - a.n_rows, len = a.max_len && a.max_len < most ? a.max_len : most;
   const int64_t tiles = (len + a.n_rows + amk::kTile - 1) / amk::kTile;
-  const int64_t runs = (tiles * a.n_kv_heads * t.row_tiles * a.n_seqs + kMinTiles - 1) / kMinTiles;
-  const int sms = sm_count();
+  const int64_t runs = ((tiles + amk::kUnitCost) * a.n_kv_heads * t.row_tiles * a.n_seqs + kMinTiles - 1) / kMinTiles;
+  const int sms = sm_count() < amk::kMaxBlocks ? sm_count() : amk::kMaxBlocks;
   t.blocks = (unsigned)(runs < sms ? runs : sms);
   t.bytes = (size_t)2 * t.blocks * t.part_rows * (a.head_dim + 1) * 4;
   return t;
@@ -156,6 +156,9 @@ amk_status check_tree(const Reason& fail, const amk_tree_args* a) {
   if (a->n_slots < a->n_rows || a->n_slots > 0x7fffffff - 1024)
     return fail(AMK_ERR_INVALID_ARG, "%u slots for %u drafted tokens", a->n_slots, a->n_rows);
   if (a->n_seqs > 65535) return fail(AMK_ERR_UNSUPPORTED, "%u sequences: at most 65535", a->n_seqs);
+  if ((a->n_slots / (double)amk::kTile + 2 + amk::kUnitCost) * a->n_kv_heads * a->n_seqs *
+          (a->n_rows * 16.0 / amk::kTile + 1) > 0x7fffffff)
+    return fail(AMK_ERR_UNSUPPORTED, "%u sequences of %u slots: more than 2^31 pieces of work", a->n_seqs, a->n_slots);
   return AMK_OK;
 }
 

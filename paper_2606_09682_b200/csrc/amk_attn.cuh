@@ -132,21 +132,29 @@ struct Unit {
   int len;                // tree: context length
 };
 
-// Tree: the key tiles of all (sequence, kv head, row block) in that order, cut into equal runs, one for each block.
+// Tree: the key tiles of all (sequence, kv head, row block) in that order, cut into equal runs, one for each block.  An
+// item counts kUnitCost tiles more than it has, in front of its first: a block that begins another item reads another Q,
+// fills the pipeline again and writes another output, which costs about as much (a batch with an empty sequence left one
+// block with eight such items: 100 us, the others 34 us).
+constexpr int kUnitCost = 3;
 __device__ __forceinline__ int tree_tiles(const AttnParams& p, int len) {   // key tiles of one item; 0: bad length
   return len < 0 || len > p.slots - p.rows ? 0 : (len + p.rows + kTile - 1) / kTile;
 }
-// flat tiles of all sequences and tiles per block, the same in every block (one warp; result in every lane)
-__device__ __forceinline__ int64_t tree_total(const AttnParams& p, int lane) {
-  int64_t sum = 0;
-  for (int b = lane; b < p.n_seqs; b += 32) sum += tree_tiles(p, p.lens[b]);
-#pragma unroll
-  for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
-  return sum * p.nkv * p.row_tiles;
+__device__ __forceinline__ int tree_slots(int tiles) { return tiles ? tiles + kUnitCost : 0; }
+// slots of a warp's 32 sequences from b0 on, this lane's
+__device__ __forceinline__ int tree_slots_of(const AttnParams& p, int b) {
+  return b < p.n_seqs ? tree_slots(tree_tiles(p, __ldg(p.lens + b))) * p.nkv * p.row_tiles : 0;
 }
-__device__ __forceinline__ int64_t tree_per_block(const AttnParams& p, int64_t total, int blocks) {
-  const int64_t per = (total + blocks - 1) / blocks;
-  return per < p.min_tiles ? p.min_tiles : per;
+__device__ __forceinline__ int warp_sum(int x) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(~0u, x, o);
+  return x;
+}
+// slots of one run, the same in every block; `first`: this lane's share of the first 32 sequences (one whole warp)
+__device__ __forceinline__ int tree_run(const AttnParams& p, int first, int lane, int blocks) {
+  int sum = first;
+  for (int b = 32 + lane; b < p.n_seqs; b += 32) sum += tree_slots_of(p, b);
+  return max((warp_sum(sum) + blocks - 1) / blocks, p.min_tiles);
 }
 
 }  // namespace amk
@@ -157,7 +165,7 @@ namespace amk {
 // Tiles of 64 elements x 128 rows of 128 bytes, swizzled by TMA's 128-byte pattern: the 16-byte chunk c of row r lies
 // at r * 128 + ((c ^ (r & 7)) << 4).
 constexpr int kBox = 64 * kTile * 2;
-constexpr int kHeadBytes = 4096;
+constexpr int kHeadBytes = 5120;
 template <int HD, bool FP8>
 struct AttnSmem {
   static constexpr int kTileBytes = HD / 64 * kBox;                // one bf16 tile of 128 rows
@@ -181,7 +189,8 @@ struct AttnHead {
   float mx[2][2][kTile];               // [tile][half]: row maxima, and at the end row sums, of half the columns
   float m[kTile], l[kTile];            // the second tile's statistics (both tiles of the same rows)
   int unit[8];
-  int64_t walk[1];
+  int walk[16][8];                     // each softmax warp's place in the walk and its unit: registers are short there
+  Unit now[16];
 };
 static_assert(sizeof(AttnHead) <= kHeadBytes, "head");
 
@@ -236,30 +245,42 @@ struct Units;
 
 template <>
 struct Units<true> {
-  int64_t left;                    // key tiles of this block's run that are still to come
+  int left;                        // slots of this block's run that are still to come
   int seq, len, tiles, item, within, items;
   __device__ __forceinline__ void init(const AttnParams& p, const AttnHead& h) {
-    left = h.walk[0];
-    seq = h.unit[0], item = h.unit[1], within = h.unit[2], len = h.unit[3];
+    seq = h.unit[0], item = h.unit[1], within = h.unit[2], len = h.unit[3], left = h.unit[4];
     tiles = tree_tiles(p, len);
     items = p.nkv * p.row_tiles;
   }
+  // the state in shared memory, one copy for a warp
+  __device__ __forceinline__ void save(int* at, int lane) const {
+    __syncwarp();
+    if (lane == 0) at[0] = left, at[1] = seq, at[2] = len, at[3] = tiles, at[4] = item, at[5] = within;
+    __syncwarp();
+  }
+  __device__ __forceinline__ void restore(const volatile int* at) {
+    left = at[0], seq = at[1], len = at[2], tiles = at[3], item = at[4], within = at[5];
+  }
   __device__ __forceinline__ bool next(const AttnParams& p, const AttnHead&, Unit& u) {
-    if (left <= 0) return false;
-    while (item == items || tiles == 0) {   // something is left: a sequence with tiles follows
-      item = 0;
-      len = __ldg(p.lens + ++seq);
-      tiles = tree_tiles(p, len);
-    }
-    const int run = left < tiles - within ? (int)left : tiles - within;
-    u.seq = seq, u.head = p.row_tiles == 1 ? item : item / p.row_tiles, u.len = len;
-    u.row0 = (item - u.head * p.row_tiles) * p.part_rows;
+    int first, last;
+    do {
+      if (left <= 0) return false;
+      while (item == items || tiles == 0) {   // something is left: a sequence with tiles follows
+        item = 0;
+        len = __ldg(p.lens + ++seq);
+        tiles = tree_tiles(p, len);
+      }
+      const int run = min(left, tiles + kUnitCost - within);
+      first = max(within - kUnitCost, 0), last = within + run - kUnitCost;
+      left -= run;
+      within = 0;
+      item++;
+    } while (last <= first);                  // (only slots that stand for the beginning)
+    u.seq = seq, u.head = p.row_tiles == 1 ? item - 1 : (item - 1) / p.row_tiles, u.len = len;
+    u.row0 = (item - 1 - u.head * p.row_tiles) * p.part_rows;
     u.n_rows = min(p.part_rows, p.rows * p.rep - u.row0);
     u.tok0 = 0, u.n_tok = p.rows, u.key0 = 0;
-    u.tile_begin = within, u.tile_end = within + run, u.item_tiles = tiles;
-    left -= run;
-    within = 0;
-    item++;
+    u.tile_begin = first, u.tile_end = last, u.item_tiles = tiles;
     return true;
   }
 };
@@ -267,6 +288,8 @@ struct Units<true> {
 template <>
 struct Units<false> {
   bool more;
+  __device__ __forceinline__ void save(int*, int) const {}
+  __device__ __forceinline__ void restore(const volatile int*) {}
   __device__ __forceinline__ void init(const AttnParams&, const AttnHead& h) { more = h.unit[0] >= 0; }
   __device__ __forceinline__ bool next(const AttnParams& p, const AttnHead& h, Unit& u) {
     if (!more) return false;
@@ -373,36 +396,34 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
   if (warp == 0) {
     // which part of the work is this block's
     if (TREE) {
-      const int64_t total = tree_total(p, lane);
-      const int64_t per = tree_per_block(p, total, gridDim.x);
-      const int64_t at = (int64_t)blockIdx.x * per, end = at + per < total ? at + per : total;
-      int64_t before = 0;
-      int seq = 0, item = 0, within = 0, len = 0;
-      if (at < end) {
-        const int64_t items = (int64_t)p.nkv * p.row_tiles;
-        for (int b0 = 0;; b0 += 32) {
-          int64_t n = b0 + lane < p.n_seqs ? tree_tiles(p, p.lens[b0 + lane]) * items : 0;
-          const int64_t own = n;
+      const int mine = tree_slots_of(p, lane);
+      const int per = tree_run(p, mine, lane, gridDim.x);
+      int at = (int)blockIdx.x * per, seq = 0, item = 0, within = 0, len = 0, left = 0;
+      for (int b0 = 0; b0 < p.n_seqs; b0 += 32) {
+        const int own = b0 ? tree_slots_of(p, b0 + lane) : mine;
+        int n = own;
 #pragma unroll
-          for (int o = 1; o < 32; o <<= 1) {
-            const int64_t x = __shfl_up_sync(~0u, n, o);
-            if (lane >= o) n += x;
-          }
-          const unsigned hit = __ballot_sync(~0u, before + n > at);
-          if (hit) {
-            const int f = __ffs(hit) - 1;
-            seq = b0 + f;
-            before += __shfl_sync(~0u, n - own, f);
-            len = p.lens[seq];
-            const int tiles = tree_tiles(p, len);
-            const int64_t rel = at - before;
-            item = (int)(rel / tiles), within = (int)(rel - (int64_t)item * tiles);
-            break;
-          }
-          before += __shfl_sync(~0u, n, 31);
+        for (int o = 1; o < 32; o <<= 1) {
+          const int x = __shfl_up_sync(~0u, n, o);
+          if (lane >= o) n += x;
         }
+        const unsigned hit = __ballot_sync(~0u, n > at);
+        if (hit && !left) {
+          const int f = __ffs(hit) - 1;
+          seq = b0 + f;
+          len = __ldg(p.lens + seq);
+          const int rel = at - __shfl_sync(~0u, n - own, f), slots = tree_slots(tree_tiles(p, len));
+          item = rel / slots, within = rel - item * slots;
+          left = per;                                 // or less: what the sequences from here on have
+          at = 0;
+          int rest = (b0 + lane > seq ? own : 0) + (lane == f ? own - rel : 0);
+          for (int b = b0 + 32 + lane; rest < per && b < p.n_seqs; b += 32) rest += tree_slots_of(p, b);
+          left = min(per, warp_sum(min(rest, per)));
+          break;
+        }
+        at -= __shfl_sync(~0u, n, 31);
       }
-      if (lane == 0) h.walk[0] = end - at, h.unit[0] = seq, h.unit[1] = item, h.unit[2] = within, h.unit[3] = len;
+      if (lane == 0) h.unit[0] = seq, h.unit[1] = item, h.unit[2] = within, h.unit[3] = len, h.unit[4] = left;
     } else {
       // the blocks of all prompts in order; the last block of a long prompt has the most keys and goes first
       const int head = blockIdx.x % p.nkv, per = 2 * kTile / p.rep;
@@ -479,7 +500,16 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
     unsigned s_phase = 0, o_phase = 0;
     int ring = 0;                                     // ring position of the unit's first tile
     bool again = false;
-    while (units.next(p, h, u)) {
+    if (TREE) units.save(h.walk[warp], lane);
+    for (;;) {
+      if (TREE) units.restore(h.walk[warp]);
+      const bool more = units.next(p, h, u);
+      if (TREE) {
+        units.save(h.walk[warp], lane);
+        if (lane == 0) h.now[warp] = u;
+        __syncwarp();
+      }
+      if (!more) break;
       const int steps = unit_steps<TREE>(p, u, dual, t);
       const int row_first = u.row0 + (dual ? 0 : t * kTile);                       // first row of this tile
       const int rows_here = dual ? u.n_rows : u.n_rows - t * kTile;                // may be <= 0
@@ -603,8 +633,9 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
             }
           }
           float top = -CUDART_INF_F;
-#pragma unroll
-          for (int x = 0; x < 2; x++) {
+#pragma unroll 1
+          for (int x = 0; x < 2; x++) {                  // (rolled: this code is cold more often than not)
+            const unsigned sees = x ? see[1] : see[0];
             unsigned w[32];
             tmem_ld32(w, ts + half * 64 + x * 32);
             tmem_wait_ld();
@@ -612,7 +643,7 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
             if (masked) {
 #pragma unroll
               for (int k = 0; k < 32; k++)
-                if (!(see[x] >> k & 1)) w[k] = 0xff800000u;          // -infinity
+                if (!(sees >> k & 1)) w[k] = 0xff800000u;          // -infinity
             }
             float mx[4];
 #pragma unroll
@@ -650,8 +681,9 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
           const float mc = m == -CUDART_INF_F ? 0.f : -m * c;
           const uint64_t c2 = pair(c, c), mc2 = pair(mc, mc);
           uint64_t sum[2] = {0, 0};
-#pragma unroll
+#pragma unroll 1
           for (int x = 0; x < 2; x++) {
+            const unsigned sees = x ? see[1] : see[0];
             unsigned w[32], r[16];
             tmem_ld32(w, ts + half * 64 + x * 32);
             tmem_wait_ld();
@@ -659,7 +691,7 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
             if (masked) {
 #pragma unroll
               for (int k = 0; k < 32; k++)
-                if (!(see[x] >> k & 1)) w[k] = 0xff800000u;
+                if (!(sees >> k & 1)) w[k] = 0xff800000u;
             }
 #pragma unroll
             for (int k = 0; k < 32; k += 2) {
@@ -711,6 +743,11 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
         if (masked && id == 0) h.skip[t] = slow;
         warp_arrive(&h.p_full[t], lane);
       }
+      if (TREE) {
+        const volatile Unit& v = h.now[warp];
+        u.seq = v.seq, u.head = v.head, u.row0 = v.row0, u.n_rows = v.n_rows, u.tile_begin = v.tile_begin;
+        u.tile_end = v.tile_end, u.item_tiles = v.item_tiles;
+      }
       ring += 2 * (u.tile_end - u.tile_begin);
       if (steps) {
         attn_wait(&h.o_done[t], o_phase & 1, h);
@@ -754,27 +791,24 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
         const int64_t slot = TREE ? (int64_t)2 * blockIdx.x + (u.tile_begin == 0 ? 1 : 0) : 0;
         const int part_row = wr + (dual ? 0 : t * kTile);
 #pragma unroll 1
-        for (int x = half * (HD / 2); x < (half + 1) * (HD / 2); x += 32) {
-          unsigned o[32];
-          float v[32];
-          tmem_ld32(o, to + x);
+        for (int x = half * (HD / 2); x < (half + 1) * (HD / 2); x += 16) {
+          unsigned o[16], o1[16];
+          float v[16];
+          tmem_ld16(o, to + x);
+          if (two) tmem_ld16(o1, to + HD + x);
           tmem_wait_ld();
           tmem_pin(o);
+          if (two) tmem_pin(o1);
 #pragma unroll
-          for (int k = 0; k < 32; k++) v[k] = __uint_as_float(o[k]) * f0;
-          if (two) {
-            tmem_ld32(o, to + HD + x);
-            tmem_wait_ld();
-            tmem_pin(o);
-#pragma unroll
-            for (int k = 0; k < 32; k++) v[k] += __uint_as_float(o[k]) * f1;
+          for (int k = 0; k < 16; k++) {
+            v[k] = __uint_as_float(o[k]) * f0;
+            if (two) v[k] += __uint_as_float(o1[k]) * f1;
+            v[k] = l == 0.f ? 0.f : v[k] * inv;
           }
-#pragma unroll
-          for (int k = 0; k < 32; k++) v[k] = l == 0.f ? 0.f : v[k] * inv;
           if (whole) {
             // over the tile's Q, 16-byte chunks permuted within a row so that neither side meets a bank twice
 #pragma unroll
-            for (int k = 0; k < 32; k += 8)
+            for (int k = 0; k < 16; k += 8)
               *(uint4*)(qs + wr * (HD * 2) + (((x + k) / 8 ^ (wr & 7)) << 4)) =
                   make_uint4(pack_bf16(v[k], v[k + 1]), pack_bf16(v[k + 2], v[k + 3]), pack_bf16(v[k + 4], v[k + 5]),
                              pack_bf16(v[k + 6], v[k + 7]));
@@ -782,7 +816,7 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
             // [slot][column / 4][row][4]: a warp's rows lie side by side
             float* part = p.part_o + ((slot * (HD / 4) + x / 4) * p.part_rows + part_row) * 4;
 #pragma unroll
-            for (int k = 0; k < 32; k += 4) *(float4*)(part + (int64_t)k * p.part_rows) = make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
+            for (int k = 0; k < 16; k += 4) *(float4*)(part + (int64_t)k * p.part_rows) = make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
           }
         }
         if (whole) {
@@ -822,7 +856,7 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
     uint64_t* empty = FP8 ? h.raw_empty : h.empty;
     const bool leader = elect_one();
     unsigned issued = 0;
-    bool on = true, gate = TREE;
+    bool on = true, gate = TREE;                      // (gate: within the first unit)
     while (uniform(units.next(p, h, u))) {
       const int tile_end = uniform(u.tile_end);
       for (int j = uniform(u.tile_begin); j < tile_end; j++) {
@@ -849,6 +883,7 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
           issued++;
         }
       }
+      gate = false;
     }
     if (uniform(*(volatile int*)&h.dead)) {    // copies in flight land before the block ends
       for (unsigned i = issued > kN ? issued - kN : 0; i < issued; i++)
@@ -970,64 +1005,69 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
 // ---- parts of one item joined (tree) ----------------------------------------------------------------------------
 // Items whose tiles one block had are complete already; sequences of a bad length become NaN.
 //   O = sum_i w_i O_i / sum_i w_i,  w_i = 2^(lse_i - max): the parts carry O_i / l_i and log2 of their sums.
-// One thread for 16 columns of a row, neighbouring threads neighbouring rows.
+// A block takes 32 rows of one item, a thread 16 columns of one of them, neighbouring threads neighbouring rows.
+constexpr int kMaxBlocks = 160;                      // blocks of a tree call at most: the weights below lie in shared memory
 template <int HD>
-__global__ void __launch_bounds__(256) attn_join_kernel(const AttnParams p, int blocks) {
-  constexpr int kGroups = HD / 16, kRows = 256 / kGroups;
-  __shared__ int64_t sh[2];
+__global__ void __launch_bounds__(HD * 2) attn_join_kernel(const AttnParams p, int blocks) {
+  __shared__ int sh[2];
+  __shared__ float weight[kMaxBlocks][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int head = blockIdx.y, seq = blockIdx.z;
-  const int tiles = tree_tiles(p, p.lens[seq]);
+  const int head = blockIdx.y, seq = blockIdx.z, row = blockIdx.x * 32 + lane, col = warp * 16;
+  const int tiles = tree_tiles(p, __ldg(p.lens + seq));
   if (warp == 0) {
-    int64_t before = 0;
-    for (int b = lane; b < seq; b += 32) before += tree_tiles(p, p.lens[b]);
-#pragma unroll
-    for (int o = 16; o; o >>= 1) before += __shfl_xor_sync(~0u, before, o);
-    const int64_t total = tree_total(p, lane);
-    if (lane == 0) sh[0] = before * p.nkv * p.row_tiles, sh[1] = tree_per_block(p, total, blocks);
+    const int mine = tree_slots_of(p, lane);
+    const int per = tree_run(p, mine, lane, blocks);
+    int before = lane < seq ? mine : 0;
+    for (int b = 32 + lane; b < seq; b += 32) before += tree_slots_of(p, b);
+    before = warp_sum(before);
+    if (lane == 0) sh[0] = before, sh[1] = per;
   }
   __syncthreads();
+  const int rt = blockIdx.x * 32 / p.part_rows, local = row - rt * p.part_rows;
+  const int first = sh[0] + (head * p.row_tiles + rt) * tree_slots(tiles) + kUnitCost, per = sh[1];
+  const int c0 = first / per, parts = tiles ? (first + tiles - 1) / per - c0 + 1 : 0;
+  if (parts == 1) return;                            // complete already
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int row = blockIdx.x * kRows + threadIdx.x % kRows, col = threadIdx.x / kRows * 16;
-  if (row >= p.rows * p.rep) return;
-  const int tok = div_rep(p, row), q_head = head * p.rep + row - tok * p.rep;
-  float v[16] = {};
+  const bool valid = row < p.rows * p.rep;
+  auto slot = [&](int b) { return (int64_t)2 * (c0 + b) + (b == 0 ? 1 : 0); };
+  for (int b = warp; b < parts; b += HD / 16)
+    weight[b][lane] = valid ? p.part_lse[slot(b) * p.part_rows + local] : -CUDART_INF_F;
+  __syncthreads();
   float lse = CUDART_NAN_F;
-  if (tiles == 0) {
-#pragma unroll
-    for (int k = 0; k < 16; k++) v[k] = CUDART_NAN_F;
-  } else {
-    const int rt = row / p.part_rows;
-    const int64_t first = sh[0] + ((int64_t)head * p.row_tiles + rt) * tiles, per = sh[1];
-    const int c0 = (int)(first / per), c1 = (int)((first + tiles - 1) / per);
-    if (c0 == c1) return;
-    const int local = row - rt * p.part_rows;
-    auto slot = [&](int b) { return (int64_t)2 * b + (b == c0 ? 1 : 0); };
+  if (warp == 0 && parts) {
     float m = -CUDART_INF_F, sum = 0.f;
-    for (int b = c0; b <= c1; b++) m = fmaxf(m, p.part_lse[slot(b) * p.part_rows + local]);
-#pragma unroll 2
-    for (int b = c0; b <= c1; b++) {
-      const float x = p.part_lse[slot(b) * p.part_rows + local];
-      const float w = x == -CUDART_INF_F ? 0.f : exp2f(x - m);    // (all -infinity: nothing was seen)
+    for (int b = 0; b < parts; b++) m = fmaxf(m, weight[b][lane]);
+    for (int b = 0; b < parts; b++) {
+      const float x = weight[b][lane], w = x == -CUDART_INF_F ? 0.f : exp2f(x - m);   // (all -infinity: nothing was seen)
+      weight[b][lane] = w;
       sum += w;
-      const float* o = p.part_o + ((slot(b) * (HD / 4) + col / 4) * p.part_rows + local) * 4;
-#pragma unroll
-      for (int k = 0; k < 16; k += 4) {
-        const float4 y = *(const float4*)(o + (int64_t)k * p.part_rows);
-        v[k] += w * y.x, v[k + 1] += w * y.y, v[k + 2] += w * y.z, v[k + 3] += w * y.w;
-      }
     }
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
-#pragma unroll
-    for (int k = 0; k < 16; k++) v[k] *= inv;
+    for (int b = 0; b < parts; b++) weight[b][lane] *= inv;
     lse = sum == 0.f ? -CUDART_INF_F : (m + log2f(sum)) * 0.6931471805599453f;
   }
+  __syncthreads();
+  if (!valid) return;
+  float v[16];
+#pragma unroll
+  for (int k = 0; k < 16; k++) v[k] = parts ? 0.f : CUDART_NAN_F;
+#pragma unroll 4
+  for (int b = 0; b < parts; b++) {
+    const float w = weight[b][lane];
+    const float* o = p.part_o + ((slot(b) * (HD / 4) + col / 4) * p.part_rows + local) * 4;
+#pragma unroll
+    for (int k = 0; k < 16; k += 4) {
+      const float4 y = *(const float4*)(o + (int64_t)k * p.part_rows);
+      v[k] += w * y.x, v[k + 1] += w * y.y, v[k + 2] += w * y.z, v[k + 3] += w * y.w;
+    }
+  }
+  const int tok = div_rep(p, row), q_head = head * p.rep + row - tok * p.rep;
   __nv_bfloat16* out = p.out + (int64_t)seq * p.o_seq + tok * p.o_row + q_head * p.o_head + col;
 #pragma unroll
   for (int k = 0; k < 16; k += 8)
     *(uint4*)(out + k) = make_uint4(pack_bf16(v[k], v[k + 1]), pack_bf16(v[k + 2], v[k + 3]), pack_bf16(v[k + 4], v[k + 5]),
                                     pack_bf16(v[k + 6], v[k + 7]));
-  if (p.lse && col == 0) p.lse[((int64_t)seq * p.rows + tok) * p.nq + q_head] = lse;
+  if (p.lse && warp == 0) p.lse[((int64_t)seq * p.rows + tok) * p.nq + q_head] = lse;
 }
 
 }  // namespace amk

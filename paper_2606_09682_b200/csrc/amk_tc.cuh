@@ -74,6 +74,13 @@ __device__ __forceinline__ void tmem_ld32(unsigned (&r)[32], unsigned addr) {
         "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
       : "r"(addr));
 }
+__device__ __forceinline__ void tmem_ld16(unsigned (&r)[16], unsigned addr) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(addr));
+}
 __device__ __forceinline__ void tmem_st16(unsigned addr, const unsigned (&r)[16]) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(addr),
@@ -93,9 +100,10 @@ __device__ __forceinline__ void tmem_st32(unsigned addr, const unsigned (&r)[32]
 }
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 // Loaded registers may be used only behind the wait; nothing but this tells the compiler so.
-__device__ __forceinline__ void tmem_pin(unsigned (&r)[32]) {
+template <int N>
+__device__ __forceinline__ void tmem_pin(unsigned (&r)[N]) {
 #pragma unroll
-  for (int i = 0; i < 32; i++) asm volatile("" : "+r"(r[i])::"memory");
+  for (int i = 0; i < N; i++) asm volatile("" : "+r"(r[i])::"memory");
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
