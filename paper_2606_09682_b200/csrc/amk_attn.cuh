@@ -165,7 +165,7 @@ namespace amk {
 // Tiles of 64 elements x 128 rows of 128 bytes, swizzled by TMA's 128-byte pattern: the 16-byte chunk c of row r lies
 // at r * 128 + ((c ^ (r & 7)) << 4).
 constexpr int kBox = 64 * kTile * 2;
-constexpr int kHeadBytes = 5120;
+constexpr int kHeadBytes = 7168;
 template <int HD, bool FP8>
 struct AttnSmem {
   static constexpr int kTileBytes = HD / 64 * kBox;                // one bf16 tile of 128 rows
@@ -191,6 +191,7 @@ struct AttnHead {
   int unit[8];
   int walk[16][8];                     // each softmax warp's place in the walk and its unit: registers are short there
   Unit now[16];
+  unsigned long long word0[2][kTile];  // first word of each row's mask
 };
 static_assert(sizeof(AttnHead) <= kHeadBytes, "head");
 
@@ -313,6 +314,10 @@ __device__ __forceinline__ int unit_steps(const AttnParams& p, const Unit& u, bo
   return (u.tok0 + div_rep(p, last)) / kTile + 1;
 }
 
+// the mask words of a drafted token (tokens behind the last: rows that nobody reads)
+__device__ __forceinline__ int64_t mask_at(const AttnParams& p, int seq, int tok) {
+  return ((int64_t)seq * p.rows + min(tok, p.rows - 1)) * ((p.rows + 63) / 64);
+}
 // 32 bits of a drafted token's mask from drafted index idx on (idx may be negative: bits below 0 are 0).  w0 is the
 // mask's first word, w its words; without a mask (w null) a chain: indices 0..tok.
 __device__ __forceinline__ unsigned tree_bits32(const unsigned long long* w, unsigned long long w0, int rows, int tok, int idx) {
@@ -504,24 +509,18 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
     for (;;) {
       if (TREE) units.restore(h.walk[warp]);
       const bool more = units.next(p, h, u);
-      if (TREE) {
-        units.save(h.walk[warp], lane);
-        if (lane == 0) h.now[warp] = u;
-        __syncwarp();
-      }
+      if (TREE) units.save(h.walk[warp], lane);
+      if (lane == 0) h.now[warp] = u;
+      __syncwarp();
       if (!more) break;
       const int steps = unit_steps<TREE>(p, u, dual, t);
       const int row_first = u.row0 + (dual ? 0 : t * kTile);                       // first row of this tile
       const int rows_here = dual ? u.n_rows : u.n_rows - t * kTile;                // may be <= 0
       const unsigned short* q = p.q + (int64_t)u.seq * p.q_seq + (int64_t)(u.key0 + u.tok0) * p.q_row +
                                 (int64_t)u.head * p.rep * p.q_head;
-      const int row = row_first + wr, tok = div_rep(p, row), hh = row - tok * p.rep;
-      const bool valid = wr < rows_here;
       const bool live = quarter * 32 < rows_here;      // this warp has rows; the others only keep step
       if (again && steps) named_barrier(tile_id, 256); // the last unit's output has left the tile's shared memory
       again = true;
-      const unsigned long long* words = nullptr;
-      unsigned long long word0 = 0;
       if (steps) {
         // Q, 16 bytes at a time, all loads in flight before the first store; rows that do not exist are zero
         constexpr int kChunks = HD / 8, kEach = kTile * kChunks / 256;
@@ -535,10 +534,8 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
             v[i] = __ldg((const uint4*)(q + tok * p.q_row + hh * p.q_head + ch * 8));
           }
         }
-        if (TREE && p.mask) {
-          words = p.mask + ((int64_t)u.seq * p.rows + min(tok, p.rows - 1)) * ((p.rows + 63) / 64);
-          word0 = __ldg(words);
-        }
+        if (TREE && p.mask && half == 0)
+          h.word0[t][wr] = __ldg(p.mask + mask_at(p, u.seq, div_rep(p, row_first + wr)));
 #pragma unroll
         for (int i = 0; i < kEach; i++) {
           const int e = i * 256 + id, r = e / kChunks, ch = e % kChunks;
@@ -561,14 +558,14 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
           }
         }
       }
-      const int key_end = TREE ? u.len + p.rows : u.tok0 + u.n_tok;                // keys nobody here sees: from it on
-      // first key that a row of this tile may not see
-      const int all_see = TREE ? u.len : u.tok0 + div_rep(p, row_first) + 1;
+      // first step whose tile holds a key that a row of this tile may not see
+      const int clear = max((TREE ? u.len : u.tok0 + div_rep(p, row_first) + 1) / kTile - u.tile_begin, 0);
+      const int mask_from = dual ? (clear - t + 1) >> 1 : clear;
       float m = -CUDART_INF_F, l = 0.f;
+      // What the steps need of the unit they read from shared memory: a register spilled here would be fetched from behind
+      // the stream of tiles.
       for (int i = 0; i < steps; i++) {
-        const int rel = dual ? 2 * i + t : i;
-        const int key = (u.tile_begin + rel) * kTile;
-        const bool masked = key + kTile > all_see;
+        const bool masked = i >= mask_from;
         attn_wait(&h.s_full[t], s_phase & 1, h);
         s_phase++;
         __syncwarp();
@@ -620,14 +617,18 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
         // it, and spilled registers would travel behind the stream of tiles.
         if (live && exact) {
           if (masked) {
+            const volatile Unit& v = h.now[warp];
+            const int row = v.row0 + (dual ? 0 : t * kTile) + wr, tok = div_rep(p, row);
 #pragma unroll
             for (int w = 0; w < 2; w++) {
-              const int first = key + half * 64 + 32 * w;
+              const int first = (v.tile_begin + (dual ? 2 * i + t : i)) * kTile + half * 64 + 32 * w;
               if (TREE) {
-                const int ctx = u.len - first;                      // context keys from `first` on
-                if (ctx < 32) see[w] = (ctx > 0 ? (1u << ctx) - 1u : 0u) | tree_bits32(words, word0, p.rows, tok, -ctx);
+                const int ctx = v.len - first;                      // context keys from `first` on
+                if (ctx < 32)
+                  see[w] = (ctx > 0 ? (1u << ctx) - 1u : 0u) |
+                           tree_bits32(p.mask ? p.mask + mask_at(p, v.seq, tok) : nullptr, h.word0[t][wr], p.rows, tok, -ctx);
               } else {
-                const int n = u.tok0 + tok + 1 - first;
+                const int n = v.tok0 + tok + 1 - first;
                 see[w] = n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u;
               }
             }
@@ -711,6 +712,9 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
         if (masked) {
           // What a mask hides must not come through 0 * V either: V rows that no row of the block sees become zero; if
           // a row that some of them see is not finite, this tile's product is made here, key by key.
+          const volatile Unit& u = h.now[warp];
+          const int rel = dual ? 2 * i + t : i, key = (u.tile_begin + rel) * kTile;
+          const int key_end = TREE ? u.len + p.rows : u.tok0 + u.n_tok;      // keys nobody here sees: from it on
           const int pos = ring + 2 * rel + 1, st = pos % L::kStages;
           attn_wait(&h.full[st], pos / L::kStages & 1, h);
           unsigned char* vt = smem + L::kRing + st * L::kTileBytes;
@@ -743,10 +747,10 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
         if (masked && id == 0) h.skip[t] = slow;
         warp_arrive(&h.p_full[t], lane);
       }
-      if (TREE) {
+      {
         const volatile Unit& v = h.now[warp];
-        u.seq = v.seq, u.head = v.head, u.row0 = v.row0, u.n_rows = v.n_rows, u.tile_begin = v.tile_begin;
-        u.tile_end = v.tile_end, u.item_tiles = v.item_tiles;
+        u.seq = v.seq, u.head = v.head, u.row0 = v.row0, u.n_rows = v.n_rows, u.key0 = v.key0, u.tok0 = v.tok0;
+        u.tile_begin = v.tile_begin, u.tile_end = v.tile_end, u.item_tiles = v.item_tiles;
       }
       ring += 2 * (u.tile_end - u.tile_begin);
       if (steps) {
@@ -763,6 +767,9 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
       }
 
       // O / l, or this block's part of it
+      const int first_row = u.row0 + (dual ? 0 : t * kTile), n_here = dual ? u.n_rows : u.n_rows - t * kTile;
+      const int row = first_row + wr, tok = div_rep(p, row), hh = row - tok * p.rep;
+      const bool valid = wr < n_here;
       float f0 = 1.f, f1 = 0.f;
       bool two = false;
       if (dual) {
@@ -827,8 +834,8 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
 #pragma unroll
           for (int i = 0; i < 32 * kChunks / 64; i++) {
             const int e = i * 64 + half * 32 + lane, r = quarter * 32 + e / kChunks, ch = e % kChunks;
-            if (r < rows_here) {
-              const int row = row_first + r, tok = div_rep(p, row), hh = row - tok * p.rep;
+            if (r < n_here) {
+              const int row = first_row + r, tok = div_rep(p, row), hh = row - tok * p.rep;
               *(uint4*)(out + tok * p.o_row + hh * p.o_head + ch * 8) =
                   *(const uint4*)(qs + r * (HD * 2) + ((ch ^ (r & 7)) << 4));
             }
