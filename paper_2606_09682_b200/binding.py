@@ -440,13 +440,12 @@ def amk_token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, top_k: int = 
         _refuse(name, "the last dimension must be contiguous")
     if top_k < 0:
         _refuse(name, "top_k is negative")
-    both = torch.empty((2, rows), dtype=torch.float32, device=dev)
+    logprob = torch.empty(rows, dtype=torch.float32, device=dev)
+    entropy = torch.empty(rows, dtype=torch.float32, device=dev)
     top_tokens = torch.empty((rows, top_k), dtype=torch.int32, device=dev)
     top_logprobs = torch.empty((rows, top_k), dtype=torch.float32, device=dev)
-    p = both.data_ptr()
     _run(lib.amk_token_logprobs, name, dev, logits.data_ptr(), 1 if dtype is torch.bfloat16 else 0, rows, vocab, stride,
-         tokens.data_ptr(), top_k, p, p + 4 * rows, top_tokens.data_ptr(), top_logprobs.data_ptr())
-    logprob, entropy = both.unbind(0)
+         tokens.data_ptr(), top_k, logprob.data_ptr(), entropy.data_ptr(), top_tokens.data_ptr(), top_logprobs.data_ptr())
     return logprob, entropy, top_tokens, top_logprobs
 
 

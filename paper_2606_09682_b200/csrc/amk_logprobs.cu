@@ -1,15 +1,15 @@
 // amk_token_logprobs: log probabilities of given tokens, row entropies and top alternatives, in one pass over the logits.
 //
-// Mathematics.  With a reference r (the running maximum) and y = (x - r) log2 e, a thread sums s = sum 2^y and
-// t = sum 2^y y over its share of the row; when the maximum rises by d (in log2), s' = 2^-d s and t' = 2^-d (t - d s).
-// Shares are joined the same way: log probability of x = (x - m) - ln s, entropy = ln s - ln 2 t / s.
+// Mathematics.  With the running maximum r, R = r log2 e rounded and y = x log2 e - R, a thread sums s = sum 2^y and
+// t = sum 2^y y over its share of the row; when R rises by d, s' = 2^-d s and t' = 2^-d (t - d s).  Shares are joined the
+// same way: log probability of x = (x - r) - ln s + ln 2 (r log2 e - R), entropy = ln s - ln 2 t / s.
 //
 // Alternatives.  Sorting is kept out of the pass: a thread keeps only the maximum of its share.  The k-th largest of
 // those maxima is a lower bound of the k-th largest logit, so the alternatives lie in the shares whose maximum reaches
 // it -- about k of the 256 -- and only those are read again (from L2), into sorted lists of 32 keys, one lane each, that
 // are merged pairwise: {value, lowest index first} as one 64-bit key.
 //
-// Bound: HBM (the logits once).  A row is one block's, or with few rows a cluster's of up to eight, whose parts meet
+// Bound: HBM (the logits once).  A row is one block's, or with few rows a cluster's of up to four, whose parts meet
 // in distributed shared memory: one launch, no scratch.
 #include <cuda_runtime.h>
 #include <math_constants.h>
@@ -20,7 +20,7 @@
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kUnroll = 4;                    // 16-byte loads a thread has in flight
+constexpr int kUnroll = 4;                    // 16-byte pieces that a thread takes at a time
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr unsigned kAll = 0xffffffffu;
 
@@ -64,11 +64,45 @@ __device__ __forceinline__ float key_value(unsigned long long k) {
   return __uint_as_float((u >> 31) ? u & 0x7fffffffu : ~u);
 }
 
-// a share's sums: reference, sum of 2^y, sum of 2^y y
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+__device__ __forceinline__ float min3(float a, float b, float c) {
+  float d;
+  asm("min.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+// two fp32 lanes in one instruction
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+  uint64_t d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
+  return d;
+}
+__device__ __forceinline__ void unpair(float& lo, float& hi, uint64_t a) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(a));
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+
+// A share's sums, for a reference r (the largest x so far): y = x log2 e - R with R the rounded r log2 e is one fused
+// multiply-add; what the rounding of R leaves, eps(r), is in every y alike and taken out of the logarithm at the end.
+constexpr float kLowest = -3.402823466e38f, kFar = 1.0e30f;
+__device__ __forceinline__ float ref(float r) { return fminf(fmaxf(r * kLog2e, kLowest), -kLowest); }
+__device__ __forceinline__ float eps(float r) { return fabsf(r) < kFar ? fmaf(r, kLog2e, -ref(r)) : 0.f; }
 struct Sums {
-  float r, s, t;
+  float r, s, t;                                             // reference, sum of 2^y, sum of 2^y y
   __device__ __forceinline__ void raise(float to) {            // a finite reference, not below the old one
-    const float d = fminf((to - r) * kLog2e, 1000.f);          // (2^-1000 is 0 here; keeps 0 * d from being NaN)
+    const float d = fminf(ref(to) - ref(r), 1000.f);           // (2^-1000 is 0 here; keeps 0 * d from being NaN)
     const float f = exp2_fast(-d);
     t = f * (t - d * s);
     s *= f;
@@ -80,14 +114,16 @@ struct Sums {
     else o.raise(r);
     s += o.s, t += o.t;
   }
-  __device__ __forceinline__ void add(float x) {
-    const float y = fmaxf((x - r) * kLog2e, -200.f);           // -infinity: 0, not 0 * infinity
+  __device__ __forceinline__ void see(float mx) {              // (infinity and NaN spoil the row's results anyway)
+    if (mx > r && mx < CUDART_INF_F) raise(mx);
+  }
+  __device__ __forceinline__ void add(float x) {               // any x: -infinity and the lowest value are 0, not 0 * infinity
+    const float y = fmaxf(fmaf(x - r, kLog2e, eps(r)), -200.f);
     const float e = exp2_fast(y);
     s += e;
     t = fmaf(e, y, t);
   }
 };
-constexpr float kLowest = -3.402823466e38f;
 
 // ---- lists of 32, one lane each, descending ---------------------------------------------------------------------
 template <class K>
@@ -152,10 +188,11 @@ __device__ __forceinline__ unsigned long long remote_u64(const void* p, unsigned
   return v;
 }
 
-// C blocks a row.  Of a block's part, thread f has the 16-byte pieces f, f + 256, ...; the first block's threads also one
+// C blocks a row.  Blocks on an SM: 5 for fp32, 3 for bf16 (its 32 values at a time need the registers; measured with 2001
+// rows of 128256: 5 blocks 192 us, 4 119 us, 3 96 us; 600 fp32 rows: 3 blocks 59 us, 4 65 us, 5 52 us).  Of a block's part, thread f has the 16-byte pieces f, f + 256, ...; the first block's threads also one
 // element each in front of the first piece, the last block's one behind the last.
 template <class T>
-__global__ void __launch_bounds__(kThreads, 4) logprobs_kernel(const T* __restrict__ logits, const Args a, int C) {
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 5 : 3) logprobs_kernel(const T* __restrict__ logits, const Args a, int C) {
   constexpr int kVec = 16 / sizeof(T);
   __shared__ unsigned long long lists[kWarps][32];
   __shared__ float part[4];                          // this block's reference, sums, NaN flag
@@ -178,28 +215,91 @@ __global__ void __launch_bounds__(kThreads, 4) logprobs_kernel(const T* __restri
   auto single = [&](int i) {
     const float v = load(x, i);
     top = max_nan(top, v);
-    if (v > sum.r && v < CUDART_INF_F) sum.raise(v);
+    sum.see(v);
     sum.add(v);
   };
   if (rank == 0 && (int)threadIdx.x < head) single(threadIdx.x);
-  for (int i0 = threadIdx.x; i0 < n; i0 += kUnroll * kThreads) {
+  int at = threadIdx.x;                              // kUnroll pieces at a time, the next ones on their way
+  {
     uint4 u[kUnroll];
+    bool more = at + (kUnroll - 1) * kThreads < n;
+    if (more) {
 #pragma unroll
-    for (int j = 0; j < kUnroll; j++)
-      if (i0 + j * kThreads < n) u[j] = __ldg(v4 + i0 + j * kThreads);
-#pragma unroll
-    for (int j = 0; j < kUnroll; j++) {
-      if (i0 + j * kThreads >= n) break;
-      float v[kVec];
-      widen(v, u[j]);
-      float mx = v[0];
-#pragma unroll
-      for (int k = 1; k < kVec; k++) mx = max_nan(mx, v[k]);
-      top = max_nan(top, mx);
-      if (mx > sum.r && mx < CUDART_INF_F) sum.raise(mx);
-#pragma unroll
-      for (int k = 0; k < kVec; k++) sum.add(v[k]);
+      for (int j = 0; j < kUnroll; j++) u[j] = __ldg(v4 + at + j * kThreads);
     }
+    uint64_t s2 = pair(sum.s, 0.f), t2 = pair(sum.t, 0.f);
+    while (more) {
+      at += kUnroll * kThreads;
+      more = at + (kUnroll - 1) * kThreads < n;
+      uint4 next[kUnroll];
+      if (more) {
+#pragma unroll
+        for (int j = 0; j < kUnroll; j++) next[j] = __ldg(v4 + at + j * kThreads);
+      }
+      float mx = -CUDART_INF_F, mn = CUDART_INF_F;
+#pragma unroll
+      for (int j = 0; j < kUnroll; j++) {
+        float v[kVec];
+        widen(v, u[j]);
+#pragma unroll
+        for (int k = 0; k < kVec; k += 2) mx = max3_nan(mx, v[k], v[k + 1]), mn = min3(mn, v[k], v[k + 1]);
+      }
+      top = max_nan(top, mx);
+      const bool rises = mx > sum.r, masked = mn < -kFar || mx > kFar;
+      if (rises || masked) {
+        float a0, a1;
+        unpair(a0, a1, s2);
+        sum.s = a0 + a1;
+        unpair(a0, a1, t2);
+        sum.t = a0 + a1;
+        sum.see(mx);
+        if (masked) {
+#pragma unroll 1
+          for (int j = 0; j < kUnroll; j++) {
+            float v[kVec];
+            widen(v, j == 0 ? u[0] : j == 1 ? u[1] : j == 2 ? u[2] : u[3]);
+#pragma unroll
+            for (int k = 0; k < kVec; k++) sum.add(v[k]);
+          }
+        }
+        s2 = pair(sum.s, 0.f), t2 = pair(sum.t, 0.f);
+      }
+      if (!masked) {
+        const uint64_t l2 = pair(kLog2e, kLog2e), r2 = pair(-ref(sum.r), -ref(sum.r));
+#pragma unroll
+        for (int j = 0; j < kUnroll; j++) {
+          float v[kVec];
+          widen(v, u[j]);
+#pragma unroll
+          for (int k = 0; k < kVec; k += 2) {
+            const uint64_t y = fma2(pair(v[k], v[k + 1]), l2, r2);
+            float y0, y1;
+            unpair(y0, y1, y);
+            const uint64_t e = pair(exp2_fast(y0), exp2_fast(y1));
+            s2 = add2(s2, e);
+            t2 = fma2(e, y, t2);
+          }
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < kUnroll; j++) u[j] = next[j];
+    }
+    float a0, a1;
+    unpair(a0, a1, s2);
+    sum.s = a0 + a1;
+    unpair(a0, a1, t2);
+    sum.t = a0 + a1;
+  }
+  for (; at < n; at += kThreads) {
+    float v[kVec];
+    widen(v, __ldg(v4 + at));
+    float mx = v[0];
+#pragma unroll
+    for (int k = 1; k < kVec; k++) mx = max_nan(mx, v[k]);
+    top = max_nan(top, mx);
+    sum.see(mx);
+#pragma unroll
+    for (int k = 0; k < kVec; k++) sum.add(v[k]);
   }
   if (rank == (unsigned)C - 1 && (int)threadIdx.x < tail) single(head + pieces * kVec + threadIdx.x);
   const bool share_nan = top != top;
@@ -224,6 +324,7 @@ __global__ void __launch_bounds__(kThreads, 4) logprobs_kernel(const T* __restri
     if (threadIdx.x == 0) bound = __uint_as_float(kth);
     __syncthreads();
     const unsigned low = __float_as_uint(bound);
+    const float lowest = low ? key_value((unsigned long long)low << 32) : -CUDART_INF_F;
     const unsigned f = __ballot_sync(kAll, share_nan || (mine && mine >= low));
     if (lane == 0) flagged[warp] = f;
     __syncthreads();
@@ -255,17 +356,15 @@ __global__ void __launch_bounds__(kThreads, 4) logprobs_kernel(const T* __restri
         for (int i0 = share; i0 < n; i0 += 32 * kThreads) {
           const int i = i0 + lane * kThreads;
           float v[kVec];
+          float mx = CUDART_NAN_F;
           if (i < n) {
             widen(v, __ldg(v4 + i));
-          } else {
 #pragma unroll
-            for (int k = 0; k < kVec; k++) v[k] = CUDART_NAN_F;
+            for (int k = 0; k < kVec; k++) mx = fmaxf(mx, v[k]);
           }
+          if (!__any_sync(kAll, mx >= lowest)) continue;
 #pragma unroll
-          for (int k = 0; k < kVec; k++) {
-            const unsigned long long key = key_of(v[k], base + i * kVec + k);
-            take((unsigned)(key >> 32) >= low ? key : 0);
-          }
+          for (int k = 0; k < kVec; k++) take(mx >= lowest && v[k] >= lowest ? key_of(v[k], base + i * kVec + k) : 0);
         }
       }
     }
@@ -304,15 +403,16 @@ __global__ void __launch_bounds__(kThreads, 4) logprobs_kernel(const T* __restri
   m = __shfl_sync(kAll, m, 0);
   const float s = __shfl_sync(kAll, sum.s, 0), t = __shfl_sync(kAll, sum.t, 0);
   const float r0 = __shfl_sync(kAll, sum.r, 0);
-  const float ls = fabsf(m) < CUDART_INF_F ? logf(s) : CUDART_NAN_F;   // no finite maximum, or a NaN
+  // NaN without a finite maximum, or with a NaN
+  const float ls = fabsf(m) < CUDART_INF_F ? logf(s) : CUDART_NAN_F, from_r = fmaf(-kLn2, eps(r0), ls);
   if (lane == 0) {
     const int tok = a.tokens[row];
-    if (a.lp) a.lp[row] = tok < 0 || tok >= vocab ? CUDART_NAN_F : load(x, tok) - r0 - ls;
+    if (a.lp) a.lp[row] = tok < 0 || tok >= vocab ? CUDART_NAN_F : load(x, tok) - r0 - from_r;
     if (a.ent) a.ent[row] = fmaf(-kLn2, t / s, ls);
   }
   if (lane < a.top) {
     a.top_id[row * a.top + lane] = best ? (int)(0xffffffffu - (unsigned)best) : -1;
-    a.top_lp[row * a.top + lane] = best ? key_value(best) - r0 - ls : CUDART_NAN_F;
+    a.top_lp[row * a.top + lane] = best ? key_value(best) - r0 - from_r : CUDART_NAN_F;
   }
 }
 
@@ -355,12 +455,13 @@ extern "C" amk_status amk_token_logprobs(const void* logits, uint32_t dtype, int
       !amk::aligned(entropy, 4) || !amk::aligned(top_tokens, 4) || !amk::aligned(top_logprobs, 4))
     return fail(AMK_ERR_INVALID_ARG, "pointers must be aligned to their elements");
   const Args a{vocab, row_stride, tokens, (int)top_k, logprob, entropy, top_tokens, top_logprobs};
-  // Blocks a row: doubled until there are two for each SM, while a block keeps 2048 logits.  (64 rows of 128256 fp32
-  // logits, top 20: 1 block a row 34 us, 8 blocks 15 us.)
+  // Blocks a row: doubled until there are two for each SM, while a block keeps 2048 logits.  (Top 20 of fp32
+  // logits, 1 / 2 / 4 / 8 blocks a row: one row of 32000 9.9 / 9.3 / 9.1 / 10.3 us, 64 of 128256 25 / 17 / 14 / 17 us, 200 of
+  // 128256 40 / 28 / 34 / 49 us.)
   int dev = 0, sms = 148, C = 1;
   if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
     (void)cudaGetLastError();
-  while (C < 8 && rows * C < 2 * sms && vocab / (2 * C) >= 2048) C *= 2;
+  while (C < 4 && rows * C < 2 * sms && vocab / (2 * C) >= 2048) C *= 2;
   const cudaStream_t st = (cudaStream_t)cuda_stream;
   const cudaError_t e = dtype ? launch<unsigned short>(logits, a, rows, C, st) : launch<float>(logits, a, rows, C, st);
   return e == cudaSuccess ? AMK_OK : fail(AMK_ERR_CUDA, "launch failed: %s", cudaGetErrorString(e));
