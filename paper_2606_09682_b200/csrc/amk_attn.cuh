@@ -114,10 +114,34 @@ __device__ __forceinline__ void exp2_poly(float& e0, float& e1, uint64_t x) {
   e0 = __uint_as_float(__float_as_uint(y0) + (__float_as_uint(t0) << 23));
   e1 = __uint_as_float(__float_as_uint(y1) + (__float_as_uint(t1) << 23));
 }
-// acc + 0 * w for two bf16 at once: NaN from the first value on that is not finite
+// Four e4m3 codes to four f16, exactly, NaN included.
+__device__ __forceinline__ void widen_e4m3(unsigned* w, unsigned codes) {
+  asm("{ .reg .b16 l, h; mov.b32 {l, h}, %2; cvt.rn.f16x2.e4m3x2 %0, l; cvt.rn.f16x2.e4m3x2 %1, h; }"
+      : "=r"(w[0]), "=r"(w[1])
+      : "r"(codes));
+}
+__device__ __forceinline__ unsigned pack_f16(float lo, float hi) {    // round to nearest even
+  unsigned r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ void unpack_f16(float& lo, float& hi, unsigned w) {
+  asm("{ .reg .b16 a, b; mov.b32 {a, b}, %2; cvt.f32.f16 %0, a; cvt.f32.f16 %1, b; }" : "=f"(lo), "=f"(hi) : "r"(w));
+}
+// Operands of the matrix instructions: bf16, or f16 over the 8-bit cache (see attn_kernel).
+template <bool HALF>
+__device__ __forceinline__ unsigned pack2(float lo, float hi) { return HALF ? pack_f16(lo, hi) : pack_bf16(lo, hi); }
+template <bool HALF>
+__device__ __forceinline__ void unpack2(float& lo, float& hi, unsigned w) {
+  if (HALF) unpack_f16(lo, hi, w);
+  else lo = bf16_lo(w), hi = bf16_hi(w);
+}
+// acc + 0 * w for two operands at once: NaN from the first value on that is not finite
+template <bool HALF>
 __device__ __forceinline__ unsigned zero_times(unsigned w, unsigned acc) {
   unsigned d;
-  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(w), "r"(0u), "r"(acc));
+  if (HALF) asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(w), "r"(0u), "r"(acc));
+  else asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(w), "r"(0u), "r"(acc));
   return d;
 }
 
@@ -165,7 +189,7 @@ namespace amk {
 // Tiles of 64 elements x 128 rows of 128 bytes, swizzled by TMA's 128-byte pattern: the 16-byte chunk c of row r lies
 // at r * 128 + ((c ^ (r & 7)) << 4).
 constexpr int kBox = 64 * kTile * 2;
-constexpr int kHeadBytes = 7168;
+constexpr int kHeadBytes = 8192;
 template <int HD, bool FP8>
 struct AttnSmem {
   static constexpr int kTileBytes = HD / 64 * kBox;                // one bf16 tile of 128 rows
@@ -191,6 +215,7 @@ struct AttnHead {
   int unit[8];
   int walk[16][8];                     // each softmax warp's place in the walk and its unit: registers are short there
   Unit now[16];
+  float row_c[2][kTile];               // 8-bit cache: scale * log2 e over the power of two that each row of Q was multiplied by
   unsigned long long word0[2][kTile];  // first word of each row's mask
 };
 static_assert(sizeof(AttnHead) <= kHeadBytes, "head");
@@ -343,7 +368,7 @@ __device__ __forceinline__ unsigned tree_bits32(const unsigned long long* w, uns
 // O += P V of 64 keys for this warp's rows, key by key and only for the keys that a row sees: for tiles with values that
 // are not finite behind a mask, where 0 * V would not be 0.  P in TMEM as the matrix unit would read it; vt: the tile, used
 // from its row `key` on.
-template <int HD>
+template <int HD, bool HALF>
 __device__ __noinline__ void product_by_key(unsigned tp, unsigned see0, unsigned see1, const unsigned char* vt, int key,
                                             unsigned to, bool more) {
   float pl[64];                                        // (in local memory: walked by key)
@@ -353,7 +378,7 @@ __device__ __noinline__ void product_by_key(unsigned tp, unsigned see0, unsigned
     tmem_wait_ld();
     tmem_pin(r);
 #pragma unroll
-    for (int k = 0; k < 32; k++) pl[2 * k] = bf16_lo(r[k]), pl[2 * k + 1] = bf16_hi(r[k]);
+    for (int k = 0; k < 32; k++) unpack2<HALF>(pl[2 * k], pl[2 * k + 1], r[k]);
   }
   for (int x = 0; x < HD; x += 32) {
     unsigned o[32];
@@ -373,8 +398,10 @@ __device__ __noinline__ void product_by_key(unsigned tp, unsigned see0, unsigned
         const unsigned vv[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
         for (int e = 0; e < 4; e++) {
-          a[ch * 8 + 2 * e] += pl[k] * bf16_lo(vv[e]);
-          a[ch * 8 + 2 * e + 1] += pl[k] * bf16_hi(vv[e]);
+          float v0, v1;
+          unpack2<HALF>(v0, v1, vv[e]);
+          a[ch * 8 + 2 * e] += pl[k] * v0;
+          a[ch * 8 + 2 * e + 1] += pl[k] * v1;
         }
       }
     }
@@ -386,6 +413,9 @@ __device__ __noinline__ void product_by_key(unsigned tp, unsigned see0, unsigned
   tmem_wait_st();
 }
 
+// Over the 8-bit cache the matrix instructions work on f16: every e4m3 code is an f16 by one conversion (to bf16 it takes
+// three more, and the six warps that widen the tiles bound the kernel), P has three bits more than in bf16, and a row of Q
+// is exact in f16 after a power of two.
 // ---- the kernel -------------------------------------------------------------------------------------------------
 template <int HD, bool TREE, bool FP8>
 __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
@@ -461,8 +491,8 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
   if (warp == kIssuer) {
     tmem_alloc(&h.tmem, 512);
     if (lane == 0) {
-      for (int i = 0; i < L::kStages; i++) mbar_init(&h.full[i], FP8 ? 4 : 1), mbar_init(&h.empty[i], 1);
-      for (int i = 0; i < L::kRawStages; i++) mbar_init(&h.raw_full[i], 1), mbar_init(&h.raw_empty[i], 4);
+      for (int i = 0; i < L::kStages; i++) mbar_init(&h.full[i], FP8 ? 6 : 1), mbar_init(&h.empty[i], 1);
+      for (int i = 0; i < L::kRawStages; i++) mbar_init(&h.raw_full[i], 1), mbar_init(&h.raw_empty[i], 6);
       for (int t = 0; t < 2; t++) {
         mbar_init(&h.q_full[t], 8), mbar_init(&h.s_full[t], 1);
         mbar_init(&h.p_full[t], 8), mbar_init(&h.o_done[t], 1);
@@ -488,10 +518,9 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
     if (warp < 16) asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
     else asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
   } else {
-    // 768 threads of 80 registers at launch: 512 x 96 + 128 x 56 + 128 x 40 = 61440, all of them
+    // 768 threads of 80 registers at launch: 512 x 96 + 256 x 48 = 61440, all of them
     if (warp < 16) asm volatile("setmaxnreg.inc.sync.aligned.u32 96;");
-    else if (warp < 20) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-    else asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+    else asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
   }
 
   if (warp < 16) {
@@ -501,7 +530,7 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
     const unsigned lanes = (unsigned)quarter * 32 << 16;
     const unsigned ts = tmem + lanes + t * kTile, to = tmem + lanes + 2 * kTile + t * HD;
     unsigned char* qs = smem + L::kQ + t * L::kTileBytes;
-    const float c = p.scale * kLog2e;
+    float c = p.scale * kLog2e;
     unsigned s_phase = 0, o_phase = 0;
     int ring = 0;                                     // ring position of the unit's first tile
     bool again = false;
@@ -536,6 +565,26 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
         }
         if (TREE && p.mask && half == 0)
           h.word0[t][wr] = __ldg(p.mask + mask_at(p, u.seq, div_rep(p, row_first + wr)));
+        if (FP8) {
+          // to f16, each row times the power of two that brings its largest value to 2^14..2^15: exact but for what is
+          // 2^-30 of that.  A row's chunks lie in neighbouring lanes.
+#pragma unroll
+          for (int i = 0; i < kEach; i++) {
+            unsigned w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+            unsigned top = 0;                         // largest magnitude, as bits
+#pragma unroll
+            for (int k = 0; k < 4; k++) top = max(top, max(w[k] & 0x7fffu, w[k] >> 16 & 0x7fffu));
+#pragma unroll
+            for (int o = kChunks / 2; o; o >>= 1) top = max(top, __shfl_xor_sync(~0u, top, o));
+            const int power = top ? min(14 + 127 - (int)(top >> 7), 120) : 0;
+            const float by = __uint_as_float((unsigned)(127 + power) << 23);
+#pragma unroll
+            for (int k = 0; k < 4; k++) w[k] = pack_f16(bf16_lo(w[k]) * by, bf16_hi(w[k]) * by);
+            v[i] = make_uint4(w[0], w[1], w[2], w[3]);
+            const int e = i * 256 + id;
+            if (e % kChunks == 0) h.row_c[t][e / kChunks] = p.scale * kLog2e * __uint_as_float((unsigned)(127 - power) << 23);
+          }
+        }
 #pragma unroll
         for (int i = 0; i < kEach; i++) {
           const int e = i * 256 + id, r = e / kChunks, ch = e % kChunks;
@@ -570,6 +619,7 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
         s_phase++;
         __syncwarp();
         tc_fence_after();
+        if (FP8 && i == 0) c = h.row_c[t][wr];
         unsigned see[2] = {~0u, ~0u};
         bool exact = i == 0 || masked;
         if (live && !exact) {
@@ -600,7 +650,7 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
                 e0 = exp2_fast(e0), e1 = exp2_fast(e1);
               }
               sum[k >> 1 & 1] = add2(sum[k >> 1 & 1], pair(e0, e1));
-              r[x * 16 + k / 2] = pack_bf16(e0, e1);
+              r[x * 16 + k / 2] = pack2<FP8>(e0, e1);
             }
             top = max3_nan(top, tops[0], tops[1]);
           }
@@ -700,7 +750,7 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
               unpair(e0, e1, fma2(pair(__uint_as_float(w[k]), __uint_as_float(w[k + 1])), c2, mc2));
               e0 = exp2_fast(e0), e1 = exp2_fast(e1);
               sum[k >> 1 & 1] = add2(sum[k >> 1 & 1], pair(e0, e1));
-              r[k / 2] = pack_bf16(e0, e1);
+              r[k / 2] = pack2<FP8>(e0, e1);
             }
             tmem_st16(ts + half * 64 + x * 16, r);    // over S columns of its own that it has read
           }
@@ -728,18 +778,18 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
               *at = make_uint4(0, 0, 0, 0);
             } else {
               const uint4 v = *at;
-              broken = zero_times(v.w, zero_times(v.z, zero_times(v.y, zero_times(v.x, broken))));
+              broken = zero_times<FP8>(v.w, zero_times<FP8>(v.z, zero_times<FP8>(v.y, zero_times<FP8>(v.x, broken))));
             }
           }
           fence_async_smem();
           slow = any_of_tile((broken & 0x7fff7fffu) != 0, tile_id);
           if (slow && live) {
             tmem_wait_st();
-            if (half == 0) product_by_key<HD>(ts, see[0], see[1], vt, 0, to, i > 0);
+            if (half == 0) product_by_key<HD, FP8>(ts, see[0], see[1], vt, 0, to, i > 0);
             tc_fence_before();
             named_barrier(pair_id, 64);
             tc_fence_after();
-            if (half == 1) product_by_key<HD>(ts + 64, see[0], see[1], vt, 64, to, true);
+            if (half == 1) product_by_key<HD, FP8>(ts + 64, see[0], see[1], vt, 64, to, true);
           }
         }
         tmem_wait_st();
@@ -900,7 +950,7 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
     // ================================ the matrix products ==============================================================
     // The whole warp walks the steps, so that addresses and phases stay warp-uniform; one lane issues.
     const bool leader = elect_one();
-    constexpr unsigned kIdS = mma_idesc(kTile, kTile, false), kIdO = mma_idesc(kTile, HD, true);
+    constexpr unsigned kIdS = mma_idesc(kTile, kTile, false, FP8), kIdO = mma_idesc(kTile, HD, true, FP8);
     const uint64_t q_desc = smem_desc(smem_u32(smem + L::kQ), 16, 1024);
     const uint64_t k_desc = smem_desc(smem_u32(smem + L::kRing), 16, 1024);
     const uint64_t v_desc = smem_desc(smem_u32(smem + L::kRing), kBox, 1024);
@@ -964,10 +1014,14 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
       mma_commit(leader, &h.fin);
       for (int n = 0; n < 1 << 16 && !__all_sync(~0u, mbar_try_wait(&h.fin, 0)); n++) {}
     }
-  } else if (FP8 && warp >= 16 && warp < 20) {
-    // ================================ 8-bit tiles widened to bf16 ======================================================
-    const int wt = threadIdx.x & 127;
-    constexpr int kChunks = HD / 16;                  // 16-byte chunks of an 8-bit row
+  } else if (FP8) {
+    // ================================ 8-bit tiles widened to f16: six warps ============================================
+    const int ct = (warp < 20 ? warp - 16 : warp - 18) * 32 + lane;
+    constexpr int kChunks = HD / 16, kAll = kChunks * kTile;   // 16-byte chunks of an 8-bit row, of a tile
+    // where this thread's first chunk goes: two of an f16 row
+    const int row0 = ct / kChunks, cc0 = ct % kChunks * 2;
+    const int at0 = cc0 / 8 * kBox + row0 * 128 + (((cc0 & 7) ^ (row0 & 7)) << 4);
+    const int at1 = cc0 / 8 * kBox + row0 * 128 + ((((cc0 & 7) + 1) ^ (row0 & 7)) << 4);
     int pos = 0;
     while (units.next(p, h, u)) {
       for (int n = 2 * (u.tile_end - u.tile_begin); n; n--, pos++) {
@@ -976,26 +1030,14 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
         attn_wait(&h.empty[st], (pos / L::kStages & 1) ^ 1, h);
         const unsigned char* src = smem + L::kRaw + raw * L::kRawBytes;
         unsigned char* dst = smem + L::kRing + st * L::kTileBytes;
-#pragma unroll 4
-        for (int i = 0; i < kChunks; i++) {
-          const int e = i * kTile + wt, r = e / kChunks, ch = e % kChunks;
-          const uint4 v = *(const uint4*)(src + e * 16);
-          const unsigned vv[4] = {v.x, v.y, v.z, v.w};
+        // 192 chunks are a whole number of rows, a multiple of 8: only the row moves on from one to the next
+#pragma unroll 2
+        for (int i = 0; i < kAll - ct; i += 192) {
+          const uint4 v = *(const uint4*)(src + (ct + i) * 16);
           unsigned w[8];
-#pragma unroll
-          for (int k = 0; k < 8; k++) {
-            unsigned half2;
-            asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(half2) : "h"((unsigned short)(vv[k >> 1] >> (k & 1) * 16)));
-            float lo, hi;
-            asm("{ .reg .b16 a, b; mov.b32 {a, b}, %2; cvt.f32.f16 %0, a; cvt.f32.f16 %1, b; }" : "=f"(lo), "=f"(hi) : "r"(half2));
-            w[k] = pack_bf16(lo, hi);                 // exact: 4 significant bits, exponents of a half
-          }
-#pragma unroll
-          for (int k = 0; k < 2; k++) {
-            const int cc = 2 * ch + k;
-            *(uint4*)(dst + cc / 8 * kBox + r * 128 + (((cc & 7) ^ (r & 7)) << 4)) =
-                make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
-          }
+          widen_e4m3(w, v.x), widen_e4m3(w + 2, v.y), widen_e4m3(w + 4, v.z), widen_e4m3(w + 6, v.w);
+          *(uint4*)(dst + at0 + i * (128 / kChunks)) = make_uint4(w[0], w[1], w[2], w[3]);
+          *(uint4*)(dst + at1 + i * (128 / kChunks)) = make_uint4(w[4], w[5], w[6], w[7]);
         }
         fence_async_smem();
         warp_arrive(&h.full[st], lane);

@@ -16,9 +16,9 @@ __device__ __forceinline__ uint64_t smem_desc(unsigned addr, unsigned lead, unsi
   return (uint64_t)((addr & 0x3ffff) >> 4) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(stride >> 4) << 32 |
          (uint64_t)1 << 46 | (uint64_t)2 << 61;
 }
-// kind::f16 with bf16 operands and fp32 accumulators, A K-major; B K-major or (b_mn) MN-major
-__host__ __device__ constexpr unsigned mma_idesc(int m, int n, bool b_mn) {
-  return 1u << 4 | 1u << 7 | 1u << 10 | (b_mn ? 1u << 16 : 0u) | (unsigned)(n >> 3) << 17 | (unsigned)(m >> 4) << 24;
+// kind::f16 with both operands bf16, or both f16, and fp32 accumulators, A K-major; B K-major or (b_mn) MN-major
+__host__ __device__ constexpr unsigned mma_idesc(int m, int n, bool b_mn, bool half) {
+  return 1u << 4 | (half ? 0u : 1u << 7 | 1u << 10) | (b_mn ? 1u << 16 : 0u) | (unsigned)(n >> 3) << 17 | (unsigned)(m >> 4) << 24;
 }
 
 // true in one lane of a converged warp

@@ -334,6 +334,27 @@ def test_tree_attention_hidden_values_reach_nothing(amk, cache):
         assert bool(torch.isnan(heads[sees]).flatten(1).any(1).all()) and bool(torch.isfinite(heads[~sees]).all()), (b, g, j)
 
 
+@pytest.mark.parametrize("hd", [64, 128])
+def test_tree_attention_every_8bit_code(amk, hd):
+    """Uniformly drawn codes, all 254 numbers among them (subnormals, both zeros, +-448); and one key alone, whose V row
+    has to come out as it is."""
+    g = gen(hd)
+    codes = torch.randint(0, 256, (2, 1, 2, 700, hd), generator=g, device=DEV).to(torch.uint8)
+    codes[(codes & 0x7F) == 0x7F] = 0x7E
+    assert len(codes.unique()) == 254
+    q = randn(g, 1, 5, 4, hd)
+    bits = np.stack([tree_bits(np.random.default_rng(3), 5)])
+    lse = torch.empty(1, 5, 4, device=DEV)
+    out = amk.amk_tree_attention(q, codes[0], codes[1], torch.tensor([690], dtype=torch.int32, device=DEV), words(bits),
+                                 scale=2.0 ** -12, lse=lse)
+    check_tree(q, codes[0], codes[1], [690], bits, out, lse, 2.0 ** -12)
+    for start in range(0, 700, 71):
+        k, v = codes[0][:, :, start:start + 1], codes[1][:, :, start:start + 1]
+        out = amk.amk_tree_attention(q[:, :1], k.contiguous(), v.contiguous(), torch.zeros(1, dtype=torch.int32, device=DEV))
+        want = v.view(torch.float8_e4m3fn).to(torch.bfloat16)[0, :, 0].repeat_interleave(2, 0)
+        assert torch.equal(out[0, 0], want)
+
+
 def test_tree_attention_bad_lengths(amk):
     rows, nq, nkv, hd, slots = 4, 4, 2, 64, 100
     q, k, v = tree_inputs(4, rows, slots, nq, nkv, hd, "bf16", 3)
