@@ -460,30 +460,54 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
       }
       if (lane == 0) h.unit[0] = seq, h.unit[1] = item, h.unit[2] = within, h.unit[3] = len, h.unit[4] = left;
     } else {
-      // the blocks of all prompts in order; the last block of a long prompt has the most keys and goes first
+      // Blocks of 256 / rep query tokens.  Those with the most keys first, so that the short ones fill the end: all prompts'
+      // blocks by their place in the prompt, the last places first (with more than 32 prompts only within each prompt).
       const int head = blockIdx.x % p.nkv, per = 2 * kTile / p.rep;
-      int idx = (int)(gridDim.x / p.nkv) - 1 - blockIdx.x / p.nkv;
+      int idx = blockIdx.x / p.nkv;
       int found = -1, tok0 = 0, n = 0, key0 = 0;
-      for (int s0 = 0; s0 < p.n_seqs; s0 += 32) {
-        int a = 0, b = 0;
-        if (s0 + lane < p.n_seqs) a = p.lens[s0 + lane], b = p.lens[s0 + lane + 1];
-        const bool ok = a >= 0 && a <= b && b <= p.rows;
-        const int own = ok ? (b - a + per - 1) / per : 0;
-        int sum = own;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const int x = __shfl_up_sync(~0u, sum, o);
-          if (lane >= o) sum += x;
-        }
-        const unsigned hit = __ballot_sync(~0u, sum > idx);
-        if (hit) {
-          const int f = __ffs(hit) - 1;
-          const int blk = idx - __shfl_sync(~0u, sum - own, f);
+      auto blocks_of = [&](int s, int& a, int& b) {
+        a = b = 0;
+        if (s < p.n_seqs) a = __ldg(p.lens + s), b = __ldg(p.lens + s + 1);
+        return a >= 0 && a <= b && b <= p.rows ? (b - a + per - 1) / per : 0;
+      };
+      if (p.n_seqs <= 32) {
+        int a, b;
+        const int own = blocks_of(lane, a, b);
+        auto from = [&](int place) { return (int)__reduce_add_sync(~0u, max(own - place, 0)); };   // blocks from a place on
+        int low = 0, high = (int)__reduce_max_sync(~0u, own);                // the largest place with more than idx of them
+        if (from(0) > idx) {
+          while (high - low > 1) {
+            const int mid = (low + high) / 2;
+            if (from(mid) > idx) low = mid;
+            else high = mid;
+          }
+          unsigned here = __ballot_sync(~0u, own > low);
+          for (int skip = idx - from(low + 1); skip; skip--) here &= here - 1;
+          const int f = __ffs(here) - 1;
           a = __shfl_sync(~0u, a, f), b = __shfl_sync(~0u, b, f);
-          found = 0, key0 = a, tok0 = blk * per, n = min(per, b - a - tok0);
-          break;
+          found = 0, key0 = a, tok0 = low * per, n = min(per, b - a - tok0);
         }
-        idx -= __shfl_sync(~0u, sum, 31);
+      } else {
+        idx = (int)(gridDim.x / p.nkv) - 1 - idx;
+        for (int s0 = 0; s0 < p.n_seqs; s0 += 32) {
+          int a, b;
+          const int own = blocks_of(s0 + lane, a, b);
+          int sum = own;
+#pragma unroll
+          for (int o = 1; o < 32; o <<= 1) {
+            const int x = __shfl_up_sync(~0u, sum, o);
+            if (lane >= o) sum += x;
+          }
+          const unsigned hit = __ballot_sync(~0u, sum > idx);
+          if (hit) {
+            const int f = __ffs(hit) - 1;
+            const int blk = idx - __shfl_sync(~0u, sum - own, f);
+            a = __shfl_sync(~0u, a, f), b = __shfl_sync(~0u, b, f);
+            found = 0, key0 = a, tok0 = blk * per, n = min(per, b - a - tok0);
+            break;
+          }
+          idx -= __shfl_sync(~0u, sum, 31);
+        }
       }
       if (lane == 0) h.unit[0] = found, h.unit[1] = head, h.unit[2] = key0, h.unit[3] = tok0, h.unit[4] = n;
     }
