@@ -33,7 +33,6 @@ struct AttnParams {
   float scale;
 };
 
-constexpr int kPoly = 1, kPolyOf = 4;   // of kPolyOf pairs of exponentials so many are made by exp2_poly
 constexpr int kTile = 128;         // rows of a Q tile, keys of a K/V tile
 // row / rep, exact for rows below 2^28
 __device__ __forceinline__ int div_rep(const AttnParams& p, int row) {
@@ -90,29 +89,6 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   uint64_t d;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
-}
-// 2^x of two values on the fma pipe, relative error 1e-7, for x in about [-126, 127]; below, 2^-126 (no matter to any sum).
-// x = n + f with f in [-1/2, 1/2]: adding 1.5 * 2^23 leaves n in the low bits, 2^f is the polynomial of degree 5 whose
-// largest relative error is least (Remez exchange, 7.5e-8), n goes into the exponent.  The exponential unit makes
-// 4 values a cycle and scheduler, which is what a tile's softmax waits for; a share of them is made here beside it.
-__device__ __forceinline__ void exp2_poly(float& e0, float& e1, uint64_t x) {
-  float x0, x1;
-  unpair(x0, x1, x);
-  x = pair(fmaxf(x0, -126.f), fmaxf(x1, -126.f));
-  constexpr float kShift = 12582912.f;
-  const uint64_t t = add2(x, pair(kShift, kShift));
-  const uint64_t f = add2(x, add2(pair(kShift, kShift), t ^ 0x8000000080000000ull));   // x - (t - shift)
-  uint64_t y = pair(1.3276472e-3f, 1.3276472e-3f);
-  y = fma2(y, f, pair(9.6755413e-3f, 9.6755413e-3f));
-  y = fma2(y, f, pair(5.5507133e-2f, 5.5507133e-2f));
-  y = fma2(y, f, pair(2.4022120e-1f, 2.4022120e-1f));
-  y = fma2(y, f, pair(6.9314697e-1f, 6.9314697e-1f));
-  y = fma2(y, f, pair(1.f, 1.f));
-  float t0, t1, y0, y1;
-  unpair(t0, t1, t);
-  unpair(y0, y1, y);
-  e0 = __uint_as_float(__float_as_uint(y0) + (__float_as_uint(t0) << 23));
-  e1 = __uint_as_float(__float_as_uint(y1) + (__float_as_uint(t1) << 23));
 }
 // Four e4m3 codes to four f16, exactly, NaN included.
 __device__ __forceinline__ void widen_e4m3(unsigned* w, unsigned codes) {
@@ -667,12 +643,8 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
               tops[k >> 1 & 1] = max3_nan(tops[k >> 1 & 1], a0, a1);
               const uint64_t z = fma2(pair(a0, a1), c2, mc2);
               float e0, e1;
-              if ((k >> 1) % kPolyOf < kPoly) {
-                exp2_poly(e0, e1, z);
-              } else {
-                unpair(e0, e1, z);
-                e0 = exp2_fast(e0), e1 = exp2_fast(e1);
-              }
+              unpair(e0, e1, z);
+              e0 = exp2_fast(e0), e1 = exp2_fast(e1);
               sum[k >> 1 & 1] = add2(sum[k >> 1 & 1], pair(e0, e1));
               r[x * 16 + k / 2] = pack2<FP8>(e0, e1);
             }
@@ -708,8 +680,8 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
             }
           }
           float top = -CUDART_INF_F;
-#pragma unroll 1
-          for (int x = 0; x < 2; x++) {                  // (rolled: this code is cold more often than not)
+#pragma unroll (TREE ? 1 : 2)
+          for (int x = 0; x < 2; x++) {                  // (rolled in short runs: this code is cold there)
             const unsigned sees = x ? see[1] : see[0];
             unsigned w[32];
             tmem_ld32(w, ts + half * 64 + x * 32);
@@ -756,7 +728,7 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
           const float mc = m == -CUDART_INF_F ? 0.f : -m * c;
           const uint64_t c2 = pair(c, c), mc2 = pair(mc, mc);
           uint64_t sum[2] = {0, 0};
-#pragma unroll 1
+#pragma unroll (TREE ? 1 : 2)
           for (int x = 0; x < 2; x++) {
             const unsigned sees = x ? see[1] : see[0];
             unsigned w[32], r[16];
