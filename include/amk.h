@@ -363,7 +363,7 @@ amk_status amk_argmax_static(const float* x, int64_t n, int32_t* token, char* ms
 typedef struct amk_prompt_args {
   uint32_t struct_size;      /* = sizeof(amk_prompt_args)                                              */
   uint32_t head_dim;         /* 64 or 128                                                              */
-  uint32_t n_q_heads;        /* multiple of n_kv_heads; n_q_heads / n_kv_heads <= 16                   */
+  uint32_t n_q_heads;        /* multiple of n_kv_heads; n_q_heads / n_kv_heads <= 16; at most 4096     */
   uint32_t n_kv_heads;
   uint32_t n_seqs;
   float scale;               /* > 0, or 0: 1 / sqrt(head_dim)                                          */
@@ -401,7 +401,7 @@ amk_status amk_prompt_attention(const amk_prompt_args* args, char* msg, size_t m
 typedef struct amk_tree_args {
   uint32_t struct_size;      /* = sizeof(amk_tree_args)                                                */
   uint32_t head_dim;         /* 64 or 128                                                              */
-  uint32_t n_q_heads;        /* multiple of n_kv_heads; n_q_heads / n_kv_heads <= 16                   */
+  uint32_t n_q_heads;        /* multiple of n_kv_heads; n_q_heads / n_kv_heads <= 16; at most 4096     */
   uint32_t n_kv_heads;
   uint32_t kv_dtype;         /* amk_kvdtype                                                            */
   uint32_t n_seqs;

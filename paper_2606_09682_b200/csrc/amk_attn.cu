@@ -79,8 +79,10 @@ cudaError_t launch_join(const AttnParams& p, unsigned blocks, cudaStream_t st) {
   at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at.val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(p.rows * p.rep + 31) / 32, (unsigned)p.nkv, (unsigned)p.n_seqs);
-  cfg.blockDim = dim3(HD * 2);                       // a warp for each 16 columns
+  cfg.gridDim = dim3((unsigned)(p.rows * p.rep + 31) / 32, (unsigned)p.nkv * (HD / 8), (unsigned)p.n_seqs);
+  // a warp for each part that an item is expected in
+  const int64_t items = (int64_t)p.nkv * p.row_tiles * p.n_seqs;
+  cfg.blockDim = dim3(32 * (unsigned)(blocks >= 6 * items ? amk::kJoinWarps : blocks >= 3 * items ? 4 : 2));
   cfg.stream = st;
   cfg.attrs = &at;
   cfg.numAttrs = 1;
@@ -111,7 +113,7 @@ TreePlan tree_plan(const amk_tree_args& a) {
   const int64_t most = a.n_slots - a.n_rows, len = a.max_len && a.max_len < most ? a.max_len : most;
   const int64_t tiles = (len + a.n_rows + amk::kTile - 1) / amk::kTile;
   const int64_t runs = ((tiles + amk::kUnitCost) * a.n_kv_heads * t.row_tiles * a.n_seqs + kMinTiles - 1) / kMinTiles;
-  const int sms = sm_count() < amk::kMaxBlocks ? sm_count() : amk::kMaxBlocks;
+  const int sms = sm_count();
   t.blocks = (unsigned)(runs < sms ? runs : sms);
   t.bytes = (size_t)2 * t.blocks * t.part_rows * (a.head_dim + 1) * 4;
   return t;
@@ -119,8 +121,8 @@ TreePlan tree_plan(const amk_tree_args& a) {
 
 amk_status check_heads(const Reason& fail, uint32_t hd, uint32_t nq, uint32_t nkv, float scale) {
   if (hd != 64 && hd != 128) return fail(AMK_ERR_UNSUPPORTED, "head_dim %u: 64 or 128", hd);
-  if (!nq || !nkv || nq % nkv || nq / nkv > 16 || nq > 65535)
-    return fail(AMK_ERR_UNSUPPORTED, "%u query heads on %u kv heads: a multiple, at most 16 to one", nq, nkv);
+  if (!nq || !nkv || nq % nkv || nq / nkv > 16 || nq > 4096)
+    return fail(AMK_ERR_UNSUPPORTED, "%u query heads on %u kv heads: a multiple, at most 16 to one and 4096", nq, nkv);
   if (!(scale >= 0.f) || isinf(scale)) return fail(AMK_ERR_INVALID_ARG, "scale must be positive and finite, or 0");
   return AMK_OK;
 }

@@ -1050,14 +1050,16 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
 // ---- parts of one item joined (tree) ----------------------------------------------------------------------------
 // Items whose tiles one block had are complete already; sequences of a bad length become NaN.
 //   O = sum_i w_i O_i / sum_i w_i,  w_i = 2^(lse_i - max): the parts carry O_i / l_i and log2 of their sums.
-// A block takes 32 rows of one item, a thread 16 columns of one of them, neighbouring threads neighbouring rows.
-constexpr int kMaxBlocks = 160;                      // blocks of a tree call at most: the weights below lie in shared memory
+// A block takes 32 rows and 8 columns of one item, a lane one row; the warps share the parts out, so that one way to
+// memory and back serves all of them, and meet in shared memory.
+constexpr int kJoinWarps = 8;
 template <int HD>
-__global__ void __launch_bounds__(HD * 2) attn_join_kernel(const AttnParams p, int blocks) {
+__global__ void __launch_bounds__(32 * kJoinWarps) attn_join_kernel(const AttnParams p, int blocks) {
   __shared__ int sh[2];
-  __shared__ float weight[kMaxBlocks][32];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int head = blockIdx.y, seq = blockIdx.z, row = blockIdx.x * 32 + lane, col = warp * 16;
+  __shared__ float some[kJoinWarps][10][32];          // each warp's maximum, sum and columns
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  constexpr int kSlices = HD / 8;
+  const int head = blockIdx.y / kSlices, seq = blockIdx.z, row = blockIdx.x * 32 + lane, col = blockIdx.y % kSlices * 8;
   const int tiles = tree_tiles(p, __ldg(p.lens + seq));
   if (warp == 0) {
     const int mine = tree_slots_of(p, lane);
@@ -1071,48 +1073,49 @@ __global__ void __launch_bounds__(HD * 2) attn_join_kernel(const AttnParams p, i
   const int rt = blockIdx.x * 32 / p.part_rows, local = row - rt * p.part_rows;
   const int first = sh[0] + (head * p.row_tiles + rt) * tree_slots(tiles) + kUnitCost, per = sh[1];
   const int c0 = first / per, parts = tiles ? (first + tiles - 1) / per - c0 + 1 : 0;
-  if (parts == 1) return;                            // complete already
+  // every thread waits for the attention kernel, also one that has nothing to do: what follows in the stream waits for
+  // this grid alone
   asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (parts == 1) return;                            // complete already
   const bool valid = row < p.rows * p.rep;
-  auto slot = [&](int b) { return (int64_t)2 * (c0 + b) + (b == 0 ? 1 : 0); };
-  for (int b = warp; b < parts; b += HD / 16)
-    weight[b][lane] = valid ? p.part_lse[slot(b) * p.part_rows + local] : -CUDART_INF_F;
-  __syncthreads();
-  float lse = CUDART_NAN_F;
-  if (warp == 0 && parts) {
-    float m = -CUDART_INF_F, sum = 0.f;
-    for (int b = 0; b < parts; b++) m = fmaxf(m, weight[b][lane]);
-    for (int b = 0; b < parts; b++) {
-      const float x = weight[b][lane], w = x == -CUDART_INF_F ? 0.f : exp2f(x - m);   // (all -infinity: nothing was seen)
-      weight[b][lane] = w;
-      sum += w;
-    }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    for (int b = 0; b < parts; b++) weight[b][lane] *= inv;
-    lse = sum == 0.f ? -CUDART_INF_F : (m + log2f(sum)) * 0.6931471805599453f;
-  }
-  __syncthreads();
-  if (!valid) return;
-  float v[16];
-#pragma unroll
-  for (int k = 0; k < 16; k++) v[k] = parts ? 0.f : CUDART_NAN_F;
+  float m = -CUDART_INF_F, sum = 0.f, v[8] = {};
+  if (valid) {
 #pragma unroll 4
-  for (int b = 0; b < parts; b++) {
-    const float w = weight[b][lane];
-    const float* o = p.part_o + ((slot(b) * (HD / 4) + col / 4) * p.part_rows + local) * 4;
-#pragma unroll
-    for (int k = 0; k < 16; k += 4) {
-      const float4 y = *(const float4*)(o + (int64_t)k * p.part_rows);
-      v[k] += w * y.x, v[k + 1] += w * y.y, v[k + 2] += w * y.z, v[k + 3] += w * y.w;
+    for (int b = warp; b < parts; b += warps) {      // part b is slot 2 (c0 + b), the first one's the slot behind
+      const int64_t slot = (int64_t)2 * (c0 + b) + (b == 0 ? 1 : 0);
+      const float x = p.part_lse[slot * p.part_rows + local];
+      const float* o = p.part_o + ((slot * (HD / 4) + col / 4) * p.part_rows + local) * 4;
+      const float4 y = *(const float4*)o, z = *(const float4*)(o + (int64_t)4 * p.part_rows);
+      const float mn = fmaxf(m, x);
+      const float f = m == mn ? 1.f : exp2f(m - mn), w = x == -CUDART_INF_F ? 0.f : exp2f(x - mn);
+      m = mn;
+      sum = sum * f + w;
+      v[0] = v[0] * f + w * y.x, v[1] = v[1] * f + w * y.y, v[2] = v[2] * f + w * y.z, v[3] = v[3] * f + w * y.w;
+      v[4] = v[4] * f + w * z.x, v[5] = v[5] * f + w * z.y, v[6] = v[6] * f + w * z.z, v[7] = v[7] * f + w * z.w;
     }
   }
-  const int tok = div_rep(p, row), q_head = head * p.rep + row - tok * p.rep;
-  __nv_bfloat16* out = p.out + (int64_t)seq * p.o_seq + tok * p.o_row + q_head * p.o_head + col;
+  some[warp][8][lane] = m, some[warp][9][lane] = sum;
 #pragma unroll
-  for (int k = 0; k < 16; k += 8)
-    *(uint4*)(out + k) = make_uint4(pack_bf16(v[k], v[k + 1]), pack_bf16(v[k + 2], v[k + 3]), pack_bf16(v[k + 4], v[k + 5]),
-                                    pack_bf16(v[k + 6], v[k + 7]));
-  if (p.lse && warp == 0) p.lse[((int64_t)seq * p.rows + tok) * p.nq + q_head] = lse;
+  for (int k = 0; k < 8; k++) some[warp][k][lane] = v[k];
+  __syncthreads();
+  if (warp || !valid) return;
+  for (int g = 1; g < warps; g++) {
+    const float x = some[g][8][lane];
+    const float mn = fmaxf(m, x);
+    const float f = m == mn ? 1.f : exp2f(m - mn), w = x == -CUDART_INF_F ? 0.f : exp2f(x - mn);   // (nothing seen: 0)
+    m = mn;
+    sum = sum * f + w * some[g][9][lane];
+#pragma unroll
+    for (int k = 0; k < 8; k++) v[k] = v[k] * f + w * some[g][k][lane];
+  }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+  for (int k = 0; k < 8; k++) v[k] = parts ? v[k] * inv : CUDART_NAN_F;
+  const float lse = !parts ? CUDART_NAN_F : sum == 0.f ? -CUDART_INF_F : (m + log2f(sum)) * 0.6931471805599453f;
+  const int tok = div_rep(p, row), q_head = head * p.rep + row - tok * p.rep;
+  *(uint4*)(p.out + (int64_t)seq * p.o_seq + tok * p.o_row + q_head * p.o_head + col) =
+      make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+  if (p.lse && col == 0) p.lse[((int64_t)seq * p.rows + tok) * p.nq + q_head] = lse;
 }
 
 }  // namespace amk

@@ -78,7 +78,7 @@ NAN = float("nan")
 @pytest.mark.parametrize("kw,code,word", [
     (dict(struct_size=8), INVALID, "struct_size"), (dict(head_dim=96), UNSUPPORTED, "head_dim 96"),
     (dict(n_q_heads=5), UNSUPPORTED, "multiple"), (dict(n_q_heads=34, n_kv_heads=2), UNSUPPORTED, "16"),
-    (dict(n_kv_heads=0), UNSUPPORTED, "heads"), (dict(n_q_heads=0), UNSUPPORTED, "heads"),
+    (dict(n_q_heads=4098), UNSUPPORTED, "4096"), (dict(n_kv_heads=0), UNSUPPORTED, "heads"), (dict(n_q_heads=0), UNSUPPORTED, "heads"),
     (dict(scale=-1.0), INVALID, "scale"), (dict(scale=NAN), INVALID, "scale"), (dict(scale=float("inf")), INVALID, "scale"),
     (dict(total=-1), INVALID, "rows"), (dict(total=1 << 31), INVALID, "rows"),
     (dict(q=0), INVALID, "NULL"), (dict(k=0), INVALID, "NULL"), (dict(v=0), INVALID, "NULL"),
