@@ -275,22 +275,23 @@ def _refuse(name: str, what: str):
     raise AmkError(AMK_ERR_INVALID_ARG, f"{name}: {what}")
 
 
-def _device_of(name: str, first: torch.Tensor, *others) -> torch.device:
-    dev = first.device
-    if dev.type != "cuda":
+def _device_of(name: str, first: torch.Tensor, *others) -> int:
+    """Index of the cuda device that all the tensors (or None) live on."""
+    index = first.get_device()                        # -1: not a cuda tensor
+    if index < 0:
         _refuse(name, "tensors must be cuda tensors")
     for t in others:
-        if t is not None and t.device != dev:
+        if t is not None and t.get_device() != index:
             _refuse(name, "tensors on different devices")
-    return dev
+    return index
 
 
-def _run(fn, name: str, device: torch.device, *args) -> None:
-    """Calls a library entry point that ends in (msg, msg_bytes, stream) on the tensors' device and its current stream."""
-    msg = getattr(_local, "msg", None)
-    if msg is None:
+def _run(fn, name: str, index: int, *args) -> None:
+    """Calls a library entry point that ends in (msg, msg_bytes, stream) on device ``index`` and its current stream."""
+    try:
+        msg = _local.msg
+    except AttributeError:
         msg = _local.msg = C.create_string_buffer(256)
-    index = device.index
     if index == torch.cuda.current_device():
         code = fn(*args, msg, 256, _raw_stream(index))
     else:
@@ -317,10 +318,11 @@ def amk_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_s
         _refuse(name, "q, k and v are bf16")
     if kshape != v.shape or kshape[0] != total or kshape[2] != hd:
         _refuse(name, "shapes of q, k and v do not fit")
-    if cu_seqlens.dtype is not torch.int32 or cu_seqlens.dim() != 1 or not cu_seqlens.is_contiguous() or not len(cu_seqlens):
+    entries = cu_seqlens.numel()
+    if cu_seqlens.dtype is not torch.int32 or cu_seqlens.dim() != 1 or not cu_seqlens.is_contiguous() or not entries:
         _refuse(name, "cu_seqlens is a contiguous int32 vector of n_seqs + 1 entries")
     if out is None:
-        out = torch.empty(shape, dtype=torch.bfloat16, device=dev)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
     elif out.shape != shape or out.dtype is not torch.bfloat16:
         _refuse(name, "out is bf16 of q's shape")
     if lse is not None and (lse.shape != (total, nq) or lse.dtype is not torch.float32 or not lse.is_contiguous()):
@@ -328,7 +330,7 @@ def amk_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_s
     (qr, qh, q1), (kr, kh, k1), (vr, vh, v1), (orow, oh, o1) = q.stride(), k.stride(), v.stride(), out.stride()
     if not (q1 == k1 == v1 == o1 == 1):
         _refuse(name, "the last dimension must be contiguous")
-    args = _PROMPT.pack(_PROMPT.size, hd, nq, kshape[1], len(cu_seqlens) - 1, scale or 0.0, total, q.data_ptr(),
+    args = _PROMPT.pack(_PROMPT.size, hd, nq, kshape[1], entries - 1, scale or 0.0, total, q.data_ptr(),
                         k.data_ptr(), v.data_ptr(), out.data_ptr(), 0 if lse is None else lse.data_ptr(),
                         cu_seqlens.data_ptr(), qr, qh, kr, kh, vr, vh, orow, oh)
     _run(lib.amk_prompt_attention, name, dev, args)
@@ -367,7 +369,7 @@ def amk_tree_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cache_
                              not mask.is_contiguous()):
         _refuse(name, "mask is contiguous int64 [n_seqs][rows][ceil(rows / 64)]")
     if out is None:
-        out = torch.empty(shape, dtype=torch.bfloat16, device=dev)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
     elif out.shape != shape or out.dtype is not torch.bfloat16:
         _refuse(name, "out is bf16 of q's shape")
     if lse is not None and (lse.shape != (seqs, rows, nq) or lse.dtype is not torch.float32 or not lse.is_contiguous()):
@@ -381,14 +383,14 @@ def amk_tree_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cache_
     plan = (_TREE.size, hd, nq, nkv, AMK_KV_BF16 if dtype is torch.bfloat16 else AMK_KV_FP8_E4M3, seqs, rows, slots,
             max_len or 0)
     if workspace is None:
-        key = (dev.index, plan)
+        key = (dev, plan)
         need = _tree_bytes.get(key)
         if need is None:
             need = amk_tree_workspace_bytes(_TREE.pack(*plan, *(0,) * 22), dev)
             if len(_tree_bytes) >= 4096:
                 _tree_bytes.clear()
             _tree_bytes[key] = need
-        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
         have = need
     else:
         if not workspace.is_contiguous():
@@ -416,9 +418,8 @@ def amk_operator_status(device=None) -> int:
     """Synchronises; AMK_OK, or AMK_ERR_TIMEOUT if a bounded wait of an attention kernel ran out on the device since last
     asked."""
     st = C.c_int()
-    dev = torch.device("cuda" if device is None else device)
-    _run(lib.amk_operator_status, "amk_operator_status",
-         torch.device("cuda", torch.cuda.current_device()) if dev.index is None else dev, C.byref(st))
+    index = None if device is None else torch.device(device).index
+    _run(lib.amk_operator_status, "amk_operator_status", torch.cuda.current_device() if index is None else index, C.byref(st))
     return st.value
 
 
@@ -440,10 +441,11 @@ def amk_token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, top_k: int = 
         _refuse(name, "the last dimension must be contiguous")
     if top_k < 0:
         _refuse(name, "top_k is negative")
-    logprob = torch.empty(rows, dtype=torch.float32, device=dev)
-    entropy = torch.empty(rows, dtype=torch.float32, device=dev)
-    top_tokens = torch.empty((rows, top_k), dtype=torch.int32, device=dev)
-    top_logprobs = torch.empty((rows, top_k), dtype=torch.float32, device=dev)
+    where = logits.device
+    logprob = torch.empty(rows, dtype=torch.float32, device=where)
+    entropy = torch.empty_like(logprob)
+    top_tokens = torch.empty(rows, top_k, dtype=torch.int32, device=where)
+    top_logprobs = torch.empty(rows, top_k, dtype=torch.float32, device=where)
     _run(lib.amk_token_logprobs, name, dev, logits.data_ptr(), 1 if dtype is torch.bfloat16 else 0, rows, vocab, stride,
          tokens.data_ptr(), top_k, logprob.data_ptr(), entropy.data_ptr(), top_tokens.data_ptr(), top_logprobs.data_ptr())
     return logprob, entropy, top_tokens, top_logprobs
