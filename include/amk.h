@@ -354,7 +354,7 @@ amk_status amk_argmax_static(const float* x, int64_t n, int32_t* token, char* ms
  *   lse           DEVICE float [total][n_q_heads], natural logarithm of each row's sum of exponentials, or NULL
  *   cu_seqlens    DEVICE int32 [n_seqs + 1]: prompt s is rows [cu[s], cu[s+1]); lengths of zero are allowed.  Rows of no
  *                 prompt (before cu[0], from cu[n_seqs] on) are left as they were.  A prompt whose bounds are
- *                 not 0 <= cu[s] <= cu[s+1] <= total is skipped.
+ *                 not 0 <= cu[s] <= cu[s+1] <= total is skipped; prompts must not overlap.
  * Pointers 16-byte aligned, strides multiples of 8 elements.  Arithmetic: scores and sums fp32, the softmax numerators
  * enter the second product as bf16 (relative error 2^-8 at most, each on its own), one rounding to bf16 at the end.
  * Errors: INVALID_ARG (struct size, NULL, alignment, strides, sizes), UNSUPPORTED (head_dim, head counts as
@@ -393,9 +393,11 @@ amk_status amk_prompt_attention(const amk_prompt_args* args, char* msg, size_t m
  *   lse           DEVICE float [n_seqs][n_rows][n_q_heads] or NULL
  *   max_len       upper bound of the lengths in cache_len, for the division of the work alone (results do not depend on
  *                 whether it holds); 0: n_slots - n_rows
- *   workspace     DEVICE, 256-byte aligned, at least amk_tree_workspace_bytes of the same arguments; scratch,
+ *   workspace     DEVICE, 256-byte aligned, at least amk_tree_workspace_bytes of the same arguments (pointers and strides
+ *                 do not matter there) on the same device; scratch,
  *                 needs no initial value; two calls that may overlap need one each
- * Pointers 16-byte aligned, strides multiples of 16 bytes.  The 8-bit cache is widened to bf16 exactly.
+ * Pointers 16-byte aligned, strides multiples of 16 bytes.  Arithmetic as amk_prompt_attention's; over the 8-bit cache the
+ * softmax numerators are f16 (2^-11), the codes exact, and q exact but for values 2^-30 below its row's largest.
  * Errors as amk_prompt_attention.
  */
 typedef struct amk_tree_args {

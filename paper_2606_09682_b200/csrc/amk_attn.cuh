@@ -6,6 +6,21 @@
 //   O = O 2^((m - m') c) + P V;  at the end O / l.
 // O is rescaled only when m rises by more than 8 / c (P then stays below 2^8, nothing is lost: P is a floating-point
 // number and l and O share the reference).
+//
+// Work.  One block an SM: two row tiles of 128 rows share every K/V tile of 128 keys (prompts, large drafts), or, where a
+// draft has 128 rows at most, take every second key tile each and are joined at the end.  A producer warp keeps a ring of
+// tiles full by TMA, one warp issues the products (S and O in TMEM, P over S as the A operand of P V), four warpgroups
+// make the softmax, so that one tile's exponentials run beside the other's products.  Prompts: a block for 256 / rep
+// tokens of a kv head.  Trees: the key tiles of the whole batch in equal runs (below), parts joined by a second kernel.
+//
+// What bounds it.  Prompts: the chain scores -> softmax -> products of a tile, 3650 cycles for 2054 cycles of products a
+// pair of tiles (the exponentials alone are 2048): 8192 tokens, 32 heads of 128 on 8, 550 GFLOP in 468 us = 1.17 PFLOP/s.
+// head_dim 64 has half the products for the same exponentials.  Trees: HBM in long runs (32 sequences of 8000 positions,
+// one token each: 1.05 GB in 168 us = 6.2 TB/s); a short call the 8 us that a cold block takes from its start to its first
+// output, of which the tiles are the least.  The 8-bit cache: its tiles' way through shared memory (raw in, f16 out, read
+// as operands).
+// Registers are what this kernel is short of: a spilled one is fetched from L2 behind the stream of tiles (shared memory
+// leaves no L1), and cost up to half the time where it stood in the steps.
 #pragma once
 #include <cuda_bf16.h>
 #include <math_constants.h>
@@ -389,9 +404,9 @@ __device__ __noinline__ void product_by_key(unsigned tp, unsigned see0, unsigned
   tmem_wait_st();
 }
 
-// Over the 8-bit cache the matrix instructions work on f16: every e4m3 code is an f16 by one conversion (to bf16 it takes
-// three more, and the six warps that widen the tiles bound the kernel), P has three bits more than in bf16, and a row of Q
-// is exact in f16 after a power of two.
+// Over the 8-bit cache the matrix instructions work on f16: two e4m3 codes are two f16 by one conversion (to bf16 it takes
+// three more), P has three bits more than in bf16, and a row of Q is exact in f16 after a power of two.  P is rounded to
+// the operands' type (2^-8 of it in bf16), the sum l is not: the roundings of a row are independent and average out.
 // ---- the kernel -------------------------------------------------------------------------------------------------
 template <int HD, bool TREE, bool FP8>
 __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)

@@ -195,6 +195,79 @@ def test_prompt_attention_many_short_prompts(amk):
     check(out, None, attention64(q, k, v, sees, hd ** -0.5))
 
 
+@pytest.mark.parametrize("n_seqs", [31, 32, 33, 65])
+def test_prompt_attention_around_32_prompts(amk, n_seqs):
+    """Blocks are looked up in another way from 33 prompts on; with one head group of 16 a block is 16 tokens."""
+    rng = np.random.default_rng(n_seqs)
+    lens = [int(x) for x in rng.integers(0, 90, n_seqs)]
+    lens[n_seqs // 2], lens[-1] = 700, 0
+    q, k, v, cu = prompt_inputs(lens, 16, 1, 64, n_seqs)
+    lse = torch.full((sum(lens), 16), math.nan, device=DEV)
+    out = amk.amk_prompt_attention(q, k, v, cu, lse=lse)
+    check_prompt(q, k, v, lens, out, lse, 0.125)
+
+
+def test_attention_a_broken_query_spoils_its_own_row_only(amk):
+    nq, nkv, hd, n = 4, 2, 128, 300
+    q, k, v, cu = prompt_inputs([n], nq, nkv, hd, 19, fused=False)
+    q = q.contiguous()
+    q[140, 1, 5], q[7, 3, 0] = math.nan, math.inf
+    out = amk.amk_prompt_attention(q, k, v, cu).float()
+    o, _, tol, _, _ = attention64(torch.nan_to_num(q, 0, 0, 0), k, v, causal(n), hd ** -0.5)
+    fine = torch.ones(n, nq, dtype=torch.bool, device=DEV)
+    fine[140, 1] = fine[7, 3] = False
+    assert bool(((out.double() - o).abs() <= tol)[fine].all())
+    assert bool(torch.isnan(out[140, 1]).all()) and not bool(torch.isfinite(out[7, 3]).any())
+
+
+def test_attentions_on_two_streams_at_once(amk):
+    """Calls that overlap, each with its own scratch, give what they give alone; what follows in a stream sees the result."""
+    q, k, v, cu = prompt_inputs([900, 300], 8, 2, 64, 23)
+    qt, kt, vt = tree_inputs(2, 9, 3000, 8, 2, 128, "bf16", 24)
+    length = torch.tensor([2900, 1500], dtype=torch.int32, device=DEV)
+    want_p, want_t = amk.amk_prompt_attention(q, k, v, cu), amk.amk_tree_attention(qt, kt, vt, length)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    got = []
+    for i in range(30):
+        with torch.cuda.stream(streams[i % 3]):
+            if i % 2:
+                got.append((want_p, amk.amk_prompt_attention(q, k, v, cu).clone()))
+            else:
+                got.append((want_t, amk.amk_tree_attention(qt, kt, vt, length).clone()))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in got)
+
+
+def test_first_call_of_a_process_may_be_captured():
+    """Everything that a call sets up once happens in the call itself, and capture allows it."""
+    code = """
+import torch
+from paper_2606_09682_b200 import binding as amk
+q = torch.randn(1, 3, 4, 64, device="cuda").to(torch.bfloat16)
+k = torch.randn(1, 2, 500, 64, device="cuda").to(torch.bfloat16)
+x, tok = torch.randn(2, 5000, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+n, cu = torch.full((1,), 400, dtype=torch.int32, device="cuda"), torch.tensor([0, 3], dtype=torch.int32, device="cuda")
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    a = amk.amk_tree_attention(q, k, k, n)
+    b = amk.amk_prompt_attention(q[0], q[0, :, :2], q[0, :, 2:], cu)
+    c = amk.amk_token_logprobs(x, tok, 3)
+    amk.amk_kv_compact(k, n, n[None], n)
+graph.replay()
+assert torch.equal(a, amk.amk_tree_attention(q, k, k, n)) and torch.equal(b, amk.amk_prompt_attention(q[0], q[0, :, :2], q[0, :, 2:], cu))
+assert all(torch.equal(u, v) for u, v in zip(c, amk.amk_token_logprobs(x, tok, 3))) and amk.amk_operator_status() == 0
+print("fine")
+"""
+    import os
+    import subprocess
+    import sys
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300,
+                       cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert r.returncode == 0 and "fine" in r.stdout, r.stderr[-2000:]
+
+
 def test_prompt_attention_is_deterministic_and_replays(amk):
     """The same bits every time, on another stream, and from a captured graph whose inputs and bounds change."""
     lens, nq, nkv, hd = [333, 100, 267], 8, 2, 128
@@ -309,6 +382,48 @@ def test_tree_attention_rows_that_see_nothing(amk, cache, len_):
     check_tree(q, k, v, [len_], bits, out, lse, hd ** -0.5)
     if not len_:
         assert bool((out[0, [0, 4, 8]] == 0).all()) and bool((lse[0, [0, 4, 8]] == -math.inf).all())
+
+
+@pytest.mark.parametrize("rows", [1, 5, 31, 33, 64, 70, 127])
+def test_tree_attention_ignores_bits_behind_the_last_token(amk, rows):
+    nq, nkv, hd, slots = 8, 2, 64, 700
+    q, k, v = tree_inputs(1, rows, slots, nq, nkv, hd, "bf16", rows)
+    bits = np.stack([tree_bits(np.random.default_rng(rows), rows)])
+    mask = words(bits)
+    if rows % 64:
+        mask[:, :, -1] |= -1 << (rows % 64)
+    for n in (0, 100, slots - rows):
+        out = amk.amk_tree_attention(q, k, v, torch.tensor([n], dtype=torch.int32, device=DEV), mask)
+        check_tree(q, k, v, [n], bits, out, None, hd ** -0.5)
+
+
+@pytest.mark.parametrize("cache", ["bf16", "fp8"])
+def test_tree_attention_largest_draft(amk, cache):
+    """1024 drafted tokens of 16 heads to one: 64 blocks of rows."""
+    rows, nq, nkv, hd, slots = 1024, 16, 1, 64, 1500
+    q, k, v = tree_inputs(1, rows, slots, nq, nkv, hd, cache, 61)
+    bits = np.stack([tree_bits(np.random.default_rng(8), rows)])
+    lse = torch.empty(1, rows, nq, device=DEV)
+    out = amk.amk_tree_attention(q, k, v, torch.tensor([476], dtype=torch.int32, device=DEV), words(bits), lse=lse)
+    check_tree(q, k, v, [476], bits, out, lse, hd ** -0.5)
+
+
+def test_tree_attention_many_sequences(amk):
+    """300 sequences, empty ones and bad lengths among them."""
+    seqs, rows, nq, nkv, hd, slots = 300, 3, 6, 3, 64, 260
+    q, k, v = tree_inputs(seqs, rows, slots, nq, nkv, hd, "bf16", 62)
+    rng = np.random.default_rng(2)
+    lens = [int(x) for x in rng.integers(0, slots - rows + 1, seqs)]
+    lens[7] = lens[299] = -3
+    lens[100], lens[0] = slots, 0
+    length = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    out = amk.amk_tree_attention(q, k, v, length)
+    chain = np.tril(np.ones((rows, rows), dtype=bool))
+    for b in range(seqs):
+        if 0 <= lens[b] <= slots - rows:
+            check_tree(q[b:b + 1], k[b:b + 1], v[b:b + 1], [lens[b]], chain[None], out[b:b + 1], None, hd ** -0.5, b)
+        else:
+            assert bool(torch.isnan(out[b].float()).all())
 
 
 @pytest.mark.parametrize("cache", ["bf16", "fp8"])
