@@ -79,7 +79,7 @@ cudaError_t launch_join(const AttnParams& p, unsigned blocks, cudaStream_t st) {
   at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at.val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(p.rows * p.rep + 31) / 32, (unsigned)p.nkv * (HD / 8), (unsigned)p.n_seqs);
+  cfg.gridDim = dim3((unsigned)(p.rows * p.rep + 31) / 32 * (HD / 8), (unsigned)p.nkv, (unsigned)p.n_seqs);
   // a warp for each part that an item is expected in
   const int64_t items = (int64_t)p.nkv * p.row_tiles * p.n_seqs;
   cfg.blockDim = dim3(32 * (unsigned)(blocks >= 6 * items ? amk::kJoinWarps : blocks >= 3 * items ? 4 : 2));

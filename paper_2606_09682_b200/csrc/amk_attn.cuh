@@ -1074,7 +1074,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attn_join_kernel(const AttnPa
   __shared__ float some[kJoinWarps][10][32];          // each warp's maximum, sum and columns
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
   constexpr int kSlices = HD / 8;
-  const int head = blockIdx.y / kSlices, seq = blockIdx.z, row = blockIdx.x * 32 + lane, col = blockIdx.y % kSlices * 8;
+  const int head = blockIdx.y, seq = blockIdx.z, row0 = blockIdx.x / kSlices * 32, row = row0 + lane, col = blockIdx.x % kSlices * 8;
   const int tiles = tree_tiles(p, __ldg(p.lens + seq));
   if (warp == 0) {
     const int mine = tree_slots_of(p, lane);
@@ -1085,7 +1085,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attn_join_kernel(const AttnPa
     if (lane == 0) sh[0] = before, sh[1] = per;
   }
   __syncthreads();
-  const int rt = blockIdx.x * 32 / p.part_rows, local = row - rt * p.part_rows;
+  const int rt = row0 / p.part_rows, local = row - rt * p.part_rows;
   const int first = sh[0] + (head * p.row_tiles + rt) * tree_slots(tiles) + kUnitCost, per = sh[1];
   const int c0 = first / per, parts = tiles ? (first + tiles - 1) / per - c0 + 1 : 0;
   // every thread waits for the attention kernel, also one that has nothing to do: what follows in the stream waits for

@@ -426,6 +426,18 @@ def test_tree_attention_many_sequences(amk):
             assert bool(torch.isnan(out[b].float()).all())
 
 
+@pytest.mark.parametrize("nq,nkv,hd", [(4096, 4096, 128), (4096, 256, 64)])
+def test_attentions_of_the_most_heads(amk, nq, nkv, hd):
+    rows, slots, lens = 2, 150, [131]
+    q, k, v = tree_inputs(1, rows, slots, nq, nkv, hd, "bf16", 17)
+    lse = torch.full((1, rows, nq), math.nan, device=DEV)
+    out = amk.amk_tree_attention(q, k, v, torch.tensor(lens, dtype=torch.int32, device=DEV), lse=lse)
+    check_tree(q, k, v, lens, np.tril(np.ones((1, rows, rows), bool)), out, lse, hd ** -0.5)
+    q, k, v, cu = prompt_inputs([3, 131], nq, nkv, hd, 18)
+    out = amk.amk_prompt_attention(q, k, v, cu)
+    check_prompt(q, k, v, [3, 131], out, None, hd ** -0.5)
+
+
 @pytest.mark.parametrize("cache", ["bf16", "fp8"])
 def test_tree_attention_hidden_values_reach_nothing(amk, cache):
     """NaN in slots behind the drafted tokens reaches nothing; in a drafted token's K or V it reaches that token's
