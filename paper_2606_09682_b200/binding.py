@@ -330,6 +330,8 @@ def amk_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_s
     (qr, qh, q1), (kr, kh, k1), (vr, vh, v1), (orow, oh, o1) = q.stride(), k.stride(), v.stride(), out.stride()
     if not (q1 == k1 == v1 == o1 == 1):
         _refuse(name, "the last dimension must be contiguous")
+    if scale is not None and not scale > 0:
+        _refuse(name, "scale must be positive")
     args = _PROMPT.pack(_PROMPT.size, hd, nq, kshape[1], entries - 1, scale or 0.0, total, q.data_ptr(),
                         k.data_ptr(), v.data_ptr(), out.data_ptr(), 0 if lse is None else lse.data_ptr(),
                         cu_seqlens.data_ptr(), qr, qh, kr, kh, vr, vh, orow, oh)
@@ -380,6 +382,8 @@ def amk_tree_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cache_
     os_, orow, oh, o1 = out.stride()
     if not (q1 == k1 == v1 == o1 == 1):
         _refuse(name, "the last dimension must be contiguous")
+    if scale is not None and not scale > 0:
+        _refuse(name, "scale must be positive")
     plan = (_TREE.size, hd, nq, nkv, AMK_KV_BF16 if dtype is torch.bfloat16 else AMK_KV_FP8_E4M3, seqs, rows, slots,
             max_len or 0)
     if workspace is None:

@@ -800,6 +800,18 @@ def test_python_layer_refuses_what_does_not_fit(amk):
     assert e.value.code == amk.AMK_ERR_UNSUPPORTED
 
 
+@pytest.mark.parametrize("scale", [0.0, -1.0, math.nan, math.inf])
+def test_python_layer_refuses_a_scale_that_is_none(amk, scale):
+    """Zero would mean the default in the C struct."""
+    q, k, v, cu = prompt_inputs([20], 4, 2, 64, 1)
+    qt, kt, vt = tree_inputs(2, 3, 50, 4, 2, 64, "bf16", 1)
+    for call in (lambda: amk.amk_prompt_attention(q, k, v, cu, scale=scale),
+                 lambda: amk.amk_tree_attention(qt, kt, vt, torch.zeros(2, dtype=torch.int32, device=DEV), scale=scale)):
+        with pytest.raises(amk.AmkError) as e:
+            call()
+        assert e.value.code == amk.AMK_ERR_INVALID_ARG
+
+
 # ---- together ---------------------------------------------------------------------------------------------------
 
 def forward(shape, w, tokens, positions, attend):
