@@ -384,6 +384,7 @@ amk_status amk_prompt_attention(const amk_prompt_args* args, char* msg, size_t m
  * len + j whose bit j is set in its row of the mask (a tree: its ancestors and itself).  n_rows = 1 without a mask
  * is the attention of the decode step.
  *   q, out        DEVICE bf16 [n_seqs][n_rows][n_q_heads][head_dim] at the given strides (elements)
+ *                 out must not overlap the inputs
  *   k, v          DEVICE, kv_dtype (amk_kvdtype): one layer of the cache, [n_seqs][n_kv_heads][n_slots][head_dim] at
  *                 the given strides (elements of that type); only rows [0, len + n_rows) are read for their values
  *   cache_len     DEVICE int32 [n_seqs]: len.  Read on the device, so a captured call follows it.  A sequence whose

@@ -55,8 +55,8 @@ cudaError_t allow_smem() {
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
-  const unsigned long long bit = 1ull << (dev & 63);
-  if (dev < 64 && (done.load(std::memory_order_acquire) & bit)) return cudaSuccess;
+  const unsigned long long bit = dev < 64 ? 1ull << dev : 0;      // (0: set at every call)
+  if (done.load(std::memory_order_acquire) & bit) return cudaSuccess;
   e = cudaFuncSetAttribute(amk::attn_kernel<HD, TREE, FP8>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                            amk::AttnSmem<HD, FP8>::kBytes);
   if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_release);

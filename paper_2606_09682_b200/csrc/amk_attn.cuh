@@ -606,6 +606,7 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
           *(uint4*)(qs + ch / 8 * kBox + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) = v[i];
         }
         fence_async_smem();
+        tc_fence_before();                             // the last unit's S and O have been read
         warp_arrive(&h.q_full[t], lane);
       }
       if (TREE) {
