@@ -174,7 +174,7 @@ extern "C" amk_status amk_prompt_attention(const amk_prompt_args* args, char* ms
   if (a.struct_size != sizeof a)
     return fail(AMK_ERR_INVALID_ARG, "struct_size %u, the library has %zu", a.struct_size, sizeof a);
   AMK_TRY(check_heads(fail, a.head_dim, a.n_q_heads, a.n_kv_heads, a.scale));
-  if (a.total < 0 || a.total > 0x7fffffff - 1024 || a.n_seqs > 0x7fffffff - 1)
+  if (a.total < 0 || a.total > 0x7fffffff - 1024 || a.n_seqs > 0x7fffffff - 1024)
     return fail(AMK_ERR_INVALID_ARG, "%lld rows in %u prompts", (long long)a.total, a.n_seqs);
   if (a.total == 0 || a.n_seqs == 0) return AMK_OK;
   if (!a.q || !a.k || !a.v || !a.out || !a.cu_seqlens) return fail(AMK_ERR_INVALID_ARG, "NULL pointer");

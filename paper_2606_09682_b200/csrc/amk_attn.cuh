@@ -181,6 +181,7 @@ namespace amk {
 // at r * 128 + ((c ^ (r & 7)) << 4).
 constexpr int kBox = 64 * kTile * 2;
 constexpr int kHeadBytes = 8192;
+constexpr int kUnitRing = 4;
 template <int HD, bool FP8>
 struct AttnSmem {
   static constexpr int kTileBytes = HD / 64 * kBox;                // one bf16 tile of 128 rows
@@ -204,6 +205,9 @@ struct AttnHead {
   float mx[2][2][kTile];               // [tile][half]: row maxima, and at the end row sums, of half the columns
   float m[kTile], l[kTile];            // the second tile's statistics (both tiles of the same rows)
   int unit[8];
+  uint64_t unit_full[kUnitRing], unit_empty[kUnitRing], next_full;   // prompts: blocks of queries, taken one after the other
+  int4 units[kUnitRing], now_of[2][2];                               // the producer's; the two last ones of each row tile
+  uint4 next;                                                        // answer of the hardware's scheduler
   int walk[16][8];                     // each softmax warp's place in the walk and its unit: registers are short there
   Unit now[16];
   float row_c[2][kTile];               // 8-bit cache: scale * log2 e over the power of two that each row of Q was multiplied by
@@ -278,7 +282,7 @@ struct Units<true> {
   __device__ __forceinline__ void restore(const volatile int* at) {
     left = at[0], seq = at[1], len = at[2], tiles = at[3], item = at[4], within = at[5];
   }
-  __device__ __forceinline__ bool next(const AttnParams& p, const AttnHead&, Unit& u) {
+  __device__ __forceinline__ bool next(const AttnParams& p, AttnHead&, Unit& u) {
     int first, last;
     do {
       if (left <= 0) return false;
@@ -302,19 +306,101 @@ struct Units<true> {
   }
 };
 
+// Prompts: the block's own unit of queries, and then those of blocks that have not been launched yet, which the producer
+// warp takes over from the hardware's scheduler one at a time, when it has asked for the last tile of the one before.  The
+// others read them from a ring.
 template <>
 struct Units<false> {
-  bool more;
-  __device__ __forceinline__ void save(int*, int) const {}
-  __device__ __forceinline__ void restore(const volatile int*) {}
-  __device__ __forceinline__ void init(const AttnParams&, const AttnHead& h) { more = h.unit[0] >= 0; }
-  __device__ __forceinline__ bool next(const AttnParams& p, const AttnHead& h, Unit& u) {
-    if (!more) return false;
-    more = false;
-    u.seq = 0, u.head = h.unit[1], u.key0 = h.unit[2], u.tok0 = h.unit[3], u.n_tok = h.unit[4];
+  int n;                           // units taken so far
+  __device__ __forceinline__ void init(const AttnParams&, const AttnHead&) { n = 0; }
+  __device__ __forceinline__ static bool set(const AttnParams& p, const int4& x, Unit& u) {
+    u.seq = 0, u.head = x.x, u.key0 = x.y, u.tok0 = x.z, u.n_tok = x.w;
     u.row0 = 0, u.n_rows = u.n_tok * p.rep, u.len = 0;
     u.tile_begin = 0, u.tile_end = u.item_tiles = (u.tok0 + u.n_tok + kTile - 1) / kTile;
-    return true;
+    return x.x >= 0;
+  }
+  __device__ __forceinline__ int4 take(AttnHead& h, int lane) {
+    const int at = n & (kUnitRing - 1);
+    int4 x = make_int4(-1, 0, 0, 0);
+    if (attn_wait(&h.unit_full[at], n / kUnitRing & 1, h)) x = *(const int4*)&h.units[at];
+    n++;
+    warp_arrive(&h.unit_empty[at], lane);
+    return x;
+  }
+  // one warp
+  __device__ __forceinline__ bool next(const AttnParams& p, AttnHead& h, Unit& u) { return set(p, take(h, threadIdx.x & 31), u); }
+  // The eight warps of a row tile together: their barriers want all of them to see the same units, also after a wait that
+  // ran out.  The barrier is also the one behind which the last unit's output has left the tile's shared memory.
+  __device__ __forceinline__ bool next_of_tile(const AttnParams& p, AttnHead& h, Unit& u, int t, int warp, int lane, int id) {
+    const int at = n & 1;
+    if ((warp & 7) == 0) {
+      const int4 x = take(h, lane);
+      if (lane == 0) h.now_of[t][at] = x;
+    } else {
+      n++;
+    }
+    named_barrier(id, 256);
+    return set(p, *(const int4*)&h.now_of[t][at], u);
+  }
+};
+
+// Where the blocks of 256 / rep query tokens lie.  Those with the most keys come first, so that the short ones fill the
+// end: all prompts' blocks by their place in the prompt, the last places first (with more than 32 prompts one prompt after
+// the other, the last places first within each).  One whole warp; lane i has prompt s0 + i.
+struct PromptBlocks {
+  int s0, before;                  // first prompt of the 32 at hand, blocks of the prompts in front of them
+  int a, b, own;                   // this lane's prompt and its blocks
+  __device__ __forceinline__ void read(const AttnParams& p, int lane) {
+    const int s = s0 + lane, per = 2 * kTile / p.rep;
+    a = b = 0;
+    if (s < p.n_seqs) a = __ldg(p.lens + s), b = __ldg(p.lens + s + 1);
+    own = a >= 0 && a <= b && b <= p.rows ? (b - a + per - 1) / per : 0;
+  }
+  __device__ __forceinline__ void init(const AttnParams& p, int lane) {
+    s0 = before = 0;
+    read(p, lane);
+  }
+  // {head, first row of the prompt, first token, tokens} of a block of the grid; head -1: there is none
+  __device__ __forceinline__ int4 find(const AttnParams& p, int block, int lane) {
+    const int per = 2 * kTile / p.rep, head = block % p.nkv;
+    int idx = block / p.nkv, f = -1, place = 0;
+    if (p.n_seqs <= 32) {
+      auto from = [&](int x) { return (int)__reduce_add_sync(~0u, max(own - x, 0)); };   // blocks from place x on
+      if (from(0) > idx) {
+        int low = 0, high = (int)__reduce_max_sync(~0u, own);              // the largest place with more than idx of them
+        while (high - low > 1) {
+          const int mid = (low + high) / 2;
+          if (from(mid) > idx) low = mid;
+          else high = mid;
+        }
+        unsigned here = __ballot_sync(~0u, own > low);
+        for (int skip = idx - from(low + 1); skip; skip--) here &= here - 1;
+        f = __ffs(here) - 1, place = low;
+      }
+    } else {
+      if (idx < before) init(p, lane);
+      for (;;) {
+        int sum = own;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int x = __shfl_up_sync(~0u, sum, o);
+          if (lane >= o) sum += x;
+        }
+        const unsigned hit = __ballot_sync(~0u, sum > idx - before);
+        if (hit) {
+          f = __ffs(hit) - 1;
+          place = __shfl_sync(~0u, sum, f) - 1 - (idx - before);
+          break;
+        }
+        if (p.n_seqs - s0 <= 32) break;
+        before += __shfl_sync(~0u, sum, 31);
+        s0 += 32;
+        read(p, lane);
+      }
+    }
+    if (f < 0) return make_int4(-1, 0, 0, 0);
+    const int a_f = __shfl_sync(~0u, a, f), b_f = __shfl_sync(~0u, b, f);
+    return make_int4(head, a_f, place * per, min(per, b_f - a_f - place * per));
   }
 };
 
@@ -450,57 +536,21 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
         at -= __shfl_sync(~0u, n, 31);
       }
       if (lane == 0) h.unit[0] = seq, h.unit[1] = item, h.unit[2] = within, h.unit[3] = len, h.unit[4] = left;
-    } else {
-      // Blocks of 256 / rep query tokens.  Those with the most keys first, so that the short ones fill the end: all prompts'
-      // blocks by their place in the prompt, the last places first (with more than 32 prompts only within each prompt).
-      const int head = blockIdx.x % p.nkv, per = 2 * kTile / p.rep;
-      int idx = blockIdx.x / p.nkv;
-      int found = -1, tok0 = 0, n = 0, key0 = 0;
-      auto blocks_of = [&](int s, int& a, int& b) {
-        a = b = 0;
-        if (s < p.n_seqs) a = __ldg(p.lens + s), b = __ldg(p.lens + s + 1);
-        return a >= 0 && a <= b && b <= p.rows ? (b - a + per - 1) / per : 0;
-      };
-      if (p.n_seqs <= 32) {
-        int a, b;
-        const int own = blocks_of(lane, a, b);
-        auto from = [&](int place) { return (int)__reduce_add_sync(~0u, max(own - place, 0)); };   // blocks from a place on
-        int low = 0, high = (int)__reduce_max_sync(~0u, own);                // the largest place with more than idx of them
-        if (from(0) > idx) {
-          while (high - low > 1) {
-            const int mid = (low + high) / 2;
-            if (from(mid) > idx) low = mid;
-            else high = mid;
-          }
-          unsigned here = __ballot_sync(~0u, own > low);
-          for (int skip = idx - from(low + 1); skip; skip--) here &= here - 1;
-          const int f = __ffs(here) - 1;
-          a = __shfl_sync(~0u, a, f), b = __shfl_sync(~0u, b, f);
-          found = 0, key0 = a, tok0 = low * per, n = min(per, b - a - tok0);
-        }
-      } else {
-        idx = (int)(gridDim.x / p.nkv) - 1 - idx;
-        for (int s0 = 0; s0 < p.n_seqs; s0 += 32) {
-          int a, b;
-          const int own = blocks_of(s0 + lane, a, b);
-          int sum = own;
-#pragma unroll
-          for (int o = 1; o < 32; o <<= 1) {
-            const int x = __shfl_up_sync(~0u, sum, o);
-            if (lane >= o) sum += x;
-          }
-          const unsigned hit = __ballot_sync(~0u, sum > idx);
-          if (hit) {
-            const int f = __ffs(hit) - 1;
-            const int blk = idx - __shfl_sync(~0u, sum - own, f);
-            a = __shfl_sync(~0u, a, f), b = __shfl_sync(~0u, b, f);
-            found = 0, key0 = a, tok0 = blk * per, n = min(per, b - a - tok0);
-            break;
-          }
-          idx -= __shfl_sync(~0u, sum, 31);
-        }
-      }
-      if (lane == 0) h.unit[0] = found, h.unit[1] = head, h.unit[2] = key0, h.unit[3] = tok0, h.unit[4] = n;
+    }
+  }
+  PromptBlocks blocks;                                // (the producer's)
+  int4 unit;
+  if (!TREE && warp == kProducer) {
+    if (lane == 0) {
+      for (int i = 0; i < kUnitRing; i++) mbar_init(&h.unit_full[i], 1), mbar_init(&h.unit_empty[i], 3);
+      mbar_init(&h.next_full, 1);
+      mbar_fence_init();
+    }
+    blocks.init(p, lane);
+    unit = blocks.find(p, blockIdx.x, lane);
+    if (lane == 0) {
+      h.units[0] = unit;
+      mbar_arrive(&h.unit_full[0]);
     }
   }
   if (warp == kIssuer) {
@@ -549,11 +599,16 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
     unsigned s_phase = 0, o_phase = 0;
     int ring = 0;                                     // ring position of the unit's first tile
     bool again = false;
-    if (TREE) units.save(h.walk[warp], lane);
+    if constexpr (TREE) units.save(h.walk[warp], lane);
     for (;;) {
-      if (TREE) units.restore(h.walk[warp]);
-      const bool more = units.next(p, h, u);
-      if (TREE) units.save(h.walk[warp], lane);
+      bool more;
+      if constexpr (TREE) {
+        units.restore(h.walk[warp]);
+        more = units.next(p, h, u);
+        units.save(h.walk[warp], lane);
+      } else {
+        more = units.next_of_tile(p, h, u, t, warp, lane, tile_id);
+      }
       if (lane == 0) h.now[warp] = u;
       __syncwarp();
       if (!more) break;
@@ -563,7 +618,7 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
       const unsigned short* q = p.q + (int64_t)u.seq * p.q_seq + (int64_t)(u.key0 + u.tok0) * p.q_row +
                                 (int64_t)u.head * p.rep * p.q_head;
       const bool live = quarter * 32 < rows_here;      // this warp has rows; the others only keep step
-      if (again && steps) named_barrier(tile_id, 256); // the last unit's output has left the tile's shared memory
+      if (TREE && again && steps) named_barrier(tile_id, 256); // the last unit's output has left the tile's shared memory
       again = true;
       if (steps) {
         // Q, 16 bytes at a time, all loads in flight before the first store; rows that do not exist are zero
@@ -609,7 +664,7 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
         tc_fence_before();                             // the last unit's S and O have been read
         warp_arrive(&h.q_full[t], lane);
       }
-      if (TREE) {
+      if constexpr (TREE) {
         // the next unit's Q into L2: behind the stream of tiles a load from HBM takes microseconds
         Units<TREE> ahead = units;
         Unit n;
@@ -926,7 +981,14 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
     const bool leader = elect_one();
     unsigned issued = 0;
     bool on = true, gate = TREE;                      // (gate: within the first unit)
-    while (uniform(units.next(p, h, u))) {
+    unsigned taken = 1;                               // prompts: units put into the ring
+    bool asked = false;
+    for (;;) {
+      if constexpr (TREE) {
+        if (!uniform(units.next(p, h, u))) break;
+      } else {
+        if (!Units<false>::set(p, unit, u)) break;
+      }
       const int tile_end = uniform(u.tile_end);
       for (int j = uniform(u.tile_begin); j < tile_end; j++) {
         for (int kv = 0; kv < 2; kv++) {
@@ -953,10 +1015,38 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
         }
       }
       gate = false;
+      if constexpr (!TREE) {
+        // the next block that has not begun yet, if there is one
+        if (!on) break;
+        expect_tx(leader, &h.next_full, 16);
+        ask_for_block(leader, &h.next, &h.next_full);
+        asked = true;
+        if (!attn_wait(&h.next_full, (taken & 1) ^ 1, h)) break;
+        asked = false;
+        const int block = uniform(block_of_answer(&h.next));
+        fence_async_smem();                           // (read before the next answer is written there)
+        unit = block < 0 ? make_int4(-1, 0, 0, 0) : blocks.find(p, block, lane);
+        const int at = taken & (kUnitRing - 1);
+        if (!attn_wait(&h.unit_empty[at], (taken / kUnitRing & 1) ^ 1, h)) break;
+        if (lane == 0) {
+          h.units[at] = unit;
+          mbar_arrive(&h.unit_full[at]);
+        }
+        __syncwarp();
+        taken++;
+        // its Q into L2
+        const unsigned short* q = p.q + (int64_t)(unit.y + unit.z) * p.q_row + (int64_t)unit.x * p.rep * p.q_head;
+        for (int r = lane; r < unit.w * p.rep; r += 32) {
+          const int tok = div_rep(p, r);
+          const unsigned short* row = q + tok * p.q_row + (r - tok * p.rep) * p.q_head;
+          for (int x = 0; x < HD; x += 64) asm volatile("prefetch.global.L2 [%0];" ::"l"(row + x));
+        }
+      }
     }
     if (uniform(*(volatile int*)&h.dead)) {    // copies in flight land before the block ends
       for (unsigned i = issued > kN ? issued - kN : 0; i < issued; i++)
         for (int n = 0; n < 1 << 16 && !__all_sync(~0u, mbar_try_wait(&full[i % kN], i / kN & 1)); n++) {}
+      for (int n = 0; asked && n < 1 << 16 && !__all_sync(~0u, mbar_try_wait(&h.next_full, (taken & 1) ^ 1)); n++) {}
     }
   } else if (warp == kIssuer) {
     // ================================ the matrix products ==============================================================

@@ -126,6 +126,30 @@ __device__ __forceinline__ void expect_tx(bool leader, uint64_t* bar, unsigned b
       "r"(bytes), "r"((unsigned)leader)
       : "memory");
 }
+// Asks the hardware's scheduler for a block of this grid that has not been launched: 16 bytes of answer into shared memory,
+// counted on the barrier.  Not to be asked again after an answer without a block.
+__device__ __forceinline__ void ask_for_block(bool leader, void* answer, uint64_t* bar) {
+  asm volatile(
+      "{ .reg .pred q; setp.ne.u32 q, %2, 0;\n"
+      "  @q clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1]; }" ::"r"(
+          smem_u32(answer)),
+      "r"(smem_u32(bar)), "r"((unsigned)leader)
+      : "memory");
+}
+// the x index of the block of an answer, which will not be launched any more; -1: there was none
+__device__ __forceinline__ int block_of_answer(const void* answer) {
+  int block;
+  asm volatile(
+      "{ .reg .b128 a; .reg .pred p;\n"
+      "  ld.shared.b128 a, [%1];\n"
+      "  clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, a;\n"
+      "  mov.s32 %0, -1;\n"
+      "  @p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %0, a; }"
+      : "=r"(block)
+      : "r"(smem_u32(answer))
+      : "memory");
+  return block;
+}
 // shared memory written by this thread becomes visible to the asynchronous units (tensor cores, TMA)
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
