@@ -10,11 +10,12 @@
 // Work.  One block an SM: two row tiles of 128 rows share every K/V tile of 128 keys (prompts, large drafts), or, where a
 // draft has 128 rows at most, take every second key tile each and are joined at the end.  A producer warp keeps a ring of
 // tiles full by TMA, one warp issues the products (S and O in TMEM, P over S as the A operand of P V), four warpgroups
-// make the softmax, so that one tile's exponentials run beside the other's products.  Prompts: a block for 256 / rep
-// tokens of a kv head.  Trees: the key tiles of the whole batch in equal runs (below), parts joined by a second kernel.
+// make the softmax, so that one tile's exponentials run beside the other's products.  Prompts: a unit of 256 / rep
+// tokens of a kv head for a block, which takes over the units of blocks that have not begun while its own last tiles are on
+// their way (one unit a block: 468 us at 8192 tokens, 41 us for eight prompts of 1 to 1291 tokens; so 440 and 35 us).  Trees: the key tiles of the whole batch in equal runs (below), parts joined by a second kernel.
 //
 // What bounds it.  Prompts: the chain scores -> softmax -> products of a tile, 3650 cycles for 2054 cycles of products a
-// pair of tiles (the exponentials alone are 2048): 8192 tokens, 32 heads of 128 on 8, 550 GFLOP in 468 us = 1.17 PFLOP/s.
+// pair of tiles (the exponentials alone are 2048): 8192 tokens, 32 heads of 128 on 8, 550 GFLOP in 440 us = 1.25 PFLOP/s.
 // head_dim 64 has half the products for the same exponentials.  Trees: HBM in long runs (32 sequences of 8000 positions,
 // one token each: 1.05 GB in 168 us = 6.2 TB/s); a short call the 8 us that a cold block takes from its start to its first
 // output, of which the tiles are the least.  The 8-bit cache: its tiles' way through shared memory (raw in, f16 out, read
@@ -404,7 +405,10 @@ struct PromptBlocks {
   }
 };
 
-// Key tiles that row tile t of the unit works on; DUAL: every second one of the unit's.
+// Key tiles that row tile t of the unit works on; DUAL: every second one of the unit's.  A unit's key tiles are taken from the
+// last one down: those that hide keys are then among the first, which wants the careful softmax anyway (prompts of
+// 1 to 1291 tokens from the first one up 36.1 us, so 34.9 us; eight ragged sequences of up to 8000 positions with 32 tokens
+// each 45.9 and 45.0 us; a single token over 1025 positions 9.2 and 9.5 us).
 template <bool TREE>
 __device__ __forceinline__ int unit_steps(const AttnParams& p, const Unit& u, bool dual, int t) {
   const int n = u.tile_end - u.tile_begin;
@@ -678,14 +682,14 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
           }
         }
       }
-      // first step whose tile holds a key that a row of this tile may not see
-      const int clear = max((TREE ? u.len : u.tok0 + div_rep(p, row_first) + 1) / kTile - u.tile_begin, 0);
-      const int mask_from = dual ? (clear - t + 1) >> 1 : clear;
+      // the steps before this one have keys that a row of this tile may not see
+      const int hiding = (dual ? u.tile_end : u.tile_begin + steps) - (TREE ? u.len : u.tok0 + div_rep(p, row_first) + 1) / kTile;
+      const int mask_to = dual ? (hiding - t + 1) >> 1 : hiding;
       float m = -CUDART_INF_F, l = 0.f;
       // What the steps need of the unit they read from shared memory: a register spilled here would be fetched from behind
       // the stream of tiles.
       for (int i = 0; i < steps; i++) {
-        const bool masked = i >= mask_from;
+        const bool masked = i < mask_to;
         attn_wait(&h.s_full[t], s_phase & 1, h);
         s_phase++;
         __syncwarp();
@@ -738,7 +742,7 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
             const int row = v.row0 + (dual ? 0 : t * kTile) + wr, tok = div_rep(p, row);
 #pragma unroll
             for (int w = 0; w < 2; w++) {
-              const int first = (v.tile_begin + (dual ? 2 * i + t : i)) * kTile + half * 64 + 32 * w;
+              const int first = (dual ? v.tile_end - 1 - 2 * i - t : v.tile_begin + steps - 1 - i) * kTile + half * 64 + 32 * w;
               if (TREE) {
                 const int ctx = v.len - first;                      // context keys from `first` on
                 if (ctx < 32)
@@ -830,9 +834,9 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
           // What a mask hides must not come through 0 * V either: V rows that no row of the block sees become zero; if
           // a row that some of them see is not finite, this tile's product is made here, key by key.
           const volatile Unit& u = h.now[warp];
-          const int rel = dual ? 2 * i + t : i, key = (u.tile_begin + rel) * kTile;
+          const int tile = dual ? u.tile_end - 1 - 2 * i - t : u.tile_begin + steps - 1 - i, key = tile * kTile;
           const int key_end = TREE ? u.len + p.rows : u.tok0 + u.n_tok;      // keys nobody here sees: from it on
-          const int pos = ring + 2 * rel + 1, st = pos % L::kStages;
+          const int pos = ring + 2 * (u.tile_end - 1 - tile) + 1, st = pos % L::kStages;
           attn_wait(&h.full[st], pos / L::kStages & 1, h);
           unsigned char* vt = smem + L::kRing + st * L::kTileBytes;
           const int r = id & 127;
@@ -989,8 +993,8 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
       } else {
         if (!Units<false>::set(p, unit, u)) break;
       }
-      const int tile_end = uniform(u.tile_end);
-      for (int j = uniform(u.tile_begin); j < tile_end; j++) {
+      const int tile_begin = uniform(u.tile_begin);
+      for (int j = uniform(u.tile_end) - 1; j >= tile_begin; j--) {
         for (int kv = 0; kv < 2; kv++) {
           const int st = issued % kN;
           if (gate && issued == 2) {   // the first Q is not to queue behind the whole ring
@@ -1062,7 +1066,8 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
     bool on = true;
     while (uniform(units.next(p, h, u))) {
       const int n0 = uniform(unit_steps<TREE>(p, u, dual, 0)), n1 = uniform(unit_steps<TREE>(p, u, dual, 1));
-      const int most = max(n0, n1), tile_begin = uniform(u.tile_begin);
+      const int most = max(n0, n1), tile_end = uniform(u.tile_end);
+      const int skip[2] = {dual || !n0 ? 0 : most - n0, 0};     // the first key tiles that row tile 0 has no part in
       int all_see[2];                                           // first key that a row of tile t may not see
 #pragma unroll
       for (int t = 0; t < 2; t++) all_see[t] = uniform(TREE ? u.len : u.tok0 + div_rep(p, u.row0 + t * kTile) + 1);
@@ -1078,36 +1083,33 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
           mma_ss(leader, tmem + t * kTile, qa + off, ka + off, kIdS, k > 0);
         }
         mma_commit(leader, &h.s_full[t]);
-        if (dual || t == 1 || i >= n1) mma_commit(leader, &h.empty[st]);
+        if (dual || t == 1 || n1 == 0) mma_commit(leader, &h.empty[st]);
       };
-#pragma unroll
-      for (int t = 0; t < 2; t++) {
-        if (!(t ? n1 : n0)) continue;
-        on = attn_wait(&h.q_full[t], q_phase[t]++ & 1, h) && on;
-        scores(t, 0);
-      }
-      for (int i = 0; i < most; i++) {
+      for (int i = -1; i < most; i++) {
 #pragma unroll
         for (int t = 0; t < 2; t++) {
-          const int n = t ? n1 : n0;
-          if (i >= n) continue;
-          const int rel = dual ? 2 * i + t : i, pos = ring + 2 * rel + 1, st = pos % L::kStages;
-          const bool masked = (tile_begin + rel + 1) * kTile > all_see[t];
-          on = attn_wait(&h.full[st], pos / L::kStages & 1, h) && on;
-          on = attn_wait(&h.p_full[t], p_phase[t]++ & 1, h) && on;
-          if (on) {
-            tc_fence_after();
-            if (!masked || !uniform(*(volatile int*)&h.skip[t])) {
-              const uint64_t va = v_desc + st * kTileStep;
+          const int end = (t ? n1 : n0) + skip[t], from = skip[t];
+          if (i >= end || from == end) continue;
+          if (i >= from) {
+            const int rel = dual ? 2 * i + t : i, pos = ring + 2 * rel + 1, st = pos % L::kStages;
+            const bool masked = (tile_end - rel) * kTile > all_see[t];
+            on = attn_wait(&h.full[st], pos / L::kStages & 1, h) && on;
+            on = attn_wait(&h.p_full[t], p_phase[t]++ & 1, h) && on;
+            if (on) {
+              tc_fence_after();
+              if (!masked || !uniform(*(volatile int*)&h.skip[t])) {
+                const uint64_t va = v_desc + st * kTileStep;
 #pragma unroll
-              for (int k = 0; k < kTile / 16; k++)
-                mma_ts(leader, tmem + 2 * kTile + t * HD, tmem + t * kTile + k / 4 * 64 + k % 4 * 8, va + k * 128, kIdO,
-                       i > 0 || k > 0);
+                for (int k = 0; k < kTile / 16; k++)
+                  mma_ts(leader, tmem + 2 * kTile + t * HD, tmem + t * kTile + k / 4 * 64 + k % 4 * 8, va + k * 128, kIdO,
+                         i > from || k > 0);
+              }
+              if (i + 1 == end) mma_commit(leader, &h.o_done[t]);
+              if (dual || t == 1 || n1 == 0) mma_commit(leader, &h.empty[st]);
             }
-            if (i + 1 == n) mma_commit(leader, &h.o_done[t]);
-            if (dual || t == 1 || i >= n1) mma_commit(leader, &h.empty[st]);
           }
-          if (i + 1 < n) scores(t, i + 1);
+          if (i + 1 == from) on = attn_wait(&h.q_full[t], q_phase[t]++ & 1, h) && on;
+          if (i + 1 >= from && i + 1 < end) scores(t, i + 1);
         }
       }
       ring += uniform(2 * (u.tile_end - u.tile_begin));
