@@ -10,11 +10,12 @@
 // Work.  One block an SM: two row tiles of 128 rows share every K/V tile of 128 keys (prompts, large drafts), or, where a
 // draft has 128 rows at most, take every second key tile each and are joined at the end.  A producer warp keeps a ring of
 // tiles full by TMA, one warp issues the products (S and O in TMEM, P over S as the A operand of P V), four warpgroups
-// make the softmax, so that one tile's exponentials run beside the other's products.  Prompts: a unit of 256 / rep
-// tokens of a kv head for a block, which takes over the units of blocks that have not begun while its own last tiles are on
-// their way (one unit a block: 468 us at 8192 tokens, 41 us for eight prompts of 1 to 1291 tokens; so 440 and 35 us).  Trees: the key tiles of the whole batch in equal runs (below), parts joined by a second kernel.
+// make the softmax, so that one tile's exponentials run beside the other's products.  Prompts: units of 256 / rep tokens of
+// a kv head, one for each block of the grid; a block that runs takes over the units of blocks that have not begun while its
+// own last tiles are on their way (one unit a block: 468 us at 8192 tokens, 41 us for eight prompts of 1 to 1291 tokens; so:
+// 440 and 35 us).  Trees: the key tiles of the whole batch in equal runs (below), parts joined by a second kernel.
 //
-// What bounds it.  Prompts: the chain scores -> softmax -> products of a tile, 3650 cycles for 2054 cycles of products a
+// What bounds it.  Prompts: the chain scores -> softmax -> products of a tile, about 3500 cycles for 2054 cycles of products a
 // pair of tiles (the exponentials alone are 2048): 8192 tokens, 32 heads of 128 on 8, 550 GFLOP in 440 us = 1.25 PFLOP/s.
 // head_dim 64 has half the products for the same exponentials.  Trees: HBM in long runs (32 sequences of 8000 positions,
 // one token each: 1.05 GB in 168 us = 6.2 TB/s); a short call the 8 us that a cold block takes from its start to its first
