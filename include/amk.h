@@ -395,8 +395,8 @@ amk_status amk_prompt_attention(const amk_prompt_args* args, char* msg, size_t m
  *   max_len       upper bound of the lengths in cache_len, for the division of the work alone (results do not depend on
  *                 whether it holds); 0: n_slots - n_rows
  *   workspace     DEVICE, 256-byte aligned, at least amk_tree_workspace_bytes of the same arguments (pointers and strides
- *                 do not matter there) on the same device; scratch,
- *                 needs no initial value; two calls that may overlap need one each
+ *                 do not matter there) on the same device, NULL if that is 0; scratch, needs no initial value; two calls
+ *                 that may overlap need one each
  * Pointers 16-byte aligned, strides multiples of 16 bytes.  Arithmetic as amk_prompt_attention's; over the 8-bit cache the
  * softmax numerators are f16 (2^-11), the codes exact, and q exact but for values 2^-30 below its row's largest.
  * Errors as amk_prompt_attention.

@@ -394,7 +394,8 @@ def amk_tree_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cache_
             if len(_tree_bytes) >= 4096:
                 _tree_bytes.clear()
             _tree_bytes[key] = need
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        if need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
         have = need
     else:
         if not workspace.is_contiguous():
@@ -402,7 +403,7 @@ def amk_tree_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cache_
         have = workspace.numel() * workspace.element_size()
     args = _TREE.pack(*plan, scale or 0.0, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
                       0 if lse is None else lse.data_ptr(), cache_len.data_ptr(), 0 if mask is None else mask.data_ptr(),
-                      workspace.data_ptr(), have, qs, qr, qh, ks, kh, kr, vs, vh, vr, os_, orow, oh)
+                      0 if workspace is None else workspace.data_ptr(), have, qs, qr, qh, ks, kh, kr, vs, vh, vr, os_, orow, oh)
     _run(lib.amk_tree_attention, name, dev, args)
     return out
 

@@ -59,8 +59,40 @@ cudaError_t allow_smem() {
   if (done.load(std::memory_order_acquire) & bit) return cudaSuccess;
   e = cudaFuncSetAttribute(amk::attn_kernel<HD, TREE, FP8>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                            amk::AttnSmem<HD, FP8>::kBytes);
+  if (e == cudaSuccess && TREE)
+    e = cudaFuncSetAttribute(amk::attn_kernel<HD, TREE, FP8>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_release);
   return e;
+}
+
+// Clusters of 2^i blocks of a tree kernel that the device can run at the same time, asked once on each device; 0: none, or it
+// does not say.
+template <int HD, bool FP8>
+int cluster_room(int i) {
+  static std::atomic<int> known[8][5];                 // plus one
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return 0;
+  }
+  if (dev < 8 && known[dev][i].load(std::memory_order_acquire)) return known[dev][i].load(std::memory_order_acquire) - 1;
+  int n = 0;
+  cudaLaunchAttribute at;
+  at.id = cudaLaunchAttributeClusterDimension;
+  at.val.clusterDim.x = 1u << i, at.val.clusterDim.y = at.val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(1u << i);
+  cfg.blockDim = dim3(FP8 ? 768 : 640);
+  cfg.dynamicSmemBytes = amk::AttnSmem<HD, FP8>::kBytes;
+  cfg.attrs = &at;
+  cfg.numAttrs = 1;
+  if (allow_smem<HD, true, FP8>() != cudaSuccess ||
+      cudaOccupancyMaxActiveClusters(&n, amk::attn_kernel<HD, true, FP8>, &cfg) != cudaSuccess) {
+    (void)cudaGetLastError();
+    n = 0;
+  }
+  if (dev < 8) known[dev][i].store(n + 1, std::memory_order_release);
+  return n;
 }
 
 template <int HD, bool TREE, bool FP8>
@@ -68,6 +100,19 @@ cudaError_t launch_attn(const AttnParams& p, const CUtensorMap& k, const CUtenso
                         cudaStream_t st) {
   const cudaError_t e = allow_smem<HD, TREE, FP8>();
   if (e != cudaSuccess) return e;
+  if (TREE && p.cluster > 1) {
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = (unsigned)p.cluster, at.val.clusterDim.y = at.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(blocks);
+    cfg.blockDim = dim3(FP8 ? 768 : 640);
+    cfg.dynamicSmemBytes = amk::AttnSmem<HD, FP8>::kBytes;
+    cfg.stream = st;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, amk::attn_kernel<HD, TREE, FP8>, p, k, v);
+  }
   amk::attn_kernel<HD, TREE, FP8><<<blocks, FP8 ? 768 : 640, amk::AttnSmem<HD, FP8>::kBytes, st>>>(p, k, v);
   return cudaGetLastError();
 }
@@ -98,9 +143,15 @@ int sm_count() {
   return n;
 }
 
-// How a tree call is divided: rows of a block, blocks, scratch.
+// How a tree call is divided: rows of a block, blocks, scratch.  A short call has a block, or a cluster of blocks, for each
+// item: one launch, no scratch.  Others have runs of equal length for all blocks and a second kernel that joins the parts.
+// Clusters are for items of two tiles a block and few rows, since the parts meet in distributed shared memory, which is
+// slower than L2.  Clusters / runs, us a call in a graph: 8 rows of 64, 17 tiles (16 blocks an item) 10.6 / 11.1; 16 rows of
+// 128, 8 tiles 13.3 / 13.3, over the 8-bit cache 16.2 / 16.8; 15 rows of 64, 4 tiles 10.3 / 11.0; 64 items of 32 rows of 128,
+// 4 tiles 15.0 / 18.3; 112 items of 128 rows of 128, 2 tiles 13.2 / 17.8; but 8 items of 32 rows of 128, 16 tiles 13.7 / 13.1;
+// 128 rows of 64, 4 tiles 14.6 / 11.6.
 struct TreePlan {
-  int part_rows, row_tiles;
+  int part_rows, row_tiles, cluster;
   unsigned blocks;
   size_t bytes;
 };
@@ -111,9 +162,25 @@ TreePlan tree_plan(const amk_tree_args& a) {
   t.part_rows = rows <= amk::kTile ? amk::kTile : 2 * amk::kTile;
   t.row_tiles = (int)((rows + t.part_rows - 1) / t.part_rows);
   const int64_t most = a.n_slots - a.n_rows, len = a.max_len && a.max_len < most ? a.max_len : most;
-  const int64_t tiles = (len + a.n_rows + amk::kTile - 1) / amk::kTile;
-  const int64_t runs = ((tiles + amk::kUnitCost) * a.n_kv_heads * t.row_tiles * a.n_seqs + kMinTiles - 1) / kMinTiles;
+  const int64_t tiles = (len + a.n_rows + amk::kTile - 1) / amk::kTile, items = (int64_t)a.n_kv_heads * t.row_tiles * a.n_seqs;
   const int sms = sm_count();
+  t.cluster = 0;
+  if (t.row_tiles == 1 && t.part_rows == amk::kTile && items <= sms) {
+    int i = 0;
+    while (i < 4 && tiles > kMinTiles << i) {
+      const int more = a.head_dim == 64 ? a.kv_dtype ? cluster_room<64, true>(i + 1) : cluster_room<64, false>(i + 1)
+                                        : a.kv_dtype ? cluster_room<128, true>(i + 1) : cluster_room<128, false>(i + 1);
+      if (more < items) break;
+      i++;
+    }
+    if (tiles <= kMinTiles << i && (i == 0 || rows * a.head_dim <= (i == 1 ? 4096 : 2048))) {
+      t.cluster = 1 << i;
+      t.blocks = (unsigned)(items << i);
+      t.bytes = 0;
+      return t;
+    }
+  }
+  const int64_t runs = ((tiles + amk::kUnitCost) * items + kMinTiles - 1) / kMinTiles;
   t.blocks = (unsigned)(runs < sms ? runs : sms);
   t.bytes = (size_t)2 * t.blocks * t.part_rows * (a.head_dim + 1) * 4;
   return t;
@@ -264,7 +331,7 @@ extern "C" amk_status amk_tree_attention(const amk_tree_args* args, char* msg, s
   AMK_TRY(check_stride(fail, "out row", a.n_rows, &a.out_row, hd, 2));
   AMK_TRY(check_stride(fail, "out head", a.n_q_heads, &a.out_head, hd, 2));
   const TreePlan t = tree_plan(a);
-  if (!a.workspace || a.workspace_bytes < t.bytes)
+  if (t.bytes && (!a.workspace || a.workspace_bytes < t.bytes))
     return fail(AMK_ERR_INVALID_ARG, "workspace of %llu bytes, %zu are needed", (unsigned long long)(a.workspace ? a.workspace_bytes : 0),
                 t.bytes);
   AttnParams p{};
@@ -276,7 +343,7 @@ extern "C" amk_status amk_tree_attention(const amk_tree_args* args, char* msg, s
   p.n_seqs = (int)a.n_seqs, p.nq = (int)a.n_q_heads, p.nkv = (int)a.n_kv_heads, p.rep = p.nq / p.nkv;
   p.rep_inv = p.rep == 1 ? 0 : (unsigned)(((1ull << 32) + p.rep - 1) / p.rep);
   p.rows = (int)a.n_rows, p.slots = (int)a.n_slots;
-  p.part_rows = t.part_rows, p.row_tiles = t.row_tiles, p.min_tiles = kMinTiles;
+  p.part_rows = t.part_rows, p.row_tiles = t.row_tiles, p.min_tiles = kMinTiles, p.cluster = t.cluster;
   p.scale = a.scale > 0.f ? a.scale : 1.f / sqrtf((float)hd);
   const bool fp8 = esz == 1;
   CUtensorMap mk, mv;
@@ -289,6 +356,6 @@ extern "C" amk_status amk_tree_attention(const amk_tree_args* args, char* msg, s
     e = fp8 ? launch_attn<64, true, true>(p, mk, mv, t.blocks, st) : launch_attn<64, true, false>(p, mk, mv, t.blocks, st);
   else
     e = fp8 ? launch_attn<128, true, true>(p, mk, mv, t.blocks, st) : launch_attn<128, true, false>(p, mk, mv, t.blocks, st);
-  if (e == cudaSuccess) e = hd == 64 ? launch_join<64>(p, t.blocks, st) : launch_join<128>(p, t.blocks, st);
+  if (e == cudaSuccess && !t.cluster) e = hd == 64 ? launch_join<64>(p, t.blocks, st) : launch_join<128>(p, t.blocks, st);
   return e == cudaSuccess ? AMK_OK : fail(AMK_ERR_CUDA, "launch failed: %s", cudaGetErrorString(e));
 }

@@ -46,6 +46,7 @@ struct AttnParams {
   int part_rows;                   // tree: 128 (both warpgroups work on the same rows) or 256
   int row_tiles;                   // tree: blocks of part_rows rows per (sequence, kv head)
   int min_tiles;                   // tree: key tiles a block takes at least
+  int cluster;                     // tree: blocks of one item, which meet at the end; 0: runs and a second kernel
   unsigned rep_inv;                // ceil(2^32 / rep), 0 for rep = 1
   float scale;
 };
@@ -512,7 +513,14 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
 
   if (warp == 0) {
     // which part of the work is this block's
-    if (TREE) {
+    if (TREE && p.cluster) {
+      const int item = blockIdx.x / p.cluster, rank = blockIdx.x - item * p.cluster, seq = item / p.nkv;
+      const int len = __ldg(p.lens + seq), tiles = tree_tiles(p, len), per = (tiles + p.cluster - 1) / p.cluster;
+      const int begin = min(rank * per, tiles);
+      if (lane == 0)
+        h.unit[0] = seq, h.unit[1] = item - seq * p.nkv, h.unit[2] = kUnitCost + begin, h.unit[3] = len,
+        h.unit[4] = min(per, tiles - begin);
+    } else if (TREE) {
       const int mine = tree_slots_of(p, lane);
       const int per = tree_run(p, mine, lane, gridDim.x);
       int at = (int)blockIdx.x * per, seq = 0, item = 0, within = 0, len = 0, left = 0;
@@ -941,6 +949,12 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
               *(uint4*)(qs + wr * (HD * 2) + (((x + k) / 8 ^ (wr & 7)) << 4)) =
                   make_uint4(pack_bf16(v[k], v[k + 1]), pack_bf16(v[k + 2], v[k + 3]), pack_bf16(v[k + 4], v[k + 5]),
                              pack_bf16(v[k + 6], v[k + 7]));
+          } else if (TREE && p.cluster) {
+            // over the ring, whose products are done: a row's 16-byte chunks permuted as above
+#pragma unroll
+            for (int k = 0; k < 16; k += 4)
+              *(float4*)(smem + L::kRing + wr * (HD * 4) + (((x + k) / 4 ^ (wr & 7)) << 4)) =
+                  make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
           } else if (valid) {
             // [slot][column / 4][row][4]: a warp's rows lie side by side
             float* part = p.part_o + ((slot * (HD / 4) + x / 4) * p.part_rows + part_row) * 4;
@@ -964,7 +978,9 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
           }
         }
         if (valid && half == 0) {
-          if (!whole) {
+          if (TREE && !whole && p.cluster) {
+            h.mx[0][0][wr] = lse2;
+          } else if (!whole) {
             p.part_lse[slot * p.part_rows + part_row] = lse2;
           } else if (p.lse) {
             const int64_t gtok = TREE ? (int64_t)u.seq * p.rows + tok : (int64_t)u.key0 + u.tok0 + tok;
@@ -1154,6 +1170,59 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
   __syncthreads();
   tc_fence_after();
   if (warp == kIssuer) tmem_free(tmem, 512);
+  if (TREE && p.cluster) {
+    // the item's parts joined in the cluster: each block takes some of the rows and reads the others' parts of them
+    if (p.cluster > 1) cluster_sync();
+    if (warp < 16) {
+      const int item = blockIdx.x / p.cluster, rank = blockIdx.x - item * p.cluster, seq = item / p.nkv;
+      const int tiles = tree_tiles(p, h.unit[3]), per = (tiles + p.cluster - 1) / p.cluster;
+      const int parts = tiles ? (tiles + per - 1) / per : 0;      // 1: complete already
+      const int all = p.rows * p.rep, each = (all + p.cluster - 1) / p.cluster, last = min(all, (rank + 1) * each);
+      constexpr int kChunks = HD / 4;
+      if (parts != 1)
+        for (int e = threadIdx.x + rank * each * kChunks; e < last * kChunks; e += 512) {
+          const int row = e / kChunks, ch = e % kChunks;
+          const float* lse_at = &h.mx[0][0][row];
+          const unsigned char* o_at = smem + L::kRing + row * (HD * 4) + ((ch ^ (row & 7)) << 4);
+          float m = -CUDART_INF_F, sum = 0.f, v[4] = {};
+          for (int b0 = 0; b0 < parts; b0 += 8) {          // eight parts' loads under way
+            float x[8];
+            float4 y[8];
+#pragma unroll
+            for (int b = 0; b < 8; b++) {
+              const int from = min(b0 + b, parts - 1);
+              x[b] = remote_f32(lse_at, from), y[b] = remote_f32x4(o_at, from);
+              if (b0 + b >= parts) x[b] = -CUDART_INF_F;
+            }
+            float mn = m;
+#pragma unroll
+            for (int b = 0; b < 8; b++) mn = fmaxf(mn, x[b]);
+            const float f = m == mn ? 1.f : exp2f(m - mn);
+            m = mn;
+            sum *= f;
+#pragma unroll
+            for (int k = 0; k < 4; k++) v[k] *= f;
+#pragma unroll
+            for (int b = 0; b < 8; b++) {
+              const float w = x[b] == -CUDART_INF_F ? 0.f : exp2f(x[b] - m);         // (nothing seen: 0)
+              sum += w;
+              v[0] += w * y[b].x, v[1] += w * y[b].y, v[2] += w * y[b].z, v[3] += w * y[b].w;
+            }
+          }
+          const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+          for (int k = 0; k < 4; k++) v[k] = parts ? v[k] * inv : CUDART_NAN_F;
+          const int tok = div_rep(p, row), head = (item - seq * p.nkv) * p.rep + row - tok * p.rep;
+          *(uint2*)(p.out + (int64_t)seq * p.o_seq + tok * p.o_row + head * p.o_head + ch * 4) =
+              make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+          if (p.lse && ch == 0)
+            p.lse[((int64_t)seq * p.rows + tok) * p.nq + head] =
+                !parts ? CUDART_NAN_F : sum == 0.f ? -CUDART_INF_F : (m + log2f(sum)) * 0.6931471805599453f;
+        }
+    }
+    __syncwarp();
+    if (p.cluster > 1) cluster_sync();                            // nobody leaves while its parts are read
+  }
 }
 
 // ---- parts of one item joined (tree) ----------------------------------------------------------------------------

@@ -426,6 +426,29 @@ def test_tree_attention_many_sequences(amk):
             assert bool(torch.isnan(out[b].float()).all())
 
 
+@pytest.mark.parametrize("cache", ["bf16", "fp8"])
+@pytest.mark.parametrize("nq,nkv,hd,rows,slots", [(4, 2, 64, 3, 2048), (2, 1, 128, 7, 2000), (8, 4, 128, 8, 1000), (9, 3, 64, 5, 500),
+                                                  (16, 8, 64, 16, 260), (32, 2, 64, 8, 256), (3, 1, 128, 1, 128)])
+def test_tree_attention_short_calls(amk, cache, nq, nkv, hd, rows, slots):
+    """Calls whose blocks join their parts in one launch: lengths that leave some or most of an item's blocks without a
+    tile, a length that breaks max_len, one that is impossible."""
+    q, k, v = tree_inputs(1, rows, slots, nq, nkv, hd, cache, slots + rows)
+    bits = tree_bits(np.random.default_rng(rows), rows)[None]
+    bits[0, rows // 2] = rows == 1
+    most = slots - rows
+    for n in sorted({0, 1, 127 - rows, 128 - rows, 129 - rows, 200, 3 * 128, most // 2, most - 1, most}):
+        if not 0 <= n <= most:
+            continue
+        length = torch.tensor([n], dtype=torch.int32, device=DEV)
+        for hint in (None, 100):
+            lse = torch.full((1, rows, nq), math.nan, device=DEV)
+            out = amk.amk_tree_attention(q, k, v, length, words(bits), max_len=hint and min(hint, slots), lse=lse)
+            check_tree(q, k, v, [n], bits, out, lse, hd ** -0.5, n)
+    lse = torch.zeros(1, rows, nq, device=DEV)
+    out = amk.amk_tree_attention(q, k, v, torch.tensor([most + 1], dtype=torch.int32, device=DEV), words(bits), lse=lse)
+    assert bool(torch.isnan(out.float()).all()) and bool(torch.isnan(lse).all())
+
+
 @pytest.mark.parametrize("nq,nkv,hd", [(4096, 4096, 128), (4096, 256, 64)])
 def test_attentions_of_the_most_heads(amk, nq, nkv, hd):
     rows, slots, lens = 2, 150, [131]
