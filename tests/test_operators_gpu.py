@@ -195,6 +195,30 @@ def test_prompt_attention_many_short_prompts(amk):
     check(out, None, attention64(q, k, v, sees, hd ** -0.5))
 
 
+@pytest.mark.parametrize("hd", [64, 128])
+def test_prompt_attention_thousands_of_prompts(amk, hd):
+    """Prompts of 0 to 40 tokens and some of 300 to 600, several units for every block; some bounds are impossible and
+    their prompts left out."""
+    rng = np.random.default_rng(hd)
+    lens = [int(x) for x in rng.integers(0, 41, 2500)]
+    for at in rng.integers(0, 2500, 12):
+        lens[at] = int(rng.integers(300, 601))
+    q, k, v, cu = prompt_inputs(lens, 6, 2, hd, 77)
+    total, ends = sum(lens), np.cumsum([0] + lens)
+    out = torch.full((total, 6, hd), 3.0, dtype=torch.bfloat16, device=DEV)
+    bad = sorted(int(x) for x in rng.choice(np.arange(1, 2499), 9, replace=False))
+    for at in bad:
+        cu[at] = total + 5 if at % 2 else -1            # the end of prompt at - 1, the beginning of prompt at
+    amk.amk_prompt_attention(q, k, v, cu, out=out)
+    skipped = {x for at in bad for x in (at - 1, at)}
+    for s, n in enumerate(lens):
+        a = int(ends[s])
+        if s in skipped:
+            assert bool((out[a:a + n] == 3).all()), s
+        elif n and (n > 200 or s % 50 == 0):
+            check_prompt(q, k, v, [n], out, None, hd ** -0.5, start=a)
+
+
 @pytest.mark.parametrize("n_seqs", [31, 32, 33, 65])
 def test_prompt_attention_around_32_prompts(amk, n_seqs):
     """Blocks are looked up in another way from 33 prompts on; with one head group of 16 a block is 16 tokens."""
