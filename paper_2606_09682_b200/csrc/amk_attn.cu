@@ -100,21 +100,19 @@ cudaError_t launch_attn(const AttnParams& p, const CUtensorMap& k, const CUtenso
                         cudaStream_t st) {
   const cudaError_t e = allow_smem<HD, TREE, FP8>();
   if (e != cudaSuccess) return e;
-  if (TREE && p.cluster > 1) {
-    cudaLaunchAttribute at;
-    at.id = cudaLaunchAttributeClusterDimension;
-    at.val.clusterDim.x = (unsigned)p.cluster, at.val.clusterDim.y = at.val.clusterDim.z = 1;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(blocks);
-    cfg.blockDim = dim3(FP8 ? 768 : 640);
-    cfg.dynamicSmemBytes = amk::AttnSmem<HD, FP8>::kBytes;
-    cfg.stream = st;
-    cfg.attrs = &at;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, amk::attn_kernel<HD, TREE, FP8>, p, k, v);
-  }
-  amk::attn_kernel<HD, TREE, FP8><<<blocks, FP8 ? 768 : 640, amk::AttnSmem<HD, FP8>::kBytes, st>>>(p, k, v);
-  return cudaGetLastError();
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;         // the kernel waits for the one before it itself
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = (unsigned)p.cluster, at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(blocks);
+  cfg.blockDim = dim3(FP8 ? 768 : 640);
+  cfg.dynamicSmemBytes = amk::AttnSmem<HD, FP8>::kBytes;
+  cfg.stream = st;
+  cfg.attrs = at;
+  cfg.numAttrs = TREE && p.cluster > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, amk::attn_kernel<HD, TREE, FP8>, p, k, v);
 }
 
 template <int HD>

@@ -511,6 +511,23 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
   const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   const bool dual = TREE && p.part_rows == kTile;
 
+  // What touches no memory of the stream's comes first: the grid may begin while the one before it ends.
+  if (warp == kIssuer) {
+    tmem_alloc(&h.tmem, 512);
+    if (lane == 0) {
+      for (int i = 0; i < L::kStages; i++) mbar_init(&h.full[i], FP8 ? 6 : 1), mbar_init(&h.empty[i], 1);
+      for (int i = 0; i < L::kRawStages; i++) mbar_init(&h.raw_full[i], 1), mbar_init(&h.raw_empty[i], 6);
+      for (int t = 0; t < 2; t++) {
+        mbar_init(&h.q_full[t], 8), mbar_init(&h.s_full[t], 1);
+        mbar_init(&h.p_full[t], 8), mbar_init(&h.o_done[t], 1);
+      }
+      mbar_init(&h.fin, 1);
+      h.dead = 0;
+      mbar_fence_init();
+    }
+  }
+  if (warp == kProducer) prefetch_map(lane == 0, &map_k), prefetch_map(lane == 0, &map_v);
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   if (warp == 0) {
     // which part of the work is this block's
     if (TREE && p.cluster) {
@@ -564,20 +581,6 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
     if (lane == 0) {
       h.units[0] = unit;
       mbar_arrive(&h.unit_full[0]);
-    }
-  }
-  if (warp == kIssuer) {
-    tmem_alloc(&h.tmem, 512);
-    if (lane == 0) {
-      for (int i = 0; i < L::kStages; i++) mbar_init(&h.full[i], FP8 ? 6 : 1), mbar_init(&h.empty[i], 1);
-      for (int i = 0; i < L::kRawStages; i++) mbar_init(&h.raw_full[i], 1), mbar_init(&h.raw_empty[i], 6);
-      for (int t = 0; t < 2; t++) {
-        mbar_init(&h.q_full[t], 8), mbar_init(&h.s_full[t], 1);
-        mbar_init(&h.p_full[t], 8), mbar_init(&h.o_done[t], 1);
-      }
-      mbar_init(&h.fin, 1);
-      h.dead = 0;
-      mbar_fence_init();
     }
   }
   tc_fence_before();

@@ -142,6 +142,9 @@ __device__ __forceinline__ void tma_load_4d(bool leader, void* dst, const CUtens
       "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar)), "r"((unsigned)leader)
       : "memory");
 }
+__device__ __forceinline__ void prefetch_map(bool leader, const CUtensorMap* map) {
+  asm volatile("{ .reg .pred q; setp.ne.u32 q, %1, 0;\n  @q prefetch.tensormap [%0]; }" ::"l"(map), "r"((unsigned)leader) : "memory");
+}
 __device__ __forceinline__ void expect_tx(bool leader, uint64_t* bar, unsigned bytes) {
   asm volatile(
       "{ .reg .pred q; setp.ne.u32 q, %2, 0;\n"
