@@ -527,7 +527,7 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
     }
   }
   if (warp == kProducer) prefetch_map(lane == 0, &map_k), prefetch_map(lane == 0, &map_v);
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  wait_for_grid_before();
   if (warp == 0) {
     // which part of the work is this block's
     if (TREE && p.cluster) {
@@ -1265,7 +1265,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attn_join_kernel(const AttnPa
   const int c0 = first / per, parts = tiles ? (first + tiles - 1) / per - c0 + 1 : 0;
   // every thread waits for the attention kernel, also one that has nothing to do: what follows in the stream waits for
   // this grid alone
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  wait_for_grid_before();
   if (parts == 1) return;                            // complete already
   const bool valid = row < p.rows * p.rep;
   float m = -CUDART_INF_F, sum = 0.f, v[8] = {};

@@ -2,6 +2,7 @@
 #include <cuda_runtime.h>
 
 #include "amk_op_util.h"
+#include "amk_ptx.cuh"
 
 namespace {
 
@@ -15,6 +16,7 @@ __global__ void __launch_bounds__(THREADS) kv_compact_kernel(uint4* kv, int64_t 
                                                              int64_t max_seq, int row_pieces, const int* base_of,
                                                              const int* keep_of, int64_t max_keep, const int* count_of) {
   const int plane = blockIdx.x % n_planes, cache = blockIdx.x / n_planes;
+  amk::wait_for_grid_before();
   const int base = base_of[cache], n = count_of[cache];
   const int* keep = keep_of + (int64_t)cache * max_keep;
   bool bad = n < 0 || n > max_keep || base < 0;
@@ -62,12 +64,18 @@ extern "C" amk_status amk_kv_compact(void* kv, int64_t n_caches, int64_t cache_s
   const cudaStream_t st = (cudaStream_t)cuda_stream;
   // (26 rows of 256 bytes in 512 planes: 3.1 us the small way; 5000 rows of 128 bytes in 352 planes, 422 MB: 256 threads x 4
   // pieces 86 us, 512 x 8 84 us, 1024 x 4 78 us, 1024 x 8 73 us = 5.8 TB/s)
-  if (max_keep * row_bytes <= 65536)
-    kv_compact_kernel<256, 4><<<(unsigned)blocks, 256, 0, st>>>((uint4*)kv, cache_stride / 16, (int)n_planes, max_seq,
-                                                                (int)(row_bytes / 16), base, keep, max_keep, count);
-  else
-    kv_compact_kernel<1024, 8><<<(unsigned)blocks, 1024, 0, st>>>((uint4*)kv, cache_stride / 16, (int)n_planes, max_seq,
-                                                                (int)(row_bytes / 16), base, keep, max_keep, count);
-  const cudaError_t e = cudaGetLastError();
+  const bool few = max_keep * row_bytes <= 65536;
+  cudaLaunchAttribute at;
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;            // the kernel waits for the one before it itself
+  at.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)blocks);
+  cfg.blockDim = dim3(few ? 256 : 1024);
+  cfg.stream = st;
+  cfg.attrs = &at;
+  cfg.numAttrs = 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, few ? kv_compact_kernel<256, 4> : kv_compact_kernel<1024, 8>, (uint4*)kv,
+                                           cache_stride / 16, (int)n_planes, max_seq, (int)(row_bytes / 16), base, keep, max_keep,
+                                           count);
   return e == cudaSuccess ? AMK_OK : fail(AMK_ERR_CUDA, "launch failed: %s", cudaGetErrorString(e));
 }

@@ -201,6 +201,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 5 : 3) logprobs_ker
   __shared__ float bound;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const unsigned rank = C > 1 ? cluster_rank() : 0;
+  amk::wait_for_grid_before();
   const int64_t row = C > 1 ? blockIdx.x / C : blockIdx.x;
   const T* x = logits + row * a.stride;
   const int vocab = (int)a.vocab;
@@ -418,19 +419,17 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 5 : 3) logprobs_ker
 
 template <class T>
 cudaError_t launch(const void* logits, const Args& a, int64_t rows, int C, cudaStream_t st) {
-  if (C == 1) {
-    logprobs_kernel<T><<<(unsigned)rows, kThreads, 0, st>>>((const T*)logits, a, 1);
-    return cudaGetLastError();
-  }
-  cudaLaunchAttribute at;
-  at.id = cudaLaunchAttributeClusterDimension;
-  at.val.clusterDim.x = (unsigned)C, at.val.clusterDim.y = at.val.clusterDim.z = 1;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;         // the kernel waits for the one before it itself
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = (unsigned)C, at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(rows * C));
   cfg.blockDim = dim3(kThreads);
   cfg.stream = st;
-  cfg.attrs = &at;
-  cfg.numAttrs = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = C > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, logprobs_kernel<T>, (const T*)logits, a, C);
 }
 

@@ -147,4 +147,8 @@ __device__ __forceinline__ uint2 ld_pair(const void* p) {
                : "memory");
   return make_uint2((unsigned)w, (unsigned)(w >> 32));
 }
+// For a grid that may begin while the one before it in its stream ends: every thread waits here until that one is complete
+// and what it wrote is visible.
+__device__ __forceinline__ void wait_for_grid_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 }  // namespace amk
