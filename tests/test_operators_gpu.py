@@ -263,6 +263,87 @@ def test_attentions_on_two_streams_at_once(amk):
     assert all(torch.equal(a, b) for a, b in got)
 
 
+@pytest.mark.parametrize("captured", [False, True])
+def test_operators_wait_for_what_is_in_front_of_them(amk, captured):
+    """The kernels may begin while the one before them ends: inputs that are written last thing before the call -- by a
+    kernel, a memset, a copy, another stream, another operator -- and outputs that are overwritten right behind it."""
+    n, nq, nkv, hd, slots, rows, vocab = 700, 8, 2, 128, 1500, 4, 50000
+    q, k, v, cu = prompt_inputs([n - 200, 200], nq, nkv, hd, 5, fused=False)
+    qt, kt, vt = tree_inputs(1, rows, slots, nq, nkv, hd, "bf16", 6)
+    logits = torch.randn(rows, vocab, generator=gen(7), device=DEV)
+    tokens = torch.tensor([1, 2, 3, 49999], dtype=torch.int32, device=DEV)
+    one = lambda x: torch.tensor([x], dtype=torch.int32, device=DEV)
+    base, keep, count = one(1400), torch.tensor([[1401, 1403, 1404]], dtype=torch.int32, device=DEV), one(3)
+    src = [t.clone() for t in (q, k, v, qt, kt, vt, logits)]
+    dst = [torch.zeros_like(t) for t in src]
+    late = [torch.zeros_like(t) for t in (cu, tokens, count)]
+    length = one(0)
+    side = torch.cuda.Stream()
+    big = torch.zeros(1 << 24, device=DEV)
+
+    def steps():
+        outs = []
+        big.add_(1.0)                                          # a long kernel, and then the inputs at the last moment
+        for d, s in zip(dst, src):
+            d.copy_(s)
+        late[0].copy_(cu)
+        outs.append(amk.amk_prompt_attention(dst[0], dst[1], dst[2], late[0]))
+        for d in dst[:3]:
+            d.zero_()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            big.add_(1.0)
+            length.fill_(1400)
+        torch.cuda.current_stream().wait_stream(side)
+        for _ in range(2):                                     # its own output is the next one's query
+            outs.append(amk.amk_tree_attention(dst[3] if len(outs) == 1 else outs[-1], dst[4], dst[5], length))
+        kv = torch.stack([dst[4][0], dst[5][0]])[None].contiguous()
+        late[2].copy_(count)
+        amk.amk_kv_compact(kv, base, keep, late[2])
+        outs.append(amk.amk_tree_attention(dst[3], kv[:, 0], kv[:, 1], length))
+        for d in dst[3:6]:
+            d.zero_()
+        length.zero_()
+        late[1].copy_(tokens)
+        outs += [x.clone() for x in amk.amk_token_logprobs(dst[6], late[1], 5)]
+        dst[6].zero_()
+        late[1].zero_()
+        kv.zero_()
+        return outs
+
+    def alone():
+        wait = torch.cuda.synchronize
+        wait()
+        outs = [amk.amk_prompt_attention(*src[:3], cu)]
+        wait()
+        at = one(1400)
+        outs.append(amk.amk_tree_attention(src[3], src[4], src[5], at))
+        wait()
+        outs.append(amk.amk_tree_attention(outs[-1], src[4], src[5], at))
+        kv = torch.stack([src[4][0], src[5][0]])[None].contiguous()
+        wait()
+        amk.amk_kv_compact(kv, base, keep, count)
+        wait()
+        outs.append(amk.amk_tree_attention(src[3], kv[:, 0], kv[:, 1], at))
+        wait()
+        outs += list(amk.amk_token_logprobs(src[6], tokens, 5))
+        wait()
+        return outs
+
+    want = alone()
+    if captured:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs = steps()
+    for _ in range(5):
+        if captured:
+            graph.replay()
+        else:
+            outs = steps()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
 def test_first_call_of_a_process_may_be_captured():
     """Everything that a call sets up once happens in the call itself, and capture allows it."""
     code = """
