@@ -19,6 +19,8 @@
 
 namespace {
 
+using namespace amk;
+
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kUnroll = 4;                    // 16-byte pieces that a thread takes at a time
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -43,11 +45,6 @@ __device__ __forceinline__ void widen(float (&v)[8], const uint4& u) {
   v[0] = amk::bf16_lo(u.x), v[1] = amk::bf16_hi(u.x), v[2] = amk::bf16_lo(u.y), v[3] = amk::bf16_hi(u.y);
   v[4] = amk::bf16_lo(u.z), v[5] = amk::bf16_hi(u.z), v[6] = amk::bf16_lo(u.w), v[7] = amk::bf16_hi(u.w);
 }
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 __device__ __forceinline__ float max_nan(float a, float b) {   // NaN if one of them is
   float d;
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
@@ -64,33 +61,9 @@ __device__ __forceinline__ float key_value(unsigned long long k) {
   return __uint_as_float((u >> 31) ? u & 0x7fffffffu : ~u);
 }
 
-__device__ __forceinline__ float max3_nan(float a, float b, float c) {
-  float d;
-  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-  return d;
-}
 __device__ __forceinline__ float min3(float a, float b, float c) {
   float d;
   asm("min.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-  return d;
-}
-// two fp32 lanes in one instruction
-__device__ __forceinline__ uint64_t pair(float lo, float hi) {
-  uint64_t d;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
-  return d;
-}
-__device__ __forceinline__ void unpair(float& lo, float& hi, uint64_t a) {
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(a));
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-  return d;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
 }
 
@@ -160,31 +133,6 @@ __device__ __forceinline__ K merge_warps(K v, K (*buf)[32], int warp, int lane) 
     __syncthreads();
     if (warp < n) v = merge32(v, buf[warp + n][31 - lane], lane);
   }
-  return v;
-}
-
-// ---- cluster ----------------------------------------------------------------------------------------------------
-__device__ __forceinline__ unsigned cluster_rank() {
-  unsigned r;
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ unsigned remote(const void* p, unsigned rank) {   // the same place in another block
-  unsigned a;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(amk::smem_u32(p)), "r"(rank));
-  return a;
-}
-__device__ __forceinline__ float remote_f32(const void* p, unsigned rank) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote(p, rank)) : "memory");
-  return v;
-}
-__device__ __forceinline__ unsigned long long remote_u64(const void* p, unsigned rank) {
-  unsigned long long v;
-  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(remote(p, rank)) : "memory");
   return v;
 }
 

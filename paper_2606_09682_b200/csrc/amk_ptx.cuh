@@ -1,5 +1,5 @@
-// Thin inline-PTX wrappers used by the decode kernel: mbarriers, bulk asynchronous copies (TMA, untiled),
-// acquire/release accesses at GPU scope, named barriers, the global nanosecond timer.
+// Thin inline-PTX wrappers used by the decode kernel and the operators around it: mbarriers, bulk asynchronous copies (TMA,
+// untiled), acquire/release accesses at GPU scope, named barriers, the global nanosecond timer, packed arithmetic, clusters.
 #pragma once
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -147,6 +147,72 @@ __device__ __forceinline__ uint2 ld_pair(const void* p) {
                : "memory");
   return make_uint2((unsigned)w, (unsigned)(w >> 32));
 }
+
+// ---- arithmetic of the operators around the step ------------------------------------------------------------------
+__device__ __forceinline__ float exp2_fast(float x) {   // 2^x, relative error 2^-22; 2^-inf = 0
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// NaN if one of them is
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+// two fp32 lanes in one instruction
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+  uint64_t d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
+  return d;
+}
+__device__ __forceinline__ void unpair(float& lo, float& hi, uint64_t a) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(a));
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+
+// ---- cluster ----------------------------------------------------------------------------------------------------
+__device__ __forceinline__ unsigned cluster_rank() {
+  unsigned r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ unsigned remote(const void* p, unsigned rank) {   // the same place in another block
+  unsigned a;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
+  return a;
+}
+__device__ __forceinline__ float remote_f32(const void* p, unsigned rank) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote(p, rank)) : "memory");
+  return v;
+}
+__device__ __forceinline__ float4 remote_f32x4(const void* p, unsigned rank) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];"
+               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+               : "r"(remote(p, rank))
+               : "memory");
+  return v;
+}
+__device__ __forceinline__ unsigned long long remote_u64(const void* p, unsigned rank) {
+  unsigned long long v;
+  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(remote(p, rank)) : "memory");
+  return v;
+}
+
 // For a grid that may begin while the one before it in its stream ends: every thread waits here until that one is complete
 // and what it wrote is visible.
 __device__ __forceinline__ void wait_for_grid_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }

@@ -107,29 +107,6 @@ __device__ __forceinline__ void tmem_pin(unsigned (&r)[N]) {
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// ---- cluster ----------------------------------------------------------------------------------------------------
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ unsigned remote(const void* p, unsigned rank) {   // the same place in another block
-  unsigned a;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
-  return a;
-}
-__device__ __forceinline__ float remote_f32(const void* p, unsigned rank) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote(p, rank)) : "memory");
-  return v;
-}
-__device__ __forceinline__ float4 remote_f32x4(const void* p, unsigned rank) {
-  float4 v;
-  asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];"
-               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
-               : "r"(remote(p, rank))
-               : "memory");
-  return v;
-}
-
 // ---- TMA --------------------------------------------------------------------------------------------------------
 // One box of a four-dimensional tensor map into shared memory, issued by the leading lane of a converged warp; the byte
 // offset of coordinate x is a multiple of 16.
