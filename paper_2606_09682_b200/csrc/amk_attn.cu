@@ -147,8 +147,8 @@ int sm_count() {
 //    slower than L2.  Clusters / runs, us a call in a graph: 8 rows of 64, 17 tiles 10.6 / 11.1; 16 rows of 128, 8 tiles
 //    13.3 / 13.3, over the 8-bit cache 16.2 / 16.8; 15 rows of 64, 4 tiles 10.3 / 11.0; but 32 rows of 128, 16 tiles
 //    13.7 / 13.1; 128 rows of 64, 4 tiles 14.6 / 11.6;
-//  - one block, where its tiles are no more than its share of the runs and six to ten more, which is what the second kernel
-//    and the parts' way through memory cost.  One block / runs: 128 items of 128 rows of 128, 4 tiles 18.2 / 22.5, 12 tiles
+//  - one block, where its tiles (and three for its beginning and end) are no more than its share of the runs and six to ten
+//    more, which is what the second kernel and the parts' way through memory cost.  One block / runs: 128 items of 128 rows of 128, 4 tiles 18.2 / 22.5, 12 tiles
 //    32.1 / 43.3; 64 items of 128 rows of 64, 8 tiles 15.7 / 19.1; 32 items of 128 rows of 128, 6 tiles 16.8 / 18.1, 12 tiles
 //    22.2 / 20.3; 8 items, 4 tiles 15.0 / 14.7; over the 8-bit cache 128 items, 8 tiles 26.8 / 42.1; 32 items, 4 tiles
 //    19.1 / 20.2, 6 tiles 21.9 / 20.8.  The lengths may be anything below the bound that is known here, and the longest
@@ -178,7 +178,7 @@ TreePlan tree_plan(const amk_tree_args& a) {
     }
     const bool meet = tiles <= kMinTiles << i && (i == 0 || rows * a.head_dim <= 2048);
     if (!meet) i = 0;
-    if (meet || (tiles <= 12 && (tiles + amk::kUnitCost) * (sms - items) <= (6 + items / 32) * sms)) {
+    if (meet || (tiles <= 12 && (tiles + 3) * (sms - items) <= (6 + items / 32) * sms)) {
       t.cluster = 1 << i;
       t.blocks = (unsigned)(items << i);
       t.bytes = 0;

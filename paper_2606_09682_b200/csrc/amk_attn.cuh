@@ -122,9 +122,11 @@ struct Unit {
 
 // Tree: the key tiles of all (sequence, kv head, row block) in that order, cut into equal runs, one for each block.  An
 // item counts kUnitCost tiles more than it has, in front of its first: a block that begins another item reads another Q,
-// fills the pipeline again and writes another output, which costs about as much (a batch with an empty sequence left one
-// block with eight such items: 100 us, the others 34 us).
-constexpr int kUnitCost = 3;
+// fills the pipeline again and writes another output or part (2 / 3 / 4 / 5 / 6 / 7 / 9 / 12 tiles, us: eight ragged
+// sequences of up to 8000 positions 65 / 50 / 49 / 45 / 45 / 45 / 45 / 46, over the 8-bit cache 76 / 58 / 55 / 52 / 52 / 52 /
+// 54 / 55; sixty of up to 2000 there 110 / 99 / 90 / 88 / 89 / 88 / 92 / 99; one of 8099 20.7 / 20.5 / 20.3 / 20.5 / 20.5 / 20.7 /
+// 20.6 / 19.8).
+constexpr int kUnitCost = 6;
 __device__ __forceinline__ int tree_tiles(const AttnParams& p, int len) {   // key tiles of one item; 0: bad length
   return len < 0 || len > p.slots - p.rows ? 0 : (len + p.rows + kTile - 1) / kTile;
 }
