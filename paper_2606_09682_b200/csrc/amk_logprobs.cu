@@ -2,7 +2,8 @@
 //
 // Mathematics.  With the running maximum r, R = r log2 e rounded and y = x log2 e - R, a thread sums s = sum 2^y and
 // t = sum 2^y y over its share of the row; when R rises by d, s' = 2^-d s and t' = 2^-d (t - d s).  Shares are joined the
-// same way: log probability of x = (x - r) - ln s + ln 2 (r log2 e - R), entropy = ln s - ln 2 t / s.
+// same way: log probability of x = (x - r) - ln s + ln 2 (r log2 e - R), entropy = ln s - ln 2 t / s.  (Far from zero R is not
+// rounded: below.)
 //
 // Alternatives.  Sorting is kept out of the pass: a thread keeps only the maximum of its share.  The k-th largest of
 // those maxima is a lower bound of the k-th largest logit, so the alternatives lie in the shares whose maximum reaches
@@ -67,15 +68,21 @@ __device__ __forceinline__ float min3(float a, float b, float c) {
   return d;
 }
 
-// A share's sums, for a reference r (the largest x so far): y = x log2 e - R with R the rounded r log2 e is one fused
-// multiply-add; what the rounding of R leaves, eps(r), is in every y alike and taken out of the logarithm at the end.
-constexpr float kLowest = -3.402823466e38f, kFar = 1.0e30f;
-__device__ __forceinline__ float ref(float r) { return fminf(fmaxf(r * kLog2e, kLowest), -kLowest); }
+// A share's sums, for a reference r: the largest x so far, or -kFar.  While |r| is below kFar, y = x log2 e - R with R the rounded
+// r log2 e is one fused multiply-add; what the rounding of R leaves, eps(r), is in every y alike and taken out of the
+// logarithm at the end.  It is half an ulp of R at most: 2^-4 at kFar, but 439 at 1e10, more than an exponential can
+// take, so from kFar on y = (x - r) log2 e and eps is 0 (at -kFar the two are the same).
+// Logits below -kFar are masks, and no more than a few tokens of a row may be without one: nothing is raised for them, they
+// are 2^-kFar there.  A block whose part holds nothing else takes its sums again.  (600 rows of 128256, all but 1 in 1000 at -1e9, top 5:
+// fp32 55 us, bf16 43 us; with every thread's own far reference 80 and 70 us.)
+constexpr float kFar = 1048576.f, kHuge = 1.0e30f;
+__device__ __forceinline__ float ref(float r) { return r * kLog2e; }               // of an r below kFar
 __device__ __forceinline__ float eps(float r) { return fabsf(r) < kFar ? fmaf(r, kLog2e, -ref(r)) : 0.f; }
 struct Sums {
   float r, s, t;                                             // reference, sum of 2^y, sum of 2^y y
   __device__ __forceinline__ void raise(float to) {            // a finite reference, not below the old one
-    const float d = fminf(ref(to) - ref(r), 1000.f);           // (2^-1000 is 0 here; keeps 0 * d from being NaN)
+    // by how much the reference rises; (2^-1000 is 0 here; keeps 0 * d from being NaN)
+    const float d = fminf(fmaf(to - r, kLog2e, eps(r) - eps(to)), 1000.f);
     const float f = exp2_fast(-d);
     t = f * (t - d * s);
     s *= f;
@@ -159,7 +166,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 5 : 3) logprobs_ker
   const uint4* v4 = (const uint4*)(x + head) + p0;
   const int base = head + p0 * kVec;                 // index of the part's first element
 
-  Sums sum{kLowest, 0.f, 0.f};
+  Sums sum{-kFar, 0.f, 0.f};
   float top = -CUDART_INF_F;                         // NaN if there was one
   auto single = [&](int i) {
     const float v = load(x, i);
@@ -194,7 +201,8 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 5 : 3) logprobs_ker
         for (int k = 0; k < kVec; k += 2) mx = max3_nan(mx, v[k], v[k + 1]), mn = min3(mn, v[k], v[k + 1]);
       }
       top = max_nan(top, mx);
-      const bool rises = mx > sum.r, masked = mn < -kFar || mx > kFar;
+      // (masked: values so low that 0 times y could be 0 times infinity, or a reference that wants the other y)
+      const bool rises = mx > sum.r, masked = mn < -kHuge || (rises && mx >= kFar) || sum.r >= kFar;
       if (rises || masked) {
         float a0, a1;
         unpair(a0, a1, s2);
@@ -321,8 +329,28 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 5 : 3) logprobs_ker
     best = merge_warps(best, lists, warp, lane);
   }
   __syncthreads();
+  float most = red[3][0];                            // the block's maximum
+#pragma unroll
+  for (int w = 1; w < kWarps; w++) most = fmaxf(most, red[3][w]);
+  if (most < -kFar && most > -CUDART_INF_F) {        // nothing but masks: the sums again, for that reference
+    Sums own{most, 0.f, 0.f};
+    if (rank == 0 && (int)threadIdx.x < head) own.add(load(x, threadIdx.x));
+#pragma unroll 1
+    for (int i = threadIdx.x; i < n; i += kThreads) {
+      float v[kVec];
+      widen(v, __ldg(v4 + i));
+#pragma unroll
+      for (int k = 0; k < kVec; k++) own.add(v[k]);
+    }
+    if (rank == (unsigned)C - 1 && (int)threadIdx.x < tail) own.add(load(x, head + pieces * kVec + threadIdx.x));
+#pragma unroll
+    for (int o = 16; o; o /= 2) own.s += shfl_xor(own.s, o), own.t += shfl_xor(own.t, o);
+    __syncthreads();                                 // (red[3] has been read)
+    if (lane == 0) red[0][warp] = most, red[1][warp] = own.s, red[2][warp] = own.t;
+    __syncthreads();
+  }
   if (warp == 0) {
-    Sums b{lane < kWarps ? red[0][lane] : kLowest, lane < kWarps ? red[1][lane] : 0.f, lane < kWarps ? red[2][lane] : 0.f};
+    Sums b{lane < kWarps ? red[0][lane] : -kFar, lane < kWarps ? red[1][lane] : 0.f, lane < kWarps ? red[2][lane] : 0.f};
     float mm = lane < kWarps ? red[3][lane] : -CUDART_INF_F;
 #pragma unroll
     for (int o = kWarps / 2; o; o /= 2) {

@@ -780,6 +780,36 @@ def test_logprobs_special_values(amk, dtype, vocab):
     assert ids.tolist() == [[-1, -1, -1]] and bool(torch.isnan(tlp).all()) and math.isnan(lp[0])
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,vocab", [(1, 40), (12, 9000), (7, 128256), (400, 5003), (3, 300001)])
+def test_logprobs_large_finite_logits(amk, dtype, rows, vocab):
+    """Rows masked with large finite values, rows whose maximum is far from zero, and rows of nothing but such values: NaN is for
+    NaN and infinities alone.  A difference of two logits is rounded once (2^-24 of it) and is no larger than the log
+    probability and log(vocab) <= 13 together; exponentials are good to 2^-21, the sums of n terms to n 2^-30."""
+    g = gen(rows + vocab)
+    far = [5e9, 1e10, 1e20, 3e6, 1e6, 1e30, 3e37, 4.5e9]
+    kinds = [lambda i, c: ((torch.full((vocab,), -c, device=DEV)).scatter_(0, torch.randperm(vocab, generator=g, device=DEV)[:4],
+                                                                          3 * torch.randn(4, generator=g, device=DEV))),
+             lambda i, c: torch.randn(vocab, generator=g, device=DEV).scatter_(0, torch.tensor([vocab // 3], device=DEV), c),
+             lambda i, c: torch.full((vocab,), -c if i % 2 else c, device=DEV),
+             lambda i, c: c * torch.randn(vocab, generator=g, device=DEV),
+             lambda i, c: torch.cat([torch.full((vocab // 2,), -c, device=DEV), torch.randn(vocab - vocab // 2, generator=g, device=DEV)]),
+             lambda i, c: torch.randn(vocab, generator=g, device=DEV) * 4 - c]
+    for at in range(0, len(far) * len(kinds), rows):
+        pick = [(kinds[(at + i) % len(kinds)], far[(at + i) // len(kinds) % len(far)], i) for i in range(rows)]
+        x = torch.stack([k(i, c) for k, c, i in pick]).to(dtype)
+        assert bool(torch.isfinite(x).all())
+        tokens = x.argmax(1).to(torch.int32)
+        tokens[1::2] = torch.randint(0, vocab, (len(tokens[1::2]),), generator=g, device=DEV).to(torch.int32)
+        got = amk.amk_token_logprobs(x, tokens, 8)
+        want = logprobs64(x, tokens, 8)
+        assert torch.equal(got[2].long(), want[2])
+        for a, b in ((got[0], want[0]), (got[1], want[1]), (got[3], want[3])):
+            tol = 2.0 ** -22 * (b.abs() + 13) + 2.0 ** -21 + vocab * 2.0 ** -30
+            bad = ~((a.double() - b).abs() <= tol)
+            assert not bool(bad.any()), (at, a[bad][:4].tolist(), b[bad][:4].tolist())
+
+
 def test_logprobs_token_agrees_with_argmax_static_and_replays(amk):
     g = gen(2)
     x = randn(g, 4, 32000, dtype=torch.float32)
