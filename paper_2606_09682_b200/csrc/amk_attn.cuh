@@ -550,7 +550,7 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
     }
     blocks.init(p, lane);
     unit = blocks.find(p, blockIdx.x, lane);
-    if (lane == 0) {
+    if (lane == 0 && unit.x >= 0) {                   // (else another block's comes first: below)
       h.units[0] = unit;
       mbar_arrive(&h.unit_full[0]);
     }
@@ -995,11 +995,20 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
       }
       return x;
     };
+    if (!TREE && unit.x < 0) {
+      // This block's index stands for no queries.  In which order blocks are launched and taken over is not specified: what
+      // the scheduler hands out instead is worked on like any unit, and the end is the answer that nothing is left.
+      unit = next_unit();
+      if (lane == 0) {
+        h.units[0] = unit;
+        mbar_arrive(&h.unit_full[0]);
+      }
+      __syncwarp();
+    }
     for (;;) {
       if constexpr (TREE) {
         if (!uniform(units.next(p, h, u))) break;
       } else if (!Units<false>::set(p, unit, u)) {
-        if (taken == 1) next_unit();                  // (there is none: the units of a grid come first)
         break;
       }
       const int tile_begin = uniform(u.tile_begin);

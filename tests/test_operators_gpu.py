@@ -231,6 +231,27 @@ def test_prompt_attention_around_32_prompts(amk, n_seqs):
     check_prompt(q, k, v, lens, out, lse, 0.125)
 
 
+@pytest.mark.parametrize("nq,nkv,hd,n_seqs", [(8, 4, 64, 30), (16, 1, 128, 5000), (2, 2, 64, 20000)])
+def test_prompt_attention_among_blocks_without_queries(amk, nq, nkv, hd, n_seqs):
+    """The grid has a block for every prompt that could need one: here nearly all find none -- empty prompts, impossible
+    bounds, far more prompts than tokens -- and only take over what is left."""
+    rng = np.random.default_rng(n_seqs)
+    lens = [0] * n_seqs
+    for at, n in zip(rng.choice(n_seqs - 2, 6, replace=False), (1, 300, 2, 77, 1030, 20)):
+        lens[int(at)] = n
+    total = sum(lens)
+    q, k, v, cu = prompt_inputs(lens, nq, nkv, hd, n_seqs, slack=400)
+    cu[-1] = total + 900                               # impossible: the last prompt is left out
+    out = torch.full((total + 400, nq, hd), 5.0, dtype=torch.bfloat16, device=DEV)
+    lse = torch.full((total + 400, nq), 5.0, device=DEV)
+    for _ in range(3):
+        amk.amk_prompt_attention(q, k, v, cu, out=out, lse=lse)
+        check_prompt(q, k, v, lens, out, lse, hd ** -0.5)
+        assert bool((out[total:] == 5).all()) and bool((lse[total:] == 5).all())
+        out[:total], lse[:total] = 5.0, 5.0
+    assert amk.amk_operator_status() == 0
+
+
 def test_attention_a_broken_query_spoils_its_own_row_only(amk):
     nq, nkv, hd, n = 4, 2, 128, 300
     q, k, v, cu = prompt_inputs([n], nq, nkv, hd, 19, fused=False)
