@@ -398,7 +398,8 @@ amk_status amk_prompt_attention(const amk_prompt_args* args, char* msg, size_t m
  *                 do not matter there) on the same device, NULL if that is 0; scratch, needs no initial value; two calls
  *                 that may overlap need one each
  * Pointers 16-byte aligned, strides multiples of 16 bytes.  Arithmetic as amk_prompt_attention's; over the 8-bit cache the
- * softmax numerators are f16 (2^-11), the codes exact, and q exact but for values 2^-30 below its row's largest.
+ * softmax numerators are f16 (each off by 2^-11 of itself or 2^-34 of its row's largest, whichever is more), the codes
+ * exact, and q exact but for values 2^-30 below its row's largest.
  * Errors as amk_prompt_attention.
  */
 typedef struct amk_tree_args {

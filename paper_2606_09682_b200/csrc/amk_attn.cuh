@@ -5,7 +5,7 @@
 //   S = Q K^T;  m' = max(m, rowmax S);  P = 2^((S - m') c), c = scale log2 e;  l = l 2^((m - m') c) + rowsum P;
 //   O = O 2^((m - m') c) + P V;  at the end O / l.
 // O is rescaled only when m rises by more than 8 / c (P then stays below 2^8, nothing is lost: P is a floating-point
-// number and l and O share the reference).
+// number and l and O share the reference).  Where P is f16 (below), 2^9 times as much is made of it.
 //
 // Work.  One block an SM: two row tiles of 128 rows share every K/V tile of 128 keys (prompts, large drafts), or, where a
 // draft has 128 rows at most, take every second key tile each and are joined at the end.  A producer warp keeps a ring of
@@ -471,12 +471,21 @@ __device__ __noinline__ void product_by_key(unsigned tp, unsigned see0, unsigned
 // Over the 8-bit cache the matrix instructions work on f16: two e4m3 codes are two f16 by one conversion (to bf16 it takes
 // three more), P has three bits more than in bf16, and a row of Q is exact in f16 after a power of two.  P is rounded to
 // the operands' type (2^-8 of it in bf16), the sum l is not: the roundings of a row are independent and average out.
+// f16 ends at 65504 and has its 11 bits down to 2^-14, the last one at 2^-24.  So that a key's share is not lost beside a far larger
+// one whose V is small, P is 2^9 2^((S - m') c) there, l and O with it, and O is rescaled when m rises by more than 6 / c: the
+// largest P of a row lies between 2^9 and 2^15, and P is off by 2^-11 of itself or 2^-34 of the largest.  (16 drafted tokens over
+// eight caches of 64 to 8111 positions, 2^x up and a rise of 15 - x: x = 7 53.4, 9 53.5, 11 56.2 us; f16 without this 53.2.)
+template <bool FP8>
+struct Numerators {
+  static constexpr float kRise = FP8 ? 6.f : 8.f, kUp = FP8 ? 9.f : 0.f;
+};
 // ---- the kernel -------------------------------------------------------------------------------------------------
 template <int HD, bool TREE, bool FP8>
 __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
     attn_kernel(const AttnParams p, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
   using L = AttnSmem<HD, FP8>;
   constexpr int kProducer = FP8 ? 20 : 16, kIssuer = kProducer + 1;
+  constexpr float kRise = Numerators<FP8>::kRise, kUp = Numerators<FP8>::kUp;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = (unsigned char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   AttnHead& h = *(AttnHead*)(smem + L::kHead);
@@ -682,9 +691,9 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
         unsigned see[2] = {~0u, ~0u};
         bool exact = i == 0 || masked;
         if (live && !exact) {
-          // The running maximum seldom rises by more than the 2^8 that P may grow to: P is made with the old one in one
+          // The running maximum seldom rises by more than P may grow: P is made with the old one in one
           // pass, and made again if it did.
-          const float mc = m == -CUDART_INF_F ? 0.f : -m * c;
+          const float mc = m == -CUDART_INF_F ? kUp : fmaf(-m, c, kUp);
           const uint64_t c2 = pair(c, c), mc2 = pair(mc, mc);
           uint64_t sum[2] = {0, 0};
           unsigned r[32];
@@ -710,7 +719,7 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
             top = max3_nan(top, tops[0], tops[1]);
           }
           // (a NaN among the scores, or a first finite one, takes the careful way too)
-          exact = any_of_pair(!((top - m) * c <= 8.f), pair_id);
+          exact = any_of_pair(!((top - m) * c <= kRise), pair_id);
           if (!exact) {
             tmem_st32(ts + half * 64, r);
             float s0, s1;
@@ -766,7 +775,7 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
           if (i == 0) {
             m = top;
           } else {
-            const bool need = top > m && (top - m) * c > 8.f;
+            const bool need = top > m && (top - m) * c > kRise;
             if (__any_sync(~0u, need)) {              // the same in both halves
               const float mn = fmaxf(m, top);
               const float f = m == mn ? 1.f : exp2_fast((m - mn) * c);
@@ -784,7 +793,7 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
               m = mn;
             }
           }
-          const float mc = m == -CUDART_INF_F ? 0.f : -m * c;
+          const float mc = m == -CUDART_INF_F ? kUp : fmaf(-m, c, kUp);
           const uint64_t c2 = pair(c, c), mc2 = pair(mc, mc);
           uint64_t sum[2] = {0, 0};
 #pragma unroll (TREE ? 1 : 2)
@@ -899,7 +908,7 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
       if (steps && live && !(dual && t == 1)) {
         const bool whole = !TREE || (u.tile_begin == 0 && u.tile_end == u.item_tiles);
         const float inv = l == 0.f ? 0.f : 1.f / l;
-        const float lse2 = l == 0.f ? -CUDART_INF_F : m * c + log2f(l);
+        const float lse2 = l == 0.f ? -CUDART_INF_F : m * c + (log2f(l) - kUp);
         const int64_t slot = TREE ? (int64_t)2 * blockIdx.x + (u.tile_begin == 0 ? 1 : 0) : 0;
         const int part_row = wr + (dual ? 0 : t * kTile);
 #pragma unroll 1

@@ -631,6 +631,34 @@ def test_tree_attention_every_8bit_code(amk, hd):
         assert torch.equal(out[0, 0], want)
 
 
+@pytest.mark.parametrize("slots,rows,nq,nkv,hd", [(300, 9, 4, 2, 64), (8192, 9, 8, 2, 128), (8192, 9, 16, 1, 64), (3000, 36, 16, 2, 128)])
+@pytest.mark.parametrize("place", ["first", "middle", "last"])
+def test_tree_attention_small_numerators_over_the_8bit_cache(amk, slots, rows, nq, nkv, hd, place):
+    """One dominating key whose V is zero, and all others 2^-10 to 2^-30 below it: the output is theirs alone.  Each numerator
+    is off by 2^-11 of itself or 2^-34 of the row's largest one, whichever is more (half of f16's last place, 2^-25, where the
+    largest is at least 2^9), beside the other terms of every case."""
+    g = gen(slots + rows)
+    n = slots - rows
+    at = {"first": 0, "middle": n // 2, "last": n - 1}[place]
+    k = torch.zeros(1, nkv, slots, hd, device=DEV)
+    k[:, :, at, 0] = 1.0
+    v = torch.randn(1, nkv, slots, hd, generator=g, device=DEV).abs()
+    v[:, :, at] = 0.0
+    k, v = (t.to(torch.float8_e4m3fn).view(torch.uint8) for t in (k, v))
+    gaps = torch.tensor([10.0, 13.0, 16.0, 18.0, 20.0, 22.0, 24.0, 27.0, 30.0], device=DEV)[torch.arange(rows, device=DEV) % 9]
+    q = torch.zeros(1, rows, nq, hd, device=DEV)
+    q[..., 0] = (gaps * math.log(2) * hd ** 0.5)[:, None]
+    q = q.to(torch.bfloat16)
+    lse = torch.empty(1, rows, nq, device=DEV)
+    out = amk.amk_tree_attention(q, k, v, torch.tensor([n], dtype=torch.int32, device=DEV), lse=lse)
+    sees = torch.ones(rows, slots, dtype=torch.bool, device=DEV)
+    sees[:, n:] = causal(rows)
+    vv = v[0].view(torch.float8_e4m3fn).float()
+    o, l, tol, tol_l, touched = attention64(q[0], k[0].view(torch.float8_e4m3fn).float().permute(1, 0, 2), vv.permute(1, 0, 2), sees, hd ** -0.5)
+    tol = tol + 2.0 ** -34 * vv.double().sum(1).repeat_interleave(nq // nkv, 0)[None]
+    check(out[0], lse[0], (o, l, tol, tol_l, touched), place)
+
+
 def test_tree_attention_bad_lengths(amk):
     rows, nq, nkv, hd, slots = 4, 4, 2, 64, 100
     q, k, v = tree_inputs(4, rows, slots, nq, nkv, hd, "bf16", 3)
