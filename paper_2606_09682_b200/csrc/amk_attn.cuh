@@ -479,6 +479,9 @@ template <bool FP8>
 struct Numerators {
   static constexpr float kRise = FP8 ? 6.f : 8.f, kUp = FP8 ? 9.f : 0.f;
 };
+// (S - m) c is made as S c - m c with the second product rounded, one instruction for two: that puts 2^-13 at most on an exponent
+// while |m c| is below this, and any amount far beyond, where the difference is taken first.
+constexpr float kFarScore = 4096.f;
 // ---- the kernel -------------------------------------------------------------------------------------------------
 template <int HD, bool TREE, bool FP8>
 __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
@@ -718,8 +721,8 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
             }
             top = max3_nan(top, tops[0], tops[1]);
           }
-          // (a NaN among the scores, or a first finite one, takes the careful way too)
-          exact = any_of_pair(!((top - m) * c <= kRise), pair_id);
+          // (a NaN among the scores, a first finite one, or a maximum far from zero takes the careful way too)
+          exact = any_of_pair(!((top - m) * c <= kRise) || fabsf(mc) > kFarScore, pair_id);
           if (!exact) {
             tmem_st32(ts + half * 64, r);
             float s0, s1;
@@ -793,8 +796,10 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
               m = mn;
             }
           }
-          const float mc = m == -CUDART_INF_F ? kUp : fmaf(-m, c, kUp);
-          const uint64_t c2 = pair(c, c), mc2 = pair(mc, mc);
+          const float mc0 = m == -CUDART_INF_F ? kUp : fmaf(-m, c, kUp);
+          const bool far = fabsf(mc0) > kFarScore;
+          const float mc = far ? kUp : mc0, less = far ? -m : 0.f;
+          const uint64_t c2 = pair(c, c), mc2 = pair(mc, mc), less2 = pair(less, less);
           uint64_t sum[2] = {0, 0};
 #pragma unroll (TREE ? 1 : 2)
           for (int x = 0; x < 2; x++) {
@@ -811,7 +816,7 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
 #pragma unroll
             for (int k = 0; k < 32; k += 2) {
               float e0, e1;
-              unpair(e0, e1, fma2(pair(__uint_as_float(w[k]), __uint_as_float(w[k + 1])), c2, mc2));
+              unpair(e0, e1, fma2(add2(pair(__uint_as_float(w[k]), __uint_as_float(w[k + 1])), less2), c2, mc2));
               e0 = exp2_fast(e0), e1 = exp2_fast(e1);
               sum[k >> 1 & 1] = add2(sum[k >> 1 & 1], pair(e0, e1));
               r[k / 2] = pack2<FP8>(e0, e1);

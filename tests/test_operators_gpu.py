@@ -659,6 +659,71 @@ def test_tree_attention_small_numerators_over_the_8bit_cache(amk, slots, rows, n
     check(out[0], lse[0], (o, l, tol, tol_l, touched), place)
 
 
+def check_exact_scores(q, k, v, sees, out, lse, scale, what=""):
+    """As check(attention64(..)) where fp32 holds every score without rounding (E = 0): q [t][nq][hd], k / v [n][nkv][hd]."""
+    rep, n = q.shape[1] // k.shape[1], k.shape[0]
+    qd, kd, vd = (t.double().permute(1, 0, 2) for t in (q, k, v))
+    x = (qd @ kd.repeat_interleave(rep, 0).transpose(1, 2) * scale).masked_fill(~sees[None], -math.inf)
+    l, p = torch.logsumexp(x, 2), torch.softmax(x, 2)  # (softmax: exp(x - l) would lose the log 2 of two equal scores of 1e17)
+    o, A = p @ vd.repeat_interleave(rep, 0), p @ vd.abs().repeat_interleave(rep, 0)
+    tol = ((2.0 ** -8 + 2.0 ** -10) * A + 2.0 ** -8 * o.abs() + 1e-30).permute(1, 0, 2)
+    tol_l = (n * 2.0 ** -24 + 2.0 ** -20 * (1 + l.abs())).permute(1, 0)
+    err, err_l = (out.double() - o.permute(1, 0, 2)).abs(), (lse.double() - l.permute(1, 0)).abs()
+    assert bool((err <= tol).all()), (what, float((err / tol).max()))
+    assert bool((err_l <= tol_l).all()), (what, float((err_l / tol_l).max()))
+
+
+def distinct_bf16(n, seed):
+    """n distinct positive bf16 values from 1 up, in an order drawn from the seed: neighbours are 2^-7 of themselves apart."""
+    order = torch.randperm(n, generator=gen(seed), device=DEV)
+    return (order.to(torch.int32) + 0x3F80).to(torch.int16).view(torch.bfloat16)
+
+
+@pytest.mark.parametrize("power", [8, 20, 40, 90])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_prompt_attention_scores_beyond_the_integers(amk, power, hd, sign):
+    """Scores so large that the product of the maximum with scale log2 e is off by more than an exponential can take: one key
+    has all the weight (of equal ones each the same).  All scores are exact in fp32 here: powers of two times bf16 values."""
+    n, nq, nkv = 900, 4, 2
+    _, _, v, cu = prompt_inputs([n - 1, 1], nq, nkv, hd, power, fused=False)
+    q = torch.full((n, nq, hd), 2.0 ** power * sign, device=DEV).to(torch.bfloat16)
+    k = distinct_bf16(300, power).repeat(3)[:, None, None].expand(n, nkv, hd).contiguous()
+    k[450:460] *= 16                                    # a key far above the others in the middle
+    scale = 2.0 ** 12 if power < 90 else 1.0
+    lse = torch.empty(n, nq, device=DEV)
+    out = amk.amk_prompt_attention(q, k, v, cu, scale=scale, lse=lse)
+    for s in (slice(0, n - 1), slice(n - 1, n)):
+        check_exact_scores(q[s], k[s], v[s], causal(s.stop - s.start), out[s], lse[s], scale)
+    assert torch.equal(out[0], v[0].repeat_interleave(2, 0))
+
+
+@pytest.mark.parametrize("cache", ["bf16", "fp8"])
+@pytest.mark.parametrize("power", [8, 20, 40, 90])
+@pytest.mark.parametrize("rows,slots,nq,nkv,hd", [(3, 700, 4, 2, 64), (5, 1900, 8, 1, 128), (40, 700, 8, 1, 64), (1, 120, 2, 2, 128)])
+def test_tree_attention_scores_beyond_the_integers(amk, cache, power, rows, slots, nq, nkv, hd):
+    """As for prompts; every key has another value, so that one key has all the weight whichever parts the keys come in."""
+    q, _, v = tree_inputs(1, rows, slots, nq, nkv, hd, cache, power)
+    n = slots - rows
+    q = torch.full_like(q, 2.0 ** power)
+    if cache == "fp8":                                  # 126 positive codes (or as many as fit); below them the same negative one
+        k = torch.full((slots,), 0xB8, device=DEV, dtype=torch.uint8)
+        at = torch.randperm(slots, generator=gen(9), device=DEV)[:126]
+        k[at] = torch.arange(127 - len(at), 127, device=DEV).to(torch.uint8)
+        k[0] = k[n // 2]
+        k[n // 2] = 0x7E
+    else:
+        k = distinct_bf16(slots, power)
+    k = k[None, None, :, None].expand(1, nkv, slots, hd).contiguous()
+    scale = 2.0 ** 14 if power < 90 else 1.0
+    lse = torch.empty(1, rows, nq, device=DEV)
+    out = amk.amk_tree_attention(q, k, v, torch.tensor([n], dtype=torch.int32, device=DEV), scale=scale, lse=lse)
+    value = (lambda t: t[0].view(torch.float8_e4m3fn).float().permute(1, 0, 2)) if cache == "fp8" else (lambda t: t[0].permute(1, 0, 2))
+    sees = torch.ones(rows, slots, dtype=torch.bool, device=DEV)
+    sees[:, n:] = causal(rows)
+    check_exact_scores(q[0], value(k), value(v), sees, out[0], lse[0], scale)
+
+
 def test_tree_attention_bad_lengths(amk):
     rows, nq, nkv, hd, slots = 4, 4, 2, 64, 100
     q, k, v = tree_inputs(4, rows, slots, nq, nkv, hd, "bf16", 3)
