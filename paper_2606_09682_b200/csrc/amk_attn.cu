@@ -187,7 +187,7 @@ TreePlan tree_plan(const amk_tree_args& a) {
   }
   const int64_t runs = ((tiles + amk::kUnitCost) * items + kMinTiles - 1) / kMinTiles;
   t.blocks = (unsigned)(runs < sms ? runs : sms);
-  t.bytes = (size_t)2 * t.blocks * t.part_rows * (a.head_dim + 1) * 4;
+  t.bytes = (size_t)2 * t.blocks * t.part_rows * (a.head_dim + 2) * 4;
   return t;
 }
 

@@ -38,7 +38,7 @@ struct AttnParams {
   const int* lens;                 // prompt: cu_seqlens; tree: cache_len
   const unsigned long long* mask;  // tree: or null
   float* part_o;                   // tree: [2 * gridDim][part_rows][HD]
-  float* part_lse;                 // tree: [2 * gridDim][part_rows]
+  float* part_lse;                 // tree: [2 * gridDim][2][part_rows]: a row's maximum and its sum
   int64_t q_seq, q_row, q_head, o_seq, o_row, o_head;
   int n_seqs, nq, nkv, rep;
   int rows;                        // prompt: all tokens; tree: drafted tokens of a sequence
@@ -913,9 +913,24 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
       if (steps && live && !(dual && t == 1)) {
         const bool whole = !TREE || (u.tile_begin == 0 && u.tile_end == u.item_tiles);
         const float inv = l == 0.f ? 0.f : 1.f / l;
-        const float lse2 = l == 0.f ? -CUDART_INF_F : m * c + (log2f(l) - kUp);
         const int64_t slot = TREE ? (int64_t)2 * blockIdx.x + (u.tile_begin == 0 ? 1 : 0) : 0;
         const int part_row = wr + (dual ? 0 : t * kTile);
+        if (valid && half == 0) {                      // (before the output: two registers less are held there)
+          // A part leaves its maximum, in units of q k, and its sum: their log2 as one number would lose the sum beside a
+          // large maximum.
+          const float part_m = FP8 ? m * (c / (p.scale * kLog2e)) : m, part_l = l * (FP8 ? 1.f / (1 << (int)kUp) : 1.f);
+          if (TREE && !whole && p.cluster) {
+            h.mx[0][0][wr] = part_m, h.mx[0][1][wr] = part_l;
+          } else if (!whole) {
+            float* part = p.part_lse + slot * 2 * p.part_rows + part_row;
+            part[0] = part_m, part[p.part_rows] = part_l;
+          } else if (p.lse) {
+            const int64_t gtok = TREE ? (int64_t)u.seq * p.rows + tok : (int64_t)u.key0 + u.tok0 + tok;
+            const float lse2 = l == 0.f ? -CUDART_INF_F : m * c + (log2f(l) - kUp);
+            p.lse[gtok * p.nq + u.head * p.rep + hh] = lse2 * 0.6931471805599453f;
+          }
+        }
+        __syncwarp();
 #pragma unroll 1
         for (int x = half * (HD / 2); x < (half + 1) * (HD / 2); x += 16) {
           unsigned o[16], o1[16];
@@ -929,7 +944,7 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
           for (int k = 0; k < 16; k++) {
             v[k] = __uint_as_float(o[k]) * f0;
             if (two) v[k] += __uint_as_float(o1[k]) * f1;
-            v[k] = l == 0.f ? 0.f : v[k] * inv;
+            v[k] = inv == 0.f ? 0.f : v[k] * inv;      // (nothing seen)
           }
           if (whole) {
             // over the tile's Q, 16-byte chunks permuted within a row so that neither side meets a bank twice
@@ -964,16 +979,6 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
               *(uint4*)(out + tok * p.o_row + hh * p.o_head + ch * 8) =
                   *(const uint4*)(qs + r * (HD * 2) + ((ch ^ (r & 7)) << 4));
             }
-          }
-        }
-        if (valid && half == 0) {
-          if (TREE && !whole && p.cluster) {
-            h.mx[0][0][wr] = lse2;
-          } else if (!whole) {
-            p.part_lse[slot * p.part_rows + part_row] = lse2;
-          } else if (p.lse) {
-            const int64_t gtok = TREE ? (int64_t)u.seq * p.rows + tok : (int64_t)u.key0 + u.tok0 + tok;
-            p.lse[gtok * p.nq + u.head * p.rep + hh] = lse2 * 0.6931471805599453f;
           }
         }
       }
@@ -1189,31 +1194,32 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
       if (parts != 1)
         for (int e = threadIdx.x + rank * each * kChunks; e < last * kChunks; e += 512) {
           const int row = e / kChunks, ch = e % kChunks;
-          const float* lse_at = &h.mx[0][0][row];
           const unsigned char* o_at = smem + L::kRing + row * (HD * 4) + ((ch ^ (row & 7)) << 4);
+          const float c = p.scale * kLog2e;
           float m = -CUDART_INF_F, sum = 0.f, v[4] = {};
-          for (int b0 = 0; b0 < parts; b0 += 8) {          // eight parts' loads under way
-            float x[8];
-            float4 y[8];
+          constexpr int kBatch = 4;                       // parts' loads under way
+          for (int b0 = 0; b0 < parts; b0 += kBatch) {
+            float x[kBatch], w[kBatch];
+            float4 y[kBatch];
 #pragma unroll
-            for (int b = 0; b < 8; b++) {
+            for (int b = 0; b < kBatch; b++) {
               const int from = min(b0 + b, parts - 1);
-              x[b] = remote_f32(lse_at, from), y[b] = remote_f32x4(o_at, from);
+              x[b] = remote_f32(&h.mx[0][0][row], from), w[b] = remote_f32(&h.mx[0][1][row], from), y[b] = remote_f32x4(o_at, from);
               if (b0 + b >= parts) x[b] = -CUDART_INF_F;
             }
             float mn = m;
 #pragma unroll
-            for (int b = 0; b < 8; b++) mn = fmaxf(mn, x[b]);
-            const float f = m == mn ? 1.f : exp2f(m - mn);
+            for (int b = 0; b < kBatch; b++) mn = fmaxf(mn, x[b]);
+            const float f = m == mn ? 1.f : exp2f((m - mn) * c);
             m = mn;
             sum *= f;
 #pragma unroll
             for (int k = 0; k < 4; k++) v[k] *= f;
 #pragma unroll
-            for (int b = 0; b < 8; b++) {
-              const float w = x[b] == -CUDART_INF_F ? 0.f : exp2f(x[b] - m);         // (nothing seen: 0)
-              sum += w;
-              v[0] += w * y[b].x, v[1] += w * y[b].y, v[2] += w * y[b].z, v[3] += w * y[b].w;
+            for (int b = 0; b < kBatch; b++) {
+              w[b] = x[b] == -CUDART_INF_F ? 0.f : w[b] * exp2f((x[b] - m) * c);         // (nothing seen: 0)
+              sum += w[b];
+              v[0] += w[b] * y[b].x, v[1] += w[b] * y[b].y, v[2] += w[b] * y[b].z, v[3] += w[b] * y[b].w;
             }
           }
           const float inv = sum == 0.f ? 0.f : 1.f / sum;
@@ -1224,7 +1230,7 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
               make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
           if (p.lse && ch == 0)
             p.lse[((int64_t)seq * p.rows + tok) * p.nq + head] =
-                !parts ? CUDART_NAN_F : sum == 0.f ? -CUDART_INF_F : (m + log2f(sum)) * 0.6931471805599453f;
+                !parts ? CUDART_NAN_F : sum == 0.f ? -CUDART_INF_F : (m * c + log2f(sum)) * 0.6931471805599453f;
         }
     }
     __syncwarp();
@@ -1234,14 +1240,14 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
 
 // ---- parts of one item joined (tree) ----------------------------------------------------------------------------
 // Items whose tiles one block had are complete already; sequences of a bad length become NaN.
-//   O = sum_i w_i O_i / sum_i w_i,  w_i = 2^(lse_i - max): the parts carry O_i / l_i and log2 of their sums.
+//   O = sum_i w_i O_i / sum_i w_i,  w_i = l_i 2^((m_i - max m) c): the parts carry O_i / l_i, m_i and l_i.
 // A block takes 32 rows and 8 columns of one item, a lane one row; the warps share the parts out, so that one way to
 // memory and back serves all of them, and meet in shared memory.
 constexpr int kJoinWarps = 8;
 template <int HD>
 __global__ void __launch_bounds__(32 * kJoinWarps) attn_join_kernel(const AttnParams p, int blocks) {
   __shared__ int sh[2];
-  __shared__ float some[kJoinWarps][10][32];          // each warp's maximum, sum and columns
+  __shared__ float some[kJoinWarps][10][32];          // each warp's columns, maximum and sum
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
   constexpr int kSlices = HD / 8;
   const int head = blockIdx.y, seq = blockIdx.z, row0 = blockIdx.x / kSlices * 32, row = row0 + lane, col = blockIdx.x % kSlices * 8;
@@ -1263,16 +1269,18 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attn_join_kernel(const AttnPa
   wait_for_grid_before();
   if (parts == 1) return;                            // complete already
   const bool valid = row < p.rows * p.rep;
+  const float c = p.scale * kLog2e;
   float m = -CUDART_INF_F, sum = 0.f, v[8] = {};
   if (valid) {
 #pragma unroll 4
     for (int b = warp; b < parts; b += warps) {      // part b is slot 2 (c0 + b), the first one's the slot behind
       const int64_t slot = (int64_t)2 * (c0 + b) + (b == 0 ? 1 : 0);
-      const float x = p.part_lse[slot * p.part_rows + local];
+      const float* at = p.part_lse + slot * 2 * p.part_rows + local;
+      const float x = at[0], l = at[p.part_rows];
       const float* o = p.part_o + ((slot * (HD / 4) + col / 4) * p.part_rows + local) * 4;
       const float4 y = *(const float4*)o, z = *(const float4*)(o + (int64_t)4 * p.part_rows);
       const float mn = fmaxf(m, x);
-      const float f = m == mn ? 1.f : exp2f(m - mn), w = x == -CUDART_INF_F ? 0.f : exp2f(x - mn);
+      const float f = m == mn ? 1.f : exp2f((m - mn) * c), w = x == -CUDART_INF_F ? 0.f : l * exp2f((x - mn) * c);
       m = mn;
       sum = sum * f + w;
       v[0] = v[0] * f + w * y.x, v[1] = v[1] * f + w * y.y, v[2] = v[2] * f + w * y.z, v[3] = v[3] * f + w * y.w;
@@ -1287,7 +1295,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attn_join_kernel(const AttnPa
   for (int g = 1; g < warps; g++) {
     const float x = some[g][8][lane];
     const float mn = fmaxf(m, x);
-    const float f = m == mn ? 1.f : exp2f(m - mn), w = x == -CUDART_INF_F ? 0.f : exp2f(x - mn);   // (nothing seen: 0)
+    const float f = m == mn ? 1.f : exp2f((m - mn) * c), w = x == -CUDART_INF_F ? 0.f : exp2f((x - mn) * c);   // (nothing seen: 0)
     m = mn;
     sum = sum * f + w * some[g][9][lane];
 #pragma unroll
@@ -1296,7 +1304,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attn_join_kernel(const AttnPa
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
   for (int k = 0; k < 8; k++) v[k] = parts ? v[k] * inv : CUDART_NAN_F;
-  const float lse = !parts ? CUDART_NAN_F : sum == 0.f ? -CUDART_INF_F : (m + log2f(sum)) * 0.6931471805599453f;
+  const float lse = !parts ? CUDART_NAN_F : sum == 0.f ? -CUDART_INF_F : (m * c + log2f(sum)) * 0.6931471805599453f;
   const int tok = div_rep(p, row), q_head = head * p.rep + row - tok * p.rep;
   *(uint4*)(p.out + (int64_t)seq * p.o_seq + tok * p.o_row + q_head * p.o_head + col) =
       make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));

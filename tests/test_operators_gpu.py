@@ -724,6 +724,27 @@ def test_tree_attention_scores_beyond_the_integers(amk, cache, power, rows, slot
     check_exact_scores(q[0], value(k), value(v), sees, out[0], lse[0], scale)
 
 
+@pytest.mark.parametrize("cache", ["bf16", "fp8"])
+@pytest.mark.parametrize("power", [6, 10, 16, 24, 60])
+@pytest.mark.parametrize("seqs,rows,slots,nq,nkv,hd", [(1, 3, 1500, 4, 2, 64), (1, 2, 9001, 8, 1, 128), (3, 40, 5000, 8, 1, 64),
+                                                       (1, 1, 6000, 32, 8, 128)])
+def test_tree_attention_equal_scores_in_parts(amk, cache, power, seqs, rows, slots, nq, nkv, hd):
+    """One large score for all keys: each weighs the same, in whichever part it comes and however many keys the part has."""
+    q, _, v = tree_inputs(seqs, rows, slots, nq, nkv, hd, cache, power)
+    v = v & 0x7F if cache == "fp8" else v.abs()
+    lens = [slots - rows, 777, 130][:seqs]
+    q = torch.full_like(q, 1.375 * 2.0 ** power)
+    k = torch.full((seqs, nkv, slots, hd), 1.5, device=DEV)
+    k = k.to(torch.float8_e4m3fn).view(torch.uint8) if cache == "fp8" else k.to(torch.bfloat16)
+    lse = torch.empty(seqs, rows, nq, device=DEV)
+    out = amk.amk_tree_attention(q, k, v, torch.tensor(lens, dtype=torch.int32, device=DEV), scale=0.125, lse=lse)
+    value = (lambda t: t.view(torch.float8_e4m3fn).float().permute(1, 0, 2)) if cache == "fp8" else (lambda t: t.permute(1, 0, 2))
+    for b, n in enumerate(lens):
+        sees = torch.ones(rows, n + rows, dtype=torch.bool, device=DEV)
+        sees[:, n:] = causal(rows)
+        check_exact_scores(q[b], value(k[b, :, :n + rows]), value(v[b, :, :n + rows]), sees, out[b], lse[b], 0.125, b)
+
+
 def test_tree_attention_bad_lengths(amk):
     rows, nq, nkv, hd, slots = 4, 4, 2, 64, 100
     q, k, v = tree_inputs(4, rows, slots, nq, nkv, hd, "bf16", 3)
