@@ -652,7 +652,10 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
             for (int k = 0; k < 4; k++) w[k] = pack_f16(bf16_lo(w[k]) * by, bf16_hi(w[k]) * by);
             v[i] = make_uint4(w[0], w[1], w[2], w[3]);
             const int e = i * 256 + id;
-            if (e % kChunks == 0) h.row_c[t][e / kChunks] = p.scale * kLog2e * __uint_as_float((unsigned)(127 - power) << 23);
+            // (no less than the smallest normal number: 0 times the -infinity of a hidden key would be NaN, and scores
+            // of 2^31 at most vanish either way)
+            if (e % kChunks == 0)
+              h.row_c[t][e / kChunks] = fmaxf(p.scale * kLog2e * __uint_as_float((unsigned)(127 - power) << 23), 1.17549435e-38f);
           }
         }
 #pragma unroll

@@ -745,6 +745,20 @@ def test_tree_attention_equal_scores_in_parts(amk, cache, power, seqs, rows, slo
         check_exact_scores(q[b], value(k[b, :, :n + rows]), value(v[b, :, :n + rows]), sees, out[b], lse[b], 0.125, b)
 
 
+@pytest.mark.parametrize("cache", ["bf16", "fp8"])
+@pytest.mark.parametrize("scale", [1e-12, 1e-30, 1e-44])
+@pytest.mark.parametrize("rows,slots,nq,nkv,hd", [(5, 300, 4, 2, 64), (70, 900, 8, 2, 128)])
+def test_tree_attention_vanishing_scores(amk, cache, scale, rows, slots, nq, nkv, hd):
+    """Queries near the smallest numbers and a scale that all but vanishes: every key that is seen weighs the same."""
+    q, k, v = tree_inputs(1, rows, slots, nq, nkv, hd, cache, 5)
+    q = q * 1e-37
+    bits = np.stack([tree_bits(np.random.default_rng(3), rows)])
+    n = slots - rows
+    lse = torch.empty(1, rows, nq, device=DEV)
+    out = amk.amk_tree_attention(q, k, v, torch.tensor([n], dtype=torch.int32, device=DEV), words(bits), scale=scale, lse=lse)
+    check_tree(q, k, v, [n], bits, out, lse, scale)
+
+
 def test_tree_attention_bad_lengths(amk):
     rows, nq, nkv, hd, slots = 4, 4, 2, 64, 100
     q, k, v = tree_inputs(4, rows, slots, nq, nkv, hd, "bf16", 3)
