@@ -366,7 +366,7 @@ typedef struct amk_prompt_args {
   uint32_t n_q_heads;        /* multiple of n_kv_heads; n_q_heads / n_kv_heads <= 16; at most 4096     */
   uint32_t n_kv_heads;
   uint32_t n_seqs;
-  float scale;               /* > 0, or 0: 1 / sqrt(head_dim)                                          */
+  float scale;               /* > 0 and scale log2 e finite, or 0: 1 / sqrt(head_dim)                  */
   int64_t total;             /* rows of q, k, v and out; below 2^31                                    */
   const void* q;
   const void* k;
@@ -412,7 +412,7 @@ typedef struct amk_tree_args {
   uint32_t n_rows;           /* drafted tokens per sequence, 1 .. AMK_TREE_MAX_ROWS                    */
   uint32_t n_slots;          /* rows of the cache                                                      */
   uint32_t max_len;
-  float scale;               /* > 0, or 0: 1 / sqrt(head_dim)                                          */
+  float scale;               /* > 0 and scale log2 e finite, or 0: 1 / sqrt(head_dim)                  */
   const void* q;
   const void* k;
   const void* v;

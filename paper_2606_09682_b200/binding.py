@@ -77,6 +77,7 @@ class amk_tree_args(C.Structure):
 # the same two structs as struct formats: packing one costs a microsecond, filling a ctypes structure several
 _PROMPT = struct.Struct("@5Ifq6P8q")
 _TREE = struct.Struct("@9If8PQ12q")
+_F32 = struct.Struct("@f")
 
 
 def _load() -> C.CDLL:
@@ -275,6 +276,19 @@ def _refuse(name: str, what: str):
     raise AmkError(AMK_ERR_INVALID_ARG, f"{name}: {what}")
 
 
+def _scale(name: str, scale: Optional[float]) -> float:
+    """The scale as the struct's fp32 holds it, where 0 stands for the default."""
+    if scale is None:
+        return 0.0
+    try:
+        held = _F32.unpack(_F32.pack(scale))[0]
+    except OverflowError:
+        held = float("inf")
+    if not 0.0 < held < float("inf"):
+        _refuse(name, f"scale {scale} must be positive and finite in fp32")
+    return held
+
+
 def _device_of(name: str, first: torch.Tensor, *others) -> int:
     """Index of the cuda device that all the tensors (or None) live on."""
     index = first.get_device()                        # -1: not a cuda tensor
@@ -330,9 +344,7 @@ def amk_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_s
     (qr, qh, q1), (kr, kh, k1), (vr, vh, v1), (orow, oh, o1) = q.stride(), k.stride(), v.stride(), out.stride()
     if not (q1 == k1 == v1 == o1 == 1):
         _refuse(name, "the last dimension must be contiguous")
-    if scale is not None and not scale > 0:
-        _refuse(name, "scale must be positive")
-    args = _PROMPT.pack(_PROMPT.size, hd, nq, kshape[1], entries - 1, scale or 0.0, total, q.data_ptr(),
+    args = _PROMPT.pack(_PROMPT.size, hd, nq, kshape[1], entries - 1, _scale(name, scale), total, q.data_ptr(),
                         k.data_ptr(), v.data_ptr(), out.data_ptr(), 0 if lse is None else lse.data_ptr(),
                         cu_seqlens.data_ptr(), qr, qh, kr, kh, vr, vh, orow, oh)
     _run(lib.amk_prompt_attention, name, dev, args)
@@ -382,8 +394,6 @@ def amk_tree_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cache_
     os_, orow, oh, o1 = out.stride()
     if not (q1 == k1 == v1 == o1 == 1):
         _refuse(name, "the last dimension must be contiguous")
-    if scale is not None and not scale > 0:
-        _refuse(name, "scale must be positive")
     plan = (_TREE.size, hd, nq, nkv, AMK_KV_BF16 if dtype is torch.bfloat16 else AMK_KV_FP8_E4M3, seqs, rows, slots,
             max_len or 0)
     if workspace is None:
@@ -401,7 +411,7 @@ def amk_tree_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cache_
         if not workspace.is_contiguous():
             _refuse(name, "the workspace must be contiguous")
         have = workspace.numel() * workspace.element_size()
-    args = _TREE.pack(*plan, scale or 0.0, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
+    args = _TREE.pack(*plan, _scale(name, scale), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
                       0 if lse is None else lse.data_ptr(), cache_len.data_ptr(), 0 if mask is None else mask.data_ptr(),
                       0 if workspace is None else workspace.data_ptr(), have, qs, qr, qh, ks, kh, kr, vs, vh, vr, os_, orow, oh)
     _run(lib.amk_tree_attention, name, dev, args)

@@ -195,7 +195,8 @@ amk_status check_heads(const Reason& fail, uint32_t hd, uint32_t nq, uint32_t nk
   if (hd != 64 && hd != 128) return fail(AMK_ERR_UNSUPPORTED, "head_dim %u: 64 or 128", hd);
   if (!nq || !nkv || nq % nkv || nq / nkv > 16 || nq > 4096)
     return fail(AMK_ERR_UNSUPPORTED, "%u query heads on %u kv heads: a multiple, at most 16 to one and 4096", nq, nkv);
-  if (!(scale >= 0.f) || isinf(scale)) return fail(AMK_ERR_INVALID_ARG, "scale must be positive and finite, or 0");
+  if (!(scale >= 0.f) || isinf(scale * amk::kLog2e))
+    return fail(AMK_ERR_INVALID_ARG, "scale must be positive, or 0, and its product with log2 e finite");
   return AMK_OK;
 }
 

@@ -117,6 +117,21 @@ def test_tree_workspace_refuses(amk):
     assert b"drafted" in msg.value
 
 
+@pytest.mark.parametrize("scale", [2.4e38, 3.4e38])
+def test_a_scale_whose_product_with_log2e_overflows_is_refused(amk, scale):
+    refused(amk.lib.amk_prompt_attention, (prompt_args(amk, scale=scale),), INVALID, "scale")
+    refused(amk.lib.amk_tree_attention, (tree_args(amk, scale=scale),), INVALID, "scale")
+
+
+@pytest.mark.parametrize("scale", [1e-46, 1e-320, 1e39, 0.0, -1.0, NAN, float("inf")])
+def test_python_scale_is_the_one_that_fp32_holds(amk, scale):
+    """A positive number that rounds to zero would mean the default."""
+    with pytest.raises(amk.AmkError) as e:
+        amk._scale("call", scale)
+    assert e.value.code == INVALID and "scale" in str(e.value)
+    assert amk._scale("call", None) == 0.0 and amk._scale("call", 0.125) == 0.125 and 0 < amk._scale("call", 1e-45) < 2e-45
+
+
 def logprob_args(**kw):
     a = dict(logits=P, dtype=0, rows=3, vocab=100, stride=100, tokens=P, top=2, lp=P, ent=P, ids=P, tlp=P)
     assert set(kw) <= set(a)

@@ -1119,6 +1119,18 @@ def test_python_layer_refuses_a_scale_that_is_none(amk, scale):
         assert e.value.code == amk.AMK_ERR_INVALID_ARG
 
 
+@pytest.mark.parametrize("scale", [1e-46, 1e-320, 1e39, 2.4e38])
+def test_python_layer_refuses_a_scale_that_fp32_cannot_hold(amk, scale):
+    """What rounds to zero would mean the default; scale and scale log2 e have to be finite."""
+    q, k, v, cu = prompt_inputs([20], 4, 2, 64, 1)
+    qt, kt, vt = tree_inputs(2, 3, 50, 4, 2, 64, "bf16", 1)
+    for call in (lambda: amk.amk_prompt_attention(q, k, v, cu, scale=scale),
+                 lambda: amk.amk_tree_attention(qt, kt, vt, torch.zeros(2, dtype=torch.int32, device=DEV), scale=scale)):
+        with pytest.raises(amk.AmkError) as e:
+            call()
+        assert e.value.code == amk.AMK_ERR_INVALID_ARG and "scale" in str(e.value)
+
+
 # ---- together ---------------------------------------------------------------------------------------------------
 
 def forward(shape, w, tokens, positions, attend):
