@@ -395,7 +395,7 @@ def amk_tree_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cache_
     if not (q1 == k1 == v1 == o1 == 1):
         _refuse(name, "the last dimension must be contiguous")
     plan = (_TREE.size, hd, nq, nkv, AMK_KV_BF16 if dtype is torch.bfloat16 else AMK_KV_FP8_E4M3, seqs, rows, slots,
-            max_len or 0)
+            0 if max_len is None else max(max_len, 1))    # (0 would mean that no bound is known)
     if workspace is None:
         key = (dev, plan)
         need = _tree_bytes.get(key)

@@ -1131,6 +1131,19 @@ def test_python_layer_refuses_a_scale_that_fp32_cannot_hold(amk, scale):
         assert e.value.code == amk.AMK_ERR_INVALID_ARG and "scale" in str(e.value)
 
 
+def test_a_bound_of_no_context_is_a_bound(amk, monkeypatch):
+    """max_len = 0 states that every context is empty; in the C struct 0 means that nothing is known."""
+    q, k, v = tree_inputs(2, 3, 9000, 4, 2, 64, "bf16", 1)
+    length = torch.zeros(2, dtype=torch.int32, device=DEV)
+    seen, run = [], amk._run
+    monkeypatch.setattr(amk, "_run", lambda fn, name, index, args: (seen.append(amk.amk_tree_args.from_buffer_copy(args).max_len),
+                                                                    run(fn, name, index, args)))
+    for bound in (None, 0, 1, 500):
+        out = amk.amk_tree_attention(q, k, v, length, max_len=bound)
+        check_tree(q, k, v, [0, 0], np.tril(np.ones((2, 3, 3), bool)), out, None, 0.125, bound)
+    assert seen == [0, 1, 1, 500]
+
+
 # ---- together ---------------------------------------------------------------------------------------------------
 
 def forward(shape, w, tokens, positions, attend):
