@@ -290,14 +290,25 @@ def _scale(name: str, scale: Optional[float]) -> float:
 
 
 def _device_of(name: str, first: torch.Tensor, *others) -> int:
-    """Index of the cuda device that all the tensors (or None) live on."""
+    """Index of the cuda device that all the tensors (or None) live on.  The operators have no backward pass: a tensor for which
+    autograd would record the call is refused."""
     index = first.get_device()                        # -1: not a cuda tensor
     if index < 0:
         _refuse(name, "tensors must be cuda tensors")
+    if first.requires_grad:
+        _no_gradient(name)
     for t in others:
-        if t is not None and t.get_device() != index:
-            _refuse(name, "tensors on different devices")
+        if t is not None:
+            if t.get_device() != index:
+                _refuse(name, "tensors on different devices")
+            if t.requires_grad:
+                _no_gradient(name)
     return index
+
+
+def _no_gradient(name: str) -> None:
+    if torch.is_grad_enabled():
+        raise AmkError(AMK_ERR_UNSUPPORTED, f"{name}: there is no gradient; detach the tensors or call under torch.no_grad()")
 
 
 def _run(fn, name: str, index: int, *args) -> None:

@@ -1144,6 +1144,28 @@ def test_a_bound_of_no_context_is_a_bound(amk, monkeypatch):
     assert seen == [0, 1, 1, 500]
 
 
+def test_python_layer_refuses_inputs_that_want_gradients(amk):
+    """The operators have no backward pass: where autograd would record the call, it is refused; elsewhere it runs."""
+    q, k, v, cu = prompt_inputs([20], 4, 2, 64, 1)
+    qt, kt, vt = tree_inputs(2, 3, 50, 4, 2, 64, "bf16", 1)
+    length = torch.zeros(2, dtype=torch.int32, device=DEV)
+    x, kv = torch.zeros(2, 90, device=DEV), torch.zeros(1, 4, 8, 64, device=DEV)
+    grad = lambda t: t.detach().clone().requires_grad_()
+    one, keep = cu[:1], cu[None, 1:]
+    calls = [lambda: amk.amk_prompt_attention(grad(q), k, v, cu), lambda: amk.amk_prompt_attention(q, grad(k), v, cu),
+             lambda: amk.amk_prompt_attention(q, k, grad(v), cu), lambda: amk.amk_prompt_attention(q, k, v, cu, out=grad(q)),
+             lambda: amk.amk_prompt_attention(q, k, v, cu, lse=grad(torch.zeros(20, 4, device=DEV))),
+             lambda: amk.amk_tree_attention(grad(qt), kt, vt, length), lambda: amk.amk_tree_attention(qt, grad(kt), vt, length),
+             lambda: amk.amk_tree_attention(qt, kt, grad(vt), length), lambda: amk.amk_tree_attention(qt, kt, vt, length, out=grad(qt)),
+             lambda: amk.amk_token_logprobs(grad(x), cu), lambda: amk.amk_kv_compact(grad(kv), one, keep, one)]
+    for i, call in enumerate(calls):
+        with pytest.raises(amk.AmkError) as e:
+            call()
+        assert e.value.code == amk.AMK_ERR_UNSUPPORTED and "gradient" in str(e.value), i
+        with torch.no_grad():
+            call()
+
+
 # ---- together ---------------------------------------------------------------------------------------------------
 
 def forward(shape, w, tokens, positions, attend):
