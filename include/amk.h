@@ -435,6 +435,11 @@ amk_status amk_tree_attention(const amk_tree_args* args, char* msg, size_t msg_b
  */
 amk_status amk_operator_status(amk_status* st, char* msg, size_t msg_bytes, void* cuda_stream);
 
+/* Test hook for these bounded waits, for the attention calls of this process from now on: a block asks for `tiles` K and V
+ * tiles at most, so that what waits for the next one runs out of time (nothing traps or hangs), after `cycles` cycles of
+ * its SM.  cycles = 0 and tiles = UINT32_MAX: as without the hook.  INVALID_ARG: more cycles than the two seconds. */
+amk_status amk_debug_operator_wait(uint32_t cycles, uint32_t tiles);
+
 /*
  * Log probabilities of given tokens, in one pass over the logits: with m = max x, s = sum e^(x-m),
  *   logprob[r] = x[token[r]] - m - log s,   entropy[r] = log s - sum e^(x-m) (x-m) / s  (natural logarithms),

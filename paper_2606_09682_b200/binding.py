@@ -112,6 +112,7 @@ def _load() -> C.CDLL:
         "amk_tree_workspace_bytes": (C.c_int, [C.c_char_p, C.POINTER(sz), C.c_char_p, sz]),
         "amk_tree_attention": (C.c_int, [C.c_char_p, C.c_char_p, sz, vp]),
         "amk_operator_status": (C.c_int, [C.POINTER(C.c_int), C.c_char_p, sz, vp]),
+        "amk_debug_operator_wait": (C.c_int, [C.c_uint32, C.c_uint32]),
         "amk_token_logprobs": (C.c_int, [vp, C.c_uint32, i64, i64, i64, vp, C.c_uint32, vp, vp, vp, vp, C.c_char_p, sz,
                                          vp]),
         "amk_kv_compact": (C.c_int, [vp, i64, i64, i64, i64, i64, vp, vp, i64, vp, C.c_char_p, sz, vp]),
@@ -130,7 +131,7 @@ EXPORTS = ("amk_status_str", "amk_packed_bytes", "amk_workspace_bytes", "amk_kv_
            "amk_debug_trace", "amk_debug_unpack", "amk_debug_drop_signal", "amk_debug_set_step_count", "amk_last_kernel_ns", "amk_destroy", "amk_quantize_int8", "amk_quantize_int8_grouped", "amk_quantize_int4",
            "amk_argmax_static", "amk_plan_export", "amk_plan_check",
            "amk_prompt_attention", "amk_tree_workspace_bytes", "amk_tree_attention", "amk_operator_status",
-           "amk_token_logprobs",
+           "amk_debug_operator_wait", "amk_token_logprobs",
            "amk_kv_compact")
 
 
@@ -447,6 +448,14 @@ def amk_operator_status(device=None) -> int:
     index = None if device is None else torch.device(device).index
     _run(lib.amk_operator_status, "amk_operator_status", torch.cuda.current_device() if index is None else index, C.byref(st))
     return st.value
+
+
+def amk_debug_operator_wait(cycles: int = 0, tiles: int = 0xFFFFFFFF) -> None:
+    """Test hook: the attentions' blocks ask for ``tiles`` tiles at most and their waits run out after ``cycles`` cycles; without
+    arguments all is as it was."""
+    code = lib.amk_debug_operator_wait(cycles, tiles)
+    if code != AMK_OK:
+        raise AmkError(code, "amk_debug_operator_wait")
 
 
 def amk_token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, top_k: int = 0):

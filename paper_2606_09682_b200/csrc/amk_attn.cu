@@ -141,6 +141,14 @@ int sm_count() {
   return n;
 }
 
+// What amk_debug_operator_wait set.
+std::atomic<unsigned> g_wait_cycles{amk::kWaitCycles};
+std::atomic<unsigned> g_tiles{~0u};
+void set_limits(AttnParams& p) {
+  p.wait_cycles = g_wait_cycles.load(std::memory_order_relaxed);
+  p.tiles = g_tiles.load(std::memory_order_relaxed);
+}
+
 // How a tree call is divided: rows of a block, blocks, scratch.  Runs of equal length for all blocks and a second kernel that
 // joins the parts, or, in one launch and without scratch, for each item
 //  - a cluster of blocks with two tiles each, where it has few rows: the parts meet in distributed shared memory, which is
@@ -270,6 +278,7 @@ extern "C" amk_status amk_prompt_attention(const amk_prompt_args* args, char* ms
   p.rep_inv = p.rep == 1 ? 0 : (unsigned)(((1ull << 32) + p.rep - 1) / p.rep);
   p.rows = (int)a.total;
   p.scale = a.scale > 0.f ? a.scale : 1.f / sqrtf((float)hd);
+  set_limits(p);
   // blocks of 256 / rep tokens: every prompt may leave one that is not full
   const int64_t blocks = (a.total / (2 * amk::kTile / p.rep) + (a.total < a.n_seqs ? a.total : a.n_seqs)) * p.nkv;
   if (blocks > 0x7fffffff) return fail(AMK_ERR_UNSUPPORTED, "%lld blocks of queries", (long long)blocks);
@@ -296,18 +305,24 @@ extern "C" amk_status amk_operator_status(amk_status* st, char* msg, size_t msg_
   const Reason fail(msg, msg_bytes, "amk_operator_status");
   if (!st) return fail(AMK_ERR_INVALID_ARG, "NULL pointer");
   *st = AMK_OK;
-  unsigned expired = 0;
+  unsigned expired[2] = {0, 0};                        // how often, and how many were told of
   cudaError_t e = cudaStreamSynchronize((cudaStream_t)cuda_stream);
   if (e == cudaSuccess)
-    e = cudaMemcpyFromSymbolAsync(&expired, amk::g_attn_expired, 4, 0, cudaMemcpyDeviceToHost, (cudaStream_t)cuda_stream);
+    e = cudaMemcpyFromSymbolAsync(expired, amk::g_attn_expired, 8, 0, cudaMemcpyDeviceToHost, (cudaStream_t)cuda_stream);
   if (e == cudaSuccess) e = cudaStreamSynchronize((cudaStream_t)cuda_stream);
-  if (e == cudaSuccess && expired) {
-    const unsigned zero = 0;
-    e = cudaMemcpyToSymbolAsync(amk::g_attn_expired, &zero, 4, 0, cudaMemcpyHostToDevice, (cudaStream_t)cuda_stream);
+  if (e == cudaSuccess && expired[0] != expired[1]) {
+    e = cudaMemcpyToSymbolAsync(amk::g_attn_expired, &expired[0], 4, 4, cudaMemcpyHostToDevice, (cudaStream_t)cuda_stream);
     if (e == cudaSuccess) e = cudaStreamSynchronize((cudaStream_t)cuda_stream);
     *st = AMK_ERR_TIMEOUT;
   }
   return e == cudaSuccess ? AMK_OK : fail(AMK_ERR_CUDA, "%s", cudaGetErrorString(e));
+}
+
+extern "C" amk_status amk_debug_operator_wait(uint32_t cycles, uint32_t tiles) {
+  if (cycles > amk::kWaitCycles) return AMK_ERR_INVALID_ARG;
+  g_wait_cycles.store(cycles ? cycles : amk::kWaitCycles, std::memory_order_relaxed);
+  g_tiles.store(tiles, std::memory_order_relaxed);
+  return AMK_OK;
 }
 
 extern "C" amk_status amk_tree_attention(const amk_tree_args* args, char* msg, size_t msg_bytes,
@@ -351,6 +366,7 @@ extern "C" amk_status amk_tree_attention(const amk_tree_args* args, char* msg, s
   p.rows = (int)a.n_rows, p.slots = (int)a.n_slots;
   p.part_rows = t.part_rows, p.row_tiles = t.row_tiles, p.min_tiles = kMinTiles, p.cluster = t.cluster;
   p.scale = a.scale > 0.f ? a.scale : 1.f / sqrtf((float)hd);
+  set_limits(p);
   const bool fp8 = esz == 1;
   CUtensorMap mk, mv;
   if (!make_map(&mk, a.k, fp8, hd, a.n_slots, p.nkv, a.n_seqs, a.k_row, a.k_head, a.k_seq) ||

@@ -48,6 +48,8 @@ struct AttnParams {
   int min_tiles;                   // tree: key tiles a block takes at least
   int cluster;                     // tree: blocks of one item, which meet at the end; 0: runs and a second kernel
   unsigned rep_inv;                // ceil(2^32 / rep), 0 for rep = 1
+  unsigned tiles;                  // K and V tiles that a block may ask for (a test's limit, else the largest number)
+  unsigned wait_cycles;            // a wait runs out after so many
   float scale;
 };
 
@@ -58,8 +60,9 @@ __device__ __forceinline__ int div_rep(const AttnParams& p, int row) {
 }
 constexpr float kLog2e = 1.4426950408889634f;
 
-// Set when a bounded wait of an attention kernel ran out; read and cleared by amk_operator_status.
-static __device__ unsigned g_attn_expired;
+// How often a bounded wait of an attention kernel ran out, and how many of these amk_operator_status has told of.  (Two numbers
+// that only grow: one that is read and then cleared loses what happens in between on another stream.)
+static __device__ unsigned g_attn_expired[2];
 
 __device__ __forceinline__ unsigned pack_bf16(float lo, float hi) {   // round to nearest even
   unsigned r;
@@ -176,10 +179,11 @@ struct AttnHead {
   uint64_t q_full[2], s_full[2], p_full[2], o_done[2], fin;
   unsigned tmem;
   int dead;                            // a bounded wait ran out: nobody waits or issues any more
+  unsigned wait_cycles;
   int skip[2];                         // this step's P V was done by the warpgroup itself
   float mx[2][2][kTile];               // [tile][half]: row maxima, and at the end row sums, of half the columns
   float m[kTile], l[kTile];            // the second tile's statistics (both tiles of the same rows)
-  int unit[8];
+  int unit[8];                         // where the block's work begins; behind it what the producer had asked for at its end
   uint64_t unit_full[kUnitRing], unit_empty[kUnitRing], next_full;   // prompts: blocks of queries, taken one after the other
   int4 units[kUnitRing], now_of[2][2];                               // the producer's; the two last ones of each row tile
   uint4 next;                                                        // answer of the hardware's scheduler
@@ -190,21 +194,21 @@ struct AttnHead {
 };
 static_assert(sizeof(AttnHead) <= kHeadBytes, "head");
 
-constexpr long long kWaitCycles = 4000000000ll;
-// A whole warp waits for the phase of the given parity, about two seconds at most (the SM's cycle counter: the global
+constexpr unsigned kWaitCycles = 4000000000u;
+// A whole warp waits for the phase of the given parity, about two seconds (kWaitCycles) at most (the SM's cycle counter: the global
 // timer is read through a unit that all SMs share); false if that ran out.  The votes keep the warp's control flow
 // uniform: behind a wait that each lane leaves by itself, the matrix instructions of one tile took ten times as long
 // to issue (700 cycles instead of 70).
 __device__ __forceinline__ bool attn_wait(uint64_t* bar, unsigned parity, AttnHead& h) {
   if (__all_sync(~0u, mbar_try_wait(bar, parity))) return true;
-  const long long t0 = clock64();
+  const unsigned t0 = clock();
   for (;;) {
     for (int i = 0; i < 32; i++)
       if (__all_sync(~0u, mbar_try_wait(bar, parity))) return true;
     if (__any_sync(~0u, *(volatile int*)&h.dead)) return false;
-    if (__any_sync(~0u, clock64() - t0 > kWaitCycles)) {
+    if (__any_sync(~0u, (unsigned)clock() - t0 > h.wait_cycles)) {
       *(volatile int*)&h.dead = 1;
-      atomicExch(&g_attn_expired, 1u);
+      atomicAdd(&g_attn_expired[0], 1u);             // (of every lane: how many does not matter)
       return false;
     }
   }
@@ -468,6 +472,36 @@ __device__ __noinline__ void product_by_key(unsigned tp, unsigned see0, unsigned
   tmem_wait_st();
 }
 
+// The block's dynamic shared memory, from a multiple of 1024 bytes on.
+__device__ __forceinline__ unsigned char* attn_smem() {
+  extern __shared__ unsigned char smem_raw[];
+  return (unsigned char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+}
+
+// The block's end, all threads, behind a barrier: if a wait ran out, copies and products in flight end (waits again, with a limit)
+// before their memory is given back.  A function of its own that finds everything by itself: whatever the kernel held in a
+// register for this cost 4 % of a long prompt.
+template <int HD, bool FP8>
+__device__ __noinline__ void end_in_flight() {
+  using L = AttnSmem<HD, FP8>;
+  constexpr unsigned kN = FP8 ? L::kRawStages : L::kStages, kProducer = FP8 ? 20 : 16;
+  AttnHead& h = *(AttnHead*)(attn_smem() + L::kHead);
+  if (!h.dead) return;
+  const unsigned warp = threadIdx.x >> 5;
+  if (warp == kProducer) {
+    uint64_t* full = FP8 ? h.raw_full : h.full;
+    const unsigned issued = (unsigned)h.unit[5], asked = (unsigned)h.unit[6], told = (unsigned)h.unit[7];
+    for (unsigned i = issued > kN ? issued - kN : 0; i < issued; i++)
+      for (int n = 0; n < 1 << 16 && !__all_sync(~0u, mbar_try_wait(&full[i % kN], i / kN & 1)); n++) {}
+    for (int n = 0; asked != told && n < 1 << 16 && !__all_sync(~0u, mbar_try_wait(&h.next_full, told & 1)); n++) {}
+  }
+  if (warp == kProducer + 1) {                         // the issuer
+    mma_commit(elect_one(), &h.fin);
+    for (int n = 0; n < 1 << 16 && !__all_sync(~0u, mbar_try_wait(&h.fin, 0)); n++) {}
+  }
+  __syncthreads();
+}
+
 // Over the 8-bit cache the matrix instructions work on f16: two e4m3 codes are two f16 by one conversion (to bf16 it takes
 // three more), P has three bits more than in bf16, and a row of Q is exact in f16 after a power of two.  P is rounded to
 // the operands' type (2^-8 of it in bf16), the sum l is not: the roundings of a row are independent and average out.
@@ -489,8 +523,7 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
   using L = AttnSmem<HD, FP8>;
   constexpr int kProducer = FP8 ? 20 : 16, kIssuer = kProducer + 1;
   constexpr float kRise = Numerators<FP8>::kRise, kUp = Numerators<FP8>::kUp;
-  extern __shared__ unsigned char smem_raw[];
-  unsigned char* smem = (unsigned char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  unsigned char* smem = attn_smem();
   AttnHead& h = *(AttnHead*)(smem + L::kHead);
   const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   const bool dual = TREE && p.part_rows == kTile;
@@ -506,7 +539,7 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
         mbar_init(&h.p_full[t], 8), mbar_init(&h.o_done[t], 1);
       }
       mbar_init(&h.fin, 1);
-      h.dead = 0;
+      h.dead = 0, h.wait_cycles = p.wait_cycles;
       mbar_fence_init();
     }
   }
@@ -1042,7 +1075,7 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
             for (int t = 0; t < 2; t++)
               if (unit_steps<TREE>(p, u, dual, t)) attn_wait(&h.q_full[t], 0, h);
           }
-          on = attn_wait(&empty[st], (issued / kN & 1) ^ 1, h) && on;
+          on = on && issued != p.tiles && attn_wait(&empty[st], (issued / kN & 1) ^ 1, h);
           if (!on) continue;
           const CUtensorMap* map = kv ? &map_v : &map_k;
           const int y = uniform(u.key0) + j * kTile, z = uniform(u.head), w = uniform(u.seq);
@@ -1079,11 +1112,7 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
         }
       }
     }
-    if (uniform(*(volatile int*)&h.dead)) {    // copies in flight land before the block ends
-      for (unsigned i = issued > kN ? issued - kN : 0; i < issued; i++)
-        for (int n = 0; n < 1 << 16 && !__all_sync(~0u, mbar_try_wait(&full[i % kN], i / kN & 1)); n++) {}
-      for (int n = 0; asked != told && n < 1 << 16 && !__all_sync(~0u, mbar_try_wait(&h.next_full, told & 1)); n++) {}
-    }
+    if (lane == 0) h.unit[5] = (int)issued, h.unit[6] = (int)asked, h.unit[7] = (int)told;
   } else if (warp == kIssuer) {
     // ================================ the matrix products ==============================================================
     // The whole warp walks the steps, so that addresses and phases stay warp-uniform; one lane issues.
@@ -1146,10 +1175,6 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
       }
       ring += uniform(2 * (u.tile_end - u.tile_begin));
     }
-    if (uniform(*(volatile int*)&h.dead)) {    // products in flight end before TMEM is given back
-      mma_commit(leader, &h.fin);
-      for (int n = 0; n < 1 << 16 && !__all_sync(~0u, mbar_try_wait(&h.fin, 0)); n++) {}
-    }
   } else if (FP8) {
     // ================================ 8-bit tiles widened to f16: six warps ============================================
     const int ct = (warp < 20 ? warp - 16 : warp - 18) * 32 + lane;
@@ -1184,6 +1209,7 @@ __global__ void __launch_bounds__(FP8 ? 768 : 640, 1)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  end_in_flight<HD, FP8>();
   if (warp == kIssuer) tmem_free(tmem, 512);
   if (TREE && p.cluster) {
     // the item's parts joined in the cluster: each block takes some of the rows and reads the others' parts of them

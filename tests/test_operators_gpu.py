@@ -365,6 +365,54 @@ def test_operators_wait_for_what_is_in_front_of_them(amk, captured):
         assert all(torch.equal(a, b) for a, b in zip(outs, want))
 
 
+@pytest.mark.parametrize("tiles", [0, 1, 2, 3])
+@pytest.mark.parametrize("kind", ["prompt", "prompts", "tree run", "tree cluster", "tree block", "tree fp8", "tree rows"])
+def test_attention_waits_run_out_and_the_next_call_is_fine(amk, kind, tiles):
+    """A block that gets no more than some of its tiles: every wait for the next one ends, the status says so once, and what
+    comes after is as ever."""
+    hd = 64
+    if kind.startswith("prompt"):
+        q, k, v, cu = prompt_inputs([700] if kind == "prompt" else [300, 0, 5, 200, 129] * 20, 4, 2, hd, 3)
+        call = lambda: amk.amk_prompt_attention(q, k, v, cu)
+    else:
+        rows, slots, nq, nkv, seqs = {"run": (9, 4000, 8, 2, 3), "cluster": (3, 2000, 4, 2, 1), "block": (20, 700, 8, 2, 50),
+                                      "fp8": (5, 3000, 8, 2, 2), "rows": (100, 1500, 8, 2, 1)}[kind.split()[1]]
+        q, k, v = tree_inputs(seqs, rows, slots, nq, nkv, hd, "fp8" if kind == "tree fp8" else "bf16", 4)
+        length = torch.full((seqs,), slots - rows, dtype=torch.int32, device=DEV)
+        call = lambda: amk.amk_tree_attention(q, k, v, length)
+    want = call()
+    assert amk.amk_operator_status() == amk.AMK_OK
+    amk.amk_debug_operator_wait(2_000_000, tiles)      # about a millisecond
+    try:
+        call()
+        assert amk.amk_operator_status() == amk.AMK_ERR_TIMEOUT
+        assert amk.amk_operator_status() == amk.AMK_OK
+    finally:
+        amk.amk_debug_operator_wait()
+    assert torch.equal(call(), want) and amk.amk_operator_status() == amk.AMK_OK
+    with pytest.raises(amk.AmkError):
+        amk.amk_debug_operator_wait(4_000_000_001)
+
+
+def test_an_expired_wait_is_told_of_once_whichever_stream_asks(amk):
+    """Two expiries on two streams, asked about in between: the second one is not lost."""
+    q, k, v, cu = prompt_inputs([300], 4, 2, 64, 3)
+    side = torch.cuda.Stream()
+    amk.amk_operator_status()
+    for stream in (torch.cuda.current_stream(), side, torch.cuda.current_stream()):
+        amk.amk_debug_operator_wait(2_000_000, 0)
+        try:
+            with torch.cuda.stream(stream):
+                amk.amk_prompt_attention(q, k, v, cu)
+            torch.cuda.synchronize()
+        finally:
+            amk.amk_debug_operator_wait()
+        amk.amk_prompt_attention(q, k, v, cu)
+        assert amk.amk_operator_status() == amk.AMK_ERR_TIMEOUT
+        with torch.cuda.stream(side):
+            assert amk.amk_operator_status() == amk.AMK_OK
+
+
 def test_first_call_of_a_process_may_be_captured():
     """Everything that a call sets up once happens in the call itself, and capture allows it."""
     code = """
