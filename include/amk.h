@@ -355,7 +355,8 @@ amk_status amk_argmax_static(const float* x, int64_t n, int32_t* token, char* ms
  *   cu_seqlens    DEVICE int32 [n_seqs + 1]: prompt s is rows [cu[s], cu[s+1]); lengths of zero are allowed.  Rows of no
  *                 prompt (before cu[0], from cu[n_seqs] on) are left as they were.  A prompt whose bounds are
  *                 not 0 <= cu[s] <= cu[s+1] <= total is skipped; prompts must not overlap.
- * Pointers 16-byte aligned, strides multiples of 8 elements.  Arithmetic: scores and sums fp32, the softmax numerators
+ * Pointers 16-byte aligned, strides multiples of 8 elements and at least head_dim (an axis of one entry may have any).
+ * Arithmetic: scores and sums fp32, the softmax numerators
  * enter the second product as bf16 (relative error 2^-8 at most, each on its own), one rounding to bf16 at the end.
  * Errors: INVALID_ARG (struct size, NULL, alignment, strides, sizes), UNSUPPORTED (head_dim, head counts as
  * amk_config's), CUDA.
@@ -397,7 +398,8 @@ amk_status amk_prompt_attention(const amk_prompt_args* args, char* msg, size_t m
  *   workspace     DEVICE, 256-byte aligned, at least amk_tree_workspace_bytes of the same arguments (pointers and strides
  *                 do not matter there) on the same device, NULL if that is 0; scratch, needs no initial value; two calls
  *                 that may overlap need one each
- * Pointers 16-byte aligned, strides multiples of 16 bytes.  Arithmetic as amk_prompt_attention's; over the 8-bit cache the
+ * Pointers 16-byte aligned, strides multiples of 16 bytes and at least head_dim elements (an axis of one entry may have
+ * any).  Arithmetic as amk_prompt_attention's; over the 8-bit cache the
  * softmax numerators are f16 (each off by 2^-11 of itself or 2^-34 of its row's largest, whichever is more), the codes
  * exact, and q exact but for values 2^-30 below its row's largest.
  * Errors as amk_prompt_attention.
@@ -466,6 +468,10 @@ amk_status amk_token_logprobs(const void* logits, uint32_t dtype, int64_t rows, 
  *   row base[c] + i  <-  old row keep[c][i],  i < count[c],
  * as if all were read before any is written.  After a draft is verified: keep = the accepted tokens' slots, base =
  * the context's length.  To drop the middle of a long context: keep = the slots to retain, base = where they go.
+ * Rows move as they are.  A K row of a decoder's cache carries the rotation of the position that it was written for, and
+ * amk_decode_step takes one position for rotation, slot and range: it can go on where every kept row's slot is that position,
+ * as it is behind accepted drafted tokens, not over a context without its middle.  There attention goes on with
+ * amk_tree_attention, whose queries and new rows come rotated: for their own positions, in the slots behind the kept ones.
  *   kv            DEVICE: n_caches caches of n_planes * max_seq * row_bytes contiguous bytes, cache_stride bytes apart
  *                 (a decoder's cache: n_planes = 2 * L * n_kv_heads, row_bytes = head_dim * element size)
  *   base, count   DEVICE int32 [n_caches];  keep  DEVICE int32 [n_caches][max_keep]

@@ -490,7 +490,8 @@ def amk_kv_compact(kv: torch.Tensor, base: torch.Tensor, keep: torch.Tensor, cou
     """In place: in every plane of every cache, row base[c] + i becomes what row keep[c][i] was, i < count[c].
     kv [n_caches][...][max_seq][hd] (cuda, each cache contiguous), base and count int32 [n_caches], keep int32
     [n_caches][max_keep], strictly ascending from at least base[c] over its first count[c] entries (a cache whose list is
-    not stays as it was)."""
+    not stays as it was).  K rows keep the rotation that they were written with: a cache that lost rows in its middle goes on
+    with amk_tree_attention (queries rotated for their true positions), not with the decode step."""
     name = "amk_kv_compact"
     if kv.dim() < 3:
         _refuse(name, "kv is [n_caches][...][max_seq][head_dim]")
@@ -633,7 +634,8 @@ class Decoder:
         return both[0], both[1]
 
     def amk_kv_compact(self, kv: torch.Tensor, base: torch.Tensor, keep: torch.Tensor, count: torch.Tensor) -> None:
-        """amk_kv_compact over this decoder's cache: base and count int32 [1], keep int32 [1][max_keep]."""
+        """amk_kv_compact over this decoder's cache: base and count int32 [1], keep int32 [1][max_keep].  ``amk_decode_step`` goes
+        on where each kept row's slot is the position that its K row was rotated for (accepted drafted tokens)."""
         s = self.shape
         amk_kv_compact(kv.view(1, 2 * s.n_layers * s.n_kv_heads, s.max_seq, s.head_dim), base, keep, count)
 

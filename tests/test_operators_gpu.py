@@ -1332,3 +1332,47 @@ def test_prompt_draft_verify_compact_and_decode(amk, name, kv_dtype):
         assert dec.amk_last_status()[0] == 0
         assert near(dec.logits, logits_ref[pos]) < tol_logits, pos
     dec.close()
+
+
+@pytest.mark.parametrize("name,kv_dtype", [("mini", "bf16"), ("mini_hd128", "bf16"), ("mini", "fp8")])
+def test_a_cache_without_its_middle_goes_on_with_the_tree_attention(amk, name, kv_dtype):
+    """The first tokens and a recent window of a decoder's cache, moved together: queries rotated for their true positions
+    attend to the kept rows and to the new ones behind them, as a plain attention over those rows does.
+    2e-2: one rounding of each attention's output to bf16 on either side (2^-8), and twice that of its numerators, through the
+    layers; the kept 8-bit rows are the same on both sides, and the three new ones differ by a step where a value lies next to
+    a border."""
+    shape = inp.SHAPES[name]
+    w = inp.make_weights(shape, 7, device=DEV, std=0.05, norm_jitter=0.1)
+    dec = amk.Decoder(shape, w, "bf16", kv_dtype=kv_dtype)
+    n, first, window, new = 60, 4, 21, 3
+    tokens = torch.randint(0, shape.vocab, (n + new,), generator=gen(4), device=DEV)
+    kv = dec.new_cache()
+    for pos in range(n):
+        dec.amk_decode_step(int(tokens[pos]), pos, kv)
+        assert dec.amk_last_status()[0] == 0
+    keep = list(range(first)) + list(range(n - window, n))
+    code = (lambda t: t.float().clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8)) if kv_dtype == "fp8" else (lambda t: t)
+    value = (lambda t: t.contiguous().view(torch.float8_e4m3fn).float()) if kv_dtype == "fp8" else (lambda t: t.float())
+    before = kv.clone()
+    Kb, Vb = (value(t)[:, :, keep] for t in dec.cache_views(before))
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)
+    dec.amk_kv_compact(kv, i32([0]), i32([keep]), i32([len(keep)]))
+    K, V = dec.cache_views(kv)
+    at, length = len(keep), i32([len(keep)])
+
+    def tree(l, q, k, v):
+        K[l, :, at:at + new], V[l, :, at:at + new] = code(k).permute(1, 0, 2), code(v).permute(1, 0, 2)
+        return amk.amk_tree_attention(q[None], K[l][None], V[l][None], length)[0]
+
+    def plain(l, q, k, v):
+        rep = shape.n_q_heads // shape.n_kv_heads
+        keys, values = (torch.cat([old[l], value(code(t)).permute(1, 0, 2)], 1).double().repeat_interleave(rep, 0)
+                        for old, t in ((Kb, k), (Vb, v)))
+        x = q.double().permute(1, 0, 2) @ keys.transpose(1, 2) * shape.head_dim ** -0.5
+        hidden = torch.ones(new, at + new, dtype=torch.bool, device=DEV).triu(at + 1)
+        return (torch.softmax(x.masked_fill(hidden, -math.inf), 2) @ values).permute(1, 0, 2).to(torch.bfloat16)
+
+    where = n + torch.arange(new, device=DEV)
+    got, want = forward(shape, w, tokens[n:], where, tree), forward(shape, w, tokens[n:], where, plain)
+    assert float((got - want).norm() / want.norm()) < 2e-2
+    dec.close()
