@@ -75,7 +75,7 @@ __device__ __forceinline__ float min3(float a, float b, float c) {
 // Logits below -kFar are masks, and no more than a few tokens of a row may be without one: nothing is raised for them, they
 // are 2^-kFar there.  A block whose part holds nothing else takes its sums again.  (600 rows of 128256, all but 1 in 1000 at -1e9, top 5:
 // fp32 55 us, bf16 43 us; with every thread's own far reference 80 and 70 us.)
-constexpr float kFar = 1048576.f, kHuge = 1.0e30f;
+constexpr float kFar = 1048576.f, kHuge = 1.0e30f, kLowest = -3.402823466e38f;
 __device__ __forceinline__ float ref(float r) { return r * kLog2e; }               // of an r below kFar
 __device__ __forceinline__ float eps(float r) { return fabsf(r) < kFar ? fmaf(r, kLog2e, -ref(r)) : 0.f; }
 struct Sums {
@@ -332,11 +332,12 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 5 : 3) logprobs_ker
   float most = red[3][0];                            // the block's maximum
 #pragma unroll
   for (int w = 1; w < kWarps; w++) most = fmaxf(most, red[3][w]);
-  if (most < -kFar && most > -CUDART_INF_F) {        // nothing but masks: the sums again, for that reference
-    Sums own{most, 0.f, 0.f};
+  if (most < -kFar) {                                // nothing but masks: the sums again, for that reference
+    Sums own{fmaxf(most, kLowest), 0.f, 0.f};        // (all of -infinity: sums of 0, below any other part's reference)
+    const int again = most > -CUDART_INF_F ? n : 0;
     if (rank == 0 && (int)threadIdx.x < head) own.add(load(x, threadIdx.x));
 #pragma unroll 1
-    for (int i = threadIdx.x; i < n; i += kThreads) {
+    for (int i = threadIdx.x; i < again; i += kThreads) {
       float v[kVec];
       widen(v, __ldg(v4 + i));
 #pragma unroll
@@ -346,7 +347,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 5 : 3) logprobs_ker
 #pragma unroll
     for (int o = 16; o; o /= 2) own.s += shfl_xor(own.s, o), own.t += shfl_xor(own.t, o);
     __syncthreads();                                 // (red[3] has been read)
-    if (lane == 0) red[0][warp] = most, red[1][warp] = own.s, red[2][warp] = own.t;
+    if (lane == 0) red[0][warp] = own.r, red[1][warp] = own.s, red[2][warp] = own.t;
     __syncthreads();
   }
   if (warp == 0) {

@@ -1007,6 +1007,30 @@ def test_logprobs_large_finite_logits(amk, dtype, rows, vocab):
             assert not bool(bad.any()), (at, a[bad][:4].tolist(), b[bad][:4].tolist())
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,vocab", [(1, 70), (70, 4980), (7, 128256), (600, 3001)])
+@pytest.mark.parametrize("low", [-1.5e6, -1e7, -5e9, -1e30, -3e38])
+def test_logprobs_low_logits_beside_minus_infinity(amk, dtype, rows, vocab, low):
+    """Rows of -infinity but for a few logits far below zero, which lie in one part of the row or in several: one, two equal
+    ones, and one with others far below it."""
+    g = gen(vocab)
+    x = torch.full((rows, vocab), -math.inf, device=DEV)
+    place = torch.stack([torch.randperm(vocab, generator=g, device=DEV)[:5] for _ in range(rows)])
+    for r in range(rows):
+        x[r, place[r, 0]] = low
+        if r % 3 == 1:
+            x[r, place[r, 1]] = low
+        if r % 3 == 2:
+            x[r, place[r, 2:]] = low * 1.06
+    x = x.to(dtype)
+    tokens = place[:, 0].to(torch.int32)
+    got, want = amk.amk_token_logprobs(x, tokens, 5), logprobs64(x, tokens, 5)
+    assert torch.equal(got[2].long(), want[2])
+    for a, b in ((got[0], want[0]), (got[1], want[1]), (got[3], want[3])):
+        tol = 2.0 ** -22 * (b.abs().nan_to_num(0, 0, 0) + 13) + 2.0 ** -21 + vocab * 2.0 ** -30
+        assert bool(((a.double() == b) | ((a.double() - b).abs() <= tol)).all())
+
+
 def test_logprobs_token_agrees_with_argmax_static_and_replays(amk):
     g = gen(2)
     x = randn(g, 4, 32000, dtype=torch.float32)
