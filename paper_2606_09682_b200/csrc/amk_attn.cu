@@ -152,15 +152,18 @@ void set_limits(AttnParams& p) {
 // How a tree call is divided: rows of a block, blocks, scratch.  Runs of equal length for all blocks and a second kernel that
 // joins the parts, or, in one launch and without scratch, for each item
 //  - a cluster of blocks with two tiles each, where it has few rows: the parts meet in distributed shared memory, which is
-//    slower than L2.  Clusters / runs, us a call in a graph: 8 rows of 64, 17 tiles 10.6 / 11.1; 16 rows of 128, 8 tiles
-//    13.3 / 13.3, over the 8-bit cache 16.2 / 16.8; 15 rows of 64, 4 tiles 10.3 / 11.0; but 32 rows of 128, 16 tiles
-//    13.7 / 13.1; 128 rows of 64, 4 tiles 14.6 / 11.6;
+//    slower than L2.  Clusters / runs, us a call in a graph: 4 items of 8 rows of 64, 17 tiles 10.6 / 12.0; 8 items of 16 rows of
+//    128, 8 tiles 12.0 / 13.7, over the 8-bit cache 15.0 / 16.4; 3 items of 15 rows of 64, 4 tiles 10.4 / 11.7.  At the limit of
+//    rows runs are not better yet (8 items of 32 rows of 128, 16 tiles 13.2 / 14.1), at 128 rows they are (8 items of 64, 4
+//    tiles 12.5 / 12.3);
 //  - one block, where its tiles (and three for its beginning and end) are no more than its share of the runs and six to ten
-//    more, which is what the second kernel and the parts' way through memory cost.  One block / runs: 128 items of 128 rows of 128, 4 tiles 18.2 / 22.5, 12 tiles
-//    32.1 / 43.3; 64 items of 128 rows of 64, 8 tiles 15.7 / 19.1; 32 items of 128 rows of 128, 6 tiles 16.8 / 18.1, 12 tiles
-//    22.2 / 20.3; 8 items, 4 tiles 15.0 / 14.7; over the 8-bit cache 128 items, 8 tiles 26.8 / 42.1; 32 items, 4 tiles
-//    19.1 / 20.2, 6 tiles 21.9 / 20.8.  The lengths may be anything below the bound that is known here, and the longest
-//    decides for single blocks, the sum for runs: no further than 12 tiles.
+//    more, which is what the second kernel and the parts' way through memory cost.  One block / runs: 128 items of 128 rows of
+//    128, 4 tiles 15.1 / 27.0, 12 tiles 30.1 / 42.3; 64 items of 128 rows of 64, 8 tiles 14.9 / 18.9; 32 items of 128 rows of 128,
+//    4 tiles 14.6 / 18.6; over the 8-bit cache 128 items, 8 tiles 24.9 / 40.1; 32 items, 4 tiles 18.8 / 22.4.  Beyond the limit: 32
+//    items, 6 tiles 16.4 / 18.8 (runs a little early), 9 tiles 18.8 / 20.0, 12 tiles 21.5 / 20.4, over the 8-bit cache 9 tiles
+//    25.7 / 24.5; 8 items, 4 tiles 14.3 / 15.0, 6 tiles 16.1 / 15.0.  The lengths may be anything below the bound that is known
+//    here, and the longest decides for single blocks, the sum for runs: no further than 12 tiles (128 full items of 16 tiles
+//    would be 36.5 / 49.0).
 struct TreePlan {
   int part_rows, row_tiles, cluster;
   unsigned blocks;

@@ -13,12 +13,13 @@
 // make the softmax, so that one tile's exponentials run beside the other's products.  Prompts: units of 256 / rep tokens of
 // a kv head, one for each block of the grid; a block that runs takes over the units of blocks that have not begun while its
 // own last tiles are on their way (one unit a block: 468 us at 8192 tokens, 41 us for eight prompts of 1 to 1291 tokens; so:
-// 440 and 35 us).  Trees: the key tiles of the whole batch in equal runs (below), parts joined by a second kernel.
+// 445 and 35 us).  Trees: the key tiles of the whole batch in equal runs (below), parts joined by a second kernel.
 //
 // What bounds it.  Prompts: the chain scores -> softmax -> products of a tile, about 3500 cycles for 2054 cycles of products a
-// pair of tiles (the exponentials alone are 2048): 8192 tokens, 32 heads of 128 on 8, 550 GFLOP in 440 us = 1.25 PFLOP/s.
+// pair of tiles (the exponentials alone are 2048): 8192 tokens, 32 heads of 128 on 8, 550 GFLOP in 445 us = 1.24 PFLOP/s for one
+// launch; in a row of calls, under the power cap, 514 us = 1.07 PFLOP/s.
 // head_dim 64 has half the products for the same exponentials.  Trees: HBM in long runs (32 sequences of 8000 positions,
-// one token each: 1.05 GB in 168 us = 6.2 TB/s); a short call the 8 us that a cold block takes from its start to its first
+// one token each: 1.05 GB in 178 us a call = 5.9 TB/s); a short call the 8 us that a cold block takes from its start to its first
 // output, of which the tiles are the least.  The 8-bit cache: its tiles' way through shared memory (raw in, f16 out, read
 // as operands).
 // Registers are what this kernel is short of: a spilled one is fetched from L2 behind the stream of tiles (shared memory

@@ -143,9 +143,11 @@ __device__ __forceinline__ K merge_warps(K v, K (*buf)[32], int warp, int lane) 
   return v;
 }
 
-// C blocks a row.  Blocks on an SM: 5 for fp32, 3 for bf16 (its 32 values at a time need the registers; measured with 2001
-// rows of 128256: 5 blocks 192 us, 4 119 us, 3 96 us; 600 fp32 rows: 3 blocks 59 us, 4 65 us, 5 52 us).  Of a block's part, thread f has the 16-byte pieces f, f + 256, ...; the first block's threads also one
-// element each in front of the first piece, the last block's one behind the last.
+// C blocks a row.  Blocks on an SM: 5 for fp32, 3 for bf16, whose 32 values at a time need the registers.  (Without alternatives /
+// with 5 / with 20 of them: 2001 bf16 rows of 128256, 5 blocks 187 / 201 / 228 us, 4 122 / 139 / 164 us, 3 94 / 111 / 132 us; 600
+// fp32 rows, 3 blocks 59 / 69 / 84 us, 4 64 / 74 / 92 us, 5 50 / 57 / 72 us.)  Of a block's part, thread f has the 16-byte pieces
+// f, f + 256, ...; the first block's threads also one element each in front of the first piece, the last block's one behind
+// the last.
 template <class T>
 __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 5 : 3) logprobs_kernel(const T* __restrict__ logits, const Args a, int C) {
   constexpr int kVec = 16 / sizeof(T);
@@ -431,9 +433,9 @@ extern "C" amk_status amk_token_logprobs(const void* logits, uint32_t dtype, int
       !amk::aligned(entropy, 4) || !amk::aligned(top_tokens, 4) || !amk::aligned(top_logprobs, 4))
     return fail(AMK_ERR_INVALID_ARG, "pointers must be aligned to their elements");
   const Args a{vocab, row_stride, tokens, (int)top_k, logprob, entropy, top_tokens, top_logprobs};
-  // Blocks a row: doubled until there are two for each SM, while a block keeps 2048 logits.  (Top 20 of fp32
-  // logits, 1 / 2 / 4 / 8 blocks a row: one row of 32000 9.9 / 9.3 / 9.1 / 10.3 us, 64 of 128256 25 / 17 / 14 / 17 us, 200 of
-  // 128256 40 / 28 / 34 / 49 us.)
+  // Blocks a row: doubled until there are two for each SM, while a block keeps 2048 logits.  (fp32 logits, calls in a row, top 5 /
+  // top 20, 1, 2, 4 and 8 blocks a row: one row of 32000 8.1 / 9.7, 8.0 / 9.6, 8.8 / 10.3, 10.6 / 12.2 us; 64 of 128256 25.4 / 29.0,
+  // 17.7 / 20.2, 15.3 / 17.3, 17.1 / 19.5 us; 200 of 128256 31.8 / 37.2, 25.4 / 29.1, 35.9 / 40.5, 47.5 / 54.8 us.)
   int dev = 0, sms = 148, C = 1;
   if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
     (void)cudaGetLastError();
