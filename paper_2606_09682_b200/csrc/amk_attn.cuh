@@ -182,7 +182,8 @@ struct AttnHead {
   int dead;                            // a bounded wait ran out: nobody waits or issues any more
   unsigned wait_cycles;
   int skip[2];                         // this step's P V was done by the warpgroup itself
-  float mx[2][2][kTile];               // [tile][half]: row maxima, and at the end row sums, of half the columns
+  float mx[2][2][kTile];               // [tile][half]: row maxima, and at the end row sums, of half the columns; last, in a
+                                       // cluster, [0]: the part's maxima and sums
   float m[kTile], l[kTile];            // the second tile's statistics (both tiles of the same rows)
   int unit[8];                         // where the block's work begins; behind it what the producer had asked for at its end
   uint64_t unit_full[kUnitRing], unit_empty[kUnitRing], next_full;   // prompts: blocks of queries, taken one after the other
