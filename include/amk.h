@@ -484,6 +484,179 @@ amk_status amk_kv_compact(void* kv, int64_t n_caches, int64_t cache_stride, int6
                           int64_t row_bytes, const int32_t* base, const int32_t* keep, int64_t max_keep,
                           const int32_t* count, char* msg, size_t msg_bytes, void* cuda_stream);
 
+/*
+ * New rows of q, k and v on their way from the projection to the attention and the cache (one layer), in one pass: queries and
+ * keys normed for each head where a weight is given, both rotated to their positions, the rotated keys and the values stored in
+ * their cache rows.  For a head x of head_dim elements at position n:
+ *   y = x w / sqrt(mean x^2 + eps)  (y = x without a weight);
+ *   z[i] = y[i] cos a - y[i+hd/2] sin a,  z[i+hd/2] = y[i+hd/2] cos a + y[i] sin a,  a = n theta^(-2i/hd),  i < hd/2,
+ * the decode step's pairs and angles (rms_eps and rope_theta of amk_config); values are stored as they are.
+ *   q, k, v       DEVICE bf16: row (token), head and element; rows and heads at the given strides (elements), elements
+ *                 contiguous.  The three may be slices of one fused projection.  v may be NULL without a cache.
+ *   q_weight, k_weight   DEVICE bf16 [head_dim], 16-byte aligned, or NULL: no norm
+ *   positions     DEVICE int32 [rows], any value
+ *   slots         DEVICE int64 [rows]: sequence * n_slots + row of the cache where the token's K and V go.  A token whose slot is
+ *                 not one of the n_seqs * n_slots (-1, say) is not stored.  Slots must be distinct.
+ *   k_cache, v_cache   DEVICE, kv_dtype: [n_seqs][n_kv_heads][n_slots][head_dim] at the given strides (elements of that type)
+ *                 as amk_tree_attention reads them; both or neither (then slots is not read).  Only the tokens' rows are written.
+ *   q_out         DEVICE bf16, rows and heads at the given strides; may be q itself at the same strides
+ *   k_out         DEVICE bf16, or NULL: the rotated keys as amk_prompt_attention takes them; may be k itself at the same strides
+ * Outputs must not overlap otherwise, neither each other nor an input.
+ * Arithmetic: fp32, angles from 64 bits, each result rounded once (to nearest even; e4m3 saturates at 448, as the step's cache).
+ * Pointers 16-byte aligned (positions 4, slots 8), strides multiples of 16 bytes and at least head_dim elements (an axis of one
+ * entry may have any).
+ * Errors: INVALID_ARG (struct size, NULL, alignment, strides, sizes, eps, theta), UNSUPPORTED (head_dim, kv_dtype, head counts), CUDA.
+ */
+typedef struct amk_rope_args {
+  uint32_t struct_size;      /* = sizeof(amk_rope_args)                                                */
+  uint32_t head_dim;         /* 64 or 128                                                              */
+  uint32_t n_q_heads;        /* 1 .. 4096                                                              */
+  uint32_t n_kv_heads;       /* 1 .. 4096                                                              */
+  uint32_t kv_dtype;         /* amk_kvdtype                                                            */
+  uint32_t n_seqs;           /* caches                                                                 */
+  uint32_t n_slots;          /* rows of a cache                                                        */
+  float eps;                 /* >= 0, finite                                                           */
+  float theta;               /* > 0, finite                                                            */
+  uint32_t reserved;         /* 0                                                                      */
+  int64_t rows;              /* tokens; below 2^31                                                     */
+  const void* q;
+  const void* k;
+  const void* v;
+  const void* q_weight;
+  const void* k_weight;
+  const int32_t* positions;
+  const int64_t* slots;
+  void* q_out;
+  void* k_out;
+  void* k_cache;
+  void* v_cache;
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head, qo_row, qo_head, ko_row, ko_head; /* strides, elements */
+  int64_t kc_seq, kc_head, kc_row, vc_seq, vc_head, vc_row;
+} amk_rope_args;
+amk_status amk_norm_rope_append(const amk_rope_args* args, char* msg, size_t msg_bytes, void* cuda_stream);
+
+/*
+ * Attention weights of cached positions (one layer): how much the queries of some tokens attend to each position, added up for
+ * each kv head over the tokens and the query heads that share it,
+ *   out[s][g][j] = decay * before[s][g][j] (j < len) + sum over i < n_rows, h in group g of exp(scale q[s][i][h] . k[s][g][j] - lse[s][i][h]),
+ * where token i, whose own row lies in slot len + i, attends to the slots j <= len + i; 0 for j >= len + n_rows.  The tokens of a
+ * whole prompt (len = 0), the last ones of a context, or the one that was just decoded; lse as the attentions leave it.  What
+ * falls behind in these sums can leave the cache: amk_evict_select.
+ *   q             DEVICE bf16 [n_seqs][n_rows][n_q_heads][head_dim] at the given strides (elements)
+ *   k             DEVICE, kv_dtype: one layer of the cache as amk_tree_attention reads it; only rows [0, len + n_rows) are read for
+ *                 their values
+ *   lse           DEVICE float [n_seqs][n_rows][n_q_heads], natural logarithms.  A row of -infinity (or +infinity) adds
+ *                 nothing, whatever its query: so a padded token is left out.  NaN makes what the row attends to NaN.
+ *   cache_len     DEVICE int32 [n_seqs]: len.  A sequence whose len is not 0 <= len <= n_slots - n_rows gets NaN in all of out.
+ *   before        DEVICE float [n_seqs][n_kv_heads][n_slots], sequences and heads at the given strides, or NULL: 0.  Only
+ *                 slots below len are used; not read where decay is 0.
+ *   out           DEVICE float, like before at strides of its own; all n_slots are written.  May be before itself at the same
+ *                 strides, must not overlap anything else.
+ *   workspace     DEVICE, 256-byte aligned, at least amk_attention_weights_workspace_bytes of the same arguments (pointers and
+ *                 strides do not matter there) on the same device, NULL if that is 0; scratch, needs no initial value; two
+ *                 calls that may overlap need one each
+ * NaN or infinity in a K row reaches only its own position.  Pointers 16-byte aligned (lse, before, out and cache_len 4), strides
+ * of q and k multiples of 16 bytes and at least head_dim elements, of before and out at least n_slots (an axis of one entry may
+ * have any).  Arithmetic: scores, exponentials and sums fp32, sums in a fixed order.
+ * Errors as amk_tree_attention.
+ */
+typedef struct amk_attention_weights_args {
+  uint32_t struct_size;      /* = sizeof(amk_attention_weights_args)                                   */
+  uint32_t head_dim;         /* 64 or 128                                                              */
+  uint32_t n_q_heads;        /* multiple of n_kv_heads; n_q_heads / n_kv_heads <= 16; at most 4096     */
+  uint32_t n_kv_heads;
+  uint32_t kv_dtype;         /* amk_kvdtype                                                            */
+  uint32_t n_seqs;
+  uint32_t n_rows;           /* tokens per sequence, at least 1                                        */
+  uint32_t n_slots;          /* rows of the cache                                                      */
+  float scale;               /* > 0 and scale log2 e finite, or 0: 1 / sqrt(head_dim)                  */
+  float decay;               /* finite                                                                 */
+  const void* q;
+  const void* k;
+  const float* lse;
+  const int32_t* cache_len;
+  const float* before;
+  float* out;
+  void* workspace;
+  uint64_t workspace_bytes;
+  int64_t q_seq, q_row, q_head, k_seq, k_head, k_row, before_seq, before_head, out_seq, out_head;
+} amk_attention_weights_args;
+amk_status amk_attention_weights_workspace_bytes(const amk_attention_weights_args* args, size_t* bytes, char* msg, size_t msg_bytes);
+amk_status amk_attention_weights(const amk_attention_weights_args* args, char* msg, size_t msg_bytes, void* cuda_stream);
+
+/*
+ * Which positions of a cache stay: of each list of scores (one for a kv head of a sequence, amk_attention_weights' output, say)
+ * the first `first` positions, the last `recent` ones and the heaviest of those between, `budget` in all; of equal scores the
+ * one with the lower index; all of a list that is no longer than the budget.  Written as amk_kv_compact takes them (base 0; a
+ * cache's K as n_seqs * n_heads caches of one plane, and its V likewise).
+ *   scores        DEVICE float [n_seqs][n_heads][n_slots], sequences and heads at the given strides (elements)
+ *   lens          DEVICE int32 [n_seqs]: positions that count, 0 .. n_slots.  A sequence of another length gets count -1 (which
+ *                 amk_kv_compact leaves alone) and its scores copied as they are.
+ *   keep          DEVICE int32 [n_seqs][n_heads][budget]: the positions that stay, ascending; -1 behind the last
+ *   count         DEVICE int32 [n_seqs][n_heads]: how many they are, min(len, budget)
+ *   moved         DEVICE float, like scores at strides of its own, or NULL: scores[keep[i]] at i < count, 0 behind.  May be
+ *                 scores itself at the same strides; must not overlap them otherwise.
+ * NaN is less than every number (-infinity too); 0 and -0 are equal.
+ * Errors: INVALID_ARG (NULL, alignment, sizes, strides below n_slots, first + recent > budget, budget outside 1 .. n_slots), CUDA.
+ */
+amk_status amk_evict_select(const float* scores, int64_t n_seqs, int64_t n_heads, int64_t n_slots, int64_t scores_seq,
+                            int64_t scores_head, const int32_t* lens, int64_t budget, int64_t first, int64_t recent,
+                            int32_t* keep, int32_t* count, float* moved, int64_t moved_seq, int64_t moved_head, char* msg,
+                            size_t msg_bytes, void* cuda_stream);
+
+/*
+ * Verification of drafted tokens, from given uniform numbers, so that what is accepted and drawn has the target's distribution.
+ * Each of n_seqs sequences has n_rows nodes, the rows of amk_tree_attention: node 0 is the token that is already chosen (always
+ * kept), nodes 1 .. n_rows - 1 are drafted, each below its parent.  With p(t) = softmax(logits[node] / temperature)(t), the walk
+ * begins at node 0 with r = p of its row and takes the node's children in the order of their indices:
+ *   child c, token t: accepted if u[c] q(t) < r(t), q the distribution that it was drawn from (draft[parent]; without draft
+ *     1 at t, a guess).  The walk goes on at c with the p of c's row.
+ *   otherwise r <- max(r - q, 0) / (its sum); where that sum is 0, r stays.
+ * Where no child is accepted, the next token is drawn from r: the first t whose sum of r(0..t) is more than u[0] times the sum of
+ * all (the last t with r(t) > 0 if rounding leaves none).  temperature 0: p is 1 at the first largest logit.
+ *   logits        DEVICE float (dtype 0) or bf16 (dtype 1) [n_seqs][n_rows][vocab], sequences and rows at the given strides
+ *                 (elements); any alignment of the element type.  -infinity has probability 0.
+ *   draft         DEVICE float [n_seqs][n_rows][vocab] at the given strides, or NULL; the rows of nodes without children are
+ *                 not read.  Numbers >= 0.
+ *   tokens        DEVICE int32 [n_seqs][n_rows]; tokens[..][0] is not read.  A drafted token outside [0, vocab) is passed over.
+ *   parents       DEVICE int32 [n_seqs][n_rows], or NULL: a chain, the parent of i is i - 1.  A node whose parent is not
+ *                 0 <= parent < node is passed over; parents[..][0] is not read.
+ *   uniforms      DEVICE float [n_seqs][n_rows], numbers in [0, 1): [0] draws the next token, [i] decides node i
+ *   temperature   DEVICE float [n_seqs], or NULL: 1
+ *   cache_len     DEVICE int32 [n_seqs], or NULL: 0.  Added to the kept nodes' indices: their slots in the cache
+ *   count, keep   DEVICE int32 [n_seqs] and [n_seqs][n_rows]: kept nodes, and cache_len + node in ascending order, -1 behind the
+ *                 last: count and keep of amk_kv_compact with base = cache_len
+ *   token         DEVICE int32 [n_seqs]: the next token; -1 where there is no distribution to draw it from (NaN among the
+ *                 logits of the row reached, a maximum of +infinity, nothing but -infinity, or a temperature that is not a
+ *                 finite number >= 0): nothing below that node is accepted then
+ *   workspace     DEVICE, 256-byte aligned, at least amk_verify_workspace_bytes of the same arguments, NULL if that is 0;
+ *                 scratch, needs no initial value; two calls that may overlap need one each
+ * Arithmetic: decisions and draws as in 64 bits (sums in 32 bits decide only where their error cannot change the answer).
+ * Errors: INVALID_ARG (struct size, NULL, alignment, sizes, strides), UNSUPPORTED (dtype, n_rows), CUDA.
+ */
+typedef struct amk_verify_args {
+  uint32_t struct_size;      /* = sizeof(amk_verify_args)                                              */
+  uint32_t dtype;            /* 0: float, 1: bf16                                                      */
+  uint32_t n_seqs;
+  uint32_t n_rows;           /* 1 .. AMK_TREE_MAX_ROWS                                                 */
+  int64_t vocab;             /* below 2^31 - 65536                                                     */
+  const void* logits;
+  const float* draft;
+  const int32_t* tokens;
+  const int32_t* parents;
+  const float* uniforms;
+  const float* temperature;
+  const int32_t* cache_len;
+  int32_t* count;
+  int32_t* keep;
+  int32_t* token;
+  void* workspace;
+  uint64_t workspace_bytes;
+  int64_t logits_seq, logits_row, draft_seq, draft_row; /* strides, elements                            */
+} amk_verify_args;
+amk_status amk_verify_workspace_bytes(const amk_verify_args* args, size_t* bytes, char* msg, size_t msg_bytes);
+amk_status amk_verify_draft(const amk_verify_args* args, char* msg, size_t msg_bytes, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -74,9 +74,38 @@ class amk_tree_args(C.Structure):
                                  "out_seq", "out_row", "out_head")]
 
 
-# the same two structs as struct formats: packing one costs a microsecond, filling a ctypes structure several
+class amk_rope_args(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("struct_size", "head_dim", "n_q_heads", "n_kv_heads", "kv_dtype", "n_seqs",
+                                          "n_slots")] + [("eps", C.c_float), ("theta", C.c_float), ("reserved", C.c_uint32),
+                                                         ("rows", C.c_int64)] + [
+        (n, C.c_void_p) for n in ("q", "k", "v", "q_weight", "k_weight", "positions", "slots", "q_out", "k_out", "k_cache",
+                                  "v_cache")] + [
+        (n, C.c_int64) for n in ("q_row", "q_head", "k_row", "k_head", "v_row", "v_head", "qo_row", "qo_head", "ko_row",
+                                 "ko_head", "kc_seq", "kc_head", "kc_row", "vc_seq", "vc_head", "vc_row")]
+
+
+class amk_attention_weights_args(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("struct_size", "head_dim", "n_q_heads", "n_kv_heads", "kv_dtype", "n_seqs",
+                                          "n_rows", "n_slots")] + [("scale", C.c_float), ("decay", C.c_float)] + [
+        (n, C.c_void_p) for n in ("q", "k", "lse", "cache_len", "before", "out", "workspace")] + [
+        ("workspace_bytes", C.c_uint64)] + [
+        (n, C.c_int64) for n in ("q_seq", "q_row", "q_head", "k_seq", "k_head", "k_row", "before_seq", "before_head",
+                                 "out_seq", "out_head")]
+
+
+class amk_verify_args(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("struct_size", "dtype", "n_seqs", "n_rows")] + [("vocab", C.c_int64)] + [
+        (n, C.c_void_p) for n in ("logits", "draft", "tokens", "parents", "uniforms", "temperature", "cache_len", "count",
+                                  "keep", "token", "workspace")] + [("workspace_bytes", C.c_uint64)] + [
+        (n, C.c_int64) for n in ("logits_seq", "logits_row", "draft_seq", "draft_row")]
+
+
+# the operators' structs as struct formats: packing one costs a microsecond, filling a ctypes structure several
 _PROMPT = struct.Struct("@5Ifq6P8q")
 _TREE = struct.Struct("@9If8PQ12q")
+_ROPE = struct.Struct("@7IffIq11P16q")
+_WEIGHTS = struct.Struct("@8Iff7PQ10q")
+_VERIFY = struct.Struct("@4Iq11PQ4q")
 _F32 = struct.Struct("@f")
 
 
@@ -116,6 +145,12 @@ def _load() -> C.CDLL:
         "amk_token_logprobs": (C.c_int, [vp, C.c_uint32, i64, i64, i64, vp, C.c_uint32, vp, vp, vp, vp, C.c_char_p, sz,
                                          vp]),
         "amk_kv_compact": (C.c_int, [vp, i64, i64, i64, i64, i64, vp, vp, i64, vp, C.c_char_p, sz, vp]),
+        "amk_norm_rope_append": (C.c_int, [C.c_char_p, C.c_char_p, sz, vp]),
+        "amk_attention_weights_workspace_bytes": (C.c_int, [C.c_char_p, C.POINTER(sz), C.c_char_p, sz]),
+        "amk_attention_weights": (C.c_int, [C.c_char_p, C.c_char_p, sz, vp]),
+        "amk_evict_select": (C.c_int, [vp, i64, i64, i64, i64, i64, vp, i64, i64, i64, vp, vp, vp, i64, i64, C.c_char_p, sz, vp]),
+        "amk_verify_workspace_bytes": (C.c_int, [C.c_char_p, C.POINTER(sz), C.c_char_p, sz]),
+        "amk_verify_draft": (C.c_int, [C.c_char_p, C.c_char_p, sz, vp]),
         "amk_plan_export": (C.c_int, [C.POINTER(amk_config), vp, sz, C.POINTER(sz)]),
         "amk_plan_check": (C.c_int, [C.POINTER(amk_config), vp, sz, C.c_char_p, sz]),
     }
@@ -132,7 +167,8 @@ EXPORTS = ("amk_status_str", "amk_packed_bytes", "amk_workspace_bytes", "amk_kv_
            "amk_argmax_static", "amk_plan_export", "amk_plan_check",
            "amk_prompt_attention", "amk_tree_workspace_bytes", "amk_tree_attention", "amk_operator_status",
            "amk_debug_operator_wait", "amk_token_logprobs",
-           "amk_kv_compact")
+           "amk_kv_compact", "amk_norm_rope_append", "amk_attention_weights_workspace_bytes", "amk_attention_weights",
+           "amk_evict_select", "amk_verify_workspace_bytes", "amk_verify_draft")
 
 
 class _Nothing:
@@ -288,6 +324,14 @@ def _scale(name: str, scale: Optional[float]) -> float:
     if not 0.0 < held < float("inf"):
         _refuse(name, f"scale {scale} must be positive and finite in fp32")
     return held
+
+
+def _f32(name: str, what: str, x: float) -> float:
+    """x as the struct's fp32 holds it; what fp32 cannot hold is refused (NaN is the library's to refuse)."""
+    try:
+        return _F32.unpack(_F32.pack(x))[0]
+    except OverflowError:
+        _refuse(name, f"{what} {x} must be finite in fp32")
 
 
 def _device_of(name: str, first: torch.Tensor, *others) -> int:
@@ -510,6 +554,230 @@ def amk_kv_compact(kv: torch.Tensor, base: torch.Tensor, keep: torch.Tensor, cou
         _refuse(name, "each cache must be contiguous")
     _run(lib.amk_kv_compact, name, dev, kv.data_ptr(), caches, kv.stride(0) * esz, total // (caches * slots * elements), slots,
          elements * esz, base.data_ptr(), keep.data_ptr(), keep.shape[1], count.data_ptr())
+
+
+_CACHE_TYPES = (torch.bfloat16, torch.uint8, torch.float8_e4m3fn)
+_NO_CACHE = (0,) * 6
+
+
+def amk_norm_rope_append(q: torch.Tensor, k: torch.Tensor, v: Optional[torch.Tensor], positions: torch.Tensor,
+                         k_cache: Optional[torch.Tensor] = None, v_cache: Optional[torch.Tensor] = None,
+                         slots: Optional[torch.Tensor] = None, q_weight: Optional[torch.Tensor] = None,
+                         k_weight: Optional[torch.Tensor] = None, eps: float = 1e-5, theta: float = 10000.0,
+                         q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """New rows q [rows][n_q][hd], k, v [rows][n_kv][hd] (bf16, any row and head strides): heads of q and k normed where a weight
+    (bf16 [hd]) is given, rotated to ``positions`` (int32 [rows]); the keys and values stored in ``k_cache``, ``v_cache``
+    ([n_seqs][n_kv][n_slots][hd], bf16, or e4m3 as uint8 / float8_e4m3fn) at ``slots`` (int64 [rows], sequence * n_slots + row; -1:
+    not stored).  Returns the rotated queries, ``q_out`` if given (q itself may be); the rotated keys are also left in ``k_out``
+    if given.  Without caches v may be None."""
+    name = "amk_norm_rope_append"
+    if q.dim() != 3 or k.dim() != 3 or (v is not None and v.dim() != 3):
+        _refuse(name, "q, k and v are [rows][heads][head_dim]")
+    rows, nq, hd = shape = q.shape
+    kshape = k.shape
+    nkv = kshape[1]
+    dev = _device_of(name, q, k, v, positions, k_cache, v_cache, slots, q_weight, k_weight, q_out, k_out)
+    bf16 = torch.bfloat16
+    if q.dtype is not bf16 or k.dtype is not bf16 or (v is not None and v.dtype is not bf16):
+        _refuse(name, "q, k and v are bf16")
+    if kshape[0] != rows or kshape[2] != hd or (v is not None and v.shape != kshape):
+        _refuse(name, "shapes of q, k and v do not fit")
+    if positions.dtype is not torch.int32 or positions.shape != (rows,) or not positions.is_contiguous():
+        _refuse(name, "positions is a contiguous int32 vector with an entry for each row")
+    for w in (q_weight, k_weight):
+        if w is not None and (w.dtype is not bf16 or w.shape != (hd,) or not w.is_contiguous()):
+            _refuse(name, "weights are contiguous bf16 vectors of head_dim")
+    if q_out is None:
+        q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    elif q_out.shape != shape or q_out.dtype is not bf16:
+        _refuse(name, "q_out is bf16 of q's shape")
+    if k_out is not None and (k_out.shape != kshape or k_out.dtype is not bf16):
+        _refuse(name, "k_out is bf16 of k's shape")
+    (qr, qh, q1), (kr, kh, k1), (outr, outh, out1) = q.stride(), k.stride(), q_out.stride()
+    vr = vh = kor = koh = 0
+    v1 = ko1 = 1
+    if v is not None:
+        vr, vh, v1 = v.stride()
+    if k_out is not None:
+        kor, koh, ko1 = k_out.stride()
+    seqs, n_slots, kind, caches, where = 0, 0, AMK_KV_BF16, _NO_CACHE, 0
+    if k_cache is not None or v_cache is not None:
+        if k_cache is None or v_cache is None or v is None or slots is None:
+            _refuse(name, "k_cache and v_cache come together, with v and slots")
+        if k_cache.dim() != 4 or k_cache.shape != v_cache.shape or k_cache.shape[1] != nkv or k_cache.shape[3] != hd:
+            _refuse(name, "the caches are [n_seqs][n_kv][n_slots][head_dim]")
+        if k_cache.dtype is not v_cache.dtype or k_cache.dtype not in _CACHE_TYPES:
+            _refuse(name, "the caches are bf16, or e4m3 as uint8 or float8_e4m3fn")
+        if slots.dtype is not torch.int64 or slots.shape != (rows,) or not slots.is_contiguous():
+            _refuse(name, "slots is a contiguous int64 vector with an entry for each row")
+        seqs, n_slots = k_cache.shape[0], k_cache.shape[2]
+        kind = AMK_KV_BF16 if k_cache.dtype is bf16 else AMK_KV_FP8_E4M3
+        (cs, ch, cr, c1), (ds, dh, dr, d1) = k_cache.stride(), v_cache.stride()
+        if c1 != 1 or d1 != 1:
+            _refuse(name, "the last dimension must be contiguous")
+        caches, where = (cs, ch, cr, ds, dh, dr), slots.data_ptr()
+    if not (q1 == k1 == v1 == out1 == ko1 == 1):
+        _refuse(name, "the last dimension must be contiguous")
+    args = _ROPE.pack(_ROPE.size, hd, nq, nkv, kind, seqs, n_slots, _f32(name, "eps", eps), _f32(name, "theta", theta), 0, rows,
+                      q.data_ptr(), k.data_ptr(), 0 if v is None else v.data_ptr(),
+                      0 if q_weight is None else q_weight.data_ptr(), 0 if k_weight is None else k_weight.data_ptr(),
+                      positions.data_ptr(), where, q_out.data_ptr(), 0 if k_out is None else k_out.data_ptr(),
+                      0 if k_cache is None else k_cache.data_ptr(), 0 if v_cache is None else v_cache.data_ptr(),
+                      qr, qh, kr, kh, vr, vh, outr, outh, kor, koh, *caches)
+    _run(lib.amk_norm_rope_append, name, dev, args)
+    return q_out
+
+
+_scratch_bytes: Dict = {}                             # of the weights and the verification, by device and shape
+
+
+def _scratch(name: str, fn, dev: int, like: torch.Tensor, given: Optional[torch.Tensor], key, packed):
+    """(workspace or None, its bytes) of a call; ``packed()`` gives the struct that the library is asked with."""
+    if given is not None:
+        if not given.is_contiguous():
+            _refuse(name, "the workspace must be contiguous")
+        return given, given.numel() * given.element_size()
+    key = (name, dev, key)
+    need = _scratch_bytes.get(key)
+    if need is None:
+        n = C.c_size_t()
+        msg = C.create_string_buffer(256)
+        with torch.cuda.device(dev):
+            code = fn(packed(), C.byref(n), msg, 256)
+        if code != AMK_OK:
+            raise AmkError(code, msg.value.decode() or name)
+        if len(_scratch_bytes) >= 4096:
+            _scratch_bytes.clear()
+        need = _scratch_bytes[key] = n.value
+    return (torch.empty(need, dtype=torch.uint8, device=like.device) if need else None), need
+
+
+def amk_attention_weights(q: torch.Tensor, k: torch.Tensor, lse: torch.Tensor, cache_len: torch.Tensor,
+                          before: Optional[torch.Tensor] = None, decay: float = 1.0, scale: Optional[float] = None,
+                          out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """What the queries q [n_seqs][rows][n_q][hd] (bf16) attend to in one layer of a cache, k [n_seqs][n_kv][slots][hd] (bf16, or
+    e4m3 as uint8 / float8_e4m3fn), added up over tokens and the heads of a group: fp32 [n_seqs][n_kv][slots].  Token i's own row
+    lies in slot cache_len + i, and it attends to the slots up to there; ``lse`` (fp32 [n_seqs][rows][n_q]) as the attentions
+    leave it, -infinity for a token to be left out.  ``before``, weighed by ``decay``, is added for slots below cache_len; ``out`` may
+    be ``before`` itself."""
+    name = "amk_attention_weights"
+    if q.dim() != 4 or k.dim() != 4:
+        _refuse(name, "q and k have four dimensions")
+    seqs, rows, nq, hd = q.shape
+    kseqs, nkv, slots, khd = k.shape
+    dev = _device_of(name, q, k, lse, cache_len, before, out, workspace)
+    if q.dtype is not torch.bfloat16:
+        _refuse(name, "q is bf16")
+    if k.dtype not in _CACHE_TYPES:
+        _refuse(name, "the cache is bf16, or e4m3 as uint8 or float8_e4m3fn")
+    if kseqs != seqs or khd != hd:
+        _refuse(name, "shapes of q and k do not fit")
+    if lse.dtype is not torch.float32 or lse.shape != (seqs, rows, nq) or not lse.is_contiguous():
+        _refuse(name, "lse is contiguous fp32 [n_seqs][rows][n_q]")
+    if cache_len.dtype is not torch.int32 or cache_len.shape != (seqs,) or not cache_len.is_contiguous():
+        _refuse(name, "cache_len is a contiguous int32 vector with an entry for each sequence")
+    shape = (seqs, nkv, slots)
+    if out is None:
+        out = torch.empty(shape, dtype=torch.float32, device=q.device)
+    elif out.shape != shape or out.dtype is not torch.float32:
+        _refuse(name, "out is fp32 [n_seqs][n_kv][slots]")
+    bs = bh = 0
+    b1 = 1
+    if before is not None:
+        if before.shape != shape or before.dtype is not torch.float32:
+            _refuse(name, "before is fp32 [n_seqs][n_kv][slots]")
+        bs, bh, b1 = before.stride()
+    (qs, qr, qh, q1), (ks, kh, kr, k1), (os_, oh, o1) = q.stride(), k.stride(), out.stride()
+    if not (q1 == k1 == 1) or (slots > 1 and not (o1 == b1 == 1)):
+        _refuse(name, "the last dimension must be contiguous")
+    plan = (_WEIGHTS.size, hd, nq, nkv, AMK_KV_BF16 if k.dtype is torch.bfloat16 else AMK_KV_FP8_E4M3, seqs, rows, slots,
+            _scale(name, scale), _f32(name, "decay", decay))
+    workspace, have = _scratch(name, lib.amk_attention_weights_workspace_bytes, dev, q, workspace, plan,
+                               lambda: _WEIGHTS.pack(*plan, *(0,) * 18))
+    args = _WEIGHTS.pack(*plan, q.data_ptr(), k.data_ptr(), lse.data_ptr(), cache_len.data_ptr(),
+                         0 if before is None else before.data_ptr(), out.data_ptr(),
+                         0 if workspace is None else workspace.data_ptr(), have, qs, qr, qh, ks, kh, kr, bs, bh, os_, oh)
+    _run(lib.amk_attention_weights, name, dev, args)
+    return out
+
+
+def amk_evict_select(scores: torch.Tensor, lens: torch.Tensor, budget: int, first: int = 0, recent: int = 0,
+                     moved: Optional[torch.Tensor] = None):
+    """Which positions of a cache stay: of scores [n_seqs][n_heads][n_slots] (fp32) over lens (int32 [n_seqs]) positions the first
+    ``first``, the last ``recent`` and the heaviest others, ``budget`` in all.  Returns (keep int32 [n_seqs][n_heads][budget],
+    ascending, -1 behind the last; count int32 [n_seqs][n_heads]; the scores of the kept positions moved together, of scores'
+    shape, 0 behind: ``moved`` if given, which may be scores itself).  Lists for ``amk_kv_compact`` with base 0: a cache's K
+    [n_seqs][n_heads][n_slots][hd] as n_seqs * n_heads caches of one plane, and its V likewise."""
+    name = "amk_evict_select"
+    if scores.dim() != 3:
+        _refuse(name, "scores are [n_seqs][n_heads][n_slots]")
+    seqs, heads, slots = shape = scores.shape
+    dev = _device_of(name, scores, lens, moved)
+    if scores.dtype is not torch.float32:
+        _refuse(name, "scores are fp32")
+    if lens.dtype is not torch.int32 or lens.shape != (seqs,) or not lens.is_contiguous():
+        _refuse(name, "lens is a contiguous int32 vector with an entry for each sequence")
+    if not 1 <= budget <= slots:
+        _refuse(name, f"budget {budget}: 1 to the slots")
+    if moved is None:
+        moved = torch.empty(shape, dtype=torch.float32, device=scores.device)
+    elif moved.shape != shape or moved.dtype is not torch.float32:
+        _refuse(name, "moved is fp32 of scores' shape")
+    (ss, sh, s1), (ms, mh, m1) = scores.stride(), moved.stride()
+    if slots > 1 and not (s1 == m1 == 1):
+        _refuse(name, "the last dimension must be contiguous")
+    keep = torch.empty(seqs, heads, budget, dtype=torch.int32, device=scores.device)
+    count = torch.empty(seqs, heads, dtype=torch.int32, device=scores.device)
+    _run(lib.amk_evict_select, name, dev, scores.data_ptr(), seqs, heads, slots, ss, sh, lens.data_ptr(), budget, first, recent,
+         keep.data_ptr(), count.data_ptr(), moved.data_ptr(), ms, mh)
+    return keep, count, moved
+
+
+def amk_verify_draft(logits: torch.Tensor, tokens: torch.Tensor, uniforms: torch.Tensor,
+                     parents: Optional[torch.Tensor] = None, draft: Optional[torch.Tensor] = None,
+                     temperature: Optional[torch.Tensor] = None, cache_len: Optional[torch.Tensor] = None,
+                     workspace: Optional[torch.Tensor] = None):
+    """Drafted tokens accepted or rejected, and the next one drawn: logits [n_seqs][rows][vocab] (fp32 or bf16) as the target gives
+    them for the rows of ``amk_tree_attention``, row 0 the token that is already chosen; tokens int32 [n_seqs][rows]; uniforms
+    fp32 [n_seqs][rows] in [0, 1), the first for the draw, the others for their nodes; parents int32 [n_seqs][rows], None: a
+    chain; ``draft`` fp32 [n_seqs][rows][vocab]: the probabilities that a node's children were drawn from, None: guesses;
+    temperature fp32 [n_seqs], None: 1, 0: greedy; cache_len int32 [n_seqs], None: 0.  Returns (count int32 [n_seqs], keep int32
+    [n_seqs][rows]: cache_len + kept nodes, -1 behind them, token int32 [n_seqs], -1 where there is none): count and keep for
+    ``amk_kv_compact`` with base = cache_len."""
+    name = "amk_verify_draft"
+    if logits.dim() != 3:
+        _refuse(name, "logits are [n_seqs][rows][vocab]")
+    seqs, rows, vocab = shape = logits.shape
+    dev = _device_of(name, logits, tokens, uniforms, parents, draft, temperature, cache_len, workspace)
+    if logits.dtype is not torch.float32 and logits.dtype is not torch.bfloat16:
+        _refuse(name, "logits are fp32 or bf16")
+    for what, t, dtype, size in (("tokens", tokens, torch.int32, (seqs, rows)), ("uniforms", uniforms, torch.float32, (seqs, rows)),
+                                 ("parents", parents, torch.int32, (seqs, rows)),
+                                 ("temperature", temperature, torch.float32, (seqs,)),
+                                 ("cache_len", cache_len, torch.int32, (seqs,))):
+        if t is not None and (t.dtype is not dtype or t.shape != size or not t.is_contiguous()):
+            _refuse(name, f"{what} is contiguous {dtype} of shape {tuple(size)}")
+    ls, lr, l1 = logits.stride()
+    ds = dr = 0
+    d1 = 1
+    if draft is not None:
+        if draft.shape != shape or draft.dtype is not torch.float32:
+            _refuse(name, "draft is fp32 of the logits' shape")
+        ds, dr, d1 = draft.stride()
+    if vocab > 1 and not (l1 == d1 == 1):
+        _refuse(name, "the last dimension must be contiguous")
+    plan = (_VERIFY.size, 1 if logits.dtype is torch.bfloat16 else 0, seqs, rows, vocab)
+    workspace, have = _scratch(name, lib.amk_verify_workspace_bytes, dev, logits, workspace, plan,
+                               lambda: _VERIFY.pack(*plan, *(0,) * 16))
+    count = torch.empty(seqs, dtype=torch.int32, device=logits.device)
+    keep = torch.empty(seqs, rows, dtype=torch.int32, device=logits.device)
+    token = torch.empty_like(count)
+    ptr = lambda t: 0 if t is None else t.data_ptr()
+    args = _VERIFY.pack(*plan, logits.data_ptr(), ptr(draft), tokens.data_ptr(), ptr(parents), uniforms.data_ptr(),
+                        ptr(temperature), ptr(cache_len), count.data_ptr(), keep.data_ptr(), token.data_ptr(), ptr(workspace),
+                        have, ls, lr, ds, dr)
+    _run(lib.amk_verify_draft, name, dev, args)
+    return count, keep, token
 
 
 def quantize_weights(weights: Dict, wdtype: str) -> Dict:

@@ -1,4 +1,4 @@
-// amk_prompt_attention and amk_tree_attention: argument checks and launches.
+// amk_prompt_attention, amk_tree_attention and amk_attention_weights: argument checks and launches.
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <math.h>
@@ -6,6 +6,8 @@
 #include <atomic>
 
 #include "amk_attn.cuh"
+#include "amk_attn_weights.cuh"
+#include "amk_op_launch.h"
 #include "amk_op_util.h"
 
 namespace {
@@ -248,6 +250,24 @@ amk_status check_tree(const Reason& fail, const amk_tree_args* a) {
   return AMK_OK;
 }
 
+// Everything about a call of the weights that can be known without its data.
+amk_status check_weights(const Reason& fail, const amk_attention_weights_args* a) {
+  if (!a) return fail(AMK_ERR_INVALID_ARG, "NULL arguments");
+  if (a->struct_size != sizeof *a)
+    return fail(AMK_ERR_INVALID_ARG, "struct_size %u, the library has %zu", a->struct_size, sizeof *a);
+  AMK_TRY(check_heads(fail, a->head_dim, a->n_q_heads, a->n_kv_heads, a->scale));
+  if (a->kv_dtype > AMK_KV_FP8_E4M3) return fail(AMK_ERR_UNSUPPORTED, "kv_dtype %u", a->kv_dtype);
+  if (!(fabsf(a->decay) < INFINITY)) return fail(AMK_ERR_INVALID_ARG, "decay must be finite");
+  if (a->n_rows < 1 || a->n_slots < a->n_rows || a->n_slots > 0x7fffffff - 1024)
+    return fail(AMK_ERR_INVALID_ARG, "%u slots for %u tokens", a->n_slots, a->n_rows);
+  if (a->n_seqs > 65535) return fail(AMK_ERR_UNSUPPORTED, "%u sequences: at most 65535", a->n_seqs);
+  // (tiles hold whole tokens: 64 rows at least)
+  if ((a->n_slots / (double)amk::kTile + 2) * a->n_kv_heads * a->n_seqs * (a->n_rows * (a->n_q_heads / a->n_kv_heads) / 64.0 + 1) > 0x7fffffff)
+    return fail(AMK_ERR_UNSUPPORTED, "%u sequences of %u tokens over %u slots: more than 2^31 pieces of work", a->n_seqs, a->n_rows,
+                a->n_slots);
+  return AMK_OK;
+}
+
 }  // namespace
 
 extern "C" amk_status amk_prompt_attention(const amk_prompt_args* args, char* msg, size_t msg_bytes,
@@ -382,5 +402,56 @@ extern "C" amk_status amk_tree_attention(const amk_tree_args* args, char* msg, s
   else
     e = fp8 ? launch_attn<128, true, true>(p, mk, mv, t.blocks, st) : launch_attn<128, true, false>(p, mk, mv, t.blocks, st);
   if (e == cudaSuccess && !t.cluster) e = hd == 64 ? launch_join<64>(p, t.blocks, st) : launch_join<128>(p, t.blocks, st);
+  return e == cudaSuccess ? AMK_OK : fail(AMK_ERR_CUDA, "launch failed: %s", cudaGetErrorString(e));
+}
+
+extern "C" amk_status amk_attention_weights_workspace_bytes(const amk_attention_weights_args* args, size_t* bytes, char* msg,
+                                                            size_t msg_bytes) {
+  const Reason fail(msg, msg_bytes, "amk_attention_weights_workspace_bytes");
+  if (!bytes) return fail(AMK_ERR_INVALID_ARG, "NULL pointer");
+  AMK_TRY(check_weights(fail, args));
+  *bytes = 0;
+  return AMK_OK;
+}
+
+extern "C" amk_status amk_attention_weights(const amk_attention_weights_args* args, char* msg, size_t msg_bytes,
+                                            void* cuda_stream) {
+  const Reason fail(msg, msg_bytes, "amk_attention_weights");
+  AMK_TRY(check_weights(fail, args));
+  amk_attention_weights_args a = *args;
+  if (a.n_seqs == 0) return AMK_OK;
+  if (a.decay == 0.f) a.before = nullptr;
+  if (!a.q || !a.k || !a.lse || !a.cache_len || !a.out) return fail(AMK_ERR_INVALID_ARG, "NULL pointer");
+  if (!amk::aligned(a.q, 16) || !amk::aligned(a.k, 16) || !amk::aligned(a.lse, 4) || !amk::aligned(a.cache_len, 4) ||
+      !amk::aligned(a.before, 4) || !amk::aligned(a.out, 4) || !amk::aligned(a.workspace, 256))
+    return fail(AMK_ERR_INVALID_ARG, "q and k must be 16-byte, lse, cache_len, before and out 4-byte, workspace 256-byte aligned");
+  const int64_t hd = a.head_dim;
+  const int esz = a.kv_dtype == AMK_KV_FP8_E4M3 ? 1 : 2;
+  AMK_TRY(check_stride(fail, "q sequence", a.n_seqs, &a.q_seq, hd, 2));
+  AMK_TRY(check_stride(fail, "q row", a.n_rows, &a.q_row, hd, 2));
+  AMK_TRY(check_stride(fail, "q head", a.n_q_heads, &a.q_head, hd, 2));
+  AMK_TRY(check_stride(fail, "k sequence", a.n_seqs, &a.k_seq, hd, esz));
+  AMK_TRY(check_stride(fail, "k head", a.n_kv_heads, &a.k_head, hd, esz));
+  AMK_TRY(check_stride(fail, "k row", a.n_slots, &a.k_row, hd, esz));
+  int64_t* sums[] = {&a.out_seq, &a.out_head, &a.before_seq, &a.before_head};
+  for (int i = 0; i < (a.before ? 4 : 2); i++) {
+    if ((i & 1 ? a.n_kv_heads : a.n_seqs) <= 1) *sums[i] = a.n_slots;
+    if (*sums[i] < a.n_slots || *sums[i] > (int64_t)1 << 36)
+      return fail(AMK_ERR_INVALID_ARG, "stride %lld of the sums: at least the %u slots", (long long)*sums[i], a.n_slots);
+  }
+  if (a.before == a.out && (a.before_seq != a.out_seq || a.before_head != a.out_head))
+    return fail(AMK_ERR_INVALID_ARG, "out is before, but at other strides");
+  amk::WeightsParams p{};
+  p.q = (const unsigned short*)a.q, p.k = a.k, p.lse = a.lse, p.lens = a.cache_len, p.before = a.before, p.out = a.out;
+  p.q_seq = a.q_seq, p.q_row = a.q_row, p.q_head = a.q_head, p.k_seq = a.k_seq, p.k_head = a.k_head, p.k_row = a.k_row;
+  p.b_seq = a.before_seq, p.b_head = a.before_head, p.o_seq = a.out_seq, p.o_head = a.out_head;
+  p.n_seqs = (int)a.n_seqs, p.nq = (int)a.n_q_heads, p.nkv = (int)a.n_kv_heads, p.rep = p.nq / p.nkv;
+  p.rows = (int)a.n_rows, p.slots = (int)a.n_slots;
+  p.scale = a.scale > 0.f ? a.scale : 1.f / sqrtf((float)hd), p.decay = a.decay;
+  const dim3 grid((a.n_slots + amk::kTile - 1) / amk::kTile, a.n_kv_heads, a.n_seqs);
+  const cudaStream_t st = (cudaStream_t)cuda_stream;
+  const auto kernel = hd == 64 ? (esz == 1 ? amk::weights_kernel<64, true> : amk::weights_kernel<64, false>)
+                               : (esz == 1 ? amk::weights_kernel<128, true> : amk::weights_kernel<128, false>);
+  const cudaError_t e = amk::launch_early(kernel, grid, amk::kTile, 0, 1, st, p);
   return e == cudaSuccess ? AMK_OK : fail(AMK_ERR_CUDA, "launch failed: %s", cudaGetErrorString(e));
 }

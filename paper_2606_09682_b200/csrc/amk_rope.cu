@@ -1,0 +1,245 @@
+// amk_norm_rope_append: heads normed, rotated and stored, one pass over new rows of q, k and v.
+//
+// Mathematics.  A lane holds eight elements i .. i+7 of a head and the eight i + hd/2 .. that they are rotated with, so that
+// only the norm's sum crosses lanes.  The angle of pair i at position n is n theta^(-2i/hd); in turns, n f_i with
+// f_i = theta^(-2i/hd) / 2 pi, it is made in 64 bits, its whole turns taken off, and only then rounded to fp32: off by 2^-25 of
+// a turn at most, at any position.  The eight angles of a lane are those of every head of its token.
+//
+// Bound: HBM, each element once in and once out.  A warp takes the heads of one token, or, with few tokens, a share of them.
+#include <cuda_bf16.h>
+#include <math.h>
+
+#include "amk.h"
+#include "amk_op_launch.h"
+#include "amk_op_util.h"
+#include "amk_ptx.cuh"
+
+namespace {
+
+using amk::Reason;
+
+struct RopeParams {
+  const unsigned short *q, *k, *v;
+  const uint4 *q_weight, *k_weight;
+  const int* positions;
+  const int64_t* slots;
+  unsigned short *q_out, *k_out;
+  void *k_cache, *v_cache;
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head, qo_row, qo_head, ko_row, ko_head;
+  int64_t kc_seq, kc_head, kc_row, vc_seq, vc_head, vc_row;
+  int64_t rows, all_slots;
+  int nq, nkv, heads;              // heads: of q, of k and, with a cache, of v
+  unsigned slots_of;               // rows of a cache
+  int split;                       // warps that share a token
+  float eps;
+  double turns[64];                // f_i
+};
+
+constexpr int kThreads = 256;
+
+__device__ __forceinline__ unsigned pack_bf16(float lo, float hi) {
+  unsigned r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ unsigned pack_e4m3(float a, float b, float c, float d) {
+  unsigned r;
+  asm("{ .reg .b16 l, h; cvt.rn.satfinite.e4m3x2.f32 l, %2, %1; cvt.rn.satfinite.e4m3x2.f32 h, %4, %3; mov.b32 %0, {l, h}; }"
+      : "=r"(r)
+      : "f"(a), "f"(b), "f"(c), "f"(d));
+  return r;
+}
+__device__ __forceinline__ void widen(float (&x)[8], const uint4& u) {
+  const unsigned w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int i = 0; i < 4; i++) x[2 * i] = amk::bf16_lo(w[i]), x[2 * i + 1] = amk::bf16_hi(w[i]);
+}
+__device__ __forceinline__ uint4 narrow(const float (&x)[8]) {
+  return make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+}
+// eight elements of a cache row from element i on
+template <bool FP8>
+__device__ __forceinline__ void store(void* cache, int64_t at, const float (&x)[8]) {
+  if (FP8)
+    *(uint2*)((unsigned char*)cache + at) = make_uint2(pack_e4m3(x[0], x[1], x[2], x[3]), pack_e4m3(x[4], x[5], x[6], x[7]));
+  else
+    *(uint4*)((unsigned short*)cache + at) = narrow(x);
+}
+
+template <int HD, bool FP8>
+__global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ RopeParams p) {
+  constexpr int kLanes = HD / 16, kGroups = 32 / kLanes, kOwn = 8 / kGroups;   // lanes of a head, heads of a warp, angles a lane makes
+  constexpr int kBatch = 4;                                                    // heads under way, times kGroups
+  const int lane = threadIdx.x & 31, l = lane % kLanes, g = lane / kLanes;
+  const int64_t w = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
+  const int64_t row = p.split == 1 ? w : w / p.split;
+  const int part = (int)(w - row * p.split);
+  amk::wait_for_grid_before();
+  if (row >= p.rows) return;
+  float c[8], s[8];
+  {
+    const double n = (double)p.positions[row];
+    float cc[kOwn], ss[kOwn];
+#pragma unroll
+    for (int j = 0; j < kOwn; j++) {
+      double t = n * p.turns[8 * l + g * kOwn + j];
+      t -= rint(t);
+      sincospif(2.f * (float)t, &ss[j], &cc[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; j++) {
+      c[j] = __shfl_sync(~0u, cc[j % kOwn], j / kOwn * kLanes + l);
+      s[j] = __shfl_sync(~0u, ss[j % kOwn], j / kOwn * kLanes + l);
+    }
+  }
+  int64_t kc = -1, vc = 0;                             // the token's row in the caches
+  if (p.k_cache) {
+    const int64_t slot = p.slots[row];
+    if (slot >= 0 && slot < p.all_slots) {
+      const int64_t seq = p.all_slots <= 0xffffffffll ? (unsigned)slot / p.slots_of : slot / p.slots_of;
+      const int64_t at = slot - seq * p.slots_of;
+      kc = seq * p.kc_seq + at * p.kc_row, vc = seq * p.vc_seq + at * p.vc_row;
+    }
+  }
+  const int e = 8 * l;
+  for (int h0 = part * kGroups + g; h0 - g < p.heads; h0 += kBatch * p.split * kGroups) {
+    uint4 lo[kBatch], hi[kBatch];
+#pragma unroll
+    for (int b = 0; b < kBatch; b++) {
+      const int h = h0 + b * p.split * kGroups;
+      lo[b] = hi[b] = make_uint4(0, 0, 0, 0);
+      if (h < p.heads) {
+        const unsigned short* x = h < p.nq              ? p.q + row * p.q_row + h * p.q_head
+                                  : h < p.nq + p.nkv ? p.k + row * p.k_row + (h - p.nq) * p.k_head
+                                                     : p.v + row * p.v_row + (h - p.nq - p.nkv) * p.v_head;
+        lo[b] = *(const uint4*)(x + e), hi[b] = *(const uint4*)(x + HD / 2 + e);
+      }
+    }
+#pragma unroll
+    for (int b = 0; b < kBatch; b++) {
+      const int h = h0 + b * p.split * kGroups;
+      if (h - g >= p.heads) break;
+      float x[8], y[8];
+      widen(x, lo[b]), widen(y, hi[b]);
+      if (h - g < p.nq + p.nkv && (p.q_weight || p.k_weight)) {
+        float sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; j++) sum = fmaf(x[j], x[j], fmaf(y[j], y[j], sum));
+#pragma unroll
+        for (int o = kLanes / 2; o; o /= 2) sum += __shfl_xor_sync(~0u, sum, o);
+        const uint4* weight = h < p.nq ? p.q_weight : h < p.nq + p.nkv ? p.k_weight : nullptr;
+        if (weight) {
+          const float f = 1.f / sqrtf(fmaf(sum, 1.f / HD, p.eps));
+          float wx[8], wy[8];
+          widen(wx, __ldg(weight + l)), widen(wy, __ldg(weight + HD / 16 + l));
+#pragma unroll
+          for (int j = 0; j < 8; j++) x[j] *= f * wx[j], y[j] *= f * wy[j];
+        }
+      }
+      if (h >= p.heads) continue;
+      if (h < p.nq + p.nkv) {
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+          const float a = x[j], d = y[j];
+          x[j] = fmaf(a, c[j], -(d * s[j]));
+          y[j] = fmaf(d, c[j], a * s[j]);
+        }
+        unsigned short* out = h < p.nq ? p.q_out + row * p.qo_row + h * p.qo_head
+                                       : p.k_out ? p.k_out + row * p.ko_row + (h - p.nq) * p.ko_head : nullptr;
+        if (out) *(uint4*)(out + e) = narrow(x), *(uint4*)(out + HD / 2 + e) = narrow(y);
+        if (h >= p.nq && kc >= 0) {
+          const int64_t at = kc + (h - p.nq) * p.kc_head + e;
+          store<FP8>(p.k_cache, at, x), store<FP8>(p.k_cache, at + HD / 2, y);
+        }
+      } else if (kc >= 0) {
+        const int64_t at = vc + (h - p.nq - p.nkv) * p.vc_head + e;
+        if (FP8) {
+          store<FP8>(p.v_cache, at, x), store<FP8>(p.v_cache, at + HD / 2, y);
+        } else {                                       // (the bits as they are)
+          *(uint4*)((unsigned short*)p.v_cache + at) = lo[b];
+          *(uint4*)((unsigned short*)p.v_cache + at + HD / 2) = hi[b];
+        }
+      }
+    }
+  }
+}
+
+// A stride (elements) of an axis of n entries, as the attentions': any will do for one entry.
+amk_status check_stride(const Reason& fail, const char* what, int64_t n, int64_t* stride, int64_t least, int esz) {
+  if (n <= 1) {
+    *stride = least;
+    return AMK_OK;
+  }
+  if (*stride < least || *stride % (16 / esz) || *stride > (int64_t)1 << 36)
+    return fail(AMK_ERR_INVALID_ARG, "%s stride %lld: a multiple of 16 bytes, at least %lld elements", what, (long long)*stride,
+                (long long)least);
+  return AMK_OK;
+}
+
+}  // namespace
+
+extern "C" amk_status amk_norm_rope_append(const amk_rope_args* args, char* msg, size_t msg_bytes, void* cuda_stream) {
+  const Reason fail(msg, msg_bytes, "amk_norm_rope_append");
+  if (!args) return fail(AMK_ERR_INVALID_ARG, "NULL arguments");
+  amk_rope_args a = *args;
+  if (a.struct_size != sizeof a)
+    return fail(AMK_ERR_INVALID_ARG, "struct_size %u, the library has %zu", a.struct_size, sizeof a);
+  if (a.reserved) return fail(AMK_ERR_INVALID_ARG, "reserved is %u, not 0", a.reserved);
+  if (a.head_dim != 64 && a.head_dim != 128) return fail(AMK_ERR_UNSUPPORTED, "head_dim %u: 64 or 128", a.head_dim);
+  if (!a.n_q_heads || !a.n_kv_heads || a.n_q_heads > 4096 || a.n_kv_heads > 4096)
+    return fail(AMK_ERR_UNSUPPORTED, "%u query heads and %u kv heads: 1 to 4096", a.n_q_heads, a.n_kv_heads);
+  if (a.kv_dtype > AMK_KV_FP8_E4M3) return fail(AMK_ERR_UNSUPPORTED, "kv_dtype %u", a.kv_dtype);
+  if (!(a.eps >= 0.f) || isinf(a.eps)) return fail(AMK_ERR_INVALID_ARG, "eps must be at least 0 and finite");
+  if (!(a.theta > 0.f) || isinf(a.theta)) return fail(AMK_ERR_INVALID_ARG, "theta must be positive and finite");
+  if (a.rows < 0 || a.rows > 0x7fffffff - 1024) return fail(AMK_ERR_INVALID_ARG, "%lld rows", (long long)a.rows);
+  const bool cached = a.k_cache != nullptr;
+  if (cached != (a.v_cache != nullptr)) return fail(AMK_ERR_INVALID_ARG, "k_cache and v_cache: both or neither");
+  if (cached && (!a.n_seqs || !a.n_slots || a.n_slots > 0x7fffffff))
+    return fail(AMK_ERR_INVALID_ARG, "%u caches of %u rows", a.n_seqs, a.n_slots);
+  if (a.rows == 0) return AMK_OK;
+  if (!a.q || !a.k || !a.positions || !a.q_out || (cached && (!a.v || !a.slots))) return fail(AMK_ERR_INVALID_ARG, "NULL pointer");
+  const void* vec[] = {a.q, a.k, a.v, a.q_weight, a.k_weight, a.q_out, a.k_out, a.k_cache, a.v_cache};
+  for (const void* p : vec)
+    if (!amk::aligned(p, 16)) return fail(AMK_ERR_INVALID_ARG, "q, k, v, weights, outputs and caches must be 16-byte aligned");
+  if (!amk::aligned(a.positions, 4) || !amk::aligned(a.slots, 8))
+    return fail(AMK_ERR_INVALID_ARG, "positions must be 4-byte, slots 8-byte aligned");
+  const int64_t hd = a.head_dim, nq = a.n_q_heads, nkv = a.n_kv_heads;
+  const int esz = a.kv_dtype == AMK_KV_FP8_E4M3 ? 1 : 2;
+  struct { const char* what; int64_t n, *stride; int esz; bool used; } strides[] = {
+      {"q row", a.rows, &a.q_row, 2, true}, {"q head", nq, &a.q_head, 2, true},
+      {"k row", a.rows, &a.k_row, 2, true}, {"k head", nkv, &a.k_head, 2, true},
+      {"v row", a.rows, &a.v_row, 2, cached}, {"v head", nkv, &a.v_head, 2, cached},
+      {"q_out row", a.rows, &a.qo_row, 2, true}, {"q_out head", nq, &a.qo_head, 2, true},
+      {"k_out row", a.rows, &a.ko_row, 2, a.k_out != nullptr}, {"k_out head", nkv, &a.ko_head, 2, a.k_out != nullptr},
+      {"k_cache sequence", a.n_seqs, &a.kc_seq, esz, cached}, {"k_cache head", nkv, &a.kc_head, esz, cached},
+      {"k_cache row", a.n_slots, &a.kc_row, esz, cached}, {"v_cache sequence", a.n_seqs, &a.vc_seq, esz, cached},
+      {"v_cache head", nkv, &a.vc_head, esz, cached}, {"v_cache row", a.n_slots, &a.vc_row, esz, cached}};
+  for (const auto& s : strides)
+    if (s.used) {
+      const amk_status st = check_stride(fail, s.what, s.n, s.stride, hd, s.esz);
+      if (st != AMK_OK) return st;
+    }
+  RopeParams p{};
+  p.q = (const unsigned short*)a.q, p.k = (const unsigned short*)a.k, p.v = (const unsigned short*)a.v;
+  p.q_weight = (const uint4*)a.q_weight, p.k_weight = (const uint4*)a.k_weight;
+  p.positions = a.positions, p.slots = a.slots;
+  p.q_out = (unsigned short*)a.q_out, p.k_out = (unsigned short*)a.k_out, p.k_cache = a.k_cache, p.v_cache = a.v_cache;
+  p.q_row = a.q_row, p.q_head = a.q_head, p.k_row = a.k_row, p.k_head = a.k_head, p.v_row = a.v_row, p.v_head = a.v_head;
+  p.qo_row = a.qo_row, p.qo_head = a.qo_head, p.ko_row = a.ko_row, p.ko_head = a.ko_head;
+  p.kc_seq = a.kc_seq, p.kc_head = a.kc_head, p.kc_row = a.kc_row, p.vc_seq = a.vc_seq, p.vc_head = a.vc_head, p.vc_row = a.vc_row;
+  p.rows = a.rows, p.all_slots = cached ? (int64_t)a.n_seqs * a.n_slots : 0, p.slots_of = a.n_slots;
+  p.nq = (int)nq, p.nkv = (int)nkv, p.heads = (int)(nq + nkv + (cached ? nkv : 0));
+  p.eps = a.eps;
+  const long double step = powl((long double)a.theta, -2.0L / hd);
+  long double f = 0.15915494309189533576888376337251436L;               // 1 / 2 pi
+  for (int i = 0; i < hd / 2; i++, f *= step) p.turns[i] = (double)f;
+  // a token's heads over several warps until there are 32 warps for each SM
+  const int64_t steps = (p.heads + 512 / hd - 1) / (512 / hd), want = (32ll * amk::multiprocessors() + a.rows - 1) / a.rows;
+  p.split = (int)(steps < want ? steps : want);
+  const int64_t blocks = (a.rows * p.split + kThreads / 32 - 1) / (kThreads / 32);
+  const cudaStream_t st = (cudaStream_t)cuda_stream;
+  const auto kernel = hd == 64 ? (esz == 1 ? rope_kernel<64, true> : rope_kernel<64, false>)
+                               : (esz == 1 ? rope_kernel<128, true> : rope_kernel<128, false>);
+  const cudaError_t e = amk::launch_early(kernel, dim3((unsigned)blocks), kThreads, 0, 1, st, p);
+  return e == cudaSuccess ? AMK_OK : fail(AMK_ERR_CUDA, "launch failed: %s", cudaGetErrorString(e));
+}

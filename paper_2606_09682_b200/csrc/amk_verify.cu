@@ -1,0 +1,508 @@
+// amk_verify_draft: drafted tokens accepted or rejected against the target's probabilities, and the next token drawn.
+//
+// Mathematics.  With e(t) = exp((x(t) - m) / T) for a row's logits x and maximum m, the weights of the walk's state are
+//   v_0 = e,  v_{k+1} = max(v_k / S_k - q, 0),  S_k = sum of v_k
+// after k rejected children (guesses: v_k is e without the rejected tokens), r = v_k / S_k.  A child is accepted if
+// u q < v_k / S_k; the token drawn is the first whose running sum of v_k is more than u[0] S_k.
+//
+// Which rows the walk reaches is known only as it goes, and each needs its S_0.  So a first kernel takes the maximum and the sum of
+// every row in 32 bits, all rows at once at the memory's rate, and a second one, a cluster of blocks for each sequence, walks
+// on those numbers alone: a decision nearer than their error (kNear) is taken again with the sum in 64 bits.  Only a row where
+// a child is rejected or a token drawn is read again (from L2), in 64 bits throughout: the border between two tokens of a
+// vocabulary of 10^5 lies within the error of 32 bits in one draw of a hundred.
+//
+// Bound: HBM in the first kernel (each row once); in the second latency, one pass over a row for each state that is needed, two or
+// three microseconds each.
+#include <cuda_runtime.h>
+#include <math_constants.h>
+
+#include <atomic>
+
+#include "amk.h"
+#include "amk_op_launch.h"
+#include "amk_op_util.h"
+#include "amk_ptx.cuh"
+
+namespace {
+
+using namespace amk;
+
+constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kEach = 32;                              // logits a thread of the first kernel has
+constexpr int kPart = kThreads * kEach;                // ... and a block
+constexpr float kLog2e = 1.4426950408889634f;
+// A row's sum in 32 bits: an exponent y = (x - m) log2 e / T is off by 2^-23 |y|, its power by 2^-23 |y| ln 2 of itself (less than
+// 2^-24 32 for the terms that count) and 2^-22, additions by less than 2^-19 together: 2^-17.
+constexpr double kNear = 1.0 / 65536;
+
+struct Stat {
+  float m, s;                                          // a row's (or a part's) maximum, and sum of exp((x - m) / T)
+  int first;                                           // temperature 0: the first index of the maximum
+  int pad;
+};
+
+struct VerifyParams {
+  const void* logits;
+  const float* draft;
+  const int *tokens, *parents;
+  const float *u, *temperature;
+  const int* cache_len;
+  int *count, *keep, *token;
+  Stat* stats;                                         // [n_seqs * rows][parts]
+  int64_t l_seq, l_row, d_seq, d_row;
+  int rows, vocab, parts, cluster;
+};
+
+__device__ __forceinline__ float load(const float* x, int64_t i) { return __ldg(x + i); }
+__device__ __forceinline__ float load(const unsigned short* x, int64_t i) { return __uint_as_float((unsigned)__ldg(x + i) << 16); }
+template <class T>
+__device__ __forceinline__ float element(const uint4& u, int k) {
+  const unsigned w = sizeof(T) == 4 ? (&u.x)[k] : (&u.x)[k / 2];
+  return sizeof(T) == 4 ? __uint_as_float(w) : k & 1 ? bf16_hi(w) : bf16_lo(w);
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+  return d;
+}
+
+// ---- the rows' maxima and sums ----------------------------------------------------------------------------------
+// A block has 16384 consecutive places of a row, counted from the 16-byte boundary at or in front of its first logit, and holds
+// them in registers.
+template <class T>
+__global__ void __launch_bounds__(kThreads) stats_kernel(const VerifyParams p) {
+  constexpr int kVec = 16 / sizeof(T), kLoads = kEach / kVec;
+  __shared__ float red[kWarps];
+  __shared__ int red_i[kWarps];
+  const int64_t r = blockIdx.x / p.parts;
+  const int part = (int)(blockIdx.x - r * p.parts);
+  const int64_t s = r / p.rows, i = r - s * p.rows;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const T* x = (const T*)p.logits + s * p.l_seq + i * p.l_row;
+  const int skew = (int)((uintptr_t)x / sizeof(T) % kVec);
+  const uint4* x4 = (const uint4*)(x - skew);
+  const int begin = part * kPart + (int)threadIdx.x * kVec - skew;         // this thread's first place, as an index of the row
+  wait_for_grid_before();
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const float t = p.temperature ? p.temperature[s] : 1.f;
+  uint4 v[kLoads];
+  float m = -CUDART_INF_F;
+  const unsigned nothing = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;     // -infinity
+#pragma unroll
+  for (int j = 0; j < kLoads; j++) {
+    const int at = begin + j * kThreads * kVec;
+    v[j] = make_uint4(nothing, nothing, nothing, nothing);
+    if (at >= 0 && at + kVec <= p.vocab) {
+      v[j] = __ldg(x4 + (at + skew) / kVec);
+    } else if (at > -kVec && at < p.vocab) {
+#pragma unroll
+      for (int k = 0; k < kVec; k++)
+        if (at + k >= 0 && at + k < p.vocab) {
+          if (sizeof(T) == 4) {
+            (&v[j].x)[k] = __float_as_uint(load(x, at + k));
+          } else {
+            const unsigned w = __float_as_uint(load(x, at + k)) >> 16;
+            (&v[j].x)[k / 2] = k & 1 ? ((&v[j].x)[k / 2] & 0xffffu) | w << 16 : ((&v[j].x)[k / 2] & 0xffff0000u) | w;
+          }
+        }
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < kLoads; j++)
+#pragma unroll
+    for (int k = 0; k < kVec; k += 2) m = max3_nan(m, element<T>(v[j], k), element<T>(v[j], k + 1));
+#pragma unroll
+  for (int o = 16; o; o /= 2) m = max_nan(m, __shfl_xor_sync(~0u, m, o));
+  if (lane == 0) red[warp] = m;
+  __syncthreads();
+  m = red[lane & (kWarps - 1)];
+#pragma unroll
+  for (int o = kWarps / 2; o; o /= 2) m = max_nan(m, __shfl_xor_sync(~0u, m, o));
+  m = __shfl_sync(~0u, m, 0);
+  float sum = 0.f;
+  int first = 0x7fffffff;
+  if (t > 0.f) {
+    if (m > -CUDART_INF_F) {
+      const float f = fminf(kLog2e / t, 3e38f);        // (a difference of 0 stays 0)
+#pragma unroll
+      for (int j = 0; j < kLoads; j++)
+#pragma unroll
+        for (int k = 0; k < kVec; k++) sum += exp2_fast((element<T>(v[j], k) - m) * f);
+    }
+  } else {
+#pragma unroll
+    for (int j = kLoads - 1; j >= 0; j--)
+#pragma unroll
+      for (int k = kVec - 1; k >= 0; k--)
+        if (element<T>(v[j], k) == m) first = begin + j * kThreads * kVec + k;
+  }
+#pragma unroll
+  for (int o = 16; o; o /= 2) {
+    sum += __shfl_xor_sync(~0u, sum, o);
+    first = min(first, __shfl_xor_sync(~0u, first, o));
+  }
+  __syncthreads();
+  if (lane == 0) red[warp] = sum, red_i[warp] = first;
+  __syncthreads();
+  if (warp == 0) {
+    sum = lane < kWarps ? red[lane] : 0.f, first = lane < kWarps ? red_i[lane] : 0x7fffffff;
+#pragma unroll
+    for (int o = kWarps / 2; o; o /= 2) {
+      sum += __shfl_xor_sync(~0u, sum, o);
+      first = min(first, __shfl_xor_sync(~0u, first, o));
+    }
+    if (lane == 0) p.stats[blockIdx.x] = Stat{m, sum, first, 0};
+  }
+}
+
+// ---- the walk ---------------------------------------------------------------------------------------------------
+__device__ __forceinline__ void st_remote(const void* mine, unsigned rank, double x) {
+  asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(remote(mine, rank)), "d"(x) : "memory");
+}
+
+constexpr int kMaxRows = AMK_TREE_MAX_ROWS, kMaxCluster = 16;
+
+struct Walk {
+  int parent[kMaxRows], token[kMaxRows];
+  float u[kMaxRows], x[kMaxRows], q[kMaxRows];         // the number, and the token's logit and drafted probability in its parent's rows
+  float m[kMaxRows], s[kMaxRows];                      // the rows' statistics
+  int first[kMaxRows];
+  double inv[kMaxRows];                                // 1 / S_0 .. 1 / S_{k-1}
+  int out[kMaxRows];                                   // guesses: the rejected tokens
+  double run[kWarps];                                  // sums of the warps' runs of this block's share of the row
+  double block[2][kMaxCluster];                        // the blocks' sums, of the last pass and the one before it
+  int over[kWarps], positive[kWarps];                  // in the search: the first place past the number, the last with a weight
+};
+
+// The weights of a state of the walk, for any token.
+template <class T>
+struct Weights {
+  const T* x;
+  const float* q;                                      // null: guesses
+  double m, inv_t;
+  int k;                                               // rejected children
+  const Walk& w;
+  __device__ __forceinline__ double operator()(float xt, float qt, int t) const {
+    double v = exp(((double)xt - m) * inv_t);
+    if (q) {
+      for (int j = 0; j < k; j++) v = fmax(fma(v, w.inv[j], -(double)qt), 0.0);
+    } else {
+      for (int j = 0; j < k; j++)
+        if (w.out[j] == t) v = 0.0;
+    }
+    return v;
+  }
+};
+
+__device__ __forceinline__ double shfl_xor(double x, int o) { return __shfl_xor_sync(~0u, x, o); }
+
+// The sum of a state's weights over the row: the runs' and the blocks' sums stay in shared memory.  The whole cluster.
+template <class T>
+__device__ __forceinline__ double pass(const VerifyParams& p, Walk& w, const Weights<T>& of, int rank, int begin, int run, int end,
+                                       int& parity) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int from = begin + warp * run, to = min(from + run, end);
+  double sum = 0.0;
+  constexpr int kAhead = 4;
+  for (int i = from + lane; i < to; i += 32 * kAhead) {
+    float xt[kAhead], qt[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; j++) {
+      const bool in = i + 32 * j < to;
+      xt[j] = in ? load(of.x, i + 32 * j) : -CUDART_INF_F;
+      qt[j] = in && of.q && of.k ? load(of.q, i + 32 * j) : 0.f;
+    }
+#pragma unroll
+    for (int j = 0; j < kAhead; j++) sum += of(xt[j], qt[j], i + 32 * j);
+  }
+#pragma unroll
+  for (int o = 16; o; o /= 2) sum += shfl_xor(sum, o);
+  __syncthreads();                                     // (the last pass's sums have been read)
+  if (lane == 0) w.run[warp] = sum;
+  __syncthreads();
+  parity ^= 1;
+  if ((int)threadIdx.x < p.cluster) {
+    double all = 0.0;
+    for (int j = 0; j < kWarps; j++) all += w.run[j];
+    if (p.cluster == 1) w.block[parity][0] = all;
+    else st_remote(&w.block[parity][rank], threadIdx.x, all);
+  }
+  if (p.cluster == 1) __syncthreads();
+  else cluster_sync();
+  double total = 0.0;
+  for (int j = 0; j < p.cluster; j++) total += w.block[parity][j];
+  return total;
+}
+
+template <class T>
+__global__ void __launch_bounds__(kThreads, 1) walk_kernel(const VerifyParams p) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  Walk& w = *(Walk*)smem;
+  const int rank = p.cluster == 1 ? 0 : (int)cluster_rank();
+  const int64_t seq = blockIdx.x / p.cluster;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const T* logits = (const T*)p.logits + seq * p.l_seq;
+  const float* draft = p.draft ? p.draft + seq * p.d_seq : nullptr;
+  wait_for_grid_before();
+  const float t = p.temperature ? p.temperature[seq] : 1.f;
+  const int* tokens = p.tokens + seq * p.rows;
+  const int* parents = p.parents ? p.parents + seq * p.rows : nullptr;
+  for (int i = threadIdx.x; i < p.rows; i += kThreads) {
+    int parent = parents && i ? parents[i] : i - 1;
+    const int tok = i ? tokens[i] : -1;
+    if (parent >= i || tok < 0 || tok >= p.vocab) parent = -1;
+    w.parent[i] = parent, w.token[i] = tok, w.u[i] = p.u[seq * p.rows + i];
+    if (parent >= 0) {
+      w.x[i] = load(logits + parent * p.l_row, tok);
+      w.q[i] = draft ? __ldg(draft + parent * p.d_row + tok) : 1.f;
+    }
+    // the row's parts
+    const Stat* st = p.stats + (seq * p.rows + i) * p.parts;
+    float m = -CUDART_INF_F, s = 0.f;
+    int first = 0x7fffffff;
+    for (int j = 0; j < p.parts; j++) m = max_nan(m, st[j].m);
+    const float f = fminf(kLog2e / t, 3e38f);
+    for (int j = 0; j < p.parts; j++) {
+      const Stat a = st[j];
+      if (a.m > -CUDART_INF_F) s += a.s * exp2_fast((a.m - m) * f);
+      if (a.m == m) first = min(first, a.first);
+    }
+    w.m[i] = m, w.s[i] = s, w.first[i] = first;
+  }
+  if (p.cluster == 1) __syncthreads();
+  else cluster_sync();                                 // (also: the other blocks have begun and can be written to)
+  const bool greedy = t == 0.f, legal = t >= 0.f && t < CUDART_INF_F;
+  const int len = p.cache_len ? p.cache_len[seq] : 0;
+  const bool tells = rank == 0 && threadIdx.x == 0;
+  int* keep = p.keep + seq * p.rows;
+  if (tells) keep[0] = len;
+
+  // this block's share of a row, in runs for its warps
+  const int share = (p.vocab + p.cluster - 1) / p.cluster, begin = min(rank * share, p.vocab), end = min(begin + share, p.vocab);
+  const int run = (share + kWarps - 1) / kWarps;
+  int at = 0, kept = 1, k = 0, parity = 0;
+  bool summed = false;                                 // S_k is known in 64 bits, and the runs' sums are those of this state
+  double total = 0.0;                                  // S_k
+  double gone = 0.0;                                   // guesses: what the rejected tokens had of the 32-bit sum
+  Weights<T> of{logits, nullptr, 0.0, 1.0 / (double)t, 0, w};
+  of.q = draft;
+  const auto valid = [&](int node) { return legal && fabsf(w.m[node]) < CUDART_INF_F; };
+  const auto enter = [&](int node) {
+    at = node, k = 0, summed = false, gone = 0.0;
+    of.x = logits + node * p.l_row, of.m = (double)w.m[node], of.k = 0;
+    if (draft) of.q = draft + node * p.d_row;
+  };
+  // S_k for the state at hand; one without any weight is not one: the state before it stays
+  const auto sum_up = [&]() {
+    while (!summed) {
+      total = pass(p, w, of, rank, begin, run, end, parity);
+      if (total > 0.0 || k == 0) summed = true;
+      else of.k = --k;
+    }
+  };
+  enter(0);
+  bool ok = valid(0);
+  for (int i = 1; i < p.rows && ok; i++) {
+    if (w.parent[i] != at) continue;
+    const double uq = (double)w.u[i] * (double)w.q[i];
+    bool accept;
+    if (greedy) {
+      accept = w.token[i] == w.first[at] && uq < 1.0;
+    } else {
+      const double e = exp(((double)w.x[i] - of.m) * of.inv_t);
+      bool decided = false;
+      accept = false;
+      if (!summed && (k == 0 || !draft)) {             // by the 32-bit sum, if that is enough
+        const double s32 = (double)w.s[at], s = s32 - gone;
+        bool before = false;
+        for (int j = 0; j < k; j++) before |= w.out[j] == w.token[i];
+        const double r = before ? 0.0 : e / s;
+        if (s > s32 / 1024 && fabs(uq - r) > kNear * r * (s32 / s)) decided = true, accept = uq < r;
+      }
+      if (!decided) {
+        sum_up();
+        accept = uq < of(w.x[i], w.q[i], w.token[i]) / total;
+      }
+    }
+    if (accept) {
+      if (tells) keep[kept] = len + i;
+      kept++;
+      enter(i);
+      ok = valid(i);
+    } else if (!greedy) {
+      if (draft) {
+        sum_up();
+        __syncthreads();
+        if (threadIdx.x == 0) w.inv[k] = 1.0 / total;
+      } else {
+        bool before = false;
+        for (int j = 0; j < k; j++) before |= w.out[j] == w.token[i];
+        if (!before) gone += exp(((double)w.x[i] - of.m) * of.inv_t);
+        __syncthreads();
+        if (threadIdx.x == 0) w.out[k] = w.token[i];
+      }
+      __syncthreads();
+      of.k = ++k;
+      summed = false;
+    }
+  }
+  if (tells) p.count[seq] = kept;
+  if (rank == 0)
+    for (int i = kept + threadIdx.x; i < p.rows; i += kThreads) keep[i] = -1;
+  if (!ok || greedy) {
+    if (tells) p.token[seq] = ok ? w.first[at] : -1;
+    return;
+  }
+  // the token: the block, the run and the place where the running sum passes the given number
+  sum_up();
+  const double want = (double)w.u[0] * total;
+  double before = 0.0, sum = 0.0;
+  int block = 0;
+  {
+    double run_sum = 0.0, last_before = 0.0;
+    int last = 0, found = -1;
+    for (int j = 0; j < p.cluster && found < 0; j++) {
+      const double b = w.block[parity][j];
+      if (run_sum + b > want) found = j, before = run_sum;
+      if (b > 0.0) last = j, last_before = run_sum;
+      run_sum += b;
+    }
+    block = found < 0 ? last : found;
+    if (found < 0) before = last_before;
+  }
+  if (rank != block) return;
+  int mine = 0;
+  {
+    double last_before = before;
+    int last = 0, found = -1;
+    sum = before;
+    for (int j = 0; j < kWarps && found < 0; j++) {
+      const double b = w.run[j];
+      if (sum + b > want) found = j, before = sum;
+      if (b > 0.0) last = j, last_before = sum;
+      sum += b;
+    }
+    mine = found < 0 ? last : found;
+    if (found < 0) before = last_before;
+  }
+  const int from = begin + mine * run, to = min(from + run, end);
+  // all warps over the one run, 512 places at a time
+  int last_positive = -1;
+  for (int i0 = from; i0 < to; i0 += kThreads) {
+    const int i = i0 + threadIdx.x;
+    const double v = i < to ? of(load(of.x, i), of.q && of.k ? load(of.q, i) : 0.f, i) : 0.0;
+    double c = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const double y = __shfl_up_sync(~0u, c, o);
+      if (lane >= o) c += y;
+    }
+    __syncthreads();
+    if (lane == 31) w.run[warp] = c;
+    __syncthreads();
+    double ahead = before;
+    for (int j = 0; j < warp; j++) ahead += w.run[j];
+    const unsigned over = __ballot_sync(~0u, v > 0.0 && ahead + c > want), some = __ballot_sync(~0u, v > 0.0);
+    if (lane == 0) {
+      w.over[warp] = over ? i0 + warp * 32 + __ffs(over) - 1 : -1;
+      w.positive[warp] = some ? i0 + warp * 32 + 31 - __clz(some) : -1;
+    }
+    __syncthreads();
+    int hit = -1;
+    for (int j = 0; j < kWarps; j++) {
+      if (hit < 0) hit = w.over[j];
+      if (w.positive[j] >= 0) last_positive = w.positive[j];
+    }
+    if (hit >= 0) {
+      if (threadIdx.x == 0) p.token[seq] = hit;
+      return;
+    }
+    for (int j = 0; j < kWarps; j++) before += w.run[j];
+  }
+  if (threadIdx.x == 0) p.token[seq] = last_positive;
+}
+
+// ---- host -------------------------------------------------------------------------------------------------------
+cudaError_t allow_smem() {
+  static std::atomic<unsigned long long> done{0};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const unsigned long long bit = dev < 64 ? 1ull << dev : 0;
+  if (done.load(std::memory_order_acquire) & bit) return cudaSuccess;
+  e = cudaFuncSetAttribute(walk_kernel<float>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(Walk));
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(walk_kernel<unsigned short>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(Walk));
+  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_release);
+  return e;
+}
+
+// Everything about a call that can be known without its pointers.
+amk_status check(const Reason& fail, const amk_verify_args* a) {
+  if (!a) return fail(AMK_ERR_INVALID_ARG, "NULL arguments");
+  if (a->struct_size != sizeof *a)
+    return fail(AMK_ERR_INVALID_ARG, "struct_size %u, the library has %zu", a->struct_size, sizeof *a);
+  if (a->dtype > 1) return fail(AMK_ERR_UNSUPPORTED, "dtype %u: 0 (float) or 1 (bf16)", a->dtype);
+  if (a->n_rows < 1 || a->n_rows > AMK_TREE_MAX_ROWS)
+    return fail(AMK_ERR_UNSUPPORTED, "%u rows: 1 to %d", a->n_rows, AMK_TREE_MAX_ROWS);
+  if (a->vocab < 1 || a->vocab > 0x7fffffff - 65536) return fail(AMK_ERR_INVALID_ARG, "%lld logits a row", (long long)a->vocab);
+  const int64_t parts = (a->vocab + 7 + kPart - 1) / kPart;
+  if ((int64_t)a->n_seqs > 0x7fffffff / 16 || (int64_t)a->n_seqs * a->n_rows > 0x7fffffff / parts)
+    return fail(AMK_ERR_INVALID_ARG, "%u sequences of %u rows", a->n_seqs, a->n_rows);
+  return AMK_OK;
+}
+
+int64_t parts_of(const amk_verify_args& a) { return (a.vocab + 7 + kPart - 1) / kPart; }
+
+}  // namespace
+
+extern "C" amk_status amk_verify_workspace_bytes(const amk_verify_args* args, size_t* bytes, char* msg, size_t msg_bytes) {
+  const Reason fail(msg, msg_bytes, "amk_verify_workspace_bytes");
+  if (!bytes) return fail(AMK_ERR_INVALID_ARG, "NULL pointer");
+  const amk_status st = check(fail, args);
+  if (st != AMK_OK) return st;
+  *bytes = sizeof(Stat) * (size_t)args->n_seqs * args->n_rows * (size_t)parts_of(*args);
+  return AMK_OK;
+}
+
+extern "C" amk_status amk_verify_draft(const amk_verify_args* args, char* msg, size_t msg_bytes, void* cuda_stream) {
+  const Reason fail(msg, msg_bytes, "amk_verify_draft");
+  const amk_status ok = check(fail, args);
+  if (ok != AMK_OK) return ok;
+  const amk_verify_args& a = *args;
+  if (a.n_seqs == 0) return AMK_OK;
+  if (!a.logits || !a.tokens || !a.uniforms || !a.count || !a.keep || !a.token) return fail(AMK_ERR_INVALID_ARG, "NULL pointer");
+  const void* words[] = {a.draft, a.tokens, a.parents, a.uniforms, a.temperature, a.cache_len, a.count, a.keep, a.token};
+  for (const void* w : words)
+    if (!aligned(w, 4)) return fail(AMK_ERR_INVALID_ARG, "pointers must be aligned to their elements");
+  if (!aligned(a.logits, a.dtype ? 2 : 4) || !aligned(a.workspace, 256))
+    return fail(AMK_ERR_INVALID_ARG, "logits must be aligned to their elements, the workspace to 256 bytes");
+  const int64_t most = (int64_t)1 << 40;
+  const bool seqs = a.n_seqs > 1, rows = a.n_rows > 1;
+  if ((rows && (a.logits_row < a.vocab || a.logits_row > most)) || (seqs && (a.logits_seq < a.vocab || a.logits_seq > most)) ||
+      (a.draft && ((rows && (a.draft_row < a.vocab || a.draft_row > most)) || (seqs && (a.draft_seq < a.vocab || a.draft_seq > most)))))
+    return fail(AMK_ERR_INVALID_ARG, "strides must be at least the %lld logits of a row", (long long)a.vocab);
+  const int64_t parts = parts_of(a);
+  const size_t need = sizeof(Stat) * (size_t)a.n_seqs * a.n_rows * (size_t)parts;
+  if (!a.workspace || a.workspace_bytes < need)
+    return fail(AMK_ERR_INVALID_ARG, "workspace of %llu bytes, %zu are needed",
+                (unsigned long long)(a.workspace ? a.workspace_bytes : 0), need);
+  cudaError_t e = allow_smem();
+  if (e != cudaSuccess) return fail(AMK_ERR_CUDA, "%s", cudaGetErrorString(e));
+  VerifyParams p{};
+  p.logits = a.logits, p.draft = a.draft, p.tokens = a.tokens, p.parents = a.parents, p.u = a.uniforms;
+  p.temperature = a.temperature, p.cache_len = a.cache_len, p.count = a.count, p.keep = a.keep, p.token = a.token;
+  p.stats = (Stat*)a.workspace;
+  p.l_seq = seqs ? a.logits_seq : 0, p.l_row = rows ? a.logits_row : 0;
+  p.d_seq = seqs ? a.draft_seq : 0, p.d_row = rows ? a.draft_row : 0;
+  p.rows = (int)a.n_rows, p.vocab = (int)a.vocab, p.parts = (int)parts;
+  const int sms = multiprocessors();
+  p.cluster = 1;
+  while (p.cluster < 8 && (int64_t)a.n_seqs * p.cluster * 2 <= sms && a.vocab / (2 * p.cluster) >= 1024) p.cluster *= 2;
+  const cudaStream_t st = (cudaStream_t)cuda_stream;
+  const unsigned stat_blocks = (unsigned)((int64_t)a.n_seqs * a.n_rows * parts), walk_blocks = a.n_seqs * (unsigned)p.cluster;
+  e = launch_early(a.dtype ? stats_kernel<unsigned short> : stats_kernel<float>, dim3(stat_blocks), kThreads, 0, 1, st, p);
+  if (e == cudaSuccess)
+    e = launch_early(a.dtype ? walk_kernel<unsigned short> : walk_kernel<float>, dim3(walk_blocks), kThreads, sizeof(Walk),
+                     (unsigned)p.cluster, st, p);
+  return e == cudaSuccess ? AMK_OK : fail(AMK_ERR_CUDA, "launch failed: %s", cudaGetErrorString(e));
+}
