@@ -146,7 +146,8 @@ int sm_count() {
 // What amk_debug_operator_wait set.
 std::atomic<unsigned> g_wait_cycles{amk::kWaitCycles};
 std::atomic<unsigned> g_tiles{~0u};
-void set_limits(AttnParams& p) {
+template <class Params>
+void set_limits(Params& p) {
   p.wait_cycles = g_wait_cycles.load(std::memory_order_relaxed);
   p.tiles = g_tiles.load(std::memory_order_relaxed);
 }
@@ -266,6 +267,55 @@ amk_status check_weights(const Reason& fail, const amk_attention_weights_args* a
     return fail(AMK_ERR_UNSUPPORTED, "%u sequences of %u tokens over %u slots: more than 2^31 pieces of work", a->n_seqs, a->n_rows,
                 a->n_slots);
   return AMK_OK;
+}
+
+// How a call of the weights is divided.
+struct WeightsPlan {
+  int tokens, q_tiles, columns;    // tokens of a tile of query rows, tiles, rows of a tile up to a multiple of 32
+  unsigned blocks;
+  size_t bytes;                    // scratch: parts of units, where these have several steps
+};
+WeightsPlan weights_plan(const amk_attention_weights_args& a) {
+  WeightsPlan t;
+  const int rep = (int)(a.n_q_heads / a.n_kv_heads), most = amk::kTile / rep;
+  t.tokens = (int64_t)a.n_rows < most ? (int)a.n_rows : most;
+  t.q_tiles = (int)((a.n_rows + t.tokens - 1) / t.tokens);
+  t.columns = (t.tokens * rep + 31) / 32 * 32;
+  const double steps = (a.n_slots / (double)amk::kTile + 1) * a.n_kv_heads * a.n_seqs * t.q_tiles;
+  const int sms = sm_count();
+  t.blocks = (unsigned)(steps < sms ? (steps < 1 ? 1 : steps) : sms);
+  t.bytes = t.q_tiles > 1 ? (size_t)2 * t.blocks * (sizeof(int4) + amk::kTile * sizeof(float)) : 0;
+  return t;
+}
+
+// The queries as {element, head of the group, kv head, token, sequence}; a box: 64 elements of all heads of a group and the
+// tokens of a tile, which lie one behind the other as its rows.
+bool make_query_map(CUtensorMap* map, const amk_attention_weights_args& a, int rep, int tokens) {
+  const EncodeTiled encode = encode_tiled();
+  if (!encode) return false;
+  const cuuint64_t dims[5] = {a.head_dim, (cuuint64_t)rep, a.n_kv_heads, a.n_rows, a.n_seqs};
+  const cuuint64_t strides[4] = {(cuuint64_t)a.q_head * 2, (cuuint64_t)a.q_head * rep * 2, (cuuint64_t)a.q_row * 2,
+                                 (cuuint64_t)a.q_seq * 2};
+  const cuuint32_t box[5] = {64, (cuuint32_t)rep, 1, (cuuint32_t)tokens, 1}, steps[5] = {1, 1, 1, 1, 1};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void*>(a.q), dims, strides, box, steps,
+                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int HD, bool FP8>
+cudaError_t launch_weights(const amk::WeightsParams& p, const CUtensorMap& q, const CUtensorMap& k, unsigned blocks, cudaStream_t st) {
+  using L = amk::WeightsSmem<HD, FP8>;
+  static std::atomic<unsigned long long> done{0};      // devices on which the kernel's shared-memory limit is raised
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const unsigned long long bit = dev < 64 ? 1ull << dev : 0;
+  if (!(done.load(std::memory_order_acquire) & bit)) {
+    e = cudaFuncSetAttribute(amk::weights_kernel<HD, FP8>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes);
+    if (e != cudaSuccess) return e;
+    done.fetch_or(bit, std::memory_order_release);
+  }
+  return amk::launch_early(amk::weights_kernel<HD, FP8>, dim3(blocks), L::kThreads, L::kBytes, 1, st, p, q, k);
 }
 
 }  // namespace
@@ -410,7 +460,7 @@ extern "C" amk_status amk_attention_weights_workspace_bytes(const amk_attention_
   const Reason fail(msg, msg_bytes, "amk_attention_weights_workspace_bytes");
   if (!bytes) return fail(AMK_ERR_INVALID_ARG, "NULL pointer");
   AMK_TRY(check_weights(fail, args));
-  *bytes = 0;
+  *bytes = weights_plan(*args).bytes;
   return AMK_OK;
 }
 
@@ -441,17 +491,27 @@ extern "C" amk_status amk_attention_weights(const amk_attention_weights_args* ar
   }
   if (a.before == a.out && (a.before_seq != a.out_seq || a.before_head != a.out_head))
     return fail(AMK_ERR_INVALID_ARG, "out is before, but at other strides");
+  const WeightsPlan t = weights_plan(a);
+  if (t.bytes && (!a.workspace || a.workspace_bytes < t.bytes))
+    return fail(AMK_ERR_INVALID_ARG, "workspace of %llu bytes, %zu are needed", (unsigned long long)(a.workspace ? a.workspace_bytes : 0),
+                t.bytes);
   amk::WeightsParams p{};
-  p.q = (const unsigned short*)a.q, p.k = a.k, p.lse = a.lse, p.lens = a.cache_len, p.before = a.before, p.out = a.out;
-  p.q_seq = a.q_seq, p.q_row = a.q_row, p.q_head = a.q_head, p.k_seq = a.k_seq, p.k_head = a.k_head, p.k_row = a.k_row;
+  p.lse = a.lse, p.lens = a.cache_len, p.before = a.before, p.out = a.out;
+  if (t.bytes) p.part_of = (int4*)a.workspace, p.part = (float*)(p.part_of + 2 * t.blocks);
   p.b_seq = a.before_seq, p.b_head = a.before_head, p.o_seq = a.out_seq, p.o_head = a.out_head;
   p.n_seqs = (int)a.n_seqs, p.nq = (int)a.n_q_heads, p.nkv = (int)a.n_kv_heads, p.rep = p.nq / p.nkv;
   p.rows = (int)a.n_rows, p.slots = (int)a.n_slots;
+  p.tokens = t.tokens, p.q_tiles = t.q_tiles, p.columns = t.columns;
   p.scale = a.scale > 0.f ? a.scale : 1.f / sqrtf((float)hd), p.decay = a.decay;
-  const dim3 grid((a.n_slots + amk::kTile - 1) / amk::kTile, a.n_kv_heads, a.n_seqs);
+  set_limits(p);
+  CUtensorMap mq, mk;
+  if (!make_query_map(&mq, a, p.rep, t.tokens) ||
+      !make_map(&mk, a.k, esz == 1, hd, a.n_slots, p.nkv, a.n_seqs, a.k_row, a.k_head, a.k_seq))
+    return fail(AMK_ERR_CUDA, "cuTensorMapEncodeTiled failed or is missing");
   const cudaStream_t st = (cudaStream_t)cuda_stream;
-  const auto kernel = hd == 64 ? (esz == 1 ? amk::weights_kernel<64, true> : amk::weights_kernel<64, false>)
-                               : (esz == 1 ? amk::weights_kernel<128, true> : amk::weights_kernel<128, false>);
-  const cudaError_t e = amk::launch_early(kernel, grid, amk::kTile, 0, 1, st, p);
+  cudaError_t e = hd == 64 ? (esz == 1 ? launch_weights<64, true>(p, mq, mk, t.blocks, st) : launch_weights<64, false>(p, mq, mk, t.blocks, st))
+                           : (esz == 1 ? launch_weights<128, true>(p, mq, mk, t.blocks, st) : launch_weights<128, false>(p, mq, mk, t.blocks, st));
+  if (e == cudaSuccess && t.bytes)
+    e = amk::launch_early(amk::weights_join_kernel, dim3(t.blocks), amk::kTile, 0, 1, st, p, (int)t.blocks);
   return e == cudaSuccess ? AMK_OK : fail(AMK_ERR_CUDA, "launch failed: %s", cudaGetErrorString(e));
 }

@@ -201,7 +201,8 @@ constexpr unsigned kWaitCycles = 4000000000u;
 // timer is read through a unit that all SMs share); false if that ran out.  The votes keep the warp's control flow
 // uniform: behind a wait that each lane leaves by itself, the matrix instructions of one tile took ten times as long
 // to issue (700 cycles instead of 70).
-__device__ __forceinline__ bool attn_wait(uint64_t* bar, unsigned parity, AttnHead& h) {
+template <class Head>
+__device__ __forceinline__ bool attn_wait(uint64_t* bar, unsigned parity, Head& h) {
   if (__all_sync(~0u, mbar_try_wait(bar, parity))) return true;
   const unsigned t0 = clock();
   for (;;) {
