@@ -27,9 +27,8 @@ namespace {
 
 using namespace amk;
 
-constexpr int kThreads = 512, kWarps = kThreads / 32;
-constexpr int kEach = 32;                              // logits a thread of the first kernel has
-constexpr int kPart = kThreads * kEach;                // ... and a block
+constexpr int kThreads = 512, kWarps = kThreads / 32;    // the walk's
+constexpr int kStatThreads = 256, kStatWarps = kStatThreads / 32, kLoads = 8;   // the first kernel's: 32 KB of logits a block
 constexpr float kLog2e = 1.4426950408889634f;
 // A row's sum in 32 bits: an exponent y = (x - m) log2 e / T is off by 2^-23 |y|, its power by 2^-23 |y| ln 2 of itself (less than
 // 2^-24 32 for the terms that count) and 2^-22, additions by less than 2^-19 together: 2^-17.
@@ -67,13 +66,12 @@ __device__ __forceinline__ float max_nan(float a, float b) {
 }
 
 // ---- the rows' maxima and sums ----------------------------------------------------------------------------------
-// A block has 16384 consecutive places of a row, counted from the 16-byte boundary at or in front of its first logit, and holds
-// them in registers.
+// A block has 32 KB of a row, counted from the 16-byte boundary at or in front of its first logit, and holds them in registers.
 template <class T>
-__global__ void __launch_bounds__(kThreads) stats_kernel(const VerifyParams p) {
-  constexpr int kVec = 16 / sizeof(T), kLoads = kEach / kVec;
-  __shared__ float red[kWarps];
-  __shared__ int red_i[kWarps];
+__global__ void __launch_bounds__(kStatThreads) stats_kernel(const VerifyParams p) {
+  constexpr int kVec = 16 / sizeof(T), kPart = kStatThreads * kLoads * kVec;
+  __shared__ float red[kStatWarps];
+  __shared__ int red_i[kStatWarps];
   const int64_t r = blockIdx.x / p.parts;
   const int part = (int)(blockIdx.x - r * p.parts);
   const int64_t s = r / p.rows, i = r - s * p.rows;
@@ -90,7 +88,7 @@ __global__ void __launch_bounds__(kThreads) stats_kernel(const VerifyParams p) {
   const unsigned nothing = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;     // -infinity
 #pragma unroll
   for (int j = 0; j < kLoads; j++) {
-    const int at = begin + j * kThreads * kVec;
+    const int at = begin + j * kStatThreads * kVec;
     v[j] = make_uint4(nothing, nothing, nothing, nothing);
     if (at >= 0 && at + kVec <= p.vocab) {
       v[j] = __ldg(x4 + (at + skew) / kVec);
@@ -115,9 +113,9 @@ __global__ void __launch_bounds__(kThreads) stats_kernel(const VerifyParams p) {
   for (int o = 16; o; o /= 2) m = max_nan(m, __shfl_xor_sync(~0u, m, o));
   if (lane == 0) red[warp] = m;
   __syncthreads();
-  m = red[lane & (kWarps - 1)];
+  m = red[lane & (kStatWarps - 1)];
 #pragma unroll
-  for (int o = kWarps / 2; o; o /= 2) m = max_nan(m, __shfl_xor_sync(~0u, m, o));
+  for (int o = kStatWarps / 2; o; o /= 2) m = max_nan(m, __shfl_xor_sync(~0u, m, o));
   m = __shfl_sync(~0u, m, 0);
   float sum = 0.f;
   int first = 0x7fffffff;
@@ -134,7 +132,7 @@ __global__ void __launch_bounds__(kThreads) stats_kernel(const VerifyParams p) {
     for (int j = kLoads - 1; j >= 0; j--)
 #pragma unroll
       for (int k = kVec - 1; k >= 0; k--)
-        if (element<T>(v[j], k) == m) first = begin + j * kThreads * kVec + k;
+        if (element<T>(v[j], k) == m) first = begin + j * kStatThreads * kVec + k;
   }
 #pragma unroll
   for (int o = 16; o; o /= 2) {
@@ -145,9 +143,9 @@ __global__ void __launch_bounds__(kThreads) stats_kernel(const VerifyParams p) {
   if (lane == 0) red[warp] = sum, red_i[warp] = first;
   __syncthreads();
   if (warp == 0) {
-    sum = lane < kWarps ? red[lane] : 0.f, first = lane < kWarps ? red_i[lane] : 0x7fffffff;
+    sum = lane < kStatWarps ? red[lane] : 0.f, first = lane < kStatWarps ? red_i[lane] : 0x7fffffff;
 #pragma unroll
-    for (int o = kWarps / 2; o; o /= 2) {
+    for (int o = kStatWarps / 2; o; o /= 2) {
       sum += __shfl_xor_sync(~0u, sum, o);
       first = min(first, __shfl_xor_sync(~0u, first, o));
     }
@@ -161,78 +159,57 @@ __device__ __forceinline__ void st_remote(const void* mine, unsigned rank, doubl
 }
 
 constexpr int kMaxRows = AMK_TREE_MAX_ROWS, kMaxCluster = 16;
+enum { kReject, kAccept, kClose };
+constexpr int kHeld = 16;                              // weights of a row that a thread keeps in registers
 
 struct Walk {
   int parent[kMaxRows], token[kMaxRows];
-  float u[kMaxRows], x[kMaxRows], q[kMaxRows];         // the number, and the token's logit and drafted probability in its parent's rows
+  float x[kMaxRows], q[kMaxRows];                      // the token's logit and drafted probability in its parent's rows
+  double e[kMaxRows], uq[kMaxRows];                    // its e there, and the number times the probability
+  int verdict[kMaxRows];                               // as a first child: accepted, rejected, or not to be said in 32 bits
   float m[kMaxRows], s[kMaxRows];                      // the rows' statistics
   int first[kMaxRows];
   double inv[kMaxRows];                                // 1 / S_0 .. 1 / S_{k-1}
   int out[kMaxRows];                                   // guesses: the rejected tokens
   double run[kWarps];                                  // sums of the warps' runs of this block's share of the row
   double block[2][kMaxCluster];                        // the blocks' sums, of the last pass and the one before it
+  double roots[32];                                    // 2^(j / 32)
   int over[kWarps], positive[kWarps];                  // in the search: the first place past the number, the last with a weight
 };
 
-// The weights of a state of the walk, for any token.
-template <class T>
-struct Weights {
-  const T* x;
-  const float* q;                                      // null: guesses
-  double m, inv_t;
-  int k;                                               // rejected children
-  const Walk& w;
-  __device__ __forceinline__ double operator()(float xt, float qt, int t) const {
-    double v = exp(((double)xt - m) * inv_t);
-    if (q) {
-      for (int j = 0; j < k; j++) v = fmax(fma(v, w.inv[j], -(double)qt), 0.0);
-    } else {
-      for (int j = 0; j < k; j++)
-        if (w.out[j] == t) v = 0.0;
+// e^y for y <= 0, off by less than 2^-43 of itself: y = (n + f) ln 2 / 32 with |f| <= 1/2, 2^(n / 32) from the table and an exponent,
+// the rest by its Taylor series (r^6 / 720 < 2^-48; r is off by 2^-53 |y|).  Below e^-700: 0.
+__device__ __forceinline__ double exp_below(double y, const double* roots) {
+  const double magic = 6755399441055744.0;             // 1.5 * 2^52: leaves the integer in the low word
+  const double t = fma(y, 46.166241308446828384, magic);
+  const int n = __double2loint(t);
+  const double r = fma(t - magic, -0.021660849392498290195, y);
+  double v = fma(r, 1.0 / 120, 1.0 / 24);
+  v = fma(v, r, 1.0 / 6), v = fma(v, r, 0.5), v = fma(v, r, 1.0), v = fma(v, r, 1.0);
+  const double w = roots[n & 31];
+  v *= __hiloint2double(__double2hiint(w) + (int)((unsigned)(n >> 5) << 20), __double2loint(w));
+  return y < -700.0 ? 0.0 : v;
+}
+
+// From the weights of one state to those of the next one, in place; token i + 32 j's is v[j].
+template <int N>
+__device__ __forceinline__ void reject(double (&v)[N], const float (&q)[N], const Walk& w, bool drafted, int j0, int i) {
+  if (drafted) {
+    const double inv = w.inv[j0];
+#pragma unroll
+    for (int j = 0; j < N; j++) {
+      const double x = fma(v[j], inv, -(double)q[j]);
+      v[j] = __double2hiint(x) < 0 ? 0.0 : x;
     }
-    return v;
+  } else {
+    const int out = w.out[j0];
+#pragma unroll
+    for (int j = 0; j < N; j++)
+      if (i + 32 * j == out) v[j] = 0.0;
   }
-};
+}
 
 __device__ __forceinline__ double shfl_xor(double x, int o) { return __shfl_xor_sync(~0u, x, o); }
-
-// The sum of a state's weights over the row: the runs' and the blocks' sums stay in shared memory.  The whole cluster.
-template <class T>
-__device__ __forceinline__ double pass(const VerifyParams& p, Walk& w, const Weights<T>& of, int rank, int begin, int run, int end,
-                                       int& parity) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int from = begin + warp * run, to = min(from + run, end);
-  double sum = 0.0;
-  constexpr int kAhead = 4;
-  for (int i = from + lane; i < to; i += 32 * kAhead) {
-    float xt[kAhead], qt[kAhead];
-#pragma unroll
-    for (int j = 0; j < kAhead; j++) {
-      const bool in = i + 32 * j < to;
-      xt[j] = in ? load(of.x, i + 32 * j) : -CUDART_INF_F;
-      qt[j] = in && of.q && of.k ? load(of.q, i + 32 * j) : 0.f;
-    }
-#pragma unroll
-    for (int j = 0; j < kAhead; j++) sum += of(xt[j], qt[j], i + 32 * j);
-  }
-#pragma unroll
-  for (int o = 16; o; o /= 2) sum += shfl_xor(sum, o);
-  __syncthreads();                                     // (the last pass's sums have been read)
-  if (lane == 0) w.run[warp] = sum;
-  __syncthreads();
-  parity ^= 1;
-  if ((int)threadIdx.x < p.cluster) {
-    double all = 0.0;
-    for (int j = 0; j < kWarps; j++) all += w.run[j];
-    if (p.cluster == 1) w.block[parity][0] = all;
-    else st_remote(&w.block[parity][rank], threadIdx.x, all);
-  }
-  if (p.cluster == 1) __syncthreads();
-  else cluster_sync();
-  double total = 0.0;
-  for (int j = 0; j < p.cluster; j++) total += w.block[parity][j];
-  return total;
-}
 
 template <class T>
 __global__ void __launch_bounds__(kThreads, 1) walk_kernel(const VerifyParams p) {
@@ -243,6 +220,7 @@ __global__ void __launch_bounds__(kThreads, 1) walk_kernel(const VerifyParams p)
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const T* logits = (const T*)p.logits + seq * p.l_seq;
   const float* draft = p.draft ? p.draft + seq * p.d_seq : nullptr;
+  if (threadIdx.x < 32) w.roots[threadIdx.x] = exp2(threadIdx.x / 32.0);
   wait_for_grid_before();
   const float t = p.temperature ? p.temperature[seq] : 1.f;
   const int* tokens = p.tokens + seq * p.rows;
@@ -250,28 +228,55 @@ __global__ void __launch_bounds__(kThreads, 1) walk_kernel(const VerifyParams p)
   for (int i = threadIdx.x; i < p.rows; i += kThreads) {
     int parent = parents && i ? parents[i] : i - 1;
     const int tok = i ? tokens[i] : -1;
+    const float u = p.u[seq * p.rows + i];
     if (parent >= i || tok < 0 || tok >= p.vocab) parent = -1;
-    w.parent[i] = parent, w.token[i] = tok, w.u[i] = p.u[seq * p.rows + i];
+    w.parent[i] = parent, w.token[i] = tok;
     if (parent >= 0) {
       w.x[i] = load(logits + parent * p.l_row, tok);
       w.q[i] = draft ? __ldg(draft + parent * p.d_row + tok) : 1.f;
+      w.uq[i] = (double)u * (double)w.q[i];
     }
-    // the row's parts
+  }
+  // the rows' parts, a lane each
+  const float f = fminf(kLog2e / t, 3e38f);
+  for (int i = warp; i < p.rows; i += kWarps) {
     const Stat* st = p.stats + (seq * p.rows + i) * p.parts;
     float m = -CUDART_INF_F, s = 0.f;
     int first = 0x7fffffff;
-    for (int j = 0; j < p.parts; j++) m = max_nan(m, st[j].m);
-    const float f = fminf(kLog2e / t, 3e38f);
-    for (int j = 0; j < p.parts; j++) {
-      const Stat a = st[j];
-      if (a.m > -CUDART_INF_F) s += a.s * exp2_fast((a.m - m) * f);
-      if (a.m == m) first = min(first, a.first);
+    for (int j0 = 0; j0 < p.parts; j0 += 32) {
+      Stat a{-CUDART_INF_F, 0.f, 0x7fffffff, 0};
+      if (j0 + lane < p.parts) a = st[j0 + lane];
+      float most = a.m;
+#pragma unroll
+      for (int o = 16; o; o /= 2) most = max_nan(most, __shfl_xor_sync(~0u, most, o));
+      const float next = max_nan(m, most);
+      float add = a.m > -CUDART_INF_F ? a.s * exp2_fast((a.m - next) * f) : 0.f;
+#pragma unroll
+      for (int o = 16; o; o /= 2) add += __shfl_xor_sync(~0u, add, o);
+      s = (m > -CUDART_INF_F ? s * exp2_fast((m - next) * f) : 0.f) + add;
+      const int here = (int)__reduce_min_sync(~0u, (unsigned)(a.m == next ? a.first : 0x7fffffff));
+      first = m == next ? min(first, here) : here;
+      m = next;
     }
-    w.m[i] = m, w.s[i] = s, w.first[i] = first;
+    if (lane == 0) w.m[i] = m, w.s[i] = s, w.first[i] = first;
   }
   if (p.cluster == 1) __syncthreads();
   else cluster_sync();                                 // (also: the other blocks have begun and can be written to)
   const bool greedy = t == 0.f, legal = t >= 0.f && t < CUDART_INF_F;
+  const double inv_t = 1.0 / (double)t;
+  for (int i = threadIdx.x; i < p.rows; i += kThreads) {
+    const int parent = w.parent[i];
+    if (parent < 0) continue;
+    const double uq = w.uq[i];
+    if (greedy) {
+      w.verdict[i] = w.token[i] == w.first[parent] && uq < 1.0 ? kAccept : kReject;
+    } else {
+      const double e = exp(((double)w.x[i] - (double)w.m[parent]) * inv_t), s = (double)w.s[parent];
+      w.e[i] = e;
+      w.verdict[i] = fabs(uq * s - e) > kNear * e ? (uq * s < e ? kAccept : kReject) : kClose;
+    }
+  }
+  __syncthreads();
   const int len = p.cache_len ? p.cache_len[seq] : 0;
   const bool tells = rank == 0 && threadIdx.x == 0;
   int* keep = p.keep + seq * p.rows;
@@ -279,70 +284,148 @@ __global__ void __launch_bounds__(kThreads, 1) walk_kernel(const VerifyParams p)
 
   // this block's share of a row, in runs for its warps
   const int share = (p.vocab + p.cluster - 1) / p.cluster, begin = min(rank * share, p.vocab), end = min(begin + share, p.vocab);
-  const int run = (share + kWarps - 1) / kWarps;
+  const int run = (share + kWarps - 1) / kWarps, from = begin + warp * run, to = min(from + run, end);
   int at = 0, kept = 1, k = 0, parity = 0;
   bool summed = false;                                 // S_k is known in 64 bits, and the runs' sums are those of this state
+  bool has_q = false;                                  // what this thread holds of the row: its drafted probabilities,
+  int held_k = -1;                                     // ... and the weights of this state (-1: none)
+  double held[kHeld];
+  float held_q[kHeld];
   double total = 0.0;                                  // S_k
   double gone = 0.0;                                   // guesses: what the rejected tokens had of the 32-bit sum
-  Weights<T> of{logits, nullptr, 0.0, 1.0 / (double)t, 0, w};
-  of.q = draft;
+  const T* x = logits;
+  const float* q = draft;
+  double m = 0.0;
+  const auto e_of = [&](float xt) { return exp_below(((double)xt - m) * inv_t, w.roots); };
   const auto valid = [&](int node) { return legal && fabsf(w.m[node]) < CUDART_INF_F; };
   const auto enter = [&](int node) {
-    at = node, k = 0, summed = false, gone = 0.0;
-    of.x = logits + node * p.l_row, of.m = (double)w.m[node], of.k = 0;
-    if (draft) of.q = draft + node * p.d_row;
+    at = node, k = 0, summed = has_q = false, held_k = -1, gone = 0.0;
+    x = logits + node * p.l_row, m = (double)w.m[node];
+    if (draft) q = draft + node * p.d_row;
+  };
+  // The sum of the state's weights over the row: the runs' and the blocks' sums stay in shared memory.  The whole cluster.
+  // A thread keeps the first of its run; what is behind them (vocabularies beyond 8192 a block) is read again each time.
+  const auto pass = [&](bool want_q) {
+    const int i0 = from + lane;
+    float xt[kHeld];
+    const bool anew = held_k < 0 || held_k > k;
+    if (anew) {
+#pragma unroll
+      for (int j = 0; j < kHeld; j++) xt[j] = i0 + 32 * j < to ? load(x, i0 + 32 * j) : -CUDART_INF_F;
+    }
+    if (want_q && !has_q) {
+#pragma unroll
+      for (int j = 0; j < kHeld; j++) held_q[j] = i0 + 32 * j < to ? __ldg(q + i0 + 32 * j) : 0.f;
+      has_q = true;
+    }
+    if (anew) {
+#pragma unroll
+      for (int j = 0; j < kHeld; j++) held[j] = e_of(xt[j]);
+      held_k = 0;
+    }
+#pragma unroll 1
+    for (; held_k < k; held_k++) reject(held, held_q, w, draft, held_k, i0);
+    double part[4] = {};
+#pragma unroll
+    for (int j = 0; j < kHeld; j++) part[j & 3] += held[j];
+    constexpr int kAhead = 8;
+#pragma unroll 1
+    for (int i = i0 + 32 * kHeld; i < to; i += 32 * kAhead) {
+      float a[kAhead], b[kAhead];
+      double v[kAhead];
+#pragma unroll
+      for (int j = 0; j < kAhead; j++) {
+        const bool in = i + 32 * j < to;
+        a[j] = in ? load(x, i + 32 * j) : -CUDART_INF_F;
+        b[j] = in && draft && k ? __ldg(q + i + 32 * j) : 0.f;
+      }
+#pragma unroll
+      for (int j = 0; j < kAhead; j++) v[j] = e_of(a[j]);
+#pragma unroll 1
+      for (int n = 0; n < k; n++) reject(v, b, w, draft, n, i);
+#pragma unroll
+      for (int j = 0; j < kAhead; j++) part[j & 3] += v[j];
+    }
+    double sum = (part[0] + part[1]) + (part[2] + part[3]);
+#pragma unroll
+    for (int o = 16; o; o /= 2) sum += shfl_xor(sum, o);
+    __syncthreads();                                   // (the last pass's sums have been read)
+    if (lane == 0) w.run[warp] = sum;
+    __syncthreads();
+    parity ^= 1;
+    if (warp == 0) {
+      double all = lane < kWarps ? w.run[lane] : 0.0;
+#pragma unroll
+      for (int o = 16; o; o /= 2) all += shfl_xor(all, o);
+      if (p.cluster == 1) w.block[parity][0] = all;
+      else if (lane < p.cluster) st_remote(&w.block[parity][rank], lane, all);
+    }
+    if (p.cluster == 1) __syncthreads();
+    else cluster_sync();
+    double all = lane < p.cluster ? w.block[parity][lane] : 0.0;
+#pragma unroll
+    for (int o = 16; o; o /= 2) all += shfl_xor(all, o);
+    return all;
   };
   // S_k for the state at hand; one without any weight is not one: the state before it stays
-  const auto sum_up = [&]() {
+  const auto sum_up = [&](bool want_q) {
     while (!summed) {
-      total = pass(p, w, of, rank, begin, run, end, parity);
+      total = pass(want_q);
       if (total > 0.0 || k == 0) summed = true;
-      else of.k = --k;
+      else --k;
     }
   };
   enter(0);
   bool ok = valid(0);
-  for (int i = 1; i < p.rows && ok; i++) {
-    if (w.parent[i] != at) continue;
-    const double uq = (double)w.u[i] * (double)w.q[i];
-    bool accept;
-    if (greedy) {
-      accept = w.token[i] == w.first[at] && uq < 1.0;
-    } else {
-      const double e = exp(((double)w.x[i] - of.m) * of.inv_t);
-      bool decided = false;
-      accept = false;
-      if (!summed && (k == 0 || !draft)) {             // by the 32-bit sum, if that is enough
-        const double s32 = (double)w.s[at], s = s32 - gone;
-        bool before = false;
-        for (int j = 0; j < k; j++) before |= w.out[j] == w.token[i];
-        const double r = before ? 0.0 : e / s;
-        if (s > s32 / 1024 && fabs(uq - r) > kNear * r * (s32 / s)) decided = true, accept = uq < r;
-      }
-      if (!decided) {
-        sum_up();
-        accept = uq < of(w.x[i], w.q[i], w.token[i]) / total;
+  for (int i = 1; ok;) {
+    // the next child
+    for (; i < p.rows; i += 32) {
+      const unsigned hit = __ballot_sync(~0u, i + lane < p.rows && w.parent[min(i + lane, p.rows - 1)] == at);
+      if (hit) {
+        i += __ffs(hit) - 1;
+        break;
       }
     }
+    if (i >= p.rows) break;
+    const int c = i++;
+    int verdict = w.verdict[c];
+    if (!greedy && (k || summed)) {
+      verdict = kClose;
+      if (!draft && !summed) {                         // a guess behind rejected ones: by what these leave of the 32-bit sum
+        const double e = w.e[c], s32 = (double)w.s[at], s = s32 - gone;
+        bool before = false;
+        for (int j = 0; j < k; j++) before |= w.out[j] == w.token[c];
+        if (before) verdict = kReject;
+        else if (s > s32 / 1024 && fabs(w.uq[c] * s - e) * s > kNear * e * s32) verdict = w.uq[c] * s < e ? kAccept : kReject;
+      }
+    }
+    if (verdict == kClose) {
+      sum_up(draft && k);
+      double v[1] = {w.e[c]};
+      const float qt[1] = {w.q[c]};
+      for (int n = 0; n < k; n++) reject(v, qt, w, draft, n, w.token[c]);
+      verdict = w.uq[c] * total < v[0] ? kAccept : kReject;
+    }
+    const bool accept = verdict == kAccept;
     if (accept) {
-      if (tells) keep[kept] = len + i;
+      if (tells) keep[kept] = len + c;
       kept++;
-      enter(i);
-      ok = valid(i);
+      enter(c);
+      ok = valid(c);
     } else if (!greedy) {
       if (draft) {
-        sum_up();
+        sum_up(true);
         __syncthreads();
         if (threadIdx.x == 0) w.inv[k] = 1.0 / total;
       } else {
         bool before = false;
-        for (int j = 0; j < k; j++) before |= w.out[j] == w.token[i];
-        if (!before) gone += exp(((double)w.x[i] - of.m) * of.inv_t);
+        for (int j = 0; j < k; j++) before |= w.out[j] == w.token[c];
+        if (!before) gone += w.e[c];
         __syncthreads();
-        if (threadIdx.x == 0) w.out[k] = w.token[i];
+        if (threadIdx.x == 0) w.out[k] = w.token[c];
       }
       __syncthreads();
-      of.k = ++k;
+      ++k;
       summed = false;
     }
   }
@@ -354,44 +437,35 @@ __global__ void __launch_bounds__(kThreads, 1) walk_kernel(const VerifyParams p)
     return;
   }
   // the token: the block, the run and the place where the running sum passes the given number
-  sum_up();
-  const double want = (double)w.u[0] * total;
-  double before = 0.0, sum = 0.0;
-  int block = 0;
-  {
-    double run_sum = 0.0, last_before = 0.0;
-    int last = 0, found = -1;
-    for (int j = 0; j < p.cluster && found < 0; j++) {
-      const double b = w.block[parity][j];
-      if (run_sum + b > want) found = j, before = run_sum;
-      if (b > 0.0) last = j, last_before = run_sum;
-      run_sum += b;
+  sum_up(draft && k);
+  const double want = (double)p.u[seq * p.rows] * total;
+  double before = 0.0;
+  // the first of n sums with which the running sum passes the number, or the last with a weight; `before`: what is in front of it
+  const auto find = [&](const double* sums, int n) {
+    const double b = lane < n ? sums[lane] : 0.0;
+    double c = b;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const double y = __shfl_up_sync(~0u, c, o);
+      if (lane >= o) c += y;
     }
-    block = found < 0 ? last : found;
-    if (found < 0) before = last_before;
-  }
-  if (rank != block) return;
-  int mine = 0;
-  {
-    double last_before = before;
-    int last = 0, found = -1;
-    sum = before;
-    for (int j = 0; j < kWarps && found < 0; j++) {
-      const double b = w.run[j];
-      if (sum + b > want) found = j, before = sum;
-      if (b > 0.0) last = j, last_before = sum;
-      sum += b;
-    }
-    mine = found < 0 ? last : found;
-    if (found < 0) before = last_before;
-  }
-  const int from = begin + mine * run, to = min(from + run, end);
+    const unsigned over = __ballot_sync(~0u, b > 0.0 && before + c > want), some = __ballot_sync(~0u, b > 0.0);
+    const int j = over ? __ffs(over) - 1 : some ? 31 - __clz(some) : 0;
+    const double in_front = __shfl_sync(~0u, c, j ? j - 1 : 0);
+    if (j) before += in_front;
+    return j;
+  };
+  if (rank != find(w.block[parity], p.cluster)) return;
+  const int mine = find(w.run, kWarps), first = begin + mine * run, behind = min(first + run, end);
+  __syncthreads();
   // all warps over the one run, 512 places at a time
   int last_positive = -1;
-  for (int i0 = from; i0 < to; i0 += kThreads) {
+  for (int i0 = first; i0 < behind; i0 += kThreads) {
     const int i = i0 + threadIdx.x;
-    const double v = i < to ? of(load(of.x, i), of.q && of.k ? load(of.q, i) : 0.f, i) : 0.0;
-    double c = v;
+    double v[1] = {i < behind ? e_of(load(x, i)) : 0.0};
+    const float qt[1] = {i < behind && draft && k ? __ldg(q + i) : 0.f};
+    for (int n = 0; n < k; n++) reject(v, qt, w, draft, n, i);
+    double c = v[0];
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const double y = __shfl_up_sync(~0u, c, o);
@@ -400,9 +474,16 @@ __global__ void __launch_bounds__(kThreads, 1) walk_kernel(const VerifyParams p)
     __syncthreads();
     if (lane == 31) w.run[warp] = c;
     __syncthreads();
-    double ahead = before;
-    for (int j = 0; j < warp; j++) ahead += w.run[j];
-    const unsigned over = __ballot_sync(~0u, v > 0.0 && ahead + c > want), some = __ballot_sync(~0u, v > 0.0);
+    double ahead = lane < kWarps ? w.run[lane] : 0.0;
+#pragma unroll
+    for (int o = 1; o < kWarps; o <<= 1) {
+      const double y = __shfl_up_sync(~0u, ahead, o);
+      if (lane >= o) ahead += y;
+    }
+    const double all = __shfl_sync(~0u, ahead, kWarps - 1);
+    ahead = __shfl_sync(~0u, ahead, warp ? warp - 1 : 0);
+    ahead = warp ? before + ahead : before;
+    const unsigned over = __ballot_sync(~0u, v[0] > 0.0 && ahead + c > want), some = __ballot_sync(~0u, v[0] > 0.0);
     if (lane == 0) {
       w.over[warp] = over ? i0 + warp * 32 + __ffs(over) - 1 : -1;
       w.positive[warp] = some ? i0 + warp * 32 + 31 - __clz(some) : -1;
@@ -417,23 +498,43 @@ __global__ void __launch_bounds__(kThreads, 1) walk_kernel(const VerifyParams p)
       if (threadIdx.x == 0) p.token[seq] = hit;
       return;
     }
-    for (int j = 0; j < kWarps; j++) before += w.run[j];
+    before += all;
   }
   if (threadIdx.x == 0) p.token[seq] = last_positive;
 }
 
 // ---- host -------------------------------------------------------------------------------------------------------
-cudaError_t allow_smem() {
-  static std::atomic<unsigned long long> done{0};
+// The walk's shared memory and clusters of 16 blocks, allowed once on each device; *room: whether such a cluster can run at all.
+template <class T>
+cudaError_t allow(bool* room) {
+  static std::atomic<unsigned long long> done{0}, large{0};
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   const unsigned long long bit = dev < 64 ? 1ull << dev : 0;
-  if (done.load(std::memory_order_acquire) & bit) return cudaSuccess;
-  e = cudaFuncSetAttribute(walk_kernel<float>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(Walk));
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(walk_kernel<unsigned short>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(Walk));
-  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_release);
-  return e;
+  if (!(done.load(std::memory_order_acquire) & bit)) {
+    e = cudaFuncSetAttribute(walk_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(Walk));
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(walk_kernel<T>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e != cudaSuccess) return e;
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = kMaxCluster, at.val.clusterDim.y = at.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(kMaxCluster), cfg.blockDim = dim3(kThreads), cfg.dynamicSmemBytes = sizeof(Walk);
+    cfg.attrs = &at, cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, walk_kernel<T>, &cfg) != cudaSuccess) (void)cudaGetLastError();
+    else if (n > 0) large.fetch_or(bit, std::memory_order_release);
+    done.fetch_or(bit, std::memory_order_release);
+  }
+  *room = large.load(std::memory_order_acquire) & bit;
+  return cudaSuccess;
+}
+
+// parts of a row; its first logit may stand up to seven places behind the 16-byte boundary that they are counted from
+int64_t parts_of(const amk_verify_args& a) {
+  const int64_t part = kStatThreads * kLoads * (a.dtype ? 8 : 4);
+  return (a.vocab + 7 + part - 1) / part;
 }
 
 // Everything about a call that can be known without its pointers.
@@ -445,13 +546,11 @@ amk_status check(const Reason& fail, const amk_verify_args* a) {
   if (a->n_rows < 1 || a->n_rows > AMK_TREE_MAX_ROWS)
     return fail(AMK_ERR_UNSUPPORTED, "%u rows: 1 to %d", a->n_rows, AMK_TREE_MAX_ROWS);
   if (a->vocab < 1 || a->vocab > 0x7fffffff - 65536) return fail(AMK_ERR_INVALID_ARG, "%lld logits a row", (long long)a->vocab);
-  const int64_t parts = (a->vocab + 7 + kPart - 1) / kPart;
+  const int64_t parts = parts_of(*a);
   if ((int64_t)a->n_seqs > 0x7fffffff / 16 || (int64_t)a->n_seqs * a->n_rows > 0x7fffffff / parts)
     return fail(AMK_ERR_INVALID_ARG, "%u sequences of %u rows", a->n_seqs, a->n_rows);
   return AMK_OK;
 }
-
-int64_t parts_of(const amk_verify_args& a) { return (a.vocab + 7 + kPart - 1) / kPart; }
 
 }  // namespace
 
@@ -486,7 +585,8 @@ extern "C" amk_status amk_verify_draft(const amk_verify_args* args, char* msg, s
   if (!a.workspace || a.workspace_bytes < need)
     return fail(AMK_ERR_INVALID_ARG, "workspace of %llu bytes, %zu are needed",
                 (unsigned long long)(a.workspace ? a.workspace_bytes : 0), need);
-  cudaError_t e = allow_smem();
+  bool room = false;
+  cudaError_t e = a.dtype ? allow<unsigned short>(&room) : allow<float>(&room);
   if (e != cudaSuccess) return fail(AMK_ERR_CUDA, "%s", cudaGetErrorString(e));
   VerifyParams p{};
   p.logits = a.logits, p.draft = a.draft, p.tokens = a.tokens, p.parents = a.parents, p.u = a.uniforms;
@@ -497,10 +597,10 @@ extern "C" amk_status amk_verify_draft(const amk_verify_args* args, char* msg, s
   p.rows = (int)a.n_rows, p.vocab = (int)a.vocab, p.parts = (int)parts;
   const int sms = multiprocessors();
   p.cluster = 1;
-  while (p.cluster < 8 && (int64_t)a.n_seqs * p.cluster * 2 <= sms && a.vocab / (2 * p.cluster) >= 1024) p.cluster *= 2;
+  while (p.cluster < (room ? kMaxCluster : 8) && (int64_t)a.n_seqs * p.cluster * 2 <= sms && a.vocab / (2 * p.cluster) >= 1024) p.cluster *= 2;
   const cudaStream_t st = (cudaStream_t)cuda_stream;
   const unsigned stat_blocks = (unsigned)((int64_t)a.n_seqs * a.n_rows * parts), walk_blocks = a.n_seqs * (unsigned)p.cluster;
-  e = launch_early(a.dtype ? stats_kernel<unsigned short> : stats_kernel<float>, dim3(stat_blocks), kThreads, 0, 1, st, p);
+  e = launch_early(a.dtype ? stats_kernel<unsigned short> : stats_kernel<float>, dim3(stat_blocks), kStatThreads, 0, 1, st, p);
   if (e == cudaSuccess)
     e = launch_early(a.dtype ? walk_kernel<unsigned short> : walk_kernel<float>, dim3(walk_blocks), kThreads, sizeof(Walk),
                      (unsigned)p.cluster, st, p);
