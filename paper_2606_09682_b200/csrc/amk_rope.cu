@@ -28,14 +28,14 @@ struct RopeParams {
   int64_t q_row, q_head, k_row, k_head, v_row, v_head, qo_row, qo_head, ko_row, ko_head;
   int64_t kc_seq, kc_head, kc_row, vc_seq, vc_head, vc_row;
   int64_t rows, all_slots;
-  int nq, nkv, heads;              // heads: of q, of k and, with a cache, of v
+  int nq, nkv;
   unsigned slots_of;               // rows of a cache
   int split;                       // warps that share a token
   float eps;
   double turns[64];                // f_i
 };
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 128, kBlocks = 5, kAhead = 8;   // kAhead: places for steps on their way, one of them the step at hand
 
 __device__ __forceinline__ unsigned pack_bf16(float lo, float hi) {
   unsigned r;
@@ -66,98 +66,167 @@ __device__ __forceinline__ void store(void* cache, int64_t at, const float (&x)[
     *(uint4*)((unsigned short*)cache + at) = narrow(x);
 }
 
+// What a head's elements are multiplied with: z[i] = f (x lo_x[i] - y lo_y[i]), z[i + hd/2] = f (y hi_y[i] + x hi_x[i]) for x, y the
+// elements i and i + hd/2 and f the norm's factor; two at a time.
+struct Turn {
+  uint64_t lo_x[4], lo_y[4], hi_y[4], hi_x[4];
+  // from the cosines and sines and the weights (null: 1)
+  __device__ __forceinline__ void set(const float (&c)[8], const float (&s)[8], const uint4* weight, int l, int half) {
+    float a[8], b[8];
+#pragma unroll
+    for (int j = 0; j < 8; j++) a[j] = b[j] = 1.f;
+    if (weight) widen(a, __ldg(weight + l)), widen(b, __ldg(weight + half + l));
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+      lo_x[j] = amk::pair(c[2 * j] * a[2 * j], c[2 * j + 1] * a[2 * j + 1]);
+      lo_y[j] = amk::pair(-s[2 * j] * b[2 * j], -s[2 * j + 1] * b[2 * j + 1]);
+      hi_y[j] = amk::pair(c[2 * j] * b[2 * j], c[2 * j + 1] * b[2 * j + 1]);
+      hi_x[j] = amk::pair(s[2 * j] * a[2 * j], s[2 * j + 1] * a[2 * j + 1]);
+    }
+  }
+};
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ void widen2(uint64_t (&x)[4], const uint4& u) {
+  const unsigned w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int i = 0; i < 4; i++) x[i] = amk::pair(amk::bf16_lo(w[i]), amk::bf16_hi(w[i]));
+}
+
+__device__ __forceinline__ void copy_async(void* dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(amk::smem_u32(dst)), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 2) : "memory"); }
+
 template <int HD, bool FP8>
-__global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ RopeParams p) {
-  constexpr int kLanes = HD / 16, kGroups = 32 / kLanes, kOwn = 8 / kGroups;   // lanes of a head, heads of a warp, angles a lane makes
-  constexpr int kBatch = 4;                                                    // heads under way, times kGroups
-  const int lane = threadIdx.x & 31, l = lane % kLanes, g = lane / kLanes;
-  const int64_t w = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
-  const int64_t row = p.split == 1 ? w : w / p.split;
-  const int part = (int)(w - row * p.split);
+__global__ void __launch_bounds__(kThreads, kBlocks) rope_kernel(const __grid_constant__ RopeParams p) {
+  constexpr int kLanes = HD / 16, kGroups = 32 / kLanes, kOwn = 8 / kGroups;   // lanes of a head, heads of a step, angles a lane makes
+  // what is on its way: every lane brings its own elements and reads them itself
+  __shared__ uint4 held[kThreads / 32][kAhead][2][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l = lane % kLanes, g = lane / kLanes, e = 8 * l;
+  const int64_t w = (int64_t)blockIdx.x * (kThreads / 32) + warp;
+  const int64_t first = p.split == 1 ? w : w / p.split, next = (int64_t)gridDim.x * (kThreads / 32) / p.split;   // (split > 1: one row each)
+  const int part = (int)(w - first * p.split);
   amk::wait_for_grid_before();
-  if (row >= p.rows) return;
-  float c[8], s[8];
-  {
-    const double n = (double)p.positions[row];
-    float cc[kOwn], ss[kOwn];
-#pragma unroll
-    for (int j = 0; j < kOwn; j++) {
-      double t = n * p.turns[8 * l + g * kOwn + j];
-      t -= rint(t);
-      sincospif(2.f * (float)t, &ss[j], &cc[j]);
+  // The steps of a token, kGroups heads each, queries, keys and values, in turn for the warps that share it.
+  const int q_steps = (p.nq + kGroups - 1) / kGroups, k_steps = (p.nkv + kGroups - 1) / kGroups;
+  const int steps = q_steps + (p.k_cache ? 2 : 1) * k_steps;
+  int64_t asked_row = first;
+  int asked = part, put = 0;                           // the next step to ask for, and where it goes
+  const auto ask = [&]() {
+    if (asked_row < p.rows) {
+      const int kind = asked < q_steps ? 0 : asked < q_steps + k_steps ? 1 : 2;
+      const int h = (asked - (kind == 0 ? 0 : kind == 1 ? q_steps : q_steps + k_steps)) * kGroups + g;
+      if (h < (kind == 0 ? p.nq : p.nkv)) {
+        const unsigned short* x = (kind == 0   ? p.q + asked_row * p.q_row + h * p.q_head
+                                   : kind == 1 ? p.k + asked_row * p.k_row + h * p.k_head
+                                               : p.v + asked_row * p.v_row + h * p.v_head) + e;
+        copy_async(&held[warp][put][0][lane], x), copy_async(&held[warp][put][1][lane], x + HD / 2);
+      }
+      asked += p.split;
+      if (asked >= steps) asked = part, asked_row += next;
     }
+    copies_end();
+    put = put + 1 == kAhead ? 0 : put + 1;
+  };
+  if (part >= steps) return;
+#pragma unroll 1
+  for (int i = 0; i < kAhead - 1; i++) ask();
+  int get = 0;
+#pragma unroll 1
+  for (int64_t row = first; row < p.rows; row += next) {
+    float c[8], s[8];
+    {
+      const double n = (double)p.positions[row];
+      float cc[kOwn], ss[kOwn];
 #pragma unroll
-    for (int j = 0; j < 8; j++) {
-      c[j] = __shfl_sync(~0u, cc[j % kOwn], j / kOwn * kLanes + l);
-      s[j] = __shfl_sync(~0u, ss[j % kOwn], j / kOwn * kLanes + l);
-    }
-  }
-  int64_t kc = -1, vc = 0;                             // the token's row in the caches
-  if (p.k_cache) {
-    const int64_t slot = p.slots[row];
-    if (slot >= 0 && slot < p.all_slots) {
-      const int64_t seq = p.all_slots <= 0xffffffffll ? (unsigned)slot / p.slots_of : slot / p.slots_of;
-      const int64_t at = slot - seq * p.slots_of;
-      kc = seq * p.kc_seq + at * p.kc_row, vc = seq * p.vc_seq + at * p.vc_row;
-    }
-  }
-  const int e = 8 * l;
-  for (int h0 = part * kGroups + g; h0 - g < p.heads; h0 += kBatch * p.split * kGroups) {
-    uint4 lo[kBatch], hi[kBatch];
+      for (int j = 0; j < kOwn; j++) {
+        double t = n * p.turns[8 * l + g * kOwn + j];
+        t -= rint(t);
+        sincospif(2.f * (float)t, &ss[j], &cc[j]);
+      }
 #pragma unroll
-    for (int b = 0; b < kBatch; b++) {
-      const int h = h0 + b * p.split * kGroups;
-      lo[b] = hi[b] = make_uint4(0, 0, 0, 0);
-      if (h < p.heads) {
-        const unsigned short* x = h < p.nq              ? p.q + row * p.q_row + h * p.q_head
-                                  : h < p.nq + p.nkv ? p.k + row * p.k_row + (h - p.nq) * p.k_head
-                                                     : p.v + row * p.v_row + (h - p.nq - p.nkv) * p.v_head;
-        lo[b] = *(const uint4*)(x + e), hi[b] = *(const uint4*)(x + HD / 2 + e);
+      for (int j = 0; j < 8; j++) {
+        c[j] = __shfl_sync(~0u, cc[j % kOwn], j / kOwn * kLanes + l);
+        s[j] = __shfl_sync(~0u, ss[j % kOwn], j / kOwn * kLanes + l);
       }
     }
-#pragma unroll
-    for (int b = 0; b < kBatch; b++) {
-      const int h = h0 + b * p.split * kGroups;
-      if (h - g >= p.heads) break;
-      float x[8], y[8];
-      widen(x, lo[b]), widen(y, hi[b]);
-      if (h - g < p.nq + p.nkv && (p.q_weight || p.k_weight)) {
-        float sum = 0.f;
-#pragma unroll
-        for (int j = 0; j < 8; j++) sum = fmaf(x[j], x[j], fmaf(y[j], y[j], sum));
-#pragma unroll
-        for (int o = kLanes / 2; o; o /= 2) sum += __shfl_xor_sync(~0u, sum, o);
-        const uint4* weight = h < p.nq ? p.q_weight : h < p.nq + p.nkv ? p.k_weight : nullptr;
+    int64_t kc = -1, vc = 0;                             // the token's row in the caches
+    if (p.k_cache) {
+      const int64_t slot = p.slots[row];
+      if (slot >= 0 && slot < p.all_slots) {
+        const int64_t seq = p.all_slots <= 0xffffffffll ? (unsigned)slot / p.slots_of : slot / p.slots_of;
+        const int64_t at = slot - seq * p.slots_of;
+        kc = seq * p.kc_seq + at * p.kc_row + e, vc = seq * p.vc_seq + at * p.vc_row + e;
+      }
+    }
+    Turn turn;
+    int step = part;
+#pragma unroll 1
+    for (int kind = 0; kind < 3; kind++) {               // queries, keys, values
+      const int before = kind == 0 ? 0 : kind == 1 ? q_steps : q_steps + k_steps, end = kind == 0 ? q_steps : kind == 1 ? before + k_steps : steps;
+      if (step >= end) continue;
+      const int heads = kind == 0 ? p.nq : p.nkv;
+      const uint4* weight = kind == 0 ? p.q_weight : p.k_weight;
+      if (kind < 2) turn.set(c, s, weight, l, HD / 16);
+      unsigned short* out = kind == 0 ? p.q_out + row * p.qo_row + e : kind == 1 && p.k_out ? p.k_out + row * p.ko_row + e : nullptr;
+      const int64_t out_head = kind == 0 ? p.qo_head : p.ko_head;
+      void* cache = kind == 0 || kc < 0 ? nullptr : kind == 1 ? p.k_cache : p.v_cache;
+      const int64_t cache_at = kind == 1 ? kc : vc, cache_head = kind == 1 ? p.kc_head : p.vc_head;
+#pragma unroll 1
+      for (; step < end; step += p.split) {
+        copies_wait();
+        const int h = (step - before) * kGroups + g;
+        uint4 lo = held[warp][get][0][lane], hi = held[warp][get][1][lane];
+        get = get + 1 == kAhead ? 0 : get + 1;
+        ask();                                           // (into the place of the step before this one)
+        if (kind == 2) {
+          if (h < heads && cache) {
+            const int64_t at = cache_at + h * cache_head;
+            if (FP8) {
+              float x[8], y[8];
+              widen(x, lo), widen(y, hi);
+              store<FP8>(cache, at, x), store<FP8>(cache, at + HD / 2, y);
+            } else {                                     // (the bits as they are)
+              *(uint4*)((unsigned short*)cache + at) = lo, *(uint4*)((unsigned short*)cache + at + HD / 2) = hi;
+            }
+          }
+          continue;
+        }
+        uint64_t x[4], y[4];
+        widen2(x, lo), widen2(y, hi);
         if (weight) {
-          const float f = 1.f / sqrtf(fmaf(sum, 1.f / HD, p.eps));
-          float wx[8], wy[8];
-          widen(wx, __ldg(weight + l)), widen(wy, __ldg(weight + HD / 16 + l));
+          uint64_t sums = mul2(x[0], x[0]), more = mul2(y[0], y[0]);
 #pragma unroll
-          for (int j = 0; j < 8; j++) x[j] *= f * wx[j], y[j] *= f * wy[j];
-        }
-      }
-      if (h >= p.heads) continue;
-      if (h < p.nq + p.nkv) {
+          for (int j = 1; j < 4; j++) sums = amk::fma2(x[j], x[j], sums), more = amk::fma2(y[j], y[j], more);
+          float a, sum;
+          amk::unpair(a, sum, amk::add2(sums, more));
+          sum += a;
 #pragma unroll
-        for (int j = 0; j < 8; j++) {
-          const float a = x[j], d = y[j];
-          x[j] = fmaf(a, c[j], -(d * s[j]));
-          y[j] = fmaf(d, c[j], a * s[j]);
+          for (int o = kLanes / 2; o; o /= 2) sum += __shfl_xor_sync(~0u, sum, o);
+          const float f = rsqrtf(fmaf(sum, 1.f / HD, p.eps));
+          const uint64_t f2 = amk::pair(f, f);
+#pragma unroll
+          for (int j = 0; j < 4; j++) x[j] = mul2(x[j], f2), y[j] = mul2(y[j], f2);
         }
-        unsigned short* out = h < p.nq ? p.q_out + row * p.qo_row + h * p.qo_head
-                                       : p.k_out ? p.k_out + row * p.ko_row + (h - p.nq) * p.ko_head : nullptr;
-        if (out) *(uint4*)(out + e) = narrow(x), *(uint4*)(out + HD / 2 + e) = narrow(y);
-        if (h >= p.nq && kc >= 0) {
-          const int64_t at = kc + (h - p.nq) * p.kc_head + e;
-          store<FP8>(p.k_cache, at, x), store<FP8>(p.k_cache, at + HD / 2, y);
+        if (h >= heads) continue;
+        float z[8], t[8];
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+          amk::unpair(z[2 * j], z[2 * j + 1], amk::fma2(x[j], turn.lo_x[j], mul2(y[j], turn.lo_y[j])));
+          amk::unpair(t[2 * j], t[2 * j + 1], amk::fma2(y[j], turn.hi_y[j], mul2(x[j], turn.hi_x[j])));
         }
-      } else if (kc >= 0) {
-        const int64_t at = vc + (h - p.nq - p.nkv) * p.vc_head + e;
-        if (FP8) {
-          store<FP8>(p.v_cache, at, x), store<FP8>(p.v_cache, at + HD / 2, y);
-        } else {                                       // (the bits as they are)
-          *(uint4*)((unsigned short*)p.v_cache + at) = lo[b];
-          *(uint4*)((unsigned short*)p.v_cache + at + HD / 2) = hi[b];
+        if (out) {
+          unsigned short* to = out + h * out_head;
+          *(uint4*)to = narrow(z), *(uint4*)(to + HD / 2) = narrow(t);
+        }
+        if (cache) {
+          const int64_t at = cache_at + h * cache_head;
+          store<FP8>(cache, at, z), store<FP8>(cache, at + HD / 2, t);
         }
       }
     }
@@ -228,15 +297,18 @@ extern "C" amk_status amk_norm_rope_append(const amk_rope_args* args, char* msg,
   p.qo_row = a.qo_row, p.qo_head = a.qo_head, p.ko_row = a.ko_row, p.ko_head = a.ko_head;
   p.kc_seq = a.kc_seq, p.kc_head = a.kc_head, p.kc_row = a.kc_row, p.vc_seq = a.vc_seq, p.vc_head = a.vc_head, p.vc_row = a.vc_row;
   p.rows = a.rows, p.all_slots = cached ? (int64_t)a.n_seqs * a.n_slots : 0, p.slots_of = a.n_slots;
-  p.nq = (int)nq, p.nkv = (int)nkv, p.heads = (int)(nq + nkv + (cached ? nkv : 0));
+  p.nq = (int)nq, p.nkv = (int)nkv;
   p.eps = a.eps;
   const long double step = powl((long double)a.theta, -2.0L / hd);
   long double f = 0.15915494309189533576888376337251436L;               // 1 / 2 pi
   for (int i = 0; i < hd / 2; i++, f *= step) p.turns[i] = (double)f;
   // a token's heads over several warps until there are 32 warps for each SM
-  const int64_t steps = (p.heads + 512 / hd - 1) / (512 / hd), want = (32ll * amk::multiprocessors() + a.rows - 1) / a.rows;
+  const int64_t group = 512 / hd, kv_steps = (nkv + group - 1) / group;
+  const int64_t steps = (nq + group - 1) / group + kv_steps * (cached ? 2 : 1), want = (32ll * amk::multiprocessors() + a.rows - 1) / a.rows;
   p.split = (int)(steps < want ? steps : want);
-  const int64_t blocks = (a.rows * p.split + kThreads / 32 - 1) / (kThreads / 32);
+  // what is resident at once; a warp goes on to further rows
+  const int64_t most = kBlocks * (int64_t)amk::multiprocessors(), need = (a.rows * p.split + kThreads / 32 - 1) / (kThreads / 32);
+  const int64_t blocks = p.split > 1 || need < most ? need : most;
   const cudaStream_t st = (cudaStream_t)cuda_stream;
   const auto kernel = hd == 64 ? (esz == 1 ? rope_kernel<64, true> : rope_kernel<64, false>)
                                : (esz == 1 ? rope_kernel<128, true> : rope_kernel<128, false>);
