@@ -4,8 +4,9 @@
 // stay anyway hold the largest key) is found digit by digit from histograms of 11, 11 and 10 bits; then the positions whose key
 // is larger stay, and of those with that very key the first ones.  Counts are integers: the result is the same every time.
 //
-// Bound: latency, three histograms and their sums of a few thousand keys that lie in shared memory; lists longer than that are
-// read again from L2 in the histograms, and chosen from in pieces.
+// Bound: the instructions of a few sweeps over keys that lie in shared memory, four to a thread at a time (a ballot for every 32 of
+// them instead: 256 lists of 8192 25.2 us, so XXX), and with few lists the barriers between the sweeps.  Lists of more than
+// 32768 scores are read again from L2 in the histograms, and chosen from in pieces.
 #include <cuda_runtime.h>
 
 #include <atomic>
@@ -18,7 +19,8 @@
 namespace {
 
 constexpr int kThreads = 1024, kWarps = kThreads / 32, kBins = 2048;
-constexpr int kPiece = 49152;                          // scores in shared memory at most
+constexpr int kSweep = 4 * kThreads;                   // keys of a sweep's round
+constexpr int kPiece = 32768;                          // keys in shared memory at most, a multiple of kSweep
 
 struct EvictParams {
   const float* scores;
@@ -37,9 +39,11 @@ __device__ __forceinline__ unsigned key_of(unsigned bits) {
 }
 
 __global__ void __launch_bounds__(kThreads) evict_kernel(const EvictParams p) {
-  extern __shared__ unsigned held[];
+  extern __shared__ uint4 smem[];
+  unsigned* keys = (unsigned*)smem;                    // of a piece; 0 behind its end, which the order puts last
+  unsigned short* chosen = (unsigned short*)(keys + p.piece);
   __shared__ unsigned bins[kBins], digit[2];
-  __shared__ int warp_a[kWarps], warp_b[kWarps];
+  __shared__ unsigned sums[kWarps];
   const int list = blockIdx.x, s = list / p.heads, h = list - s * p.heads;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const unsigned* in = (const unsigned*)p.scores + s * p.seq + h * p.head;
@@ -54,107 +58,136 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(const EvictParams p) {
       for (int i = threadIdx.x; i < p.slots; i += kThreads) out[i] = in[i];
     return;
   }
-  const bool all = n <= p.budget, whole = n <= p.piece;
-  unsigned border = 0;                                 // keys above it stay, and `equal` of those that have it
-  int equal = n;
-  if (!all) {
-    if (whole) {
-      for (int i = threadIdx.x; i < n; i += kThreads) held[i] = in[i];
-    }
-    int left = p.budget;
-    unsigned above = 0;                                // the digits found so far
-#pragma unroll 1
-    for (int pass = 0; pass < 3; pass++) {
-      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, width = pass == 2 ? 1024 : 2048;
-      for (int i = threadIdx.x; i < kBins; i += kThreads) bins[i] = 0;
-      __syncthreads();
-      for (int i = threadIdx.x; i < n; i += kThreads) {
-        const unsigned key = i < p.first || i >= n - p.recent ? ~0u : key_of(whole ? held[i] : in[i]);
-        if (pass == 0 || key >> (pass == 1 ? 21 : 10) == above) atomicAdd(&bins[key >> shift & (width - 1)], 1u);
-      }
-      __syncthreads();
-      // the digit: the largest one at or above which `left` keys lie.  Two bins a thread, from the largest down.
-      const int top = kBins - 1 - 2 * (int)threadIdx.x;
-      const int a = (int)bins[top], b = (int)bins[top - 1];
-      int sum = a + b;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int x = __shfl_up_sync(~0u, sum, o);
-        if (lane >= o) sum += x;
-      }
-      if (lane == 31) warp_a[warp] = sum;
-      __syncthreads();
-      const int own = warp_a[lane];                    // (32 warps, 32 lanes)
-      sum += __reduce_add_sync(~0u, lane < warp ? own : 0);
-      const int before = sum - a - b;
-      if (before < left && before + a >= left) digit[0] = top, digit[1] = before;
-      if (before + a < left && sum >= left) digit[0] = top - 1, digit[1] = before + a;
-      __syncthreads();
-      above = above << (pass == 2 ? 10 : 11) | digit[0];
-      left -= (int)digit[1];
-    }
-    border = above;
-    equal = left;
-  }
-  // which ones stay, piece by piece in ascending order; a warp has a run of a piece.  A piece is in shared memory before any of
-  // its rows moves, and rows move down only: `moved` may be the scores themselves.
-  int kept = 0, same = 0;                              // so far, among all keys / among those of the border
-  const int per_piece = all ? n : p.piece;
-  for (int from = 0; from < n && !all; from += per_piece) {
-    const int m = min(per_piece, n - from), run = ((m + kWarps - 1) / kWarps + 31) & ~31;
-    if (!whole) {
-      __syncthreads();
-      for (int i = threadIdx.x; i < m; i += kThreads) held[i] = in[from + i];
-      __syncthreads();
-    }
-    const int begin = min(warp * run, m), end = min(begin + run, m);
-    int more = 0, ties = 0;
-    for (int i = begin + lane; i < end; i += 32) {
-      const int at = from + i;
-      const unsigned key = at < p.first || at >= n - p.recent ? ~0u : key_of(held[i]);
-      more += key > border, ties += key == border;
-    }
-    more = __reduce_add_sync(~0u, more), ties = __reduce_add_sync(~0u, ties);
-    __syncthreads();
-    if (lane == 0) warp_a[warp] = more, warp_b[warp] = ties;
-    __syncthreads();
-    const int wa = warp_a[lane], wb = warp_b[lane];
-    const int more_before = __reduce_add_sync(~0u, lane < warp ? wa : 0), all_more = __reduce_add_sync(~0u, wa);
-    int tie = same + __reduce_add_sync(~0u, lane < warp ? wb : 0);
-    const int all_ties = __reduce_add_sync(~0u, wb);
-    // kept holds min(same, equal) ties
-    int place = kept + more_before + min(tie, equal) - min(same, equal);
-    for (int i0 = begin; i0 < end; i0 += 32) {
-      const int i = i0 + lane, at = from + i;
-      unsigned bits = 0, key = 0;
-      if (i < end) {
-        bits = held[i];
-        key = at < p.first || at >= n - p.recent ? ~0u : key_of(bits);
-      }
-      const unsigned over = __ballot_sync(~0u, i < end && key > border), eq = __ballot_sync(~0u, i < end && key == border);
-      const unsigned below = (1u << lane) - 1u;
-      const bool stays = (over >> lane & 1) || ((eq >> lane & 1) && tie + __popc(eq & below) < equal);
-      const unsigned in_all = __ballot_sync(~0u, stays);
-      if (stays) {
-        const int to = place + __popc(in_all & below);
-        keep[to] = at;
-        if (out) out[to] = bits;
-      }
-      place += __popc(in_all), tie += __popc(eq);
-    }
-    kept += all_more + min(same + all_ties, equal) - min(same, equal);
-    same += all_ties;
-  }
-  const int count = all ? n : p.budget;
-  if (all)
+  const int count = min(n, p.budget);
+  if (threadIdx.x == 0) p.count[list] = count;
+  for (int i = count + threadIdx.x; i < p.budget; i += kThreads) keep[i] = -1;
+  if (n <= p.budget) {
     for (int i = threadIdx.x; i < n; i += kThreads) {
       keep[i] = i;
       if (out && out != in) out[i] = in[i];
     }
-  if (threadIdx.x == 0) p.count[list] = count;
-  for (int i = count + threadIdx.x; i < p.budget; i += kThreads) keep[i] = -1;
+    if (out)
+      for (int i = n + threadIdx.x; i < p.slots; i += kThreads) out[i] = 0;
+    return;
+  }
+  const auto key_at = [&](int i) { return i < p.first || i >= n - p.recent ? ~0u : key_of(in[i]); };
+  const auto bring = [&](int from) {                   // the keys of a piece; its rounds
+    const int m = min(p.piece, n - from), rounds = (m + kSweep - 1) / kSweep;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < rounds * kSweep; i += kThreads) keys[i] = i < m ? key_at(from + i) : 0;
+    return rounds;
+  };
+  const bool whole = n <= p.piece;
+  int rounds = 0;
+  for (int i = threadIdx.x; i < kBins; i += kThreads) bins[i] = 0;
+  if (whole) rounds = bring(0);
+  // keys above the border stay, and `equal` of those that have it
+  unsigned border = 0;
+  int equal = p.budget;
+#pragma unroll 1
+  for (int pass = 0; pass < 3; pass++) {
+    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, width = pass == 2 ? 1023 : 2047;
+    const auto count_key = [&](unsigned key) {
+      if (pass == 0 || key >> (pass == 1 ? 21 : 10) == border) atomicAdd(&bins[key >> shift & width], 1u);
+    };
+    __syncthreads();
+    if (whole) {
+      for (int r = 0; r < rounds; r++) {
+        const uint4 k = smem[r * kThreads + threadIdx.x];
+        count_key(k.x), count_key(k.y), count_key(k.z), count_key(k.w);
+      }
+    } else {
+#pragma unroll 4
+      for (int i = threadIdx.x; i < n; i += kThreads) count_key(key_at(i));
+    }
+    __syncthreads();
+    // the digit: the largest one at or above which `equal` keys lie.  Two bins a thread, from the largest down.
+    const int top = kBins - 1 - 2 * (int)threadIdx.x;
+    const int a = (int)bins[top], b = (int)bins[top - 1];
+    bins[top] = bins[top - 1] = 0;
+    int sum = a + b;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(~0u, sum, o);
+      if (lane >= o) sum += x;
+    }
+    if (lane == 31) sums[warp] = (unsigned)sum;
+    __syncthreads();
+    const int own = (int)sums[lane];                   // (32 warps, 32 lanes)
+    sum += __reduce_add_sync(~0u, lane < warp ? own : 0);
+    const int before = sum - a - b;
+    if (before < equal && before + a >= equal) digit[0] = (unsigned)top, digit[1] = (unsigned)before;
+    if (before + a < equal && sum >= equal) digit[0] = (unsigned)top - 1, digit[1] = (unsigned)(before + a);
+    __syncthreads();
+    border = border << (pass == 2 ? 10 : 11) | digit[0];
+    equal -= (int)digit[1];
+  }
+  // Which ones stay, piece by piece in ascending order, a run of a piece for each warp.  Counts of keys above the border stand in
+  // the upper half of a word, of those that have it in the lower half.  Rows move down only, and all scores of 1024 rows are read
+  // before one of them is written: `moved` may be the scores themselves.
+  int above = 0, same = 0;                             // in the pieces in front
+  for (int from = 0; from < n; from += p.piece) {
+    if (!whole) {
+      __syncthreads();
+      rounds = bring(from);
+      __syncthreads();
+    }
+    const auto packed = [&](unsigned key) { return key > border ? 0x10000u : key == border ? 1u : 0u; };
+    const uint4* mine = smem + warp * rounds * 32 + lane;
+    unsigned all = 0;
+    for (int r = 0; r < rounds; r++) {
+      const uint4 k = mine[r * 32];
+      all += packed(k.x) + packed(k.y) + packed(k.z) + packed(k.w);
+    }
+    all = __reduce_add_sync(~0u, all);
+    __syncthreads();
+    if (lane == 0) sums[warp] = all;
+    __syncthreads();
+    const unsigned own = sums[lane], total = __reduce_add_sync(~0u, own);
+    unsigned run = __reduce_add_sync(~0u, lane < warp ? own : 0);
+    const int base = above + min(same, equal);         // rows that stay in the pieces in front
+    for (int r = 0; r < rounds; r++) {
+      const uint4 k = mine[r * 32];
+      const unsigned c[4] = {packed(k.x), packed(k.y), packed(k.z), packed(k.w)};
+      const unsigned four = c[0] + c[1] + c[2] + c[3];
+      unsigned scan = four;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const unsigned x = __shfl_up_sync(~0u, scan, o);
+        if (lane >= o) scan += x;
+      }
+      unsigned at = run + scan - four;
+      run += __shfl_sync(~0u, scan, 31);
+      if (four) {
+        const int i = ((warp * rounds + r) * 32 + lane) * 4;
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+          const int ties = same + (int)(at & 0xffffu);
+          if (c[j] > 1 || (c[j] && ties < equal)) chosen[above + (int)(at >> 16) + min(ties, equal) - base] = (unsigned short)(i + j);
+          at += c[j];
+        }
+      }
+    }
+    above += (int)(total >> 16), same += (int)(total & 0xffffu);
+    const int rows = above + min(same, equal) - base;
+    __syncthreads();
+    for (int i0 = 0; i0 < rows; i0 += kThreads) {
+      const int i = i0 + threadIdx.x;
+      int row = 0;
+      unsigned bits = 0;
+      if (i < rows) {
+        row = from + chosen[i];
+        if (out) bits = in[row];
+      }
+      if (out == in) __syncthreads();
+      if (i < rows) {
+        keep[base + i] = row;
+        if (out) out[base + i] = bits;
+      }
+    }
+  }
   if (out) {
-    __syncthreads();                                   // (in place: every piece has been read)
+    if (out == in) __syncthreads();                    // (every row has been read)
     for (int i = count + threadIdx.x; i < p.slots; i += kThreads) out[i] = 0;
   }
 }
@@ -166,7 +199,7 @@ cudaError_t allow_smem() {
   if (e != cudaSuccess) return e;
   const unsigned long long bit = dev < 64 ? 1ull << dev : 0;
   if (done.load(std::memory_order_acquire) & bit) return cudaSuccess;
-  e = cudaFuncSetAttribute(evict_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPiece * 4);
+  e = cudaFuncSetAttribute(evict_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPiece * 6);
   if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_release);
   return e;
 }
@@ -201,10 +234,10 @@ extern "C" amk_status amk_evict_select(const float* scores, int64_t n_seqs, int6
     return fail(AMK_ERR_INVALID_ARG, "moved is scores, but at other strides");
   cudaError_t e = allow_smem();
   if (e != cudaSuccess) return fail(AMK_ERR_CUDA, "%s", cudaGetErrorString(e));
-  const int piece = (int)(n_slots < kPiece ? n_slots : kPiece);
+  const int piece = n_slots < kPiece ? ((int)n_slots + kSweep - 1) / kSweep * kSweep : kPiece;
   const EvictParams p{scores, moved, lens, keep, count, scores_seq, scores_head, moved_seq, moved_head, (int)n_heads,
                       (int)n_slots, (int)budget, (int)first, (int)recent, piece};
-  e = amk::launch_early(evict_kernel, dim3((unsigned)(n_seqs * n_heads)), kThreads, (size_t)piece * 4, 1,
+  e = amk::launch_early(evict_kernel, dim3((unsigned)(n_seqs * n_heads)), kThreads, (size_t)piece * 6, 1,
                         (cudaStream_t)cuda_stream, p);
   return e == cudaSuccess ? AMK_OK : fail(AMK_ERR_CUDA, "launch failed: %s", cudaGetErrorString(e));
 }
