@@ -4,9 +4,9 @@
 // stay anyway hold the largest key) is found digit by digit from histograms of 11, 11 and 10 bits; then the positions whose key
 // is larger stay, and of those with that very key the first ones.  Counts are integers: the result is the same every time.
 //
-// Bound: the instructions of a few sweeps over keys that lie in shared memory, four to a thread at a time (a ballot for every 32 of
-// them instead: 256 lists of 8192 25.2 us, so XXX), and with few lists the barriers between the sweeps.  Lists of more than
-// 32768 scores are read again from L2 in the histograms, and chosen from in pieces.
+// Bound: instructions (a ballot for every 32 keys: 256 lists of 8192 25.2 us; sweeps over shared memory, four keys to a thread:
+// 16.1 us; keys in registers, a run for each thread: XXX us), and with few lists the barriers between the sweeps.  Lists of more than
+// 32768 slots are read again from L2 in the histograms, and chosen from in pieces.
 #include <cuda_runtime.h>
 
 #include <atomic>
@@ -28,134 +28,222 @@ struct EvictParams {
   const int* lens;
   int *keep, *count;
   int64_t seq, head, moved_seq, moved_head;
-  int heads, slots, budget, first, recent, piece;      // piece: scores that the shared memory holds
+  int heads, slots, budget, first, recent;
 };
 
 // larger for larger scores; 0 for NaN, less than 2^32 - 1 for every number
 __device__ __forceinline__ unsigned key_of(unsigned bits) {
-  if ((bits & 0x7fffffffu) > 0x7f800000u) return 0;
-  if (bits == 0x80000000u) bits = 0;
-  return bits & 0x80000000u ? ~bits : bits | 0x80000000u;
+  const float x = __uint_as_float(bits) + 0.f;         // (-0 becomes 0)
+  const unsigned u = __float_as_uint(x);
+  return x == x ? u ^ ((unsigned)((int)u >> 31) | 0x80000000u) : 0u;
 }
 
-__global__ void __launch_bounds__(kThreads) evict_kernel(const EvictParams p) {
-  extern __shared__ uint4 smem[];
-  unsigned* keys = (unsigned*)smem;                    // of a piece; 0 behind its end, which the order puts last
-  unsigned short* chosen = (unsigned short*)(keys + p.piece);
-  __shared__ unsigned bins[kBins], digit[2];
-  __shared__ unsigned sums[kWarps];
+// A list and what its block does whatever it holds.
+struct List {
+  const unsigned* in;
+  unsigned* out;
+  int* keep;
+  int n;
+};
+// true: there is nothing to choose, and all is done
+__device__ __forceinline__ bool begin_list(const EvictParams& p, List& a) {
   const int list = blockIdx.x, s = list / p.heads, h = list - s * p.heads;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const unsigned* in = (const unsigned*)p.scores + s * p.seq + h * p.head;
-  unsigned* out = p.moved ? (unsigned*)p.moved + s * p.moved_seq + h * p.moved_head : nullptr;
-  int* keep = p.keep + (int64_t)list * p.budget;
-  amk::wait_for_grid_before();
-  const int n = p.lens[s];
-  if (n < 0 || n > p.slots) {
+  a.in = (const unsigned*)p.scores + s * p.seq + h * p.head;
+  a.out = p.moved ? (unsigned*)p.moved + s * p.moved_seq + h * p.moved_head : nullptr;
+  a.keep = p.keep + (int64_t)list * p.budget;
+  a.n = p.lens[s];
+  if (a.n < 0 || a.n > p.slots) {
     if (threadIdx.x == 0) p.count[list] = -1;
-    for (int i = threadIdx.x; i < p.budget; i += kThreads) keep[i] = -1;
-    if (out && out != in)
-      for (int i = threadIdx.x; i < p.slots; i += kThreads) out[i] = in[i];
-    return;
+    for (int i = threadIdx.x; i < p.budget; i += kThreads) a.keep[i] = -1;
+    if (a.out && a.out != a.in)
+      for (int i = threadIdx.x; i < p.slots; i += kThreads) a.out[i] = a.in[i];
+    return true;
   }
-  const int count = min(n, p.budget);
+  const int count = min(a.n, p.budget);
   if (threadIdx.x == 0) p.count[list] = count;
-  for (int i = count + threadIdx.x; i < p.budget; i += kThreads) keep[i] = -1;
-  if (n <= p.budget) {
-    for (int i = threadIdx.x; i < n; i += kThreads) {
-      keep[i] = i;
-      if (out && out != in) out[i] = in[i];
-    }
-    if (out)
-      for (int i = n + threadIdx.x; i < p.slots; i += kThreads) out[i] = 0;
-    return;
+  for (int i = count + threadIdx.x; i < p.budget; i += kThreads) a.keep[i] = -1;
+  if (a.n > p.budget) return false;
+  for (int i = threadIdx.x; i < a.n; i += kThreads) {
+    a.keep[i] = i;
+    if (a.out && a.out != a.in) a.out[i] = a.in[i];
   }
-  const auto key_at = [&](int i) { return i < p.first || i >= n - p.recent ? ~0u : key_of(in[i]); };
-  const auto bring = [&](int from) {                   // the keys of a piece; its rounds
-    const int m = min(p.piece, n - from), rounds = (m + kSweep - 1) / kSweep;
-#pragma unroll 4
-    for (int i = threadIdx.x; i < rounds * kSweep; i += kThreads) keys[i] = i < m ? key_at(from + i) : 0;
-    return rounds;
-  };
-  const bool whole = n <= p.piece;
-  int rounds = 0;
-  for (int i = threadIdx.x; i < kBins; i += kThreads) bins[i] = 0;
-  if (whole) rounds = bring(0);
-  // keys above the border stay, and `equal` of those that have it
-  unsigned border = 0;
-  int equal = p.budget;
-#pragma unroll 1
+  if (a.out)
+    for (int i = a.n + threadIdx.x; i < p.slots; i += kThreads) a.out[i] = 0;
+  return true;
+}
+
+__device__ __forceinline__ int warp_scan(int x, int lane) {
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(~0u, x, o);
+    if (lane >= o) x += y;
+  }
+  return x;
+}
+
+struct Shared {
+  unsigned bins[kBins], digit[2], sums[kWarps];
+};
+
+// Keys above the border stay, and `equal` of those that have it.  each(f): calls f with every key of this thread.  bins are 0.
+template <class Each>
+__device__ __forceinline__ void find_border(Shared& h, unsigned& border, int& equal, const Each& each) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  border = 0;
+#pragma unroll
   for (int pass = 0; pass < 3; pass++) {
-    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, width = pass == 2 ? 1023 : 2047;
-    const auto count_key = [&](unsigned key) {
-      if (pass == 0 || key >> (pass == 1 ? 21 : 10) == border) atomicAdd(&bins[key >> shift & width], 1u);
-    };
+    constexpr int kShift[3] = {21, 10, 0}, kWidth[3] = {11, 11, 10};
     __syncthreads();
-    if (whole) {
-      for (int r = 0; r < rounds; r++) {
-        const uint4 k = smem[r * kThreads + threadIdx.x];
-        count_key(k.x), count_key(k.y), count_key(k.z), count_key(k.w);
-      }
-    } else {
-#pragma unroll 4
-      for (int i = threadIdx.x; i < n; i += kThreads) count_key(key_at(i));
-    }
+    each([&](unsigned key) {
+      if (pass == 0 || key >> (kShift[pass] + kWidth[pass]) == border) atomicAdd(&h.bins[key >> kShift[pass] & ((1u << kWidth[pass]) - 1)], 1u);
+    });
     __syncthreads();
     // the digit: the largest one at or above which `equal` keys lie.  Two bins a thread, from the largest down.
     const int top = kBins - 1 - 2 * (int)threadIdx.x;
-    const int a = (int)bins[top], b = (int)bins[top - 1];
-    bins[top] = bins[top - 1] = 0;
-    int sum = a + b;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int x = __shfl_up_sync(~0u, sum, o);
-      if (lane >= o) sum += x;
-    }
-    if (lane == 31) sums[warp] = (unsigned)sum;
+    uint2* pair = (uint2*)&h.bins[top - 1];
+    const int a = (int)pair->y, b = (int)pair->x;
+    *pair = make_uint2(0, 0);
+    int sum = warp_scan(a + b, lane);
+    if (lane == 31) h.sums[warp] = (unsigned)sum;
     __syncthreads();
-    const int own = (int)sums[lane];                   // (32 warps, 32 lanes)
+    const int own = (int)h.sums[lane];                 // (32 warps, 32 lanes)
     sum += __reduce_add_sync(~0u, lane < warp ? own : 0);
     const int before = sum - a - b;
-    if (before < equal && before + a >= equal) digit[0] = (unsigned)top, digit[1] = (unsigned)before;
-    if (before + a < equal && sum >= equal) digit[0] = (unsigned)top - 1, digit[1] = (unsigned)(before + a);
-    __syncthreads();
-    border = border << (pass == 2 ? 10 : 11) | digit[0];
-    equal -= (int)digit[1];
-  }
-  // Which ones stay, piece by piece in ascending order, a run of a piece for each warp.  Counts of keys above the border stand in
-  // the upper half of a word, of those that have it in the lower half.  Rows move down only, and all scores of 1024 rows are read
-  // before one of them is written: `moved` may be the scores themselves.
-  int above = 0, same = 0;                             // in the pieces in front
-  for (int from = 0; from < n; from += p.piece) {
-    if (!whole) {
-      __syncthreads();
-      rounds = bring(from);
-      __syncthreads();
+    if (before < equal && sum >= equal) {
+      const bool first = before + a >= equal;
+      h.digit[0] = (unsigned)(first ? top : top - 1), h.digit[1] = (unsigned)(first ? before : before + a);
     }
-    const auto packed = [&](unsigned key) { return key > border ? 0x10000u : key == border ? 1u : 0u; };
+    __syncthreads();
+    border = border << kWidth[pass] | h.digit[0];
+    equal -= (int)h.digit[1];
+  }
+}
+
+// Rows [base, base + rows) of the outputs, from the indices chosen behind `from`.  All scores of 1024 rows are read before one of
+// them is written, and rows move down only: `out` may be `in`.
+__device__ __forceinline__ void write_rows(const List& a, const unsigned short* chosen, int from, int base, int rows) {
+  for (int i0 = 0; i0 < rows; i0 += kThreads) {
+    const int i = i0 + threadIdx.x;
+    int row = 0;
+    unsigned bits = 0;
+    if (i < rows) {
+      row = from + chosen[i];
+      if (a.out) bits = a.in[row];
+    }
+    if (a.out == a.in) __syncthreads();
+    if (i < rows) {
+      a.keep[base + i] = row;
+      if (a.out) a.out[base + i] = bits;
+    }
+  }
+}
+__device__ __forceinline__ void clear_behind(const EvictParams& p, const List& a) {
+  if (!a.out) return;
+  if (a.out == a.in) __syncthreads();                  // (every row has been read)
+  for (int i = p.budget + threadIdx.x; i < p.slots; i += kThreads) a.out[i] = 0;
+}
+
+// Counts of keys above the border stand in the upper half of a word, of those that have it in the lower half.
+__device__ __forceinline__ unsigned packed(unsigned key, unsigned border) { return key > border ? 0x10000u : key == border ? 1u : 0u; }
+
+// Up to 1024 E slots: a thread's keys, E in a row, in registers.
+template <int E>
+__global__ void __launch_bounds__(kThreads) evict_held_kernel(const EvictParams p) {
+  extern __shared__ uint4 smem[];
+  unsigned short* chosen = (unsigned short*)smem;
+  __shared__ Shared h;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  List a;
+  *(uint2*)&h.bins[2 * threadIdx.x] = make_uint2(0, 0);
+  amk::wait_for_grid_before();
+  if (begin_list(p, a)) return;
+  const int i0 = threadIdx.x * E;
+  unsigned key[E];                                     // 0 behind the end, which the order puts last
+  if (((uintptr_t)a.in & 15) == 0 && i0 + E <= a.n) {
+#pragma unroll
+    for (int j = 0; j < E; j += 4) {
+      const uint4 x = *(const uint4*)(a.in + i0 + j);
+      key[j] = key_of(x.x), key[j + 1] = key_of(x.y), key[j + 2] = key_of(x.z), key[j + 3] = key_of(x.w);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < E; j++) key[j] = i0 + j < a.n ? key_of(a.in[i0 + j]) : 0u;
+  }
+  if (i0 < p.first || i0 + E > a.n - p.recent) {
+#pragma unroll
+    for (int j = 0; j < E; j++)
+      if (i0 + j < a.n && (i0 + j < p.first || i0 + j >= a.n - p.recent)) key[j] = ~0u;
+  }
+  unsigned border;
+  int equal = p.budget;
+  find_border(h, border, equal, [&](auto f) {
+#pragma unroll
+    for (int j = 0; j < E; j++) f(key[j]);
+  });
+  unsigned own = 0;
+#pragma unroll
+  for (int j = 0; j < E; j++) own += packed(key[j], border);
+  unsigned at = (unsigned)warp_scan((int)own, lane);
+  if (lane == 31) h.sums[warp] = at;
+  __syncthreads();
+  const unsigned other = h.sums[lane];
+  at += __reduce_add_sync(~0u, lane < warp ? other : 0) - own;
+  if (own) {
+    int more = (int)(at >> 16), ties = (int)(at & 0xffffu);
+#pragma unroll
+    for (int j = 0; j < E; j++) {
+      const bool over = key[j] > border, even = key[j] == border;
+      if (over || (even && ties < equal)) chosen[more + min(ties, equal)] = (unsigned short)(i0 + j);
+      more += over, ties += even;
+    }
+  }
+  __syncthreads();
+  write_rows(a, chosen, 0, 0, p.budget);
+  clear_behind(p, a);
+}
+
+// Any number of slots: the list is read again for each histogram, and then in pieces that lie in shared memory, a run of a piece for
+// each warp.
+__global__ void __launch_bounds__(kThreads) evict_kernel(const EvictParams p) {
+  extern __shared__ uint4 smem[];
+  unsigned* keys = (unsigned*)smem;                    // of a piece; 0 behind its end, which the order puts last
+  unsigned short* chosen = (unsigned short*)(keys + kPiece);
+  __shared__ Shared h;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  List a;
+  *(uint2*)&h.bins[2 * threadIdx.x] = make_uint2(0, 0);
+  amk::wait_for_grid_before();
+  if (begin_list(p, a)) return;
+  const auto key_at = [&](int i) { return i < p.first || i >= a.n - p.recent ? ~0u : key_of(a.in[i]); };
+  unsigned border;
+  int equal = p.budget;
+  find_border(h, border, equal, [&](auto f) {
+#pragma unroll 4
+    for (int i = threadIdx.x; i < a.n; i += kThreads) f(key_at(i));
+  });
+  int above = 0, same = 0;                             // in the pieces in front
+  for (int from = 0; from < a.n; from += kPiece) {
+    const int m = min(kPiece, a.n - from), rounds = (m + kSweep - 1) / kSweep;
+    __syncthreads();
+#pragma unroll 4
+    for (int i = threadIdx.x; i < rounds * kSweep; i += kThreads) keys[i] = i < m ? key_at(from + i) : 0;
+    __syncthreads();
     const uint4* mine = smem + warp * rounds * 32 + lane;
     unsigned all = 0;
     for (int r = 0; r < rounds; r++) {
       const uint4 k = mine[r * 32];
-      all += packed(k.x) + packed(k.y) + packed(k.z) + packed(k.w);
+      all += packed(k.x, border) + packed(k.y, border) + packed(k.z, border) + packed(k.w, border);
     }
     all = __reduce_add_sync(~0u, all);
+    if (lane == 0) h.sums[warp] = all;
     __syncthreads();
-    if (lane == 0) sums[warp] = all;
-    __syncthreads();
-    const unsigned own = sums[lane], total = __reduce_add_sync(~0u, own);
+    const unsigned own = h.sums[lane], total = __reduce_add_sync(~0u, own);
     unsigned run = __reduce_add_sync(~0u, lane < warp ? own : 0);
     const int base = above + min(same, equal);         // rows that stay in the pieces in front
     for (int r = 0; r < rounds; r++) {
       const uint4 k = mine[r * 32];
-      const unsigned c[4] = {packed(k.x), packed(k.y), packed(k.z), packed(k.w)};
-      const unsigned four = c[0] + c[1] + c[2] + c[3];
-      unsigned scan = four;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const unsigned x = __shfl_up_sync(~0u, scan, o);
-        if (lane >= o) scan += x;
-      }
+      const unsigned c[4] = {packed(k.x, border), packed(k.y, border), packed(k.z, border), packed(k.w, border)};
+      const unsigned four = c[0] + c[1] + c[2] + c[3], scan = (unsigned)warp_scan((int)four, lane);
       unsigned at = run + scan - four;
       run += __shfl_sync(~0u, scan, 31);
       if (four) {
@@ -169,27 +257,15 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(const EvictParams p) {
       }
     }
     above += (int)(total >> 16), same += (int)(total & 0xffffu);
-    const int rows = above + min(same, equal) - base;
     __syncthreads();
-    for (int i0 = 0; i0 < rows; i0 += kThreads) {
-      const int i = i0 + threadIdx.x;
-      int row = 0;
-      unsigned bits = 0;
-      if (i < rows) {
-        row = from + chosen[i];
-        if (out) bits = in[row];
-      }
-      if (out == in) __syncthreads();
-      if (i < rows) {
-        keep[base + i] = row;
-        if (out) out[base + i] = bits;
-      }
-    }
+    write_rows(a, chosen, from, base, above + min(same, equal) - base);
   }
-  if (out) {
-    if (out == in) __syncthreads();                    // (every row has been read)
-    for (int i = count + threadIdx.x; i < p.slots; i += kThreads) out[i] = 0;
-  }
+  clear_behind(p, a);
+}
+
+template <int E>
+cudaError_t launch_held(const EvictParams& p, unsigned lists, cudaStream_t st) {
+  return amk::launch_early(evict_held_kernel<E>, dim3(lists), kThreads, (size_t)2 * p.budget + 16, 1, st, p);
 }
 
 cudaError_t allow_smem() {
@@ -200,6 +276,7 @@ cudaError_t allow_smem() {
   const unsigned long long bit = dev < 64 ? 1ull << dev : 0;
   if (done.load(std::memory_order_acquire) & bit) return cudaSuccess;
   e = cudaFuncSetAttribute(evict_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPiece * 6);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(evict_held_kernel<32>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPiece * 2 + 16);
   if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_release);
   return e;
 }
@@ -232,12 +309,16 @@ extern "C" amk_status amk_evict_select(const float* scores, int64_t n_seqs, int6
     return fail(AMK_ERR_INVALID_ARG, "strides must be at least the %lld slots", (long long)n_slots);
   if (moved == scores && (moved_seq != scores_seq || moved_head != scores_head))
     return fail(AMK_ERR_INVALID_ARG, "moved is scores, but at other strides");
+  const EvictParams p{scores, moved, lens, keep, count, scores_seq, scores_head, moved_seq, moved_head, (int)n_heads,
+                      (int)n_slots, (int)budget, (int)first, (int)recent};
+  const unsigned lists = (unsigned)(n_seqs * n_heads);
+  const cudaStream_t st = (cudaStream_t)cuda_stream;
   cudaError_t e = allow_smem();
   if (e != cudaSuccess) return fail(AMK_ERR_CUDA, "%s", cudaGetErrorString(e));
-  const int piece = n_slots < kPiece ? ((int)n_slots + kSweep - 1) / kSweep * kSweep : kPiece;
-  const EvictParams p{scores, moved, lens, keep, count, scores_seq, scores_head, moved_seq, moved_head, (int)n_heads,
-                      (int)n_slots, (int)budget, (int)first, (int)recent, piece};
-  e = amk::launch_early(evict_kernel, dim3((unsigned)(n_seqs * n_heads)), kThreads, (size_t)piece * 6, 1,
-                        (cudaStream_t)cuda_stream, p);
+  if (n_slots <= 4 * kThreads) e = launch_held<4>(p, lists, st);
+  else if (n_slots <= 8 * kThreads) e = launch_held<8>(p, lists, st);
+  else if (n_slots <= 16 * kThreads) e = launch_held<16>(p, lists, st);
+  else if (n_slots <= 32 * kThreads) e = launch_held<32>(p, lists, st);
+  else e = amk::launch_early(evict_kernel, dim3(lists), kThreads, (size_t)kPiece * 6, 1, st, p);
   return e == cudaSuccess ? AMK_OK : fail(AMK_ERR_CUDA, "launch failed: %s", cudaGetErrorString(e));
 }
