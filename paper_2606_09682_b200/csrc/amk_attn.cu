@@ -34,16 +34,16 @@ EncodeTiled encode_tiled() {
   return fn;
 }
 
-// A cache or a projection as {element, row, head, sequence}; boxes of 128 rows x 64 elements (bf16, swizzled for the
+// A cache or a projection as {element, row, head, sequence}; boxes of 128 (box_rows) rows x 64 elements (bf16, swizzled for the
 // tensor cores) or whole 8-bit rows.  Strides in elements; an axis of one entry has a legal stride already.
 bool make_map(CUtensorMap* map, const void* base, bool fp8, int64_t hd, int64_t rows, int64_t heads, int64_t seqs,
-              int64_t row, int64_t head, int64_t seq) {
+              int64_t row, int64_t head, int64_t seq, int box_rows = amk::kTile) {
   const EncodeTiled encode = encode_tiled();
   if (!encode) return false;
   const cuuint64_t esz = fp8 ? 1 : 2;
   const cuuint64_t dims[4] = {(cuuint64_t)hd, (cuuint64_t)rows, (cuuint64_t)heads, (cuuint64_t)seqs};
   const cuuint64_t strides[3] = {(cuuint64_t)row * esz, (cuuint64_t)head * esz, (cuuint64_t)seq * esz};
-  const cuuint32_t box[4] = {fp8 ? (cuuint32_t)hd : 64u, (cuuint32_t)amk::kTile, 1, 1}, steps[4] = {1, 1, 1, 1};
+  const cuuint32_t box[4] = {fp8 ? (cuuint32_t)hd : 64u, (cuuint32_t)box_rows, 1, 1}, steps[4] = {1, 1, 1, 1};
   return encode(map, fp8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base),
                 dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
                 fp8 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
@@ -269,11 +269,12 @@ amk_status check_weights(const Reason& fail, const amk_attention_weights_args* a
   return AMK_OK;
 }
 
-// How a call of the weights is divided.
+// How a call of the weights is divided: few rows (all of a kv head's in one tile) or many.
 struct WeightsPlan {
+  int q_stages, k_stages, raw_stages;   // tiles in shared memory
   int tokens, q_tiles, columns;    // tokens of a tile of query rows, tiles, rows of a tile up to a multiple of 32
   unsigned blocks;
-  size_t bytes;                    // scratch: parts of units, where these have several steps
+  size_t bytes;                    // scratch: parts of units
 };
 WeightsPlan weights_plan(const amk_attention_weights_args& a) {
   WeightsPlan t;
@@ -281,10 +282,17 @@ WeightsPlan weights_plan(const amk_attention_weights_args& a) {
   t.tokens = (int64_t)a.n_rows < most ? (int)a.n_rows : most;
   t.q_tiles = (int)((a.n_rows + t.tokens - 1) / t.tokens);
   t.columns = (t.tokens * rep + 31) / 32 * 32;
-  const double steps = (a.n_slots / (double)amk::kTile + 1) * a.n_kv_heads * a.n_seqs * t.q_tiles;
+  const bool many = t.q_tiles > 1;
+  const int twice = a.head_dim == 64 ? 2 : 1;
+  if (a.kv_dtype == AMK_KV_FP8_E4M3) {
+    t.k_stages = (many ? 1 : 2) * twice, t.q_stages = (many ? 3 : 2) * twice, t.raw_stages = (many ? 2 : 4) * twice;
+  } else {
+    t.k_stages = (many ? 2 : 4) * twice, t.q_stages = (many ? 3 : 2) * twice, t.raw_stages = 0;
+  }
+  const double span = (many ? amk::kManySpan : amk::kTile), steps = (a.n_slots / span + 1) * a.n_kv_heads * a.n_seqs * t.q_tiles;
   const int sms = sm_count();
   t.blocks = (unsigned)(steps < sms ? (steps < 1 ? 1 : steps) : sms);
-  t.bytes = t.q_tiles > 1 ? (size_t)2 * t.blocks * (sizeof(int4) + amk::kTile * sizeof(float)) : 0;
+  t.bytes = many ? (size_t)2 * t.blocks * (sizeof(int4) + amk::kManySpan * sizeof(float)) : 0;
   return t;
 }
 
@@ -304,18 +312,20 @@ bool make_query_map(CUtensorMap* map, const amk_attention_weights_args& a, int r
 
 template <int HD, bool FP8>
 cudaError_t launch_weights(const amk::WeightsParams& p, const CUtensorMap& q, const CUtensorMap& k, unsigned blocks, cudaStream_t st) {
-  using L = amk::WeightsSmem<HD, FP8>;
-  static std::atomic<unsigned long long> done{0};      // devices on which the kernel's shared-memory limit is raised
+  constexpr int kBytes = amk::WeightsSmem<HD, FP8, amk::kTile>::kBytes;             // (the same for both)
+  static std::atomic<unsigned long long> done{0};      // devices on which the kernels' shared-memory limits are raised
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   const unsigned long long bit = dev < 64 ? 1ull << dev : 0;
   if (!(done.load(std::memory_order_acquire) & bit)) {
-    e = cudaFuncSetAttribute(amk::weights_kernel<HD, FP8>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes);
+    e = cudaFuncSetAttribute(amk::weights_few_kernel<HD, FP8>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(amk::weights_many_kernel<HD, FP8>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
     if (e != cudaSuccess) return e;
     done.fetch_or(bit, std::memory_order_release);
   }
-  return amk::launch_early(amk::weights_kernel<HD, FP8>, dim3(blocks), L::kThreads, L::kBytes, 1, st, p, q, k);
+  if (p.q_tiles > 1) return amk::launch_early(amk::weights_many_kernel<HD, FP8>, dim3(blocks), amk::kManyThreads, kBytes, 1, st, p, q, k);
+  return amk::launch_early(amk::weights_few_kernel<HD, FP8>, dim3(blocks), amk::kFewThreads<FP8>, kBytes, 1, st, p, q, k);
 }
 
 }  // namespace
@@ -502,16 +512,18 @@ extern "C" amk_status amk_attention_weights(const amk_attention_weights_args* ar
   p.n_seqs = (int)a.n_seqs, p.nq = (int)a.n_q_heads, p.nkv = (int)a.n_kv_heads, p.rep = p.nq / p.nkv;
   p.rows = (int)a.n_rows, p.slots = (int)a.n_slots;
   p.tokens = t.tokens, p.q_tiles = t.q_tiles, p.columns = t.columns;
+  p.rep_inv = p.rep == 1 ? 0 : (unsigned)(((1ull << 32) + p.rep - 1) / p.rep);
+  p.q_stages = t.q_stages, p.k_stages = t.k_stages, p.raw_stages = t.raw_stages;
   p.scale = a.scale > 0.f ? a.scale : 1.f / sqrtf((float)hd), p.decay = a.decay;
   set_limits(p);
   CUtensorMap mq, mk;
   if (!make_query_map(&mq, a, p.rep, t.tokens) ||
-      !make_map(&mk, a.k, esz == 1, hd, a.n_slots, p.nkv, a.n_seqs, a.k_row, a.k_head, a.k_seq))
+      !make_map(&mk, a.k, esz == 1, hd, a.n_slots, p.nkv, a.n_seqs, a.k_row, a.k_head, a.k_seq, t.q_tiles > 1 ? amk::kManySpan : amk::kTile))
     return fail(AMK_ERR_CUDA, "cuTensorMapEncodeTiled failed or is missing");
   const cudaStream_t st = (cudaStream_t)cuda_stream;
   cudaError_t e = hd == 64 ? (esz == 1 ? launch_weights<64, true>(p, mq, mk, t.blocks, st) : launch_weights<64, false>(p, mq, mk, t.blocks, st))
                            : (esz == 1 ? launch_weights<128, true>(p, mq, mk, t.blocks, st) : launch_weights<128, false>(p, mq, mk, t.blocks, st));
   if (e == cudaSuccess && t.bytes)
-    e = amk::launch_early(amk::weights_join_kernel, dim3(t.blocks), amk::kTile, 0, 1, st, p, (int)t.blocks);
+    e = amk::launch_early(amk::weights_join_kernel, dim3(t.blocks), amk::kManySpan, 0, 1, st, p, (int)t.blocks);
   return e == cudaSuccess ? AMK_OK : fail(AMK_ERR_CUDA, "launch failed: %s", cudaGetErrorString(e));
 }

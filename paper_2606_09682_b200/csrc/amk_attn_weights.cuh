@@ -1,14 +1,16 @@
-// The kernel of amk_attention_weights: what the queries of some tokens attend to, added up for each cached position.
+// The kernels of amk_attention_weights: what the queries of some tokens attend to, added up for each cached position.
 //
 // Mathematics.  With the log-sum-exps known there is no maximum to find: w(j) = sum over the query rows (a row is a token and one
-// of the query heads of a kv head) of 2^(S c - L), c = scale log2 e, L = lse log2 e.  The product is taken as S^T = K Q^T, so that a
-// position is a lane of TMEM and its sum stays in one thread's register: no exchange between lanes.
+// of the query heads of a kv head) of 2^(S c - L), c = scale log2 e, L = lse log2 e.
 //
-// Work.  One block an SM.  A unit is a tile of 128 positions of a kv head, a step of it the product with one tile of query rows
-// (as many whole tokens as fit into 128 rows); the steps of all units, in that order, are cut into equal runs, one for each
-// block.  A unit that a run's border cuts leaves its parts in scratch and a second kernel adds them, in the order of the blocks.
-// A producer warp brings K tiles (once a unit) and Q tiles (once a step, or once a head where one tile holds all rows) by
-// TMA, one warp issues the products into four accumulators, four warpgroups take every fourth step each.
+// Few rows (128 or less for a kv head: a decoded token, a draft, the last tokens of a prompt): every K tile of 128 positions meets
+// one tile of queries, and what counts is K's way from HBM.  weights_few_kernel takes S^T = K Q^T: a position is a lane of TMEM.
+//
+// Many rows: what counts are the exponentials, 16 a cycle and SM, four times as long as the products.  weights_many_kernel takes
+// S = Q K^T: a query row is a lane, whose L is a scalar, and a thread keeps the sums of 64 positions in registers over all
+// query tiles of a unit; lanes are added up once, at its end.  (With the positions in the lanes there too every column's L is
+// read from shared memory, in front of every exponential, and each warp adds a chain of its own: 7001 tokens, 32 heads of
+// 128 on 8: 257 us; so: XXX us.)
 #pragma once
 #include "amk_attn.cuh"
 
@@ -19,12 +21,14 @@ struct WeightsParams {
   const int* lens;
   const float* before;
   float* out;
-  float* part;                     // [2 * gridDim][128]: sums of cut units
-  int4* part_of;                   // [2 * gridDim]: {sequence, head, tile, whether the next block goes on}; sequence -1: none
+  float* part;                     // many rows: [2 * gridDim][192]: sums of cut units
+  int4* part_of;                   // [2 * gridDim]: {sequence, head, unit, whether the next block goes on}; sequence -1: none
   int64_t b_seq, b_head, o_seq, o_head;
   int n_seqs, nq, nkv, rep, rows, slots;
   int tokens, q_tiles;             // tokens of a tile of query rows, tiles of all
-  int columns;                     // rows of a tile, up to a multiple of 32
+  int q_stages, k_stages, raw_stages;   // tiles in shared memory
+  int columns;                     // few rows: rows of the tile, up to a multiple of 32
+  unsigned rep_inv;                // ceil(2^32 / rep), 0 for rep = 1
   unsigned tiles;                  // K tiles that a block may ask for (a test's limit, else the largest number)
   unsigned wait_cycles;
   float scale, decay;
@@ -40,96 +44,65 @@ __device__ __forceinline__ void tma_load_5d(bool leader, void* dst, const CUtens
       "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(v), "r"(smem_u32(bar)), "r"((unsigned)leader)
       : "memory");
 }
-// Four e4m3 codes to four bf16, exactly: the seven bits without the sign, read as a bf16 four places lower, are 2^-120 times the
-// code's value (also below the normal ones), for all but NaN.
-__device__ __forceinline__ void widen_e4m3_bf16(unsigned* w, unsigned codes) {
+
+// A tile of e4m3 codes to bf16 (both exact), laid out as the matrix instructions want it: chunks of 16 codes from `first` on, every
+// `threads`-th.  Over f16, for which there is one instruction for two codes (128 x 128 codes, eight warps: 650 cycles; by shifts
+// and a product with 2^120: 1130).  Half of a row's lanes store their second piece first: they lie in the same banks.
+template <int HD, int ROWS, int BATCH>
+__device__ __forceinline__ void widen_tile(unsigned char* dst, const unsigned char* src, int first, int threads) {
+  constexpr int kChunks = HD / 16;                     // of a row
+  for (int i0 = first; i0 < ROWS * kChunks; i0 += threads * BATCH) {
+    uint4 v[BATCH];
 #pragma unroll
-  for (int i = 0; i < 2; i++) {
-    const unsigned a = __byte_perm(codes, 0, i ? 0x3424 : 0x1404), r = (a & 0x80008000u) | (a >> 4 & 0x07f007f0u);
-    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(w[i]) : "r"(r), "r"(0x7b807b80u), "r"(0x80008000u));
-    if (((a & 0x7f007f00u) + 0x01000100u) & 0x80008000u) {
-      if ((a & 0x7f00u) == 0x7f00u) w[i] |= 0x7fffu;
-      if ((a & 0x7f000000u) == 0x7f000000u) w[i] |= 0x7fff0000u;
-    }
-  }
-}
-
-constexpr int kSumRing = 8;
-template <int HD, bool FP8>
-struct WeightsSmem {
-  static constexpr int kTileBytes = HD / 64 * kBox;
-  static constexpr int kStages = FP8 ? 2 : 3;                      // K tiles (bf16)
-  static constexpr int kQStages = HD == 128 ? 3 : 4;
-  static constexpr int kRawBytes = FP8 ? HD * kTile : 0, kRawStages = FP8 ? 2 : 0;
-  static constexpr int kQ = 0;
-  static constexpr int kRing = kQStages * kTileBytes;
-  static constexpr int kRaw = kRing + kStages * kTileBytes;
-  static constexpr int kHead = kRaw + kRawStages * kRawBytes;
-  static constexpr int kBytes = kHead + 24576 + 1024;              // + alignment of the dynamic buffer
-  static constexpr int kThreads = FP8 ? 704 : 576;
-  static_assert(kBytes <= 227 * 1024, "shared memory of one SM");
-};
-struct WeightsHead {
-  float sums[kSumRing][4][kTile];      // the warpgroups' shares of a unit
-  float less[4][2][kTile];             // [warpgroup][step of it & 1]: -lse log2 e of the rows; -infinity: adds nothing
-  uint64_t k_full[4], k_empty[4], raw_full[4], raw_empty[4], q_full[4], q_empty[4], s_full[4], s_empty[4], sums_full[kSumRing], fin;
-  unsigned tmem;
-  int dead;
-  unsigned wait_cycles;
-  int start[5];                        // where the block's run begins: sequence, head, tile, step; its steps
-};
-static_assert(sizeof(WeightsHead) <= 24576, "head");
-
-// ---- units ------------------------------------------------------------------------------------------------------
-__device__ __forceinline__ int weights_tiles(const WeightsParams& p, int len) {         // 0: impossible length
-  return len < 0 || len > p.slots - p.rows ? 0 : (len + p.rows + kTile - 1) / kTile;
-}
-// the first tile of query rows that sees a tile of positions
-__device__ __forceinline__ int first_q_tile(const WeightsParams& p, int len, int tile) {
-  return max(0, tile * kTile - len) / p.tokens;
-}
-__device__ __forceinline__ int weights_steps(const WeightsParams& p, int len) {         // of one head
-  const int tiles = weights_tiles(p, len);
-  if (p.q_tiles == 1 || !tiles) return tiles;
-  const int full = min(tiles, len / kTile + 1);                    // tiles that all rows see
-  int n = full * p.q_tiles;
-  for (int j = full; j < tiles; j++) n += p.q_tiles - first_q_tile(p, len, j);
-  return n;
-}
-struct WeightsUnit {
-  int seq, head, len, tile;
-  int first;                       // first tile of query rows of the unit
-  int begin, end, all;             // steps of this block, steps of the unit
-};
-struct WeightsWalk {
-  int left, seq, len, head, tile, tiles, step;
-  __device__ __forceinline__ void init(const WeightsParams& p, const WeightsHead& h) {
-    seq = h.start[0], head = h.start[1], tile = h.start[2], step = h.start[3], left = h.start[4];
-    len = left ? __ldg(p.lens + seq) : 0;
-    tiles = weights_tiles(p, len);
-  }
-  __device__ __forceinline__ bool next(const WeightsParams& p, WeightsUnit& u) {
-    if (left <= 0) return false;
-    while (tile >= tiles) {        // something is left: a unit follows
-      tile = 0;
-      if (tiles && head + 1 < p.nkv) {
-        head++;
-      } else {
-        head = 0;
-        len = __ldg(p.lens + ++seq);
-        tiles = weights_tiles(p, len);
+    for (int b = 0; b < BATCH; b++)
+      if (i0 + b * threads < ROWS * kChunks) v[b] = *(const uint4*)(src + (i0 + b * threads) * 16);
+#pragma unroll
+    for (int b = 0; b < BATCH; b++) {
+      const int i = i0 + b * threads;
+      if (i >= ROWS * kChunks) break;
+      const unsigned c[4] = {v[b].x, v[b].y, v[b].z, v[b].w};
+      unsigned w[8];
+#pragma unroll
+      for (int k = 0; k < 4; k++) {
+        unsigned h[2];
+        widen_e4m3(h, c[k]);
+        float lo, hi;
+        unpack_f16(lo, hi, h[0]);
+        w[2 * k] = pack_bf16(lo, hi);
+        unpack_f16(lo, hi, h[1]);
+        w[2 * k + 1] = pack_bf16(lo, hi);
       }
+      const int row = i / kChunks, cc = i % kChunks * 2, swap = cc >> 3 & 1;
+      unsigned char* to = dst + (cc >> 3) * (ROWS * 128) + row * 128;
+      const uint4 x = make_uint4(w[0], w[1], w[2], w[3]), y = make_uint4(w[4], w[5], w[6], w[7]);
+      *(uint4*)(to + ((((cc & 7) + swap) ^ (row & 7)) << 4)) = swap ? y : x;
+      *(uint4*)(to + ((((cc & 7) + 1 - swap) ^ (row & 7)) << 4)) = swap ? x : y;
     }
-    u.seq = seq, u.head = head, u.len = len, u.tile = tile;
-    u.first = first_q_tile(p, len, tile);
-    u.all = p.q_tiles - u.first;
-    u.begin = step, u.end = min(u.all, step + left);
-    left -= u.end - u.begin;
-    step = 0;
-    tile++;
-    return true;
   }
-};
+}
+
+// The unit of exponentials makes 16 a cycle and SM, so some are made on the fma pipe: 2^x = 2^n 2^f with n the nearest integer,
+// 2^f a polynomial with the constant 1 whose largest relative error on [-1/2, 1/2] is least (9.1e-8; 1.7e-7 as computed;
+// coefficients from that linear programme).  x is kept at or above -127, where 2^n is made as 0 (so -infinity gives 0), and
+// at or below 128, where it is infinity; NaN stays NaN.
+__device__ __forceinline__ float clamp_exponent(float x) {
+  float a, b;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(a) : "f"(x), "f"(-127.f));
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(b) : "f"(a), "f"(128.f));
+  return b;
+}
+__device__ __forceinline__ uint64_t add_powers(uint64_t x, uint64_t acc) {           // acc + 2^x
+  const float magic = 12582912.f;                      // 1.5 * 2^23: leaves the integer in the low bits
+  float a, b;
+  unpair(a, b, x);
+  const uint64_t y = pair(clamp_exponent(a), clamp_exponent(b)), t = add2(y, pair(magic, magic));
+  const uint64_t f = fma2(add2(t, pair(-magic, -magic)), pair(-1.f, -1.f), y);
+  uint64_t v = fma2(pair(0.0013264727f, 0.0013264727f), f, pair(0.009671513f, 0.009671513f));
+  v = fma2(v, f, pair(0.055507336f, 0.055507336f)), v = fma2(v, f, pair(0.24022242f, 0.24022242f));
+  v = fma2(v, f, pair(0.693147f, 0.693147f)), v = fma2(v, f, pair(1.f, 1.f));
+  unpair(a, b, t);
+  return fma2(v, pair(__uint_as_float((__float_as_uint(a) << 23) + 0x3f800000u), __uint_as_float((__float_as_uint(b) << 23) + 0x3f800000u)), acc);
+}
 
 // a position's sum, finished
 __device__ __forceinline__ void weights_write(const WeightsParams& p, int seq, int head, int len, int key, float sum) {
@@ -139,6 +112,227 @@ __device__ __forceinline__ void weights_write(const WeightsParams& p, int seq, i
   p.out[seq * p.o_seq + head * p.o_head + key] = sum;
 }
 
+// ---- units ------------------------------------------------------------------------------------------------------
+// A unit is SPAN positions of a kv head, a step of it the product with one tile of query rows (as many whole tokens as fit into 128
+// rows).  The steps of all units, sequence by sequence, head by head, are cut into equal runs, one for each block.
+template <int SPAN>
+__device__ __forceinline__ int weights_units(const WeightsParams& p, int len) {         // of one head; 0: impossible length
+  return len < 0 || len > p.slots - p.rows ? 0 : (len + p.rows + SPAN - 1) / SPAN;
+}
+// the first tile of query rows that sees a position of a unit
+template <int SPAN>
+__device__ __forceinline__ int first_q_tile(const WeightsParams& p, int len, int unit) {
+  const int behind = unit * SPAN - len;
+  return SPAN == kTile || behind <= 0 ? 0 : behind / p.tokens;
+}
+// units of one head whose every position all rows see
+template <int SPAN>
+__device__ __forceinline__ int full_units(const WeightsParams& p, int len, int units) {
+  return SPAN == kTile ? units : min(units, len / SPAN + 1);
+}
+template <int SPAN>
+__device__ __forceinline__ int weights_steps(const WeightsParams& p, int len) {         // of one head
+  const int units = weights_units<SPAN>(p, len), full = full_units<SPAN>(p, len, units);
+  int n = full * p.q_tiles;
+  for (int j = full; j < units; j++) n += p.q_tiles - first_q_tile<SPAN>(p, len, j);
+  return n;
+}
+struct WeightsUnit {
+  int seq, head, len, at;          // at: which unit of the head
+  int first;                       // first tile of query rows of the unit
+  int begin, end, all;             // steps of this block, steps of the unit
+};
+template <int SPAN>
+struct WeightsWalk {
+  int left, seq, len, head, at, units, step;
+  __device__ __forceinline__ void init(const WeightsParams& p, const int* start) {
+    seq = start[0], head = start[1], at = start[2], step = start[3], left = start[4], len = start[5];
+    units = weights_units<SPAN>(p, len);
+  }
+  __device__ __forceinline__ bool next(const WeightsParams& p, WeightsUnit& u) {
+    if (left <= 0) return false;
+    while (at >= units) {          // something is left: a unit follows
+      at = 0;
+      if (units && head + 1 < p.nkv) {
+        head++;
+      } else {
+        head = 0;
+        len = __ldg(p.lens + ++seq);
+        units = weights_units<SPAN>(p, len);
+      }
+    }
+    u.seq = seq, u.head = head, u.len = len, u.at = at;
+    u.first = first_q_tile<SPAN>(p, len, at);
+    u.all = SPAN == kTile ? 1 : p.q_tiles - u.first;
+    u.begin = step, u.end = min(u.all, step + left);
+    left -= u.end - u.begin;
+    step = 0;
+    at++;
+    return true;
+  }
+};
+// Where this block's run begins, and its steps (one whole warp): {sequence, head, unit, step, steps, length of the sequence}
+template <int SPAN>
+__device__ __forceinline__ void find_run(const WeightsParams& p, int* start) {
+  const int lane = threadIdx.x & 31;
+  auto steps_of = [&](int s) { return s < p.n_seqs ? weights_steps<SPAN>(p, __ldg(p.lens + s)) * p.nkv : 0; };
+  const int mine = steps_of(lane);
+  int total = mine;
+  for (int s = 32 + lane; s < p.n_seqs; s += 32) total += steps_of(s);
+  total = warp_sum(total);
+  const int per = (total + (int)gridDim.x - 1) / (int)gridDim.x;
+  int at = (int)blockIdx.x * per, seq = 0, head = 0, unit = 0, step = 0, left = 0, len = 0;
+  if ((int64_t)blockIdx.x * per < total) {
+    left = min(per, total - at);
+    for (int s0 = 0; s0 < p.n_seqs; s0 += 32) {
+      const int own = s0 ? steps_of(s0 + lane) : mine;
+      int n = own;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int x = __shfl_up_sync(~0u, n, o);
+        if (lane >= o) n += x;
+      }
+      const unsigned hit = __ballot_sync(~0u, n > at);
+      if (hit) {
+        const int f = __ffs(hit) - 1;
+        seq = s0 + f;
+        int rel = at - __shfl_sync(~0u, n - own, f);
+        const int of_head = __shfl_sync(~0u, own, f) / p.nkv;
+        len = __ldg(p.lens + seq);
+        head = rel / of_head, rel -= head * of_head;
+        if (SPAN == kTile) {
+          unit = rel;
+        } else {
+          const int full = full_units<SPAN>(p, len, weights_units<SPAN>(p, len));
+          if (rel < full * p.q_tiles) {
+            unit = rel / p.q_tiles, step = rel - unit * p.q_tiles;
+          } else {
+            rel -= full * p.q_tiles;
+            for (unit = full;; unit++) {
+              const int steps = p.q_tiles - first_q_tile<SPAN>(p, len, unit);
+              if (rel < steps) break;
+              rel -= steps;
+            }
+            step = rel;
+          }
+        }
+        break;
+      }
+      at -= __shfl_sync(~0u, n, 31);
+    }
+  }
+  if (lane == 0) start[0] = seq, start[1] = head, start[2] = unit, start[3] = step, start[4] = left, start[5] = len;
+}
+// Slots behind the units, and sequences of an impossible length.
+template <int SPAN>
+__device__ __forceinline__ void fill_behind(const WeightsParams& p, int threads) {
+  for (int r = blockIdx.x; r < p.n_seqs * p.nkv; r += gridDim.x) {
+    const int s = r / p.nkv, units = weights_units<SPAN>(p, __ldg(p.lens + s));
+    float* out = p.out + s * p.o_seq + (r - s * p.nkv) * p.o_head;
+    for (int64_t i = (int64_t)units * SPAN + threadIdx.x; i < p.slots; i += threads) out[i] = units ? 0.f : CUDART_NAN_F;
+  }
+}
+
+// ---- shared memory ----------------------------------------------------------------------------------------------
+// 192 KB divided between Q tiles (128 rows), K tiles (SPAN rows) and, over the 8-bit cache, K tiles as they come.  With few rows the K
+// tiles are what streams, else the Q tiles: a tile is on its way for 1.5 us, and the ring that streams has to hold what the
+// others need meanwhile.
+constexpr int kMaxStages = 10;
+template <int HD, bool FP8, int SPAN>
+struct WeightsSmem {
+  static constexpr int kTileBytes = HD / 64 * kBox, kBoxK = 64 * SPAN * 2, kBytesK = HD / 64 * kBoxK;
+  static constexpr int kRawBytes = FP8 ? HD * SPAN : 0;
+  static constexpr int kHead = 192 * 1024, kHeadBytes = 16384;
+  static constexpr int kBytes = kHead + kHeadBytes + 1024;         // + alignment of the dynamic buffer
+  static_assert(kBytes <= 227 * 1024, "shared memory of one SM");
+};
+struct WeightsHead {
+  uint64_t k_full[kMaxStages], k_empty[kMaxStages], raw_full[kMaxStages], raw_empty[kMaxStages], q_full[kMaxStages], q_empty[kMaxStages];
+  uint64_t s_full[4], s_empty[4], fin;
+  unsigned tmem;
+  int dead;
+  unsigned wait_cycles;
+  int start[6];                        // where the block's run begins
+  alignas(16) float less[12][kTile];   // few rows: [warp]: -lse log2 e of the rows; -infinity: adds nothing
+  alignas(16) float sums[3][4][64];    // many rows: [warpgroup][warp]: sums of its 32 rows
+};
+static_assert(sizeof(WeightsHead) <= 16384, "head");
+// a place in a ring of tiles and the parity of its round
+struct RingAt {
+  int at = 0;
+  unsigned round = 0;
+  __device__ __forceinline__ void next(int n) {
+    if (++at == n) at = 0, round ^= 1;
+  }
+};
+
+// What both kernels begin with.  widen_arrivals, s_arrivals: warps that arrive at a widened tile and at a free accumulator.
+template <int HD, bool FP8>
+__device__ __forceinline__ void weights_begin(const WeightsParams& p, WeightsHead& h, unsigned char* smem, int issuer_warp, int warp,
+                                              int lane, int widen_arrivals, int s_arrivals, int threads) {
+  if (warp == issuer_warp) {
+    tmem_alloc(&h.tmem, 512);
+    if (lane == 0) {
+      for (int i = 0; i < p.k_stages; i++) mbar_init(&h.k_full[i], FP8 ? widen_arrivals : 1), mbar_init(&h.k_empty[i], 1);
+      for (int i = 0; i < p.raw_stages; i++) mbar_init(&h.raw_full[i], 1), mbar_init(&h.raw_empty[i], widen_arrivals);
+      for (int i = 0; i < p.q_stages; i++) mbar_init(&h.q_full[i], 1), mbar_init(&h.q_empty[i], 1);
+      for (int i = 0; i < 4; i++) mbar_init(&h.s_full[i], 1), mbar_init(&h.s_empty[i], s_arrivals);
+      mbar_init(&h.fin, 1);
+      h.dead = 0, h.wait_cycles = p.wait_cycles;
+      mbar_fence_init();
+    }
+  }
+  // rows of a Q tile that no box fills
+  const int filled = p.tokens * p.rep * 8;
+  if (filled < kTile * 8) {
+    for (int i = threadIdx.x; i < p.q_stages * HD / 64 * kBox / 16; i += threads)
+      if (i % (kBox / 16) >= filled) ((uint4*)smem)[i] = make_uint4(0, 0, 0, 0);
+    fence_async_smem();
+  }
+}
+// The producer's K tile of SPAN positions from key0 on.
+template <int HD, bool FP8, int SPAN>
+__device__ __forceinline__ void ask_for_k(bool leader, const CUtensorMap* map, unsigned char* k_tiles, unsigned char* raw_tiles, int at,
+                                          int key0, int head, int seq, uint64_t* full) {
+  using L = WeightsSmem<HD, FP8, SPAN>;
+  expect_tx(leader, full, FP8 ? L::kRawBytes : L::kBytesK);
+  if (FP8) {
+    tma_load_4d(leader, raw_tiles + at * L::kRawBytes, map, 0, key0, head, seq, full);
+  } else {
+#pragma unroll
+    for (int x = 0; x < HD; x += 64) tma_load_4d(leader, k_tiles + at * L::kBytesK + x / 64 * L::kBoxK, map, x, key0, head, seq, full);
+  }
+}
+template <int HD, bool FP8>
+__device__ __forceinline__ void ask_for_q(bool leader, const WeightsParams& p, const CUtensorMap* map, unsigned char* smem, int at, int head,
+                                          int tok0, int seq, uint64_t* full) {
+  expect_tx(leader, full, (unsigned)(p.tokens * p.rep) * HD * 2);
+#pragma unroll
+  for (int x = 0; x < HD; x += 64) tma_load_5d(leader, smem + at * HD / 64 * kBox + x / 64 * kBox, map, x, 0, head, tok0, seq, full);
+}
+// The block's end, behind a barrier: if a wait ran out, copies and products in flight end (waits again, with a limit) before their
+// memory is given back.
+__device__ __noinline__ void weights_end(WeightsHead& h, int warp, int producer, uint64_t* k_full, unsigned k_asked, unsigned k_stages,
+                                         unsigned q_asked, unsigned q_stages) {
+  if (h.dead) {
+    if (warp == producer) {
+      const auto drain = [&](uint64_t* full, unsigned asked, unsigned stages) {
+        for (unsigned i = asked > stages ? asked - stages : 0; i < asked; i++)
+          for (int n = 0; n < 1 << 16 && !__all_sync(~0u, mbar_try_wait(&full[i % stages], i / stages & 1)); n++) {}
+      };
+      drain(k_full, k_asked, k_stages);
+      drain(h.q_full, q_asked, q_stages);
+    }
+    if (warp == producer + 1) {
+      mma_commit(elect_one(), &h.fin);
+      for (int n = 0; n < 1 << 16 && !__all_sync(~0u, mbar_try_wait(&h.fin, 0)); n++) {}
+    }
+    __syncthreads();
+  }
+  if (warp == producer + 1) tmem_free(h.tmem, 512);
+}
+
+// ---- few rows ---------------------------------------------------------------------------------------------------
 // The sum of a tile with values that are not finite, element by element: what is left out or hidden must not come in.
 __device__ __noinline__ float weights_careful(unsigned ts, const float* less, int columns, int from, float c) {
   float sum = 0.f;
@@ -155,319 +349,430 @@ __device__ __noinline__ float weights_careful(unsigned ts, const float* less, in
   }
   return sum;
 }
+// What a thread adds up of 16 positions (lanes of TMEM) and 32 columns: it has two columns of every eight, of positions l / 4 (acc[0])
+// and l / 4 + 8 (acc[1]).  So a column's `less` is read once for eight positions and not for each.  less: this lane's first.
+// Positions see the columns from `from` on only, counted from this lane's first.
+__device__ __forceinline__ void add_columns(uint64_t (&acc)[2], const unsigned (&w)[16], const float* less, uint64_t c2, bool hides, int from0,
+                                            int from1) {
+#pragma unroll
+  for (int b = 0; b < 4; b++) {
+    const float2 l = *(const float2*)(less + 8 * b);
+#pragma unroll
+    for (int g = 0; g < 2; g++) {
+      float e0, e1;
+      unpair(e0, e1, fma2(pair(__uint_as_float(w[4 * b + 2 * g]), __uint_as_float(w[4 * b + 2 * g + 1])), c2, pair(l.x, l.y)));
+      e0 = exp2_fast(e0), e1 = exp2_fast(e1);
+      if (hides) {
+        const int from = g ? from1 : from0;
+        if (8 * b < from) e0 = 0.f;
+        if (8 * b + 1 < from) e1 = 0.f;
+      }
+      acc[g] = add2(acc[g], pair(e0, e1));
+    }
+  }
+}
 
+constexpr int kFewGroups = 3, kWideners = 4;           // warpgroups for the exponentials, warps that widen 8-bit tiles
+template <bool FP8>
+constexpr int kFewThreads = 32 * (4 * kFewGroups + 2 + (FP8 ? kWideners : 0));
+
+// A producer warp brings K tiles, and Q once a head, by TMA, one warp issues the products into four accumulators in turn, three
+// warpgroups take every third product each, so that the next one is there when they have done one.
 template <int HD, bool FP8>
-__global__ void __launch_bounds__(FP8 ? 704 : 576, 1)
-    weights_kernel(const WeightsParams p, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k) {
-  using L = WeightsSmem<HD, FP8>;
-  constexpr int kProducer = 16, kIssuer = 17;
+__global__ void __launch_bounds__(kFewThreads<FP8>, 1)
+    weights_few_kernel(const WeightsParams p, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k) {
+  using L = WeightsSmem<HD, FP8, kTile>;
+  constexpr int kProducer = 4 * kFewGroups, kIssuer = kProducer + 1;
   unsigned char* smem = attn_smem();
   WeightsHead& h = *(WeightsHead*)(smem + L::kHead);
   const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
-
-  if (warp == kIssuer) {
-    tmem_alloc(&h.tmem, 512);
-    if (lane == 0) {
-      for (int i = 0; i < L::kStages; i++) mbar_init(&h.k_full[i], FP8 ? 4 : 1), mbar_init(&h.k_empty[i], 1);
-      for (int i = 0; i < L::kRawStages; i++) mbar_init(&h.raw_full[i], 1), mbar_init(&h.raw_empty[i], 4);
-      for (int i = 0; i < L::kQStages; i++) mbar_init(&h.q_full[i], 1), mbar_init(&h.q_empty[i], 1);
-      for (int i = 0; i < 4; i++) mbar_init(&h.s_full[i], 1), mbar_init(&h.s_empty[i], 4);
-      for (int i = 0; i < kSumRing; i++) mbar_init(&h.sums_full[i], 16);
-      mbar_init(&h.fin, 1);
-      h.dead = 0, h.wait_cycles = p.wait_cycles;
-      mbar_fence_init();
-    }
-  }
+  weights_begin<HD, FP8>(p, h, smem, kIssuer, warp, lane, kWideners, 4, kFewThreads<FP8>);
   if (warp == kProducer) prefetch_map(lane == 0, &map_q), prefetch_map(lane == 0, &map_k);
-  // rows of a Q tile that no box fills
-  for (int i = threadIdx.x; i < L::kQStages * L::kTileBytes / 16; i += L::kThreads)
-    if (i % (kBox / 16) >= p.tokens * p.rep * 8) ((uint4*)(smem + L::kQ))[i] = make_uint4(0, 0, 0, 0);
-  fence_async_smem();
   wait_for_grid_before();
-  if (warp == 0) {
-    // which run is this block's
-    auto steps_of = [&](int s) { return s < p.n_seqs ? weights_steps(p, __ldg(p.lens + s)) * p.nkv : 0; };
-    const int mine = steps_of(lane);
-    int total = mine;
-    for (int s = 32 + lane; s < p.n_seqs; s += 32) total += steps_of(s);
-    total = warp_sum(total);
-    const int per = (total + (int)gridDim.x - 1) / (int)gridDim.x;
-    int at = (int)blockIdx.x * per, seq = 0, head = 0, tile = 0, step = 0, left = 0;
-    if ((int64_t)blockIdx.x * per < total) {
-      left = min(per, total - at);
-      for (int s0 = 0; s0 < p.n_seqs; s0 += 32) {
-        const int own = s0 ? steps_of(s0 + lane) : mine;
-        int n = own;
+  if (warp == 0) find_run<kTile>(p, h.start);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const unsigned tmem = uniform(h.tmem);
+  unsigned k_asked = 0, q_asked = 0;                   // the producer's
+  unsigned char *k_tiles = smem + p.q_stages * L::kTileBytes, *raw_tiles = k_tiles + p.k_stages * L::kTileBytes;
+  WeightsWalk<kTile> walk;
+  walk.init(p, h.start);
+  WeightsUnit u;
+  if (warp < kProducer) {
+    // ================================ exponentials and sums ============================================================
+    const int wg = warp >> 2, id = (warp & 3) * 32 + (lane >> 2) + 8 * (lane & 3);       // id: this thread's position of a tile
+    const unsigned lanes = tmem + ((unsigned)(warp & 3) * 32 << 16);
+    const float c = p.scale * kLog2e;
+    float* row = h.less[warp];
+    const float* mine_of = row + 2 * (lane & 3);
+    int l_seq = -1, l_head = -1;                       // whose rows `row` has
+    for (int j = 0; walk.next(p, u); j++) {
+      if (j % kFewGroups != wg) continue;
+      const int key0 = u.at * kTile;
+      if (u.seq != l_seq || u.head != l_head) {        // every warp brings the rows for itself
+        l_seq = u.seq, l_head = u.head;
+        const float* lse = p.lse + (int64_t)u.seq * p.rows * p.nq + u.head * p.rep;
+        float l[4];
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const int x = __shfl_up_sync(~0u, n, o);
-          if (lane >= o) n += x;
+        for (int k = 0; k < 4; k++) {
+          const int r = lane + 32 * k, t = p.rep_inv ? (int)__umulhi((unsigned)r, p.rep_inv) : r;
+          l[k] = t < p.rows ? __ldg(lse + (int64_t)t * p.nq + r - t * p.rep) : CUDART_INF_F;
         }
-        const unsigned hit = __ballot_sync(~0u, n > at);
-        if (hit) {
-          const int f = __ffs(hit) - 1;
-          seq = s0 + f;
-          int rel = at - __shfl_sync(~0u, n - own, f);
-          const int len = __ldg(p.lens + seq), of_head = __shfl_sync(~0u, own, f) / p.nkv;
-          head = rel / of_head, rel -= head * of_head;
-          const int tiles = weights_tiles(p, len), full = p.q_tiles == 1 ? tiles : min(tiles, len / kTile + 1);
-          if (rel < full * p.q_tiles) {
-            tile = rel / p.q_tiles, step = rel - tile * p.q_tiles;
-          } else {
-            rel -= full * p.q_tiles;
-            for (tile = full;; tile++) {
-              const int steps = p.q_tiles - first_q_tile(p, len, tile);
-              if (rel < steps) break;
-              rel -= steps;
-            }
-            step = rel;
-          }
-          break;
-        }
-        at -= __shfl_sync(~0u, n, 31);
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < 4; k++) row[lane + 32 * k] = fabsf(l[k]) == CUDART_INF_F ? -CUDART_INF_F : -l[k] * kLog2e;
+        __syncwarp();
       }
+      const bool hides = key0 + kTile - 1 > u.len;
+      // the first column that this lane's first position sees, less its first column; a position further on sees rep less
+      const int from = hides ? (min(max(key0 - u.len, -kTile), kTile) + (warp & 3) * 32 + (lane >> 2)) * p.rep - 2 * (lane & 3) : 0;
+      const unsigned ts = lanes + (j & 3) * kTile;
+      attn_wait(&h.s_full[j & 3], j >> 2 & 1, h);
+      __syncwarp();
+      tc_fence_after();
+      const uint64_t c2 = pair(c, c);
+      uint64_t acc[2][2] = {};                         // [16 positions][8 of them]
+      // 16 positions are on their way while 16 are worked on
+      unsigned w0[16], w1[16];
+      tmem_ld_16x256b_x4(w0, ts);
+#pragma unroll 1
+      for (int x = 0; x < p.columns; x += 32) {
+        tmem_wait_ld();
+        tmem_pin(w0);
+        tmem_ld_16x256b_x4(w1, ts + (16 << 16) + x);
+        add_columns(acc[0], w0, mine_of + x, c2, hides, from - x, from - x + 8 * p.rep);
+        tmem_wait_ld();
+        tmem_pin(w1);
+        if (x + 32 < p.columns) tmem_ld_16x256b_x4(w0, ts + x + 32);
+        add_columns(acc[1], w1, mine_of + x, c2, hides, from - x + 16 * p.rep, from - x + 24 * p.rep);
+      }
+      float a[4];
+#pragma unroll
+      for (int k = 0; k < 4; k++) {
+        float lo, hi;
+        unpair(lo, hi, acc[k >> 1][k & 1]);
+        a[k] = lo + hi;
+        a[k] += __shfl_xor_sync(~0u, a[k], 1);
+        a[k] += __shfl_xor_sync(~0u, a[k], 2);
+      }
+      // a position for each lane: l / 4 + 8 (l % 4)
+      float sum = lane & 2 ? (lane & 1 ? a[3] : a[2]) : (lane & 1 ? a[1] : a[0]);
+      if (__any_sync(~0u, !(sum < CUDART_INF_F))) {
+        const float s = weights_careful(ts, row, p.columns, hides ? min(max(key0 + (warp & 3) * 32 + lane - u.len, 0), kTile) * p.rep : 0, c);
+        sum = __shfl_sync(~0u, s, (lane >> 2) + 8 * (lane & 3));
+      }
+      tc_fence_before();
+      warp_arrive(&h.s_empty[j & 3], lane);
+      weights_write(p, u.seq, u.head, u.len, key0 + id, sum);
     }
-    if (lane == 0) h.start[0] = seq, h.start[1] = head, h.start[2] = tile, h.start[3] = step, h.start[4] = left;
+    fill_behind<kTile>(p, 128 * kFewGroups);
+  } else if (warp == kProducer) {
+    // ================================ tiles ============================================================================
+    const bool leader = elect_one();
+    const int n_k = FP8 ? p.raw_stages : p.k_stages;   // the ring that K comes into
+    int q_seq = -1, q_head = -1;
+    RingAt k, q;
+    bool on = true;
+    while (walk.next(p, u)) {
+      uint64_t *full = FP8 ? &h.raw_full[k.at] : &h.k_full[k.at], *empty = FP8 ? &h.raw_empty[k.at] : &h.k_empty[k.at];
+      on = attn_wait(empty, k.round ^ 1, h) && on && k_asked < p.tiles;
+      if (on) {
+        ask_for_k<HD, FP8, kTile>(leader, &map_k, k_tiles, raw_tiles, k.at, u.at * kTile, u.head, u.seq, full);
+        k_asked++;
+      }
+      k.next(n_k);
+      if (u.seq == q_seq && u.head == q_head) continue;
+      q_seq = u.seq, q_head = u.head;
+      on = attn_wait(&h.q_empty[q.at], q.round ^ 1, h) && on;
+      if (on) {
+        ask_for_q<HD, FP8>(leader, p, &map_q, smem, q.at, u.head, 0, u.seq, &h.q_full[q.at]);
+        q_asked++;
+      }
+      q.next(p.q_stages);
+    }
+  } else if (warp == kIssuer) {
+    // ================================ the matrix products ==============================================================
+    const bool leader = elect_one();
+    const unsigned id_s = mma_idesc(kTile, 0, false, false) | (unsigned)(p.columns >> 3) << 17;
+    const uint64_t q_desc = smem_desc(smem_u32(smem), 16, 1024), k_desc = smem_desc(smem_u32(k_tiles), 16, 1024);
+    constexpr uint64_t kTileStep = L::kTileBytes >> 4;
+    int q_seq = -1, q_head = -1, held = -1;            // held: the Q tile that is worked on
+    RingAt k, q;
+    bool on = true;
+    for (int j = 0; uniform(walk.next(p, u)); j++) {
+      if (uniform(u.seq != q_seq || u.head != q_head)) {
+        q_seq = u.seq, q_head = u.head;
+        if (on && held >= 0) mma_commit(leader, &h.q_empty[held]);
+        held = uniform(q.at);
+        on = attn_wait(&h.q_full[held], q.round, h) && on;
+        q.next(p.q_stages);
+      }
+      on = attn_wait(&h.k_full[k.at], k.round, h) && on;
+      const int at = uniform(j & 3);
+      on = attn_wait(&h.s_empty[at], (j >> 2 & 1) ^ 1, h) && on;
+      if (on) {
+        tc_fence_after();
+        const uint64_t ka = k_desc + uniform(k.at) * kTileStep, qa = q_desc + held * kTileStep;
+#pragma unroll
+        for (int e = 0; e < HD / 16; e++) {
+          const int off = (e / 4 * kBox + e % 4 * 32) >> 4;
+          mma_ss(leader, tmem + at * kTile, ka + off, qa + off, id_s, e > 0);
+        }
+        mma_commit(leader, &h.s_full[at]);
+        mma_commit(leader, &h.k_empty[k.at]);
+      }
+      k.next(p.k_stages);
+    }
+  } else if (FP8) {
+    // ================================ 8-bit tiles widened to bf16 ======================================================
+    RingAt raw, k;
+    while (walk.next(p, u)) {
+      attn_wait(&h.raw_full[raw.at], raw.round, h);
+      attn_wait(&h.k_empty[k.at], k.round ^ 1, h);
+      widen_tile<HD, kTile, 4>(k_tiles + k.at * L::kTileBytes, raw_tiles + raw.at * L::kRawBytes, (warp - kIssuer - 1) * 32 + lane, 32 * kWideners);
+      fence_async_smem();
+      warp_arrive(&h.k_full[k.at], lane);
+      warp_arrive(&h.raw_empty[raw.at], lane);
+      k.next(p.k_stages), raw.next(p.raw_stages);
+    }
   }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  weights_end(h, warp, kProducer, FP8 ? h.raw_full : h.k_full, k_asked, FP8 ? p.raw_stages : p.k_stages, q_asked, p.q_stages);
+}
+
+// ---- many rows --------------------------------------------------------------------------------------------------
+// kPoly of a thread's 32 pairs of exponentials are made on the fma pipe (0 / 4 / 8 / 12: 7001 tokens, 32 heads of 128 on 8: XXX us).
+constexpr int kPoly = 6;
+// 16 positions' sums over this lane's row: 2^(S c + less).  HIDES: positions from `end` on are hidden.
+template <bool HIDES, int FIRST>
+__device__ __forceinline__ void add_row(uint64_t (&acc)[32], const unsigned (&w)[16], uint64_t c2, uint64_t less2, int end) {
+#pragma unroll
+  for (int k = 0; k < 8; k++) {
+    const uint64_t x = fma2(pair(__uint_as_float(w[2 * k]), __uint_as_float(w[2 * k + 1])), c2, less2);
+    uint64_t& a = acc[FIRST / 2 + k];
+    if (!HIDES && (FIRST / 2 + k) * kPoly % 32 < kPoly) {
+      a = add_powers(x, a);
+    } else {
+      float e0, e1;
+      unpair(e0, e1, x);
+      e0 = exp2_fast(e0), e1 = exp2_fast(e1);
+      if (HIDES) e0 = FIRST + 2 * k < end ? e0 : 0.f, e1 = FIRST + 2 * k + 1 < end ? e1 : 0.f;
+      a = add2(a, pair(e0, e1));
+    }
+  }
+}
+
+// Lanes that differ in bit O: each keeps one half of 4 O sums, and adds the other one's.
+template <int O>
+__device__ __forceinline__ void exchange(float (&v)[64], int lane) {
+  const bool upper = lane & O;
+#pragma unroll
+  for (int i = 0; i < 2 * O; i++) {
+    const float give = upper ? v[i] : v[i + 2 * O], take = upper ? v[i + 2 * O] : v[i];
+    v[i] = take + __shfl_xor_sync(~0u, give, O);
+  }
+}
+
+// A unit is 192 positions, 64 for each of three warpgroups (four warpgroups have too few registers for 64 sums: 450 us, spilled), the
+// products of the steps in two accumulators in turn.  A unit that a run's border cuts leaves its parts in scratch and a second
+// kernel adds them, in the order of the blocks.
+constexpr int kManySpan = 192, kManyThreads = 448;
+template <int HD, bool FP8>
+__global__ void __launch_bounds__(kManyThreads, 1)
+    weights_many_kernel(const WeightsParams p, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k) {
+  using L = WeightsSmem<HD, FP8, kManySpan>;
+  constexpr int kProducer = 12, kIssuer = 13, kSpan = kManySpan;
+  unsigned char* smem = attn_smem();
+  WeightsHead& h = *(WeightsHead*)(smem + L::kHead);
+  const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+  weights_begin<HD, FP8>(p, h, smem, kIssuer, warp, lane, 12, 12, kManyThreads);
+  if (warp == kProducer) prefetch_map(lane == 0, &map_q), prefetch_map(lane == 0, &map_k);
+  wait_for_grid_before();
+  if (warp == 0) find_run<kSpan>(p, h.start);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const unsigned tmem = uniform(h.tmem);
   unsigned k_asked = 0, q_asked = 0;                   // the producer's
-
-  WeightsWalk walk;
-  walk.init(p, h);
+  unsigned char *k_tiles = smem + p.q_stages * L::kTileBytes, *raw_tiles = k_tiles + p.k_stages * L::kBytesK;
+  WeightsWalk<kSpan> walk;
+  walk.init(p, h.start);
   WeightsUnit u;
-  if (warp < 16) {
+  if (warp < kProducer) {
     // ================================ exponentials and sums ============================================================
-    const int wg = warp >> 2, id = threadIdx.x & 127;
-    const unsigned ts = tmem + ((unsigned)(warp & 3) * 32 << 16) + wg * kTile;
+    const int wg = warp >> 2, r = (warp & 3) * 32 + lane;      // r: this thread's row of a Q tile
+    const unsigned lanes = tmem + ((unsigned)(warp & 3) * 32 << 16) + wg * 64;
+    const int own_tok = p.rep_inv ? (int)__umulhi((unsigned)r, p.rep_inv) : r, own_head = r - own_tok * p.rep;
     const float c = p.scale * kLog2e;
-    // slots behind the tiles, and sequences of an impossible length
-    for (int r = blockIdx.x; r < p.n_seqs * p.nkv; r += gridDim.x) {
-      const int s = r / p.nkv, len = __ldg(p.lens + s), tiles = weights_tiles(p, len);
-      float* out = p.out + s * p.o_seq + (r - s * p.nkv) * p.o_head;
-      for (int64_t i = (int64_t)tiles * kTile + threadIdx.x; i < p.slots; i += 512) out[i] = tiles ? 0.f : CUDART_NAN_F;
-    }
-    const int own_tok = id / p.rep, own_head = id - own_tok * p.rep;   // the query row of a tile whose lse this thread brings
-    const bool own_row = own_tok < p.tokens;
-    int g = 0, mine = 0, shared = 0;                   // steps in front of this unit, steps of this warpgroup, units of several steps
+    const uint64_t c2 = pair(c, c);
+    unsigned j = 0;                                    // steps in front
+    RingAt raw, k;
     bool cut0 = false, cut1 = false;
     while (walk.next(p, u)) {
-      const int n = u.end - u.begin, key0 = u.tile * kTile, key = key0 + id;
-      const float* lse = p.lse + (int64_t)u.seq * p.rows * p.nq + u.head * p.rep + own_head;
-      const auto less_of = [&](int i) {                // of this thread's row of step i
-        const int tok = (u.first + u.begin + i) * p.tokens + own_tok;
-        float l = CUDART_INF_F;
-        if (own_row && tok < p.rows) l = __ldg(lse + (int64_t)tok * p.nq);
-        return fabsf(l) == CUDART_INF_F ? -CUDART_INF_F : -l * kLog2e;
+      if (FP8) {                                       // widened by all
+        attn_wait(&h.raw_full[raw.at], raw.round, h);
+        attn_wait(&h.k_empty[k.at], k.round ^ 1, h);
+        widen_tile<HD, kSpan, 2>(k_tiles + k.at * L::kBytesK, raw_tiles + raw.at * L::kRawBytes, threadIdx.x, 32 * kProducer);
+        fence_async_smem();
+        warp_arrive(&h.k_full[k.at], lane);
+        warp_arrive(&h.raw_empty[raw.at], lane);
+        k.next(p.k_stages), raw.next(p.raw_stages);
+      }
+      const int base = u.at * kSpan + wg * 64;         // first position of this warpgroup
+      const float* lse = p.lse + ((int64_t)u.seq * p.rows + own_tok) * p.nq + u.head * p.rep + own_head;
+      const auto lse_of = [&](int tok0) {              // of this thread's row of the tile from token tok0 on
+        return own_tok < p.tokens && tok0 + own_tok < p.rows ? __ldg(lse + (int64_t)tok0 * p.nq) : CUDART_INF_F;
       };
-      float sum = 0.f;
-      int i = (wg - g) & 3;
-      float less = i < n ? less_of(i) : 0.f;
-      for (; i < n; i += 4, mine++) {
-        float* row = h.less[wg][mine & 1];
-        row[id] = less;
-        named_barrier(1 + wg, 128);
-        const int tok0 = (u.first + u.begin + i) * p.tokens;
-        const bool hides = key0 + kTile - 1 - u.len > tok0;
-        const int from = hides ? min(max(key - u.len - tok0, 0), kTile) * p.rep : 0;    // first row that sees this position
-        if (i + 4 < n) less = less_of(i + 4);
-        attn_wait(&h.s_full[wg], mine & 1, h);
+      int tok0 = (u.first + u.begin) * p.tokens;
+      float l = lse_of(tok0);
+      uint64_t acc[32];                                // sums of 64 positions
+#pragma unroll
+      for (int i = 0; i < 32; i++) acc[i] = 0;
+#pragma unroll 1
+      for (int i = u.begin; i < u.end; i++, j++) {
+        const bool out = fabsf(l) == CUDART_INF_F;     // (a row that adds nothing sees nothing)
+        const int end = out ? 0 : u.len + tok0 + own_tok + 1 - base;
+        const float less = out ? -CUDART_INF_F : -l * kLog2e;
+        const bool hides = __any_sync(~0u, end < 64), sees = __any_sync(~0u, end > 0);
+        tok0 += p.tokens;
+        if (i + 1 < u.end) l = lse_of(tok0);
+        const unsigned ts = lanes + (j & 1) * 256;
+        attn_wait(&h.s_full[j & 1], j >> 1 & 1, h);
         __syncwarp();
         tc_fence_after();
-        const uint64_t c2 = pair(c, c);
-        uint64_t acc[2] = {0, 0};
-#pragma unroll 1
-        for (int x = 0; x < p.columns; x += 32) {
-          unsigned w[32];
-          tmem_ld32(w, ts + x);
-          tmem_wait_ld();
-          tmem_pin(w);
-#pragma unroll
-          for (int k = 0; k < 32; k += 4) {
-            const float4 l = *(const float4*)(row + x + k);
-            float e[4];
-            unpair(e[0], e[1], fma2(pair(__uint_as_float(w[k]), __uint_as_float(w[k + 1])), c2, pair(l.x, l.y)));
-            unpair(e[2], e[3], fma2(pair(__uint_as_float(w[k + 2]), __uint_as_float(w[k + 3])), c2, pair(l.z, l.w)));
-#pragma unroll
-            for (int j = 0; j < 4; j++) {
-              e[j] = exp2_fast(e[j]);
-              if (hides && x + k + j < from) e[j] = 0.f;
-            }
-            acc[0] = add2(acc[0], pair(e[0], e[1])), acc[1] = add2(acc[1], pair(e[2], e[3]));
-          }
+        if (sees) {
+          const uint64_t less2 = pair(less, less);
+          unsigned w0[16], w1[16];                     // 16 columns are on their way while 16 are worked on
+          const auto have = [&](unsigned (&w)[16]) {
+            tmem_wait_ld();
+            tmem_pin(w);
+          };
+          tmem_ld16(w0, ts);
+          have(w0);
+          tmem_ld16(w1, ts + 16);
+          if (!hides) add_row<false, 0>(acc, w0, c2, less2, 0);
+          else add_row<true, 0>(acc, w0, c2, less2, end);
+          have(w1);
+          tmem_ld16(w0, ts + 32);
+          if (!hides) add_row<false, 16>(acc, w1, c2, less2, 0);
+          else add_row<true, 16>(acc, w1, c2, less2, end);
+          have(w0);
+          tmem_ld16(w1, ts + 48);
+          if (!hides) add_row<false, 32>(acc, w0, c2, less2, 0);
+          else add_row<true, 32>(acc, w0, c2, less2, end);
+          have(w1);
+          if (!hides) add_row<false, 48>(acc, w1, c2, less2, 0);
+          else add_row<true, 48>(acc, w1, c2, less2, end);
         }
-        float a, b;
-        unpair(a, b, add2(acc[0], acc[1]));
-        a += b;
-        if (__any_sync(~0u, !(a < CUDART_INF_F))) a = weights_careful(ts, row, p.columns, from, c);
-        sum += a;
         tc_fence_before();
-        warp_arrive(&h.s_empty[wg], lane);
+        warp_arrive(&h.s_empty[j & 1], lane);
       }
-      const int last = (g + n - 1) & 3;                // the warpgroup that finishes the unit
-      if (n > 1) {
-        const int at = shared % kSumRing;
-        if (wg != last && ((wg - g) & 3) < n) h.sums[at][wg][id] = sum;
-        warp_arrive(&h.sums_full[at], lane);
-        if (wg == last) {
-          attn_wait(&h.sums_full[at], shared / kSumRing & 1, h);
-          float all = 0.f;
+      // The 32 rows of the warp: at each exchange a lane keeps half of its positions and gives away the others, so that it ends
+      // with two of them; then the four warps.
+      float v[64];
 #pragma unroll
-          for (int j = 0; j < 4; j++)
-            if (((j - g) & 3) < n) all += j == wg ? sum : h.sums[at][j][id];
-          sum = all;
-        }
-        shared++;
-      }
+      for (int i = 0; i < 32; i++) unpair(v[2 * i], v[2 * i + 1], acc[i]);
+      exchange<16>(v, lane), exchange<8>(v, lane), exchange<4>(v, lane), exchange<2>(v, lane), exchange<1>(v, lane);
+      // lane l has positions 2 l and 2 l + 1
+      *(float2*)&h.sums[wg][warp & 3][2 * lane] = make_float2(v[0], v[1]);
+      named_barrier(1 + wg, 128);
       const bool whole = u.begin == 0 && u.end == u.all;
-      if (wg == last) {
+      const int id = threadIdx.x & 127;
+      if (id < 64) {
+        const float sum = (h.sums[wg][0][id] + h.sums[wg][1][id]) + (h.sums[wg][2][id] + h.sums[wg][3][id]);
         if (whole) {
-          weights_write(p, u.seq, u.head, u.len, key, sum);
+          weights_write(p, u.seq, u.head, u.len, base + id, sum);
         } else {
-          const int at = 2 * blockIdx.x + (u.begin == 0);
-          p.part[(int64_t)at * kTile + id] = sum;
-          if (id == 0) p.part_of[at] = make_int4(u.seq, u.head, u.tile, u.end < u.all);
+          const int rec = 2 * blockIdx.x + (u.begin == 0);
+          p.part[(int64_t)rec * kSpan + wg * 64 + id] = sum;
+          if (id == 0 && wg == 0) p.part_of[rec] = make_int4(u.seq, u.head, u.at, u.end < u.all);
         }
       }
+      named_barrier(1 + wg, 128);                      // (the sums have been read)
       if (!whole) (u.begin == 0 ? cut1 : cut0) = true;
-      g += n;
     }
-    if (threadIdx.x == 0 && p.part) {
+    if (threadIdx.x == 0) {
       if (!cut0) p.part_of[2 * blockIdx.x] = make_int4(-1, 0, 0, 0);
       if (!cut1) p.part_of[2 * blockIdx.x + 1] = make_int4(-1, 0, 0, 0);
     }
+    fill_behind<kSpan>(p, 32 * kProducer);
   } else if (warp == kProducer) {
     // ================================ tiles ============================================================================
     const bool leader = elect_one();
-    const unsigned q_bytes = (unsigned)(p.tokens * p.rep) * HD * 2;
-    int q_seq = -1, q_head = -1;
+    const int n_k = FP8 ? p.raw_stages : p.k_stages;   // the ring that K comes into
+    RingAt k, q;
     bool on = true;
     while (walk.next(p, u)) {
-      const int n = FP8 ? L::kRawStages : L::kStages, st = k_asked % n;
-      uint64_t *full = FP8 ? &h.raw_full[st] : &h.k_full[st], *empty = FP8 ? &h.raw_empty[st] : &h.k_empty[st];
-      on = on && attn_wait(empty, (k_asked / n & 1) ^ 1, h) && k_asked < p.tiles;
+      uint64_t *full = FP8 ? &h.raw_full[k.at] : &h.k_full[k.at], *empty = FP8 ? &h.raw_empty[k.at] : &h.k_empty[k.at];
+      on = attn_wait(empty, k.round ^ 1, h) && on && k_asked < p.tiles;
       if (on) {
-        expect_tx(leader, full, FP8 ? L::kRawBytes : L::kTileBytes);
-        if (FP8) {
-          tma_load_4d(leader, smem + L::kRaw + st * L::kRawBytes, &map_k, 0, u.tile * kTile, u.head, u.seq, full);
-        } else {
-#pragma unroll
-          for (int x = 0; x < HD; x += 64)
-            tma_load_4d(leader, smem + L::kRing + st * L::kTileBytes + x / 64 * kBox, &map_k, x, u.tile * kTile, u.head, u.seq, full);
-        }
+        ask_for_k<HD, FP8, kSpan>(leader, &map_k, k_tiles, raw_tiles, k.at, u.at * kSpan, u.head, u.seq, full);
         k_asked++;
       }
+      k.next(n_k);
       for (int i = u.begin; i < u.end; i++) {
-        if (p.q_tiles == 1 && u.seq == q_seq && u.head == q_head) continue;      // it is there already
-        q_seq = u.seq, q_head = u.head;
-        const int qs = q_asked % L::kQStages;
-        on = on && attn_wait(&h.q_empty[qs], (q_asked / L::kQStages & 1) ^ 1, h);
-        if (!on) continue;
-        expect_tx(leader, &h.q_full[qs], q_bytes);
-#pragma unroll
-        for (int x = 0; x < HD; x += 64)
-          tma_load_5d(leader, smem + L::kQ + qs * L::kTileBytes + x / 64 * kBox, &map_q, x, 0, u.head, (u.first + i) * p.tokens, u.seq,
-                      &h.q_full[qs]);
-        q_asked++;
+        on = attn_wait(&h.q_empty[q.at], q.round ^ 1, h) && on;
+        if (on) {
+          ask_for_q<HD, FP8>(leader, p, &map_q, smem, q.at, u.head, (u.first + i) * p.tokens, u.seq, &h.q_full[q.at]);
+          q_asked++;
+        }
+        q.next(p.q_stages);
       }
     }
   } else if (warp == kIssuer) {
     // ================================ the matrix products ==============================================================
     const bool leader = elect_one();
-    const unsigned id_s = mma_idesc(kTile, 0, false, false) | (unsigned)(p.columns >> 3) << 17;
-    const uint64_t q_desc = smem_desc(smem_u32(smem + L::kQ), 16, 1024), k_desc = smem_desc(smem_u32(smem + L::kRing), 16, 1024);
-    constexpr uint64_t kTileStep = L::kTileBytes >> 4;
-    int g = 0, k_at = 0, q_at = -1, q_seq = -1, q_head = -1;
+    constexpr unsigned kIdS = mma_idesc(kTile, kSpan, false, false);
+    const uint64_t q_desc = smem_desc(smem_u32(smem), 16, 1024), k_desc = smem_desc(smem_u32(k_tiles), 16, 1024);
+    RingAt k, q;
+    unsigned j = 0;                                    // steps in front
     bool on = true;
-    while (walk.next(p, u)) {
-      const int ks = uniform(k_at % L::kStages);
-      on = on && attn_wait(&h.k_full[ks], k_at / L::kStages & 1, h);
-      for (int i = uniform(u.begin); i < uniform(u.end); i++, g++) {
-        if (p.q_tiles > 1 || u.seq != q_seq || u.head != q_head) {
-          q_seq = u.seq, q_head = u.head;
-          if (on && q_at >= 0) mma_commit(leader, &h.q_empty[q_at % L::kQStages]);
-          q_at++;
-          on = on && attn_wait(&h.q_full[q_at % L::kQStages], q_at / L::kQStages & 1, h);
-        }
-        const int qs = uniform(q_at % L::kQStages), at = uniform(g & 3);
-        on = on && attn_wait(&h.s_empty[at], (g >> 2 & 1) ^ 1, h);
-        if (!on) continue;
-        tc_fence_after();
-        const uint64_t ka = k_desc + ks * kTileStep, qa = q_desc + qs * kTileStep;
+    while (uniform(walk.next(p, u))) {
+      on = attn_wait(&h.k_full[k.at], k.round, h) && on;
+      const uint64_t ka = k_desc + uniform(k.at) * (uint64_t)(L::kBytesK >> 4);
+      const int n = uniform(u.end - u.begin);
+      for (int i = 0; i < n; i++, j++) {
+        on = attn_wait(&h.q_full[q.at], q.round, h) && on;
+        const uint64_t qa = q_desc + uniform(q.at) * (uint64_t)(L::kTileBytes >> 4);
+        const int at = uniform(j & 1);
+        on = attn_wait(&h.s_empty[at], (j >> 1 & 1) ^ 1, h) && on;
+        if (on) {
+          tc_fence_after();
 #pragma unroll
-        for (int k = 0; k < HD / 16; k++) {
-          const int off = (k / 4 * kBox + k % 4 * 32) >> 4;
-          mma_ss(leader, tmem + at * kTile, ka + off, qa + off, id_s, k > 0);
+          for (int e = 0; e < HD / 16; e++)
+            mma_ss(leader, tmem + at * 256, qa + ((e / 4 * kBox + e % 4 * 32) >> 4), ka + ((e / 4 * L::kBoxK + e % 4 * 32) >> 4), kIdS, e > 0);
+          mma_commit(leader, &h.s_full[at]);
+          mma_commit(leader, &h.q_empty[q.at]);
         }
-        mma_commit(leader, &h.s_full[at]);
+        q.next(p.q_stages);
       }
-      if (on) mma_commit(leader, &h.k_empty[ks]);
-      k_at++;
-    }
-  } else if (FP8) {
-    // ================================ 8-bit tiles widened to bf16: four warps ==========================================
-    const int ct = (warp - 18) * 32 + lane;
-    constexpr int kChunks = HD / 16;                   // 16-byte chunks of an 8-bit row, each two of a bf16 row
-    constexpr int kRaws = FP8 ? L::kRawStages : 1;
-    int pos = 0;
-    while (walk.next(p, u)) {
-      const int raw = pos % kRaws, st = pos % L::kStages;
-      attn_wait(&h.raw_full[raw], pos / kRaws & 1, h);
-      attn_wait(&h.k_empty[st], (pos / L::kStages & 1) ^ 1, h);
-      const unsigned char* src = smem + L::kRaw + raw * L::kRawBytes;
-      unsigned char* dst = smem + L::kRing + st * L::kTileBytes;
-#pragma unroll 2
-      for (int i = ct; i < kTile * kChunks; i += 128) {
-        const int row = i / kChunks, cc = i % kChunks * 2;
-        const uint4 v = *(const uint4*)(src + i * 16);
-        unsigned w[8];
-        widen_e4m3_bf16(w, v.x), widen_e4m3_bf16(w + 2, v.y), widen_e4m3_bf16(w + 4, v.z), widen_e4m3_bf16(w + 6, v.w);
-        unsigned char* to = dst + cc / 8 * kBox + row * 128;
-        *(uint4*)(to + (((cc & 7) ^ (row & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
-        *(uint4*)(to + ((((cc & 7) + 1) ^ (row & 7)) << 4)) = make_uint4(w[4], w[5], w[6], w[7]);
-      }
-      fence_async_smem();
-      warp_arrive(&h.k_full[st], lane);
-      warp_arrive(&h.raw_empty[raw], lane);
-      pos++;
+      if (on) mma_commit(leader, &h.k_empty[k.at]);
+      k.next(p.k_stages);
     }
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (h.dead) {                                        // copies and products in flight end before their memory is given back
-    constexpr unsigned kN = FP8 ? L::kRawStages : L::kStages;
-    if (warp == kProducer) {
-      uint64_t* full = FP8 ? h.raw_full : h.k_full;
-      for (unsigned i = k_asked > kN ? k_asked - kN : 0; i < k_asked; i++)
-        for (int n = 0; n < 1 << 16 && !__all_sync(~0u, mbar_try_wait(&full[i % kN], i / kN & 1)); n++) {}
-      for (unsigned i = q_asked > L::kQStages ? q_asked - L::kQStages : 0; i < q_asked; i++)
-        for (int n = 0; n < 1 << 16 && !__all_sync(~0u, mbar_try_wait(&h.q_full[i % L::kQStages], i / L::kQStages & 1)); n++) {}
-    }
-    if (warp == kIssuer) {
-      mma_commit(elect_one(), &h.fin);
-      for (int n = 0; n < 1 << 16 && !__all_sync(~0u, mbar_try_wait(&h.fin, 0)); n++) {}
-    }
-    __syncthreads();
-  }
-  if (warp == kIssuer) tmem_free(tmem, 512);
+  weights_end(h, warp, kProducer, FP8 ? h.raw_full : h.k_full, k_asked, FP8 ? p.raw_stages : p.k_stages, q_asked, p.q_stages);
 }
 
 // The parts of units that a border cut: one block for each block of the first kernel in whose run such a unit begins.
-static __global__ void __launch_bounds__(kTile) weights_join_kernel(const WeightsParams p, int blocks) {
+static __global__ void __launch_bounds__(kManySpan) weights_join_kernel(const WeightsParams p, int blocks) {
+  constexpr int kSpan = kManySpan;                     // (as many threads)
   wait_for_grid_before();
   int at = 2 * blockIdx.x + 1;
   const int4 of = p.part_of[at];
   if (of.x < 0) return;
-  float sum = p.part[(int64_t)at * kTile + threadIdx.x];
+  float sum = p.part[(int64_t)at * kSpan + threadIdx.x];
   for (at++; at < 2 * blocks; at += 2) {
-    sum += p.part[(int64_t)at * kTile + threadIdx.x];
+    sum += p.part[(int64_t)at * kSpan + threadIdx.x];
     if (!p.part_of[at].w) break;
   }
-  weights_write(p, of.x, of.y, p.lens[of.x], of.z * kTile + threadIdx.x, sum);
+  weights_write(p, of.x, of.y, p.lens[of.x], of.z * kSpan + threadIdx.x, sum);
 }
 
 }  // namespace amk
