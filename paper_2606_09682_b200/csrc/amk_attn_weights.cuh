@@ -7,7 +7,7 @@
 // one tile of queries, and what counts is K's way from HBM.  weights_few_kernel takes S^T = K Q^T: a position is a lane of TMEM.
 //
 // Many rows: what counts are the exponentials, 16 a cycle and SM, four times as long as the products.  weights_many_kernel takes
-// S = Q K^T: a query row is a lane, whose L is a scalar, and a thread keeps the sums of 64 positions in registers over all
+// S = Q K^T: a query row is a lane, whose L is a scalar, and a thread keeps the sums of 40 positions in registers over all
 // query tiles of a unit; lanes are added up once, at its end.  (With the positions in the lanes there too every column's L is
 // read from shared memory, in front of every exponential, and each warp adds a chain of its own: 7001 tokens, 32 heads of
 // 128 on 8: 257 us; so: XXX us.)
@@ -21,7 +21,7 @@ struct WeightsParams {
   const int* lens;
   const float* before;
   float* out;
-  float* part;                     // many rows: [2 * gridDim][192]: sums of cut units
+  float* part;                     // many rows: [2 * gridDim][160]: sums of cut units
   int4* part_of;                   // [2 * gridDim]: {sequence, head, unit, whether the next block goes on}; sequence -1: none
   int64_t b_seq, b_head, o_seq, o_head;
   int n_seqs, nq, nkv, rep, rows, slots;
@@ -79,29 +79,6 @@ __device__ __forceinline__ void widen_tile(unsigned char* dst, const unsigned ch
       *(uint4*)(to + ((((cc & 7) + 1 - swap) ^ (row & 7)) << 4)) = swap ? x : y;
     }
   }
-}
-
-// The unit of exponentials makes 16 a cycle and SM, so some are made on the fma pipe: 2^x = 2^n 2^f with n the nearest integer,
-// 2^f a polynomial with the constant 1 whose largest relative error on [-1/2, 1/2] is least (9.1e-8; 1.7e-7 as computed;
-// coefficients from that linear programme).  x is kept at or above -127, where 2^n is made as 0 (so -infinity gives 0), and
-// at or below 128, where it is infinity; NaN stays NaN.
-__device__ __forceinline__ float clamp_exponent(float x) {
-  float a, b;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(a) : "f"(x), "f"(-127.f));
-  asm("min.NaN.f32 %0, %1, %2;" : "=f"(b) : "f"(a), "f"(128.f));
-  return b;
-}
-__device__ __forceinline__ uint64_t add_powers(uint64_t x, uint64_t acc) {           // acc + 2^x
-  const float magic = 12582912.f;                      // 1.5 * 2^23: leaves the integer in the low bits
-  float a, b;
-  unpair(a, b, x);
-  const uint64_t y = pair(clamp_exponent(a), clamp_exponent(b)), t = add2(y, pair(magic, magic));
-  const uint64_t f = fma2(add2(t, pair(-magic, -magic)), pair(-1.f, -1.f), y);
-  uint64_t v = fma2(pair(0.0013264727f, 0.0013264727f), f, pair(0.009671513f, 0.009671513f));
-  v = fma2(v, f, pair(0.055507336f, 0.055507336f)), v = fma2(v, f, pair(0.24022242f, 0.24022242f));
-  v = fma2(v, f, pair(0.693147f, 0.693147f)), v = fma2(v, f, pair(1.f, 1.f));
-  unpair(a, b, t);
-  return fma2(v, pair(__uint_as_float((__float_as_uint(a) << 23) + 0x3f800000u), __uint_as_float((__float_as_uint(b) << 23) + 0x3f800000u)), acc);
 }
 
 // a position's sum, finished
@@ -254,7 +231,7 @@ struct WeightsHead {
   unsigned wait_cycles;
   int start[6];                        // where the block's run begins
   alignas(16) float less[12][kTile];   // few rows: [warp]: -lse log2 e of the rows; -infinity: adds nothing
-  alignas(16) float sums[3][4][64];    // many rows: [warpgroup][warp]: sums of its 32 rows
+  alignas(16) float sums[4][4][40];    // many rows: [warpgroup][warp]: sums of its 32 rows
 };
 static_assert(sizeof(WeightsHead) <= 16384, "head");
 // a place in a ring of tiles and the parity of its round
@@ -544,51 +521,44 @@ __global__ void __launch_bounds__(kFewThreads<FP8>, 1)
 }
 
 // ---- many rows --------------------------------------------------------------------------------------------------
-// kPoly of a thread's 32 pairs of exponentials are made on the fma pipe (0 / 4 / 8 / 12: 7001 tokens, 32 heads of 128 on 8: XXX us).
-constexpr int kPoly = 6;
-// 16 positions' sums over this lane's row: 2^(S c + less).  HIDES: positions from `end` on are hidden.
-template <bool HIDES, int FIRST>
-__device__ __forceinline__ void add_row(uint64_t (&acc)[32], const unsigned (&w)[16], uint64_t c2, uint64_t less2, int end) {
+// N positions' sums over this lane's row: 2^(S c + less).  Hidden: positions from `end` on.
+template <int FIRST, int N>
+__device__ __forceinline__ void add_row(uint64_t (&acc)[20], const unsigned (&w)[N], uint64_t c2, uint64_t less2, bool hides, int end) {
 #pragma unroll
-  for (int k = 0; k < 8; k++) {
-    const uint64_t x = fma2(pair(__uint_as_float(w[2 * k]), __uint_as_float(w[2 * k + 1])), c2, less2);
-    uint64_t& a = acc[FIRST / 2 + k];
-    if (!HIDES && (FIRST / 2 + k) * kPoly % 32 < kPoly) {
-      a = add_powers(x, a);
-    } else {
-      float e0, e1;
-      unpair(e0, e1, x);
-      e0 = exp2_fast(e0), e1 = exp2_fast(e1);
-      if (HIDES) e0 = FIRST + 2 * k < end ? e0 : 0.f, e1 = FIRST + 2 * k + 1 < end ? e1 : 0.f;
-      a = add2(a, pair(e0, e1));
-    }
+  for (int k = 0; k < N / 2; k++) {
+    float e0, e1;
+    unpair(e0, e1, fma2(pair(__uint_as_float(w[2 * k]), __uint_as_float(w[2 * k + 1])), c2, less2));
+    e0 = exp2_fast(e0), e1 = exp2_fast(e1);
+    if (hides) e0 = FIRST + 2 * k < end ? e0 : 0.f, e1 = FIRST + 2 * k + 1 < end ? e1 : 0.f;
+    acc[FIRST / 2 + k] = add2(acc[FIRST / 2 + k], pair(e0, e1));
   }
 }
 
-// Lanes that differ in bit O: each keeps one half of 4 O sums, and adds the other one's.
-template <int O>
-__device__ __forceinline__ void exchange(float (&v)[64], int lane) {
+// Lanes that differ in bit O: each keeps one half of 2 N sums, and adds the other one's.
+template <int O, int N, int ALL>
+__device__ __forceinline__ void exchange(float (&v)[ALL], int lane) {
   const bool upper = lane & O;
 #pragma unroll
-  for (int i = 0; i < 2 * O; i++) {
-    const float give = upper ? v[i] : v[i + 2 * O], take = upper ? v[i + 2 * O] : v[i];
+  for (int i = 0; i < N; i++) {
+    const float give = upper ? v[i] : v[i + N], take = upper ? v[i + N] : v[i];
     v[i] = take + __shfl_xor_sync(~0u, give, O);
   }
 }
 
-// A unit is 192 positions, 64 for each of three warpgroups (four warpgroups have too few registers for 64 sums: 450 us, spilled), the
-// products of the steps in two accumulators in turn.  A unit that a run's border cuts leaves its parts in scratch and a second
-// kernel adds them, in the order of the blocks.
-constexpr int kManySpan = 192, kManyThreads = 448;
+// A unit is 160 positions, 40 for each of four warpgroups, the products of the steps in three accumulators in turn: a warp waits for
+// nobody but the issuer, which is two steps ahead.  (Two accumulators of 192 positions, three warpgroups: their release, the
+// product and its arrival were as long as the exponentials, 250 us; four warpgroups of 64 positions have too few registers,
+// 450 us.)  A unit that a run's border cuts leaves its parts in scratch and a second kernel adds them, in the order of the blocks.
+constexpr int kManySpan = 160, kManyThreads = 576, kManyBuffers = 3;
 template <int HD, bool FP8>
 __global__ void __launch_bounds__(kManyThreads, 1)
     weights_many_kernel(const WeightsParams p, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k) {
   using L = WeightsSmem<HD, FP8, kManySpan>;
-  constexpr int kProducer = 12, kIssuer = 13, kSpan = kManySpan;
+  constexpr int kProducer = 16, kIssuer = 17, kSpan = kManySpan, kEach = kSpan / 4;
   unsigned char* smem = attn_smem();
   WeightsHead& h = *(WeightsHead*)(smem + L::kHead);
   const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
-  weights_begin<HD, FP8>(p, h, smem, kIssuer, warp, lane, 12, 12, kManyThreads);
+  weights_begin<HD, FP8>(p, h, smem, kIssuer, warp, lane, kProducer, kProducer, kManyThreads);
   if (warp == kProducer) prefetch_map(lane == 0, &map_q), prefetch_map(lane == 0, &map_k);
   wait_for_grid_before();
   if (warp == 0) find_run<kSpan>(p, h.start);
@@ -605,12 +575,12 @@ __global__ void __launch_bounds__(kManyThreads, 1)
   if (warp < kProducer) {
     // ================================ exponentials and sums ============================================================
     const int wg = warp >> 2, r = (warp & 3) * 32 + lane;      // r: this thread's row of a Q tile
-    const unsigned lanes = tmem + ((unsigned)(warp & 3) * 32 << 16) + wg * 64;
+    const unsigned lanes = tmem + ((unsigned)(warp & 3) * 32 << 16) + wg * kEach;
     const int own_tok = p.rep_inv ? (int)__umulhi((unsigned)r, p.rep_inv) : r, own_head = r - own_tok * p.rep;
     const float c = p.scale * kLog2e;
     const uint64_t c2 = pair(c, c);
-    unsigned j = 0;                                    // steps in front
-    RingAt raw, k;
+    RingAt raw, k, s;                                  // s: the accumulator
+
     bool cut0 = false, cut1 = false;
     while (walk.next(p, u)) {
       if (FP8) {                                       // widened by all
@@ -622,73 +592,72 @@ __global__ void __launch_bounds__(kManyThreads, 1)
         warp_arrive(&h.raw_empty[raw.at], lane);
         k.next(p.k_stages), raw.next(p.raw_stages);
       }
-      const int base = u.at * kSpan + wg * 64;         // first position of this warpgroup
+      const int base = u.at * kSpan + wg * kEach;      // first position of this warpgroup
       const float* lse = p.lse + ((int64_t)u.seq * p.rows + own_tok) * p.nq + u.head * p.rep + own_head;
       const auto lse_of = [&](int tok0) {              // of this thread's row of the tile from token tok0 on
         return own_tok < p.tokens && tok0 + own_tok < p.rows ? __ldg(lse + (int64_t)tok0 * p.nq) : CUDART_INF_F;
       };
       int tok0 = (u.first + u.begin) * p.tokens;
-      float l = lse_of(tok0);
-      uint64_t acc[32];                                // sums of 64 positions
+      float l = lse_of(tok0), l1 = u.begin + 1 < u.end ? lse_of(tok0 + p.tokens) : 0.f;     // two steps ahead
+      uint64_t acc[kEach / 2];                         // sums of 40 positions
 #pragma unroll
-      for (int i = 0; i < 32; i++) acc[i] = 0;
+      for (int i = 0; i < kEach / 2; i++) acc[i] = 0;
+      // Some columns are on their way while others are worked on.
+      unsigned w0[16], w1[16], w2[8];
+      const auto have = [&](auto& w) {
+        tmem_wait_ld();
+        tmem_pin(w);
+      };
 #pragma unroll 1
-      for (int i = u.begin; i < u.end; i++, j++) {
+      for (int i = u.begin; i < u.end; i++) {
         const bool out = fabsf(l) == CUDART_INF_F;     // (a row that adds nothing sees nothing)
         const int end = out ? 0 : u.len + tok0 + own_tok + 1 - base;
         const float less = out ? -CUDART_INF_F : -l * kLog2e;
-        const bool hides = __any_sync(~0u, end < 64), sees = __any_sync(~0u, end > 0);
+        const uint64_t less2 = pair(less, less);
+        const bool hides = __any_sync(~0u, end < kEach);
         tok0 += p.tokens;
-        if (i + 1 < u.end) l = lse_of(tok0);
-        const unsigned ts = lanes + (j & 1) * 256;
-        attn_wait(&h.s_full[j & 1], j >> 1 & 1, h);
+        l = l1;
+        if (i + 2 < u.end) l1 = lse_of(tok0 + p.tokens);
+        attn_wait(&h.s_full[s.at], s.round, h);
         __syncwarp();
         tc_fence_after();
-        if (sees) {
-          const uint64_t less2 = pair(less, less);
-          unsigned w0[16], w1[16];                     // 16 columns are on their way while 16 are worked on
-          const auto have = [&](unsigned (&w)[16]) {
-            tmem_wait_ld();
-            tmem_pin(w);
-          };
-          tmem_ld16(w0, ts);
-          have(w0);
-          tmem_ld16(w1, ts + 16);
-          if (!hides) add_row<false, 0>(acc, w0, c2, less2, 0);
-          else add_row<true, 0>(acc, w0, c2, less2, end);
-          have(w1);
-          tmem_ld16(w0, ts + 32);
-          if (!hides) add_row<false, 16>(acc, w1, c2, less2, 0);
-          else add_row<true, 16>(acc, w1, c2, less2, end);
-          have(w0);
-          tmem_ld16(w1, ts + 48);
-          if (!hides) add_row<false, 32>(acc, w0, c2, less2, 0);
-          else add_row<true, 32>(acc, w0, c2, less2, end);
-          have(w1);
-          if (!hides) add_row<false, 48>(acc, w1, c2, less2, 0);
-          else add_row<true, 48>(acc, w1, c2, less2, end);
-        }
+        const unsigned ts = lanes + s.at * kSpan;
+        tmem_ld16(w0, ts);
+        have(w0);
+        tmem_ld16(w1, ts + 16);
+        add_row<0>(acc, w0, c2, less2, hides, end);
+        have(w1);
+        tmem_ld8(w2, ts + 32);
+        add_row<16>(acc, w1, c2, less2, hides, end);
+        have(w2);
         tc_fence_before();
-        warp_arrive(&h.s_empty[j & 1], lane);
+        warp_arrive(&h.s_empty[s.at], lane);
+        s.next(kManyBuffers);
+        add_row<32>(acc, w2, c2, less2, hides, end);
       }
-      // The 32 rows of the warp: at each exchange a lane keeps half of its positions and gives away the others, so that it ends
-      // with two of them; then the four warps.
-      float v[64];
+      // The 32 rows of the warp: at each exchange a lane keeps half of its positions and gives away the others; then the four warps.
+      float v[32], x[8];
 #pragma unroll
-      for (int i = 0; i < 32; i++) unpair(v[2 * i], v[2 * i + 1], acc[i]);
-      exchange<16>(v, lane), exchange<8>(v, lane), exchange<4>(v, lane), exchange<2>(v, lane), exchange<1>(v, lane);
-      // lane l has positions 2 l and 2 l + 1
-      *(float2*)&h.sums[wg][warp & 3][2 * lane] = make_float2(v[0], v[1]);
+      for (int i = 0; i < 16; i++) unpair(v[2 * i], v[2 * i + 1], acc[i]);
+#pragma unroll
+      for (int i = 0; i < 4; i++) unpair(x[2 * i], x[2 * i + 1], acc[16 + i]);
+      exchange<16, 16>(v, lane), exchange<8, 8>(v, lane), exchange<4, 4>(v, lane), exchange<2, 2>(v, lane), exchange<1, 1>(v, lane);
+      exchange<16, 4>(x, lane), exchange<8, 2>(x, lane), exchange<4, 1>(x, lane);
+      x[0] += __shfl_xor_sync(~0u, x[0], 2);
+      x[0] += __shfl_xor_sync(~0u, x[0], 1);
+      float* sums = h.sums[wg][warp & 3];
+      sums[lane] = v[0];                               // lane l has position l
+      if (!(lane & 3)) sums[32 + (lane >> 2)] = x[0];
       named_barrier(1 + wg, 128);
       const bool whole = u.begin == 0 && u.end == u.all;
       const int id = threadIdx.x & 127;
-      if (id < 64) {
+      if (id < kEach) {
         const float sum = (h.sums[wg][0][id] + h.sums[wg][1][id]) + (h.sums[wg][2][id] + h.sums[wg][3][id]);
         if (whole) {
           weights_write(p, u.seq, u.head, u.len, base + id, sum);
         } else {
           const int rec = 2 * blockIdx.x + (u.begin == 0);
-          p.part[(int64_t)rec * kSpan + wg * 64 + id] = sum;
+          p.part[(int64_t)rec * kSpan + wg * kEach + id] = sum;
           if (id == 0 && wg == 0) p.part_of[rec] = make_int4(u.seq, u.head, u.at, u.end < u.all);
         }
       }
@@ -728,27 +697,26 @@ __global__ void __launch_bounds__(kManyThreads, 1)
     const bool leader = elect_one();
     constexpr unsigned kIdS = mma_idesc(kTile, kSpan, false, false);
     const uint64_t q_desc = smem_desc(smem_u32(smem), 16, 1024), k_desc = smem_desc(smem_u32(k_tiles), 16, 1024);
-    RingAt k, q;
-    unsigned j = 0;                                    // steps in front
+    RingAt k, q, s;                                    // s: the accumulator
     bool on = true;
     while (uniform(walk.next(p, u))) {
       on = attn_wait(&h.k_full[k.at], k.round, h) && on;
       const uint64_t ka = k_desc + uniform(k.at) * (uint64_t)(L::kBytesK >> 4);
       const int n = uniform(u.end - u.begin);
-      for (int i = 0; i < n; i++, j++) {
+      for (int i = 0; i < n; i++) {
         on = attn_wait(&h.q_full[q.at], q.round, h) && on;
         const uint64_t qa = q_desc + uniform(q.at) * (uint64_t)(L::kTileBytes >> 4);
-        const int at = uniform(j & 1);
-        on = attn_wait(&h.s_empty[at], (j >> 1 & 1) ^ 1, h) && on;
+        const int at = uniform(s.at);
+        on = attn_wait(&h.s_empty[at], s.round ^ 1, h) && on;
         if (on) {
           tc_fence_after();
 #pragma unroll
           for (int e = 0; e < HD / 16; e++)
-            mma_ss(leader, tmem + at * 256, qa + ((e / 4 * kBox + e % 4 * 32) >> 4), ka + ((e / 4 * L::kBoxK + e % 4 * 32) >> 4), kIdS, e > 0);
+            mma_ss(leader, tmem + at * kSpan, qa + ((e / 4 * kBox + e % 4 * 32) >> 4), ka + ((e / 4 * L::kBoxK + e % 4 * 32) >> 4), kIdS, e > 0);
           mma_commit(leader, &h.s_full[at]);
           mma_commit(leader, &h.q_empty[q.at]);
         }
-        q.next(p.q_stages);
+        q.next(p.q_stages), s.next(kManyBuffers);
       }
       if (on) mma_commit(leader, &h.k_empty[k.at]);
       k.next(p.k_stages);

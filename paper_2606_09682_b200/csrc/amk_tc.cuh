@@ -81,6 +81,11 @@ __device__ __forceinline__ void tmem_ld16(unsigned (&r)[16], unsigned addr) {
         "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
       : "r"(addr));
 }
+__device__ __forceinline__ void tmem_ld8(unsigned (&r)[8], unsigned addr) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(addr));
+}
 // 32 columns of 16 lanes, each eight by eight as a product's fragments lie: register 4 b + 2 h + e of lane l is column
 // 8 b + 2 (l % 4) + e of lane l / 4 + 8 h.
 __device__ __forceinline__ void tmem_ld_16x256b_x4(unsigned (&r)[16], unsigned addr) {
