@@ -349,7 +349,7 @@ __device__ __forceinline__ void add_columns(uint64_t (&acc)[2], const unsigned (
   }
 }
 
-constexpr int kFewGroups = 3, kWideners = 4;           // warpgroups for the exponentials, warps that widen 8-bit tiles
+constexpr int kFewGroups = 3, kWideners = 8;           // warpgroups for the exponentials, warps that widen 8-bit tiles
 template <bool FP8>
 constexpr int kFewThreads = 32 * (4 * kFewGroups + 2 + (FP8 ? kWideners : 0));
 

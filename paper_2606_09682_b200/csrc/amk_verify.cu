@@ -28,7 +28,7 @@ namespace {
 using namespace amk;
 
 constexpr int kThreads = 512, kWarps = kThreads / 32;    // the walk's
-constexpr int kStatThreads = 256, kStatWarps = kStatThreads / 32, kLoads = 8;   // the first kernel's: 32 KB of logits a block
+constexpr int kStatThreads = 256, kStatWarps = kStatThreads / 32, kLoads = 4;   // the first kernel's: 16 KB of logits a block
 constexpr float kLog2e = 1.4426950408889634f;
 // A row's sum in 32 bits: an exponent y = (x - m) log2 e / T is off by 2^-23 |y|, its power by 2^-23 |y| ln 2 of itself (less than
 // 2^-24 32 for the terms that count) and 2^-22, additions by less than 2^-19 together: 2^-17.
@@ -66,9 +66,9 @@ __device__ __forceinline__ float max_nan(float a, float b) {
 }
 
 // ---- the rows' maxima and sums ----------------------------------------------------------------------------------
-// A block has 32 KB of a row, counted from the 16-byte boundary at or in front of its first logit, and holds them in registers.
+// A block has 16 KB of a row, counted from the 16-byte boundary at or in front of its first logit, and holds them in registers.
 template <class T>
-__global__ void __launch_bounds__(kStatThreads) stats_kernel(const VerifyParams p) {
+__global__ void __launch_bounds__(kStatThreads, 8) stats_kernel(const VerifyParams p) {
   constexpr int kVec = 16 / sizeof(T), kPart = kStatThreads * kLoads * kVec;
   __shared__ float red[kStatWarps];
   __shared__ int red_i[kStatWarps];
@@ -271,7 +271,9 @@ __global__ void __launch_bounds__(kThreads, 1) walk_kernel(const VerifyParams p)
     if (greedy) {
       w.verdict[i] = w.token[i] == w.first[parent] && uq < 1.0 ? kAccept : kReject;
     } else {
-      const double e = exp(((double)w.x[i] - (double)w.m[parent]) * inv_t), s = (double)w.s[parent];
+      const double y = ((double)w.x[i] - (double)w.m[parent]) * inv_t, s = (double)w.s[parent];
+      double e = exp_below(y, w.roots);
+      if (e == 0.0) e = exp(y);
       w.e[i] = e;
       w.verdict[i] = fabs(uq * s - e) > kNear * e ? (uq * s < e ? kAccept : kReject) : kClose;
     }
