@@ -575,6 +575,234 @@ def test_streams_graphs_and_order(amk):
     assert all(torch.equal(a, b) for a, b in zip(replayed, again)) and not torch.equal(replayed[0], eager[0])
 
 
+@pytest.mark.parametrize("cache", ["bf16", "fp8"])
+@pytest.mark.parametrize("nq,nkv,hd,rows,slots,seqs", [(7, 1, 128, 2500, 3600, 2), (8, 2, 64, 3, 260, 40), (4, 1, 64, 90, 330, 40), (12, 4, 128, 43, 500, 70)])
+def test_attention_weights_long_and_many(amk, nq, nkv, hd, rows, slots, seqs, cache):
+    """Many tiles of queries, units cut between blocks; more sequences than a warp looks at once, some of impossible length."""
+    g = gen(rows + seqs)
+    q, k = randn(g, seqs, rows, nq, hd), randn(g, seqs, nkv, slots, hd)
+    k = code(k) if cache == "fp8" else k
+    rng = np.random.default_rng(rows)
+    lens = [int(x) for x in rng.integers(0, slots - rows + 1, seqs)]
+    if seqs > 2:
+        lens[1], lens[5], lens[-1] = -3, slots, 0
+    lse = true_lse(q, k, lens, hd ** -0.5)
+    want, tol = weights64(q, k, lse, lens, None, 1, hd ** -0.5)
+    got = amk.amk_attention_weights(q, k, lse, i32(lens))
+    weights_agree(got, want, tol)
+    assert torch.equal(torch.nan_to_num(got, 7.0), torch.nan_to_num(amk.amk_attention_weights(q, k, lse, i32(lens)), 7.0))
+
+
+@pytest.mark.parametrize("cache", ["bf16", "fp8"])
+@pytest.mark.parametrize("rows,tiles", [(3, 0), (3, 1), (200, 0), (200, 1)])
+def test_attention_weights_expired_wait(amk, rows, tiles, cache):
+    """Tiles that never come: the waits run out, the status says so once, and the next call is right."""
+    g = gen(1)
+    q, k, lens = randn(g, 2, rows, 8, 128), randn(g, 2, 1, 1500, 128), [1300, 900]
+    k = code(k) if cache == "fp8" else k
+    lse = true_lse(q, k, lens, 128 ** -0.5)
+    q, k, lse = (t.repeat(24, *[1] * (t.dim() - 1)) for t in (q, k, lse))     # several units for each block
+    lens = lens * 24
+    call = lambda: amk.amk_attention_weights(q, k, lse, i32(lens))
+    want = call()
+    assert amk.amk_operator_status() == amk.AMK_OK
+    amk.amk_debug_operator_wait(2_000_000, tiles)      # about a millisecond
+    try:
+        call()
+        assert amk.amk_operator_status() == amk.AMK_ERR_TIMEOUT
+        assert amk.amk_operator_status() == amk.AMK_OK
+    finally:
+        amk.amk_debug_operator_wait()
+    assert torch.equal(call(), want) and amk.amk_operator_status() == amk.AMK_OK
+
+
+def test_first_calls_of_a_process_may_be_captured():
+    """Everything that a call sets up once happens in the call itself, and capture allows it."""
+    code_ = """
+import torch
+from paper_2606_09682_b200 import binding as amk
+g = torch.Generator(device="cuda").manual_seed(1)
+r = lambda *s: torch.randn(*s, device="cuda", generator=g)
+x, pos = r(6, 8, 64).bfloat16(), torch.arange(6, device="cuda", dtype=torch.int32)
+kc, vc, n = r(1, 2, 700, 64).bfloat16(), r(1, 2, 700, 64).bfloat16(), torch.full((1,), 500, dtype=torch.int32, device="cuda")
+q2, lse2 = r(1, 150, 4, 64).bfloat16(), r(1, 150, 4) + 9
+lse, logits, tok, u = r(1, 6, 4) + 9, r(1, 6, 9000), torch.zeros(1, 6, dtype=torch.int32, device="cuda"), torch.rand(1, 6, device="cuda", generator=g)
+sc = r(2, 3, 40000).abs()
+two = torch.full((2,), 39999, dtype=torch.int32, device="cuda")
+def run():
+    q = amk.amk_norm_rope_append(x[:, :4], x[:, 4:6], x[:, 6:], pos, kc, vc, pos.long() + 500)
+    return [q, amk.amk_attention_weights(q[None], kc, lse, n), amk.amk_attention_weights(q2, kc, lse2, n), *amk.amk_evict_select(sc, two, 90, 2, 3),
+            *amk.amk_evict_select(sc[:, :, :30000], two - 10000, 20000), *amk.amk_verify_draft(logits, tok, u)]
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    a = run()
+graph.replay()
+assert all(torch.equal(b, c) for b, c in zip(a, run())) and amk.amk_operator_status() == 0
+print("fine")
+"""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code_], capture_output=True, text=True, timeout=300, cwd=root)
+    assert r.returncode == 0 and "fine" in r.stdout, r.stderr[-2000:]
+
+
+def test_scratch_of_two_graphs(amk):
+    """Two captured calls with a workspace each, replayed on two streams at once, again and again."""
+    g = gen(12)
+    q, k = randn(g, 2, 300, 8, 64), randn(g, 2, 2, 900, 64)
+    lens = [[500, 31], [0, 600]]
+    lse = [true_lse(q, k, n, 0.125) for n in lens]
+    logits, tokens, u, _, probs = draft_case(g, 3, 6, 20000, torch.float32, "probs", False)
+    want, graphs, streams, outs = [], [], [], []
+    for i in range(2):
+        n, uu = i32(lens[i]), u if i else (1 - u) * 0.999
+        want.append([amk.amk_attention_weights(q, k, lse[i], n), *amk.amk_verify_draft(logits, tokens, uu, draft=probs)])
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs.append([amk.amk_attention_weights(q, k, lse[i], n), *amk.amk_verify_draft(logits, tokens, uu, draft=probs)])
+        graphs.append((graph, n, uu))
+        streams.append(torch.cuda.Stream())
+    for _ in range(20):
+        for graph, stream in zip(graphs, streams):
+            with torch.cuda.stream(stream):
+                graph[0].replay()
+    torch.cuda.synchronize()
+    for a, b in zip(want, outs):
+        assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+# ---- with the decode step ---------------------------------------------------------------------------------------
+
+def layers(shape, w, tokens, attend):
+    """The model in plain fp32 torch around ``attend(layer, q, k, v)``: q, k, v bf16 [tokens][heads][hd], not rotated yet."""
+    f = lambda t: t.float()
+    norm = lambda x, g: x * torch.rsqrt((x * x).mean(-1, keepdim=True) + shape.rms_eps) * f(g)
+    x = f(w["embed"])[tokens.long()]
+    n = len(tokens)
+    for l in range(shape.n_layers):
+        h = norm(x, w["attn_norm"][l])
+        q, k, v = ((h @ f(w[m][l]).t()).view(n, -1, shape.head_dim).to(torch.bfloat16) for m in ("wq", "wk", "wv"))
+        x = x + attend(l, q, k, v).float().reshape(n, -1) @ f(w["wo"][l]).t()
+        h = norm(x, w["mlp_norm"][l])
+        x = x + (torch.nn.functional.silu(h @ f(w["wgate"][l]).t()) * (h @ f(w["wup"][l]).t())) @ f(w["wdown"][l]).t()
+    return norm(x, w["final_norm"]) @ f(w["embed"] if shape.tied else w["lm_head"]).t()
+
+
+@pytest.mark.parametrize("name,kv_dtype", [("mini", "bf16"), ("mini_hd128", "bf16"), ("mini_ragged", "bf16"), ("mini", "fp8")])
+def test_prompt_draft_verify_evict_and_decode(amk, name, kv_dtype):
+    """A prompt rotated and stored in a decoder's cache, a draft chain verified over it, the accepted tokens kept and the decode step
+    going on; then the positions with the least attention weight leave, and the tree attention goes on over what stays.
+    4e-2 for logits: q, k and v rounded to bf16 before the rotation and after it, the attention's output once (2^-8 each),
+    through the layers; 4.4e-2 more for the 8-bit cache, whose entries may fall on the other side of a border (a step of 2^-3
+    for 2^-3 of them)."""
+    shape = inp.SHAPES[name]
+    w = inp.make_weights(shape, 99, device=DEV, std=0.05, norm_jitter=0.1)
+    dec = amk.Decoder(shape, w, "bf16", kv_dtype=kv_dtype)
+    nkv, hd = shape.n_kv_heads, shape.head_dim
+    n, n_new = 37, 9
+    prompt = torch.randint(0, shape.vocab, (n,), generator=gen(3), device=DEV)
+    kv_ref, toks, logits_ref = dec.new_cache(), prompt.tolist(), []
+    for pos in range(n + n_new):
+        dec.amk_decode_step(toks[pos], pos, kv_ref)
+        assert dec.amk_last_status()[0] == 0
+        logits_ref.append(dec.logits.clone())
+        if pos + 1 >= len(toks):
+            toks.append(int(dec.next_token))
+    kv = dec.new_cache()
+    K, V = dec.cache_views(kv)
+    bf16 = lambda t: t.contiguous().view(torch.float8_e4m3fn).to(torch.bfloat16) if t.dtype == torch.uint8 else t
+    near = lambda a, b: float((a - b).norm() / b.norm())
+    tol = 4e-2 + (4.4e-2 if kv_dtype == "fp8" else 0.0)
+
+    # the prompt
+    at = torch.arange(n, device=DEV)
+    cu = i32([0, n])
+    sums = torch.zeros(shape.n_layers, nkv, shape.max_seq, device=DEV)       # attention weights of every layer's positions
+
+    def prompt_layer(l, q, k, v):
+        q = amk.amk_norm_rope_append(q, k, v, at.to(torch.int32), K[l][None], V[l][None], at, theta=shape.rope_theta)
+        lse = torch.empty(n, shape.n_q_heads, device=DEV)
+        out = amk.amk_prompt_attention(q, bf16(K[l])[:, :n].transpose(0, 1), bf16(V[l])[:, :n].transpose(0, 1), cu, lse=lse)
+        amk.amk_attention_weights(q[None], K[l][None], lse[None], i32([0]), out=sums[l][None])
+        return out
+
+    logits = layers(shape, w, prompt, prompt_layer)
+    assert near(logits[-1], logits_ref[n - 1]) < tol
+    assert bool(((sums.sum(2) / (n * shape.n_q_heads / nkv) - 1).abs() < 1e-3).all())
+
+    # a chain: the token that the prompt ends in (true[0] is already chosen), three true ones and a wrong one
+    true = toks[n:n + n_new]
+    draft = true[:4] + [(true[4] + 1) % shape.vocab, true[5]]
+    rows, length = len(draft), i32([n])
+    where = n + torch.arange(rows, device=DEV)
+
+    def draft_layer(l, q, k, v):
+        q = amk.amk_norm_rope_append(q, k, v, where.to(torch.int32), K[l][None], V[l][None], where, theta=shape.rope_theta)
+        lse = torch.empty(1, rows, shape.n_q_heads, device=DEV)
+        out = amk.amk_tree_attention(q[None], K[l][None], V[l][None], length, lse=lse)[0]
+        drafted.append((q, lse))
+        return out
+
+    drafted = []
+    logits = layers(shape, w, torch.tensor(draft, device=DEV), draft_layer)
+    for i in range(4):
+        assert near(logits[i], logits_ref[n + i]) < tol, i
+    count, keep, token = amk.amk_verify_draft(logits[None].contiguous(), i32([draft]), torch.rand(1, rows, device=DEV), cache_len=length,
+                                              temperature=torch.zeros(1, device=DEV))
+    best = logits.argmax(1).tolist()
+    kept = 1
+    while kept < rows and draft[kept] == best[kept - 1]:
+        kept += 1
+    assert count.tolist() == [kept] and keep.tolist() == [[n + i if i < kept else -1 for i in range(rows)]] and token.tolist() == [best[kept - 1]]
+    assert kept == 4                                     # (what the decode step itself chose)
+    # the accepted tokens' weights count, the others' are left out
+    for l, (q, lse) in enumerate(drafted):
+        lse[0, kept:] = -math.inf
+        amk.amk_attention_weights(q[None], K[l][None], lse, length, sums[l][None], out=sums[l][None])
+    total = n * shape.n_q_heads / nkv + kept * shape.n_q_heads / nkv
+    assert bool(((sums.sum(2) / total - 1).abs() < 1e-3).all())
+    dec.amk_kv_compact(kv, length, keep, count)
+    for pos in range(n + kept, n + n_new):
+        dec.amk_decode_step(toks[pos], pos, kv)
+        assert near(dec.logits, logits_ref[pos]) < tol, pos
+
+    # a budget for every layer and head; the rows behind the kept ones are free again
+    have, budget = n + kept, 20
+    before = (bf16(K).double(), bf16(V).double())
+    lens = i32([have] * shape.n_layers)
+    keep, count, moved = amk.amk_evict_select(sums, lens, budget, 2, 5)
+    assert count.unique().tolist() == [budget]
+    lists, counts = keep.view(-1, budget), count.view(-1)
+    for half in (K, V):
+        amk.amk_kv_compact(half.view(shape.n_layers * nkv, 1, shape.max_seq, hd), torch.zeros_like(counts), lists, counts)
+    assert torch.equal(moved[:, :, :budget], torch.gather(sums, 2, keep.long()))
+    old = [torch.gather(b, 2, keep.long()[..., None].expand(-1, -1, -1, hd)) for b in before]
+    for half, want in zip((K, V), old):
+        assert torch.equal(bf16(half[:, :, :budget]).double(), want)
+    new = torch.tensor([have], device=DEV)
+    slot = i32([budget])
+
+    def tree(l, q, k, v):
+        q = amk.amk_norm_rope_append(q, k, v, new.to(torch.int32), K[l][None], V[l][None], torch.full((1,), budget, device=DEV), theta=shape.rope_theta)
+        return amk.amk_tree_attention(q[None], K[l][None], V[l][None], slot)[0]
+
+    def plain(l, q, k, v):
+        qr, kr = rotated64(q, None, new, shape.rope_theta, 0)[0], rotated64(k, None, new, shape.rope_theta, 0)[0]
+        rep = shape.n_q_heads // nkv
+        keys, values = (torch.cat([o[l], t.double().transpose(0, 1)], 1).repeat_interleave(rep, 0) for o, t in zip(old, (kr, v)))
+        x = qr.permute(1, 0, 2) @ keys.transpose(1, 2) * hd ** -0.5
+        return (torch.softmax(x, 2) @ values).permute(1, 0, 2).to(torch.bfloat16)
+
+    token = torch.tensor([toks[have]], device=DEV)
+    got, want = layers(shape, w, token, tree), layers(shape, w, token, plain)
+    assert near(got, want) < (2e-2 if kv_dtype == "bf16" else 6.4e-2)
+    dec.close()
+
+
 def test_refused(amk):
     """What the Python layer and the library refuse, with the reason; a CPU tensor among CUDA ones too."""
     x, pos = torch.zeros(4, 8, 64, dtype=torch.bfloat16, device=DEV), i32([0, 1, 2, 3])
