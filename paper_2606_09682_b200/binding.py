@@ -326,14 +326,6 @@ def _scale(name: str, scale: Optional[float]) -> float:
     return held
 
 
-def _f32(name: str, what: str, x: float) -> float:
-    """x as the struct's fp32 holds it; what fp32 cannot hold is refused (NaN is the library's to refuse)."""
-    try:
-        return _F32.unpack(_F32.pack(x))[0]
-    except OverflowError:
-        _refuse(name, f"{what} {x} must be finite in fp32")
-
-
 def _device_of(name: str, first: torch.Tensor, *others) -> int:
     """Index of the cuda device that all the tensors (or None) live on.  The operators have no backward pass: a tensor for which
     autograd would record the call is refused."""
@@ -556,8 +548,18 @@ def amk_kv_compact(kv: torch.Tensor, base: torch.Tensor, keep: torch.Tensor, cou
          elements * esz, base.data_ptr(), keep.data_ptr(), keep.shape[1], count.data_ptr())
 
 
-_CACHE_TYPES = (torch.bfloat16, torch.uint8, torch.float8_e4m3fn)
-_NO_CACHE = (0,) * 6
+_BF16, _F32T, _I32, _I64 = torch.bfloat16, torch.float32, torch.int32, torch.int64
+_CACHE_KIND = {torch.bfloat16: AMK_KV_BF16, torch.uint8: AMK_KV_FP8_E4M3, torch.float8_e4m3fn: AMK_KV_FP8_E4M3}
+_NO_CACHE = (0, 0, 0, 0, 0, 0)
+
+
+def _whole(name: str, index: int, what: str, t: torch.Tensor, dtype, shape) -> int:
+    """Address of a contiguous tensor of integers (or of numbers that have no gradient) on device ``index``; refused otherwise."""
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        _refuse(name, f"{what} is contiguous {dtype} of shape {tuple(shape)}")
+    if t.get_device() != index:
+        _refuse(name, "tensors on different devices")
+    return t.data_ptr()
 
 
 def amk_norm_rope_append(q: torch.Tensor, k: torch.Tensor, v: Optional[torch.Tensor], positions: torch.Tensor,
@@ -571,59 +573,61 @@ def amk_norm_rope_append(q: torch.Tensor, k: torch.Tensor, v: Optional[torch.Ten
     not stored).  Returns the rotated queries, ``q_out`` if given (q itself may be); the rotated keys are also left in ``k_out``
     if given.  Without caches v may be None."""
     name = "amk_norm_rope_append"
-    if q.dim() != 3 or k.dim() != 3 or (v is not None and v.dim() != 3):
+    shape, kshape = q.shape, k.shape
+    if len(shape) != 3 or len(kshape) != 3 or (v is not None and v.dim() != 3):
         _refuse(name, "q, k and v are [rows][heads][head_dim]")
-    rows, nq, hd = shape = q.shape
-    kshape = k.shape
-    nkv = kshape[1]
-    dev = _device_of(name, q, k, v, positions, k_cache, v_cache, slots, q_weight, k_weight, q_out, k_out)
-    bf16 = torch.bfloat16
-    if q.dtype is not bf16 or k.dtype is not bf16 or (v is not None and v.dtype is not bf16):
+    rows, nq, hd = shape
+    krows, nkv, khd = kshape
+    dev = _device_of(name, q, k, v, k_cache, v_cache, q_weight, k_weight, q_out, k_out)
+    if q.dtype is not _BF16 or k.dtype is not _BF16 or (v is not None and v.dtype is not _BF16):
         _refuse(name, "q, k and v are bf16")
-    if kshape[0] != rows or kshape[2] != hd or (v is not None and v.shape != kshape):
+    if krows != rows or khd != hd or (v is not None and v.shape != kshape):
         _refuse(name, "shapes of q, k and v do not fit")
-    if positions.dtype is not torch.int32 or positions.shape != (rows,) or not positions.is_contiguous():
-        _refuse(name, "positions is a contiguous int32 vector with an entry for each row")
-    for w in (q_weight, k_weight):
-        if w is not None and (w.dtype is not bf16 or w.shape != (hd,) or not w.is_contiguous()):
-            _refuse(name, "weights are contiguous bf16 vectors of head_dim")
+    at = _whole(name, dev, "positions", positions, _I32, (rows,))
+    wq = wk = 0
+    if q_weight is not None:
+        wq = _whole(name, dev, "q_weight", q_weight, _BF16, (hd,))
+    if k_weight is not None:
+        wk = _whole(name, dev, "k_weight", k_weight, _BF16, (hd,))
     if q_out is None:
         q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
-    elif q_out.shape != shape or q_out.dtype is not bf16:
+    elif q_out.shape != shape or q_out.dtype is not _BF16:
         _refuse(name, "q_out is bf16 of q's shape")
-    if k_out is not None and (k_out.shape != kshape or k_out.dtype is not bf16):
-        _refuse(name, "k_out is bf16 of k's shape")
     (qr, qh, q1), (kr, kh, k1), (outr, outh, out1) = q.stride(), k.stride(), q_out.stride()
-    vr = vh = kor = koh = 0
+    vp = vr = vh = kop = kor = koh = 0
     v1 = ko1 = 1
     if v is not None:
         vr, vh, v1 = v.stride()
+        vp = v.data_ptr()
     if k_out is not None:
+        if k_out.shape != kshape or k_out.dtype is not _BF16:
+            _refuse(name, "k_out is bf16 of k's shape")
         kor, koh, ko1 = k_out.stride()
-    seqs, n_slots, kind, caches, where = 0, 0, AMK_KV_BF16, _NO_CACHE, 0
+        kop = k_out.data_ptr()
+    seqs = n_slots = kind = where = kcp = vcp = 0
+    caches = _NO_CACHE
     if k_cache is not None or v_cache is not None:
         if k_cache is None or v_cache is None or v is None or slots is None:
             _refuse(name, "k_cache and v_cache come together, with v and slots")
-        if k_cache.dim() != 4 or k_cache.shape != v_cache.shape or k_cache.shape[1] != nkv or k_cache.shape[3] != hd:
+        cshape, ctype = k_cache.shape, k_cache.dtype
+        if len(cshape) != 4 or cshape != v_cache.shape or cshape[1] != nkv or cshape[3] != hd:
             _refuse(name, "the caches are [n_seqs][n_kv][n_slots][head_dim]")
-        if k_cache.dtype is not v_cache.dtype or k_cache.dtype not in _CACHE_TYPES:
+        kind = _CACHE_KIND.get(ctype)
+        if kind is None or v_cache.dtype is not ctype:
             _refuse(name, "the caches are bf16, or e4m3 as uint8 or float8_e4m3fn")
-        if slots.dtype is not torch.int64 or slots.shape != (rows,) or not slots.is_contiguous():
-            _refuse(name, "slots is a contiguous int64 vector with an entry for each row")
-        seqs, n_slots = k_cache.shape[0], k_cache.shape[2]
-        kind = AMK_KV_BF16 if k_cache.dtype is bf16 else AMK_KV_FP8_E4M3
+        where = _whole(name, dev, "slots", slots, _I64, (rows,))
+        seqs, _, n_slots, _ = cshape
         (cs, ch, cr, c1), (ds, dh, dr, d1) = k_cache.stride(), v_cache.stride()
         if c1 != 1 or d1 != 1:
             _refuse(name, "the last dimension must be contiguous")
-        caches, where = (cs, ch, cr, ds, dh, dr), slots.data_ptr()
+        caches, kcp, vcp = (cs, ch, cr, ds, dh, dr), k_cache.data_ptr(), v_cache.data_ptr()
     if not (q1 == k1 == v1 == out1 == ko1 == 1):
         _refuse(name, "the last dimension must be contiguous")
-    args = _ROPE.pack(_ROPE.size, hd, nq, nkv, kind, seqs, n_slots, _f32(name, "eps", eps), _f32(name, "theta", theta), 0, rows,
-                      q.data_ptr(), k.data_ptr(), 0 if v is None else v.data_ptr(),
-                      0 if q_weight is None else q_weight.data_ptr(), 0 if k_weight is None else k_weight.data_ptr(),
-                      positions.data_ptr(), where, q_out.data_ptr(), 0 if k_out is None else k_out.data_ptr(),
-                      0 if k_cache is None else k_cache.data_ptr(), 0 if v_cache is None else v_cache.data_ptr(),
-                      qr, qh, kr, kh, vr, vh, outr, outh, kor, koh, *caches)
+    try:
+        args = _ROPE.pack(_ROPE.size, hd, nq, nkv, kind, seqs, n_slots, eps, theta, 0, rows, q.data_ptr(), k.data_ptr(), vp, wq, wk, at,
+                          where, q_out.data_ptr(), kop, kcp, vcp, qr, qh, kr, kh, vr, vh, outr, outh, kor, koh, *caches)
+    except OverflowError:
+        _refuse(name, f"eps {eps} and theta {theta} must be finite in fp32")
     _run(lib.amk_norm_rope_append, name, dev, args)
     return q_out
 
@@ -632,24 +636,26 @@ _scratch_bytes: Dict = {}                             # of the weights and the v
 
 
 def _scratch(name: str, fn, dev: int, like: torch.Tensor, given: Optional[torch.Tensor], key, packed):
-    """(workspace or None, its bytes) of a call; ``packed()`` gives the struct that the library is asked with."""
+    """(workspace or None, its address and bytes) of a call; ``packed(*key)`` gives the struct that the library is asked with."""
     if given is not None:
         if not given.is_contiguous():
             _refuse(name, "the workspace must be contiguous")
-        return given, given.numel() * given.element_size()
-    key = (name, dev, key)
-    need = _scratch_bytes.get(key)
+        return given, given.data_ptr(), given.numel() * given.element_size()
+    need = _scratch_bytes.get((dev, key))
     if need is None:
         n = C.c_size_t()
         msg = C.create_string_buffer(256)
         with torch.cuda.device(dev):
-            code = fn(packed(), C.byref(n), msg, 256)
+            code = fn(packed(*key), C.byref(n), msg, 256)
         if code != AMK_OK:
             raise AmkError(code, msg.value.decode() or name)
         if len(_scratch_bytes) >= 4096:
             _scratch_bytes.clear()
-        need = _scratch_bytes[key] = n.value
-    return (torch.empty(need, dtype=torch.uint8, device=like.device) if need else None), need
+        need = _scratch_bytes[dev, key] = n.value
+    if not need:
+        return None, 0, 0
+    space = torch.empty(need, dtype=torch.uint8, device=like.device)
+    return space, space.data_ptr(), need
 
 
 def amk_attention_weights(q: torch.Tensor, k: torch.Tensor, lse: torch.Tensor, cache_len: torch.Tensor,
@@ -661,42 +667,44 @@ def amk_attention_weights(q: torch.Tensor, k: torch.Tensor, lse: torch.Tensor, c
     leave it, -infinity for a token to be left out.  ``before``, weighed by ``decay``, is added for slots below cache_len; ``out`` may
     be ``before`` itself."""
     name = "amk_attention_weights"
-    if q.dim() != 4 or k.dim() != 4:
+    qshape, kshape = q.shape, k.shape
+    if len(qshape) != 4 or len(kshape) != 4:
         _refuse(name, "q and k have four dimensions")
-    seqs, rows, nq, hd = q.shape
-    kseqs, nkv, slots, khd = k.shape
-    dev = _device_of(name, q, k, lse, cache_len, before, out, workspace)
-    if q.dtype is not torch.bfloat16:
+    seqs, rows, nq, hd = qshape
+    kseqs, nkv, slots, khd = kshape
+    dev = _device_of(name, q, k, lse, before, out, workspace)
+    if q.dtype is not _BF16:
         _refuse(name, "q is bf16")
-    if k.dtype not in _CACHE_TYPES:
+    kind = _CACHE_KIND.get(k.dtype)
+    if kind is None:
         _refuse(name, "the cache is bf16, or e4m3 as uint8 or float8_e4m3fn")
     if kseqs != seqs or khd != hd:
         _refuse(name, "shapes of q and k do not fit")
-    if lse.dtype is not torch.float32 or lse.shape != (seqs, rows, nq) or not lse.is_contiguous():
-        _refuse(name, "lse is contiguous fp32 [n_seqs][rows][n_q]")
-    if cache_len.dtype is not torch.int32 or cache_len.shape != (seqs,) or not cache_len.is_contiguous():
-        _refuse(name, "cache_len is a contiguous int32 vector with an entry for each sequence")
+    lp = _whole(name, dev, "lse", lse, _F32T, (seqs, rows, nq))
+    np_ = _whole(name, dev, "cache_len", cache_len, _I32, (seqs,))
     shape = (seqs, nkv, slots)
     if out is None:
-        out = torch.empty(shape, dtype=torch.float32, device=q.device)
-    elif out.shape != shape or out.dtype is not torch.float32:
+        out = torch.empty(seqs, nkv, slots, dtype=_F32T, device=q.device)
+    elif out.shape != shape or out.dtype is not _F32T:
         _refuse(name, "out is fp32 [n_seqs][n_kv][slots]")
-    bs = bh = 0
+    bp = bs = bh = 0
     b1 = 1
     if before is not None:
-        if before.shape != shape or before.dtype is not torch.float32:
+        if before.shape != shape or before.dtype is not _F32T:
             _refuse(name, "before is fp32 [n_seqs][n_kv][slots]")
         bs, bh, b1 = before.stride()
+        bp = before.data_ptr()
     (qs, qr, qh, q1), (ks, kh, kr, k1), (os_, oh, o1) = q.stride(), k.stride(), out.stride()
     if not (q1 == k1 == 1) or (slots > 1 and not (o1 == b1 == 1)):
         _refuse(name, "the last dimension must be contiguous")
-    plan = (_WEIGHTS.size, hd, nq, nkv, AMK_KV_BF16 if k.dtype is torch.bfloat16 else AMK_KV_FP8_E4M3, seqs, rows, slots,
-            _scale(name, scale), _f32(name, "decay", decay))
-    workspace, have = _scratch(name, lib.amk_attention_weights_workspace_bytes, dev, q, workspace, plan,
-                               lambda: _WEIGHTS.pack(*plan, *(0,) * 18))
-    args = _WEIGHTS.pack(*plan, q.data_ptr(), k.data_ptr(), lse.data_ptr(), cache_len.data_ptr(),
-                         0 if before is None else before.data_ptr(), out.data_ptr(),
-                         0 if workspace is None else workspace.data_ptr(), have, qs, qr, qh, ks, kh, kr, bs, bh, os_, oh)
+    plan = (_WEIGHTS.size, hd, nq, nkv, kind, seqs, rows, slots)
+    workspace, space, have = _scratch(name, lib.amk_attention_weights_workspace_bytes, dev, q, workspace, plan,
+                                      lambda *plan: _WEIGHTS.pack(*plan, *(0,) * 20))
+    try:
+        args = _WEIGHTS.pack(*plan, _scale(name, scale), decay, q.data_ptr(), k.data_ptr(), lp, np_, bp, out.data_ptr(), space, have,
+                             qs, qr, qh, ks, kh, kr, bs, bh, os_, oh)
+    except OverflowError:
+        _refuse(name, f"decay {decay} must be finite in fp32")
     _run(lib.amk_attention_weights, name, dev, args)
     return out
 
@@ -709,27 +717,29 @@ def amk_evict_select(scores: torch.Tensor, lens: torch.Tensor, budget: int, firs
     shape, 0 behind: ``moved`` if given, which may be scores itself).  Lists for ``amk_kv_compact`` with base 0: a cache's K
     [n_seqs][n_heads][n_slots][hd] as n_seqs * n_heads caches of one plane, and its V likewise."""
     name = "amk_evict_select"
-    if scores.dim() != 3:
+    shape = scores.shape
+    if len(shape) != 3:
         _refuse(name, "scores are [n_seqs][n_heads][n_slots]")
-    seqs, heads, slots = shape = scores.shape
-    dev = _device_of(name, scores, lens, moved)
-    if scores.dtype is not torch.float32:
+    seqs, heads, slots = shape
+    dev = _device_of(name, scores, moved)
+    if scores.dtype is not _F32T:
         _refuse(name, "scores are fp32")
-    if lens.dtype is not torch.int32 or lens.shape != (seqs,) or not lens.is_contiguous():
-        _refuse(name, "lens is a contiguous int32 vector with an entry for each sequence")
+    lp = _whole(name, dev, "lens", lens, _I32, (seqs,))
     if not 1 <= budget <= slots:
         _refuse(name, f"budget {budget}: 1 to the slots")
+    ss, sh, s1 = scores.stride()
     if moved is None:
-        moved = torch.empty(shape, dtype=torch.float32, device=scores.device)
-    elif moved.shape != shape or moved.dtype is not torch.float32:
+        moved = torch.empty_like(scores, memory_format=torch.contiguous_format)
+    elif moved.shape != shape or moved.dtype is not _F32T:
         _refuse(name, "moved is fp32 of scores' shape")
-    (ss, sh, s1), (ms, mh, m1) = scores.stride(), moved.stride()
+    ms, mh, m1 = moved.stride()
     if slots > 1 and not (s1 == m1 == 1):
         _refuse(name, "the last dimension must be contiguous")
-    keep = torch.empty(seqs, heads, budget, dtype=torch.int32, device=scores.device)
-    count = torch.empty(seqs, heads, dtype=torch.int32, device=scores.device)
-    _run(lib.amk_evict_select, name, dev, scores.data_ptr(), seqs, heads, slots, ss, sh, lens.data_ptr(), budget, first, recent,
-         keep.data_ptr(), count.data_ptr(), moved.data_ptr(), ms, mh)
+    where = scores.device
+    keep = torch.empty(seqs, heads, budget, dtype=_I32, device=where)
+    count = torch.empty(seqs, heads, dtype=_I32, device=where)
+    _run(lib.amk_evict_select, name, dev, scores.data_ptr(), seqs, heads, slots, ss, sh, lp, budget, first, recent, keep.data_ptr(),
+         count.data_ptr(), moved.data_ptr(), ms, mh)
     return keep, count, moved
 
 
@@ -745,36 +755,35 @@ def amk_verify_draft(logits: torch.Tensor, tokens: torch.Tensor, uniforms: torch
     [n_seqs][rows]: cache_len + kept nodes, -1 behind them, token int32 [n_seqs], -1 where there is none): count and keep for
     ``amk_kv_compact`` with base = cache_len."""
     name = "amk_verify_draft"
-    if logits.dim() != 3:
+    shape = logits.shape
+    if len(shape) != 3:
         _refuse(name, "logits are [n_seqs][rows][vocab]")
-    seqs, rows, vocab = shape = logits.shape
-    dev = _device_of(name, logits, tokens, uniforms, parents, draft, temperature, cache_len, workspace)
-    if logits.dtype is not torch.float32 and logits.dtype is not torch.bfloat16:
+    seqs, rows, vocab = shape
+    dev = _device_of(name, logits, uniforms, draft, temperature, workspace)
+    kind = logits.dtype
+    if kind is not _F32T and kind is not _BF16:
         _refuse(name, "logits are fp32 or bf16")
-    for what, t, dtype, size in (("tokens", tokens, torch.int32, (seqs, rows)), ("uniforms", uniforms, torch.float32, (seqs, rows)),
-                                 ("parents", parents, torch.int32, (seqs, rows)),
-                                 ("temperature", temperature, torch.float32, (seqs,)),
-                                 ("cache_len", cache_len, torch.int32, (seqs,))):
-        if t is not None and (t.dtype is not dtype or t.shape != size or not t.is_contiguous()):
-            _refuse(name, f"{what} is contiguous {dtype} of shape {tuple(size)}")
+    nodes, each = (seqs, rows), (seqs,)
+    tp, up = _whole(name, dev, "tokens", tokens, _I32, nodes), _whole(name, dev, "uniforms", uniforms, _F32T, nodes)
+    pp = 0 if parents is None else _whole(name, dev, "parents", parents, _I32, nodes)
+    hp = 0 if temperature is None else _whole(name, dev, "temperature", temperature, _F32T, each)
+    np_ = 0 if cache_len is None else _whole(name, dev, "cache_len", cache_len, _I32, each)
     ls, lr, l1 = logits.stride()
-    ds = dr = 0
+    dp = ds = dr = 0
     d1 = 1
     if draft is not None:
-        if draft.shape != shape or draft.dtype is not torch.float32:
+        if draft.shape != shape or draft.dtype is not _F32T:
             _refuse(name, "draft is fp32 of the logits' shape")
         ds, dr, d1 = draft.stride()
+        dp = draft.data_ptr()
     if vocab > 1 and not (l1 == d1 == 1):
         _refuse(name, "the last dimension must be contiguous")
-    plan = (_VERIFY.size, 1 if logits.dtype is torch.bfloat16 else 0, seqs, rows, vocab)
-    workspace, have = _scratch(name, lib.amk_verify_workspace_bytes, dev, logits, workspace, plan,
-                               lambda: _VERIFY.pack(*plan, *(0,) * 16))
-    count = torch.empty(seqs, dtype=torch.int32, device=logits.device)
-    keep = torch.empty(seqs, rows, dtype=torch.int32, device=logits.device)
-    token = torch.empty_like(count)
-    ptr = lambda t: 0 if t is None else t.data_ptr()
-    args = _VERIFY.pack(*plan, logits.data_ptr(), ptr(draft), tokens.data_ptr(), ptr(parents), uniforms.data_ptr(),
-                        ptr(temperature), ptr(cache_len), count.data_ptr(), keep.data_ptr(), token.data_ptr(), ptr(workspace),
+    plan = (_VERIFY.size, 1 if kind is _BF16 else 0, seqs, rows, vocab)
+    workspace, space, have = _scratch(name, lib.amk_verify_workspace_bytes, dev, logits, workspace, plan,
+                                      lambda *plan: _VERIFY.pack(*plan, *(0,) * 16))
+    count = torch.empty(seqs, dtype=_I32, device=logits.device)
+    token, keep = torch.empty_like(count), torch.empty_like(tokens)
+    args = _VERIFY.pack(*plan, logits.data_ptr(), dp, tp, pp, up, hp, np_, count.data_ptr(), keep.data_ptr(), token.data_ptr(), space,
                         have, ls, lr, ds, dr)
     _run(lib.amk_verify_draft, name, dev, args)
     return count, keep, token
