@@ -431,7 +431,7 @@ amk_status amk_tree_workspace_bytes(const amk_tree_args* args, size_t* bytes, ch
 amk_status amk_tree_attention(const amk_tree_args* args, char* msg, size_t msg_bytes, void* cuda_stream);
 
 /*
- * The attention kernels bound every wait inside them (two seconds).  Synchronises the stream and reports in *st (HOST
+ * The attention kernels (amk_attention_weights' too) bound every wait inside them (two seconds).  Synchronises the stream and reports in *st (HOST
  * out) whether one ran out on the current device since this was last asked: AMK_OK, or AMK_ERR_TIMEOUT (the outputs
  * of the calls since then are undefined; the next call is legal).
  */

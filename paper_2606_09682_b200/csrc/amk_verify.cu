@@ -11,8 +11,9 @@
 // a child is rejected or a token drawn is read again (from L2), in 64 bits throughout: the border between two tokens of a
 // vocabulary of 10^5 lies within the error of 32 bits in one draw of a hundred.
 //
-// Bound: HBM in the first kernel (each row once); in the second latency, one pass over a row for each state that is needed, two or
-// three microseconds each.
+// Bound: HBM in the first kernel (each row once: 24.6 MB in about 8 us); in the second latency, about 8 us and one pass over a row for
+// each state that is needed, two or three microseconds each.  (8 sequences of 6 rows of 128256, drafted probabilities: 26.5 us;
+// 6 of 26 rows, 16 bits: 30 us.  With verdicts, states and sums made anew at each step and clusters of 8: 34 and 69 us.)
 #include <cuda_runtime.h>
 #include <math_constants.h>
 
