@@ -507,11 +507,12 @@ __global__ void __launch_bounds__(kFewThreads<FP8>, 1)
     }
   } else if (FP8) {
     // ================================ 8-bit tiles widened to bf16 ======================================================
+    const int first = (warp - kIssuer - 1) % kWideners * 32 + lane;      // (below 256, which the compiler sees: a whole number of chunks)
     RingAt raw, k;
     while (walk.next(p, u)) {
       attn_wait(&h.raw_full[raw.at], raw.round, h);
       attn_wait(&h.k_empty[k.at], k.round ^ 1, h);
-      widen_tile<HD, kTile, 4>(k_tiles + k.at * L::kTileBytes, raw_tiles + raw.at * L::kRawBytes, (warp - kIssuer - 1) * 32 + lane, 32 * kWideners);
+      widen_tile<HD, kTile, 4>(k_tiles + k.at * L::kTileBytes, raw_tiles + raw.at * L::kRawBytes, first, 32 * kWideners);
       fence_async_smem();
       warp_arrive(&h.k_full[k.at], lane);
       warp_arrive(&h.raw_empty[raw.at], lane);

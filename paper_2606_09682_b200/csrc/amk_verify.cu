@@ -7,7 +7,8 @@
 //
 // Which rows the walk reaches is known only as it goes, and each needs its S_0.  So a first kernel takes the maximum and the sum of
 // every row in 32 bits, all rows at once at the memory's rate, and a second one, a cluster of blocks for each sequence, walks
-// on those numbers alone: a decision nearer than their error (kNear) is taken again with the sum in 64 bits.  Only a row where
+// on those numbers alone (a cluster that takes its rows' sums itself, in one launch: one sequence of 6 rows of 128256 15.3 us, so
+// 11.9; eight of them 28.8 and 22.5): a decision nearer than their error (kNear) is taken again with the sum in 64 bits.  Only a row where
 // a child is rejected or a token drawn is read again (from L2), in 64 bits throughout: the border between two tokens of a
 // vocabulary of 10^5 lies within the error of 32 bits in one draw of a hundred.
 //
