@@ -6,7 +6,7 @@
 // Few rows (128 or less for a kv head: a decoded token, a draft, the last tokens of a prompt): every K tile of 128 positions meets
 // one tile of queries, and what counts is K's way from HBM.  weights_few_kernel takes S^T = K Q^T: a position is a lane of TMEM.
 // (32 tokens, 32 heads of 128 on 8, four caches of 4097 to 8001 positions: 51 MB in 15.6 us, of which about 8 are a cold block's
-// first tile and last output: the tiles come at HBM's rate.  13 tokens over eight 8-bit caches: 45 MB in 25.2 us, the tiles'
+// first tile and last output: the tiles come at HBM's rate.  13 tokens over eight 8-bit caches: 45 MB in 22.7 us, the tiles'
 // widening.)
 //
 // Many rows: what counts are the exponentials, 16 a cycle and SM, twice as long as the products.  weights_many_kernel takes
