@@ -2,8 +2,8 @@
 //
 // Mathematics.  A lane holds eight elements i .. i+7 of a head and the eight i + hd/2 .. that they are rotated with, so that
 // only the norm's sum crosses lanes.  The angle of pair i at position n is n theta^(-2i/hd); in turns, n f_i with
-// f_i = theta^(-2i/hd) / 2 pi, it is made in 64 bits, its whole turns taken off, and only then rounded to fp32: off by 2^-25 of
-// a turn at most, at any position.  The eight angles of a lane are those of every head of its token.
+// f_i = theta^(-2i/hd) / 2 pi, it is made in 64 bits, its whole turns taken off, and only then rounded to fp32: off by 2^-24 of
+// a turn at most, at any position (theta >= 1).  The eight angles of a lane are those of every head of its token.
 //
 // Bound: HBM, each element once in and once out.  A warp takes the heads of one token, or, with few tokens, a share of them, and
 // goes on to further tokens.  Heads come by asynchronous copies, seven steps ahead, into places of shared memory that each lane
@@ -214,7 +214,20 @@ __global__ void __launch_bounds__(kThreads, kBlocks) rope_kernel(const __grid_co
           sum += a;
 #pragma unroll
           for (int o = kLanes / 2; o; o /= 2) sum += __shfl_xor_sync(~0u, sum, o);
-          const float f = rsqrtf(fmaf(sum, 1.f / HD, p.eps));
+          const float mean = fmaf(sum, 1.f / HD, p.eps);
+          float f = rsqrtf(mean);
+          if (!(mean > 1e-30f && mean < INFINITY)) {   // squares beyond fp32: once more, times 2^-96 or 2^96 (bf16's range is fp32's)
+            const float by = mean <= 1e-30f ? 0x1p96f : 0x1p-96f;
+            const uint64_t by2 = amk::pair(by, by);
+            sums = more = 0;
+#pragma unroll
+            for (int j = 0; j < 4; j++) x[j] = mul2(x[j], by2), y[j] = mul2(y[j], by2), sums = amk::fma2(x[j], x[j], sums), more = amk::fma2(y[j], y[j], more);
+            amk::unpair(a, sum, amk::add2(sums, more));
+            sum += a;
+#pragma unroll
+            for (int o = kLanes / 2; o; o /= 2) sum += __shfl_xor_sync(((1u << kLanes) - 1) << (lane & ~(kLanes - 1)), sum, o);
+            f = rsqrtf(fmaf(sum, 1.f / HD, p.eps * by * by));
+          }
           const uint64_t f2 = amk::pair(f, f);
 #pragma unroll
           for (int j = 0; j < 4; j++) x[j] = mul2(x[j], f2), y[j] = mul2(y[j], f2);
@@ -294,6 +307,8 @@ extern "C" amk_status amk_norm_rope_append(const amk_rope_args* args, char* msg,
       const amk_status st = check_stride(fail, s.what, s.n, s.stride, hd, s.esz);
       if (st != AMK_OK) return st;
     }
+  if ((a.q_out == a.q && (a.qo_row != a.q_row || a.qo_head != a.q_head)) || (a.k_out == a.k && (a.ko_row != a.k_row || a.ko_head != a.k_head)))
+    return fail(AMK_ERR_INVALID_ARG, "q_out is q or k_out is k, but at other strides");
   RopeParams p{};
   p.q = (const unsigned short*)a.q, p.k = (const unsigned short*)a.k, p.v = (const unsigned short*)a.v;
   p.q_weight = (const uint4*)a.q_weight, p.k_weight = (const uint4*)a.k_weight;

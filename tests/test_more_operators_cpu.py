@@ -106,6 +106,11 @@ def test_norm_rope_append_refuses(amk, kw, code, word):
     refused(amk.lib.amk_norm_rope_append, (rope_args(amk, **kw),), code, "amk_norm_rope_append: ", word)
 
 
+@pytest.mark.parametrize("kw", [dict(), dict(q_out=P + 4096, k_out=P), dict(qo_row=512, k_out=P, ko_row=520), dict(qo_row=512, qo_head=72)])
+def test_norm_rope_append_refuses_outputs_over_inputs_at_other_strides(amk, kw):
+    refused(amk.lib.amk_norm_rope_append, (rope_args(amk, **kw),), INVALID, "amk_norm_rope_append: ", "other strides")
+
+
 @pytest.mark.parametrize("kw,code,word", [
     (dict(struct_size=8), INVALID, "struct_size"), (dict(head_dim=32), UNSUPPORTED, "head_dim"), (dict(n_q_heads=34), UNSUPPORTED, "16"),
     (dict(n_q_heads=3), UNSUPPORTED, "multiple"), (dict(kv_dtype=2), UNSUPPORTED, "kv_dtype"), (dict(decay=NAN), INVALID, "decay"),
