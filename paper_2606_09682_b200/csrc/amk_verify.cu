@@ -266,6 +266,7 @@ __global__ void __launch_bounds__(kThreads, 1) walk_kernel(const VerifyParams p)
   else cluster_sync();                                 // (also: the other blocks have begun and can be written to)
   const bool greedy = t == 0.f, legal = t >= 0.f && t < CUDART_INF_F;
   const double inv_t = 1.0 / (double)t;
+  const bool rough = t < 1e-37f || t > 1e30f;          // log2 e / t or x - m may be beyond fp32: the sums in 32 bits say nothing
   for (int i = threadIdx.x; i < p.rows; i += kThreads) {
     const int parent = w.parent[i];
     if (parent < 0) continue;
@@ -277,7 +278,7 @@ __global__ void __launch_bounds__(kThreads, 1) walk_kernel(const VerifyParams p)
       double e = exp_below(y, w.roots);
       if (e == 0.0) e = exp(y);
       w.e[i] = e;
-      w.verdict[i] = fabs(uq * s - e) > kNear * e ? (uq * s < e ? kAccept : kReject) : kClose;
+      w.verdict[i] = !rough && fabs(uq * s - e) > kNear * e ? (uq * s < e ? kAccept : kReject) : kClose;
     }
   }
   __syncthreads();
@@ -395,7 +396,7 @@ __global__ void __launch_bounds__(kThreads, 1) walk_kernel(const VerifyParams p)
     int verdict = w.verdict[c];
     if (!greedy && (k || summed)) {
       verdict = kClose;
-      if (!draft && !summed) {                         // a guess behind rejected ones: by what these leave of the 32-bit sum
+      if (!draft && !summed && !rough) {               // a guess behind rejected ones: by what these leave of the 32-bit sum
         const double e = w.e[c], s32 = (double)w.s[at], s = s32 - gone;
         bool before = false;
         for (int j = 0; j < k; j++) before |= w.out[j] == w.token[c];

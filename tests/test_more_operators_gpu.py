@@ -132,6 +132,23 @@ def test_norm_rope_append_far_positions(amk):
 
 
 @pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("eps", [0.0, 1e-5])
+def test_norm_rope_append_norms_beyond_32_bits(amk, hd, eps):
+    """Heads whose squares are more than fp32's largest number or less than its smallest, next to ordinary ones."""
+    g = gen(hd)
+    powers = torch.tensor([0, 120, -120, 70, -70, 64, -64, 63, -50, -49, 60, 100, -100, 0, 1], device=DEV)
+    q, k = randn(g, 40, 15, hd, dtype=torch.float32), randn(g, 40, 3, hd, dtype=torch.float32)
+    q, k = (q * torch.pow(2.0, powers[:, None].float())).to(torch.bfloat16), (k * 2.0 ** 100).to(torch.bfloat16)
+    w = (1 + 0.3 * randn(g, hd, dtype=torch.float32)).to(torch.bfloat16)
+    pos = torch.arange(40, device=DEV, dtype=torch.int32) * 7
+    k_out = torch.empty_like(k)
+    got = amk.amk_norm_rope_append(q, k, None, pos, q_weight=w, k_weight=w, eps=eps, k_out=k_out)
+    for out, x in ((got, q), (k_out, k)):
+        want, both = rotated64(x, w, pos, 10000.0, float(np.float32(eps)))
+        near16(out, want, both)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
 def test_norm_rope_append_in_place_and_strides(amk, hd):
     g = gen(hd)
     rows, nq, nkv = 21, 6, 2
@@ -498,6 +515,17 @@ def test_verify_draft_odd_inputs(amk):
         pw[:, :, 3:504] = probs
         verified(amk, wide[:, :, skew:skew + 501], t, u2, draft=pw[:, :, 3:504])
     assert [t.shape[0] for t in amk.amk_verify_draft(logits[:0], tokens[:0], u[:0])] == [0, 0, 0]
+
+
+@pytest.mark.parametrize("kind", ["probs", "point"])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_verify_draft_temperatures_beyond_32_bits(amk, kind, dtype):
+    """Logits and temperatures so large that differences of logits overflow fp32, and so small that 1 / T does."""
+    for size in (1e38, 1e37, 1e31, 1e-36, 1e-38, 1e-39):
+        for seed in range(4):
+            x, tokens, u, parents, probs = draft_case(gen(40 + seed), 12, 8, 300, torch.float32, kind, seed % 2 == 0)
+            logits = (x.clamp(-3, 3) * size).to(dtype)
+            verified(amk, logits, tokens, u, parents, probs, torch.full((12,), size, device=DEV))
 
 
 def test_verify_draft_same_distribution_accepts_all(amk):
