@@ -9,7 +9,8 @@
 // goes on to further tokens.  Heads come by asynchronous copies, seven steps ahead, into places of shared memory that each lane
 // writes and reads alone: loads into registers cost the registers that keep enough bytes under way (8111 tokens of 32 + 8 + 8
 // heads of 128, normed, 202 MB: 49.5 us with four steps in registers and scalar arithmetic, 40.5 with packed arithmetic and the
-// weights in the rotation's factors, 37.8 so, 5.3 TB/s; without norms 35.3; a copy of as many bytes 31.7).
+// weights in the rotation's factors, 37.8 with copies, 38.3 with the norms beyond fp32, 5.3 TB/s; without norms 35.3; a copy of as
+// many bytes 31.7).
 #include <cuda_bf16.h>
 #include <math.h>
 

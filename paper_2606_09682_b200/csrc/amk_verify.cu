@@ -13,7 +13,7 @@
 // vocabulary of 10^5 lies within the error of 32 bits in one draw of a hundred.
 //
 // Bound: HBM in the first kernel (each row once: 24.6 MB in about 8 us); in the second latency, about 8 us and one pass over a row for
-// each state that is needed, two or three microseconds each.  (8 sequences of 6 rows of 128256, drafted probabilities: 26.5 us;
+// each state that is needed, two or three microseconds each.  (8 sequences of 6 rows of 128256, drafted probabilities: 26.8 us;
 // 6 of 26 rows, 16 bits: 30 us.  With verdicts, states and sums made anew at each step and clusters of 8: 34 and 69 us.)
 #include <cuda_runtime.h>
 #include <math_constants.h>
