@@ -557,7 +557,8 @@ amk_status amk_norm_rope_append(const amk_rope_args* args, char* msg, size_t msg
  *                 calls that may overlap need one each
  * NaN or infinity in a K row reaches only its own position.  Pointers 16-byte aligned (lse, before, out and cache_len 4), strides
  * of q and k multiples of 16 bytes and at least head_dim elements, of before and out at least n_slots (an axis of one entry may
- * have any).  Arithmetic: scores, exponentials and sums fp32, sums in a fixed order.
+ * have any).  Arithmetic: scores, exponentials and sums fp32, sums in a fixed order; an exponent is off by about 2^-22 of the score
+ * and of lse, so that weights of scores beyond 10^5 are good to a few per cent only, and beyond 10^7 to no digit.
  * Errors as amk_tree_attention.
  */
 typedef struct amk_attention_weights_args {
