@@ -13,7 +13,8 @@ SOURCES = ["amk_host.cu", "amk_kernel.cu", "amk_kernel_trace.cu", "amk_pack.cu",
            "amk_attn.cu", "amk_logprobs.cu", "amk_compact.cu",
            "amk_rope.cu", "amk_evict.cu", "amk_verify.cu"]
 HEADERS = ["amk_layout.h", "amk_internal.h", "amk_ptx.cuh", "amk_kernel_impl.cuh", "amk_op_util.h",
-           "amk_op_launch.h", "amk_attn.cuh", "amk_attn_weights.cuh", "amk_tc.cuh", os.path.join(ROOT, "include", "amk.h")]
+           "amk_op_launch.h", "amk_attn.cuh", "amk_attn_weights.cuh", "amk_weights_units.h", "amk_tc.cuh",
+           os.path.join(ROOT, "include", "amk.h")]
 
 
 def _stale() -> bool:

@@ -17,19 +17,19 @@
 // quarter; the issue of instructions and the waits between them are what is left.)
 #pragma once
 #include "amk_attn.cuh"
+#include "amk_weights_units.h"
 
 namespace amk {
 
-struct WeightsParams {
+static_assert(kFewSpan == kTile, "few rows: a unit is a tile");
+struct WeightsParams : WeightsWork {
   const float* lse;
-  const int* lens;
   const float* before;
   float* out;
   float* part;                     // many rows: [2 * gridDim][160]: sums of cut units
   int4* part_of;                   // [2 * gridDim]: {sequence, head, unit, whether the next block goes on}; sequence -1: none
   int64_t b_seq, b_head, o_seq, o_head;
-  int n_seqs, nq, nkv, rep, rows, slots;
-  int tokens, q_tiles;             // tokens of a tile of query rows, tiles of all
+  int nq, rep;
   int q_stages, k_stages, raw_stages;   // tiles in shared memory
   int columns;                     // few rows: rows of the tile, up to a multiple of 32
   unsigned rep_inv;                // ceil(2^32 / rep), 0 for rep = 1
@@ -93,65 +93,7 @@ __device__ __forceinline__ void weights_write(const WeightsParams& p, int seq, i
   p.out[seq * p.o_seq + head * p.o_head + key] = sum;
 }
 
-// ---- units ------------------------------------------------------------------------------------------------------
-// A unit is SPAN positions of a kv head, a step of it the product with one tile of query rows (as many whole tokens as fit into 128
-// rows).  The steps of all units, sequence by sequence, head by head, are cut into equal runs, one for each block.
-template <int SPAN>
-__device__ __forceinline__ int weights_units(const WeightsParams& p, int len) {         // of one head; 0: impossible length
-  return len < 0 || len > p.slots - p.rows ? 0 : (len + p.rows + SPAN - 1) / SPAN;
-}
-// the first tile of query rows that sees a position of a unit
-template <int SPAN>
-__device__ __forceinline__ int first_q_tile(const WeightsParams& p, int len, int unit) {
-  const int behind = unit * SPAN - len;
-  return SPAN == kTile || behind <= 0 ? 0 : behind / p.tokens;
-}
-// units of one head whose every position all rows see
-template <int SPAN>
-__device__ __forceinline__ int full_units(const WeightsParams& p, int len, int units) {
-  return SPAN == kTile ? units : min(units, len / SPAN + 1);
-}
-template <int SPAN>
-__device__ __forceinline__ int weights_steps(const WeightsParams& p, int len) {         // of one head
-  const int units = weights_units<SPAN>(p, len), full = full_units<SPAN>(p, len, units);
-  int n = full * p.q_tiles;
-  for (int j = full; j < units; j++) n += p.q_tiles - first_q_tile<SPAN>(p, len, j);
-  return n;
-}
-struct WeightsUnit {
-  int seq, head, len, at;          // at: which unit of the head
-  int first;                       // first tile of query rows of the unit
-  int begin, end, all;             // steps of this block, steps of the unit
-};
-template <int SPAN>
-struct WeightsWalk {
-  int left, seq, len, head, at, units, step;
-  __device__ __forceinline__ void init(const WeightsParams& p, const int* start) {
-    seq = start[0], head = start[1], at = start[2], step = start[3], left = start[4], len = start[5];
-    units = weights_units<SPAN>(p, len);
-  }
-  __device__ __forceinline__ bool next(const WeightsParams& p, WeightsUnit& u) {
-    if (left <= 0) return false;
-    while (at >= units) {          // something is left: a unit follows
-      at = 0;
-      if (units && head + 1 < p.nkv) {
-        head++;
-      } else {
-        head = 0;
-        len = __ldg(p.lens + ++seq);
-        units = weights_units<SPAN>(p, len);
-      }
-    }
-    u.seq = seq, u.head = head, u.len = len, u.at = at;
-    u.first = first_q_tile<SPAN>(p, len, at);
-    u.all = SPAN == kTile ? 1 : p.q_tiles - u.first;
-    u.begin = step, u.end = min(u.all, step + left);
-    left -= u.end - u.begin;
-    step = 0;
-    at++;
-    return true;
-  }
-};
+// ---- runs -------------------------------------------------------------------------------------------------------
 // Where this block's run begins, and its steps (one whole warp): {sequence, head, unit, step, steps, length of the sequence}
 template <int SPAN>
 __device__ __forceinline__ void find_run(const WeightsParams& p, int* start) {
@@ -181,22 +123,7 @@ __device__ __forceinline__ void find_run(const WeightsParams& p, int* start) {
         const int of_head = __shfl_sync(~0u, own, f) / p.nkv;
         len = __ldg(p.lens + seq);
         head = rel / of_head, rel -= head * of_head;
-        if (SPAN == kTile) {
-          unit = rel;
-        } else {
-          const int full = full_units<SPAN>(p, len, weights_units<SPAN>(p, len));
-          if (rel < full * p.q_tiles) {
-            unit = rel / p.q_tiles, step = rel - unit * p.q_tiles;
-          } else {
-            rel -= full * p.q_tiles;
-            for (unit = full;; unit++) {
-              const int steps = p.q_tiles - first_q_tile<SPAN>(p, len, unit);
-              if (rel < steps) break;
-              rel -= steps;
-            }
-            step = rel;
-          }
-        }
+        weights_place<SPAN>(p, len, rel, unit, step);
         break;
       }
       at -= __shfl_sync(~0u, n, 31);
@@ -554,7 +481,7 @@ __device__ __forceinline__ void exchange(float (&v)[ALL], int lane) {
 // nobody but the issuer, which is two steps ahead.  (Two accumulators of 192 positions, three warpgroups: their release, the
 // product and its arrival were as long as the exponentials, 250 us; four warpgroups of 64 positions have too few registers,
 // 450 us.)  A unit that a run's border cuts leaves its parts in scratch and a second kernel adds them, in the order of the blocks.
-constexpr int kManySpan = 160, kManyThreads = 576, kManyBuffers = 3;
+constexpr int kManyThreads = 576, kManyBuffers = 3;
 template <int HD, bool FP8>
 __global__ void __launch_bounds__(kManyThreads, 1)
     weights_many_kernel(const WeightsParams p, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k) {

@@ -1,0 +1,35 @@
+"""GPU tests of the operators between projection, attention and cache at the ends of what their calls allow, against the same plain
+implementations in 64 bits and with the same tolerances as test_more_operators_gpu.py."""
+import pytest
+import torch
+
+from test_more_operators_gpu import DEV, code, gen, i32, randn, true_lse, weights64, weights_agree
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def amk():
+    from paper_2606_09682_b200 import binding
+    return binding
+
+
+# ---- attention weights ------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("cache", ["bf16", "fp8"])
+@pytest.mark.parametrize("nq,nkv,hd,rows,slots", [(8, 2, 64, 300, 900), (16, 1, 128, 70, 700), (4, 2, 64, 3, 700)])
+@pytest.mark.parametrize("bad", [-320, -1000, -20000000, -(1 << 31), 2147483647])
+def test_attention_weights_impossible_lengths_among_others(amk, nq, nkv, hd, rows, slots, cache, bad):
+    """A sequence of impossible length gets NaN, and the others their weights, wherever it stands."""
+    g = gen(rows)
+    for lens in ([bad, 500, 31], [500, bad, 0], [slots - rows, 31, bad], [bad, 77, bad, bad, 200, bad]):
+        q, k = randn(g, len(lens), rows, nq, hd), randn(g, len(lens), nkv, slots, hd)
+        k = code(k) if cache == "fp8" else k
+        lse = true_lse(q, k, lens, hd ** -0.5)
+        want, tol = weights64(q, k, lse, lens, None, 1, hd ** -0.5)
+        # in the middle of a larger tensor: what lies around out stays as it is
+        room = torch.full((len(lens) + 2, nkv, slots), 7.0, device=DEV)
+        got = amk.amk_attention_weights(q, k, lse, i32(lens), out=room[1:-1])
+        assert [bool(torch.isnan(got[s]).all()) for s in range(len(lens))] == [n == bad for n in lens]
+        weights_agree(got, want, tol)
+        assert bool((room[0] == 7).all()) and bool((room[-1] == 7).all())
