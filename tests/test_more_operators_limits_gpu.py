@@ -1,5 +1,7 @@
 """GPU tests of the operators between projection, attention and cache at the ends of what their calls allow, against the same plain
 implementations in 64 bits and with the same tolerances as test_more_operators_gpu.py."""
+import math
+
 import pytest
 import torch
 
@@ -33,3 +35,23 @@ def test_attention_weights_impossible_lengths_among_others(amk, nq, nkv, hd, row
         assert [bool(torch.isnan(got[s]).all()) for s in range(len(lens))] == [n == bad for n in lens]
         weights_agree(got, want, tol)
         assert bool((room[0] == 7).all()) and bool((room[-1] == 7).all())
+
+
+# ---- verification -----------------------------------------------------------------------------------------------
+
+def test_verify_draft_sums_of_many_parts(amk):
+    """A vocabulary of 2^26 whose small probabilities come to 3e-5 of the row's sum, though any 2^17 of them in a row are less than
+    half a step of it in 32 bits: a guess of the likely token is accepted up to its probability and no further."""
+    vocab = 1 << 26
+    logits = torch.full((1, 2, vocab), math.log(0.99) - 41 * math.log(2), device=DEV)
+    logits[0, 0, 0] = 0.0
+    logits[0, 1], logits[0, 1, 5] = -math.inf, 0.0
+    tokens = i32([[0, 0]])
+    rest = float(torch.exp(logits[0, 0, 1:].double()).sum())
+    assert 2.9e-5 < rest < 3.1e-5
+    for below in (2e-5, 2.8e-5, 3.2e-5, 4e-5):
+        u = torch.tensor([[0.0, 1.0 - below]], device=DEV)                  # the draw: the first token with a probability
+        accepted = float(u[0, 1].double()) < 1 / (1 + rest)
+        assert accepted == (below > rest)
+        count, keep, token = amk.amk_verify_draft(logits, tokens, u)
+        assert (count.tolist(), keep.tolist(), token.tolist()) == (([2], [[0, 1]], [5]) if accepted else ([1], [[0, -1]], [1])), below
