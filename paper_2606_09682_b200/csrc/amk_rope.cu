@@ -217,8 +217,10 @@ __global__ void __launch_bounds__(kThreads, kBlocks) rope_kernel(const __grid_co
           for (int o = kLanes / 2; o; o /= 2) sum += __shfl_xor_sync(~0u, sum, o);
           const float mean = fmaf(sum, 1.f / HD, p.eps);
           float f = rsqrtf(mean);
-          if (!(mean > 1e-30f && mean < INFINITY)) {   // squares beyond fp32: once more, times 2^-96 or 2^96 (bf16's range is fp32's)
-            const float by = mean <= 1e-30f ? 0x1p96f : 0x1p-96f;
+          // Squares beyond fp32: once more, times 2^96 or 2^-70 (bf16's range is fp32's).  Of a head whose mean square is 2^128 or more an
+          // element keeps its eight bits if it is 2^-71 at least, and smaller ones come out below bf16's least number, 2^-133, before the weight.
+          if (!(mean > 1e-30f && mean < INFINITY)) {
+            const float by = mean <= 1e-30f ? 0x1p96f : 0x1p-70f;
             const uint64_t by2 = amk::pair(by, by);
             sums = more = 0;
 #pragma unroll

@@ -2,10 +2,11 @@
 implementations in 64 bits and with the same tolerances as test_more_operators_gpu.py."""
 import math
 
+import numpy as np
 import pytest
 import torch
 
-from test_more_operators_gpu import DEV, code, gen, i32, randn, true_lse, weights64, weights_agree
+from test_more_operators_gpu import DEV, code, gen, i32, near16, randn, rotated64, true_lse, weights64, weights_agree
 
 pytestmark = pytest.mark.gpu
 
@@ -14,6 +15,29 @@ pytestmark = pytest.mark.gpu
 def amk():
     from paper_2606_09682_b200 import binding
     return binding
+
+
+# ---- norm, rotation, storing ------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_norm_rope_append_small_elements_of_heads_beyond_32_bits(amk, hd):
+    """Heads whose squares are beyond fp32, with elements so much smaller that the normed ones are barely normal bf16 numbers: those
+    that are 2^-125 or more at position 0, and those whose rotated sums keep 2^-19 of themselves above bf16's least step elsewhere."""
+    g = gen(hd)
+    for position, least in ((0, -58), (777, -41)):
+        for largest in (69, 100, 127):
+            # rms: 2^largest / sqrt(hd), between 2^64 and 2^124
+            x = (1 + torch.rand(4, 3, hd, generator=g, device=DEV)) * torch.pow(2.0, torch.randint(least, 60, (4, 3, hd), generator=g, device=DEV) + float(largest - 69))
+            x[:, :, 5], x[:, :, 5 + hd // 2] = 2.0 ** largest, -(2.0 ** largest)
+            x = x.to(torch.bfloat16)
+            q, k = x[:, :2], x[:, 2:]
+            w = (1 + 0.3 * torch.rand(hd, generator=g, device=DEV)).to(torch.bfloat16)
+            pos = torch.full((4,), position, dtype=torch.int32, device=DEV)
+            k_out = torch.empty_like(k)
+            got = amk.amk_norm_rope_append(q, k, None, pos, q_weight=w, k_weight=w, k_out=k_out)
+            for out, y in ((got, q), (k_out, k)):
+                want, both = rotated64(y, w, pos, 10000.0, float(np.float32(1e-5)))
+                near16(out, want, both)
 
 
 # ---- attention weights ------------------------------------------------------------------------------------------
