@@ -6,7 +6,8 @@ import numpy as np
 import pytest
 import torch
 
-from test_more_operators_gpu import DEV, code, gen, i32, near16, randn, rotated64, true_lse, weights64, weights_agree
+from test_more_operators_gpu import (DEV, code, evict_plain, gen, i32, near16, randn, rotated64, same_bits, true_lse, weights64,
+                                     weights_agree)
 
 pytestmark = pytest.mark.gpu
 
@@ -59,6 +60,35 @@ def test_attention_weights_impossible_lengths_among_others(amk, nq, nkv, hd, row
         assert [bool(torch.isnan(got[s]).all()) for s in range(len(lens))] == [n == bad for n in lens]
         weights_agree(got, want, tol)
         assert bool((room[0] == 7).all()) and bool((room[-1] == 7).all())
+
+
+# ---- choice of what stays ---------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("slots", [4096, 4097, 8192, 8193, 16384, 16385, 32767, 32768, 32769, 65536, 65537])
+@pytest.mark.parametrize("kind", ["normal", "few", "odd", "same"])
+def test_evict_select_at_the_kernels_limits(amk, slots, kind):
+    """The largest and smallest lists of each kernel, at budgets that leave nearly all and nearly none, lists at odd addresses."""
+    rng = np.random.default_rng(slots)
+    shape = (2, 2, slots)
+    x = rng.standard_normal(shape).astype(np.float32)
+    if kind == "few":
+        x = np.floor(np.abs(x) * 1.5).astype(np.float32)
+    if kind == "odd":
+        x = rng.choice(np.array([0.0, -0.0, np.inf, -np.inf, np.nan, -np.nan, 1e-45, -1e-45, 3e38, 1.0, -1.0], np.float32), shape)
+    if kind == "same":
+        x = np.full(shape, 0.125, np.float32)
+    wide = torch.zeros(2, 2, slots + 3, device=DEV)
+    wide[:, :, 1:-2] = torch.from_numpy(x).to(DEV)
+    scores = wide[:, :, 1:-2]
+    for budget, first, recent in ((1, 0, 0), (slots // 3, 4, 100), (slots - 1, 0, 0), (slots - 1, 5, slots - 10), (slots, 1, 2)):
+        lens = [slots, slots - 1 if budget == slots // 3 else slots]
+        k, c, m = evict_plain(x, lens, budget, first, recent)
+        for s in (scores, scores.contiguous()):
+            keep, count, moved = amk.amk_evict_select(s, i32(lens), budget, first, recent)
+            assert np.array_equal(count.cpu().numpy(), c) and np.array_equal(keep.cpu().numpy(), k)
+            assert same_bits(moved.cpu().numpy(), m) and same_bits(s.cpu().numpy(), x)
+        assert amk.amk_evict_select(s, i32(lens), budget, first, recent, moved=s)[2] is s and same_bits(s.cpu().numpy(), m)
+    assert not bool(wide[:, :, 0].any()) and not bool(wide[:, :, -2:].any())
 
 
 # ---- verification -----------------------------------------------------------------------------------------------
