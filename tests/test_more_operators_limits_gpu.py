@@ -6,8 +6,8 @@ import numpy as np
 import pytest
 import torch
 
-from test_more_operators_gpu import (DEV, code, evict_plain, gen, i32, near16, randn, rotated64, same_bits, true_lse, weights64,
-                                     weights_agree)
+from test_more_operators_gpu import (DEV, code, draft_case, evict_plain, gen, i32, near16, randn, rotated64, same_bits, true_lse,
+                                     verified, weights64, weights_agree)
 
 pytestmark = pytest.mark.gpu
 
@@ -109,3 +109,36 @@ def test_verify_draft_sums_of_many_parts(amk):
         assert accepted == (below > rest)
         count, keep, token = amk.amk_verify_draft(logits, tokens, u)
         assert (count.tolist(), keep.tolist(), token.tolist()) == (([2], [[0, 1]], [5]) if accepted else ([1], [[0, -1]], [1])), below
+
+
+@pytest.mark.parametrize("kind", ["probs", "point"])
+@pytest.mark.parametrize("seqs,rows,vocab", [(1, 6, 300007), (3, 5, 140001), (80, 4, 60011), (150, 5, 20000), (76, 4, 128256)])
+def test_verify_draft_rejections_in_long_rows(amk, seqs, rows, vocab, kind):
+    """Several rejected children of node 0 where a block's share of a row is more than its threads keep: the rest is read and
+    rejected again for each of them."""
+    g = gen(seqs + rows)
+    logits, tokens, u, _, probs = draft_case(g, seqs, rows, vocab, torch.float32, kind, False, near=2.0)
+    logits = (logits - logits.amax(2, keepdim=True)) * 0.3                  # nothing is likely
+    parents = torch.zeros(seqs, rows, dtype=torch.int32, device=DEV)
+    parents[::3, rows - 1] = 1
+    u[:, 1] = torch.where(torch.rand(seqs, generator=g, device=DEV) < 0.8, 0.999, u[:, 1])
+    tokens[1::4, 3] = tokens[1::4, 2]
+    count, _, token = verified(amk, logits, tokens, u, parents, probs)
+    assert kind == "probs" or bool((count == 1).any())                      # all children rejected, the token from what they left
+    temperature = torch.tensor([0.7, 1.3, 0.0], device=DEV).repeat(seqs)[:seqs].contiguous()
+    verified(amk, logits.to(torch.bfloat16), tokens, u, parents, probs, temperature)
+
+
+@pytest.mark.parametrize("seqs,children,vocab", [(1, 6, 300007), (2, 3, 140001), (80, 3, 60011), (150, 4, 20000)])
+def test_verify_draft_every_child_rejected_in_long_rows(amk, seqs, children, vocab):
+    """Drafted tokens that the draft likes better than the target does, all below node 0: each one is rejected, and the token is drawn
+    from what `children` rejections leave."""
+    g = gen(vocab)
+    logits = randn(g, seqs, children + 1, vocab, dtype=torch.float32)
+    probs = torch.softmax(logits + randn(g, seqs, children + 1, vocab, dtype=torch.float32), 2)
+    more = probs[:, 0].double() - torch.softmax(logits[:, 0].double(), 1)
+    tokens = torch.cat([torch.zeros(seqs, 1, dtype=torch.long, device=DEV), more.topk(children, 1).indices], 1).to(torch.int32)
+    u = torch.full((seqs, children + 1), 1.0 - 2.0 ** -23, device=DEV)
+    u[:, 0] = torch.rand(seqs, generator=g, device=DEV)
+    count = verified(amk, logits, tokens, u, torch.zeros(seqs, children + 1, dtype=torch.int32, device=DEV), probs)[0]
+    assert count.tolist() == [1] * seqs
