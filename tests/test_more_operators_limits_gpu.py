@@ -62,6 +62,23 @@ def test_attention_weights_impossible_lengths_among_others(amk, nq, nkv, hd, row
         assert bool((room[0] == 7).all()) and bool((room[-1] == 7).all())
 
 
+@pytest.mark.parametrize("nq,nkv,hd", [(9, 3, 64), (32, 8, 128), (16, 1, 128), (7, 1, 128)])
+@pytest.mark.parametrize("rows,slots,lens", [(1, 300, [0, 299, 127, 128]), (5, 700, [0, 600, 123, 695]), (200, 1000, [0, 1, 800]), (700, 700, [0])])
+@pytest.mark.parametrize("cache", ["bf16", "fp8"])
+def test_attention_weights_of_a_row_add_up_to_one(amk, nq, nkv, hd, rows, slots, lens, cache):
+    """A row's weights add up to exp(its true log-sum-exp - the given one in 32 bits): to 1 within half a step of that, and what the
+    positions may be off by."""
+    g = gen(rows * 5 + nq)
+    q, k = randn(g, len(lens), rows, nq, hd), randn(g, len(lens), nkv, slots, hd)
+    k = code(k) if cache == "fp8" else k
+    lse = true_lse(q, k, lens, hd ** -0.5)
+    _, tol = weights64(q, k, lse, lens, None, 1, hd ** -0.5)
+    n = rows * nq // nkv
+    off = (amk.amk_attention_weights(q, k, lse, i32(lens)).double().sum(2) / n - 1).abs()
+    allowed = tol.sum(2) / n + 1.01 * 2.0 ** -24 * lse.abs().amax((1, 2), keepdim=False)[:, None].double()
+    assert bool((off <= allowed).all()) and float(allowed.max()) < 1e-3
+
+
 # ---- choice of what stays ---------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("slots", [4096, 4097, 8192, 8193, 16384, 16385, 32767, 32768, 32769, 65536, 65537])
@@ -142,3 +159,45 @@ def test_verify_draft_every_child_rejected_in_long_rows(amk, seqs, children, voc
     u[:, 0] = torch.rand(seqs, generator=g, device=DEV)
     count = verified(amk, logits, tokens, u, torch.zeros(seqs, children + 1, dtype=torch.int32, device=DEV), probs)[0]
     assert count.tolist() == [1] * seqs
+
+
+def test_verify_draft_of_the_targets_own_distribution_is_accepted(amk):
+    """q = p rounded to 32 bits, off by 2^-24 of itself at most, is accepted by every number up to 1 - 2^-23: all of a chain, and in the
+    target's order where a node has several children, the first one."""
+    g = gen(31)
+    for vocab in (5000, 128256):
+        x = randn(g, 6, 8, vocab, dtype=torch.float32)
+        probs = torch.softmax(x.double(), 2).float()
+        drawn = torch.multinomial(probs.view(-1, vocab), 1, generator=g).view(6, 8).to(torch.int32)
+        chain = torch.cat([drawn[:, :1], drawn[:, :-1]], 1).contiguous()                # node i's token comes from row i - 1
+        u = torch.full((6, 8), 1.0 - 2.0 ** -23, device=DEV)
+        u[:, 0] = 0.5
+        assert verified(amk, x, chain, u, draft=probs)[0].tolist() == [8] * 6
+        below = drawn[:, :1].expand(6, 8).contiguous()
+        count, keep, _ = verified(amk, x, below, u, torch.zeros(6, 8, dtype=torch.int32, device=DEV), probs)
+        assert count.tolist() == [2] * 6 and keep[:, 1].tolist() == [1] * 6
+
+
+# ---- forms of a call --------------------------------------------------------------------------------------------
+
+def test_given_workspaces_and_8_bit_types(amk):
+    """A workspace that the caller keeps gives the same bits as one that is allocated, and an 8-bit cache may be called e4m3."""
+    g = gen(17)
+    q, k = randn(g, 2, 300, 8, 64), code(randn(g, 2, 2, 900, 64))
+    lens = [500, 31]
+    lse, n = true_lse(q, k, lens, 0.125), i32(lens)
+    space = torch.empty(1 << 20, dtype=torch.uint8, device=DEV)
+    want = amk.amk_attention_weights(q, k, lse, n)
+    for cache in (k, k.view(torch.float8_e4m3fn)):
+        for rows in (300, 5):
+            a = amk.amk_attention_weights(q[:, :rows], cache, lse[:, :rows].contiguous(), n, workspace=space.fill_(255))
+            assert torch.equal(a, want if rows == 300 else amk.amk_attention_weights(q[:, :rows], k, lse[:, :rows].contiguous(), n))
+    logits, tokens, u, _, probs = draft_case(g, 3, 6, 20000, torch.float32, "probs", False)
+    for a, b in zip(amk.amk_verify_draft(logits, tokens, u, draft=probs, workspace=space.fill_(255)), amk.amk_verify_draft(logits, tokens, u, draft=probs)):
+        assert torch.equal(a, b)
+    x, pos = randn(g, 4, 8, 64), i32([5, 6, 7, 8])
+    caches = [torch.zeros(1, 2, 9, 64, dtype=torch.uint8, device=DEV) for _ in range(4)]
+    typed = [c.view(torch.float8_e4m3fn) for c in caches[2:]]
+    for kc, vc in (caches[:2], typed):
+        amk.amk_norm_rope_append(x[:, :4], x[:, 4:6], x[:, 6:], pos, kc, vc, pos.long())
+    assert torch.equal(caches[0], caches[2]) and torch.equal(caches[1], caches[3]) and bool(caches[0].any())
