@@ -503,6 +503,7 @@ amk_status amk_kv_compact(void* kv, int64_t n_caches, int64_t cache_stride, int6
  *   k_out         DEVICE bf16, or NULL: the rotated keys as amk_prompt_attention takes them; may be k itself at the same strides
  * Outputs must not overlap otherwise, neither each other nor an input.
  * Arithmetic: fp32, angles from 64 bits, each result rounded once (to nearest even; e4m3 saturates at 448, as the step's cache).
+ * An angle is off by less than 2^-23 of a turn at any position where theta >= 1; below, by 2^-52 of the turns that it is, besides.
  * Pointers 16-byte aligned (positions 4, slots 8), strides multiples of 16 bytes and at least head_dim elements (an axis of one
  * entry may have any).
  * Errors: INVALID_ARG (struct size, NULL, alignment, strides, sizes, eps, theta), UNSUPPORTED (head_dim, kv_dtype, head counts), CUDA.
@@ -547,7 +548,8 @@ amk_status amk_norm_rope_append(const amk_rope_args* args, char* msg, size_t msg
  *                 their values
  *   lse           DEVICE float [n_seqs][n_rows][n_q_heads], natural logarithms.  A row of -infinity (or +infinity) adds
  *                 nothing, whatever its query: so a padded token is left out.  NaN makes what the row attends to NaN.
- *   cache_len     DEVICE int32 [n_seqs]: len.  A sequence whose len is not 0 <= len <= n_slots - n_rows gets NaN in all of out.
+ *   cache_len     DEVICE int32 [n_seqs]: len.  A sequence whose len is not 0 <= len <= n_slots - n_rows gets NaN in all of out (in a
+ *                 padded batch too: n_rows counts the padded tokens); the others are not touched by it.
  *   before        DEVICE float [n_seqs][n_kv_heads][n_slots], sequences and heads at the given strides, or NULL: 0.  Only
  *                 slots below len are used; not read where decay is 0.
  *   out           DEVICE float, like before at strides of its own; all n_slots are written.  May be before itself at the same
@@ -598,6 +600,8 @@ amk_status amk_attention_weights(const amk_attention_weights_args* args, char* m
  *   moved         DEVICE float, like scores at strides of its own, or NULL: scores[keep[i]] at i < count, 0 behind.  May be
  *                 scores itself at the same strides; must not overlap them otherwise.
  * NaN is less than every number (-infinity too); 0 and -0 are equal.
+ * K rows keep the rotation of their old positions: attention over what stays goes on with amk_tree_attention, whose queries
+ * come rotated for their true positions, and not with the decode step.
  * Errors: INVALID_ARG (NULL, alignment, sizes, strides below n_slots, first + recent > budget, budget outside 1 .. n_slots), CUDA.
  */
 amk_status amk_evict_select(const float* scores, int64_t n_seqs, int64_t n_heads, int64_t n_slots, int64_t scores_seq,
@@ -613,6 +617,8 @@ amk_status amk_evict_select(const float* scores, int64_t n_seqs, int64_t n_heads
  *   child c, token t: accepted if u[c] q(t) < r(t), q the distribution that it was drawn from (draft[parent]; without draft
  *     1 at t, a guess).  The walk goes on at c with the p of c's row.
  *   otherwise r <- max(r - q, 0) / (its sum); where that sum is 0, r stays.
+ * The target's distribution needs children of a node that were drawn independently of one another from draft[node] (the same token
+ * may come twice): drafts drawn without replacement have another distribution for each child, which cannot be given here.
  * Where no child is accepted, the next token is drawn from r: the first t whose sum of r(0..t) is more than u[0] times the sum of
  * all (the last t with r(t) > 0 if rounding leaves none).  temperature 0: p is 1 at the first largest logit.
  *   logits        DEVICE float (dtype 0) or bf16 (dtype 1) [n_seqs][n_rows][vocab], sequences and rows at the given strides

@@ -665,7 +665,7 @@ def amk_attention_weights(q: torch.Tensor, k: torch.Tensor, lse: torch.Tensor, c
     e4m3 as uint8 / float8_e4m3fn), added up over tokens and the heads of a group: fp32 [n_seqs][n_kv][slots].  Token i's own row
     lies in slot cache_len + i, and it attends to the slots up to there; ``lse`` (fp32 [n_seqs][rows][n_q]) as the attentions
     leave it, -infinity for a token to be left out.  ``before``, weighed by ``decay``, is added for slots below cache_len; ``out`` may
-    be ``before`` itself."""
+    be ``before`` itself.  A sequence whose cache_len + rows (padded ones too) is more than its slots gets NaN."""
     name = "amk_attention_weights"
     qshape, kshape = q.shape, k.shape
     if len(qshape) != 4 or len(kshape) != 4:
@@ -715,7 +715,8 @@ def amk_evict_select(scores: torch.Tensor, lens: torch.Tensor, budget: int, firs
     ``first``, the last ``recent`` and the heaviest others, ``budget`` in all.  Returns (keep int32 [n_seqs][n_heads][budget],
     ascending, -1 behind the last; count int32 [n_seqs][n_heads]; the scores of the kept positions moved together, of scores'
     shape, 0 behind: ``moved`` if given, which may be scores itself).  Lists for ``amk_kv_compact`` with base 0: a cache's K
-    [n_seqs][n_heads][n_slots][hd] as n_seqs * n_heads caches of one plane, and its V likewise."""
+    [n_seqs][n_heads][n_slots][hd] as n_seqs * n_heads caches of one plane, and its V likewise.  Over what stays go on with
+    ``amk_tree_attention``, not with the decode step."""
     name = "amk_evict_select"
     shape = scores.shape
     if len(shape) != 3:
@@ -750,7 +751,7 @@ def amk_verify_draft(logits: torch.Tensor, tokens: torch.Tensor, uniforms: torch
     """Drafted tokens accepted or rejected, and the next one drawn: logits [n_seqs][rows][vocab] (fp32 or bf16) as the target gives
     them for the rows of ``amk_tree_attention``, row 0 the token that is already chosen; tokens int32 [n_seqs][rows]; uniforms
     fp32 [n_seqs][rows] in [0, 1), the first for the draw, the others for their nodes; parents int32 [n_seqs][rows], None: a
-    chain; ``draft`` fp32 [n_seqs][rows][vocab]: the probabilities that a node's children were drawn from, None: guesses;
+    chain; ``draft`` fp32 [n_seqs][rows][vocab]: the probabilities that a node's children were each drawn from, independently, None: guesses;
     temperature fp32 [n_seqs], None: 1, 0: greedy; cache_len int32 [n_seqs], None: 0.  Returns (count int32 [n_seqs], keep int32
     [n_seqs][rows]: cache_len + kept nodes, -1 behind them, token int32 [n_seqs], -1 where there is none): count and keep for
     ``amk_kv_compact`` with base = cache_len."""

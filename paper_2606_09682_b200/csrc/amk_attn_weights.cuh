@@ -5,16 +5,17 @@
 //
 // Few rows (128 or less for a kv head: a decoded token, a draft, the last tokens of a prompt): every K tile of 128 positions meets
 // one tile of queries, and what counts is K's way from HBM.  weights_few_kernel takes S^T = K Q^T: a position is a lane of TMEM.
-// (32 tokens, 32 heads of 128 on 8, four caches of 4097 to 8001 positions: 51 MB in 15.6 us, of which about 8 are a cold block's
-// first tile and last output: the tiles come at HBM's rate.  13 tokens over eight 8-bit caches: 45 MB in 22.7 us, the tiles'
-// widening.)
+// (32 tokens, 32 heads of 128 on 8, four caches of 4097 to 8001 positions: 51 MB in 15.7 us, eleven tiles a block.  Blocks of 1 / 2 / 4 /
+// 8 / 16 tiles from HBM take 6.6 / 7.6 / 9.5 / 13.2 / 19.8 us: 5.7 us for the launch, the division, the first tile and the last
+// output, and 0.9 us a tile, 0.77 at the rate of a copy.  13 tokens over eight 8-bit caches: 45 MB in 22.7 us, the tiles' widening.)
 //
 // Many rows: what counts are the exponentials, 16 a cycle and SM, twice as long as the products.  weights_many_kernel takes
 // S = Q K^T: a query row is a lane, whose L is a scalar, and a thread keeps the sums of 40 positions in registers over all
-// query tiles of a unit; lanes are added up once, at its end.  (7001 tokens, 32 heads of 128 on 8, 784 M exponentials: 250 us, 74 % of
+// query tiles of a unit; lanes are added up once, at its end.  (7001 tokens, 32 heads of 128 on 8, 784 M exponentials: 248 us, 74 % of
 // their unit's rate; with the positions in the lanes there too, where every column's L is read from shared memory, 257 us.  A
 // share of the exponentials as a polynomial on the fma pipe gained nothing in either: 250 / 260 / 271 us at none, an eighth and a
-// quarter; the issue of instructions and the waits between them are what is left.)
+// quarter; the issue of instructions, 6.5 for each exponential, and the waits between them are what is left.  Over an 8-bit cache
+// the same warps widen the tiles: 297 us.)
 #pragma once
 #include "amk_attn.cuh"
 #include "amk_weights_units.h"

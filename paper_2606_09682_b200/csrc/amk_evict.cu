@@ -4,9 +4,12 @@
 // stay anyway hold the largest key) is found digit by digit from histograms of 11, 11 and 10 bits; then the positions whose key
 // is larger stay, and of those with that very key the first ones.  Counts are integers: the result is the same every time.
 //
-// Bound: instructions (a ballot for every 32 keys: 256 lists of 8192 25.2 us; sweeps over shared memory, four keys to a thread:
-// 16.1 us; keys in registers, a run for each thread: 10.4 us), and with few lists the barriers between the sweeps.  Lists of more than
-// 32768 slots are read again from L2 in the histograms, and chosen from in pieces.
+// Bound: nothing alone.  While its blocks run an SM issues in 62 % of the cycles; of the 20 cycles from one instruction of a warp to
+// its next, 4 wait for the scheduler, 3.5 at the barriers between the sweeps, 2 each for arithmetic, for shared memory and its
+// atomics, and for memory; with few lists the barriers are what counts.  (256 lists of 8192: with a ballot for every 32 keys 25.2 us;
+// sweeps over shared memory, four keys to a thread, 16.1; keys in registers, a run for each thread, 10.4, of equal scores 10.0.  128
+// lists of 16384 9.6, 64 of 32768 18.8.)  Lists of more than 32768 slots are read again from L2 in the histograms, and chosen from in
+// pieces, by one block: 24 lists of 100001 109 us.
 #include <cuda_runtime.h>
 
 #include <atomic>

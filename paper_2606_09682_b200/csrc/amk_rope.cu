@@ -2,15 +2,15 @@
 //
 // Mathematics.  A lane holds eight elements i .. i+7 of a head and the eight i + hd/2 .. that they are rotated with, so that
 // only the norm's sum crosses lanes.  The angle of pair i at position n is n theta^(-2i/hd); in turns, n f_i with
-// f_i = theta^(-2i/hd) / 2 pi, it is made in 64 bits, its whole turns taken off, and only then rounded to fp32: off by 2^-24 of
-// a turn at most, at any position (theta >= 1).  The eight angles of a lane are those of every head of its token.
+// f_i = theta^(-2i/hd) / 2 pi, it is made in 64 bits, its whole turns taken off, and only then rounded to fp32: off by 2^-26 of
+// a turn, and near position 2^31 by 2^-24 more (theta >= 1).  The eight angles of a lane are those of every head of its token.
 //
 // Bound: HBM, each element once in and once out.  A warp takes the heads of one token, or, with few tokens, a share of them, and
 // goes on to further tokens.  Heads come by asynchronous copies, seven steps ahead, into places of shared memory that each lane
 // writes and reads alone: loads into registers cost the registers that keep enough bytes under way (8111 tokens of 32 + 8 + 8
 // heads of 128, normed, 202 MB: 49.5 us with four steps in registers and scalar arithmetic, 40.5 with packed arithmetic and the
 // weights in the rotation's factors, 37.8 with copies, 38.3 with the norms beyond fp32, 5.3 TB/s; without norms 35.3; a copy of as
-// many bytes 31.7).
+// many bytes 31.7; into an 8-bit cache 38.6, 183 MB).
 #include <cuda_bf16.h>
 #include <math.h>
 

@@ -7,14 +7,19 @@
 //
 // Which rows the walk reaches is known only as it goes, and each needs its S_0.  So a first kernel takes the maximum and the sum of
 // every row in 32 bits, all rows at once at the memory's rate, and a second one, a cluster of blocks for each sequence, walks
-// on those numbers alone (a cluster that takes its rows' sums itself, in one launch: one sequence of 6 rows of 128256 15.3 us, so
-// 11.9; eight of them 28.8 and 22.5): a decision nearer than their error (kNear) is taken again with the sum in 64 bits.  Only a row where
+// on those numbers alone (a cluster that takes its rows' sums itself, in one launch: guesses for one sequence of 6 rows of 128256 15.3
+// us, so 11.9; for eight of them 28.8 and 22.5): a decision nearer than their error (kNear) is taken again with the sum in 64 bits.  Only a row where
 // a child is rejected or a token drawn is read again (from L2), in 64 bits throughout: the border between two tokens of a
 // vocabulary of 10^5 lies within the error of 32 bits in one draw of a hundred.
 //
-// Bound: HBM in the first kernel (each row once: 24.6 MB in about 8 us); in the second latency, about 8 us and one pass over a row for
-// each state that is needed, two or three microseconds each.  (8 sequences of 6 rows of 128256, drafted probabilities: 26.8 us;
-// 6 of 26 rows, 16 bits: 30 us.  With verdicts, states and sums made anew at each step and clusters of 8: 34 and 69 us.)
+// Bound: HBM in the first kernel (each row once: 24.6 MB in about 8 us); in the second latency.  Of one sequence of 6 rows of 128256 both
+// take 6.5 us with a greedy answer; a draw adds 3.7 (a pass over the row, the sums' exchange, the search), an accepted child 1, a
+// rejected guess 1 (the draw's pass is over what they leave), the first child that is rejected with its probabilities 5.1 and each
+// further one 2.5 (a pass, for the state's sum, and its exchange).  Of eight sequences all but the first kernel take twice as long:
+// their 128 blocks in clusters of 16 behave as two waves (four sequences of the measured chains 14.1 us, eight 26.9, nine 32, sixteen
+// 39).  From 75 sequences on each has one block, which keeps 8192 tokens and makes the weights of the others anew in every pass: 80
+// sequences 243 us.  (6 sequences of 26 rows, 16 bits: 30 us.  With verdicts, states and sums made anew at each step and clusters of
+// 8, the chains of eight 34 us and these 69.)
 #include <cuda_runtime.h>
 #include <math_constants.h>
 
